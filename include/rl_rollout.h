@@ -11,7 +11,8 @@
  * of every sampled token.
  *
  * General rules
- *  - All pointers in the signatures are HOST pointers; the library owns every device buffer.
+ *  - All pointers in the signatures are HOST pointers; the library owns every device buffer.  (rl_sample_device_logits and the
+ *    operators of the policy update, at the end, take device pointers and a stream instead and state their own rules.)
  *  - The caller owns every buffer it passes in or receives results in.
  *  - Every function returns 0 (RL_OK) or a negative rl_status; a failing call changes no
  *    trajectory or allocator state (pages are reserved for the whole call before any write).
@@ -309,6 +310,100 @@ int rl_timing_read_steps(rl_model* m, double* step_gpu_ms, int64_t* steps, int r
  * freshly allocated device buffer, averaged over `iters` passes: the read ceiling of the GPU the
  * library runs on, to set beside the nominal HBM figure.  Allocates and frees its own buffer. */
 int rl_measure_stream_read(size_t bytes, int32_t iters, double* gb_per_s);
+
+/* ---- operators of the policy update ------------------------------------------------------ */
+
+/*
+ * The update that follows a rollout runs its trajectories through the decoder again and takes the gradient of the objective
+ * (Section 2.3.2, RL training; the masked GRPO objective of rl_grpo_objective).  These calls are the decoder's operators in the
+ * form that it needs, forward and backward; the projections between them are plain matrix products.
+ *
+ * Rules of these calls
+ *  - Pointers named d_* are DEVICE pointers; `stream` is a hipStream_t (NULL: the default stream).  The kernels are enqueued on it
+ *    and the call returns without waiting.  Nothing is allocated: a call that needs scratch memory takes a workspace, whose size
+ *    the *_workspace function beside it gives (0 for arguments that the call itself refuses).  Its contents need not be set
+ *    and mean nothing afterwards; calls that may overlap in time need workspaces of their own.  The calls can be captured in a
+ *    HIP graph.
+ *  - dtype: type of the tensors (void pointers): RL_DTYPE_F32 or RL_DTYPE_BF16.  Statistics, sums and softmax are kept in 32 bits or
+ *    more, results rounded once (stated where an operand is).  Sums have a fixed order: the same call gives the same bits.
+ *  - Strides count elements and may be any that stay inside the tensor; the last dimension is contiguous.  Tensors without strides in the
+ *    signature are contiguous.  16-byte aligned pointers and strides in multiples of 16 bytes take the fast kernels.
+ *  - Errors: ARG (null pointer, size or type out of range, workspace too small), HIP (a launch failed).  What lies in device
+ *    memory cannot be refused; what the calls do about it is stated.  Nothing outside the tensors is read or written for it.
+ */
+#define RL_DTYPE_F32 0
+#define RL_DTYPE_BF16 1
+
+/*
+ * RMS norm (centered = 0) or layer norm (1) of outer x inner rows of `width` elements, row (o, i) at o * outer_stride +
+ * i * inner_stride (heads of a fused projection): n = (x - mean) * rstd, y = n * weight + bias, rstd = 1 / sqrt(mean((x - mean)^2) +
+ * eps), mean = 0 in the RMS form.  d_bias may be NULL.  y: contiguous rows.  d_rstd, d_mean: one float per row, for the backward
+ * call; d_mean is not used when centered = 0.
+ * Backward: d_dx [rows, width], d_dweight [width] and, unless NULL, d_dbias [width], from d_dy with strides of its own.
+ */
+int rl_norm_forward(const void* d_x, int64_t outer, int32_t inner, int32_t width, int64_t outer_stride, int64_t inner_stride,
+                    const void* d_weight, const void* d_bias, float eps, int32_t centered, int32_t dtype, void* d_y,
+                    float* d_mean, float* d_rstd, void* stream);
+int64_t rl_norm_workspace(int64_t rows, int32_t width, int32_t biased);      /* of the backward call; biased: with d_dbias */
+int rl_norm_backward(const void* d_dy, int64_t dy_outer_stride, int64_t dy_inner_stride, const void* d_x, int64_t outer,
+                     int32_t inner, int32_t width, int64_t outer_stride, int64_t inner_stride, const void* d_weight,
+                     const float* d_mean, const float* d_rstd, int32_t centered, int32_t dtype, void* d_dx, void* d_dweight,
+                     void* d_dbias, void* d_workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Rotary positions of query and key heads.  Pair i < rot_dim / 2 of a head is elements (i, i + rot_dim / 2), or (2 i, 2 i + 1) when
+ * interleaved; (a, b) becomes (a c - b s, b c + a s) with (c, s) = table[position][i]; elements from rot_dim on are copied.
+ * inverse = 1 takes -s: the backward pass.  d_table: [n_positions][rot_dim / 2] pairs of floats (any scaling of the angles for long
+ * contexts is in it).  d_positions: one per token; a token whose position is outside the table gets NaN in its rotated part.
+ * d_k may be NULL with n_k_heads = 0.  Output may be the input itself.  head_dim at most 512.
+ */
+int rl_rotary(const void* d_q, void* d_q_out, int32_t n_q_heads, int64_t q_token_stride, int64_t q_head_stride,
+              int64_t q_out_token_stride, int64_t q_out_head_stride, const void* d_k, void* d_k_out, int32_t n_k_heads,
+              int64_t k_token_stride, int64_t k_head_stride, int64_t k_out_token_stride, int64_t k_out_head_stride,
+              int64_t tokens, int32_t head_dim, int32_t rot_dim, int32_t interleaved, int32_t inverse,
+              const int32_t* d_positions, const float* d_table, int32_t n_positions, int32_t dtype, void* stream);
+
+/*
+ * Attention over packed sequences with grouped heads: query head h reads KV head h / (n_q_heads / n_kv_heads).  Sequence s has the
+ * queries d_cu_q[s] .. d_cu_q[s + 1] - 1 and the keys and values d_cu_k[s] .. d_cu_k[s + 1] - 1 (n_seq + 1 ascending offsets each,
+ * on the device, from 0 to total_q and total_k; tokens of no sequence are left out).  Causal: query i of lq sees the keys
+ * j <= i + lk - lq, so fewer queries than keys are the last ones of their sequence.  z = scale * q.k, d_lse[head][token] =
+ * log(sum of e^z), o = sum of e^(z - lse) v.  A query that sees no key gets o = 0 and lse = -infinity, and no gradient.
+ * head_dim at most 128.  o and all gradients are contiguous [tokens, heads, head_dim].
+ * Backward: from do, the forward call's inputs and its o and lse; probabilities are formed again.  In bf16 the probabilities and
+ * the gradients of the scores are rounded to bf16 where they enter a matrix product.
+ * A value that is no number or infinite can reach every query of its own sequence, even one that does not see it; never another.
+ */
+int rl_attention_forward(const void* d_q, int64_t q_token_stride, int64_t q_head_stride, const void* d_k, int64_t k_token_stride,
+                         int64_t k_head_stride, const void* d_v, int64_t v_token_stride, int64_t v_head_stride,
+                         const int32_t* d_cu_q, const int32_t* d_cu_k, int32_t n_seq, int32_t total_q, int32_t total_k,
+                         int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float scale, int32_t causal, int32_t dtype,
+                         void* d_o, float* d_lse, void* stream);
+int64_t rl_attention_workspace(int32_t total_q, int32_t n_q_heads);      /* of the backward call */
+int rl_attention_backward(const void* d_do, const void* d_q, int64_t q_token_stride, int64_t q_head_stride, const void* d_k,
+                          int64_t k_token_stride, int64_t k_head_stride, const void* d_v, int64_t v_token_stride,
+                          int64_t v_head_stride, const void* d_o, const float* d_lse, const int32_t* d_cu_q,
+                          const int32_t* d_cu_k, int32_t n_seq, int32_t total_q, int32_t total_k, int32_t n_q_heads,
+                          int32_t n_kv_heads, int32_t head_dim, float scale, int32_t causal, int32_t dtype, void* d_dq,
+                          void* d_dk, void* d_dv, void* d_workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Log-probs of target tokens from hidden rows (behind the final norm) and the lm-head, without keeping the logits: z = hidden W^T /
+ * temperature, d_lse[row] = log(sum of e^z), d_logp[row] = z[target] - lse.  A row with a negative target (observation
+ * tokens: Section 2.2, the loss mask of Section 2.3.2) takes no part: both are 0 and it costs nothing.  A target of `vocab` or above
+ * gives NaN.  W: [vocab, hidden], contiguous.  temperature > 0.
+ * Backward: d_dlogp[row] is the gradient of the objective by the row's log-prob; d_dhidden [rows, hidden] (0 for rows without target)
+ * and d_dweight [vocab, hidden].  Rows with dlogp = 0 take no part either.  The logits are formed again, a piece of the vocabulary
+ * at a time; their gradients are rounded to dtype where they enter the two products.  Workspace 256-byte aligned.
+ */
+int64_t rl_token_logprobs_workspace(int32_t rows, int32_t hidden, int32_t vocab, int32_t dtype, int32_t backward);
+int rl_token_logprobs_forward(const void* d_hidden, int64_t row_stride, int32_t rows, int32_t hidden, const void* d_weight,
+                              int32_t vocab, const int32_t* d_targets, float temperature, int32_t dtype, float* d_logp,
+                              float* d_lse, void* d_workspace, int64_t workspace_bytes, void* stream);
+int rl_token_logprobs_backward(const float* d_dlogp, const void* d_hidden, int64_t row_stride, int32_t rows, int32_t hidden,
+                               const void* d_weight, int32_t vocab, const int32_t* d_targets, const float* d_lse,
+                               float temperature, int32_t dtype, void* d_dhidden, void* d_dweight, void* d_workspace,
+                               int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

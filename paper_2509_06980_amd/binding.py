@@ -14,6 +14,8 @@ EXPORTED_SYMBOLS = [
     "rl_timing_read", "rl_timing_read_steps", "rl_timing_read_decode_bytes", "rl_measure_stream_read",
     "rl_decode_step_with_appends", "rl_decode_step_forced_with_appends", "rl_grpo_objective", "rl_debug_pass_plan",
     "rl_debug_residual_plan", "rl_debug_many_row_loads", "rl_debug_staging_plan",
+    "rl_norm_forward", "rl_norm_workspace", "rl_norm_backward", "rl_rotary", "rl_attention_forward", "rl_attention_workspace",
+    "rl_attention_backward", "rl_token_logprobs_workspace", "rl_token_logprobs_forward", "rl_token_logprobs_backward",
 ]
 
 
@@ -97,6 +99,18 @@ def load_library():
     lib.rl_timing_read_decode_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_double),
                                                 C.POINTER(C.c_int64), C.c_int]
     lib.rl_measure_stream_read.argtypes = [C.c_size_t, C.c_int32, C.POINTER(C.c_double)]
+    p, i, l, f = C.c_void_p, C.c_int32, C.c_int64, C.c_float      # the policy update's operators: device addresses
+    lib.rl_norm_forward.argtypes = [p, l, i, i, l, l, p, p, f, i, i, p, p, p, p]
+    lib.rl_norm_backward.argtypes = [p, l, l, p, l, i, i, l, l, p, p, p, i, i, p, p, p, p, l, p]
+    lib.rl_rotary.argtypes = [p, p, i, l, l, l, l, p, p, i, l, l, l, l, l, i, i, i, i, p, p, i, i, p]
+    lib.rl_attention_forward.argtypes = [p, l, l, p, l, l, p, l, l, p, p, i, i, i, i, i, i, f, i, i, p, p, p]
+    lib.rl_attention_backward.argtypes = [p, p, l, l, p, l, l, p, l, l, p, p, p, p, i, i, i, i, i, i, f, i, i, p, p, p, p, l, p]
+    lib.rl_token_logprobs_forward.argtypes = [p, l, i, i, p, i, p, f, i, p, p, p, l, p]
+    lib.rl_token_logprobs_backward.argtypes = [p, p, l, i, i, p, i, p, p, f, i, p, p, p, l, p]
+    for name, args in (("rl_norm_workspace", [l, i, i]), ("rl_attention_workspace", [i, i]),
+                       ("rl_token_logprobs_workspace", [i, i, i, i, i])):
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = l
     _lib = lib
     return lib
 

@@ -15,6 +15,9 @@ SOURCES = {
     # the sampler's integer weights must not see fused multiply-adds
     "kernels_sampler.hip": ["-ffp-contract=off"],
     "kernels_objective.hip": [],
+    "kernels_rows.hip": [],
+    "kernels_packed_attention.hip": [],
+    "kernels_token_logprob.hip": [],
     "engine.hip": [],
 }
 

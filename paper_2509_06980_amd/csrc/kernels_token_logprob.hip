@@ -1,0 +1,494 @@
+// Log-probs of target tokens from hidden rows and the lm-head's weights, with their gradient, without keeping the logits.
+#include <algorithm>
+
+#include "token_logprob.h"
+
+namespace {
+
+// =============================================================================================
+// z = h W^T / T, lse = log sum_v e^(z_v), logp = z_y - lse.  Backward: dz_v = g / T ([v = y] - e^(z_v - lse)), dh = dz W, dW = dz^T h.
+// Forward: the product's epilogue leaves (max, sum of e^(z - max)) of every row and strip of the vocabulary, a second kernel joins
+// the strips.  Backward: a piece of the vocabulary at a time, its logits are formed again and only dz is stored, in the type of the
+// weights, since it is an operand of the two products behind it; dh is added up over the pieces in 32 bits and rounded once.
+// Rows without target (observation tokens) or, backward, with g = 0 take no part: the others are gathered first.
+// =============================================================================================
+
+// Kept rows in order (one workgroup: a scan of the targets).  place[t]: where row t went, -1: nowhere, -2: its target lies
+// behind the vocabulary, which shows as NaN.  Forward (g null): logp and lse of the others are written here.
+__global__ __launch_bounds__(1024) void keep_rows_kernel(const int32_t* __restrict__ targets, int rows, int vocab, const float* __restrict__ g,
+                                                         const float* __restrict__ lse_in, float inv_t, int32_t* __restrict__ count,
+                                                         int32_t* __restrict__ list, int32_t* __restrict__ place,
+                                                         int32_t* __restrict__ target, float* __restrict__ lse_kept,
+                                                         float* __restrict__ g_kept, float* __restrict__ logp, float* __restrict__ lse) {
+  __shared__ int waves[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int done = 0;
+  for (int t0 = 0; t0 < rows; t0 += 1024) {
+    const int t = t0 + threadIdx.x, y = t < rows ? targets[t] : -1;
+    const float gt = g && t < rows ? g[t] : 1.f;
+    const bool keep = y >= 0 && y < vocab && gt != 0.f;
+    const uint64_t mask = __ballot(keep);
+    if (lane == 0) waves[wave] = __popcll(mask);
+    __syncthreads();
+    int before = done, all = 0;
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      if (i < wave) before += waves[i];
+      all += waves[i];
+    }
+    done += all;
+    const int at = before + __popcll(mask & ((1ull << lane) - 1));
+    if (keep) {
+      list[at] = t;
+      target[at] = y;
+      if (g) {
+        lse_kept[at] = lse_in[t];
+        g_kept[at] = gt * inv_t;
+      }
+    }
+    if (t < rows) {
+      const float none = y >= vocab ? __builtin_nanf("") : 0.f;
+      if (g) {
+        place[t] = keep ? at : y >= vocab ? -2 : -1;
+      } else if (!keep) {
+        logp[t] = none;
+        lse[t] = none;
+      }
+    }
+    __syncthreads();
+  }
+  for (int i = done + threadIdx.x; i < (int)((done + kRowPad - 1) / kRowPad * kRowPad); i += 1024) {
+    target[i] = -1;
+    if (g) lse_kept[i] = 0.f, g_kept[i] = 0.f;
+  }
+  if (threadIdx.x == 0) *count = done;
+}
+
+// Kept rows of h one after the other, zeros behind column `hidden` and behind the last row up to the padding.
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void gather_rows_kernel(const T* __restrict__ h, int64_t stride, int hidden, int ld,
+                                                          const int32_t* __restrict__ list, const int32_t* __restrict__ count,
+                                                          T* __restrict__ out) {
+  const int r = blockIdx.x, n = *count;
+  if (r >= (n + kRowPad - 1) / kRowPad * kRowPad) return;
+  const T* src = h + (r < n ? list[r] : 0) * stride;
+  for (int c = threadIdx.x * VEC; c < ld; c += 256 * VEC) {
+    float v[VEC];
+    if (r < n && c < hidden) {
+      ldv<VEC>(src + c, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; e++) v[e] = 0.f;
+    }
+    stv<VEC>(out + (size_t)r * ld + c, v);
+  }
+}
+
+// ---- products in 32 bits for every type and size ----------------------------------------------
+// C[i, j] = sum_k A[i, k] B[j, k], tiles of 128 x 128, four waves of 64 x 64 on 32x32x2 matrix instructions, 16 k at a time through
+// LDS as [k][row].  An operand is K-major (element (i, k) at i * ld + k) or not (at k * ld + i).
+template <typename T>
+struct Operand {
+  const T* p;
+  int64_t ld;
+  int n, vec;      // rows; 16-byte accesses allowed
+};
+template <typename T, bool KMAJOR>
+__device__ __forceinline__ void fetch8(const Operand<T>& o, int i0, int k0, int k1, float (&v)[8]) {
+  const int tid = threadIdx.x;
+  const int i = KMAJOR ? i0 + tid / 2 : i0 + tid % 16 * 8, k = KMAJOR ? k0 + tid % 2 * 8 : k0 + tid / 16;
+  const bool line = KMAJOR ? i < o.n : k < k1;
+  const T* p = KMAJOR ? o.p + (int64_t)i * o.ld + k : o.p + (int64_t)k * o.ld + i;
+  const int left = !line ? 0 : KMAJOR ? k1 - k : o.n - i;
+  if (left >= 8 && o.vec) {
+    if constexpr (sizeof(T) == 2) {
+      ldv<8>(p, v);
+    } else {
+      float a[4], b[4];
+      ldv<4>(p, a);
+      ldv<4>(p + 4, b);
+#pragma unroll
+      for (int e = 0; e < 4; e++) v[e] = a[e], v[4 + e] = b[e];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = e < left ? ldf(p + e) : 0.f;
+  }
+}
+constexpr int kPitch = 128 + 4;
+template <bool KMAJOR>
+__device__ __forceinline__ void put8(float (*to)[kPitch], const float (&v)[8]) {
+  const int tid = threadIdx.x;
+  if constexpr (KMAJOR) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) to[tid % 2 * 8 + e][tid / 2] = v[e];
+  } else {
+    *(float4*)&to[tid / 16][tid % 16 * 8] = make_float4(v[0], v[1], v[2], v[3]);
+    *(float4*)&to[tid / 16][tid % 16 * 8 + 4] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+}
+template <typename T, bool AK, bool BK, typename TB>
+__device__ __forceinline__ void product128(const Operand<T>& A, const Operand<TB>& B, int i0, int j0, int k0, int k1, f32x16 (&acc)[2][2]) {
+  __shared__ float as[16][kPitch], bs[16][kPitch];
+  const int lane = threadIdx.x & 63, wm = (threadIdx.x >> 7) * 64, wn = ((threadIdx.x >> 6) & 1) * 64;
+#pragma unroll
+  for (int a = 0; a < 2; a++)
+#pragma unroll
+    for (int b = 0; b < 2; b++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) acc[a][b][e] = 0.f;
+  float va[8], vb[8];
+  if (k0 < k1) {
+    fetch8<T, AK>(A, i0, k0, k1, va);
+    fetch8<TB, BK>(B, j0, k0, k1, vb);
+  }
+  for (int k = k0; k < k1; k += 16) {
+    __syncthreads();
+    put8<AK>(as, va);
+    put8<BK>(bs, vb);
+    __syncthreads();
+    if (k + 16 < k1) {
+      fetch8<T, AK>(A, i0, k + 16, k1, va);
+      fetch8<TB, BK>(B, j0, k + 16, k1, vb);
+    }
+#pragma unroll
+    for (int s = 0; s < 16; s += 2) {
+      float x[2], y[2];
+#pragma unroll
+      for (int a = 0; a < 2; a++) {
+        x[a] = as[s + (lane >> 5)][wm + 32 * a + (lane & 31)];
+        y[a] = bs[s + (lane >> 5)][wn + 32 * a + (lane & 31)];
+      }
+#pragma unroll
+      for (int a = 0; a < 2; a++)
+#pragma unroll
+        for (int b = 0; b < 2; b++) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[a], y[b], acc[a][b], 0, 0, 0);
+    }
+  }
+}
+// element e of a 32 x 32 result: column lane % 32, row
+__device__ __forceinline__ int row32(int lane, int e) { return 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3); }
+
+// logits of 128 tokens of the vocabulary (rows of the result) and 128 hidden rows (its columns: a lane holds one row's)
+template <typename T>
+__global__ __launch_bounds__(256) void logits_strip_kernel(const T* __restrict__ h, int ld, const T* __restrict__ w, int64_t ldw, int vocab,
+                                                           int hidden, int vec, KeptRows kept, float inv_t, float2* __restrict__ part,
+                                                           int padded, float* __restrict__ zt) {
+  const int n = *kept.count, j0 = blockIdx.x * 128, i0 = blockIdx.y * 128;
+  if (j0 >= n) return;
+  f32x16 acc[2][2];
+  product128<T, true, true>(Operand<T>{w, ldw, vocab, vec}, Operand<T>{h, ld, n, 1}, i0, j0, 0, hidden, acc);
+  __shared__ float2 half[2][128];
+  const int lane = threadIdx.x & 63, wm = threadIdx.x >> 7, wn = (threadIdx.x >> 6) & 1;
+#pragma unroll
+  for (int b = 0; b < 2; b++) {
+    const int col = wn * 64 + b * 32 + (lane & 31), j = j0 + col, y = j < n ? kept.target[j] : -1;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int a = 0; a < 2; a++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        const int v = i0 + wm * 64 + a * 32 + row32(lane, e);
+        acc[a][b][e] = v < vocab ? acc[a][b][e] * inv_t : -INFINITY;
+        if (v == y) zt[j] = acc[a][b][e];
+        top = fmaxf(top, acc[a][b][e]);
+      }
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int a = 0; a < 2; a++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) sum += expf(acc[a][b][e] - ref);
+    sum += __shfl_xor(sum, 32, 64);
+    if (lane < 32) half[wm][col] = make_float2(top, sum);
+  }
+  __syncthreads();
+  if (threadIdx.x < 128 && j0 + (int)threadIdx.x < n) {
+    const float2 a = half[0][threadIdx.x], b = half[1][threadIdx.x];
+    const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.f : top;
+    part[(size_t)blockIdx.y * padded + j0 + threadIdx.x] = make_float2(top, a.y * expf(a.x - ref) + b.y * expf(b.x - ref));
+  }
+}
+
+// 64 kept rows: their strips joined by 16 threads each, in a fixed order
+__global__ __launch_bounds__(1024) void join_strips_kernel(const float2* __restrict__ part, int strips, int padded, const float* __restrict__ zt,
+                                                           const int32_t* __restrict__ list, const int32_t* __restrict__ count,
+                                                           float* __restrict__ logp, float* __restrict__ lse) {
+  __shared__ float2 share[16][64];
+  const int n = *count, r = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6;
+  if (blockIdx.x * 64 >= n) return;
+  float top = -INFINITY, sum = 0.f;
+  auto join = [&](float2 p) {
+    const float t = fmaxf(top, p.x), ref = t == -INFINITY ? 0.f : t;
+    sum = sum * expf(top - ref) + p.y * expf(p.x - ref);
+    top = t;
+  };
+  if (r < n)
+    for (int i = k; i < strips; i += 16) join(part[(size_t)i * padded + r]);
+  share[k][threadIdx.x & 63] = make_float2(top, sum);
+  __syncthreads();
+  if (k == 0 && r < n) {
+#pragma unroll
+    for (int i = 1; i < 16; i++) join(share[i][threadIdx.x & 63]);
+    const float l = top + logf(sum);
+    logp[list[r]] = zt[r] - l;
+    lse[list[r]] = l;
+  }
+}
+
+// dz of 128 tokens of a piece and 128 hidden rows; zeros where there is no token or no row
+template <typename T>
+__global__ __launch_bounds__(256) void logits_gradient_kernel(const T* __restrict__ h, int ld, const T* __restrict__ w, int64_t ldw, int vocab,
+                                                              int hidden, int vec, KeptRows kept, float inv_t, VocabPiece piece,
+                                                              T* __restrict__ dz) {
+  const int n = *kept.count, j0 = blockIdx.x * 128, i0 = piece.v0 + blockIdx.y * 128;
+  if (j0 >= (n + kRowPad - 1) / kRowPad * kRowPad) return;
+  f32x16 acc[2][2];
+  product128<T, true, true>(Operand<T>{w, ldw, vocab, vec}, Operand<T>{h, ld, n, 1}, i0, j0, 0, hidden, acc);
+  const int lane = threadIdx.x & 63, wm = threadIdx.x >> 7, wn = (threadIdx.x >> 6) & 1;
+#pragma unroll
+  for (int b = 0; b < 2; b++) {
+    const int j = j0 + wn * 64 + b * 32 + (lane & 31), y = kept.target[j];
+    const float l = kept.lse[j], g = kept.g[j];
+#pragma unroll
+    for (int a = 0; a < 2; a++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        const int v = i0 + wm * 64 + a * 32 + row32(lane, e);
+        const float d = j < n && v < vocab ? g * ((v == y ? 1.f : 0.f) - expf(acc[a][b][e] * inv_t - l)) : 0.f;
+        st1(dz + (size_t)j * piece.ld + (v - piece.v0), d);
+      }
+  }
+}
+
+// slice z of dh (+)= dz W over its share of the piece
+template <typename T>
+__global__ __launch_bounds__(256) void hidden_gradient_kernel(const T* __restrict__ dz, VocabPiece piece, const T* __restrict__ w, int64_t ldw,
+                                                              int hidden, int vec, const int32_t* __restrict__ count, int per_slice,
+                                                              float* __restrict__ dh, size_t slice_stride, int first) {
+  const int n = *count, i0 = blockIdx.x * 128, j0 = blockIdx.y * 128;
+  if (i0 >= n) return;
+  const int k0 = blockIdx.z * per_slice, k1 = min(k0 + per_slice, piece.width);
+  f32x16 acc[2][2];
+  product128<T, true, false>(Operand<T>{dz, piece.ld, n, 1}, Operand<T>{w + (int64_t)piece.v0 * ldw, ldw, hidden, vec}, i0, j0, k0, k1, acc);
+  const int lane = threadIdx.x & 63, wm = threadIdx.x >> 7, wn = (threadIdx.x >> 6) & 1;
+  float* out = dh + blockIdx.z * slice_stride;
+#pragma unroll
+  for (int a = 0; a < 2; a++)
+#pragma unroll
+    for (int b = 0; b < 2; b++) {
+      const int j = j0 + wn * 64 + b * 32 + (lane & 31);
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        const int i = i0 + wm * 64 + a * 32 + row32(lane, e);
+        if (i < n && j < hidden) {
+          float* p = out + (size_t)i * hidden + j;
+          *p = first ? acc[a][b][e] : *p + acc[a][b][e];
+        }
+      }
+    }
+}
+
+// dW of a piece = dz^T h
+template <typename T>
+__global__ __launch_bounds__(256) void weight_gradient_kernel(const T* __restrict__ dz, VocabPiece piece, const T* __restrict__ h, int ld,
+                                                              int hidden, const int32_t* __restrict__ count, T* __restrict__ dw) {
+  const int n = *count, i0 = blockIdx.y * 128, j0 = blockIdx.x * 128;
+  f32x16 acc[2][2];
+  product128<T, false, false>(Operand<T>{dz, piece.ld, piece.width, 1}, Operand<T>{h, ld, hidden, 1}, i0, j0, 0, n, acc);
+  const int lane = threadIdx.x & 63, wm = threadIdx.x >> 7, wn = (threadIdx.x >> 6) & 1;
+#pragma unroll
+  for (int a = 0; a < 2; a++)
+#pragma unroll
+    for (int b = 0; b < 2; b++) {
+      const int j = j0 + wn * 64 + b * 32 + (lane & 31);
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        const int i = i0 + wm * 64 + a * 32 + row32(lane, e);
+        if (i < piece.width && j < hidden) st1(dw + (size_t)(piece.v0 + i) * hidden + j, acc[a][b][e]);
+      }
+    }
+}
+
+// rows of dh: the slices' sum, zeros where a row takes no part
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void hidden_gradient_rows_kernel(const float* __restrict__ slices, int n_slices, size_t slice_stride, int hidden,
+                                                                   const int32_t* __restrict__ place, T* __restrict__ dh) {
+  const int t = blockIdx.x, at = place[t];
+  for (int c = threadIdx.x * VEC; c < hidden; c += 256 * VEC) {
+    float v[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; e++) v[e] = at == -2 ? __builtin_nanf("") : 0.f;
+    if (at >= 0)
+      for (int s = 0; s < n_slices; s++) {
+        float x[VEC];
+        ldv<VEC>(slices + s * slice_stride + (size_t)at * hidden + c, x);
+#pragma unroll
+        for (int e = 0; e < VEC; e++) v[e] += x[e];
+      }
+    stv<VEC>(dh + (size_t)t * hidden + c, v);
+  }
+}
+
+// no rows at all: the weights' gradient is zero
+__global__ __launch_bounds__(256) void zeros_kernel(uint16_t* __restrict__ p, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
+}
+
+// ---- where everything lies in the workspace ----------------------------------------------------
+// A piece's dz takes up to 512 MB: enough tokens of the vocabulary for full launches at any number of rows that fits a card, and
+// little beside 288 GB.
+const int64_t kPieceBytes = 512ll << 20;
+struct Workspace {
+  int64_t padded;            // rows, padded
+  int ld;                    // of the gathered rows
+  int strips;                // forward
+  int width;                 // backward: vocabulary of a piece
+  int slices, per_slice;     // backward: of the product dz W
+  int64_t count, list, place, target, lse, g, zt, rows, part, dz, dh, bytes;
+};
+Workspace plan(int64_t rows, int hidden, int vocab, int dtype, bool backward) {
+  const int el = dtype == RL_DTYPE_BF16 ? 2 : 4;
+  Workspace w{};
+  w.padded = up(rows, kRowPad);
+  w.ld = (int)up(hidden, 64);
+  auto take = [&](int64_t n) {
+    const int64_t at = w.bytes;
+    w.bytes = up(at + n, 256);
+    return at;
+  };
+  w.count = take(4);
+  w.list = take(w.padded * 4);
+  w.target = take(w.padded * 4);
+  w.rows = take(w.padded * w.ld * el);
+  if (!backward) {
+    w.strips = (vocab + 127) / 128;
+    w.zt = take(w.padded * 4);
+    w.part = take(w.padded * w.strips * 8);
+    return w;
+  }
+  w.place = take(w.padded * 4);
+  w.lse = take(w.padded * 4);
+  w.g = take(w.padded * 4);
+  const int64_t fit = std::max<int64_t>(kPieceBytes / (w.padded * el) / 256 * 256, 2048), pieces = (vocab + fit - 1) / fit;
+  w.width = (int)up((vocab + pieces - 1) / pieces, 256);
+  // slices of the vocabulary until the product has two workgroups a CU
+  const int64_t tiles = w.padded / 128 * ((hidden + 127) / 128);
+  w.slices = (int)std::min<int64_t>(std::max<int64_t>(512 / tiles, 1), std::min(w.width / 256, 16));
+  w.per_slice = (int)up((w.width + w.slices - 1) / w.slices, 64);
+  w.dz = take(w.padded * w.width * el);
+  w.dh = take(w.padded * hidden * 4 * w.slices);
+  return w;
+}
+
+const char* logprob_argument(int64_t rows, int32_t hidden, int32_t vocab, float temperature, int32_t dtype) {
+  if (dtype != RL_DTYPE_F32 && dtype != RL_DTYPE_BF16) return "dtype is RL_DTYPE_F32 or RL_DTYPE_BF16";
+  if (rows < 0 || rows > (1 << 24) || hidden < 1 || hidden > 65536 || vocab < 1 || vocab > (1 << 22)) return "rows, hidden or vocab out of range";
+  if (!(temperature > 0.f) || temperature - temperature != 0.f || !(1.f / temperature <= 3.4e38f))
+    return "temperature is a positive finite number with a finite reciprocal";
+  return nullptr;
+}
+
+template <typename T>
+void gather(const void* h, int64_t stride, int hidden, const Workspace& w, char* ws, hipStream_t s) {
+  constexpr int VEC = 16 / sizeof(T);
+  const int32_t *list = (int32_t*)(ws + w.list), *count = (int32_t*)(ws + w.count);
+  if (hidden % VEC == 0 && stride % VEC == 0 && aligned16(h))
+    gather_rows_kernel<T, VEC><<<(unsigned)w.padded, 256, 0, s>>>((const T*)h, stride, hidden, w.ld, list, count, (T*)(ws + w.rows));
+  else
+    gather_rows_kernel<T, 1><<<(unsigned)w.padded, 256, 0, s>>>((const T*)h, stride, hidden, w.ld, list, count, (T*)(ws + w.rows));
+}
+
+template <typename T>
+int forward(const void* h, int64_t stride, int rows, int hidden, const void* weight, int vocab, const int32_t* targets, float inv_t,
+            float* logp, float* lse, char* ws, hipStream_t s) {
+  const Workspace w = plan(rows, hidden, vocab, sizeof(T) == 2 ? RL_DTYPE_BF16 : RL_DTYPE_F32, false);
+  const KeptRows kept{(int32_t*)(ws + w.count), (int32_t*)(ws + w.target), nullptr, nullptr};
+  keep_rows_kernel<<<1, 1024, 0, s>>>(targets, rows, vocab, nullptr, nullptr, inv_t, (int32_t*)(ws + w.count), (int32_t*)(ws + w.list),
+                                      nullptr, (int32_t*)(ws + w.target), nullptr, nullptr, logp, lse);
+  gather<T>(h, stride, hidden, w, ws, s);
+  const int vec = hidden % (16 / sizeof(T)) == 0 && aligned16(weight);
+  logits_strip_kernel<T><<<dim3((rows + 127) / 128, w.strips), 256, 0, s>>>((const T*)(ws + w.rows), w.ld, (const T*)weight, hidden, vocab, hidden,
+                                                                           vec, kept, inv_t, (float2*)(ws + w.part), (int)w.padded,
+                                                                           (float*)(ws + w.zt));
+  join_strips_kernel<<<(rows + 63) / 64, 1024, 0, s>>>((const float2*)(ws + w.part), w.strips, (int)w.padded, (const float*)(ws + w.zt),
+                                                       (const int32_t*)(ws + w.list), kept.count, logp, lse);
+  return launched();
+}
+
+template <typename T>
+int backward(const float* g, const void* h, int64_t stride, int rows, int hidden, const void* weight, int vocab, const int32_t* targets,
+             const float* lse, float inv_t, void* dh, void* dw, char* ws, hipStream_t s) {
+  const Workspace w = plan(rows, hidden, vocab, sizeof(T) == 2 ? RL_DTYPE_BF16 : RL_DTYPE_F32, true);
+  const KeptRows kept{(int32_t*)(ws + w.count), (int32_t*)(ws + w.target), (float*)(ws + w.lse), (float*)(ws + w.g)};
+  keep_rows_kernel<<<1, 1024, 0, s>>>(targets, rows, vocab, g, lse, inv_t, (int32_t*)(ws + w.count), (int32_t*)(ws + w.list),
+                                      (int32_t*)(ws + w.place), (int32_t*)(ws + w.target), (float*)(ws + w.lse), (float*)(ws + w.g), nullptr,
+                                      nullptr);
+  gather<T>(h, stride, hidden, w, ws, s);
+  const int vec = hidden % (16 / sizeof(T)) == 0 && aligned16(weight);
+  const T *hr = (const T*)(ws + w.rows), *wt = (const T*)weight;
+  T* dz = (T*)(ws + w.dz);
+  const unsigned rt = (rows + 127) / 128, ht = (hidden + 127) / 128;
+  for (int v0 = 0; v0 < vocab; v0 += w.width) {
+    const VocabPiece piece{v0, std::min(w.width, vocab - v0), w.width};
+    const unsigned vt = (piece.width + 127) / 128;
+    logits_gradient_kernel<T><<<dim3((unsigned)(w.padded / 128), vt), 256, 0, s>>>(hr, w.ld, wt, hidden, vocab, hidden, vec, kept, inv_t, piece, dz);
+    hidden_gradient_kernel<T><<<dim3(rt, ht, w.slices), 256, 0, s>>>(dz, piece, wt, hidden, hidden, vec, kept.count, w.per_slice,
+                                                                    (float*)(ws + w.dh), (size_t)w.padded * hidden, v0 == 0);
+    weight_gradient_kernel<T><<<dim3(ht, vt), 256, 0, s>>>(dz, piece, hr, w.ld, hidden, kept.count, (T*)dw);
+  }
+  const float* slices = (const float*)(ws + w.dh);
+  const int32_t* place = (const int32_t*)(ws + w.place);
+  constexpr int VEC = 16 / sizeof(T);
+  if (hidden % VEC == 0 && aligned16(dh))
+    hidden_gradient_rows_kernel<T, VEC><<<rows, 256, 0, s>>>(slices, w.slices, (size_t)w.padded * hidden, hidden, place, (T*)dh);
+  else
+    hidden_gradient_rows_kernel<T, 1><<<rows, 256, 0, s>>>(slices, w.slices, (size_t)w.padded * hidden, hidden, place, (T*)dh);
+  return launched();
+}
+
+}  // namespace
+
+extern "C" int64_t rl_token_logprobs_workspace(int32_t rows, int32_t hidden, int32_t vocab, int32_t dtype, int32_t backward) {
+  if (rows < 1 || logprob_argument(rows, hidden, vocab, 1.f, dtype)) return 0;
+  return plan(rows, hidden, vocab, dtype, backward != 0).bytes;
+}
+
+extern "C" int rl_token_logprobs_forward(const void* d_hidden, int64_t row_stride, int32_t rows, int32_t hidden, const void* d_weight,
+                                         int32_t vocab, const int32_t* d_targets, float temperature, int32_t dtype, float* d_logp,
+                                         float* d_lse, void* d_workspace, int64_t workspace_bytes, void* stream) {
+  if (const char* m = logprob_argument(rows, hidden, vocab, temperature, dtype)) return rl_fail(RL_E_ARG, m);
+  if (rows == 0) return RL_OK;
+  if (!d_hidden || !d_weight || !d_targets || !d_logp || !d_lse || !d_workspace) return rl_fail(RL_E_ARG, "null pointer");
+  if (workspace_bytes < rl_token_logprobs_workspace(rows, hidden, vocab, dtype, 0))
+    return rl_fail(RL_E_ARG, "workspace smaller than rl_token_logprobs_workspace says");
+  if ((uintptr_t)d_workspace & 255) return rl_fail(RL_E_ARG, "workspace not aligned to 256 bytes");
+  const float inv_t = 1.f / temperature;
+#define RL_GO(T) forward<T>(d_hidden, row_stride, rows, hidden, d_weight, vocab, d_targets, inv_t, d_logp, d_lse, (char*)d_workspace, (hipStream_t)stream)
+  return dtype == RL_DTYPE_F32 ? RL_GO(float) : RL_GO(bf16_t);
+#undef RL_GO
+}
+
+extern "C" int rl_token_logprobs_backward(const float* d_dlogp, const void* d_hidden, int64_t row_stride, int32_t rows, int32_t hidden,
+                                          const void* d_weight, int32_t vocab, const int32_t* d_targets, const float* d_lse,
+                                          float temperature, int32_t dtype, void* d_dhidden, void* d_dweight, void* d_workspace,
+                                          int64_t workspace_bytes, void* stream) {
+  if (const char* m = logprob_argument(rows, hidden, vocab, temperature, dtype)) return rl_fail(RL_E_ARG, m);
+  if (rows == 0) {
+    if (!d_dweight) return rl_fail(RL_E_ARG, "null pointer");
+    const int64_t n = (int64_t)vocab * hidden * (dtype == RL_DTYPE_BF16 ? 1 : 2);
+    zeros_kernel<<<1024, 256, 0, (hipStream_t)stream>>>((uint16_t*)d_dweight, n);
+    return launched();
+  }
+  if (!d_dlogp || !d_hidden || !d_weight || !d_targets || !d_lse || !d_dhidden || !d_dweight || !d_workspace)
+    return rl_fail(RL_E_ARG, "null pointer");
+  if (workspace_bytes < rl_token_logprobs_workspace(rows, hidden, vocab, dtype, 1))
+    return rl_fail(RL_E_ARG, "workspace smaller than rl_token_logprobs_workspace says");
+  if ((uintptr_t)d_workspace & 255) return rl_fail(RL_E_ARG, "workspace not aligned to 256 bytes");
+  const float inv_t = 1.f / temperature;
+#define RL_GO(T) \
+  backward<T>(d_dlogp, d_hidden, row_stride, rows, hidden, d_weight, vocab, d_targets, d_lse, inv_t, d_dhidden, d_dweight, \
+              (char*)d_workspace, (hipStream_t)stream)
+  return dtype == RL_DTYPE_F32 ? RL_GO(float) : RL_GO(bf16_t);
+#undef RL_GO
+}

@@ -1,0 +1,51 @@
+// Attention over packed sequences: what its kernels share.
+#pragma once
+#include "policy_common.h"
+
+// Sequence s: queries [cu_q[s], cu_q[s + 1]), keys [cu_k[s], cu_k[s + 1]).  Causal: query i of lq sees the keys j <= i + lk - lq,
+// so the last query sees all of them and, where lq > lk, the first lq - lk see none.
+struct PackedShape {
+  const int32_t *cu_q, *cu_k;
+  int n_seq, total_q, total_k;
+  int nq, nkv, d;
+  int64_t qt, qh, kt, kh, vt, vh, ot, oh;      // strides of token and head in elements; dO and the gradients are contiguous
+  float scale;
+  int causal;
+};
+
+// Tiles of `rows` rows of every sequence, numbered through without a list: the tiles of sequence s begin at floor(cu[s] / rows) + s,
+// which leaves each sequence as many numbers as it needs (floor((a + n) / rows) + 1 >= floor(a / rows) + ceil(n / rows)) and some
+// without a tile.  packed_tiles: how many numbers there are.  Whatever cu holds, what comes back lies inside [0, total].
+struct PackedTile {
+  int seq, first, len;      // first token of the sequence and its length, in the tiled tensor
+  int row0;                 // first row of the tile within the sequence; >= len: no such tile
+};
+static inline __host__ __device__ int packed_tiles(int total, int n_seq, int rows) { return total / rows + n_seq; }
+__device__ __forceinline__ int packed_bound(const int32_t* cu, int s, int total) {
+  const int c = cu[s];
+  return c < 0 ? 0 : c > total ? total : c;
+}
+__device__ __forceinline__ PackedTile packed_tile(const int32_t* cu, int n_seq, int total, int rows, int tile) {
+  int lo = 0, hi = n_seq;      // sequence `lo` begins at or before the tile, `hi` behind it
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (packed_bound(cu, mid, total) / rows + mid <= tile) lo = mid;
+    else hi = mid;
+  }
+  PackedTile t;
+  t.seq = lo;
+  t.first = packed_bound(cu, lo, total);
+  const int end = packed_bound(cu, lo + 1, total);
+  t.len = end > t.first ? end - t.first : 0;
+  const int row0 = tile - (t.first / rows + lo);
+  t.row0 = row0 < 0 ? t.len : row0 <= t.len / rows ? row0 * rows : t.len;
+  return t;
+}
+
+// bf16, head sizes up to 128 in multiples of 8, 16-byte aligned rows.
+bool attention_takes_mfma(const PackedShape& p, const void* q, const void* k, const void* v, const void* o);
+void launch_attention_mfma_forward(hipStream_t s, const PackedShape& p, const bf16_t* q, const bf16_t* k, const bf16_t* v, bf16_t* o,
+                                   float* lse);
+void launch_attention_mfma_backward(hipStream_t s, const PackedShape& p, const bf16_t* dout, const bf16_t* q, const bf16_t* k,
+                                    const bf16_t* v, const bf16_t* o, const float* lse, bf16_t* dq, bf16_t* dk, bf16_t* dv,
+                                    float* delta);
