@@ -18,6 +18,7 @@ SOURCES = {
     "kernels_rows.hip": [],
     "kernels_packed_attention.hip": [],
     "kernels_token_logprob.hip": [],
+    "kernels_token_logprob_mfma.hip": [],
     "engine.hip": [],
 }
 

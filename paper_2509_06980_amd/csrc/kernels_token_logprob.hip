@@ -370,11 +370,13 @@ Workspace plan(int64_t rows, int hidden, int vocab, int dtype, bool backward) {
   w.place = take(w.padded * 4);
   w.lse = take(w.padded * 4);
   w.g = take(w.padded * 4);
-  const int64_t fit = std::max<int64_t>(kPieceBytes / (w.padded * el) / 256 * 256, 2048), pieces = (vocab + fit - 1) / fit;
+  const int64_t fit = std::max<int64_t>(std::min<int64_t>(kPieceBytes / (w.padded * el), ((1ll << 31) - (1 << 20)) / (hidden * el)) / 256 * 256, 1024);
+  const int64_t pieces = (vocab + fit - 1) / fit;
   w.width = (int)up((vocab + pieces - 1) / pieces, 256);
-  // slices of the vocabulary until the product has two workgroups a CU
+  // slices of the vocabulary: fp32 until the product has two workgroups a CU
   const int64_t tiles = w.padded / 128 * ((hidden + 127) / 128);
-  w.slices = (int)std::min<int64_t>(std::max<int64_t>(512 / tiles, 1), std::min(w.width / 256, 16));
+  w.slices = el == 2 ? token_logprob_slices((int)rows, hidden, w.width)
+                     : (int)std::min<int64_t>(std::max<int64_t>(512 / tiles, 1), std::min(w.width / 256, 16));
   w.per_slice = (int)up((w.width + w.slices - 1) / w.slices, 64);
   w.dz = take(w.padded * w.width * el);
   w.dh = take(w.padded * hidden * 4 * w.slices);
@@ -407,11 +409,22 @@ int forward(const void* h, int64_t stride, int rows, int hidden, const void* wei
   keep_rows_kernel<<<1, 1024, 0, s>>>(targets, rows, vocab, nullptr, nullptr, inv_t, (int32_t*)(ws + w.count), (int32_t*)(ws + w.list),
                                       nullptr, (int32_t*)(ws + w.target), nullptr, nullptr, logp, lse);
   gather<T>(h, stride, hidden, w, ws, s);
+  int strips = w.strips;
+  bool mfma = false;
+  if constexpr (sizeof(T) == 2) {
+    mfma = token_logprob_takes_mfma(w.padded, w.ld, hidden, 0, weight, nullptr);
+    if (mfma) {
+      strips = (vocab + kStripMfma - 1) / kStripMfma;
+      launch_logits_strips_mfma(s, (const bf16_t*)(ws + w.rows), w.ld, rows, w.padded, (const bf16_t*)weight, vocab, hidden, kept, inv_t,
+                                (float2*)(ws + w.part), (float*)(ws + w.zt));
+    }
+  }
   const int vec = hidden % (16 / sizeof(T)) == 0 && aligned16(weight);
-  logits_strip_kernel<T><<<dim3((rows + 127) / 128, w.strips), 256, 0, s>>>((const T*)(ws + w.rows), w.ld, (const T*)weight, hidden, vocab, hidden,
+  if (!mfma)
+    logits_strip_kernel<T><<<dim3((rows + 127) / 128, w.strips), 256, 0, s>>>((const T*)(ws + w.rows), w.ld, (const T*)weight, hidden, vocab, hidden,
                                                                            vec, kept, inv_t, (float2*)(ws + w.part), (int)w.padded,
                                                                            (float*)(ws + w.zt));
-  join_strips_kernel<<<(rows + 63) / 64, 1024, 0, s>>>((const float2*)(ws + w.part), w.strips, (int)w.padded, (const float*)(ws + w.zt),
+  join_strips_kernel<<<(rows + 63) / 64, 1024, 0, s>>>((const float2*)(ws + w.part), strips, (int)w.padded, (const float*)(ws + w.zt),
                                                        (const int32_t*)(ws + w.list), kept.count, logp, lse);
   return launched();
 }
@@ -428,10 +441,20 @@ int backward(const float* g, const void* h, int64_t stride, int rows, int hidden
   const int vec = hidden % (16 / sizeof(T)) == 0 && aligned16(weight);
   const T *hr = (const T*)(ws + w.rows), *wt = (const T*)weight;
   T* dz = (T*)(ws + w.dz);
+  const bool mfma = sizeof(T) == 2 && token_logprob_takes_mfma(w.padded, w.ld, hidden, w.width, weight, dw);
   const unsigned rt = (rows + 127) / 128, ht = (hidden + 127) / 128;
   for (int v0 = 0; v0 < vocab; v0 += w.width) {
     const VocabPiece piece{v0, std::min(w.width, vocab - v0), w.width};
     const unsigned vt = (piece.width + 127) / 128;
+    if constexpr (sizeof(T) == 2) {
+      if (mfma) {
+        launch_logits_gradient_mfma(s, hr, w.ld, rows, w.padded, wt, vocab, hidden, kept, inv_t, piece, dz);
+        launch_hidden_gradient_mfma(s, dz, piece, rows, w.padded, wt, vocab, hidden, kept, w.slices, w.per_slice, (float*)(ws + w.dh),
+                                    (size_t)w.padded * hidden, v0 == 0);
+        launch_weight_gradient_mfma(s, dz, piece, hr, w.ld, w.padded, hidden, kept, (bf16_t*)dw);
+        continue;
+      }
+    }
     logits_gradient_kernel<T><<<dim3((unsigned)(w.padded / 128), vt), 256, 0, s>>>(hr, w.ld, wt, hidden, vocab, hidden, vec, kept, inv_t, piece, dz);
     hidden_gradient_kernel<T><<<dim3(rt, ht, w.slices), 256, 0, s>>>(dz, piece, wt, hidden, hidden, vec, kept.count, w.per_slice,
                                                                     (float*)(ws + w.dh), (size_t)w.padded * hidden, v0 == 0);

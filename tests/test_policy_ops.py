@@ -381,7 +381,7 @@ def test_token_logprobs(rows, hidden, vocab, sampled, dt):
 
 @pytest.mark.parametrize("dt", [BF, FP])
 def test_token_logprobs_over_several_pieces_of_the_vocabulary(dt):
-    # pieces hold at least 2048 tokens: rows enough that the budget of a piece stays at that, few of them with a target
+    # pieces hold at least 1024 tokens: rows enough that the budget of a piece stays at that, few of them with a target
     g = gen(2)
     rows, hidden, vocab = (70_000 if dt == FP else 140_000), 64, 5000
     w, h = randn(g, vocab, hidden, dt=dt, std=0.25), randn(g, rows, hidden, dt=dt)
