@@ -19,7 +19,8 @@ __global__ __launch_bounds__(1024) void keep_rows_kernel(const int32_t* __restri
                                                          const float* __restrict__ lse_in, float inv_t, int32_t* __restrict__ count,
                                                          int32_t* __restrict__ list, int32_t* __restrict__ place,
                                                          int32_t* __restrict__ target, float* __restrict__ lse_kept,
-                                                         float* __restrict__ g_kept, float* __restrict__ logp, float* __restrict__ lse) {
+                                                         float* __restrict__ g_kept, float* __restrict__ logp, float* __restrict__ lse,
+                                                         SliceRule rule) {
   __shared__ int waves[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int done = 0;
@@ -61,7 +62,14 @@ __global__ __launch_bounds__(1024) void keep_rows_kernel(const int32_t* __restri
     target[i] = -1;
     if (g) lse_kept[i] = 0.f, g_kept[i] = 0.f;
   }
-  if (threadIdx.x == 0) *count = done;
+  if (threadIdx.x == 0) {
+    count[0] = done;
+    if (g) {
+      const int n = choose_slices(rule, done);
+      count[1] = n;
+      count[2] = ((rule.width + n - 1) / n + 63) / 64 * 64;
+    }
+  }
 }
 
 // Kept rows of h one after the other, zeros behind column `hidden` and behind the last row up to the padding.
@@ -264,11 +272,10 @@ __global__ __launch_bounds__(256) void logits_gradient_kernel(const T* __restric
 // slice z of dh (+)= dz W over its share of the piece
 template <typename T>
 __global__ __launch_bounds__(256) void hidden_gradient_kernel(const T* __restrict__ dz, VocabPiece piece, const T* __restrict__ w, int64_t ldw,
-                                                              int hidden, int vec, const int32_t* __restrict__ count, int per_slice,
-                                                              float* __restrict__ dh, size_t slice_stride, int first) {
+                                                              int hidden, int vec, const int32_t* __restrict__ count, float* __restrict__ dh, size_t slice_stride, int first) {
   const int n = *count, i0 = blockIdx.x * 128, j0 = blockIdx.y * 128;
-  if (i0 >= n) return;
-  const int k0 = blockIdx.z * per_slice, k1 = min(k0 + per_slice, piece.width);
+  if (i0 >= n || (int)blockIdx.z >= count[1]) return;
+  const int k0 = blockIdx.z * count[2], k1 = min(k0 + count[2], piece.width);
   f32x16 acc[2][2];
   product128<T, true, false>(Operand<T>{dz, piece.ld, n, 1}, Operand<T>{w + (int64_t)piece.v0 * ldw, ldw, hidden, vec}, i0, j0, k0, k1, acc);
   const int lane = threadIdx.x & 63, wm = threadIdx.x >> 7, wn = (threadIdx.x >> 6) & 1;
@@ -312,9 +319,9 @@ __global__ __launch_bounds__(256) void weight_gradient_kernel(const T* __restric
 
 // rows of dh: the slices' sum, zeros where a row takes no part
 template <typename T, int VEC>
-__global__ __launch_bounds__(256) void hidden_gradient_rows_kernel(const float* __restrict__ slices, int n_slices, size_t slice_stride, int hidden,
-                                                                   const int32_t* __restrict__ place, T* __restrict__ dh) {
-  const int t = blockIdx.x, at = place[t];
+__global__ __launch_bounds__(256) void hidden_gradient_rows_kernel(const float* __restrict__ slices, const int32_t* __restrict__ count, size_t slice_stride,
+                                                                   int hidden, const int32_t* __restrict__ place, T* __restrict__ dh) {
+  const int t = blockIdx.x, at = place[t], n_slices = count[1];
   for (int c = threadIdx.x * VEC; c < hidden; c += 256 * VEC) {
     float v[VEC];
 #pragma unroll
@@ -338,26 +345,26 @@ __global__ __launch_bounds__(256) void zeros_kernel(uint16_t* __restrict__ p, in
 // ---- where everything lies in the workspace ----------------------------------------------------
 // A piece's dz takes up to 512 MB: enough tokens of the vocabulary for full launches at any number of rows that fits a card, and
 // little beside 288 GB.
-const int64_t kPieceBytes = 512ll << 20;
+const int64_t kPieceBytes = 1ll << 30;
 struct Workspace {
   int64_t padded;            // rows, padded
   int ld;                    // of the gathered rows
   int strips;                // forward
-  int width;                 // backward: vocabulary of a piece
-  int slices, per_slice;     // backward: of the product dz W
+  int width, ldz;            // backward: vocabulary of a piece, row length of dz
+  SliceRule slices;          // backward: of the product dz W
   int64_t count, list, place, target, lse, g, zt, rows, part, dz, dh, bytes;
 };
 Workspace plan(int64_t rows, int hidden, int vocab, int dtype, bool backward) {
   const int el = dtype == RL_DTYPE_BF16 ? 2 : 4;
   Workspace w{};
   w.padded = up(rows, kRowPad);
-  w.ld = (int)up(hidden, 64);
+  w.ld = (int)(up(hidden, 128) + (up(hidden, 128) % 256 == 0 ? 128 : 0));
   auto take = [&](int64_t n) {
     const int64_t at = w.bytes;
     w.bytes = up(at + n, 256);
     return at;
   };
-  w.count = take(4);
+  w.count = take(12);
   w.list = take(w.padded * 4);
   w.target = take(w.padded * 4);
   w.rows = take(w.padded * w.ld * el);
@@ -373,13 +380,16 @@ Workspace plan(int64_t rows, int hidden, int vocab, int dtype, bool backward) {
   const int64_t fit = std::max<int64_t>(std::min<int64_t>(kPieceBytes / (w.padded * el), ((1ll << 31) - (1 << 20)) / (hidden * el)) / 256 * 256, 1024);
   const int64_t pieces = (vocab + fit - 1) / fit;
   w.width = (int)up((vocab + pieces - 1) / pieces, 256);
-  // slices of the vocabulary: fp32 until the product has two workgroups a CU
-  const int64_t tiles = w.padded / 128 * ((hidden + 127) / 128);
-  w.slices = el == 2 ? token_logprob_slices((int)rows, hidden, w.width)
-                     : (int)std::min<int64_t>(std::max<int64_t>(512 / tiles, 1), std::min(w.width / 256, 16));
-  w.per_slice = (int)up((w.width + w.slices - 1) / w.slices, 64);
-  w.dz = take(w.padded * w.width * el);
-  w.dh = take(w.padded * hidden * 4 * w.slices);
+  // bf16: 0.6 us for 32 k of a tile of 256 rows, 0.35 of 128 rows, measured; fp32: 1.8.  Up to 64 slices, 512 MB of sums.
+  w.slices.rows = el == 2 ? token_logprob_tile_rows((int)rows) : 128;
+  w.slices.tiles_j = el == 2 ? (hidden + 255) / 256 : (hidden + 127) / 128;
+  w.slices.width = w.width;
+  w.slices.most = (int)std::max<int64_t>(std::min({(int64_t)64, kPieceBytes / 2 / (w.padded * hidden * 4), (int64_t)w.width / 256}), 1);
+  w.slices.chunk_us = el == 2 ? (w.slices.rows == 256 ? 0.6f : 0.35f) : 1.8f;
+  w.slices.slice_us = (float)(hidden * 8 / 4.8e6);
+  w.ldz = w.width + 128;
+  w.dz = take(w.padded * w.ldz * el);
+  w.dh = take(w.padded * hidden * 4 * w.slices.most);
   return w;
 }
 
@@ -407,7 +417,7 @@ int forward(const void* h, int64_t stride, int rows, int hidden, const void* wei
   const Workspace w = plan(rows, hidden, vocab, sizeof(T) == 2 ? RL_DTYPE_BF16 : RL_DTYPE_F32, false);
   const KeptRows kept{(int32_t*)(ws + w.count), (int32_t*)(ws + w.target), nullptr, nullptr};
   keep_rows_kernel<<<1, 1024, 0, s>>>(targets, rows, vocab, nullptr, nullptr, inv_t, (int32_t*)(ws + w.count), (int32_t*)(ws + w.list),
-                                      nullptr, (int32_t*)(ws + w.target), nullptr, nullptr, logp, lse);
+                                      nullptr, (int32_t*)(ws + w.target), nullptr, nullptr, logp, lse, SliceRule{});
   gather<T>(h, stride, hidden, w, ws, s);
   int strips = w.strips;
   bool mfma = false;
@@ -436,37 +446,37 @@ int backward(const float* g, const void* h, int64_t stride, int rows, int hidden
   const KeptRows kept{(int32_t*)(ws + w.count), (int32_t*)(ws + w.target), (float*)(ws + w.lse), (float*)(ws + w.g)};
   keep_rows_kernel<<<1, 1024, 0, s>>>(targets, rows, vocab, g, lse, inv_t, (int32_t*)(ws + w.count), (int32_t*)(ws + w.list),
                                       (int32_t*)(ws + w.place), (int32_t*)(ws + w.target), (float*)(ws + w.lse), (float*)(ws + w.g), nullptr,
-                                      nullptr);
+                                      nullptr, w.slices);
   gather<T>(h, stride, hidden, w, ws, s);
   const int vec = hidden % (16 / sizeof(T)) == 0 && aligned16(weight);
   const T *hr = (const T*)(ws + w.rows), *wt = (const T*)weight;
   T* dz = (T*)(ws + w.dz);
-  const bool mfma = sizeof(T) == 2 && token_logprob_takes_mfma(w.padded, w.ld, hidden, w.width, weight, dw);
+  const bool mfma = sizeof(T) == 2 && token_logprob_takes_mfma(w.padded, w.ld, hidden, w.ldz, weight, dw);
   const unsigned rt = (rows + 127) / 128, ht = (hidden + 127) / 128;
   for (int v0 = 0; v0 < vocab; v0 += w.width) {
-    const VocabPiece piece{v0, std::min(w.width, vocab - v0), w.width};
+    const VocabPiece piece{v0, std::min(w.width, vocab - v0), w.ldz};
     const unsigned vt = (piece.width + 127) / 128;
     if constexpr (sizeof(T) == 2) {
       if (mfma) {
         launch_logits_gradient_mfma(s, hr, w.ld, rows, w.padded, wt, vocab, hidden, kept, inv_t, piece, dz);
-        launch_hidden_gradient_mfma(s, dz, piece, rows, w.padded, wt, vocab, hidden, kept, w.slices, w.per_slice, (float*)(ws + w.dh),
+        launch_hidden_gradient_mfma(s, dz, piece, rows, w.padded, wt, vocab, hidden, kept, w.slices.most, (float*)(ws + w.dh),
                                     (size_t)w.padded * hidden, v0 == 0);
         launch_weight_gradient_mfma(s, dz, piece, hr, w.ld, w.padded, hidden, kept, (bf16_t*)dw);
         continue;
       }
     }
     logits_gradient_kernel<T><<<dim3((unsigned)(w.padded / 128), vt), 256, 0, s>>>(hr, w.ld, wt, hidden, vocab, hidden, vec, kept, inv_t, piece, dz);
-    hidden_gradient_kernel<T><<<dim3(rt, ht, w.slices), 256, 0, s>>>(dz, piece, wt, hidden, hidden, vec, kept.count, w.per_slice,
-                                                                    (float*)(ws + w.dh), (size_t)w.padded * hidden, v0 == 0);
+    hidden_gradient_kernel<T><<<dim3(rt, ht, w.slices.most), 256, 0, s>>>(dz, piece, wt, hidden, hidden, vec, kept.count,
+                                                                         (float*)(ws + w.dh), (size_t)w.padded * hidden, v0 == 0);
     weight_gradient_kernel<T><<<dim3(ht, vt), 256, 0, s>>>(dz, piece, hr, w.ld, hidden, kept.count, (T*)dw);
   }
   const float* slices = (const float*)(ws + w.dh);
   const int32_t* place = (const int32_t*)(ws + w.place);
   constexpr int VEC = 16 / sizeof(T);
   if (hidden % VEC == 0 && aligned16(dh))
-    hidden_gradient_rows_kernel<T, VEC><<<rows, 256, 0, s>>>(slices, w.slices, (size_t)w.padded * hidden, hidden, place, (T*)dh);
+    hidden_gradient_rows_kernel<T, VEC><<<rows, 256, 0, s>>>(slices, kept.count, (size_t)w.padded * hidden, hidden, place, (T*)dh);
   else
-    hidden_gradient_rows_kernel<T, 1><<<rows, 256, 0, s>>>(slices, w.slices, (size_t)w.padded * hidden, hidden, place, (T*)dh);
+    hidden_gradient_rows_kernel<T, 1><<<rows, 256, 0, s>>>(slices, kept.count, (size_t)w.padded * hidden, hidden, place, (T*)dh);
   return launched();
 }
 

@@ -33,7 +33,7 @@ struct Product {
   int64_t lda, ldb;
   int a_n, b_n;                  // rows of a, b in memory (k-strided: k that may be read)
   int tiles_i, tiles_j;          // tiles_i: upper bound where the count of kept rows decides
-  int k, per_slice, slices;      // k = 0: the kept rows
+  int k, slices;                 // k = 0: the kept rows; slices: of k, upper bound
   int group;                     // row tiles that an XCD takes together
   KeptRows kept;
   // logits
@@ -59,7 +59,8 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Product P) {
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, wm = wave >> 1, wn = wave & 1;
   const int kept = __builtin_amdgcn_readfirstlane(*P.kept.count);
   // tiles that have work, numbered so that an XCD (workgroups are dealt to the 8 of them in turn) takes a compact block of one slice
-  const int ti = EPI == EPI_OUT ? P.tiles_i : min(P.tiles_i, (kept + 64 * MB - 1) / (64 * MB)), tiles = ti * P.tiles_j, total = tiles * P.slices;
+  const int ti = EPI == EPI_OUT ? P.tiles_i : min(P.tiles_i, (kept + 64 * MB - 1) / (64 * MB)), tiles = ti * P.tiles_j;
+  const int slices = EPI == EPI_SLICE ? __builtin_amdgcn_readfirstlane(P.kept.count[1]) : 1, total = tiles * slices;
   if ((int)blockIdx.x >= total) return;
   int i0, j0, z;
   {
@@ -71,8 +72,8 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Product P) {
     j0 = __builtin_amdgcn_readfirstlane(in / gm) * BN;
     z = __builtin_amdgcn_readfirstlane(z);
   }
-  const int k_all = EPI == EPI_OUT ? kept : P.k, k_lo = z * P.per_slice, k_hi = min(k_all, k_lo + P.per_slice);
-  const int c0 = k_lo >> 5, c1 = (k_hi + 31) >> 5;      // per_slice is a multiple of 32
+  const int k_all = EPI == EPI_OUT ? kept : P.k, per_slice = EPI == EPI_SLICE ? __builtin_amdgcn_readfirstlane(P.kept.count[2]) : k_all;
+  const int k_lo = z * per_slice, c0 = k_lo >> 5, c1 = (min(k_all, k_lo + per_slice) + 31) >> 5;
   // operands behind these descriptors: what is read past their end arrives as zeros
   const u32x4 ra = TA ? buffer_rsrc(P.a + i0, (unsigned)(((int64_t)P.a_n * P.lda - i0) * 2))
                       : buffer_rsrc(P.a + (int64_t)i0 * P.lda, (unsigned)((int64_t)min(P.a_n - i0, 64 * MB) * P.lda * 2));
@@ -341,19 +342,7 @@ bool token_logprob_takes_mfma(int64_t padded, int ld, int hidden, int width, con
          (int64_t)std::max(width, 256) * hidden * 2 < most / 2;
 }
 
-int token_logprob_slices(int rows, int hidden, int width) {
-  // us: a round of tiles on 256 CUs takes what its k take (0.5 us per 32 k; 128-row tiles 0.3) and 3 to begin and end; a slice's
-  // sums are written and read once
-  const int mb = row_blocks(rows);
-  const int64_t tiles = (int64_t)((rows + 64 * mb - 1) / (64 * mb)) * ((hidden + BN - 1) / BN);
-  double best = 1e30;
-  int slices = 1;
-  for (int s = 1; s <= 32 && (s == 1 || width / s >= 256); s++) {
-    const double t = (double)((tiles * s + 255) / 256) * ((double)width / s / 32 * (mb == 4 ? 0.5 : 0.3) + 3) + s * (double)rows * hidden * 8 / 4.8e6;
-    if (t < best) best = t, slices = s;
-  }
-  return slices;
-}
+int token_logprob_tile_rows(int rows) { return 64 * row_blocks(rows); }
 
 void launch_logits_strips_mfma(hipStream_t s, const bf16_t* h, int ld, int rows, int64_t padded, const bf16_t* w, int vocab, int hidden,
                                const KeptRows& kept, float inv_t, float2* part, float* zt) {
@@ -362,7 +351,7 @@ void launch_logits_strips_mfma(hipStream_t s, const bf16_t* h, int ld, int rows,
   p.a = h, p.lda = ld, p.a_n = (int)padded;
   p.b = w, p.ldb = hidden, p.b_n = vocab;
   p.tiles_i = (rows + 64 * mb - 1) / (64 * mb), p.tiles_j = (vocab + BN - 1) / BN;
-  p.k = (int)up(hidden, 32), p.per_slice = p.k, p.slices = 1, p.group = 4;
+  p.k = (int)up(hidden, 32), p.slices = 1, p.group = 4;
   p.kept = kept, p.vocab = vocab, p.v0 = 0, p.scale = (float)(1.4426950408889634 * inv_t), p.inv_t = inv_t;
   p.part = part, p.padded = (int)padded, p.zt = zt;
   if (mb == 4) go<false, false, 4, 4, EPI_STRIP>(p, s);
@@ -376,21 +365,21 @@ void launch_logits_gradient_mfma(hipStream_t s, const bf16_t* h, int ld, int row
   p.a = h, p.lda = ld, p.a_n = (int)padded;
   p.b = w + (int64_t)piece.v0 * hidden, p.ldb = hidden, p.b_n = vocab - piece.v0;
   p.tiles_i = (rows + 64 * mb - 1) / (64 * mb), p.tiles_j = (piece.width + BN - 1) / BN;
-  p.k = (int)up(hidden, 32), p.per_slice = p.k, p.slices = 1, p.group = 4;
+  p.k = (int)up(hidden, 32), p.slices = 1, p.group = 4;
   p.kept = kept, p.vocab = vocab, p.v0 = piece.v0, p.scale = (float)(1.4426950408889634 * inv_t), p.inv_t = inv_t;
-  p.out = dz, p.ldo = piece.ld, p.out_rows = (int)padded, p.out_cols = piece.ld;
+  p.out = dz, p.ldo = piece.ld, p.out_rows = (int)padded, p.out_cols = (int)up(piece.width, BN);
   if (mb == 4) go<false, false, 4, 4, EPI_DZ>(p, s);
   else go<false, false, 2, 6, EPI_DZ>(p, s);
 }
 
 void launch_hidden_gradient_mfma(hipStream_t s, const bf16_t* dz, const VocabPiece& piece, int rows, int64_t padded, const bf16_t* w, int vocab,
-                                 int hidden, const KeptRows& kept, int slices, int per_slice, float* dh, size_t slice_stride, bool first) {
+                                 int hidden, const KeptRows& kept, int most_slices, float* dh, size_t slice_stride, bool first) {
   Product p{};
   const int mb = row_blocks(rows);
   p.a = dz, p.lda = piece.ld, p.a_n = (int)padded;
   p.b = w + (int64_t)piece.v0 * hidden, p.ldb = hidden, p.b_n = std::min(piece.ld, vocab - piece.v0);
   p.tiles_i = (rows + 64 * mb - 1) / (64 * mb), p.tiles_j = (hidden + BN - 1) / BN;
-  p.k = piece.width, p.per_slice = per_slice, p.slices = slices, p.group = 4;
+  p.k = piece.width, p.slices = most_slices, p.group = 4;
   p.kept = kept, p.slice = dh, p.slice_stride = slice_stride, p.ldo = hidden, p.out_cols = hidden, p.first = first;
   if (mb == 4) go<false, true, 4, 4, EPI_SLICE>(p, s);
   else go<false, true, 2, 6, EPI_SLICE>(p, s);
@@ -402,7 +391,7 @@ void launch_weight_gradient_mfma(hipStream_t s, const bf16_t* dz, const VocabPie
   p.a = dz, p.lda = piece.ld, p.a_n = (int)padded;
   p.b = h, p.ldb = ld, p.b_n = (int)padded;
   p.tiles_i = (piece.width + 255) / 256, p.tiles_j = (hidden + BN - 1) / BN;
-  p.k = 0, p.per_slice = 1 << 30, p.slices = 1, p.group = 4;
+  p.k = 0, p.slices = 1, p.group = 4;
   p.kept = kept, p.out = dw + (int64_t)piece.v0 * hidden, p.ldo = hidden, p.out_rows = piece.width, p.out_cols = hidden;
   go<true, true, 4, 4, EPI_OUT>(p, s);
 }

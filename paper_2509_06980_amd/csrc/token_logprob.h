@@ -2,9 +2,25 @@
 #pragma once
 #include "policy_common.h"
 
+// K-slices of the product dz W: the device chooses them, since it alone knows how many rows are kept.
+struct SliceRule {
+  int rows, tiles_j, width, most;      // rows of a tile, tiles along hidden, vocabulary of a piece, slices that there is room for
+  float chunk_us, slice_us;            // time of a tile's 32 k; of writing and reading a slice's sums of one row
+};
+// The number of slices that ends first: a round of tiles on 256 CUs takes what its k take and 6 us to begin and end.
+static __device__ __forceinline__ int choose_slices(const SliceRule& r, int kept) {
+  const int tiles = (kept + r.rows - 1) / r.rows * r.tiles_j;
+  float best = 3e38f;
+  int slices = 1;
+  for (int s = 1; s <= r.most; s++) {
+    const float t = (float)((tiles * s + 255) / 256) * ((float)r.width / (float)(32 * s) * r.chunk_us + 6.f) + (float)s * (float)kept * r.slice_us;
+    if (t < best) best = t, slices = s;
+  }
+  return slices;
+}
 // The rows that take part are gathered to the front; how many there are only the device knows.
 struct KeptRows {
-  const int32_t* count;      // kept rows
+  const int32_t* count;      // kept rows; backward also [1]: K-slices of dz W, [2]: vocabulary of one (multiple of 64)
   const int32_t* target;     // [rows padded] target of a kept row, -1 in the padding
   const float* lse;          // backward: log-sum-exp of a kept row
   const float* g;            // backward: gradient of its log-prob / temperature, 0 in the padding
@@ -24,9 +40,8 @@ void launch_logits_strips_mfma(hipStream_t s, const bf16_t* h, int ld, int rows,
                                const KeptRows& kept, float inv_t, float2* part, float* zt);
 void launch_logits_gradient_mfma(hipStream_t s, const bf16_t* h, int ld, int rows, int64_t padded, const bf16_t* w, int vocab, int hidden,
                                  const KeptRows& kept, float inv_t, const VocabPiece& piece, bf16_t* dz);
-// K-slices of dz W that suit `rows` rows
-int token_logprob_slices(int rows, int hidden, int width);
+int token_logprob_tile_rows(int rows);      // rows of a tile
 void launch_hidden_gradient_mfma(hipStream_t s, const bf16_t* dz, const VocabPiece& piece, int rows, int64_t padded, const bf16_t* w, int vocab,
-                                 int hidden, const KeptRows& kept, int slices, int per_slice, float* dh, size_t slice_stride, bool first);
+                                 int hidden, const KeptRows& kept, int most_slices, float* dh, size_t slice_stride, bool first);
 void launch_weight_gradient_mfma(hipStream_t s, const bf16_t* dz, const VocabPiece& piece, const bf16_t* h, int ld, int64_t padded, int hidden,
                                  const KeptRows& kept, bf16_t* dw);
