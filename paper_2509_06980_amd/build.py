@@ -17,6 +17,7 @@ SOURCES = {
     "kernels_objective.hip": [],
     "kernels_rows.hip": [],
     "kernels_packed_attention.hip": [],
+    "kernels_packed_attention_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "kernels_token_logprob.hip": [],
     "kernels_token_logprob_mfma.hip": [],
     "engine.hip": [],

@@ -304,6 +304,8 @@ extern "C" int rl_attention_forward(const void* d_q, int64_t q_token_stride, int
   if (dtype == RL_DTYPE_F32) {
     if (head_dim <= 64) forward<float, 64>(s, p, d_q, d_k, d_v, d_o, d_lse);
     else forward<float, 128>(s, p, d_q, d_k, d_v, d_o, d_lse);
+  } else if (attention_takes_mfma(p, d_q, d_k, d_v, d_o, nullptr)) {
+    launch_attention_mfma_forward(s, p, (const bf16_t*)d_q, (const bf16_t*)d_k, (const bf16_t*)d_v, (bf16_t*)d_o, d_lse);
   } else {
     if (head_dim <= 64) forward<bf16_t, 64>(s, p, d_q, d_k, d_v, d_o, d_lse);
     else forward<bf16_t, 128>(s, p, d_q, d_k, d_v, d_o, d_lse);
@@ -336,6 +338,9 @@ extern "C" int rl_attention_backward(const void* d_do, const void* d_q, int64_t 
   if (dtype == RL_DTYPE_F32) {
     if (head_dim <= 64) RL_GO(float, 64);
     else RL_GO(float, 128);
+  } else if (attention_takes_mfma(p, d_q, d_k, d_v, d_o, d_do) && aligned16(d_dq) && aligned16(d_dk) && aligned16(d_dv)) {
+    launch_attention_mfma_backward(s, p, (const bf16_t*)d_do, (const bf16_t*)d_q, (const bf16_t*)d_k, (const bf16_t*)d_v, (const bf16_t*)d_o,
+                                   d_lse, (bf16_t*)d_dq, (bf16_t*)d_dk, (bf16_t*)d_dv, delta);
   } else {
     if (head_dim <= 64) RL_GO(bf16_t, 64);
     else RL_GO(bf16_t, 128);

@@ -1,0 +1,621 @@
+// Attention over packed sequences in bf16 on matrix instructions, forward and backward.
+#include <atomic>
+#include <type_traits>
+#include <utility>
+
+#include "lds_load.h"
+#include "packed_attention.h"
+
+namespace {
+
+// =============================================================================================
+// Three kernels of one shape: a workgroup of four waves owns 128 rows of one side (queries: forward and dq; keys: dk and dv), a wave 32
+// of them as columns of its 32x32x16 products, their operands in registers.  The other side streams through LDS, 64 rows a
+// stage, two stages, straight from memory, and serves as row operand:
+//   forward   z^T = K Q^T,  o^T += V^T p^T
+//   dq        z^T = K Q^T,  dp^T = V dO^T,  dq^T += K^T dz^T
+//   dk, dv    z = Q K^T,  dp = dO V^T,  dv^T += dO^T p,  dk^T += Q^T dz
+// So a lane holds scores of one of its own rows (columns) in registers, and they are the column operand of the next product as they
+// are: the result of a product has rows 8 (e / 4) + 4 (lane / 32) + e % 4 in register e, so registers 8 s .. 8 s + 7 are the 16 k of
+// step s in an order that the row operand, read from LDS by its transposing read, follows.  No score crosses lanes.
+// The backward pass forms the scores twice, in both kernels (14 instead of 10 products' flops), rather than add dq up by atomics in an
+// order that changes, or write the gradients of the scores out.  Bound by the matrix units and, beside them, by the LDS: a
+// wave reads 1 KB per product instruction.
+// LDS: rows of D elements, 16-byte piece p of row r at p ^ f(r).  f moves 16 rows of one piece (read as they lie) to different
+// banks, and the 4 rows x 32 columns of a transposing read as well.
+// =============================================================================================
+constexpr int BM = 128, BN = 64;      // rows owned, rows of a stage
+constexpr int DKV_ROWS = 64;          // keys owned by a workgroup of attention_dkv_kernel
+constexpr int kFar = 0x7fff0000;      // a lane's offset behind every buffer's end: zeros
+constexpr float kLog2e = 1.44269504088896341f;
+
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) float lds_float;
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+
+__device__ __forceinline__ f32x16 mfma(const u32x4& row, const u32x4& col, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, row), __builtin_bit_cast(bf16x8, col), c, 0, 0, 0);
+}
+// The same into the accumulation registers: left to itself the compiler moves sums that live through a loop between the two halves
+// of the register file.  s_nop: it does not know how far back the operands were written.
+__device__ __forceinline__ void accumulate(f32x16& c, const u32x4& row, const u32x4& col) {
+  asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(row), "v"(col));
+}
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int e = 0; e < 16; e++) z[e] = 0.f;
+  return z;
+}
+
+// f(0), f(1), ... f(N - 1) with the numbers as types
+template <int... I, typename F>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) {
+  each_of(std::make_integer_sequence<int, N>(), f);
+}
+
+// Tiles of 64 rows of a tensor on their way into LDS.  The descriptor ends with the sequence's last row: rows behind it are zeros.
+template <int D>
+struct Stream {
+  static constexpr int N = D / 32;                 // 1 KB loads of a wave per tile
+  u32x4 rsrc;
+  int off[N];
+  unsigned step;
+  __device__ __forceinline__ void init(const bf16_t* p, int64_t stride, int len, int d, int wave, int lane) {
+    rsrc = buffer_rsrc(p, (unsigned)(((int64_t)(len - 1) * stride + d) * 2));
+    step = (unsigned)stride * (BN * 2);
+    constexpr int PIECES = D / 8, ROWS = 64 / PIECES;      // of a row; of a load
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+      const int r = (j * 4 + wave) * ROWS + lane / PIECES, p8 = (lane % PIECES) ^ swizzle(r);
+      off[j] = p8 * 8 < d ? (int)(r * stride * 2) + p8 * 16 : kFar;
+    }
+    asm volatile("s_nop 4" ::: "memory");      // scalars from vector instructions, read by the loads
+  }
+  static __device__ __forceinline__ int swizzle(int r) {
+    return D == 128 ? ((r & 3) << 2) | (r >> 2 & 3) : ((r >> 1 & 1) << 2) | (r >> 2 & 3);
+  }
+  __device__ __forceinline__ void load(int tile, unsigned lds, int wave) const {
+#pragma unroll
+    for (int j = 0; j < N; j++) load_to_lds(lds + (unsigned)(j * 4 + wave) * 1024u, off[j], rsrc, (unsigned)tile * step);
+  }
+};
+
+// Lane parts of the reads from a tile.
+template <int D>
+struct Reads {
+  lds_char* lds;
+  int row, tr;
+  __device__ __forceinline__ Reads(lds_char* p, int lane) : lds(p) {
+    const int i = lane & 15, h = lane >> 5, w = lane >> 4 & 1;
+    row = (lane & 31) * (D * 2) + ((h ^ Stream<D>::swizzle(lane & 31)) << 4);
+    const int f = D == 128 ? (i >> 2) << 2 : (i >> 3 & 1) << 2;
+    tr = (4 * h + (i >> 2)) * (D * 2) + ((f | ((2 * w + (i >> 1 & 1)) ^ h)) << 4) + ((i & 1) << 3);
+  }
+  // 32 rows from row 32 x on, k = columns 16 s .. + 15
+  __device__ __forceinline__ u32x4 rows(int at, int x, int s) const {
+    return *(lds_u32x4*)(lds + at + x * 32 * (D * 2) + (row ^ (s << 5)));
+  }
+  // rows = columns 32 b .. + 31, k = rows 32 x + 16 s .. + 15 in the order of a result's registers
+  __device__ __forceinline__ u32x4 columns(int at, int x, int s, int b) const {
+    const int base = at + (32 * x + 16 * s) * (D * 2), a = tr ^ (b << 6);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + base + a));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + base + 8 * (D * 2) + (a ^ 32)));
+    return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+// column operand of a wave's 32 rows: row lane % 32, columns 16 s + 8 (lane / 32) .. + 7
+template <int D>
+__device__ __forceinline__ void own_rows(const bf16_t* p, int64_t stride, int row, int len, int d, int lane, u32x4 (&q)[D / 16]) {
+#pragma unroll
+  for (int s = 0; s < D / 16; s++) {
+    const int c = 16 * s + 8 * (lane >> 5);
+    const bool in = row < len && c < d;
+    q[s] = *(const u32x4*)(in ? p + (int64_t)row * stride + c : p);      // len >= 1: no branch around a load
+    if (!in) q[s] = u32x4{0, 0, 0, 0};
+  }
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+  const bf16x2 v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+// registers 8 s .. 8 s + 7 of a result as the column operand of step s
+__device__ __forceinline__ u32x4 as_operand(const f32x16& v, int s) {
+  return u32x4{pack2(v[8 * s], v[8 * s + 1]), pack2(v[8 * s + 2], v[8 * s + 3]), pack2(v[8 * s + 4], v[8 * s + 5]), pack2(v[8 * s + 6], v[8 * s + 7])};
+}
+// row (of the streamed side) of register e
+__device__ __forceinline__ int row_of(int e, int lane) { return 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3); }
+// a wave's result^T [D x 32 rows] to memory, times f; lane's row at p
+template <int D>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float f, bf16_t* p, int d, int lane) {
+#pragma unroll
+  for (int b = 0; b < D / 32; b++)
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+      const int c = 32 * b + 8 * q + 4 * (lane >> 5);
+      if (c < d) *(uint2*)(p + c) = make_uint2(pack2(acc[b][4 * q] * f, acc[b][4 * q + 1] * f), pack2(acc[b][4 * q + 2] * f, acc[b][4 * q + 3] * f));
+    }
+}
+
+// What a workgroup of the query side works on.
+struct QuerySide {
+  PackedTile t;
+  int h, hk, k0, lk, shift, last;      // last: keys [0, last) are seen by some row of the tile
+};
+__device__ __forceinline__ bool query_side(const PackedShape& p, QuerySide& w) {
+  // KV heads fastest, so workgroups on one XCD share keys; row tiles from the last to the first: causal ones begin with the longest
+  const int id = blockIdx.x, n = packed_tiles(p.total_q, p.n_seq, BM);
+  w.hk = id % p.nkv;
+  w.h = w.hk * (p.nq / p.nkv) + id / p.nkv % (p.nq / p.nkv);
+  w.t = packed_tile(p.cu_q, p.n_seq, p.total_q, BM, n - 1 - id / p.nq);
+  if (w.t.row0 >= w.t.len) return false;
+  w.k0 = packed_bound(p.cu_k, w.t.seq, p.total_k);
+  w.lk = max(packed_bound(p.cu_k, w.t.seq + 1, p.total_k) - w.k0, 0);
+  w.shift = w.lk - w.t.len;
+  w.last = p.causal ? min(w.lk, max(min(w.t.row0 + BM, w.t.len) + w.shift, 0)) : w.lk;
+  return true;
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void attention_forward_kernel(PackedShape p, const bf16_t* __restrict__ q, const bf16_t* __restrict__ k,
+                                                                   const bf16_t* __restrict__ v, bf16_t* __restrict__ o,
+                                                                   float* __restrict__ lse) {
+  constexpr int TILE = BN * D * 2, STAGE = 2 * TILE;
+  extern __shared__ u32x4 smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  QuerySide w;
+  if (!query_side(p, w)) return;
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+  const Reads<D> lds((lds_char*)(__attribute__((address_space(3))) void*)smem, lane);
+  const int mine = w.t.row0 + wave * 32 + (lane & 31);      // lane's query
+  u32x4 qr[D / 16];
+  own_rows<D>(q + (int64_t)w.t.first * p.qt + (int64_t)w.h * p.qh, p.qt, mine, w.t.len, p.d, lane, qr);
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int b = 0; b < D / 32; b++) acc[b] = zero16();
+  float ref = -INFINITY, sum = 0.f;      // ref: log2 units; sum of this half's terms
+  const float c = p.scale * kLog2e;
+  const int seen = p.causal ? min(w.lk, mine + w.shift + 1) : w.lk;             // lane's query sees the keys [0, seen)
+  const int row_a = w.t.row0 + wave * 32, row_b = min(row_a + 32, w.t.len);     // wave's queries
+  const int all = row_a >= w.t.len ? 0 : p.causal ? min(w.lk, row_a + w.shift + 1) : w.lk;      // keys that all of them see
+  const int some = row_a >= w.t.len ? 0 : p.causal ? min(w.lk, row_b + w.shift) : w.lk;         // ... that one sees
+  const int tiles = (w.last + BN - 1) / BN;
+  Stream<D> ks, vs;
+  if (tiles > 0) {
+    ks.init(k + (int64_t)w.k0 * p.kt + (int64_t)w.hk * p.kh, p.kt, w.lk, p.d, wave, lane);
+    vs.init(v + (int64_t)w.k0 * p.vt + (int64_t)w.hk * p.vh, p.vt, w.lk, p.d, wave, lane);
+    ks.load(0, lds0, wave);
+    vs.load(0, lds0 + TILE, wave);
+  }
+  auto tile = [&](int j0, int at, auto masked) {
+    f32x16 z[2];
+#pragma unroll
+    for (int x = 0; x < 2; x++) {
+      z[x] = zero16();
+#pragma unroll
+      for (int s = 0; s < D / 16; s++) z[x] = mfma(lds.rows(at, x, s), qr[s], z[x]);
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        z[x][e] *= c;
+        if (decltype(masked)::value && j0 + 32 * x + row_of(e, lane) >= seen) z[x][e] = -INFINITY;
+        top = fmaxf(top, z[x][e]);
+      }
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    // the reference of the exponents moves only where a term would exceed 2^8: rounding is relative, and sums stay far from overflow
+    if (__any(top > ref + 8.f)) {
+      const float now = fmaxf(ref, top), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - now);
+      ref = now;
+      sum *= f;
+#pragma unroll
+      for (int b = 0; b < D / 32; b++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) acc[b][e] *= f;
+    }
+    const float r = ref == -INFINITY ? 0.f : ref;      // nothing seen yet: e^-inf = 0
+#pragma unroll
+    for (int x = 0; x < 2; x++) {
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        z[x][e] = __builtin_amdgcn_exp2f(z[x][e] - r);
+        sum += z[x][e];
+      }
+#pragma unroll
+      for (int s = 0; s < 2; s++) {
+        const u32x4 pr = as_operand(z[x], s);      // probabilities rounded to bf16; their sum is not
+#pragma unroll
+        for (int b = 0; b < D / 32; b++) acc[b] = mfma(lds.columns(at + TILE, x, s, b), pr, acc[b]);
+      }
+    }
+  };
+  for (int t = 0; t < tiles; t++) {
+    const int at = (t & 1) * STAGE;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();      // tile t has landed, the other stage is read out
+    if (t + 1 < tiles) {
+      ks.load(t + 1, lds0 + (unsigned)(STAGE - at), wave);
+      vs.load(t + 1, lds0 + (unsigned)(STAGE - at + TILE), wave);
+    }
+    const int j0 = t * BN;
+    if (j0 + BN <= all) tile(j0, at, std::false_type());
+    else if (j0 < some) tile(j0, at, std::true_type());
+  }
+  sum += __shfl_xor(sum, 32, 64);
+  if (mine < w.t.len) {
+    const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;      // no key: zeros; no number stays so
+    store_rows<D>(acc, inv, o + (int64_t)(w.t.first + mine) * p.ot + (int64_t)w.h * p.oh, p.d, lane);
+    if (lane < 32) lse[(size_t)w.h * p.total_q + w.t.first + mine] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * (1.f / kLog2e);
+  }
+}
+
+// dq, and delta = rowsum(dO o), which the other kernel reads
+template <int D>
+__global__ __launch_bounds__(256, 2) void attention_dq_kernel(PackedShape p, const bf16_t* __restrict__ dout, const bf16_t* __restrict__ q,
+                                                              const bf16_t* __restrict__ k, const bf16_t* __restrict__ v,
+                                                              const bf16_t* __restrict__ o, const float* __restrict__ lse,
+                                                              bf16_t* __restrict__ dq, float* __restrict__ delta) {
+  constexpr int TILE = BN * D * 2, STAGE = 2 * TILE;
+  extern __shared__ u32x4 smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  QuerySide w;
+  if (!query_side(p, w)) return;
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+  const Reads<D> lds((lds_char*)(__attribute__((address_space(3))) void*)smem, lane);
+  const int mine = w.t.row0 + wave * 32 + (lane & 31);
+  u32x4 qr[D / 16], gr[D / 16];
+  float dl = 0.f;
+  own_rows<D>(dout + (int64_t)w.t.first * p.ot + (int64_t)w.h * p.oh, p.ot, mine, w.t.len, p.d, lane, gr);
+  own_rows<D>(o + (int64_t)w.t.first * p.ot + (int64_t)w.h * p.oh, p.ot, mine, w.t.len, p.d, lane, qr);
+#pragma unroll
+  for (int s = 0; s < D / 16; s++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      dl = fmaf(bf2f((bf16_t)(gr[s][i] & 0xffffu)), bf2f((bf16_t)(qr[s][i] & 0xffffu)), dl);
+      dl = fmaf(bf2f((bf16_t)(gr[s][i] >> 16)), bf2f((bf16_t)(qr[s][i] >> 16)), dl);
+    }
+  dl += __shfl_xor(dl, 32, 64);
+  const size_t stat = (size_t)w.h * p.total_q + w.t.first + mine;
+  float l = 0.f;
+  if (mine < w.t.len) {
+    if (lane < 32) delta[stat] = dl;
+    l = lse[stat] * kLog2e;
+  }
+  own_rows<D>(q + (int64_t)w.t.first * p.qt + (int64_t)w.h * p.qh, p.qt, mine, w.t.len, p.d, lane, qr);
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int b = 0; b < D / 32; b++) acc[b] = zero16();
+  const float c = p.scale * kLog2e;
+  const int seen = p.causal ? min(w.lk, mine + w.shift + 1) : w.lk;
+  const int row_a = w.t.row0 + wave * 32, row_b = min(row_a + 32, w.t.len);
+  const int all = row_a >= w.t.len ? 0 : p.causal ? min(w.lk, row_a + w.shift + 1) : w.lk;
+  const int some = row_a >= w.t.len ? 0 : p.causal ? min(w.lk, row_b + w.shift) : w.lk;
+  const int tiles = (w.last + BN - 1) / BN;
+  Stream<D> ks, vs;
+  if (tiles > 0) {
+    ks.init(k + (int64_t)w.k0 * p.kt + (int64_t)w.hk * p.kh, p.kt, w.lk, p.d, wave, lane);
+    vs.init(v + (int64_t)w.k0 * p.vt + (int64_t)w.hk * p.vh, p.vt, w.lk, p.d, wave, lane);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // plain loads above are done: none is counted with those into LDS
+    ks.load(0, lds0, wave);
+    vs.load(0, lds0 + TILE, wave);
+  }
+  // 32 keys, in slots of one row operand, read three slots ahead, its product, and a share of the arithmetic on the scores
+  constexpr int S = D / 16, SLOTS = 3 * S, AHEAD = 3, PER = 16 / S;
+  auto tile = [&](int j0, int at, int x, bool masked) {
+    u32x4 a[4], dz[2];
+    f32x16 z, dp;
+    auto read = [&](auto slot) {
+      constexpr int n = decltype(slot)::value, m = n % S;
+      if constexpr (n < S) return lds.rows(at, x, n);
+      else if constexpr (n < 2 * S) return lds.rows(at + TILE, x, m);
+      else return lds.columns(at, x, m / (D / 32), m % (D / 32));
+    };
+    each<AHEAD>([&](auto n) { a[decltype(n)::value] = read(n); });
+#pragma unroll
+    for (int e = 0; e < 16; e++) z[e] = 0.f, dp[e] = -dl;
+    each<SLOTS>([&](auto slot) {
+      constexpr int n = decltype(slot)::value, m = n % S, later = n + AHEAD;
+      if constexpr (later < SLOTS) a[later & 3] = read(std::integral_constant<int, later>());
+      const u32x4 row = a[n & 3];
+      if constexpr (n < S) {                   // scores
+        z = mfma(row, qr[n], z);
+      } else if constexpr (n < 2 * S) {        // gradients of the probabilities, less delta; probabilities
+        dp = mfma(row, gr[m], dp);
+#pragma unroll
+        for (int e = m * PER; e < (m + 1) * PER; e++) z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], c, -l));
+        if constexpr (m == S - 1) {
+          if (masked) {
+#pragma unroll
+            for (int e = 0; e < 16; e++)
+              if (j0 + 32 * x + row_of(e, lane) >= seen) z[e] = 0.f;
+          }
+#pragma unroll
+          for (int e = 0; e < 16; e++) dp[e] *= z[e];
+          dz[0] = as_operand(dp, 0);
+          dz[1] = as_operand(dp, 1);
+        }
+      } else {
+        acc[m % (D / 32)] = mfma(row, dz[m / (D / 32)], acc[m % (D / 32)]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  for (int t = 0; t < tiles; t++) {
+    const int at = (t & 1) * STAGE;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    if (t + 1 < tiles) {
+      ks.load(t + 1, lds0 + (unsigned)(STAGE - at), wave);
+      vs.load(t + 1, lds0 + (unsigned)(STAGE - at + TILE), wave);
+    }
+    const int j0 = t * BN;
+    if (j0 < some) {
+      tile(j0, at, 0, j0 + 32 > all);
+      tile(j0, at, 1, j0 + BN > all);
+    }
+  }
+  if (mine < w.t.len) store_rows<D>(acc, p.scale, dq + (int64_t)(w.t.first + mine) * p.ot + (int64_t)w.h * p.oh, p.d, lane);
+}
+
+// dk and dv of 64 keys of one KV head.  Eight waves: two blocks of 32 keys x four streams, a stream takes every fourth (query head of
+// the group, 32 queries) that sees the keys; the streams' sums are added up in LDS at the end, in their order.  A wave has its keys as
+// operand and both sums in registers (128 of them, the accumulation half of the file), the values lie in LDS: with them two waves a
+// SIMD would not fit.  A step is laid out by hand in slots of one row operand, read two slots ahead, its product, and a share of
+// the arithmetic on the scores of the products before.
+template <int D>
+__global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, const bf16_t* __restrict__ dout, const bf16_t* __restrict__ q,
+                                                               const bf16_t* __restrict__ k, const bf16_t* __restrict__ v,
+                                                               const float* __restrict__ lse, const float* __restrict__ delta,
+                                                               bf16_t* __restrict__ dk, bf16_t* __restrict__ dv) {
+  constexpr int TILE = 32 * D * 2, STAGE = 2 * TILE + 256;      // of a stream: queries, dO, then lse and delta of the queries
+  constexpr int S = D / 16, SLOTS = 4 * S, AHEAD = 2, PER = 16 / S;
+  extern __shared__ u32x4 smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, block = wave & 1, stream = wave >> 1;
+  const int hk = blockIdx.x % p.nkv, group = p.nq / p.nkv;
+  const PackedTile t = packed_tile(p.cu_k, p.n_seq, p.total_k, DKV_ROWS, blockIdx.x / p.nkv);
+  if (t.row0 >= t.len) return;
+  const int q0 = packed_bound(p.cu_q, t.seq, p.total_q), lq = max(packed_bound(p.cu_q, t.seq + 1, p.total_q) - q0, 0);
+  const int shift = t.len - lq;
+  lds_char* const lds_base = (lds_char*)(__attribute__((address_space(3))) void*)smem;
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+  const int own = stream * 2 * STAGE;      // of the stream's two stages
+  lds_char *const base = lds_base + own, *const value_base = lds_base + 8 * STAGE + block * TILE;
+  f32x16 ak[D / 32], av[D / 32];
+#pragma unroll
+  for (int b = 0; b < D / 32; b++) ak[b] = av[b] = zero16();
+  {
+    Stream<D> vs;      // the values: 64 rows by the first four waves
+    vs.init(v + (int64_t)t.first * p.vt + (int64_t)hk * p.vh, p.vt, t.len, p.d, wave & 3, lane);
+    if (wave < 4) vs.load(t.row0 / DKV_ROWS, lds0 + 8 * STAGE, wave);
+  }
+  const int first = p.causal ? max(t.row0 - shift, 0) / 32 : 0, per_head = max((lq + 31) / 32 - first, 0);
+  const int rounds = (per_head * group + 3) / 4;
+  const int mine = t.row0 + 32 * block + (lane & 31);                                   // lane's key
+  const int seen = p.causal ? max(mine - shift, 0) : 0;                                 // queries [seen, lq) see it
+  const int all = p.causal ? max(t.row0 + 32 * block + 31 - shift, 0) : 0;              // queries from here on see all keys of the wave
+  u32x4 kr[S];
+  own_rows<D>(k + (int64_t)t.first * p.kt + (int64_t)hk * p.kh, p.kt, mine, t.len, p.d, lane, kr);
+  const float c2 = p.scale * kLog2e;
+  // The waves of a stream share its loads: the first takes the queries, the second dO; 1 KB a load, ROWS rows.  A scalar offset never
+  // leaves its buffer; a stream without work reads nothing but zeros.
+  constexpr int ROWS = 512 / D, LOADS = 32 / ROWS;
+  const bf16_t* const from = block ? dout : q;
+  const int64_t ts = block ? p.ot : p.qt, hs = block ? p.oh : p.qh;
+  const float* const stats_from = block ? delta : lse;
+  int off[4];
+#pragma unroll
+  for (int j = 0; j < 4; j++) {
+    const int r = lane / (D / 8), p8 = (lane % (D / 8)) ^ Stream<D>::swizzle(j * ROWS + r);
+    off[j] = p8 * 8 < p.d ? (int)(r * ts * 2) + p8 * 16 : kFar;
+  }
+  const unsigned full = (unsigned)(((int64_t)(lq - 1) * ts + p.d) * 2);
+  int item = stream, h = hk * group;      // next tile of the current head
+  u32x4 rsrc;
+  unsigned bytes;
+  float stat;
+  auto load = [&](int at) {
+    while (h < (hk + 1) * group && item >= per_head) {
+      item -= per_head;
+      h++;
+    }
+    const bool some = h < (hk + 1) * group;
+    bytes = some ? full : 0u;
+    rsrc = buffer_rsrc(from + (int64_t)q0 * ts + (int64_t)h * hs, bytes);
+    asm volatile("s_nop 4" ::: "memory");      // scalars from vector instructions, read by the loads below
+    const int i = first + item;
+#pragma unroll
+    for (int j = 0; j < LOADS; j++)
+      load_to_lds(lds0 + (unsigned)(own + at + block * TILE + j * 1024), off[j & 3], rsrc, min((unsigned)(i * 32 + j * ROWS) * (unsigned)ts * 2u, bytes));
+    // queries without a key and rows behind the end: probability 2^-inf.  delta enters with its sign changed
+    const int row = i * 32 + (lane & 31);
+    const bool in = some && row < lq;
+    float x = in ? stats_from[(size_t)h * p.total_q + q0 + row] : 0.f;
+    stat = block ? -x : !in || x == -INFINITY ? INFINITY : x * kLog2e;
+  };
+  auto put = [&](int at) {
+    if (lane < 32) *((lds_float*)(lds_base + own + at + 2 * TILE) + 32 * block + lane) = stat;
+  };
+  auto step = [&](int i0, int at) {
+    // addresses are formed anew in every step: kept, they would not fit beside the rest
+    Reads<D> lds(base, lane), values(value_base, lane);
+    asm volatile("" : "+v"(lds.row), "+v"(lds.tr), "+v"(values.row));
+    u32x4 a[3], vr[2], pr[2], dz[2];
+    f32x16 z, dp;
+    f32x4 l[2];      // lse of the queries of register group g, read a group ahead
+    const lds_float* stats = (const lds_float*)(lds_base + own + at + 2 * TILE) + 4 * (lane >> 5);
+    auto read = [&](auto slot) {      // row operand of a slot
+      constexpr int n = decltype(slot)::value, m = n % S;
+      if constexpr (n < S) return lds.rows(at, 0, n);
+      else if constexpr (n < 2 * S) return lds.rows(at + TILE, 0, m);
+      else return lds.columns(n < 3 * S ? at + TILE : at, 0, m / (D / 32), m % (D / 32));
+    };
+    each<AHEAD>([&](auto n) { a[decltype(n)::value] = read(n); });
+    z = zero16();
+    each<SLOTS>([&](auto slot) {
+      constexpr int n = decltype(slot)::value, m = n % S, later = n + AHEAD;
+      if constexpr (later < SLOTS) a[later % 3] = read(std::integral_constant<int, later>());
+      if constexpr (n + 1 >= S && n + 1 < 2 * S) vr[(n + 1) & 1] = values.rows(0, 0, n + 1 - S);
+      const u32x4 x = a[n % 3];
+      if constexpr (n < S) {                   // scores
+        z = mfma(x, kr[n], z);
+        if constexpr (n == S - 2) {
+#pragma unroll
+          for (int g = 0; g < 4; g++) {
+            const f32x4 dl = *(const lds_f32x4*)(stats + 32 + 8 * g);
+#pragma unroll
+            for (int r = 0; r < 4; r++) dp[4 * g + r] = dl[r];
+          }
+          l[0] = *(const lds_f32x4*)stats;
+        }
+      } else if constexpr (n < 2 * S) {        // gradients of the probabilities, less delta; probabilities
+        dp = mfma(x, vr[n & 1], dp);
+        constexpr int g = m * PER / 4;
+        if constexpr (m * PER % 4 == 0 && g < 3) l[(g + 1) & 1] = *(const lds_f32x4*)(stats + 8 * (g + 1));
+#pragma unroll
+        for (int e = m * PER; e < (m + 1) * PER; e++) z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], c2, -l[g & 1][e & 3]));
+        if constexpr (m == S - 1) {
+          if (i0 < all) {      // the diagonal runs through the tile
+#pragma unroll
+            for (int e = 0; e < 16; e++)
+              if (i0 + row_of(e, lane) < seen) z[e] = 0.f;
+          }
+          pr[0] = as_operand(z, 0);
+          pr[1] = as_operand(z, 1);
+        }
+      } else if constexpr (n < 3 * S) {        // dv; gradients of the scores
+        accumulate(av[m % (D / 32)], x, pr[m / (D / 32)]);
+#pragma unroll
+        for (int e = m * PER; e < (m + 1) * PER; e++) dp[e] *= z[e];
+        if constexpr (m == S - 1) {
+          dz[0] = as_operand(dp, 0);
+          dz[1] = as_operand(dp, 1);
+        }
+      } else {                                 // dk
+        accumulate(ak[m % (D / 32)], x, dz[m / (D / 32)]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  if (rounds > 0) {
+    load(0);
+    put(0);
+  }
+  for (int r = 0, at = 0; r < rounds; r++, at = STAGE - at) {
+    const int i0 = (first + item) * 32;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();      // this round's rows have landed, the other stage is read out
+    if (r + 1 < rounds) {
+      item += 4;
+      load(STAGE - at);
+    }
+    step(i0, at);
+    if (r + 1 < rounds) put(STAGE - at);
+  }
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");      // results of the assembly's last products
+  // the streams' sums: [stream][key][D + 4] in LDS; 8 threads add up and store a key
+  constexpr int PITCH = D + 4;
+  lds_float* const sums = (lds_float*)lds_base;
+  auto join = [&](const f32x16 (&acc)[D / 32], float f, bf16_t* out) {
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < D / 32; b++)
+#pragma unroll
+      for (int g = 0; g < 4; g++)
+        *(lds_f32x4*)(sums + (stream * DKV_ROWS + 32 * block + (lane & 31)) * PITCH + 32 * b + 8 * g + 4 * (lane >> 5)) =
+            f32x4{acc[b][4 * g], acc[b][4 * g + 1], acc[b][4 * g + 2], acc[b][4 * g + 3]};
+    __syncthreads();
+    const int key = threadIdx.x >> 3;
+    if (t.row0 + key < t.len) {
+      bf16_t* row = out + (int64_t)(t.first + t.row0 + key) * p.nkv * p.d + (int64_t)hk * p.d;
+#pragma unroll
+      for (int j = 0; j < D / 64; j++) {
+        const int col = (threadIdx.x & 7) * 8 + 64 * j;
+        float y[8];
+#pragma unroll
+        for (int w = 0; w < 4; w++) {
+          const lds_float* part = sums + (w * DKV_ROWS + key) * PITCH + col;
+          const f32x4 lo = *(const lds_f32x4*)part, hi = *(const lds_f32x4*)(part + 4);
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            y[e] = w ? y[e] + lo[e] : lo[e];
+            y[4 + e] = w ? y[4 + e] + hi[e] : hi[e];
+          }
+        }
+        if (col < p.d)
+          *(u32x4*)(row + col) = u32x4{pack2(y[0] * f, y[1] * f), pack2(y[2] * f, y[3] * f), pack2(y[4] * f, y[5] * f), pack2(y[6] * f, y[7] * f)};
+      }
+    }
+  };
+  join(ak, p.scale, dk);
+  join(av, 1.f, dv);
+}
+
+// More than 64 KB of dynamic LDS need an opt-in, once per kernel and device.
+template <typename K>
+void allow_lds(std::atomic<uint64_t>& done, K kernel, int bytes) {
+  int dev = 0;
+  (void)hipGetDevice(&dev);
+  const uint64_t bit = 1ull << (dev & 63);
+  if (done.load(std::memory_order_acquire) & bit) return;
+  (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  done.fetch_or(bit, std::memory_order_release);
+}
+
+template <int D>
+void forward(hipStream_t s, const PackedShape& p, const bf16_t* q, const bf16_t* k, const bf16_t* v, bf16_t* o, float* lse) {
+  static std::atomic<uint64_t> done;
+  const int lds = 4 * BN * D * 2;
+  allow_lds(done, attention_forward_kernel<D>, lds);
+  attention_forward_kernel<D><<<(unsigned)(packed_tiles(p.total_q, p.n_seq, BM) * p.nq), 256, lds, s>>>(p, q, k, v, o, lse);
+}
+template <int D>
+void backward(hipStream_t s, const PackedShape& p, const bf16_t* dout, const bf16_t* q, const bf16_t* k, const bf16_t* v, const bf16_t* o,
+              const float* lse, bf16_t* dq, bf16_t* dk, bf16_t* dv, float* delta) {
+  static std::atomic<uint64_t> done[2];
+  const int lds = 4 * BN * D * 2;
+  if (p.total_q > 0) {
+    allow_lds(done[0], attention_dq_kernel<D>, lds);
+    attention_dq_kernel<D><<<(unsigned)(packed_tiles(p.total_q, p.n_seq, BM) * p.nq), 256, lds, s>>>(p, dout, q, k, v, o, lse, dq, delta);
+  }
+  if (p.total_k > 0) {
+    constexpr int ring = 8 * (2 * 32 * D * 2 + 256) + DKV_ROWS * D * 2, sums = 4 * DKV_ROWS * (D + 4) * 4, bytes = ring > sums ? ring : sums;
+    allow_lds(done[1], attention_dkv_kernel<D>, bytes);
+    attention_dkv_kernel<D><<<(unsigned)(packed_tiles(p.total_k, p.n_seq, DKV_ROWS) * p.nkv), 512, bytes, s>>>(p, dout, q, k, v, lse, delta, dk, dv);
+  }
+}
+
+}  // namespace
+
+bool attention_takes_mfma(const PackedShape& p, const void* q, const void* k, const void* v, const void* o, const void* dout) {
+  // a sequence's rows behind one descriptor with 32-bit offsets; rows that do not overlap, so that the descriptor's end is the
+  // last row's; 16-byte pieces
+  const int64_t most = (1ll << 31) - (1 << 20);
+  auto takes = [&](const void* x, int64_t ts, int64_t hs, int total) {
+    return aligned16(x) && ts % 8 == 0 && hs % 8 == 0 && ts >= p.d && ts * 2 * ((int64_t)total + 2 * BN) < most;
+  };
+  return p.d % 8 == 0 && takes(q, p.qt, p.qh, p.total_q) && takes(k, p.kt, p.kh, p.total_k) && takes(v, p.vt, p.vh, p.total_k) &&
+         takes(o, p.ot, p.oh, p.total_q) && takes(dout, p.ot, p.oh, p.total_q) && (int64_t)packed_tiles(p.total_q, p.n_seq, BM) * p.nq < (1ll << 31) &&
+         (int64_t)packed_tiles(p.total_k, p.n_seq, DKV_ROWS) * p.nkv < (1ll << 31);
+}
+
+void launch_attention_mfma_forward(hipStream_t s, const PackedShape& p, const bf16_t* q, const bf16_t* k, const bf16_t* v, bf16_t* o,
+                                   float* lse) {
+  if (p.d <= 64) forward<64>(s, p, q, k, v, o, lse);
+  else forward<128>(s, p, q, k, v, o, lse);
+}
+void launch_attention_mfma_backward(hipStream_t s, const PackedShape& p, const bf16_t* dout, const bf16_t* q, const bf16_t* k,
+                                    const bf16_t* v, const bf16_t* o, const float* lse, bf16_t* dq, bf16_t* dk, bf16_t* dv,
+                                    float* delta) {
+  if (p.d <= 64) backward<64>(s, p, dout, q, k, v, o, lse, dq, dk, dv, delta);
+  else backward<128>(s, p, dout, q, k, v, o, lse, dq, dk, dv, delta);
+}

@@ -42,8 +42,9 @@ __device__ __forceinline__ PackedTile packed_tile(const int32_t* cu, int n_seq, 
   return t;
 }
 
-// bf16, head sizes up to 128 in multiples of 8, 16-byte aligned rows.
-bool attention_takes_mfma(const PackedShape& p, const void* q, const void* k, const void* v, const void* o);
+// bf16 on matrix instructions: head sizes in multiples of 8, 16-byte aligned rows, nothing beyond 2 GB in one tensor.  o and dout are
+// checked for their alignment alone (null: not in the call).
+bool attention_takes_mfma(const PackedShape& p, const void* q, const void* k, const void* v, const void* o, const void* dout);
 void launch_attention_mfma_forward(hipStream_t s, const PackedShape& p, const bf16_t* q, const bf16_t* k, const bf16_t* v, bf16_t* o,
                                    float* lse);
 void launch_attention_mfma_backward(hipStream_t s, const PackedShape& p, const bf16_t* dout, const bf16_t* q, const bf16_t* k,
