@@ -314,7 +314,7 @@ extern "C" int rl_attention_forward(const void* d_q, int64_t q_token_stride, int
 }
 
 extern "C" int64_t rl_attention_workspace(int32_t total_q, int32_t n_q_heads) {
-  return total_q < 0 || n_q_heads < 1 ? 0 : (int64_t)total_q * n_q_heads * (int64_t)sizeof(float);
+  return total_q < 0 || n_q_heads < 1 ? 0 : (int64_t)total_q * n_q_heads * 2 * (int64_t)sizeof(float);
 }
 
 extern "C" int rl_attention_backward(const void* d_do, const void* d_q, int64_t q_token_stride, int64_t q_head_stride, const void* d_k,

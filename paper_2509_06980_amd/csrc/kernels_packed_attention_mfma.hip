@@ -25,7 +25,7 @@ namespace {
 // banks, and the 4 rows x 32 columns of a transposing read as well.
 // =============================================================================================
 constexpr int BM = 128, BN = 64;      // rows owned, rows of a stage
-constexpr int DKV_ROWS = 64;          // keys owned by a workgroup of attention_dkv_kernel
+constexpr int DKV_ROWS = 128;         // keys owned by a workgroup of attention_dkv_kernel
 constexpr int kFar = 0x7fff0000;      // a lane's offset behind every buffer's end: zeros
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -83,7 +83,7 @@ struct Stream {
   }
   __device__ __forceinline__ void load(int tile, unsigned lds, int wave) const {
 #pragma unroll
-    for (int j = 0; j < N; j++) load_to_lds(lds + (unsigned)(j * 4 + wave) * 1024u, off[j], rsrc, (unsigned)tile * step);
+    for (int j = 0; j < N; j++) load_to_lds(lds + (unsigned)(j * 4 + wave) * 1024u, off[j], rsrc, min((unsigned)tile * step, rsrc[2]));
   }
 };
 
@@ -259,12 +259,13 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(PackedShape p
   }
 }
 
-// dq, and delta = rowsum(dO o), which the other kernel reads
+// dq, and what the other kernel reads of a query: - lse / scale, with which its sums of q.k begin (where it sees no key an infinity that
+// makes the probabilities 0), and - delta = - rowsum(dO o)
 template <int D>
 __global__ __launch_bounds__(256, 2) void attention_dq_kernel(PackedShape p, const bf16_t* __restrict__ dout, const bf16_t* __restrict__ q,
                                                               const bf16_t* __restrict__ k, const bf16_t* __restrict__ v,
                                                               const bf16_t* __restrict__ o, const float* __restrict__ lse,
-                                                              bf16_t* __restrict__ dq, float* __restrict__ delta) {
+                                                              bf16_t* __restrict__ dq, float* __restrict__ stats) {
   constexpr int TILE = BN * D * 2, STAGE = 2 * TILE;
   extern __shared__ u32x4 smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -288,8 +289,12 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(PackedShape p, con
   const size_t stat = (size_t)w.h * p.total_q + w.t.first + mine;
   float l = 0.f;
   if (mine < w.t.len) {
-    if (lane < 32) delta[stat] = dl;
     l = lse[stat] * kLog2e;
+    if (l == -INFINITY) l = INFINITY;
+    if (lane < 32) {
+      stats[stat] = l / -(p.scale * kLog2e);
+      stats[stat + (size_t)p.nq * p.total_q] = -dl;
+    }
   }
   own_rows<D>(q + (int64_t)w.t.first * p.qt + (int64_t)w.h * p.qh, p.qt, mine, w.t.len, p.d, lane, qr);
   f32x16 acc[D / 32];
@@ -367,124 +372,132 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(PackedShape p, con
   if (mine < w.t.len) store_rows<D>(acc, p.scale, dq + (int64_t)(w.t.first + mine) * p.ot + (int64_t)w.h * p.oh, p.d, lane);
 }
 
-// dk and dv of 64 keys of one KV head.  Eight waves: two blocks of 32 keys x four streams, a stream takes every fourth (query head of
-// the group, 32 queries) that sees the keys; the streams' sums are added up in LDS at the end, in their order.  A wave has its keys as
+// dk and dv of 32 BLOCKS keys of one KV head.  Eight waves: BLOCKS blocks of 32 keys x 8 / BLOCKS streams, which take the (query head of
+// the group, 32 queries) that see the keys in turn, through a ring of LDS stages of their own; the streams' sums are added up in LDS at the end, in their order.  A wave has its keys as
 // operand and both sums in registers (128 of them, the accumulation half of the file), the values lie in LDS: with them two waves a
-// SIMD would not fit.  A step is laid out by hand in slots of one row operand, read two slots ahead, its product, and a share of
+// SIMD would not fit.  A step is laid out by hand in slots of one row operand, read three slots ahead, its product, and a share of
 // the arithmetic on the scores of the products before.
-template <int D>
+template <int D, int BLOCKS, int R>
 __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, const bf16_t* __restrict__ dout, const bf16_t* __restrict__ q,
                                                                const bf16_t* __restrict__ k, const bf16_t* __restrict__ v,
-                                                               const float* __restrict__ lse, const float* __restrict__ delta,
-                                                               bf16_t* __restrict__ dk, bf16_t* __restrict__ dv) {
-  constexpr int TILE = 32 * D * 2, STAGE = 2 * TILE + 256;      // of a stream: queries, dO, then lse and delta of the queries
-  constexpr int S = D / 16, SLOTS = 4 * S, AHEAD = 2, PER = 16 / S;
+                                                               const float* __restrict__ query_stats, bf16_t* __restrict__ dk,
+                                                               bf16_t* __restrict__ dv) {
+  constexpr int STREAMS = 8 / BLOCKS, KEYS = 32 * BLOCKS;
+  constexpr int TILE = 32 * D * 2, STAGE = 2 * TILE + 512;      // of a stream: queries, dO, then - lse / scale and - delta of the queries
+  constexpr int S = D / 16, SLOTS = 4 * S, AHEAD = 3, VA = 2, PER = 16 / S;
   extern __shared__ u32x4 smem[];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, block = wave & 1, stream = wave >> 1;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, block = wave % BLOCKS, stream = wave / BLOCKS;
   const int hk = blockIdx.x % p.nkv, group = p.nq / p.nkv;
-  const PackedTile t = packed_tile(p.cu_k, p.n_seq, p.total_k, DKV_ROWS, blockIdx.x / p.nkv);
+  const PackedTile t = packed_tile(p.cu_k, p.n_seq, p.total_k, KEYS, blockIdx.x / p.nkv);
   if (t.row0 >= t.len) return;
   const int q0 = packed_bound(p.cu_q, t.seq, p.total_q), lq = max(packed_bound(p.cu_q, t.seq + 1, p.total_q) - q0, 0);
   const int shift = t.len - lq;
   lds_char* const lds_base = (lds_char*)(__attribute__((address_space(3))) void*)smem;
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
-  const int own = stream * 2 * STAGE;      // of the stream's two stages
-  lds_char *const base = lds_base + own, *const value_base = lds_base + 8 * STAGE + block * TILE;
+  const int own = stream * R * STAGE;      // of the stream's stages
+  lds_char *const base = lds_base + own, *const value_base = lds_base + STREAMS * R * STAGE + block * TILE;
   f32x16 ak[D / 32], av[D / 32];
 #pragma unroll
   for (int b = 0; b < D / 32; b++) ak[b] = av[b] = zero16();
   {
-    Stream<D> vs;      // the values: 64 rows by the first four waves
+    Stream<D> vs;      // the values: 64 rows by four waves
     vs.init(v + (int64_t)t.first * p.vt + (int64_t)hk * p.vh, p.vt, t.len, p.d, wave & 3, lane);
-    if (wave < 4) vs.load(t.row0 / DKV_ROWS, lds0 + 8 * STAGE, wave);
+    if (2 * (wave >> 2) < BLOCKS) vs.load(t.row0 / 64 + (wave >> 2), lds0 + STREAMS * R * STAGE + (unsigned)(wave >> 2) * (2 * TILE), wave & 3);
   }
   const int first = p.causal ? max(t.row0 - shift, 0) / 32 : 0, per_head = max((lq + 31) / 32 - first, 0);
-  const int rounds = (per_head * group + 3) / 4;
+  const int rounds = (per_head * group + STREAMS - 1) / STREAMS;
   const int mine = t.row0 + 32 * block + (lane & 31);                                   // lane's key
-  const int seen = p.causal ? max(mine - shift, 0) : 0;                                 // queries [seen, lq) see it
   const int all = p.causal ? max(t.row0 + 32 * block + 31 - shift, 0) : 0;              // queries from here on see all keys of the wave
   u32x4 kr[S];
   own_rows<D>(k + (int64_t)t.first * p.kt + (int64_t)hk * p.kh, p.kt, mine, t.len, p.d, lane, kr);
   const float c2 = p.scale * kLog2e;
-  // The waves of a stream share its loads: the first takes the queries, the second dO; 1 KB a load, ROWS rows.  A scalar offset never
-  // leaves its buffer; a stream without work reads nothing but zeros.
-  constexpr int ROWS = 512 / D, LOADS = 32 / ROWS;
-  const bf16_t* const from = block ? dout : q;
-  const int64_t ts = block ? p.ot : p.qt, hs = block ? p.oh : p.qh;
-  const float* const stats_from = block ? delta : lse;
-  int off[4];
-#pragma unroll
-  for (int j = 0; j < 4; j++) {
-    const int r = lane / (D / 8), p8 = (lane % (D / 8)) ^ Stream<D>::swizzle(j * ROWS + r);
-    off[j] = p8 * 8 < p.d ? (int)(r * ts * 2) + p8 * 16 : kFar;
-  }
+  // The waves of a stream share its loads: the first half takes the queries, the second dO; 1 KB a load, ROWS rows.  A scalar offset
+  // never leaves its buffer; a stream without work reads nothing but zeros, which add nothing (queries behind the end are zeros too).
+  constexpr int ROWS = 512 / D, LOADS = 2 * (32 / ROWS) / BLOCKS;
+  const bool second = block >= BLOCKS / 2;
+  const int j0 = block % (BLOCKS / 2) * LOADS;
+  const bf16_t* const from = second ? dout : q;
+  const int64_t ts = second ? p.ot : p.qt, hs = second ? p.oh : p.qh;
+  const float* const stats_from = query_stats + (second ? (size_t)p.nq * p.total_q : 0);
   const unsigned full = (unsigned)(((int64_t)(lq - 1) * ts + p.d) * 2);
   int item = stream, h = hk * group;      // next tile of the current head
-  u32x4 rsrc;
-  unsigned bytes;
-  float stat;
   auto load = [&](int at) {
     while (h < (hk + 1) * group && item >= per_head) {
       item -= per_head;
       h++;
     }
     const bool some = h < (hk + 1) * group;
-    bytes = some ? full : 0u;
-    rsrc = buffer_rsrc(from + (int64_t)q0 * ts + (int64_t)h * hs, bytes);
+    const unsigned bytes = some ? full : 0u, sbytes = some ? (unsigned)lq * 4u : 0u;
+    const int hd = some ? h : 0;
+    const u32x4 rsrc = buffer_rsrc(from + (int64_t)q0 * ts + (int64_t)hd * hs, bytes);
+    const u32x4 srsrc = buffer_rsrc(stats_from + (size_t)hd * p.total_q + q0, sbytes);
     asm volatile("s_nop 4" ::: "memory");      // scalars from vector instructions, read by the loads below
     const int i = first + item;
+    int ln = lane;
+    asm volatile("" : "+v"(ln));      // the offsets are formed anew: registers
+    const int r = ln / (D / 8), row_off = r * (int)ts * 2;
 #pragma unroll
-    for (int j = 0; j < LOADS; j++)
-      load_to_lds(lds0 + (unsigned)(own + at + block * TILE + j * 1024), off[j & 3], rsrc, min((unsigned)(i * 32 + j * ROWS) * (unsigned)ts * 2u, bytes));
-    // queries without a key and rows behind the end: probability 2^-inf.  delta enters with its sign changed
-    const int row = i * 32 + (lane & 31);
-    const bool in = some && row < lq;
-    float x = in ? stats_from[(size_t)h * p.total_q + q0 + row] : 0.f;
-    stat = block ? -x : !in || x == -INFINITY ? INFINITY : x * kLog2e;
+    for (int j = 0; j < LOADS; j++) {
+      const int p8 = (ln % (D / 8)) ^ Stream<D>::swizzle((j0 + j) * ROWS + r);
+      load_to_lds(lds0 + (unsigned)(own + at + (second ? TILE : 0) + (j0 + j) * 1024), p8 * 8 < p.d ? row_off + p8 * 16 : kFar, rsrc,
+                  min((unsigned)(i * 32 + (j0 + j) * ROWS) * (unsigned)ts * 2u, bytes));
+    }
+    load_dword_to_lds(lds0 + (unsigned)(own + at + 2 * TILE + (second ? 256 : 0)), ln < 32 ? ln * 4 : kFar, srsrc, min((unsigned)i * 128u, sbytes));
   };
-  auto put = [&](int at) {
-    if (lane < 32) *((lds_float*)(lds_base + own + at + 2 * TILE) + 32 * block + lane) = stat;
+  // One round of 32 queries.  MID: the first operands of the next round are read at the end of this one, its rows have landed by then;
+  // the barrier stands in the middle of the round for the first four waves and at its beginning for the others.  That keeps the two
+  // waves of a SIMD half a round apart: one has its products while the other waits for scores.
+  constexpr bool MID = R == 3;
+  u32x4 a[4];
+  auto read = [&](const Reads<D>& lds, auto slot, int at) {      // row operand of a slot
+    constexpr int n = decltype(slot)::value, m = n % S;
+    if constexpr (n < S) return lds.rows(at, 0, n);
+    else if constexpr (n < 2 * S) return lds.rows(at + TILE, 0, m);
+    else return lds.columns(n < 3 * S ? at + TILE : at, 0, m / (D / 32), m % (D / 32));
   };
-  auto step = [&](int i0, int at) {
+  auto begin = [&](int at) {
+    const Reads<D> lds(base, lane);
+    each<AHEAD>([&](auto n) { a[decltype(n)::value] = read(lds, n, at); });
+  };
+  auto step = [&](int i0, int at, int after, auto middle) {
     // addresses are formed anew in every step: kept, they would not fit beside the rest
     Reads<D> lds(base, lane), values(value_base, lane);
     asm volatile("" : "+v"(lds.row), "+v"(lds.tr), "+v"(values.row));
-    u32x4 a[3], vr[2], pr[2], dz[2];
+    u32x4 vr[VA + 1], pr[2], dz[2];
     f32x16 z, dp;
-    f32x4 l[2];      // lse of the queries of register group g, read a group ahead
     const lds_float* stats = (const lds_float*)(lds_base + own + at + 2 * TILE) + 4 * (lane >> 5);
-    auto read = [&](auto slot) {      // row operand of a slot
-      constexpr int n = decltype(slot)::value, m = n % S;
-      if constexpr (n < S) return lds.rows(at, 0, n);
-      else if constexpr (n < 2 * S) return lds.rows(at + TILE, 0, m);
-      else return lds.columns(n < 3 * S ? at + TILE : at, 0, m / (D / 32), m % (D / 32));
-    };
-    each<AHEAD>([&](auto n) { a[decltype(n)::value] = read(n); });
-    z = zero16();
+#pragma unroll
+    for (int g = 0; g < 4; g++) {
+      const f32x4 l = *(const lds_f32x4*)(stats + 8 * g);
+#pragma unroll
+      for (int r = 0; r < 4; r++) z[4 * g + r] = l[r];
+    }
     each<SLOTS>([&](auto slot) {
       constexpr int n = decltype(slot)::value, m = n % S, later = n + AHEAD;
-      if constexpr (later < SLOTS) a[later % 3] = read(std::integral_constant<int, later>());
-      if constexpr (n + 1 >= S && n + 1 < 2 * S) vr[(n + 1) & 1] = values.rows(0, 0, n + 1 - S);
-      const u32x4 x = a[n % 3];
+      if constexpr (MID && (n == 0 || n == 2 * S)) {
+        if ((wave >> 2) == (n == 0)) middle();
+      }
+      if constexpr (later < SLOTS) a[later & 3] = read(lds, std::integral_constant<int, later>(), at);
+      else if constexpr (MID) a[later & 3] = read(lds, std::integral_constant<int, later - SLOTS>(), after);
+      if constexpr (n + VA >= S && n + VA < 2 * S) vr[(n + VA) % (VA + 1)] = values.rows(0, 0, n + VA - S);
+      const u32x4 x = a[n & 3];
       if constexpr (n < S) {                   // scores
         z = mfma(x, kr[n], z);
         if constexpr (n == S - 2) {
 #pragma unroll
           for (int g = 0; g < 4; g++) {
-            const f32x4 dl = *(const lds_f32x4*)(stats + 32 + 8 * g);
+            const f32x4 dl = *(const lds_f32x4*)(stats + 64 + 8 * g);
 #pragma unroll
             for (int r = 0; r < 4; r++) dp[4 * g + r] = dl[r];
           }
-          l[0] = *(const lds_f32x4*)stats;
         }
       } else if constexpr (n < 2 * S) {        // gradients of the probabilities, less delta; probabilities
-        dp = mfma(x, vr[n & 1], dp);
-        constexpr int g = m * PER / 4;
-        if constexpr (m * PER % 4 == 0 && g < 3) l[(g + 1) & 1] = *(const lds_f32x4*)(stats + 8 * (g + 1));
+        dp = mfma(x, vr[n % (VA + 1)], dp);
 #pragma unroll
-        for (int e = m * PER; e < (m + 1) * PER; e++) z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], c2, -l[g & 1][e & 3]));
+        for (int e = m * PER; e < (m + 1) * PER; e++) z[e] = __builtin_amdgcn_exp2f(z[e] * c2);
         if constexpr (m == S - 1) {
-          if (i0 < all) {      // the diagonal runs through the tile
+          if (i0 < all) {      // the diagonal runs through the tile: queries from `seen` on see the lane's key
+            const int seen = t.row0 + 32 * block + (lane & 31) - shift;
 #pragma unroll
             for (int e = 0; e < 16; e++)
               if (i0 + row_of(e, lane) < seen) z[e] = 0.f;
@@ -506,23 +519,48 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
       __builtin_amdgcn_sched_barrier(0);
     });
   };
-  if (rounds > 0) {
-    load(0);
-    put(0);
-  }
-  for (int r = 0, at = 0; r < rounds; r++, at = STAGE - at) {
-    const int i0 = (first + item) * 32;
+  // Loads go R - 1 rounds ahead, whether there is work or not.  Tiles of the rounds in work are counted apart from those loaded: the
+  // same walk over (head, tile).
+  int done = stream;
+  int at = 0, next = (R - 1) * STAGE;
+  auto landed = [&]() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();      // this round's rows have landed, the other stage is read out
-    if (r + 1 < rounds) {
-      item += 4;
-      load(STAGE - at);
+    __builtin_amdgcn_s_barrier();
+  };
+  auto load_next = [&]() {
+    load(next);
+    item += STREAMS;
+    next = next + STAGE == R * STAGE ? 0 : next + STAGE;
+  };
+#pragma unroll
+  for (int r = 0; r < R - 1; r++) {
+    load(r * STAGE);
+    item += STREAMS;
+  }
+  if constexpr (MID) {
+    landed();
+    begin(0);
+  }
+  for (int r = 0; r < rounds; r++) {
+    while (done >= per_head) done -= per_head;
+    const int i0 = (first + done) * 32, after = at + STAGE == R * STAGE ? 0 : at + STAGE;
+    if constexpr (MID) {
+      // the next round's rows have landed for every wave, and every wave is done with the round before
+      step(i0, at, after, [&]() {
+        landed();
+        load_next();
+      });
+    } else {
+      landed();      // this round's rows, and every wave is done with the round before
+      load_next();
+      begin(at);
+      step(i0, at, after, []() {});
     }
-    step(i0, at);
-    if (r + 1 < rounds) put(STAGE - at);
+    at = after;
+    done += STREAMS;
   }
   asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");      // results of the assembly's last products
-  // the streams' sums: [stream][key][D + 4] in LDS; 8 threads add up and store a key
+  // the streams' sums: [stream][key][D + 4] in LDS; several threads add up and store a key
   constexpr int PITCH = D + 4;
   lds_float* const sums = (lds_float*)lds_base;
   auto join = [&](const f32x16 (&acc)[D / 32], float f, bf16_t* out) {
@@ -531,19 +569,20 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
     for (int b = 0; b < D / 32; b++)
 #pragma unroll
       for (int g = 0; g < 4; g++)
-        *(lds_f32x4*)(sums + (stream * DKV_ROWS + 32 * block + (lane & 31)) * PITCH + 32 * b + 8 * g + 4 * (lane >> 5)) =
+        *(lds_f32x4*)(sums + (stream * KEYS + 32 * block + (lane & 31)) * PITCH + 32 * b + 8 * g + 4 * (lane >> 5)) =
             f32x4{acc[b][4 * g], acc[b][4 * g + 1], acc[b][4 * g + 2], acc[b][4 * g + 3]};
     __syncthreads();
-    const int key = threadIdx.x >> 3;
+    constexpr int SHARE = 512 / KEYS;      // threads of a key
+    const int key = threadIdx.x / SHARE;
     if (t.row0 + key < t.len) {
       bf16_t* row = out + (int64_t)(t.first + t.row0 + key) * p.nkv * p.d + (int64_t)hk * p.d;
 #pragma unroll
-      for (int j = 0; j < D / 64; j++) {
-        const int col = (threadIdx.x & 7) * 8 + 64 * j;
+      for (int j = 0; j < D / 8 / SHARE; j++) {
+        const int col = (threadIdx.x % SHARE) * 8 + 8 * SHARE * j;
         float y[8];
 #pragma unroll
-        for (int w = 0; w < 4; w++) {
-          const lds_float* part = sums + (w * DKV_ROWS + key) * PITCH + col;
+        for (int w = 0; w < STREAMS; w++) {
+          const lds_float* part = sums + (w * KEYS + key) * PITCH + col;
           const f32x4 lo = *(const lds_f32x4*)part, hi = *(const lds_f32x4*)(part + 4);
 #pragma unroll
           for (int e = 0; e < 4; e++) {
@@ -571,6 +610,13 @@ void allow_lds(std::atomic<uint64_t>& done, K kernel, int bytes) {
   done.fetch_or(bit, std::memory_order_release);
 }
 
+// Keys of a workgroup of dk and dv.  128 (each tile of queries read by four waves, three stages) where there are workgroups enough
+// for that, 64 otherwise.
+bool many_keys(const PackedShape& p) {
+  const int64_t n = (int64_t)p.total_k * p.nkv / 128;
+  return n >= 1024 || (n >= 512 && p.n_seq <= 2);
+}
+
 template <int D>
 void forward(hipStream_t s, const PackedShape& p, const bf16_t* q, const bf16_t* k, const bf16_t* v, bf16_t* o, float* lse) {
   static std::atomic<uint64_t> done;
@@ -580,17 +626,23 @@ void forward(hipStream_t s, const PackedShape& p, const bf16_t* q, const bf16_t*
 }
 template <int D>
 void backward(hipStream_t s, const PackedShape& p, const bf16_t* dout, const bf16_t* q, const bf16_t* k, const bf16_t* v, const bf16_t* o,
-              const float* lse, bf16_t* dq, bf16_t* dk, bf16_t* dv, float* delta) {
-  static std::atomic<uint64_t> done[2];
+              const float* lse, bf16_t* dq, bf16_t* dk, bf16_t* dv, float* stats) {
+  static std::atomic<uint64_t> done[3];
   const int lds = 4 * BN * D * 2;
   if (p.total_q > 0) {
     allow_lds(done[0], attention_dq_kernel<D>, lds);
-    attention_dq_kernel<D><<<(unsigned)(packed_tiles(p.total_q, p.n_seq, BM) * p.nq), 256, lds, s>>>(p, dout, q, k, v, o, lse, dq, delta);
+    attention_dq_kernel<D><<<(unsigned)(packed_tiles(p.total_q, p.n_seq, BM) * p.nq), 256, lds, s>>>(p, dout, q, k, v, o, lse, dq, stats);
   }
   if (p.total_k > 0) {
-    constexpr int ring = 8 * (2 * 32 * D * 2 + 256) + DKV_ROWS * D * 2, sums = 4 * DKV_ROWS * (D + 4) * 4, bytes = ring > sums ? ring : sums;
-    allow_lds(done[1], attention_dkv_kernel<D>, bytes);
-    attention_dkv_kernel<D><<<(unsigned)(packed_tiles(p.total_k, p.n_seq, DKV_ROWS) * p.nkv), 512, bytes, s>>>(p, dout, q, k, v, lse, delta, dk, dv);
+    auto go = [&](auto blocks, auto stages) {
+      constexpr int BLOCKS = decltype(blocks)::value, R = decltype(stages)::value, STREAMS = 8 / BLOCKS, KEYS = 32 * BLOCKS;
+      constexpr int ring = STREAMS * R * (2 * 32 * D * 2 + 512) + KEYS * D * 2, sums = STREAMS * KEYS * (D + 4) * 4, bytes = ring > sums ? ring : sums;
+      auto kernel = attention_dkv_kernel<D, BLOCKS, R>;
+      allow_lds(done[BLOCKS / 2], kernel, bytes);
+      kernel<<<(unsigned)(packed_tiles(p.total_k, p.n_seq, KEYS) * p.nkv), 512, bytes, s>>>(p, dout, q, k, v, stats, dk, dv);
+    };
+    if (many_keys(p)) go(std::integral_constant<int, 4>(), std::integral_constant<int, 3>());
+    else go(std::integral_constant<int, 2>(), std::integral_constant<int, D == 128 ? 2 : 3>());
   }
 }
 
@@ -603,9 +655,10 @@ bool attention_takes_mfma(const PackedShape& p, const void* q, const void* k, co
   auto takes = [&](const void* x, int64_t ts, int64_t hs, int total) {
     return aligned16(x) && ts % 8 == 0 && hs % 8 == 0 && ts >= p.d && ts * 2 * ((int64_t)total + 2 * BN) < most;
   };
-  return p.d % 8 == 0 && takes(q, p.qt, p.qh, p.total_q) && takes(k, p.kt, p.kh, p.total_k) && takes(v, p.vt, p.vh, p.total_k) &&
+  // the backward pass divides by the scale
+  return fabsf(p.scale) > 1e-30f && p.d % 8 == 0 && takes(q, p.qt, p.qh, p.total_q) && takes(k, p.kt, p.kh, p.total_k) && takes(v, p.vt, p.vh, p.total_k) &&
          takes(o, p.ot, p.oh, p.total_q) && takes(dout, p.ot, p.oh, p.total_q) && (int64_t)packed_tiles(p.total_q, p.n_seq, BM) * p.nq < (1ll << 31) &&
-         (int64_t)packed_tiles(p.total_k, p.n_seq, DKV_ROWS) * p.nkv < (1ll << 31);
+         (int64_t)packed_tiles(p.total_k, p.n_seq, 64) * p.nkv < (1ll << 31);
 }
 
 void launch_attention_mfma_forward(hipStream_t s, const PackedShape& p, const bf16_t* q, const bf16_t* k, const bf16_t* v, bf16_t* o,
@@ -615,7 +668,7 @@ void launch_attention_mfma_forward(hipStream_t s, const PackedShape& p, const bf
 }
 void launch_attention_mfma_backward(hipStream_t s, const PackedShape& p, const bf16_t* dout, const bf16_t* q, const bf16_t* k,
                                     const bf16_t* v, const bf16_t* o, const float* lse, bf16_t* dq, bf16_t* dk, bf16_t* dv,
-                                    float* delta) {
-  if (p.d <= 64) backward<64>(s, p, dout, q, k, v, o, lse, dq, dk, dv, delta);
-  else backward<128>(s, p, dout, q, k, v, o, lse, dq, dk, dv, delta);
+                                    float* stats) {
+  if (p.d <= 64) backward<64>(s, p, dout, q, k, v, o, lse, dq, dk, dv, stats);
+  else backward<128>(s, p, dout, q, k, v, o, lse, dq, dk, dv, stats);
 }

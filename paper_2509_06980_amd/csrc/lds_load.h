@@ -29,3 +29,9 @@ __device__ __forceinline__ void load_to_lds(unsigned lds, int voff, u32x4 rsrc, 
                "s"(soff)
                : "memory", "m0");
 }
+// The same with 4 bytes per lane (lane l's at lds + 4 l).
+__device__ __forceinline__ void load_dword_to_lds(unsigned lds, int voff, u32x4 rsrc, unsigned soff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc),
+               "s"(soff)
+               : "memory", "m0");
+}

@@ -49,4 +49,4 @@ void launch_attention_mfma_forward(hipStream_t s, const PackedShape& p, const bf
                                    float* lse);
 void launch_attention_mfma_backward(hipStream_t s, const PackedShape& p, const bf16_t* dout, const bf16_t* q, const bf16_t* k,
                                     const bf16_t* v, const bf16_t* o, const float* lse, bf16_t* dq, bf16_t* dk, bf16_t* dv,
-                                    float* delta);
+                                    float* stats);      // stats: 2 floats a query and head
