@@ -87,26 +87,34 @@ struct Stream {
   }
 };
 
-// Lane parts of the reads from a tile.
+// Reads from tiles.  A lane's addresses differ in bits 5 to 7 alone, by exclusive or with a constant; tiles begin at multiples of 256
+// bytes, so moving to another one leaves those bits: one addition a tile, one exclusive or a read, the rest is in the instruction.
 template <int D>
 struct Reads {
-  lds_char* lds;
-  int row, tr;
-  __device__ __forceinline__ Reads(lds_char* p, int lane) : lds(p) {
+  lds_char *row, *tr;
+  __device__ __forceinline__ Reads(lds_char* base, int lane) {
     const int i = lane & 15, h = lane >> 5, w = lane >> 4 & 1;
-    row = (lane & 31) * (D * 2) + ((h ^ Stream<D>::swizzle(lane & 31)) << 4);
     const int f = D == 128 ? (i >> 2) << 2 : (i >> 3 & 1) << 2;
-    tr = (4 * h + (i >> 2)) * (D * 2) + ((f | ((2 * w + (i >> 1 & 1)) ^ h)) << 4) + ((i & 1) << 3);
+    row = base + (lane & 31) * (D * 2) + ((h ^ Stream<D>::swizzle(lane & 31)) << 4);
+    tr = base + (4 * h + (i >> 2)) * (D * 2) + ((f | ((2 * w + (i >> 1 & 1)) ^ h)) << 4) + ((i & 1) << 3);
   }
-  // 32 rows from row 32 x on, k = columns 16 s .. + 15
+  __device__ __forceinline__ void move(int bytes) {
+    row += bytes;
+    tr += bytes;
+    asm volatile("" : "+v"(row), "+v"(tr));      // or the compiler keeps every read's address in a register of its own
+  }
+  static __device__ __forceinline__ lds_char* turned(lds_char* p, unsigned bits) {
+    return (lds_char*)((unsigned)(uintptr_t)p ^ bits);
+  }
+  // 32 rows from row 32 x of the tile `at` bytes on, k = columns 16 s .. + 15
   __device__ __forceinline__ u32x4 rows(int at, int x, int s) const {
-    return *(lds_u32x4*)(lds + at + x * 32 * (D * 2) + (row ^ (s << 5)));
+    return *(lds_u32x4*)(turned(row, s << 5) + (at + x * 32 * (D * 2)));
   }
   // rows = columns 32 b .. + 31, k = rows 32 x + 16 s .. + 15 in the order of a result's registers
   __device__ __forceinline__ u32x4 columns(int at, int x, int s, int b) const {
-    const int base = at + (32 * x + 16 * s) * (D * 2), a = tr ^ (b << 6);
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + base + a));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + base + 8 * (D * 2) + (a ^ 32)));
+    const int off = at + (32 * x + 16 * s) * (D * 2);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(turned(tr, b << 6) + off));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(turned(tr, b << 6 | 32) + (off + 8 * (D * 2))));
     return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 };
@@ -174,7 +182,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(PackedShape p
   QuerySide w;
   if (!query_side(p, w)) return;
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
-  const Reads<D> lds((lds_char*)(__attribute__((address_space(3))) void*)smem, lane);
+  Reads<D> lds((lds_char*)(__attribute__((address_space(3))) void*)smem, lane);      // of the stage in work
   const int mine = w.t.row0 + wave * 32 + (lane & 31);      // lane's query
   u32x4 qr[D / 16];
   own_rows<D>(q + (int64_t)w.t.first * p.qt + (int64_t)w.h * p.qh, p.qt, mine, w.t.len, p.d, lane, qr);
@@ -195,13 +203,13 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(PackedShape p
     ks.load(0, lds0, wave);
     vs.load(0, lds0 + TILE, wave);
   }
-  auto tile = [&](int j0, int at, auto masked) {
+  auto tile = [&](int j0, auto masked) {
     f32x16 z[2];
 #pragma unroll
     for (int x = 0; x < 2; x++) {
       z[x] = zero16();
 #pragma unroll
-      for (int s = 0; s < D / 16; s++) z[x] = mfma(lds.rows(at, x, s), qr[s], z[x]);
+      for (int s = 0; s < D / 16; s++) z[x] = mfma(lds.rows(0, x, s), qr[s], z[x]);
     }
     float top = -INFINITY;
 #pragma unroll
@@ -235,7 +243,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(PackedShape p
       for (int s = 0; s < 2; s++) {
         const u32x4 pr = as_operand(z[x], s);      // probabilities rounded to bf16; their sum is not
 #pragma unroll
-        for (int b = 0; b < D / 32; b++) acc[b] = mfma(lds.columns(at + TILE, x, s, b), pr, acc[b]);
+        for (int b = 0; b < D / 32; b++) acc[b] = mfma(lds.columns(TILE, x, s, b), pr, acc[b]);
       }
     }
   };
@@ -248,8 +256,9 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(PackedShape p
       vs.load(t + 1, lds0 + (unsigned)(STAGE - at + TILE), wave);
     }
     const int j0 = t * BN;
-    if (j0 + BN <= all) tile(j0, at, std::false_type());
-    else if (j0 < some) tile(j0, at, std::true_type());
+    if (j0 + BN <= all) tile(j0, std::false_type());
+    else if (j0 < some) tile(j0, std::true_type());
+    lds.move(t & 1 ? -STAGE : STAGE);
   }
   sum += __shfl_xor(sum, 32, 64);
   if (mine < w.t.len) {
@@ -272,7 +281,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(PackedShape p, con
   QuerySide w;
   if (!query_side(p, w)) return;
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
-  const Reads<D> lds((lds_char*)(__attribute__((address_space(3))) void*)smem, lane);
+  Reads<D> lds((lds_char*)(__attribute__((address_space(3))) void*)smem, lane);      // of the stage in work
   const int mine = w.t.row0 + wave * 32 + (lane & 31);
   u32x4 qr[D / 16], gr[D / 16];
   float dl = 0.f;
@@ -316,14 +325,14 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(PackedShape p, con
   }
   // 32 keys, in slots of one row operand, read three slots ahead, its product, and a share of the arithmetic on the scores
   constexpr int S = D / 16, SLOTS = 3 * S, AHEAD = 3, PER = 16 / S;
-  auto tile = [&](int j0, int at, int x, bool masked) {
+  auto tile = [&](int j0, int x, bool masked) {
     u32x4 a[4], dz[2];
     f32x16 z, dp;
     auto read = [&](auto slot) {
       constexpr int n = decltype(slot)::value, m = n % S;
-      if constexpr (n < S) return lds.rows(at, x, n);
-      else if constexpr (n < 2 * S) return lds.rows(at + TILE, x, m);
-      else return lds.columns(at, x, m / (D / 32), m % (D / 32));
+      if constexpr (n < S) return lds.rows(0, x, n);
+      else if constexpr (n < 2 * S) return lds.rows(TILE, x, m);
+      else return lds.columns(0, x, m / (D / 32), m % (D / 32));
     };
     each<AHEAD>([&](auto n) { a[decltype(n)::value] = read(n); });
 #pragma unroll
@@ -365,9 +374,10 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(PackedShape p, con
     }
     const int j0 = t * BN;
     if (j0 < some) {
-      tile(j0, at, 0, j0 + 32 > all);
-      tile(j0, at, 1, j0 + BN > all);
+      tile(j0, 0, j0 + 32 > all);
+      tile(j0, 1, j0 + BN > all);
     }
+    lds.move(t & 1 ? -STAGE : STAGE);
   }
   if (mine < w.t.len) store_rows<D>(acc, p.scale, dq + (int64_t)(w.t.first + mine) * p.ot + (int64_t)w.h * p.oh, p.d, lane);
 }
@@ -449,20 +459,20 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
   // waves of a SIMD half a round apart: one has its products while the other waits for scores.
   constexpr bool MID = R == 3;
   u32x4 a[4];
-  auto read = [&](const Reads<D>& lds, auto slot, int at) {      // row operand of a slot
+  Reads<D> lds(base, lane);      // of the round in work
+  const Reads<D> values(value_base, lane);
+  auto read = [&](auto slot) {      // row operand of a slot
     constexpr int n = decltype(slot)::value, m = n % S;
-    if constexpr (n < S) return lds.rows(at, 0, n);
-    else if constexpr (n < 2 * S) return lds.rows(at + TILE, 0, m);
-    else return lds.columns(n < 3 * S ? at + TILE : at, 0, m / (D / 32), m % (D / 32));
+    if constexpr (n < S) return lds.rows(0, 0, n);
+    else if constexpr (n < 2 * S) return lds.rows(TILE, 0, m);
+    else return lds.columns(n < 3 * S ? TILE : 0, 0, m / (D / 32), m % (D / 32));
   };
-  auto begin = [&](int at) {
-    const Reads<D> lds(base, lane);
-    each<AHEAD>([&](auto n) { a[decltype(n)::value] = read(lds, n, at); });
+  auto begin = [&]() {
+    each<AHEAD>([&](auto n) { a[decltype(n)::value] = read(n); });
   };
   auto step = [&](int i0, int at, int after, auto middle) {
-    // addresses are formed anew in every step: kept, they would not fit beside the rest
-    Reads<D> lds(base, lane), values(value_base, lane);
-    asm volatile("" : "+v"(lds.row), "+v"(lds.tr), "+v"(values.row));
+    lds_char* value_row = values.row;
+    asm volatile("" : "+v"(value_row));
     u32x4 vr[VA + 1], pr[2], dz[2];
     f32x16 z, dp;
     const lds_float* stats = (const lds_float*)(lds_base + own + at + 2 * TILE) + 4 * (lane >> 5);
@@ -477,9 +487,12 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
       if constexpr (MID && (n == 0 || n == 2 * S)) {
         if ((wave >> 2) == (n == 0)) middle();
       }
-      if constexpr (later < SLOTS) a[later & 3] = read(lds, std::integral_constant<int, later>(), at);
-      else if constexpr (MID) a[later & 3] = read(lds, std::integral_constant<int, later - SLOTS>(), after);
-      if constexpr (n + VA >= S && n + VA < 2 * S) vr[(n + VA) % (VA + 1)] = values.rows(0, 0, n + VA - S);
+      if constexpr (later < SLOTS) a[later & 3] = read(std::integral_constant<int, later>());
+      else if constexpr (MID) {
+        if constexpr (later == SLOTS) lds.move(after - at);      // every read of this round is under way
+        a[later & 3] = read(std::integral_constant<int, later - SLOTS>());
+      }
+      if constexpr (n + VA >= S && n + VA < 2 * S) vr[(n + VA) % (VA + 1)] = *(lds_u32x4*)Reads<D>::turned(value_row, (n + VA - S) << 5);
       const u32x4 x = a[n & 3];
       if constexpr (n < S) {                   // scores
         z = mfma(x, kr[n], z);
@@ -539,7 +552,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
   }
   if constexpr (MID) {
     landed();
-    begin(0);
+    begin();
   }
   for (int r = 0; r < rounds; r++) {
     while (done >= per_head) done -= per_head;
@@ -553,8 +566,9 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
     } else {
       landed();      // this round's rows, and every wave is done with the round before
       load_next();
-      begin(at);
+      begin();
       step(i0, at, after, []() {});
+      lds.move(after - at);
     }
     at = after;
     done += STREAMS;
