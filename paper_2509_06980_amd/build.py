@@ -1,12 +1,15 @@
-"""Build librl_rollout.so (HIP, gfx950) in-tree with hipcc."""
+"""Build librl_rollout.so (HIP, gfx950) in-tree with hipcc, and its binding to torch tensors (host code) with g++."""
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "librl_rollout.so")
+TORCH_OUT = os.path.join(HERE, "_policy_torch.so")
 COMMON = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-result"]
 SOURCES = {
@@ -48,7 +51,22 @@ def build(verbose=False):
                        capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
+    build_torch_binding()
     return OUT
+
+
+def build_torch_binding():
+    """_policy_torch.so: the policy update's operators on torch tensors, linked against the library beside it."""
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-fPIC", "-shared", "-std=c++17", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=1",
+           "-I" + os.path.join(torch, "include"), "-I" + os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "policy_torch.cpp"), "-o", TORCH_OUT,
+           "-L" + os.path.join(torch, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python",
+           "-L" + HERE, "-l:librl_rollout.so", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for policy_torch.cpp:\n{r.stderr}")
+    return TORCH_OUT
 
 
 if __name__ == "__main__":

@@ -13,14 +13,25 @@ namespace {
 // Row r is at (r / inner) * so + (r % inner) * si: heads of a fused projection need no copy.
 // =============================================================================================
 struct Rows {
-  int64_t n, so, si;
-  int inner;
-  __device__ __forceinline__ int64_t at(int64_t r) const {
+  int n;                          // below 2^31
+  int64_t so, si;
+  unsigned inner, magic, shift;
+  // r / inner = (r * magic >> 32) >> shift for r < 2^31: magic = ceil(2^(32 + shift) / inner), 2^shift < inner <= 2^(shift + 1)
+  Rows(int64_t rows, int64_t outer_stride, int64_t inner_stride, int inner_rows)
+      : n((int)rows), so(outer_stride), si(inner_stride), inner((unsigned)inner_rows), magic(0), shift(0) {
+    if (inner < 2) return;
+    while ((2ull << shift) < inner) shift++;
+    magic = (unsigned)(((1ull << (32 + shift)) + inner - 1) / inner);
+  }
+  __device__ __forceinline__ int64_t at(int r) const {
     if (inner == 1) return r * so;
-    const int64_t o = r / inner;
-    return o * so + (r - o * inner) * si;
+    const int o = (int)(__umulhi((unsigned)r, magic) >> shift);
+    return o * so + (int64_t)(r - o * (int)inner) * si;
   }
 };
+
+// Pieces of a thread that lie inside every row that row_plan gives the plan (L, NV): those of the next smaller plan.
+constexpr int full_pieces(int L, int NV) { return L < 64 ? 0 : NV == 8 ? 6 : L == 256 && NV == 6 ? 4 : NV - 1; }
 
 template <int L>
 __device__ __forceinline__ float group_sum(float v, float* lds) {
@@ -41,10 +52,10 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(const T* __restrict__
                                                            float* __restrict__ mean_out, float* __restrict__ rstd_out) {
   __shared__ float lds[4];
   const int lane = threadIdx.x % L;
-  const int64_t row = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+  const int row = (int)blockIdx.x * (256 / L) + (L >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : threadIdx.x / L);
   const bool live = row < rows.n;      // groups without a row run along: their lanes take part in no other group's sums
   const T* xr = x + (live ? rows.at(row) : 0);
-  T* yr = y + (live ? row : 0) * width;
+  T* yr = y + (int64_t)(live ? row : 0) * width;
   const float inv = 1.f / (float)width;
   float mu = 0.f, rstd;
   if constexpr (NV > 0) {
@@ -124,74 +135,128 @@ __global__ __launch_bounds__(256) void norm_forward_kernel(const T* __restrict__
   }
 }
 
-// Workgroup p walks over the rows p * (256 / L) + i * gridDim * (256 / L) and leaves its share of dw (and db, behind all of dw)
-// in part[p][width]; norm_reduce_kernel adds the shares in a fixed order.
-template <typename T, int VEC, int L, int NV>
-__global__ __launch_bounds__(256) void norm_backward_kernel(const T* __restrict__ dy, Rows drows, const T* __restrict__ x, Rows rows,
-                                                            int width, const T* __restrict__ w, const float* __restrict__ mean,
-                                                            const float* __restrict__ rstd, int centered, int biased,
-                                                            T* __restrict__ dx, float* __restrict__ part) {
+// VEC elements as they lie in memory, in as few registers
+template <typename T, int VEC>
+struct Raw {
+  using type = u32x4;
+};
+template <typename T>
+struct Raw<T, 1> {
+  using type = T;
+};
+template <typename T, int VEC>
+__device__ __forceinline__ void widen(const typename Raw<T, VEC>::type& r, float (&v)[VEC]) {
+  if constexpr (VEC == 1) v[0] = ldf(&r);
+  else ldv<VEC>((const T*)&r, v);
+}
+
+// Workgroup p walks over the rows p G + i G gridDim, G = THREADS / L of them at a time, and leaves its share of dw (and db, behind all
+// of dw) in part[p][width]; norm_reduce_kernel adds the shares in a fixed order.  One workgroup a CU of as many waves as the
+// registers allow: as much on its way as memory needs, and few shares.
+template <typename T, int VEC, int L, int NV, bool BIASED, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_backward_kernel(const T* __restrict__ dy, Rows drows, const T* __restrict__ x, Rows rows,
+                                                                int width, const T* __restrict__ w, const float* __restrict__ mean,
+                                                                const float* __restrict__ rstd, int centered, T* __restrict__ dx,
+                                                                float* __restrict__ part) {
   __shared__ float lds[4];
-  const int lane = threadIdx.x % L, group = threadIdx.x / L;
+  const int lane = threadIdx.x % L, group = L >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : threadIdx.x / L;
   const float inv = 1.f / (float)width;
   float* pw = part + (size_t)blockIdx.x * width;
   float* pb = pw + (size_t)gridDim.x * width;
-  constexpr int G = 256 / L;
+  constexpr int G = THREADS / L, W = L < 64 ? 64 / L : 1;      // groups; of a wave
+  using R = typename Raw<T, VEC>::type;
   if constexpr (NV > 0) {
     __shared__ float sum[G == 1 ? 1 : L * NV * VEC];
-    float aw[NV][VEC], ab[NV][VEC], g[NV][VEC];
+    float aw[NV][VEC], ab[BIASED ? NV : 1][VEC];
+    R xr[NV], dr[NV];
+    float mu = 0.f, r = 0.f;
+    auto inside = [&](int i) { return i < full_pieces(L, NV) || (i * L + lane) * VEC < width; };
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-      const int c = (i * L + lane) * VEC;
 #pragma unroll
-      for (int e = 0; e < VEC; e++) aw[i][e] = ab[i][e] = g[i][e] = 0.f;
-      if (c < width) ldv<VEC>(w + c, g[i]);
+      for (int e = 0; e < VEC; e++) aw[i][e] = 0.f;
+      if constexpr (BIASED) {
+#pragma unroll
+        for (int e = 0; e < VEC; e++) ab[i][e] = 0.f;
+      }
     }
-    for (int64_t r0 = (int64_t)blockIdx.x * G; r0 < rows.n; r0 += (int64_t)gridDim.x * G) {
-      const int64_t row = r0 + group;
+    auto fetch = [&](int row) {      // rows behind the last: zeros, which add nothing
       const bool live = row < rows.n;
-      float n[NV][VEC], d[NV][VEC];
-      const float mu = live && centered ? mean[row] : 0.f, r = live ? rstd[row] : 0.f;
-      const T* xr = x + (live ? rows.at(row) : 0);
-      const T* dr = dy + (live ? drows.at(row) : 0);
+      mu = live && centered ? mean[row] : 0.f;
+      r = live ? rstd[row] : 0.f;
+      const T* xp = x + (live ? rows.at(row) : 0);
+      const T* dp = dy + (live ? drows.at(row) : 0);
 #pragma unroll
       for (int i = 0; i < NV; i++) {
         const int c = (i * L + lane) * VEC;
-        if (live && c < width) {
-          ldv<VEC>(xr + c, n[i]);
-          ldv<VEC>(dr + c, d[i]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < VEC; e++) n[i][e] = mu, d[i][e] = 0.f;
+        xr[i] = R{}, dr[i] = R{};
+        if (live && inside(i)) {
+          xr[i] = *(const R*)(xp + c);
+          dr[i] = *(const R*)(dp + c);
         }
       }
+    };
+    const int step = (int)gridDim.x * G;      // r0 + step stays below 2^31 + 2^18
+    for (unsigned r0 = blockIdx.x * G; r0 < (unsigned)rows.n; r0 += step) {
+      const int row = min((int)min(r0 + group, 0x7fffffffu), rows.n);
+      // the row stays as it lies in memory and is widened twice
+      fetch(row);
+      const T* wp = w;
+      asm volatile("" : "+s"(wp));      // read anew for every row: kept in 32 bits, the weights would take the registers
+      auto widened = [&](int i, float (&gw)[VEC], float (&n)[VEC], float (&d)[VEC]) {
+        R g{};
+        if (inside(i)) g = *(const R*)(wp + (i * L + lane) * VEC);
+        widen<T, VEC>(g, gw);
+        widen<T, VEC>(xr[i], n);
+        widen<T, VEC>(dr[i], d);
+#pragma unroll
+        for (int e = 0; e < VEC; e++) n[e] = inside(i) ? (n[e] - mu) * r : 0.f;
+      };
       float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-      for (int i = 0; i < NV; i++)
+      for (int i = 0; i < NV; i++) {
+        float gw[VEC], n[VEC], d[VEC];
+        widened(i, gw, n, d);
 #pragma unroll
         for (int e = 0; e < VEC; e++) {
-          n[i][e] = (n[i][e] - mu) * r;
-          aw[i][e] += d[i][e] * n[i][e];
-          ab[i][e] += d[i][e];
-          d[i][e] *= g[i][e];
-          s1 += d[i][e] * n[i][e];
-          s2 += d[i][e];
+          aw[i][e] += d[e] * n[e];
+          asm volatile("" : "+v"(aw[i][e]));      // added here: put off to the row's end, every factor stays in a register
+          if constexpr (BIASED) {
+            ab[i][e] += d[e];
+            asm volatile("" : "+v"(ab[i][e]));
+          }
+          s1 += d[e] * gw[e] * n[e];
+          s2 += d[e] * gw[e];
         }
+        __builtin_amdgcn_sched_barrier(0);      // one piece in 32 bits at a time
+      }
       s1 = group_sum<L>(s1, lds) * inv;
       s2 = centered ? group_sum<L>(s2, lds) * inv : 0.f;
-      T* out = dx + (live ? row : 0) * width;
+      const bool live = row < rows.n;
+      T* out = dx + (int64_t)(live ? row : 0) * width;
 #pragma unroll
       for (int i = 0; i < NV; i++) {
-        const int c = (i * L + lane) * VEC;
-        if (live && c < width) {
+        if constexpr (VEC > 1) asm volatile("" : "+v"(xr[i]), "+v"(dr[i]));      // or the compiler keeps both forms
+        if (live && inside(i)) {
+          float gw[VEC], n[VEC], d[VEC];
+          widened(i, gw, n, d);
 #pragma unroll
-          for (int e = 0; e < VEC; e++) d[i][e] = (d[i][e] - n[i][e] * s1 - s2) * r;
-          stv<VEC>(out + c, d[i]);
+          for (int e = 0; e < VEC; e++) d[e] = (d[e] * gw[e] - n[e] * s1 - s2) * r;
+          stv<VEC>(out + (i * L + lane) * VEC, d);
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-    // the groups' shares one after the other
-    auto joined = [&](const float (&a)[NV][VEC], float* to) {
+    // the groups' shares: of a wave by shuffles, then one wave after the other
+    auto joined = [&](auto& a, float* to) {
+      if constexpr (L < 64) {
+#pragma unroll
+        for (int i = 0; i < NV; i++)
+#pragma unroll
+          for (int e = 0; e < VEC; e++)
+#pragma unroll
+            for (int o = L; o < 64; o *= 2) a[i][e] += __shfl_xor(a[i][e], o, 64);
+      }
       if constexpr (G == 1) {
 #pragma unroll
         for (int i = 0; i < NV; i++) {
@@ -202,7 +267,7 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(const T* __restrict_
         }
         return;
       }
-      for (int k = 0; k < G; k++) {
+      for (int k = 0; k < G; k += W) {
         if (group == k) {
 #pragma unroll
           for (int i = 0; i < NV; i++)
@@ -214,27 +279,22 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(const T* __restrict_
         }
         __syncthreads();
       }
-      if (group == 0) {
-#pragma unroll
-        for (int i = 0; i < NV; i++) {
-          const int c = (i * L + lane) * VEC;
-#pragma unroll
-          for (int e = 0; e < VEC; e++)
-            if (c + e < width) to[c + e] = sum[(i * VEC + e) * L + lane];
-        }
+      for (int c = threadIdx.x; c < width; c += THREADS) {
+        const int piece = c / VEC;
+        to[c] = sum[(piece / L * VEC + c % VEC) * L + piece % L];
       }
       __syncthreads();
     };
     joined(aw, pw);
-    if (biased) joined(ab, pb);
+    if constexpr (BIASED) joined(ab, pb);
   } else {
     for (int c = lane * VEC; c < width; c += L * VEC)
 #pragma unroll
       for (int e = 0; e < VEC; e++) {
         pw[c + e] = 0.f;
-        if (biased) pb[c + e] = 0.f;
+        if (BIASED) pb[c + e] = 0.f;
       }
-    for (int64_t row = blockIdx.x; row < rows.n; row += gridDim.x) {
+    for (unsigned row = blockIdx.x; row < (unsigned)rows.n; row += gridDim.x) {
       const float mu = centered ? mean[row] : 0.f, r = rstd[row];
       const T* xr = x + rows.at(row);
       const T* dr = dy + drows.at(row);
@@ -247,7 +307,7 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(const T* __restrict_
         for (int e = 0; e < VEC; e++) {
           n[e] = (n[e] - mu) * r;
           pw[c + e] += d[e] * n[e];
-          if (biased) pb[c + e] += d[e];
+          if (BIASED) pb[c + e] += d[e];
           s1 += d[e] * g[e] * n[e];
           s2 += d[e] * g[e];
         }
@@ -260,30 +320,30 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(const T* __restrict_
         ldv<VEC>(w + c, g);
 #pragma unroll
         for (int e = 0; e < VEC; e++) d[e] = (d[e] * g[e] - (n[e] - mu) * r * s1 - s2) * r;
-        stv<VEC>(dx + row * width + c, d);
+        stv<VEC>(dx + (int64_t)row * width + c, d);
       }
     }
   }
 }
 
-// out[c] = sum over n shares of part[p][c]: 16 threads a column, each every 16th share.
+// out[c] = sum over n shares of part[p][c]: 32 threads a column, each every 32nd share.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float* __restrict__ part, int n, int width, T* __restrict__ dw,
                                                            T* __restrict__ db) {
-  __shared__ float sum[16][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6;
+  __shared__ float sum[32][33];
+  const int x = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
   const float* p = part + (size_t)blockIdx.y * n * width;
   float s = 0.f;
-  if (c < width)
-    for (int i = k; i < n; i += 16) s += p[(size_t)i * width + c];
-  sum[k][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (k == 0 && c < width) {
-    s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; i++) s += sum[i][threadIdx.x & 63];
-    st1((blockIdx.y ? db : dw) + c, s);
+  if (c < width) {
+#pragma unroll 8
+    for (int i = k; i < n; i += 32) s += p[(size_t)i * width + c];
   }
+  sum[k][x] = s;
+  __syncthreads();
+  s = sum[x][k];      // column k, shares x
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if (x == 0 && blockIdx.x * 32 + k < width) st1((blockIdx.y ? db : dw) + blockIdx.x * 32 + k, s);
 }
 
 // Threads that hold a row, and pieces of a row a thread holds (0: the row is read again instead).
@@ -292,9 +352,9 @@ RowPlan row_plan(int width, int vec) {
   const int n = (width + vec - 1) / vec;
   for (int l = 8; l <= 64; l *= 2)
     if (n <= l) return {l, 1};
-  for (int v = 2; v <= 8; v *= 2)
+  for (int v : {2, 3, 4, 5, 6, 8})
     if (n <= 64 * v) return {64, v};
-  for (int v = 4; v <= 8; v *= 2)
+  for (int v : {3, 4, 6, 8})
     if (n <= 256 * v) return {256, v};
   return {256, 0};
 }
@@ -305,13 +365,20 @@ void with_row_plan(const RowPlan& p, F f) {
   };
 #define RL_I(x) std::integral_constant<int, x>()
   is(RL_I(8), RL_I(1)); is(RL_I(16), RL_I(1)); is(RL_I(32), RL_I(1)); is(RL_I(64), RL_I(1)); is(RL_I(64), RL_I(2));
-  is(RL_I(64), RL_I(4)); is(RL_I(64), RL_I(8)); is(RL_I(256), RL_I(4)); is(RL_I(256), RL_I(8)); is(RL_I(256), RL_I(0));
+  is(RL_I(64), RL_I(3)); is(RL_I(64), RL_I(4)); is(RL_I(64), RL_I(5)); is(RL_I(64), RL_I(6)); is(RL_I(64), RL_I(8));
+  is(RL_I(256), RL_I(3)); is(RL_I(256), RL_I(4)); is(RL_I(256), RL_I(6)); is(RL_I(256), RL_I(8)); is(RL_I(256), RL_I(0));
 #undef RL_I
 }
-// Workgroups of the backward pass: two a CU, each with several rows.
-int norm_shares(int64_t rows, const RowPlan& p) {
-  const int64_t n = (rows + 256 / p.L - 1) / (256 / p.L);
-  return (int)(n < 512 ? n : 512);
+// Workgroups of the backward pass: one a CU; of four waves (rows that take a workgroup), two.
+const int kShares = 512;
+constexpr int norm_threads(int L, int NV, int vec, bool biased) {
+  const int regs = NV * (vec * (biased ? 2 : 1) + (vec == 8 ? 20 : 14)) + 45;      // what the compiler takes, about
+  return L == 256 || regs > 256 ? 256 : regs > 128 ? 512 : 1024;
+}
+int norm_shares(int rows, const RowPlan& p, int vec, bool biased) {
+  const int threads = norm_threads(p.L, p.NV, vec, biased), group = threads / p.L, most = threads == 256 ? 512 : 256;
+  const int n = (rows - 1) / group + 1;
+  return n < most ? n : most;
 }
 template <typename T>
 constexpr int kVec = 16 / sizeof(T);
@@ -322,7 +389,7 @@ int norm_forward(const void* x, const Rows& rows, int width, const void* w, cons
   const RowPlan p = row_plan(width, VEC);
   with_row_plan(p, [&](auto l, auto v) {
     constexpr int L = decltype(l)::value, NV = decltype(v)::value;
-    norm_forward_kernel<T, VEC, L, NV><<<(unsigned)((rows.n + 256 / L - 1) / (256 / L)), 256, 0, s>>>(
+    norm_forward_kernel<T, VEC, L, NV><<<(unsigned)((rows.n - 1) / (256 / L) + 1), 256, 0, s>>>(
         (const T*)x, rows, width, (const T*)w, (const T*)b, eps, centered, (T*)y, mean, rstd);
   });
   return launched();
@@ -331,20 +398,23 @@ template <typename T, int VEC>
 int norm_backward(const void* dy, const Rows& drows, const void* x, const Rows& rows, int width, const void* w, const float* mean,
                   const float* rstd, int centered, void* dx, void* dw, void* db, float* part, hipStream_t s) {
   const RowPlan p = row_plan(width, VEC);
-  const int n = norm_shares(rows.n, p);
+  const int n = norm_shares(rows.n, p, VEC, db != nullptr);
   with_row_plan(p, [&](auto l, auto v) {
     constexpr int L = decltype(l)::value, NV = decltype(v)::value;
-    norm_backward_kernel<T, VEC, L, NV><<<n, 256, 0, s>>>((const T*)dy, drows, (const T*)x, rows, width, (const T*)w, mean, rstd,
-                                                         centered, db != nullptr, (T*)dx, part);
+    auto go = [&](auto biased) {
+      constexpr int THREADS = norm_threads(L, NV, VEC, decltype(biased)::value);
+      norm_backward_kernel<T, VEC, L, NV, decltype(biased)::value, THREADS><<<n, THREADS, 0, s>>>(
+          (const T*)dy, drows, (const T*)x, rows, width, (const T*)w, mean, rstd, centered, (T*)dx, part);
+    };
+    if (db) go(std::true_type());
+    else go(std::false_type());
   });
-  norm_reduce_kernel<T><<<dim3((width + 63) / 64, db ? 2 : 1), 1024, 0, s>>>(part, n, width, (T*)dw, (T*)db);
+  norm_reduce_kernel<T><<<dim3((width + 31) / 32, db ? 2 : 1), 1024, 0, s>>>(part, n, width, (T*)dw, (T*)db);
   return launched();
 }
 
-const int64_t kMaxRows = 1ll << 36;      // (row, piece) counts stay inside a grid of 2^31 - 1 workgroups
-
 const char* norm_argument(const void* x, int64_t outer, int32_t inner, int32_t width, int32_t dtype) {
-  if (outer < 0 || inner < 1 || width < 1 || outer > kMaxRows / inner / 64) return "outer, inner or width out of range";
+  if (outer < 0 || inner < 1 || width < 1 || outer > 0x7fffffff / inner) return "outer, inner or width out of range (rows: below 2^31)";
   if (dtype != RL_DTYPE_F32 && dtype != RL_DTYPE_BF16) return "dtype is RL_DTYPE_F32 or RL_DTYPE_BF16";
   if (outer > 0 && !x) return "null pointer";
   return nullptr;
@@ -359,7 +429,7 @@ extern "C" int rl_norm_forward(const void* d_x, int64_t outer, int32_t inner, in
   if (!(eps >= 0.f)) return rl_fail(RL_E_ARG, "eps is negative or no number");
   if (outer == 0) return RL_OK;
   if (!d_weight || !d_y || !d_rstd || (centered && !d_mean)) return rl_fail(RL_E_ARG, "null pointer");
-  const Rows rows{outer * inner, outer_stride, inner_stride, inner};
+  const Rows rows(outer * inner, outer_stride, inner_stride, inner);
   auto vec = [&](int n) {
     return width % n == 0 && outer_stride % n == 0 && (inner == 1 || inner_stride % n == 0) && aligned16(d_x) && aligned16(d_weight) &&
            aligned16(d_bias) && aligned16(d_y);
@@ -373,7 +443,7 @@ extern "C" int rl_norm_forward(const void* d_x, int64_t outer, int32_t inner, in
 
 extern "C" int64_t rl_norm_workspace(int64_t rows, int32_t width, int32_t biased) {
   if (rows < 0 || width < 1) return 0;
-  const int64_t n = rows < 512 ? rows : 512;      // as many shares as any plan makes
+  const int64_t n = rows < kShares ? rows : kShares;      // as many shares as any plan makes
   return n * width * (biased ? 2 : 1) * (int64_t)sizeof(float);
 }
 
@@ -386,7 +456,7 @@ extern "C" int rl_norm_backward(const void* d_dy, int64_t dy_outer_stride, int64
   if (outer > 0 && (!d_dy || !d_rstd || !d_dx || !d_workspace || (centered && !d_mean))) return rl_fail(RL_E_ARG, "null pointer");
   if (workspace_bytes < rl_norm_workspace(outer * inner, width, d_dbias != nullptr)) return rl_fail(RL_E_ARG, "workspace smaller than rl_norm_workspace says");
   if ((uintptr_t)d_workspace & 3) return rl_fail(RL_E_ARG, "workspace not aligned to 4 bytes");
-  const Rows rows{outer * inner, outer_stride, inner_stride, inner}, drows{outer * inner, dy_outer_stride, dy_inner_stride, inner};
+  const Rows rows(outer * inner, outer_stride, inner_stride, inner), drows(outer * inner, dy_outer_stride, dy_inner_stride, inner);
   auto vec = [&](int n) {
     return width % n == 0 && outer_stride % n == 0 && dy_outer_stride % n == 0 &&
            (inner == 1 || (inner_stride % n == 0 && dy_inner_stride % n == 0)) && aligned16(d_x) && aligned16(d_dy) && aligned16(d_weight) &&
@@ -397,9 +467,9 @@ extern "C" int rl_norm_backward(const void* d_dy, int64_t dy_outer_stride, int64
   norm_backward<T, V>(d_dy, drows, d_x, rows, width, d_weight, d_mean, d_rstd, centered, d_dx, d_dweight, d_dbias, (float*)d_workspace, s)
   if (outer == 0) {      // no rows: sums of nothing
     if (dtype == RL_DTYPE_F32)
-      norm_reduce_kernel<float><<<dim3((width + 63) / 64, d_dbias ? 2 : 1), 1024, 0, s>>>(nullptr, 0, width, (float*)d_dweight, (float*)d_dbias);
+      norm_reduce_kernel<float><<<dim3((width + 31) / 32, d_dbias ? 2 : 1), 1024, 0, s>>>(nullptr, 0, width, (float*)d_dweight, (float*)d_dbias);
     else
-      norm_reduce_kernel<bf16_t><<<dim3((width + 63) / 64, d_dbias ? 2 : 1), 1024, 0, s>>>(nullptr, 0, width, (bf16_t*)d_dweight, (bf16_t*)d_dbias);
+      norm_reduce_kernel<bf16_t><<<dim3((width + 31) / 32, d_dbias ? 2 : 1), 1024, 0, s>>>(nullptr, 0, width, (bf16_t*)d_dweight, (bf16_t*)d_dbias);
     return launched();
   }
   if (dtype == RL_DTYPE_F32) return vec(4) ? RL_GO(float, 4) : RL_GO(float, 1);
