@@ -369,7 +369,7 @@ Workspace plan(int64_t rows, int hidden, int vocab, int dtype, bool backward) {
   w.target = take(w.padded * 4);
   w.rows = take(w.padded * w.ld * el);
   if (!backward) {
-    w.strips = (vocab + 127) / 128;
+    w.strips = (vocab + 63) / 64;      // as many as any tile leaves
     w.zt = take(w.padded * 4);
     w.part = take(w.padded * w.strips * 8);
     return w;
@@ -380,12 +380,11 @@ Workspace plan(int64_t rows, int hidden, int vocab, int dtype, bool backward) {
   const int64_t fit = std::max<int64_t>(std::min<int64_t>(kPieceBytes / (w.padded * el), ((1ll << 31) - (1 << 20)) / (hidden * el)) / 256 * 256, 1024);
   const int64_t pieces = (vocab + fit - 1) / fit;
   w.width = (int)up((vocab + pieces - 1) / pieces, 256);
-  // bf16: 0.6 us for 32 k of a tile of 256 rows, 0.35 of 128 rows, measured; fp32: 1.8.  Up to 64 slices, 512 MB of sums.
-  w.slices.rows = el == 2 ? token_logprob_tile_rows((int)rows) : 128;
-  w.slices.tiles_j = el == 2 ? (hidden + 255) / 256 : (hidden + 127) / 128;
+  // slices of the vocabulary in dz W: up to 64, 512 MB of sums
+  if (el == 2) token_logprob_slice_tile<bf16_t>((int)rows, hidden, w.slices);
+  else token_logprob_slice_tile<float>((int)rows, hidden, w.slices);
   w.slices.width = w.width;
   w.slices.most = (int)std::max<int64_t>(std::min({(int64_t)64, kPieceBytes / 2 / (w.padded * hidden * 4), (int64_t)w.width / 256}), 1);
-  w.slices.chunk_us = el == 2 ? (w.slices.rows == 256 ? 0.6f : 0.35f) : 1.8f;
   w.slices.slice_us = (float)(hidden * 8 / 4.8e6);
   w.ldz = w.width + 128;
   w.dz = take(w.padded * w.ldz * el);
@@ -419,19 +418,14 @@ int forward(const void* h, int64_t stride, int rows, int hidden, const void* wei
   keep_rows_kernel<<<1, 1024, 0, s>>>(targets, rows, vocab, nullptr, nullptr, inv_t, (int32_t*)(ws + w.count), (int32_t*)(ws + w.list),
                                       nullptr, (int32_t*)(ws + w.target), nullptr, nullptr, logp, lse, SliceRule{});
   gather<T>(h, stride, hidden, w, ws, s);
-  int strips = w.strips;
-  bool mfma = false;
-  if constexpr (sizeof(T) == 2) {
-    mfma = token_logprob_takes_mfma(w.padded, w.ld, hidden, 0, weight, nullptr);
-    if (mfma) {
-      strips = (vocab + kStripMfma - 1) / kStripMfma;
-      launch_logits_strips_mfma(s, (const bf16_t*)(ws + w.rows), w.ld, rows, w.padded, (const bf16_t*)weight, vocab, hidden, kept, inv_t,
-                                (float2*)(ws + w.part), (float*)(ws + w.zt));
-    }
-  }
+  int strips = (vocab + 127) / 128;
+  const bool mfma = token_logprob_takes_mfma<T>(w.padded, w.ld, hidden, 0, weight, nullptr);
+  if (mfma)
+    strips = launch_logits_strips_mfma<T>(s, (const T*)(ws + w.rows), w.ld, rows, w.padded, (const T*)weight, vocab, hidden, kept, inv_t,
+                                          (float2*)(ws + w.part), (float*)(ws + w.zt));
   const int vec = hidden % (16 / sizeof(T)) == 0 && aligned16(weight);
   if (!mfma)
-    logits_strip_kernel<T><<<dim3((rows + 127) / 128, w.strips), 256, 0, s>>>((const T*)(ws + w.rows), w.ld, (const T*)weight, hidden, vocab, hidden,
+    logits_strip_kernel<T><<<dim3((rows + 127) / 128, strips), 256, 0, s>>>((const T*)(ws + w.rows), w.ld, (const T*)weight, hidden, vocab, hidden,
                                                                            vec, kept, inv_t, (float2*)(ws + w.part), (int)w.padded,
                                                                            (float*)(ws + w.zt));
   join_strips_kernel<<<(rows + 63) / 64, 1024, 0, s>>>((const float2*)(ws + w.part), strips, (int)w.padded, (const float*)(ws + w.zt),
@@ -451,19 +445,17 @@ int backward(const float* g, const void* h, int64_t stride, int rows, int hidden
   const int vec = hidden % (16 / sizeof(T)) == 0 && aligned16(weight);
   const T *hr = (const T*)(ws + w.rows), *wt = (const T*)weight;
   T* dz = (T*)(ws + w.dz);
-  const bool mfma = sizeof(T) == 2 && token_logprob_takes_mfma(w.padded, w.ld, hidden, w.ldz, weight, dw);
+  const bool mfma = token_logprob_takes_mfma<T>(w.padded, w.ld, hidden, w.ldz, weight, dw);
   const unsigned rt = (rows + 127) / 128, ht = (hidden + 127) / 128;
   for (int v0 = 0; v0 < vocab; v0 += w.width) {
     const VocabPiece piece{v0, std::min(w.width, vocab - v0), w.ldz};
     const unsigned vt = (piece.width + 127) / 128;
-    if constexpr (sizeof(T) == 2) {
-      if (mfma) {
-        launch_logits_gradient_mfma(s, hr, w.ld, rows, w.padded, wt, vocab, hidden, kept, inv_t, piece, dz);
-        launch_hidden_gradient_mfma(s, dz, piece, rows, w.padded, wt, vocab, hidden, kept, w.slices.most, (float*)(ws + w.dh),
-                                    (size_t)w.padded * hidden, v0 == 0);
-        launch_weight_gradient_mfma(s, dz, piece, hr, w.ld, w.padded, hidden, kept, (bf16_t*)dw);
-        continue;
-      }
+    if (mfma) {
+      launch_logits_gradient_mfma<T>(s, hr, w.ld, rows, w.padded, wt, vocab, hidden, kept, inv_t, piece, dz);
+      launch_hidden_gradient_mfma<T>(s, dz, piece, rows, w.padded, wt, vocab, hidden, kept, w.slices.most, (float*)(ws + w.dh),
+                                     (size_t)w.padded * hidden, v0 == 0);
+      launch_weight_gradient_mfma<T>(s, dz, piece, hr, w.ld, w.padded, hidden, kept, (T*)dw);
+      continue;
     }
     logits_gradient_kernel<T><<<dim3((unsigned)(w.padded / 128), vt), 256, 0, s>>>(hr, w.ld, wt, hidden, vocab, hidden, vec, kept, inv_t, piece, dz);
     hidden_gradient_kernel<T><<<dim3(rt, ht, w.slices.most), 256, 0, s>>>(dz, piece, wt, hidden, hidden, vec, kept.count,

@@ -1,4 +1,4 @@
-// The products of the token log-probs and of their gradient in bf16 on matrix instructions.
+// The products of the token log-probs and of their gradient on matrix instructions, operands straight from memory into LDS.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -9,27 +9,29 @@
 namespace {
 
 // =============================================================================================
-// One kernel for the four products, C[i, j] = sum_k A[i, k] B[j, k] over tiles of 64 MB rows i and 256 columns j, four waves of
-// 32 MB x 128 on 32x32x16 matrix instructions:
-//   logits          A = hidden rows            B = weights                epilogue: (max, sum) of a row's 256 logits, or dz
+// One kernel for the four products, C[i, j] = sum_k A[i, k] B[j, k] over tiles of 64 MB rows i and 64 NB columns j, four waves of
+// 32 MB x 32 NB on 32x32x16 (fp32: 32x32x2) matrix instructions:
+//   logits          A = hidden rows            B = weights                epilogue: (max, sum) of a tile's logits of a row, or dz
 //   dz W            A = dz                     B = weights, k-strided     epilogue: a slice's sum in 32 bits
-//   dz^T hidden     A = dz, k-strided          B = rows, k-strided        epilogue: bf16
+//   dz^T hidden     A = dz, k-strided          B = rows, k-strided        epilogue: rounded
 // Bound by the matrix units (2 flops x rows x hidden x vocab each, 2.5 PFLOP/s peak, held by power below 1.5 for random data), for few
-// rows by the weights' bytes.  A chunk of 32 k of both operands goes straight from memory into one of R stages in LDS, R - 1 ahead;
-// operands are read 16 k ahead of the instructions that use them, one barrier a chunk.
+// rows by the weights' bytes; fp32: 155 TFLOP/s.  A chunk of 64 bytes of k (32; fp32 16) of both operands goes straight from memory into
+// one of R stages in LDS, R - 1 ahead; operands are read half a chunk ahead of the instructions that use them, one barrier a chunk.
 // Operands as they lie in memory, no copy of the weights in another order:
 //   k-contiguous: [row][32 k], 64 bytes a row.  The 16-byte piece p of row r is kept at p ^ (r / 4 % 4), so the 16 rows that a
 //     read takes in one go lie in different banks.
-//   k-strided (TA, TB): [32 k][256 columns], 512 bytes a k, read with the transposing LDS read: 16 lanes take 4 k x 16 columns, lane i
-//     gets column i of the 4 k.  The 64-byte block b of row k is kept at b ^ (k % 4): the 4 k of a read lie in different banks.
+//   k-strided (TA, TB): [k][columns].  bf16: read with the transposing LDS read, 16 lanes take 4 k x 16 columns, lane i gets column i of
+//     the 4 k.  The 64-byte block b of row k is kept at b ^ (k % 4): the 4 k of a read lie in different banks.  fp32: read one by one, two
+//     blocks of row k and two of row k + 4 at once, which are kept at b ^ 2 (k / 4 % 2).
+// fp32 instructions take 2 k, of a lane's 16 bytes element e in step e: k = e and 4 + e of the eight, the same for both operands.
 // =============================================================================================
-constexpr int BN = 256;      // columns of a tile
 enum { EPI_STRIP, EPI_DZ, EPI_SLICE, EPI_OUT };
 
 typedef __attribute__((address_space(3))) char lds_char;
 
+template <typename T>
 struct Product {
-  const bf16_t *a, *b;
+  const T *a, *b;
   int64_t lda, ldb;
   int a_n, b_n;                  // rows of a, b in memory (k-strided: k that may be read)
   int tiles_i, tiles_j;          // tiles_i: upper bound where the count of kept rows decides
@@ -43,23 +45,24 @@ struct Product {
   int padded;
   float* zt;
   // results
-  bf16_t* out;
+  T* out;
   float* slice;
   size_t slice_stride;
   int64_t ldo;
   int out_rows, out_cols, first;
 };
 
-template <bool TA, bool TB, int MB, int R, int EPI>
-__global__ __launch_bounds__(256, 1) void product_kernel(Product P) {
+template <typename T, bool TA, bool TB, int MB, int NB, int R, int EPI>
+__global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Product<T> P) {
   constexpr bool SWAP = EPI != EPI_SLICE;        // a lane holds one row's values, else one column's
-  constexpr int NA = 4 * MB, PW = MB + 4, BUF = (NA + 16) * 1024, F = PW / 2;
-  static_assert(!TA || MB == 4, "a k-strided A has 256 columns");
+  constexpr int BM = 64 * MB, BN = 64 * NB, EL = sizeof(T), KC = 64 / EL, V = 16 / EL;
+  constexpr int NA = 4 * MB, PW = MB + NB, BUF = (NA + 4 * NB) * 1024, F = PW / 2;
+  static_assert((!TA || BM * EL >= 256) && (!TB || BN * EL >= 256), "four blocks of 64 bytes a row");
   extern __shared__ u32x4 smem[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, wm = wave >> 1, wn = wave & 1;
   const int kept = __builtin_amdgcn_readfirstlane(*P.kept.count);
   // tiles that have work, numbered so that an XCD (workgroups are dealt to the 8 of them in turn) takes a compact block of one slice
-  const int ti = EPI == EPI_OUT ? P.tiles_i : min(P.tiles_i, (kept + 64 * MB - 1) / (64 * MB)), tiles = ti * P.tiles_j;
+  const int ti = EPI == EPI_OUT ? P.tiles_i : min(P.tiles_i, (kept + BM - 1) / BM), tiles = ti * P.tiles_j;
   const int slices = EPI == EPI_SLICE ? __builtin_amdgcn_readfirstlane(P.kept.count[1]) : 1, total = tiles * slices;
   if ((int)blockIdx.x >= total) return;
   int i0, j0, z;
@@ -68,82 +71,97 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Product P) {
     z = vid / tiles;
     const int v = vid - z * tiles, per = P.group * P.tiles_j, grp = v / per, first = grp * P.group, gm = min(P.group, ti - first), in = v - grp * per;
     // the divisions leave them in vector registers
-    i0 = __builtin_amdgcn_readfirstlane(first + in % gm) * 64 * MB;
+    i0 = __builtin_amdgcn_readfirstlane(first + in % gm) * BM;
     j0 = __builtin_amdgcn_readfirstlane(in / gm) * BN;
     z = __builtin_amdgcn_readfirstlane(z);
   }
   const int k_all = EPI == EPI_OUT ? kept : P.k, per_slice = EPI == EPI_SLICE ? __builtin_amdgcn_readfirstlane(P.kept.count[2]) : k_all;
-  const int k_lo = z * per_slice, c0 = k_lo >> 5, c1 = (min(k_all, k_lo + per_slice) + 31) >> 5;
+  const int k_lo = z * per_slice, c0 = k_lo / KC, c1 = (min(k_all, k_lo + per_slice) + KC - 1) / KC;
   // operands behind these descriptors: what is read past their end arrives as zeros
-  const u32x4 ra = TA ? buffer_rsrc(P.a + i0, (unsigned)(((int64_t)P.a_n * P.lda - i0) * 2))
-                      : buffer_rsrc(P.a + (int64_t)i0 * P.lda, (unsigned)((int64_t)min(P.a_n - i0, 64 * MB) * P.lda * 2));
-  const u32x4 rb = TB ? buffer_rsrc(P.b + j0, (unsigned)(((int64_t)P.b_n * P.ldb - j0) * 2))
-                      : buffer_rsrc(P.b + (int64_t)j0 * P.ldb, (unsigned)((int64_t)min(P.b_n - j0, BN) * P.ldb * 2));
+  const u32x4 ra = TA ? buffer_rsrc(P.a + i0, (unsigned)(((int64_t)P.a_n * P.lda - i0) * EL))
+                      : buffer_rsrc(P.a + (int64_t)i0 * P.lda, (unsigned)((int64_t)min(P.a_n - i0, BM) * P.lda * EL));
+  const u32x4 rb = TB ? buffer_rsrc(P.b + j0, (unsigned)(((int64_t)P.b_n * P.ldb - j0) * EL))
+                      : buffer_rsrc(P.b + (int64_t)j0 * P.ldb, (unsigned)((int64_t)min(P.b_n - j0, BN) * P.ldb * EL));
   const unsigned sa = TA ? (unsigned)P.lda * 64u : 64u, sb = TB ? (unsigned)P.ldb * 64u : 64u;      // bytes of a chunk's step
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
-  int va[MB], vb[4];      // this lane's offset of each piece that its wave loads
-  auto offset = [&](int piece, int64_t ld, bool strided) {
+  int va[MB], vb[NB];      // this lane's offset of each piece that its wave loads
+  auto offset = [&](int piece, int64_t ld, bool strided, int row_bytes) {
     const int n = piece * 4 + wave;
     if (strided) {
-      const int k = n * 2 + (lane >> 5);
-      return (int)(k * ld * 2) + ((((lane & 31) >> 2) ^ (k & 3)) << 6) + ((lane & 3) << 4);
+      const int lanes = row_bytes / 16, k = n * (64 / lanes) + lane / lanes, p = lane % lanes;
+      const int block = (p >> 2) ^ (EL == 2 ? k & 3 : (k >> 2 & 1) << 1);
+      return (int)(k * ld * EL) + (block << 6) + ((p & 3) << 4);
     }
-    return (int)((n * 16 + (lane >> 2)) * ld * 2) + (((lane & 3) ^ (lane >> 4 & 3)) << 4);
+    return (int)((n * 16 + (lane >> 2)) * ld * EL) + (((lane & 3) ^ (lane >> 4 & 3)) << 4);
   };
 #pragma unroll
-  for (int j = 0; j < MB; j++) va[j] = offset(j, P.lda, TA);
+  for (int j = 0; j < MB; j++) va[j] = offset(j, P.lda, TA, BM * EL);
 #pragma unroll
-  for (int j = 0; j < 4; j++) vb[j] = offset(j, P.ldb, TB);
+  for (int j = 0; j < NB; j++) vb[j] = offset(j, P.ldb, TB, BN * EL);
   // piece j of this wave of a chunk; chunks behind the slice's end: the last one again, never read
   auto load = [&](int chunk, int j, int stage) {
     const unsigned dst = lds0 + (unsigned)stage * BUF + (unsigned)(j * 4 + wave) * 1024u, c = (unsigned)min(chunk, c1 - 1);
     if (j < MB) load_to_lds(dst, va[j], ra, c * sa);
     else load_to_lds(dst, vb[j - MB], rb, c * sb);
   };
-  f32x16 acc[MB][4];
+  f32x16 acc[MB][NB];
 #pragma unroll
   for (int a = 0; a < MB; a++)
 #pragma unroll
-    for (int b = 0; b < 4; b++)
+    for (int b = 0; b < NB; b++)
 #pragma unroll
       for (int e = 0; e < 16; e++) acc[a][b][e] = 0.f;
   auto mfma = [&](const u32x4& row, const u32x4& col, f32x16& c) {
-    c = SWAP ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, col), __builtin_bit_cast(bf16x8, row), c, 0, 0, 0)
-             : __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, row), __builtin_bit_cast(bf16x8, col), c, 0, 0, 0);
-  };
-  // lane parts of the operand reads: k-contiguous by 16-k half, k-strided by 32-column block
-  int la[TA ? 4 : 2], lb[TB ? 4 : 2];
-  auto part = [&](int (&l)[4]) {
-    const int s = lane >> 2 & 3;
+    const u32x4 &x = SWAP ? col : row, &y = SWAP ? row : col;
+    if constexpr (EL == 2) {
+      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
+    } else {
+      const f32x4 u = __builtin_bit_cast(f32x4, x), w = __builtin_bit_cast(f32x4, y);
 #pragma unroll
-    for (int x = 0; x < 4; x++) l[x] = ((lane >> 5) * 8 + s) * 512 + ((x ^ s) << 6) + ((lane >> 4 & 1) << 5) + ((lane & 3) << 3);
+      for (int e = 0; e < 4; e++) c = __builtin_amdgcn_mfma_f32_32x32x2f32(u[e], w[e], c, 0, 0, 0);
+    }
   };
-  auto part2 = [&](int (&l)[2]) {
+  // lane parts of the operand reads: k-contiguous by half a chunk, k-strided by 32-column block
+  int la[TA ? MB : 2], lb[TB ? NB : 2];
+  auto part = [&](int x, int row_bytes) {
+    if constexpr (EL == 2) {
+      const int s = lane >> 2 & 3;
+      return ((lane >> 5) * 8 + s) * row_bytes + ((x ^ s) << 6) + ((lane >> 4 & 1) << 5) + ((lane & 3) << 3);
+    } else {
+      return (lane >> 5) * 4 * row_bytes + (((2 * x) ^ (lane >> 5 << 1)) << 6) + ((lane & 31) << 2);
+    }
+  };
+  auto part2 = [&](int x) { return (lane & 31) * 64 + (((x * 2 + (lane >> 5)) ^ (lane >> 2 & 3)) << 4); };
 #pragma unroll
-    for (int x = 0; x < 2; x++) l[x] = (lane & 31) * 64 + (((x * 2 + (lane >> 5)) ^ (lane >> 2 & 3)) << 4);
-  };
-  if constexpr (TA) part(la);
-  else part2(la);
-  if constexpr (TB) part(lb);
-  else part2(lb);
+  for (int x = 0; x < (TA ? MB : 2); x++) la[x] = TA ? part(wm * MB + x, BM * EL) : part2(x);
+#pragma unroll
+  for (int x = 0; x < (TB ? NB : 2); x++) lb[x] = TB ? part(wn * NB + x, BN * EL) : part2(x);
   lds_char* const lds = (lds_char*)(__attribute__((address_space(3))) void*)smem;
-  auto strided = [&](int at) {
-    typedef __attribute__((address_space(3))) s16x4 l4;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((l4*)(lds + at)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((l4*)(lds + at + 2048));
-    return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  auto strided = [&](int at, auto row_bytes) {
+    constexpr int RB = decltype(row_bytes)::value;
+    if constexpr (EL == 2) {
+      typedef __attribute__((address_space(3))) s16x4 l4;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((l4*)(lds + at)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((l4*)(lds + at + 4 * RB));
+      return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      u32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; e++) v[e] = *(__attribute__((address_space(3))) unsigned*)(lds + at + e * RB);
+      return v;
+    }
   };
   auto read_a = [&](int x, int kb, int stage) {
     const int base = stage * BUF;
-    if constexpr (TA) return strided(base + kb * 8192 + wm * 256 + la[x]);
+    if constexpr (TA) return strided(base + kb * (KC / 2) * BM * EL + la[x], std::integral_constant<int, BM * EL>());
     else return *(__attribute__((address_space(3))) u32x4*)(lds + base + (wm * MB + x) * 2048 + la[kb]);
   };
   auto read_b = [&](int x, int kb, int stage) {
     const int base = stage * BUF + NA * 1024;
-    if constexpr (TB) return strided(base + kb * 8192 + wn * 256 + lb[x]);
-    else return *(__attribute__((address_space(3))) u32x4*)(lds + base + (wn * 4 + x) * 2048 + lb[kb]);
+    if constexpr (TB) return strided(base + kb * (KC / 2) * BN * EL + lb[x], std::integral_constant<int, BN * EL>());
+    else return *(__attribute__((address_space(3))) u32x4*)(lds + base + (wn * NB + x) * 2048 + lb[kb]);
   };
   if (c1 > c0) {
-    u32x4 av[2][MB], bv[2][4];
+    u32x4 av[2][MB], bv[2][NB];
 #pragma unroll
     for (int c = 0; c < R - 1; c++)
 #pragma unroll
@@ -155,7 +173,7 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Product P) {
 #pragma unroll
     for (int x = 0; x < MB; x++) av[0][x] = read_a(x, 0, 0);
 #pragma unroll
-    for (int x = 0; x < 4; x++) bv[0][x] = read_b(x, 0, 0);
+    for (int x = 0; x < NB; x++) bv[0][x] = read_b(x, 0, 0);
     int sc = 0, sl = R - 1;                  // stages of chunks c and c + R - 1 (that of chunk c - 1)
     for (int c = c0; c < c1; c++) {
       const int sn = sc + 1 == R ? 0 : sc + 1;
@@ -169,11 +187,10 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Product P) {
         }
         const int stage = st == 0 ? sc : sn, kb = 1 - st;
         // the operands of the next 16 k, in the order of their use
-        constexpr int order[8] = {0, MB, MB + 1, MB + 2, MB + 3, 1, 2, 3};
 #pragma unroll
-        for (int q = 0; q < MB + 4; q++)
-          if (q * MB / (MB + 4) == a) {
-            const int x = order[q];
+        for (int q = 0; q < MB + NB; q++)
+          if (q * MB / (MB + NB) == a) {
+            const int x = q == 0 ? 0 : q <= NB ? MB + q - 1 : q - NB;
             if (x < MB) av[1 - st][x] = read_a(x, kb, stage);
             else bv[1 - st][x - MB] = read_b(x - MB, kb, stage);
           }
@@ -184,7 +201,7 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Product P) {
           if (st == 1 && j < F && j * MB / F == a) load(c + R, j, sc);
         }
 #pragma unroll
-        for (int b = 0; b < 4; b++) mfma(av[st][a], bv[st][b], acc[a][b]);
+        for (int b = 0; b < NB; b++) mfma(av[st][a], bv[st][b], acc[a][b]);
         __builtin_amdgcn_sched_barrier(0);
       }
       sl = sc;
@@ -208,8 +225,8 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Product P) {
 #pragma unroll
     for (int a = 0; a < MB; a++) {
 #pragma unroll
-      for (int b = 0; b < 4; b++) {
-        const int j = wn * 128 + b * 32 + (lane & 31), r = (wm * MB + a) * 32 + 4 * (lane >> 5);
+      for (int b = 0; b < NB; b++) {
+        const int j = wn * 32 * NB + b * 32 + (lane & 31), r = (wm * MB + a) * 32 + 4 * (lane >> 5);
         if (j0 + j < P.out_cols) {
           const unsigned at = (unsigned)r * ld + j;
 #pragma unroll
@@ -225,7 +242,7 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Product P) {
     }
     return;
   }
-  const int jw = wn * 128 + 4 * (lane >> 5);      // column of register e of block b: jw + 32 b + 8 (e / 4) + e % 4
+  const int jw = wn * 32 * NB + 4 * (lane >> 5);      // column of register e of block b: jw + 32 b + 8 (e / 4) + e % 4
   const bool crosses = (EPI == EPI_STRIP || EPI == EPI_DZ) && P.v0 + j0 + BN > P.vocab;
   if constexpr (EPI == EPI_STRIP) {
     float2* half = (float2*)smem;
@@ -240,7 +257,7 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Product P) {
           return decltype(some)::value && j0 + j >= P.vocab ? -INFINITY : v;
         };
 #pragma unroll
-        for (int b = 0; b < 4; b++)
+        for (int b = 0; b < NB; b++)
 #pragma unroll
           for (int e = 0; e < 16; e++) {
             const float v = at(b, e);
@@ -250,27 +267,27 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Product P) {
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         const float ref = top == -INFINITY ? 0.f : top * P.scale;
 #pragma unroll
-        for (int b = 0; b < 4; b++)
+        for (int b = 0; b < NB; b++)
 #pragma unroll
           for (int e = 0; e < 16; e++) sum += __builtin_amdgcn_exp2f(fmaf(at(b, e), P.scale, -ref));
         sum += __shfl_xor(sum, 32, 64);
       };
       if (crosses || __any(y >= 0 && y < BN)) strip(std::true_type());
       else strip(std::false_type());
-      if (lane < 32) half[wn * 64 * MB + il] = make_float2(top, sum);
+      if (lane < 32) half[wn * BM + il] = make_float2(top, sum);
       __builtin_amdgcn_sched_barrier(0);      // one row block at a time
     }
     __syncthreads();
-    if (tid < 64 * MB && i0 + tid < kept) {
-      const float2 a = half[tid], b = half[64 * MB + tid];
+    if (tid < BM && i0 + tid < kept) {
+      const float2 a = half[tid], b = half[BM + tid];
       const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.f : top;
       P.part[(size_t)(j0 / BN) * P.padded + i0 + tid] =
           make_float2(top * P.inv_t, a.y * exp2f((a.x - ref) * P.scale) + b.y * exp2f((b.x - ref) * P.scale));
     }
     return;
   }
-  // bf16 tile through LDS: rows of 512 bytes, 16 apart
-  constexpr int PITCH = BN * 2 + 16;
+  // the tile through LDS, rows 16 bytes apart
+  constexpr int PITCH = BN * EL + 16;
 #pragma unroll
   for (int a = 0; a < MB; a++) {
     const int il = (wm * MB + a) * 32 + (lane & 31);
@@ -278,12 +295,12 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Product P) {
       const int i = i0 + il, y = P.kept.target[i] - P.v0 - j0;
       const float g = P.kept.g[i], l = P.kept.lse[i] * 1.44269504f;
 #pragma unroll
-      for (int b = 0; b < 4; b++)
+      for (int b = 0; b < NB; b++)
 #pragma unroll
         for (int e = 0; e < 16; e++) acc[a][b][e] = -g * __builtin_amdgcn_exp2f(fmaf(acc[a][b][e], P.scale, -l));
       if (crosses || __any(y >= 0 && y < BN)) {
 #pragma unroll
-        for (int b = 0; b < 4; b++)
+        for (int b = 0; b < NB; b++)
 #pragma unroll
           for (int e = 0; e < 16; e++) {
             const int j = jw + 32 * b + 8 * (e >> 2) + (e & 3);
@@ -294,104 +311,150 @@ __global__ __launch_bounds__(256, 1) void product_kernel(Product P) {
     }
     auto out = [&](int b, int e) { return EPI == EPI_DZ ? acc[a][b][e] : val(a, b, e); };
 #pragma unroll
-    for (int b = 0; b < 4; b++)
+    for (int b = 0; b < NB; b++)
 #pragma unroll
       for (int q = 0; q < 4; q++) {
-        typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
-        const bf16x4 w = {(__bf16)out(b, 4 * q), (__bf16)out(b, 4 * q + 1), (__bf16)out(b, 4 * q + 2), (__bf16)out(b, 4 * q + 3)};
-        *(__attribute__((address_space(3))) bf16x4*)(lds + il * PITCH + (jw + 32 * b + 8 * q) * 2) = w;
+        lds_char* const to = lds + il * PITCH + (jw + 32 * b + 8 * q) * EL;
+        if constexpr (EL == 2) {
+          typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
+          *(__attribute__((address_space(3))) bf16x4*)to = bf16x4{(__bf16)out(b, 4 * q), (__bf16)out(b, 4 * q + 1), (__bf16)out(b, 4 * q + 2), (__bf16)out(b, 4 * q + 3)};
+        } else {
+          *(__attribute__((address_space(3))) f32x4*)to = f32x4{out(b, 4 * q), out(b, 4 * q + 1), out(b, 4 * q + 2), out(b, 4 * q + 3)};
+        }
         if (q == 3) __builtin_amdgcn_sched_barrier(0);
       }
   }
   __syncthreads();
-  const int c = (tid & 31) * 8;
+  constexpr int LANES = BN / V;      // of a row
+  const int c = tid % LANES * V;
   if (j0 + c < P.out_cols) {
 #pragma unroll 4
-    for (int r = tid >> 5; r < 64 * MB; r += 8) {
+    for (int r = tid / LANES; r < BM; r += 256 / LANES) {
       if (i0 + r >= P.out_rows) break;
-      const u32x4 v = *(__attribute__((address_space(3))) u32x4*)(lds + r * PITCH + c * 2);
+      const u32x4 v = *(__attribute__((address_space(3))) u32x4*)(lds + r * PITCH + c * EL);
       __builtin_nontemporal_store(v, (u32x4*)(P.out + (int64_t)(i0 + r) * P.ldo + j0 + c));
     }
   }
 }
 
-template <bool TA, bool TB, int MB, int R, int EPI>
-void go(const Product& p, hipStream_t s) {
-  constexpr int ring = R * (4 * MB + 16) * 1024, tile = 64 * MB * (BN * 2 + 16);
+template <typename T, bool TA, bool TB, int MB, int NB, int R, int EPI>
+void go(const Product<T>& p, hipStream_t s) {
+  constexpr int ring = R * (MB + NB) * 4096, tile = 64 * MB * (64 * NB * (int)sizeof(T) + 16);
   constexpr int lds = EPI != EPI_SLICE && tile > ring ? tile : ring;
+  auto kernel = product_kernel<T, TA, TB, MB, NB, R, EPI>;
   static std::atomic<uint64_t> done;      // more than 64 KB of LDS need an opt-in, once per kernel and device
   int dev = 0;
   (void)hipGetDevice(&dev);
   const uint64_t bit = 1ull << (dev & 63);
   if (!(done.load(std::memory_order_acquire) & bit)) {
-    (void)hipFuncSetAttribute((const void*)product_kernel<TA, TB, MB, R, EPI>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     done.fetch_or(bit, std::memory_order_release);
   }
-  product_kernel<TA, TB, MB, R, EPI><<<(unsigned)(p.tiles_i * p.tiles_j * p.slices), 256, lds, s>>>(p);
+  kernel<<<(unsigned)(p.tiles_i * p.tiles_j * p.slices), 256, lds, s>>>(p);
 }
 
-// rows of up to 128 take tiles of 128
-int row_blocks(int rows) { return rows <= 128 ? 2 : 4; }
+// Tile of a product, in 64 rows and 64 columns.  bf16: 256 x 256, for up to 128 rows 128 x 256.  fp32 (16 times the matrix time a byte):
+// 128 x 128, and 64 x 64 where those would leave CUs idle.
+struct Tile { int mb, nb; };
+template <typename T>
+Tile tile_of(int64_t rows, int64_t columns, int64_t slices, bool gathered) {
+  if (sizeof(T) == 2) return {gathered && rows <= 128 ? 2 : 4, 4};
+  const bool small = (rows + 127) / 128 * ((columns + 127) / 128) * slices < 256;
+  return {small ? 1 : 2, small ? 1 : 2};
+}
+template <typename T, bool TA, bool TB, int EPI>
+void go(Product<T>& p, const Tile& t, int64_t rows, int64_t columns, hipStream_t s) {
+  p.tiles_i = (int)((rows + 64 * t.mb - 1) / (64 * t.mb)), p.tiles_j = (int)((columns + 64 * t.nb - 1) / (64 * t.nb));
+  if constexpr (sizeof(T) == 2) {
+    if constexpr (!TA) {
+      if (t.mb == 2) return go<T, TA, TB, 2, 4, 6, EPI>(p, s);
+    }
+    go<T, TA, TB, 4, 4, 4, EPI>(p, s);
+  } else {
+    if (t.mb == 1) go<T, TA, TB, 1, 1, 8, EPI>(p, s);
+    else go<T, TA, TB, 2, 2, 4, EPI>(p, s);
+  }
+}
 
 }  // namespace
 
+template <typename T>
 bool token_logprob_takes_mfma(int64_t padded, int ld, int hidden, int width, const void* weight, const void* dweight) {
   // 32-bit offsets into one descriptor: the rows as k-strided operand, dz, a piece of the weights
-  const int64_t most = (1ll << 32) - (1 << 20);
-  return hidden % 8 == 0 && aligned16(weight) && aligned16(dweight) && padded * ld * 2 < most && padded * width * 2 < most &&
-         (int64_t)std::max(width, 256) * hidden * 2 < most / 2;
+  const int64_t most = (1ll << 32) - (1 << 20), el = sizeof(T);
+  return hidden % (16 / el) == 0 && aligned16(weight) && aligned16(dweight) && padded * ld * el < most && padded * width * el < most &&
+         (int64_t)std::max(width, 256) * hidden * el < most / 2;
 }
 
-int token_logprob_tile_rows(int rows) { return 64 * row_blocks(rows); }
+template <typename T>
+void token_logprob_slice_tile(int rows, int hidden, SliceRule& r) {
+  // us of a tile's 32 k, measured; fp32: two workgroups a CU share its matrix units.  64 x 64 tiles where 64 slices of 128 x 128 tiles are
+  // too few.
+  const Tile t = tile_of<T>(rows, hidden, 16, true);
+  r.rows = 64 * t.mb;
+  r.tiles_j = (hidden + 64 * t.nb - 1) / (64 * t.nb);
+  r.chunk_us = sizeof(T) == 2 ? (t.mb == 4 ? 0.6f : 0.35f) : t.mb == 2 ? 2.4f : 0.6f;
+}
 
-void launch_logits_strips_mfma(hipStream_t s, const bf16_t* h, int ld, int rows, int64_t padded, const bf16_t* w, int vocab, int hidden,
-                               const KeptRows& kept, float inv_t, float2* part, float* zt) {
-  Product p{};
-  const int mb = row_blocks(rows);
+template <typename T>
+int launch_logits_strips_mfma(hipStream_t s, const T* h, int ld, int rows, int64_t padded, const T* w, int vocab, int hidden,
+                              const KeptRows& kept, float inv_t, float2* part, float* zt) {
+  Product<T> p{};
   p.a = h, p.lda = ld, p.a_n = (int)padded;
   p.b = w, p.ldb = hidden, p.b_n = vocab;
-  p.tiles_i = (rows + 64 * mb - 1) / (64 * mb), p.tiles_j = (vocab + BN - 1) / BN;
-  p.k = (int)up(hidden, 32), p.slices = 1, p.group = 4;
+  p.k = hidden, p.slices = 1, p.group = 4;
   p.kept = kept, p.vocab = vocab, p.v0 = 0, p.scale = (float)(1.4426950408889634 * inv_t), p.inv_t = inv_t;
   p.part = part, p.padded = (int)padded, p.zt = zt;
-  if (mb == 4) go<false, false, 4, 4, EPI_STRIP>(p, s);
-  else go<false, false, 2, 6, EPI_STRIP>(p, s);
+  const Tile t = tile_of<T>(rows, vocab, 1, true);
+  go<T, false, false, EPI_STRIP>(p, t, rows, vocab, s);
+  return p.tiles_j;
 }
 
-void launch_logits_gradient_mfma(hipStream_t s, const bf16_t* h, int ld, int rows, int64_t padded, const bf16_t* w, int vocab, int hidden,
-                                 const KeptRows& kept, float inv_t, const VocabPiece& piece, bf16_t* dz) {
-  Product p{};
-  const int mb = row_blocks(rows);
+template <typename T>
+void launch_logits_gradient_mfma(hipStream_t s, const T* h, int ld, int rows, int64_t padded, const T* w, int vocab, int hidden,
+                                 const KeptRows& kept, float inv_t, const VocabPiece& piece, T* dz) {
+  Product<T> p{};
   p.a = h, p.lda = ld, p.a_n = (int)padded;
   p.b = w + (int64_t)piece.v0 * hidden, p.ldb = hidden, p.b_n = vocab - piece.v0;
-  p.tiles_i = (rows + 64 * mb - 1) / (64 * mb), p.tiles_j = (piece.width + BN - 1) / BN;
-  p.k = (int)up(hidden, 32), p.slices = 1, p.group = 4;
+  p.k = hidden, p.slices = 1, p.group = 4;
   p.kept = kept, p.vocab = vocab, p.v0 = piece.v0, p.scale = (float)(1.4426950408889634 * inv_t), p.inv_t = inv_t;
-  p.out = dz, p.ldo = piece.ld, p.out_rows = (int)padded, p.out_cols = (int)up(piece.width, BN);
-  if (mb == 4) go<false, false, 4, 4, EPI_DZ>(p, s);
-  else go<false, false, 2, 6, EPI_DZ>(p, s);
+  p.out = dz, p.ldo = piece.ld, p.out_rows = (int)padded, p.out_cols = (int)up(piece.width, 256);
+  // whole multiples of 256 columns: the products behind it read beyond the vocabulary's end
+  go<T, false, false, EPI_DZ>(p, tile_of<T>(rows, piece.width, 1, true), rows, p.out_cols, s);
 }
 
-void launch_hidden_gradient_mfma(hipStream_t s, const bf16_t* dz, const VocabPiece& piece, int rows, int64_t padded, const bf16_t* w, int vocab,
-                                 int hidden, const KeptRows& kept, int most_slices, float* dh, size_t slice_stride, bool first) {
-  Product p{};
-  const int mb = row_blocks(rows);
+template <typename T>
+void launch_hidden_gradient_mfma(hipStream_t s, const T* dz, const VocabPiece& piece, int rows, int64_t padded, const T* w, int vocab, int hidden,
+                                 const KeptRows& kept, int most_slices, float* dh, size_t slice_stride, bool first) {
+  Product<T> p{};
   p.a = dz, p.lda = piece.ld, p.a_n = (int)padded;
   p.b = w + (int64_t)piece.v0 * hidden, p.ldb = hidden, p.b_n = std::min(piece.ld, vocab - piece.v0);
-  p.tiles_i = (rows + 64 * mb - 1) / (64 * mb), p.tiles_j = (hidden + BN - 1) / BN;
   p.k = piece.width, p.slices = most_slices, p.group = 4;
   p.kept = kept, p.slice = dh, p.slice_stride = slice_stride, p.ldo = hidden, p.out_cols = hidden, p.first = first;
-  if (mb == 4) go<false, true, 4, 4, EPI_SLICE>(p, s);
-  else go<false, true, 2, 6, EPI_SLICE>(p, s);
+  go<T, false, true, EPI_SLICE>(p, tile_of<T>(rows, hidden, 16, true), rows, hidden, s);
 }
 
-void launch_weight_gradient_mfma(hipStream_t s, const bf16_t* dz, const VocabPiece& piece, const bf16_t* h, int ld, int64_t padded, int hidden,
-                                 const KeptRows& kept, bf16_t* dw) {
-  Product p{};
+template <typename T>
+void launch_weight_gradient_mfma(hipStream_t s, const T* dz, const VocabPiece& piece, const T* h, int ld, int64_t padded, int hidden,
+                                 const KeptRows& kept, T* dw) {
+  Product<T> p{};
   p.a = dz, p.lda = piece.ld, p.a_n = (int)padded;
   p.b = h, p.ldb = ld, p.b_n = (int)padded;
-  p.tiles_i = (piece.width + 255) / 256, p.tiles_j = (hidden + BN - 1) / BN;
   p.k = 0, p.slices = 1, p.group = 4;
   p.kept = kept, p.out = dw + (int64_t)piece.v0 * hidden, p.ldo = hidden, p.out_rows = piece.width, p.out_cols = hidden;
-  go<true, true, 4, 4, EPI_OUT>(p, s);
+  go<T, true, true, EPI_OUT>(p, tile_of<T>(piece.width, hidden, 1, false), piece.width, hidden, s);
 }
+
+#define RL_OF(T)                                                                                                                              \
+  template bool token_logprob_takes_mfma<T>(int64_t, int, int, int, const void*, const void*);                                                \
+  template void token_logprob_slice_tile<T>(int, int, SliceRule&);                                                                            \
+  template int launch_logits_strips_mfma<T>(hipStream_t, const T*, int, int, int64_t, const T*, int, int, const KeptRows&, float, float2*,    \
+                                            float*);                                                                                          \
+  template void launch_logits_gradient_mfma<T>(hipStream_t, const T*, int, int, int64_t, const T*, int, int, const KeptRows&, float,          \
+                                               const VocabPiece&, T*);                                                                        \
+  template void launch_hidden_gradient_mfma<T>(hipStream_t, const T*, const VocabPiece&, int, int64_t, const T*, int, int, const KeptRows&,   \
+                                               int, float*, size_t, bool);                                                                    \
+  template void launch_weight_gradient_mfma<T>(hipStream_t, const T*, const VocabPiece&, const T*, int, int64_t, int, const KeptRows&, T*);
+RL_OF(float)
+RL_OF(bf16_t)
+#undef RL_OF

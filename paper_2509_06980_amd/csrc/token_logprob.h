@@ -32,16 +32,24 @@ struct VocabPiece {
   int v0, width, ld;
 };
 
-// ---- bf16 on matrix instructions: hidden in multiples of 8, 16-byte aligned weights, nothing beyond 4 GB in one operand ----------
-// h: kept rows [padded][ld]; `rows`: an upper bound of how many they are.  width: vocabulary of a piece (forward: 0).
+// ---- matrix instructions with operands straight from memory: hidden in whole 16 bytes, 16-byte aligned weights, nothing beyond 4 GB in
+// one operand -------------------------------------------------------------------------------------
+// h: kept rows [padded][ld]; `rows`: an upper bound of how many they are.  width: row length of dz (forward: 0).
+template <typename T>
 bool token_logprob_takes_mfma(int64_t padded, int ld, int hidden, int width, const void* weight, const void* dweight);
-const int kStripMfma = 256;      // tokens of the vocabulary that one (max, sum) pair covers
-void launch_logits_strips_mfma(hipStream_t s, const bf16_t* h, int ld, int rows, int64_t padded, const bf16_t* w, int vocab, int hidden,
-                               const KeptRows& kept, float inv_t, float2* part, float* zt);
-void launch_logits_gradient_mfma(hipStream_t s, const bf16_t* h, int ld, int rows, int64_t padded, const bf16_t* w, int vocab, int hidden,
-                                 const KeptRows& kept, float inv_t, const VocabPiece& piece, bf16_t* dz);
-int token_logprob_tile_rows(int rows);      // rows of a tile
-void launch_hidden_gradient_mfma(hipStream_t s, const bf16_t* dz, const VocabPiece& piece, int rows, int64_t padded, const bf16_t* w, int vocab,
-                                 int hidden, const KeptRows& kept, int most_slices, float* dh, size_t slice_stride, bool first);
-void launch_weight_gradient_mfma(hipStream_t s, const bf16_t* dz, const VocabPiece& piece, const bf16_t* h, int ld, int64_t padded, int hidden,
-                                 const KeptRows& kept, bf16_t* dw);
+// Returns how many strips of the vocabulary it leaves a (max, sum) pair for, 64 tokens each or more.
+template <typename T>
+int launch_logits_strips_mfma(hipStream_t s, const T* h, int ld, int rows, int64_t padded, const T* w, int vocab, int hidden,
+                              const KeptRows& kept, float inv_t, float2* part, float* zt);
+template <typename T>
+void launch_logits_gradient_mfma(hipStream_t s, const T* h, int ld, int rows, int64_t padded, const T* w, int vocab, int hidden,
+                                 const KeptRows& kept, float inv_t, const VocabPiece& piece, T* dz);
+// Tile of dz W and its time
+template <typename T>
+void token_logprob_slice_tile(int rows, int hidden, SliceRule& r);
+template <typename T>
+void launch_hidden_gradient_mfma(hipStream_t s, const T* dz, const VocabPiece& piece, int rows, int64_t padded, const T* w, int vocab, int hidden,
+                                 const KeptRows& kept, int most_slices, float* dh, size_t slice_stride, bool first);
+template <typename T>
+void launch_weight_gradient_mfma(hipStream_t s, const T* dz, const VocabPiece& piece, const T* h, int ld, int64_t padded, int hidden,
+                                 const KeptRows& kept, T* dw);
