@@ -1,4 +1,7 @@
 // Attention over packed sequences, forward and backward: entry points, and the kernels for every type and layout.
+#include <atomic>
+#include <type_traits>
+
 #include "packed_attention.h"
 
 namespace {
@@ -8,21 +11,35 @@ namespace {
 // again: dv = p^T do, delta = rowsum(do o), dz = p (do v^T - delta), dq = scale dz k, dk = scale dz^T q.
 // These kernels take both types, any head size up to 128 and any strides.  They compute in 32 bits throughout, products on
 // 16x16x4 matrix instructions: lane l holds row (column) l % 16 at k = l / 16 of an operand, the result has column l % 16 and rows
-// 4 (l / 16) + r.  Tiles of 64 rows, a wave 16 of them, walk over tiles of 32 rows of the other side in LDS.
+// 4 (l / 16) + r.  A wave has 16 rows of its side and walks over the other side, 32 rows at a time, in LDS.  SPLIT = 1: the four waves have
+// different rows and share what is in LDS; SPLIT = 4: they have the same 16 rows, each takes every fourth 32 of the other side, and
+// their sums are joined at the end.  The first reads a quarter of the bytes, the second has four times the workgroups and a quarter
+// of the steps: it is taken where the first would not fill the chip (4 sequences of 57 to 104 rows, forward and backward: 93 us against 41).
 // A query head reads KV head h / (nq / nkv); the gradient of a KV head is added up over its query heads in the workgroup that owns
 // its rows, in a fixed order.
 // =============================================================================================
-constexpr int BM = 64, BN = 32;
+constexpr int BN = 32;      // rows of the other side that a wave takes at a time
+constexpr int PAD = 12;      // of a row in LDS: 16 rows at one column, 4 k apart, lie in 64 different banks
 typedef float f32;
 
 __device__ __forceinline__ f32x4 mfma4(f32 a, f32 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
-// rows [r0, r0 + n) of a tensor into LDS, rows from `len` on and columns from d on as zeros
+// rows [r0, r0 + n) of a tensor into LDS, rows from `len` on and columns from d on as zeros; vec: four elements at a time
 template <typename T, int D, int S>
-__device__ __forceinline__ void stage(const T* base, int64_t stride, int r0, int n, int len, int d, f32 (*to)[S]) {
-  for (int i = threadIdx.x; i < n * D; i += 256) {
-    const int r = i / D, c = i - r * D;
-    to[r][c] = r0 + r < len && c < d ? ldf(base + (int64_t)(r0 + r) * stride + c) : 0.f;
+__device__ __forceinline__ void stage(const T* base, int64_t stride, int r0, int n, int len, int d, bool vec, f32 (*to)[S]) {
+  if (vec) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n * (D / 4); i += 256) {
+      const int r = i / (D / 4), c = i % (D / 4) * 4;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r0 + r < len && c < d) ld4(base + (int64_t)(r0 + r) * stride + c, v.x, v.y, v.z, v.w);
+      *(float4*)&to[r][c] = v;
+    }
+  } else {
+    for (int i = threadIdx.x; i < n * D; i += 256) {
+      const int r = i / D, c = i - r * D;
+      to[r][c] = r0 + r < len && c < d ? ldf(base + (int64_t)(r0 + r) * stride + c) : 0.f;
+    }
   }
 }
 // row operand of 16 rows x D in registers: lane's row (clamped into [0, len)), element 4 s + lane / 16
@@ -35,11 +52,33 @@ __device__ __forceinline__ void operand(const T* base, int64_t stride, int row, 
   }
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attention_rows_forward(PackedShape p, const T* __restrict__ q, const T* __restrict__ k,
+// The waves' shares of a sum [16 rows][D], in the layout of a result, added up in their order; f(row, column, sum) for every element.
+template <int D, typename F>
+__device__ __forceinline__ void join_waves(const f32x4 (&acc)[D / 16], f32* lds, F f) {
+  constexpr int S = D + 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < D / 16; j++)
+#pragma unroll
+    for (int r = 0; r < 4; r++) lds[(wave * 16 + 4 * (lane >> 4) + r) * S + 16 * j + (lane & 15)] = acc[j][r];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 16 * D; i += 256) {
+    const int row = i / D, c = i - row * D;
+    f(row, c, (lds[row * S + c] + lds[(16 + row) * S + c]) + (lds[(32 + row) * S + c] + lds[(48 + row) * S + c]));
+  }
+}
+
+template <typename T, int D, int SPLIT>
+__global__ __launch_bounds__(256) void attention_rows_forward(PackedShape p, int vec, const T* __restrict__ q, const T* __restrict__ k,
                                                               const T* __restrict__ v, T* __restrict__ o, float* __restrict__ lse) {
-  __shared__ f32 ks[BN][D + 4], vs[BN][D + 16], ps[4][16][BN + 4];
+  constexpr int BM = 64 / SPLIT, BT = BN * SPLIT;
+  extern __shared__ f32 dynamic[];
+  f32(*ks)[D + PAD] = (f32(*)[D + PAD])dynamic;
+  f32(*vs)[D + PAD] = (f32(*)[D + PAD])(dynamic + BT * (D + PAD));
+  f32(*ps)[16][BN + 4] = (f32(*)[16][BN + 4])(dynamic + BT * 2 * (D + PAD));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y, l16 = lane & 15, l4 = lane >> 4;
+  const int mine = SPLIT == 1 ? wave * 16 : 0, part = SPLIT == 1 ? 0 : wave * BN;      // wave's rows, and its share of what is in LDS
   const PackedTile t = packed_tile(p.cu_q, p.n_seq, p.total_q, BM, blockIdx.x);
   if (t.row0 >= t.len) return;
   const int k0 = packed_bound(p.cu_k, t.seq, p.total_k), lk = max(packed_bound(p.cu_k, t.seq + 1, p.total_k) - k0, 0);
@@ -47,31 +86,31 @@ __global__ __launch_bounds__(256) void attention_rows_forward(PackedShape p, con
   const T* kb = k + (int64_t)k0 * p.kt + (int64_t)hk * p.kh;
   const T* vb = v + (int64_t)k0 * p.vt + (int64_t)hk * p.vh;
   f32 a[D / 4], m[4], sum[4];
-  operand<T, D>(q + (int64_t)t.first * p.qt + (int64_t)h * p.qh, p.qt, t.row0 + wave * 16 + l16, t.len, p.d, lane, a);
+  operand<T, D>(q + (int64_t)t.first * p.qt + (int64_t)h * p.qh, p.qt, t.row0 + mine + l16, t.len, p.d, lane, a);
   f32x4 acc[D / 16];
 #pragma unroll
   for (int j = 0; j < D / 16; j++) acc[j] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int r = 0; r < 4; r++) m[r] = -INFINITY, sum[r] = 0.f;
   const int last = p.causal ? min(lk, max(t.row0 + BM + shift, 0)) : lk;
-  for (int j0 = 0; j0 < last; j0 += BN) {
+  for (int j0 = 0; j0 < last; j0 += BT) {
     __syncthreads();
-    stage<T, D>(kb, p.kt, j0, BN, lk, p.d, ks);
-    stage<T, D>(vb, p.vt, j0, BN, lk, p.d, vs);
+    stage<T, D>(kb, p.kt, j0, BT, lk, p.d, vec, ks);
+    stage<T, D>(vb, p.vt, j0, BT, lk, p.d, vec, vs);
     __syncthreads();
     f32x4 z[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int s = 0; s < D / 4; s++)
 #pragma unroll
-      for (int b = 0; b < 2; b++) z[b] = mfma4(a[s], ks[b * 16 + l16][4 * s + l4], z[b]);
+      for (int b = 0; b < 2; b++) z[b] = mfma4(a[s], ks[part + b * 16 + l16][4 * s + l4], z[b]);
 #pragma unroll
     for (int r = 0; r < 4; r++) {
-      const int i = t.row0 + wave * 16 + 4 * l4 + r;
+      const int i = t.row0 + mine + 4 * l4 + r;
       const int end = p.causal ? min(lk, i + shift + 1) : lk;      // keys [0, end) are seen
       f32 top = m[r];
 #pragma unroll
       for (int b = 0; b < 2; b++) {
-        z[b][r] = j0 + b * 16 + l16 < end ? z[b][r] * p.scale : -INFINITY;
+        z[b][r] = j0 + part + b * 16 + l16 < end ? z[b][r] * p.scale : -INFINITY;
         top = fmaxf(top, z[b][r]);
       }
 #pragma unroll
@@ -93,38 +132,78 @@ __global__ __launch_bounds__(256) void attention_rows_forward(PackedShape p, con
 #pragma unroll
     for (int s = 0; s < BN / 4; s++)
 #pragma unroll
-      for (int j = 0; j < D / 16; j++) acc[j] = mfma4(ps[wave][l16][4 * s + l4], vs[4 * s + l4][16 * j + l16], acc[j]);
+      for (int j = 0; j < D / 16; j++) acc[j] = mfma4(ps[wave][l16][4 * s + l4], vs[part + 4 * s + l4][16 * j + l16], acc[j]);
   }
+  __shared__ f32 tops[4][16], sums[4][16];
 #pragma unroll
   for (int r = 0; r < 4; r++) {
     f32 s = sum[r];
 #pragma unroll
     for (int x = 8; x > 0; x >>= 1) s += __shfl_xor(s, x, 64);
-    const int i = t.row0 + wave * 16 + 4 * l4 + r;
-    if (i >= t.len) continue;
-    const f32 inv = s > 0.f ? 1.f / s : s == 0.f ? 0.f : s;      // no key: zeros; no number stays so
-    T* out = o + (int64_t)(t.first + i) * p.ot + (int64_t)h * p.oh;
+    sum[r] = s;
+    if (SPLIT > 1 && l16 == 0) tops[wave][4 * l4 + r] = m[r], sums[wave][4 * l4 + r] = s;
+  }
+  if constexpr (SPLIT > 1) {      // one reference for the four shares
+    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < D / 16; j++)
-      if (16 * j + l16 < p.d) st1(out + 16 * j + l16, acc[j][r] * inv);
-    if (l16 == 0) lse[(size_t)h * p.total_q + t.first + i] = m[r] + logf(s);
+    for (int r = 0; r < 4; r++) {
+      const int row = 4 * l4 + r;
+      f32 top = tops[0][row], s = 0.f;
+#pragma unroll
+      for (int w = 1; w < 4; w++) top = fmaxf(top, tops[w][row]);
+      const f32 ref = top == -INFINITY ? 0.f : top, old = expf(m[r] - ref);
+#pragma unroll
+      for (int w = 0; w < 4; w++) s += sums[w][row] * expf(tops[w][row] - ref);
+#pragma unroll
+      for (int j = 0; j < D / 16; j++) acc[j][r] *= old;
+      m[r] = top, sum[r] = s;
+    }
+  }
+  f32 inv[4];
+#pragma unroll
+  for (int r = 0; r < 4; r++) {
+    const int i = t.row0 + mine + 4 * l4 + r;
+    inv[r] = sum[r] > 0.f ? 1.f / sum[r] : sum[r] == 0.f ? 0.f : sum[r];      // no key: zeros; no number stays so
+    if (i < t.len && l16 == 0 && (SPLIT == 1 || wave == 0)) lse[(size_t)h * p.total_q + t.first + i] = m[r] + logf(sum[r]);
+#pragma unroll
+    for (int j = 0; j < D / 16; j++) acc[j][r] *= inv[r];
+  }
+  T* out = o + (int64_t)(t.first + t.row0) * p.ot + (int64_t)h * p.oh;
+  if constexpr (SPLIT > 1) {
+    join_waves<D>(acc, dynamic, [&](int row, int c, f32 x) {
+      if (t.row0 + row < t.len && c < p.d) st1(out + row * p.ot + c, x);
+    });
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      const int row = mine + 4 * l4 + r;
+      if (t.row0 + row >= t.len) continue;
+#pragma unroll
+      for (int j = 0; j < D / 16; j++)
+        if (16 * j + l16 < p.d) st1(out + row * p.ot + 16 * j + l16, acc[j][r]);
+    }
   }
 }
 
-// dq of 64 query rows, and delta, which the other kernel reads
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attention_rows_dq(PackedShape p, const T* __restrict__ dout, const T* __restrict__ q,
+// dq of 64 / SPLIT query rows, and delta, which the other kernel reads
+template <typename T, int D, int SPLIT>
+__global__ __launch_bounds__(256) void attention_rows_dq(PackedShape p, int vec, const T* __restrict__ dout, const T* __restrict__ q,
                                                          const T* __restrict__ k, const T* __restrict__ v, const T* __restrict__ o,
                                                          const float* __restrict__ lse, T* __restrict__ dq, float* __restrict__ delta) {
-  __shared__ f32 ks[BN][D + 16], vs[BN][D + 4], ds[4][16][BN + 4];
+  constexpr int BM = 64 / SPLIT, BT = BN * SPLIT;
+  extern __shared__ f32 dynamic[];
+  f32(*ks)[D + PAD] = (f32(*)[D + PAD])dynamic;
+  f32(*vs)[D + PAD] = (f32(*)[D + PAD])(dynamic + BT * (D + PAD));
+  f32(*ds)[16][BN + 4] = (f32(*)[16][BN + 4])(dynamic + BT * 2 * (D + PAD));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y, l16 = lane & 15, l4 = lane >> 4;
+  const int own = SPLIT == 1 ? wave * 16 : 0, part = SPLIT == 1 ? 0 : wave * BN;
   const PackedTile t = packed_tile(p.cu_q, p.n_seq, p.total_q, BM, blockIdx.x);
   if (t.row0 >= t.len) return;
   const int k0 = packed_bound(p.cu_k, t.seq, p.total_k), lk = max(packed_bound(p.cu_k, t.seq + 1, p.total_k) - k0, 0);
   const int hk = h / (p.nq / p.nkv), shift = lk - t.len;
   const T* kb = k + (int64_t)k0 * p.kt + (int64_t)hk * p.kh;
   const T* vb = v + (int64_t)k0 * p.vt + (int64_t)hk * p.vh;
-  const int mine = t.row0 + wave * 16 + l16;
+  const int mine = t.row0 + own + l16;
   const int64_t ds_ = (int64_t)p.nq * p.d;      // token stride of dO and dq
   f32 a[D / 4], g[D / 4], dl = 0.f;
   operand<T, D>(q + (int64_t)t.first * p.qt + (int64_t)h * p.qh, p.qt, mine, t.len, p.d, lane, a);
@@ -136,12 +215,12 @@ __global__ __launch_bounds__(256) void attention_rows_dq(PackedShape p, const T*
     for (int s = 0; s < D / 4; s++) dl += g[s] * y[s];
     dl += __shfl_xor(dl, 16, 64);
     dl += __shfl_xor(dl, 32, 64);
-    if (lane < 16 && mine < t.len) delta[(size_t)h * p.total_q + t.first + mine] = dl;
+    if (lane < 16 && mine < t.len && (SPLIT == 1 || wave == 0)) delta[(size_t)h * p.total_q + t.first + mine] = dl;
   }
   f32 l[4], dr[4];
 #pragma unroll
   for (int r = 0; r < 4; r++) {
-    const int i = t.row0 + wave * 16 + 4 * l4 + r;
+    const int i = t.row0 + own + 4 * l4 + r;
     l[r] = i < t.len ? lse[(size_t)h * p.total_q + t.first + i] : 0.f;
     dr[r] = __shfl(dl, 4 * l4 + r, 64);
   }
@@ -149,54 +228,66 @@ __global__ __launch_bounds__(256) void attention_rows_dq(PackedShape p, const T*
 #pragma unroll
   for (int j = 0; j < D / 16; j++) acc[j] = {0.f, 0.f, 0.f, 0.f};
   const int last = p.causal ? min(lk, max(t.row0 + BM + shift, 0)) : lk;
-  for (int j0 = 0; j0 < last; j0 += BN) {
+  for (int j0 = 0; j0 < last; j0 += BT) {
     __syncthreads();
-    stage<T, D>(kb, p.kt, j0, BN, lk, p.d, ks);
-    stage<T, D>(vb, p.vt, j0, BN, lk, p.d, vs);
+    stage<T, D>(kb, p.kt, j0, BT, lk, p.d, vec, ks);
+    stage<T, D>(vb, p.vt, j0, BT, lk, p.d, vec, vs);
     __syncthreads();
     f32x4 z[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, dp[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int s = 0; s < D / 4; s++)
 #pragma unroll
       for (int b = 0; b < 2; b++) {
-        z[b] = mfma4(a[s], ks[b * 16 + l16][4 * s + l4], z[b]);
-        dp[b] = mfma4(g[s], vs[b * 16 + l16][4 * s + l4], dp[b]);
+        z[b] = mfma4(a[s], ks[part + b * 16 + l16][4 * s + l4], z[b]);
+        dp[b] = mfma4(g[s], vs[part + b * 16 + l16][4 * s + l4], dp[b]);
       }
 #pragma unroll
     for (int r = 0; r < 4; r++) {
-      const int i = t.row0 + wave * 16 + 4 * l4 + r, end = p.causal ? min(lk, i + shift + 1) : lk;
+      const int i = t.row0 + own + 4 * l4 + r, end = p.causal ? min(lk, i + shift + 1) : lk;
 #pragma unroll
       for (int b = 0; b < 2; b++)
-        ds[wave][4 * l4 + r][b * 16 + l16] = j0 + b * 16 + l16 < end ? expf(z[b][r] * p.scale - l[r]) * (dp[b][r] - dr[r]) * p.scale : 0.f;
+        ds[wave][4 * l4 + r][b * 16 + l16] = j0 + part + b * 16 + l16 < end ? expf(z[b][r] * p.scale - l[r]) * (dp[b][r] - dr[r]) * p.scale : 0.f;
     }
     __syncthreads();
 #pragma unroll
     for (int s = 0; s < BN / 4; s++)
 #pragma unroll
-      for (int j = 0; j < D / 16; j++) acc[j] = mfma4(ds[wave][l16][4 * s + l4], ks[4 * s + l4][16 * j + l16], acc[j]);
+      for (int j = 0; j < D / 16; j++) acc[j] = mfma4(ds[wave][l16][4 * s + l4], ks[part + 4 * s + l4][16 * j + l16], acc[j]);
   }
+  T* out = dq + (int64_t)(t.first + t.row0) * ds_ + (int64_t)h * p.d;
+  if constexpr (SPLIT > 1) {
+    join_waves<D>(acc, dynamic, [&](int row, int c, f32 x) {
+      if (t.row0 + row < t.len && c < p.d) st1(out + row * ds_ + c, x);
+    });
+  } else {
 #pragma unroll
-  for (int r = 0; r < 4; r++) {
-    const int i = t.row0 + wave * 16 + 4 * l4 + r;
-    if (i >= t.len) continue;
-    T* out = dq + (int64_t)(t.first + i) * ds_ + (int64_t)h * p.d;
+    for (int r = 0; r < 4; r++) {
+      const int row = own + 4 * l4 + r;
+      if (t.row0 + row >= t.len) continue;
 #pragma unroll
-    for (int j = 0; j < D / 16; j++)
-      if (16 * j + l16 < p.d) st1(out + 16 * j + l16, acc[j][r]);
+      for (int j = 0; j < D / 16; j++)
+        if (16 * j + l16 < p.d) st1(out + row * ds_ + 16 * j + l16, acc[j][r]);
+    }
   }
 }
 
-// dk and dv of 64 key rows of one KV head, over its query heads and the query tiles that see them
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attention_rows_dkv(PackedShape p, const T* __restrict__ dout, const T* __restrict__ q,
+// dk and dv of 64 / SPLIT key rows of one KV head, over its query heads and the query tiles that see them
+template <typename T, int D, int SPLIT>
+__global__ __launch_bounds__(256) void attention_rows_dkv(PackedShape p, int vec, const T* __restrict__ dout, const T* __restrict__ q,
                                                           const T* __restrict__ k, const T* __restrict__ v, const float* __restrict__ lse,
                                                           const float* __restrict__ delta, T* __restrict__ dk, T* __restrict__ dv) {
-  __shared__ f32 qs[BN][D + 16], gs[BN][D + 16], pt[4][16][BN + 4], dt[4][16][BN + 4];
+  constexpr int BM = 64 / SPLIT, BT = BN * SPLIT;
+  extern __shared__ f32 dynamic[];
+  f32(*qs)[D + PAD] = (f32(*)[D + PAD])dynamic;
+  f32(*gs)[D + PAD] = (f32(*)[D + PAD])(dynamic + BT * (D + PAD));
+  f32(*pt)[16][BN + 4] = (f32(*)[16][BN + 4])(dynamic + 2 * BT * (D + PAD));
+  f32(*dt)[16][BN + 4] = pt + 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hk = blockIdx.y, l16 = lane & 15, l4 = lane >> 4;
+  const int own = SPLIT == 1 ? wave * 16 : 0, part = SPLIT == 1 ? 0 : wave * BN;
   const PackedTile t = packed_tile(p.cu_k, p.n_seq, p.total_k, BM, blockIdx.x);
   if (t.row0 >= t.len) return;
   const int q0 = packed_bound(p.cu_q, t.seq, p.total_q), lq = max(packed_bound(p.cu_q, t.seq + 1, p.total_q) - q0, 0);
-  const int group = p.nq / p.nkv, shift = t.len - lq, mine = t.row0 + wave * 16 + l16;
+  const int group = p.nq / p.nkv, shift = t.len - lq, mine = t.row0 + own + l16;
   const int64_t ds_ = (int64_t)p.nq * p.d, dks = (int64_t)p.nkv * p.d;
   f32 a[D / 4], b[D / 4];
   operand<T, D>(k + (int64_t)t.first * p.kt + (int64_t)hk * p.kh, p.kt, mine, t.len, p.d, lane, a);
@@ -208,28 +299,28 @@ __global__ __launch_bounds__(256) void attention_rows_dkv(PackedShape p, const T
   for (int h = hk * group; h < (hk + 1) * group; h++) {
     const T* qb = q + (int64_t)q0 * p.qt + (int64_t)h * p.qh;
     const T* gb = dout + (int64_t)q0 * ds_ + (int64_t)h * p.d;
-    for (int i0 = first; i0 < lq; i0 += BN) {
+    for (int i0 = first; i0 < lq; i0 += BT) {
       __syncthreads();
-      stage<T, D>(qb, p.qt, i0, BN, lq, p.d, qs);
-      stage<T, D>(gb, ds_, i0, BN, lq, p.d, gs);
+      stage<T, D>(qb, p.qt, i0, BT, lq, p.d, vec, qs);
+      stage<T, D>(gb, ds_, i0, BT, lq, p.d, vec, gs);
       __syncthreads();
       f32x4 z[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, dp[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
       for (int s = 0; s < D / 4; s++)
 #pragma unroll
         for (int c = 0; c < 2; c++) {
-          z[c] = mfma4(a[s], qs[c * 16 + l16][4 * s + l4], z[c]);
-          dp[c] = mfma4(b[s], gs[c * 16 + l16][4 * s + l4], dp[c]);
+          z[c] = mfma4(a[s], qs[part + c * 16 + l16][4 * s + l4], z[c]);
+          dp[c] = mfma4(b[s], gs[part + c * 16 + l16][4 * s + l4], dp[c]);
         }
 #pragma unroll
       for (int c = 0; c < 2; c++) {
-        const int i = i0 + c * 16 + l16;
+        const int i = i0 + part + c * 16 + l16;
         const bool in = i < lq;
         const f32 l = in ? lse[(size_t)h * p.total_q + q0 + i] : 0.f, dl = in ? delta[(size_t)h * p.total_q + q0 + i] : 0.f;
         const int end = !in ? 0 : p.causal ? min(t.len, i + shift + 1) : t.len;      // this query sees the keys [0, end)
 #pragma unroll
         for (int r = 0; r < 4; r++) {
-          const f32 e = t.row0 + wave * 16 + 4 * l4 + r < end ? expf(z[c][r] * p.scale - l) : 0.f;
+          const f32 e = t.row0 + own + 4 * l4 + r < end ? expf(z[c][r] * p.scale - l) : 0.f;
           pt[wave][4 * l4 + r][c * 16 + l16] = e;
           dt[wave][4 * l4 + r][c * 16 + l16] = e != 0.f ? e * (dp[c][r] - dl) * p.scale : 0.f;
         }
@@ -240,40 +331,93 @@ __global__ __launch_bounds__(256) void attention_rows_dkv(PackedShape p, const T
         const f32 x = pt[wave][l16][4 * s + l4], y = dt[wave][l16][4 * s + l4];
 #pragma unroll
         for (int j = 0; j < D / 16; j++) {
-          av[j] = mfma4(x, gs[4 * s + l4][16 * j + l16], av[j]);
-          ak[j] = mfma4(y, qs[4 * s + l4][16 * j + l16], ak[j]);
+          av[j] = mfma4(x, gs[part + 4 * s + l4][16 * j + l16], av[j]);
+          ak[j] = mfma4(y, qs[part + 4 * s + l4][16 * j + l16], ak[j]);
         }
       }
     }
   }
+  const int64_t at = (int64_t)(t.first + t.row0) * dks + (int64_t)hk * p.d;
+  if constexpr (SPLIT > 1) {
+    auto to = [&](T* out) {
+      return [&, out](int row, int c, f32 x) {
+        if (t.row0 + row < t.len && c < p.d) st1(out + at + row * dks + c, x);
+      };
+    };
+    join_waves<D>(ak, dynamic, to(dk));
+    join_waves<D>(av, dynamic, to(dv));
+  } else {
 #pragma unroll
-  for (int r = 0; r < 4; r++) {
-    const int i = t.row0 + wave * 16 + 4 * l4 + r;
-    if (i >= t.len) continue;
-    const int64_t at = (int64_t)(t.first + i) * dks + (int64_t)hk * p.d;
+    for (int r = 0; r < 4; r++) {
+      const int row = own + 4 * l4 + r;
+      if (t.row0 + row >= t.len) continue;
 #pragma unroll
-    for (int j = 0; j < D / 16; j++)
-      if (16 * j + l16 < p.d) {
-        st1(dk + at + 16 * j + l16, ak[j][r]);
-        st1(dv + at + 16 * j + l16, av[j][r]);
-      }
+      for (int j = 0; j < D / 16; j++)
+        if (16 * j + l16 < p.d) {
+          st1(dk + at + row * dks + 16 * j + l16, ak[j][r]);
+          st1(dv + at + row * dks + 16 * j + l16, av[j][r]);
+        }
+    }
   }
+}
+
+// Four elements at a time: aligned rows of whole fours.
+template <typename T>
+bool fours(const void* x, int64_t ts, int64_t hs, int d) {
+  return ((uintptr_t)x & (4 * sizeof(T) - 1)) == 0 && ts % 4 == 0 && hs % 4 == 0 && d % 4 == 0;
+}
+template <auto kernel, typename... A>
+void launch_rows(int tiles, int heads, int lds, hipStream_t s, A... args) {
+  static std::atomic<uint64_t> done;      // more than 64 KB of LDS need an opt-in, once per kernel and device
+  int dev = 0;
+  (void)hipGetDevice(&dev);
+  const uint64_t bit = 1ull << (dev & 63);
+  if (lds > 65536 && !(done.load(std::memory_order_acquire) & bit)) {
+    (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    done.fetch_or(bit, std::memory_order_release);
+  }
+  kernel<<<dim3(tiles, heads), 256, lds, s>>>(args...);
+}
+// Rows split over four waves where whole tiles would be fewer than two workgroups a CU.
+bool split_rows(int total, int n_seq, int heads) { return (int64_t)packed_tiles(total, n_seq, 64) * heads < 512; }
+template <int D>
+constexpr int rows_lds(int split) {      // what the largest of the kernels needs: two tiles, two sets of scores
+  return (BN * split * 2 * (D + PAD) + 2 * 4 * 16 * (BN + 4)) * 4;
 }
 
 template <typename T, int D>
 void forward(hipStream_t s, const PackedShape& p, const void* q, const void* k, const void* v, void* o, float* lse) {
-  attention_rows_forward<T, D><<<dim3(packed_tiles(p.total_q, p.n_seq, BM), p.nq), 256, 0, s>>>(p, (const T*)q, (const T*)k, (const T*)v,
-                                                                                                (T*)o, lse);
+  const int vec = fours<T>(k, p.kt, p.kh, p.d) && fours<T>(v, p.vt, p.vh, p.d);
+  if (split_rows(p.total_q, p.n_seq, p.nq))
+    launch_rows<attention_rows_forward<T, D, 4>>(packed_tiles(p.total_q, p.n_seq, 16), p.nq, rows_lds<D>(4), s, p, vec, (const T*)q, (const T*)k,
+                (const T*)v, (T*)o, lse);
+  else
+    launch_rows<attention_rows_forward<T, D, 1>>(packed_tiles(p.total_q, p.n_seq, 64), p.nq, rows_lds<D>(1), s, p, vec, (const T*)q, (const T*)k,
+                (const T*)v, (T*)o, lse);
 }
 template <typename T, int D>
 void backward(hipStream_t s, const PackedShape& p, const void* dout, const void* q, const void* k, const void* v, const void* o,
               const float* lse, void* dq, void* dk, void* dv, float* delta) {
-  if (p.total_q > 0)
-    attention_rows_dq<T, D><<<dim3(packed_tiles(p.total_q, p.n_seq, BM), p.nq), 256, 0, s>>>(
-        p, (const T*)dout, (const T*)q, (const T*)k, (const T*)v, (const T*)o, lse, (T*)dq, delta);
-  if (p.total_k > 0)
-    attention_rows_dkv<T, D><<<dim3(packed_tiles(p.total_k, p.n_seq, BM), p.nkv), 256, 0, s>>>(
-        p, (const T*)dout, (const T*)q, (const T*)k, (const T*)v, lse, delta, (T*)dk, (T*)dv);
+  const int by_key = fours<T>(k, p.kt, p.kh, p.d) && fours<T>(v, p.vt, p.vh, p.d);
+  const int by_query = fours<T>(q, p.qt, p.qh, p.d) && fours<T>(dout, p.ot, p.oh, p.d);
+  if (p.total_q > 0) {
+    auto go = [&](auto split) {
+      constexpr int S = decltype(split)::value;
+      launch_rows<attention_rows_dq<T, D, S>>(packed_tiles(p.total_q, p.n_seq, 64 / S), p.nq, rows_lds<D>(S), s, p, by_key, (const T*)dout,
+                  (const T*)q, (const T*)k, (const T*)v, (const T*)o, lse, (T*)dq, delta);
+    };
+    if (split_rows(p.total_q, p.n_seq, p.nq)) go(std::integral_constant<int, 4>());
+    else go(std::integral_constant<int, 1>());
+  }
+  if (p.total_k > 0) {
+    auto go = [&](auto split) {
+      constexpr int S = decltype(split)::value;
+      launch_rows<attention_rows_dkv<T, D, S>>(packed_tiles(p.total_k, p.n_seq, 64 / S), p.nkv, rows_lds<D>(S), s, p, by_query, (const T*)dout,
+                  (const T*)q, (const T*)k, (const T*)v, lse, delta, (T*)dk, (T*)dv);
+    };
+    if (split_rows(p.total_k, p.n_seq, p.nkv)) go(std::integral_constant<int, 4>());
+    else go(std::integral_constant<int, 1>());
+  }
 }
 
 const char* attention_argument(const PackedShape& p, int32_t dtype) {
