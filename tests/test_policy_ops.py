@@ -267,6 +267,22 @@ def test_attention(case, causal, dt):
         within(name, got, want[name], err[name])
 
 
+@pytest.mark.parametrize("dt,lq,lk,nq,nk,d", [
+    (BF, [4111], None, 16, 16, 128), (BF, [4111], None, 16, 16, 64), (BF, [3000, 1301], [3501, 1000], 16, 16, 128),
+    (FP, [40, 3, 77] * 12, None, 16, 16, 64), (FP, [33, 90] * 14, [50, 64] * 14, 16, 16, 128), (BF, [40] * 30, None, 16, 16, 33)])
+def test_attention_where_whole_tiles_fill_the_chip(dt, lq, lk, nq, nk, d):
+    # many keys of few sequences (dk and dv by 128 keys), and rows enough that no tile is split over waves
+    lk = lk or lq
+    g = gen(sum(lq))
+    q, k, v, do = randn(g, sum(lq), nq, d, dt=dt), randn(g, sum(lk), nk, d, dt=dt), randn(g, sum(lk), nk, d, dt=dt), randn(g, sum(lq), nq, d, dt=dt)
+    cq, ck = offsets(lq), offsets(lk)
+    o, lse = ops.attention_forward(q, k, v, cq, ck)
+    dq, dk, dv = ops.attention_backward(do, q, k, v, o, lse, cq, ck)
+    want, err = attention_reference(q, k, v, do, lq, lk, True, d ** -0.5, dt, True)
+    for name, got in (("o", o), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        within(name, got, want[name], err[name])
+
+
 @pytest.mark.parametrize("dt", [BF, FP])
 def test_attention_of_views_and_large_scores(dt):
     g = gen(3)
