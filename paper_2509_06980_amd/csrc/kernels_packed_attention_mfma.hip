@@ -176,53 +176,38 @@ template <int D>
 __global__ __launch_bounds__(256, 2) void attention_forward_kernel(PackedShape p, const bf16_t* __restrict__ q, const bf16_t* __restrict__ k,
                                                                    const bf16_t* __restrict__ v, bf16_t* __restrict__ o,
                                                                    float* __restrict__ lse) {
-  constexpr int TILE = BN * D * 2, STAGE = 2 * TILE;
+  constexpr int TILE = BN * D * 2;      // LDS: two tiles of keys, three of values
   extern __shared__ u32x4 smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   QuerySide w;
   if (!query_side(p, w)) return;
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
-  Reads<D> lds((lds_char*)(__attribute__((address_space(3))) void*)smem, lane);      // of the stage in work
+  Reads<D> lds((lds_char*)(__attribute__((address_space(3))) void*)smem, lane);      // of the keys, of the values in work
+  lds.tr += 2 * TILE;
   const int mine = w.t.row0 + wave * 32 + (lane & 31);      // lane's query
   u32x4 qr[D / 16];
   own_rows<D>(q + (int64_t)w.t.first * p.qt + (int64_t)w.h * p.qh, p.qt, mine, w.t.len, p.d, lane, qr);
+  const unsigned flip = p.scale < 0.f ? 0x80008000u : 0u;      // c > 0 below: the largest product is the largest score
+#pragma unroll
+  for (int s = 0; s < D / 16; s++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) qr[s][i] ^= flip;
   f32x16 acc[D / 32];
 #pragma unroll
   for (int b = 0; b < D / 32; b++) acc[b] = zero16();
   float ref = -INFINITY, sum = 0.f;      // ref: log2 units; sum of this half's terms
-  const float c = p.scale * kLog2e;
+  const float c = fabsf(p.scale) * kLog2e;
   const int seen = p.causal ? min(w.lk, mine + w.shift + 1) : w.lk;             // lane's query sees the keys [0, seen)
   const int row_a = w.t.row0 + wave * 32, row_b = min(row_a + 32, w.t.len);     // wave's queries
   const int all = row_a >= w.t.len ? 0 : p.causal ? min(w.lk, row_a + w.shift + 1) : w.lk;      // keys that all of them see
   const int some = row_a >= w.t.len ? 0 : p.causal ? min(w.lk, row_b + w.shift) : w.lk;         // ... that one sees
-  const int tiles = (w.last + BN - 1) / BN;
-  Stream<D> ks, vs;
-  if (tiles > 0) {
-    ks.init(k + (int64_t)w.k0 * p.kt + (int64_t)w.hk * p.kh, p.kt, w.lk, p.d, wave, lane);
-    vs.init(v + (int64_t)w.k0 * p.vt + (int64_t)w.hk * p.vh, p.vt, w.lk, p.d, wave, lane);
-    ks.load(0, lds0, wave);
-    vs.load(0, lds0 + TILE, wave);
-  }
-  auto tile = [&](int j0, auto masked) {
-    f32x16 z[2];
-#pragma unroll
-    for (int x = 0; x < 2; x++) {
-      z[x] = zero16();
-#pragma unroll
-      for (int s = 0; s < D / 16; s++) z[x] = mfma(lds.rows(0, x, s), qr[s], z[x]);
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int x = 0; x < 2; x++)
-#pragma unroll
-      for (int e = 0; e < 16; e++) {
-        z[x][e] *= c;
-        if (decltype(masked)::value && j0 + 32 * x + row_of(e, lane) >= seen) z[x][e] = -INFINITY;
-        top = fmaxf(top, z[x][e]);
-      }
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    // the reference of the exponents moves only where a term would exceed 2^8: rounding is relative, and sums stay far from overflow
+  const int tiles = (w.last + BN - 1) / BN, steps = (max(some, 0) + 31) / 32;
+  // top: the largest of the lane's 16 products; moves the reference of the exponents only where a term would exceed 2^8:
+  // rounding is relative, and sums stay far from overflow
+  auto refer = [&](float top) {
+    top *= c;
     if (__any(top > ref + 8.f)) {
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
       const float now = fmaxf(ref, top), f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - now);
       ref = now;
       sum *= f;
@@ -231,34 +216,105 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(PackedShape p
 #pragma unroll
         for (int e = 0; e < 16; e++) acc[b][e] *= f;
     }
-    const float r = ref == -INFINITY ? 0.f : ref;      // nothing seen yet: e^-inf = 0
+  };
+  auto mask = [&](f32x16& z, int j) {      // keys from j on
+    if (j + 32 > all) {
 #pragma unroll
-    for (int x = 0; x < 2; x++) {
-#pragma unroll
-      for (int e = 0; e < 16; e++) {
-        z[x][e] = __builtin_amdgcn_exp2f(z[x][e] - r);
-        sum += z[x][e];
-      }
-#pragma unroll
-      for (int s = 0; s < 2; s++) {
-        const u32x4 pr = as_operand(z[x], s);      // probabilities rounded to bf16; their sum is not
-#pragma unroll
-        for (int b = 0; b < D / 32; b++) acc[b] = mfma(lds.columns(TILE, x, s, b), pr, acc[b]);
-      }
+      for (int e = 0; e < 16; e++)
+        if (j + row_of(e, lane) >= seen) z[e] = -INFINITY;
     }
   };
-  for (int t = 0; t < tiles; t++) {
-    const int at = (t & 1) * STAGE;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();      // tile t has landed, the other stage is read out
-    if (t + 1 < tiles) {
-      ks.load(t + 1, lds0 + (unsigned)(STAGE - at), wave);
-      vs.load(t + 1, lds0 + (unsigned)(STAGE - at + TILE), wave);
+  // A step of 32 keys, in slots as in the backward pass: first the scores of the next step beside the exponentials of this one, then
+  // this one's values beside the largest of the next scores.
+  constexpr int S = D / 16, AHEAD = 3, EXPS = 3 * S / 2;
+  u32x4 a[4];
+  auto step = [&](auto half, auto more, int n, f32x16& z, f32x16& next, auto middle) {
+    constexpr int H = decltype(half)::value;
+    constexpr bool MORE = decltype(more)::value;
+    const float r = ref == -INFINITY ? 0.f : ref;      // nothing seen yet: e^-inf = 0
+    float top = -INFINITY;
+    u32x4 pr[2];
+    if constexpr (MORE) next = zero16();
+    each<2 * S>([&](auto slot) {
+      constexpr int m = decltype(slot)::value, later = m + AHEAD;
+      if constexpr (m == S && H == 0) middle();      // the next tile has landed
+      if constexpr (later == 2 * S && H == 0 && MORE) {      // every read of this tile's keys is under way
+        lds.row += (n >> 1 & 1) ? -TILE : TILE;
+        asm volatile("" : "+v"(lds.row));
+      }
+      if constexpr (later < S) {
+        if constexpr (MORE) a[later & 3] = lds.rows(0, 1 - H, later);
+      } else if constexpr (later < 2 * S) {
+        a[later & 3] = lds.columns(0, H, (later - S) / (D / 32), (later - S) % (D / 32));
+      } else if constexpr (MORE) {
+        a[later & 3] = lds.rows(0, H, later - 2 * S);
+      }
+      if constexpr (m < S) {
+        if constexpr (MORE) next = mfma(a[m & 3], qr[m], next);
+      } else {
+        acc[(m - S) % (D / 32)] = mfma(a[m & 3], pr[(m - S) / (D / 32)], acc[(m - S) % (D / 32)]);
+      }
+      if constexpr (m < EXPS) {
+#pragma unroll
+        for (int e = m * 16 / EXPS; e < (m + 1) * 16 / EXPS; e++) {
+          z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], c, -r));
+          sum += z[e];
+        }
+        asm volatile("" : "+v"(sum));      // here, not all at the end
+        if constexpr (m == S - 1) pr[0] = as_operand(z, 0);      // probabilities rounded to bf16; their sum is not
+        if constexpr (m == EXPS - 1) pr[1] = as_operand(z, 1);
+      } else if constexpr (MORE) {
+        if constexpr (m == EXPS) mask(next, 32 * n + 32);
+#pragma unroll
+        for (int e = (m - EXPS) * 32 / S; e < (m - EXPS + 1) * 32 / S; e++) top = fmaxf(top, next[e]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (MORE) refer(top);
+  };
+  Stream<D> ks, vs;
+  if (tiles > 0) {
+    ks.init(k + (int64_t)w.k0 * p.kt + (int64_t)w.hk * p.kh, p.kt, w.lk, p.d, wave, lane);
+    vs.init(v + (int64_t)w.k0 * p.vt + (int64_t)w.hk * p.vh, p.vt, w.lk, p.d, wave, lane);
+    ks.load(0, lds0, wave);
+    vs.load(0, lds0 + 2 * TILE, wave);
+    if (tiles > 1) {
+      ks.load(1, lds0 + TILE, wave);
+      vs.load(1, lds0 + 3 * TILE, wave);
     }
-    const int j0 = t * BN;
-    if (j0 + BN <= all) tile(j0, std::false_type());
-    else if (j0 < some) tile(j0, std::true_type());
-    lds.move(t & 1 ? -STAGE : STAGE);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+  }
+  f32x16 z[2];
+  if (steps > 0) {
+    z[0] = zero16();
+#pragma unroll
+    for (int s = 0; s < S; s++) z[0] = mfma(lds.rows(0, 0, s), qr[s], z[0]);
+    mask(z[0], 0);
+    float top = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; e++) top = fmaxf(top, z[0][e]);
+    refer(top);
+    each<AHEAD>([&](auto m) { a[decltype(m)::value] = lds.rows(0, 1, decltype(m)::value); });
+  }
+  const std::integral_constant<int, 0> first;
+  const std::integral_constant<int, 1> second;
+  for (int t = 0; t < tiles; t++) {
+    const int n = 2 * t;
+    // Tile t + 1 has landed, for every wave; every wave is done with the keys of tile t and with the values of tile t - 1.
+    auto middle = [&]() {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      if (t + 2 < tiles) {
+        ks.load(t + 2, lds0 + (unsigned)(t & 1) * TILE, wave);
+        vs.load(t + 2, lds0 + 2 * TILE + (unsigned)((t + 2) % 3) * TILE, wave);
+      }
+    };
+    if (n < steps) step(first, std::true_type(), n, z[0], z[1], middle);
+    else middle();
+    if (n + 1 < steps) step(second, std::true_type(), n + 1, z[1], z[0], []() {});
+    lds.tr += t % 3 == 2 ? -2 * TILE : TILE;
+    asm volatile("" : "+v"(lds.tr));
   }
   sum += __shfl_xor(sum, 32, 64);
   if (mine < w.t.len) {
@@ -634,7 +690,7 @@ bool many_keys(const PackedShape& p) {
 template <int D>
 void forward(hipStream_t s, const PackedShape& p, const bf16_t* q, const bf16_t* k, const bf16_t* v, bf16_t* o, float* lse) {
   static std::atomic<uint64_t> done;
-  const int lds = 4 * BN * D * 2;
+  const int lds = 5 * BN * D * 2;
   allow_lds(done, attention_forward_kernel<D>, lds);
   attention_forward_kernel<D><<<(unsigned)(packed_tiles(p.total_q, p.n_seq, BM) * p.nq), 256, lds, s>>>(p, q, k, v, o, lse);
 }
