@@ -226,8 +226,8 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(PackedShape p
   };
   // A step of 32 keys, in slots as in the backward pass: first the scores of the next step beside the exponentials of this one, then
   // this one's values beside the largest of the next scores.
-  constexpr int S = D / 16, AHEAD = 3, EXPS = 3 * S / 2;
-  u32x4 a[4];
+  constexpr int S = D / 16, AHEAD = D == 128 ? 5 : 4, EXPS = 3 * S / 2;
+  u32x4 a[8];
   auto step = [&](auto half, auto more, int n, f32x16& z, f32x16& next, auto middle) {
     constexpr int H = decltype(half)::value;
     constexpr bool MORE = decltype(more)::value;
@@ -243,16 +243,16 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(PackedShape p
         asm volatile("" : "+v"(lds.row));
       }
       if constexpr (later < S) {
-        if constexpr (MORE) a[later & 3] = lds.rows(0, 1 - H, later);
+        if constexpr (MORE) a[later & 7] = lds.rows(0, 1 - H, later);
       } else if constexpr (later < 2 * S) {
-        a[later & 3] = lds.columns(0, H, (later - S) / (D / 32), (later - S) % (D / 32));
+        a[later & 7] = lds.columns(0, H, (later - S) / (D / 32), (later - S) % (D / 32));
       } else if constexpr (MORE) {
-        a[later & 3] = lds.rows(0, H, later - 2 * S);
+        a[later & 7] = lds.rows(0, H, later - 2 * S);
       }
       if constexpr (m < S) {
-        if constexpr (MORE) next = mfma(a[m & 3], qr[m], next);
+        if constexpr (MORE) next = mfma(a[m & 7], qr[m], next);
       } else {
-        acc[(m - S) % (D / 32)] = mfma(a[m & 3], pr[(m - S) / (D / 32)], acc[(m - S) % (D / 32)]);
+        acc[(m - S) % (D / 32)] = mfma(a[m & 7], pr[(m - S) / (D / 32)], acc[(m - S) % (D / 32)]);
       }
       if constexpr (m < EXPS) {
 #pragma unroll
