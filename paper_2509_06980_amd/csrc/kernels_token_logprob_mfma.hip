@@ -28,6 +28,7 @@ namespace {
 enum { EPI_STRIP, EPI_DZ, EPI_SLICE, EPI_OUT };
 
 typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
 
 template <typename T>
 struct Product {
@@ -52,12 +53,23 @@ struct Product {
   int out_rows, out_cols, first;
 };
 
+// LDS of a workgroup: the ring of stages, behind it what an epilogue takes, so that it does not touch the next tile's chunks
+template <typename T, int MB, int NB, int R, int EPI>
+struct Lds {
+  static constexpr int RING = R * (MB + NB) * 4096;
+  static constexpr int ROWS = (MB + 1) / 2, ARRAYS = EPI == EPI_STRIP ? 1 : EPI == EPI_DZ ? 3 : 0;      // of 256 bytes a wave: target; g, lse
+  static constexpr int ROW_DATA = 4 * ARRAYS * ROWS * 256;
+  static constexpr int SC = sizeof(T) == 2 ? 64 : 16, PITCH = SC * sizeof(T) + 16;                      // columns stored at a time
+  static constexpr int BYTES = RING + ROW_DATA + (EPI == EPI_STRIP ? 2 * 64 * MB * 8 : EPI == EPI_SLICE ? 0 : 4 * 32 * PITCH);
+};
 template <typename T, bool TA, bool TB, int MB, int NB, int R, int EPI>
 __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Product<T> P) {
   constexpr bool SWAP = EPI != EPI_SLICE;        // a lane holds one row's values, else one column's
   constexpr int BM = 64 * MB, BN = 64 * NB, EL = sizeof(T), KC = 64 / EL, V = 16 / EL;
   constexpr int NA = 4 * MB, PW = MB + NB, BUF = (NA + 4 * NB) * 1024, F = PW / 2;
   static_assert((!TA || BM * EL >= 256) && (!TB || BN * EL >= 256), "four blocks of 64 bytes a row");
+  using L = Lds<T, MB, NB, R, EPI>;
+  constexpr int RING = L::RING, ROWS = L::ROWS, ARRAYS = L::ARRAYS, ROW_DATA = L::ROW_DATA, SC = L::SC, PITCH = L::PITCH;
   extern __shared__ u32x4 smem[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, wm = wave >> 1, wn = wave & 1;
   const int kept = __builtin_amdgcn_readfirstlane(*P.kept.count);
@@ -65,23 +77,21 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
   const int ti = EPI == EPI_OUT ? P.tiles_i : min(P.tiles_i, (kept + BM - 1) / BM), tiles = ti * P.tiles_j;
   const int slices = EPI == EPI_SLICE ? __builtin_amdgcn_readfirstlane(P.kept.count[1]) : 1, total = tiles * slices;
   if ((int)blockIdx.x >= total) return;
-  int i0, j0, z;
-  {
-    const int base = total >> 3, rem = total & 7, x = blockIdx.x & 7, vid = x * base + min(x, rem) + ((int)blockIdx.x >> 3);
-    z = vid / tiles;
-    const int v = vid - z * tiles, per = P.group * P.tiles_j, grp = v / per, first = grp * P.group, gm = min(P.group, ti - first), in = v - grp * per;
-    // the divisions leave them in vector registers
-    i0 = __builtin_amdgcn_readfirstlane(first + in % gm) * BM;
-    j0 = __builtin_amdgcn_readfirstlane(in / gm) * BN;
-    z = __builtin_amdgcn_readfirstlane(z);
-  }
   const int k_all = EPI == EPI_OUT ? kept : P.k, per_slice = EPI == EPI_SLICE ? __builtin_amdgcn_readfirstlane(P.kept.count[2]) : k_all;
-  const int k_lo = z * per_slice, c0 = k_lo / KC, c1 = (min(k_all, k_lo + per_slice) + KC - 1) / KC;
-  // operands behind these descriptors: what is read past their end arrives as zeros
-  const u32x4 ra = TA ? buffer_rsrc(P.a + i0, (unsigned)(((int64_t)P.a_n * P.lda - i0) * EL))
-                      : buffer_rsrc(P.a + (int64_t)i0 * P.lda, (unsigned)((int64_t)min(P.a_n - i0, BM) * P.lda * EL));
-  const u32x4 rb = TB ? buffer_rsrc(P.b + j0, (unsigned)(((int64_t)P.b_n * P.ldb - j0) * EL))
-                      : buffer_rsrc(P.b + (int64_t)j0 * P.ldb, (unsigned)((int64_t)min(P.b_n - j0, BN) * P.ldb * EL));
+  struct Place {
+    int i0, j0, z, c0, c1;      // first row and column, slice, its chunks of k
+  };
+  auto place = [&](int id) {
+    const int base = total >> 3, rem = total & 7, x = id & 7, vid = x * base + min(x, rem) + (id >> 3), slice = vid / tiles;
+    const int v = vid - slice * tiles, per = P.group * P.tiles_j, grp = v / per, first = grp * P.group, gm = min(P.group, ti - first), in = v - grp * per;
+    Place t;      // the divisions leave these in vector registers
+    t.i0 = __builtin_amdgcn_readfirstlane(first + in % gm) * BM;
+    t.j0 = __builtin_amdgcn_readfirstlane(in / gm) * BN;
+    t.z = __builtin_amdgcn_readfirstlane(slice);
+    const int k_lo = t.z * per_slice;
+    t.c0 = k_lo / KC, t.c1 = (min(k_all, k_lo + per_slice) + KC - 1) / KC;
+    return t;
+  };
   const unsigned sa = TA ? (unsigned)P.lda * 64u : 64u, sb = TB ? (unsigned)P.ldb * 64u : 64u;      // bytes of a chunk's step
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
   int va[MB], vb[NB];      // this lane's offset of each piece that its wave loads
@@ -98,19 +108,31 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
   for (int j = 0; j < MB; j++) va[j] = offset(j, P.lda, TA, BM * EL);
 #pragma unroll
   for (int j = 0; j < NB; j++) vb[j] = offset(j, P.ldb, TB, BN * EL);
-  // piece j of this wave of a chunk; chunks behind the slice's end: the last one again, never read
-  auto load = [&](int chunk, int j, int stage) {
-    const unsigned dst = lds0 + (unsigned)stage * BUF + (unsigned)(j * 4 + wave) * 1024u, c = (unsigned)min(chunk, c1 - 1);
-    if (j < MB) load_to_lds(dst, va[j], ra, c * sa);
-    else load_to_lds(dst, vb[j - MB], rb, c * sb);
+  // The loads run R - 1 chunks ahead of the products, from one tile of the workgroup into the next: tile `at`, its chunk c, operands
+  // behind its descriptors (what is read past their end arrives as zeros).  Behind the last tile: its last chunk again, never read.
+  u32x4 ra, rb;
+  int at = (int)blockIdx.x - (int)gridDim.x, lc = 0, lend = 0;
+  auto advance = [&]() {
+    if (++lc < lend) return;
+    for (at += gridDim.x; at < total; at += gridDim.x) {
+      const Place t = place(at);
+      if (t.c1 <= t.c0) continue;
+      ra = TA ? buffer_rsrc(P.a + t.i0, (unsigned)(((int64_t)P.a_n * P.lda - t.i0) * EL))
+              : buffer_rsrc(P.a + (int64_t)t.i0 * P.lda, (unsigned)((int64_t)min(P.a_n - t.i0, BM) * P.lda * EL));
+      rb = TB ? buffer_rsrc(P.b + t.j0, (unsigned)(((int64_t)P.b_n * P.ldb - t.j0) * EL))
+              : buffer_rsrc(P.b + (int64_t)t.j0 * P.ldb, (unsigned)((int64_t)min(P.b_n - t.j0, BN) * P.ldb * EL));
+      lc = t.c0, lend = t.c1;
+      asm volatile("s_nop 4" ::: "memory");      // scalars from vector instructions, read by the loads
+      return;
+    }
+    lc = lend - 1;
+  };
+  auto load = [&](int j, int stage) {      // piece j of this wave
+    const unsigned dst = lds0 + (unsigned)stage * BUF + (unsigned)(j * 4 + wave) * 1024u;
+    if (j < MB) load_to_lds(dst, va[j], ra, (unsigned)lc * sa);
+    else load_to_lds(dst, vb[j - MB], rb, (unsigned)lc * sb);
   };
   f32x16 acc[MB][NB];
-#pragma unroll
-  for (int a = 0; a < MB; a++)
-#pragma unroll
-    for (int b = 0; b < NB; b++)
-#pragma unroll
-      for (int e = 0; e < 16; e++) acc[a][b][e] = 0.f;
   auto mfma = [&](const u32x4& row, const u32x4& col, f32x16& c) {
     const u32x4 &x = SWAP ? col : row, &y = SWAP ? row : col;
     if constexpr (EL == 2) {
@@ -160,22 +182,50 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
     if constexpr (TB) return strided(base + kb * (KC / 2) * BN * EL + lb[x], std::integral_constant<int, BN * EL>());
     else return *(__attribute__((address_space(3))) u32x4*)(lds + base + (wn * NB + x) * 2048 + lb[kb]);
   };
-  if (c1 > c0) {
-    u32x4 av[2][MB], bv[2][NB];
+  advance();
+  if (lend > 0) {
+#pragma unroll 1
+    for (int c = 0; c < R - 1; c++) {
 #pragma unroll
-    for (int c = 0; c < R - 1; c++)
+      for (int j = 0; j < PW; j++) load(j, c);
+      advance();
+    }
 #pragma unroll
-      for (int j = 0; j < PW; j++) load(c0 + c, j, c);
-#pragma unroll
-    for (int j = 0; j < F; j++) load(c0 + R - 1, j, R - 1);
+    for (int j = 0; j < F; j++) load(j, R - 1);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"((R - 2) * PW + F) : "memory");
     __builtin_amdgcn_s_barrier();
+  }
+  int sc = 0, sl = R - 1;                  // stages of chunks c and c + R - 1 (that of chunk c - 1)
+  for (int id = blockIdx.x; id < total; id += gridDim.x) {
+  const Place here = place(id);
+  const int i0 = here.i0, j0 = here.j0, z = here.z;
+  if constexpr (EPI == EPI_STRIP || EPI == EPI_DZ) {      // what the epilogue needs of the wave's rows
+    auto fetch = [&](const void* p, int which) {
+      const u32x4 r = buffer_rsrc(p, (unsigned)P.a_n * 4u);
+      asm volatile("s_nop 4" ::: "memory");
 #pragma unroll
-    for (int x = 0; x < MB; x++) av[0][x] = read_a(x, 0, 0);
+      for (int m = 0; m < ROWS; m++)
+        load_dword_to_lds(lds0 + RING + (unsigned)(wave * ARRAYS + which) * (ROWS * 256u) + m * 256u, lane * 4, r, (unsigned)(i0 + wm * 32 * MB + m * 64) * 4u);
+    };
+    fetch(P.kept.target, 0);
+    if constexpr (EPI == EPI_DZ) {
+      fetch(P.kept.g, 1);
+      fetch(P.kept.lse, 2);
+    }
+  }
 #pragma unroll
-    for (int x = 0; x < NB; x++) bv[0][x] = read_b(x, 0, 0);
-    int sc = 0, sl = R - 1;                  // stages of chunks c and c + R - 1 (that of chunk c - 1)
-    for (int c = c0; c < c1; c++) {
+  for (int a = 0; a < MB; a++)
+#pragma unroll
+    for (int b = 0; b < NB; b++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) acc[a][b][e] = 0.f;
+  if (here.c1 > here.c0) {      // its first chunk has landed for every wave
+    u32x4 av[2][MB], bv[2][NB];
+#pragma unroll
+    for (int x = 0; x < MB; x++) av[0][x] = read_a(x, 0, sc);
+#pragma unroll
+    for (int x = 0; x < NB; x++) bv[0][x] = read_b(x, 0, sc);
+    for (int c = here.c0; c < here.c1; c++) {
       const int sn = sc + 1 == R ? 0 : sc + 1;
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -184,6 +234,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
         if (g == MB) {     // chunk c + 1 has landed for every wave, chunk c is read out by every wave
           asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((R - 2) * PW) : "memory");
           __builtin_amdgcn_s_barrier();
+          advance();
         }
         const int stage = st == 0 ? sc : sn, kb = 1 - st;
         // the operands of the next 16 k, in the order of their use
@@ -197,8 +248,8 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
         // this step's share of the loads: the rest of chunk c + R - 1, then the first F pieces of chunk c + R
 #pragma unroll
         for (int j = 0; j < PW; j++) {
-          if (st == 0 && j >= F && (j - F) * MB / (PW - F) == a) load(c + R - 1, j, sl);
-          if (st == 1 && j < F && j * MB / F == a) load(c + R, j, sc);
+          if (st == 0 && j >= F && (j - F) * MB / (PW - F) == a) load(j, sl);
+          if (st == 1 && j < F && j * MB / F == a) load(j, sc);
         }
 #pragma unroll
         for (int b = 0; b < NB; b++) mfma(av[st][a], bv[st][b], acc[a][b]);
@@ -208,16 +259,22 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
       sc = sn;
     }
   }
-  // all loads into LDS are done; results of the last instructions may be read by the assembly below
-  asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
-  __syncthreads();                                      // and nobody reads the stages any more
+  // results of the last instructions may be read by the assembly below; the rows' data is older than the loads still under way, if
+  // those are all of this tile
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+  if ((EPI == EPI_STRIP || EPI == EPI_DZ) && here.c1 - here.c0 < R) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
+  int ln = lane;
+  asm volatile("" : "+v"(ln));      // or what follows from the lane alone is kept in registers through the products
   // one element of a result: read as a whole, the 16 registers of an accumulator would be copied and spill
   auto val = [&](int a, int b, int e) {
-    if (MB == 2) return acc[a][b][e];
+    if (MB * NB <= 8) return acc[a][b][e];
     float x;
     asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[a][b][e]));
     return x;
+  };
+  auto row_data = [&](int a, int which) {
+    return *(__attribute__((address_space(3))) unsigned*)(lds + RING + (wave * ARRAYS + which) * (ROWS * 256) + (a * 32 + (ln & 31)) * 4);
   };
   if constexpr (EPI == EPI_SLICE) {
     float* const out = P.slice + z * P.slice_stride + (int64_t)i0 * P.ldo + j0;      // offsets inside a tile fit 32 bits
@@ -226,7 +283,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
     for (int a = 0; a < MB; a++) {
 #pragma unroll
       for (int b = 0; b < NB; b++) {
-        const int j = wn * 32 * NB + b * 32 + (lane & 31), r = (wm * MB + a) * 32 + 4 * (lane >> 5);
+        const int j = wn * 32 * NB + b * 32 + (ln & 31), r = (wm * MB + a) * 32 + 4 * (ln >> 5);
         if (j0 + j < P.out_cols) {
           const unsigned at = (unsigned)r * ld + j;
 #pragma unroll
@@ -240,15 +297,15 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
         __builtin_amdgcn_sched_barrier(0);      // one block's addresses at a time
       }
     }
-    return;
+    continue;
   }
-  const int jw = wn * 32 * NB + 4 * (lane >> 5);      // column of register e of block b: jw + 32 b + 8 (e / 4) + e % 4
+  const int jw = wn * 32 * NB + 4 * (ln >> 5);      // column of register e of block b: jw + 32 b + 8 (e / 4) + e % 4
   const bool crosses = (EPI == EPI_STRIP || EPI == EPI_DZ) && P.v0 + j0 + BN > P.vocab;
   if constexpr (EPI == EPI_STRIP) {
-    float2* half = (float2*)smem;
+    __attribute__((address_space(3))) f32x2* const half = (__attribute__((address_space(3))) f32x2*)(lds + RING + ROW_DATA);
 #pragma unroll
     for (int a = 0; a < MB; a++) {
-      const int il = (wm * MB + a) * 32 + (lane & 31), i = i0 + il, y = i < kept ? P.kept.target[i] - j0 : -1;
+      const int il = (wm * MB + a) * 32 + (ln & 31), i = i0 + il, y = (int)row_data(a, 0) - j0;      // padding: negative
       float top = -INFINITY, sum = 0.f;
       auto strip = [&](auto some) {      // some: a target or the vocabulary's end is in the tile
         auto at = [&](int b, int e) {
@@ -274,73 +331,73 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
       };
       if (crosses || __any(y >= 0 && y < BN)) strip(std::true_type());
       else strip(std::false_type());
-      if (lane < 32) half[wn * BM + il] = make_float2(top, sum);
+      if (ln < 32) half[wn * BM + il] = f32x2{top, sum};
       __builtin_amdgcn_sched_barrier(0);      // one row block at a time
     }
-    __syncthreads();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
     if (tid < BM && i0 + tid < kept) {
-      const float2 a = half[tid], b = half[BM + tid];
-      const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.f : top;
+      const f32x2 a = half[tid], b = half[BM + tid];
+      const float top = fmaxf(a[0], b[0]), ref = top == -INFINITY ? 0.f : top;
       P.part[(size_t)(j0 / BN) * P.padded + i0 + tid] =
-          make_float2(top * P.inv_t, a.y * exp2f((a.x - ref) * P.scale) + b.y * exp2f((b.x - ref) * P.scale));
+          make_float2(top * P.inv_t, a[1] * exp2f((a[0] - ref) * P.scale) + b[1] * exp2f((b[0] - ref) * P.scale));
     }
-    return;
+    continue;
   }
-  // the tile through LDS, rows 16 bytes apart
-  constexpr int PITCH = BN * EL + 16;
+  // 32 rows x SC columns at a time through LDS of the wave's own, rows 16 bytes apart, so that a row is stored in pieces of SC
+  lds_char* const mine = lds + RING + ROW_DATA + wave * (32 * PITCH);
+  auto store = [&](int a, auto out) {      // out(b, e): element e of block b
 #pragma unroll
-  for (int a = 0; a < MB; a++) {
-    const int il = (wm * MB + a) * 32 + (lane & 31);
-    if constexpr (EPI == EPI_DZ) {
-      const int i = i0 + il, y = P.kept.target[i] - P.v0 - j0;
-      const float g = P.kept.g[i], l = P.kept.lse[i] * 1.44269504f;
+    for (int n = 0; n < 32 * NB / SC; n++) {
 #pragma unroll
-      for (int b = 0; b < NB; b++)
-#pragma unroll
-        for (int e = 0; e < 16; e++) acc[a][b][e] = -g * __builtin_amdgcn_exp2f(fmaf(acc[a][b][e], P.scale, -l));
-      if (crosses || __any(y >= 0 && y < BN)) {
-#pragma unroll
-        for (int b = 0; b < NB; b++)
-#pragma unroll
-          for (int e = 0; e < 16; e++) {
-            const int j = jw + 32 * b + 8 * (e >> 2) + (e & 3);
-            if (j == y) acc[a][b][e] += g;
-            if (P.v0 + j0 + j >= P.vocab) acc[a][b][e] = 0.f;
-          }
-      }
-    }
-    auto out = [&](int b, int e) { return EPI == EPI_DZ ? acc[a][b][e] : val(a, b, e); };
-#pragma unroll
-    for (int b = 0; b < NB; b++)
-#pragma unroll
-      for (int q = 0; q < 4; q++) {
-        lds_char* const to = lds + il * PITCH + (jw + 32 * b + 8 * q) * EL;
+      for (int u = 0; u < SC / 8; u++) {
+        const int b = (n * SC + 8 * u) / 32, e = (n * SC + 8 * u) % 32 / 2;
+        lds_char* const to = mine + (ln & 31) * PITCH + (8 * u + 4 * (ln >> 5)) * EL;
         if constexpr (EL == 2) {
           typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
-          *(__attribute__((address_space(3))) bf16x4*)to = bf16x4{(__bf16)out(b, 4 * q), (__bf16)out(b, 4 * q + 1), (__bf16)out(b, 4 * q + 2), (__bf16)out(b, 4 * q + 3)};
+          *(__attribute__((address_space(3))) bf16x4*)to = bf16x4{(__bf16)out(b, e), (__bf16)out(b, e + 1), (__bf16)out(b, e + 2), (__bf16)out(b, e + 3)};
         } else {
-          *(__attribute__((address_space(3))) f32x4*)to = f32x4{out(b, 4 * q), out(b, 4 * q + 1), out(b, 4 * q + 2), out(b, 4 * q + 3)};
+          *(__attribute__((address_space(3))) f32x4*)to = f32x4{out(b, e), out(b, e + 1), out(b, e + 2), out(b, e + 3)};
         }
-        if (q == 3) __builtin_amdgcn_sched_barrier(0);
       }
-  }
-  __syncthreads();
-  constexpr int LANES = BN / V;      // of a row
-  const int c = tid % LANES * V;
-  if (j0 + c < P.out_cols) {
-#pragma unroll 4
-    for (int r = tid / LANES; r < BM; r += 256 / LANES) {
-      if (i0 + r >= P.out_rows) break;
-      const u32x4 v = *(__attribute__((address_space(3))) u32x4*)(lds + r * PITCH + c * EL);
-      __builtin_nontemporal_store(v, (u32x4*)(P.out + (int64_t)(i0 + r) * P.ldo + j0 + c));
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      constexpr int LANES = SC / V;      // of a row
+      const int c = wn * 32 * NB + n * SC + ln % LANES * V, r0 = (wm * MB + a) * 32;
+#pragma unroll
+      for (int r = ln / LANES; r < 32; r += 64 / LANES) {
+        const u32x4 v = *(__attribute__((address_space(3))) u32x4*)(mine + r * PITCH + ln % LANES * 16);
+        if (j0 + c < P.out_cols && i0 + r0 + r < P.out_rows)
+          __builtin_nontemporal_store(v, (u32x4*)(P.out + (int64_t)(i0 + r0 + r) * P.ldo + j0 + c));
+      }
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+#pragma unroll
+  for (int a = 0; a < MB; a++) {
+    if constexpr (EPI == EPI_DZ) {
+      const int y = (int)row_data(a, 0) - P.v0 - j0;
+      const float g = __builtin_bit_cast(float, row_data(a, 1)), l = __builtin_bit_cast(float, row_data(a, 2)) * 1.44269504f;
+      auto dz = [&](int b, int e) { return -g * __builtin_amdgcn_exp2f(fmaf(val(a, b, e), P.scale, -l)); };
+      if (crosses || __any(y >= 0 && y < BN)) {
+        store(a, [&](int b, int e) {
+          const int j = jw + 32 * b + 8 * (e >> 2) + (e & 3);
+          return P.v0 + j0 + j >= P.vocab ? 0.f : j == y ? dz(b, e) + g : dz(b, e);
+        });
+      } else {
+        store(a, dz);
+      }
+    } else {
+      store(a, [&](int b, int e) { return val(a, b, e); });
     }
   }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // loads into this LDS
 }
 
 template <typename T, bool TA, bool TB, int MB, int NB, int R, int EPI>
 void go(const Product<T>& p, hipStream_t s) {
-  constexpr int ring = R * (MB + NB) * 4096, tile = 64 * MB * (64 * NB * (int)sizeof(T) + 16);
-  constexpr int lds = EPI != EPI_SLICE && tile > ring ? tile : ring;
+  constexpr int lds = Lds<T, MB, NB, R, EPI>::BYTES;
   auto kernel = product_kernel<T, TA, TB, MB, NB, R, EPI>;
   static std::atomic<uint64_t> done;      // more than 64 KB of LDS need an opt-in, once per kernel and device
   int dev = 0;
@@ -350,7 +407,8 @@ void go(const Product<T>& p, hipStream_t s) {
     (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     done.fetch_or(bit, std::memory_order_release);
   }
-  kernel<<<(unsigned)(p.tiles_i * p.tiles_j * p.slices), 256, lds, s>>>(p);
+  // as many workgroups as the 256 CUs hold at once
+  kernel<<<(unsigned)std::min<int64_t>((int64_t)p.tiles_i * p.tiles_j * p.slices, MB * NB > 4 ? 256 : 512), 256, lds, s>>>(p);
 }
 
 // Tile of a product, in 64 rows and 64 columns.  bf16: 256 x 256, for up to 128 rows 128 x 256.  fp32 (16 times the matrix time a byte):
@@ -367,7 +425,7 @@ void go(Product<T>& p, const Tile& t, int64_t rows, int64_t columns, hipStream_t
   p.tiles_i = (int)((rows + 64 * t.mb - 1) / (64 * t.mb)), p.tiles_j = (int)((columns + 64 * t.nb - 1) / (64 * t.nb));
   if constexpr (sizeof(T) == 2) {
     if constexpr (!TA) {
-      if (t.mb == 2) return go<T, TA, TB, 2, 4, 6, EPI>(p, s);
+      if (t.mb == 2) return go<T, TA, TB, 2, 4, 5, EPI>(p, s);
     }
     go<T, TA, TB, 4, 4, 4, EPI>(p, s);
   } else {
