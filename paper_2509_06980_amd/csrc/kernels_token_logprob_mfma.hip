@@ -308,6 +308,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
       const int il = (wm * MB + a) * 32 + (ln & 31), i = i0 + il, y = (int)row_data(a, 0) - j0;      // padding: negative
       float top = -INFINITY, sum = 0.f;
       auto strip = [&](auto some) {      // some: a target or the vocabulary's end is in the tile
+        float x[NB][16];
         auto at = [&](int b, int e) {
           const int j = jw + 32 * b + 8 * (e >> 2) + (e & 3);
           const float v = val(a, b, e);
@@ -317,7 +318,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
         for (int b = 0; b < NB; b++)
 #pragma unroll
           for (int e = 0; e < 16; e++) {
-            const float v = at(b, e);
+            const float v = x[b][e] = at(b, e);
             if (decltype(some)::value && jw + 32 * b + 8 * (e >> 2) + (e & 3) == y) P.zt[i] = v * P.inv_t;
             top = fmaxf(top, v);
           }
@@ -326,7 +327,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
 #pragma unroll
         for (int b = 0; b < NB; b++)
 #pragma unroll
-          for (int e = 0; e < 16; e++) sum += __builtin_amdgcn_exp2f(fmaf(at(b, e), P.scale, -ref));
+          for (int e = 0; e < 16; e++) sum += __builtin_amdgcn_exp2f(fmaf(x[b][e], P.scale, -ref));
         sum += __shfl_xor(sum, 32, 64);
       };
       if (crosses || __any(y >= 0 && y < BN)) strip(std::true_type());
