@@ -23,6 +23,10 @@ namespace {
 // wave reads 1 KB per product instruction.
 // LDS: rows of D elements, 16-byte piece p of row r at p ^ f(r).  f moves 16 rows of one piece (read as they lie) to different
 // banks, and the 4 rows x 32 columns of a transposing read as well.
+// The two waves of a SIMD ought to be in different parts of a step, one at the products alone while the other has exponentials to
+// form.  Issue priority (s_setprio) for the part with the arithmetic keeps them so; measured for one sequence of 8192, 16 heads of
+// 128, with it and without: forward 278 and 297 us, dq 359 and 386, dk and dv 557 and 583.  Where it begins and ends is worth as much: dq
+// with its end half a pass later 389.
 // =============================================================================================
 constexpr int BM = 128, BN = 64;      // rows owned, rows of a stage
 constexpr int DKV_ROWS = 128;         // keys owned by a workgroup of attention_dkv_kernel
@@ -237,6 +241,8 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(PackedShape p
     if constexpr (MORE) next = zero16();
     each<2 * S>([&](auto slot) {
       constexpr int m = decltype(slot)::value, later = m + AHEAD;
+      if constexpr (m == S / 2) __builtin_amdgcn_s_setprio(1);
+      if constexpr (m == EXPS) __builtin_amdgcn_s_setprio(0);
       if constexpr (m == S && H == 0) middle();      // the next tile has landed
       if constexpr (later == 2 * S && H == 0 && MORE) {      // every read of this tile's keys is under way
         lds.row += (n >> 1 & 1) ? -TILE : TILE;
@@ -395,6 +401,8 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(PackedShape p, con
     for (int e = 0; e < 16; e++) z[e] = 0.f, dp[e] = -dl;
     each<SLOTS>([&](auto slot) {
       constexpr int n = decltype(slot)::value, m = n % S, later = n + AHEAD;
+      if constexpr (n == S / 2) __builtin_amdgcn_s_setprio(1);
+      if constexpr (n == 2 * S) __builtin_amdgcn_s_setprio(0);
       if constexpr (later < SLOTS) a[later & 3] = read(std::integral_constant<int, later>());
       const u32x4 row = a[n & 3];
       if constexpr (n < S) {                   // scores
@@ -540,6 +548,8 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
     }
     each<SLOTS>([&](auto slot) {
       constexpr int n = decltype(slot)::value, m = n % S, later = n + AHEAD;
+      if constexpr (n == 0) __builtin_amdgcn_s_setprio(1);
+      if constexpr (n == 2 * S) __builtin_amdgcn_s_setprio(0);
       if constexpr (MID && (n == 0 || n == 2 * S)) {
         if ((wave >> 2) == (n == 0)) middle();
       }
