@@ -378,8 +378,10 @@ void launch_rows(int tiles, int heads, int lds, hipStream_t s, A... args) {
   }
   kernel<<<dim3(tiles, heads), 256, lds, s>>>(args...);
 }
-// Rows split over four waves where whole tiles would be fewer than two workgroups a CU.
-bool split_rows(int total, int n_seq, int heads) { return (int64_t)packed_tiles(total, n_seq, 64) * heads < 512; }
+// 16 rows split over four waves in place of 64 rows, 16 a wave, where tiles of 64 would leave half the CUs idle.  Measured, forward and
+// backward of one sequence in 64 and 128 dimensions: 1024 tokens, 4 heads (68 tiles) 148 and 347 us, unsplit 324 and 629; 8 heads (136) 373
+// and 668, unsplit 370 and 678; 16 heads (272) 617 and 1049, unsplit 497 and 858.
+bool split_rows(int total, int n_seq, int heads) { return (int64_t)packed_tiles(total, n_seq, 64) * heads < 128; }
 template <int D>
 constexpr int rows_lds(int split) {      // what the largest of the kernels needs: two tiles, two sets of scores
   return (BN * split * 2 * (D + PAD) + 2 * 4 * 16 * (BN + 4)) * 4;

@@ -412,13 +412,15 @@ void go(const Product<T>& p, hipStream_t s) {
   kernel<<<(unsigned)std::min<int64_t>((int64_t)p.tiles_i * p.tiles_j * p.slices, MB * NB > 4 ? 256 : 512), 256, lds, s>>>(p);
 }
 
-// Tile of a product, in 64 rows and 64 columns.  bf16: 256 x 256, for up to 128 rows 128 x 256.  fp32 (16 times the matrix time a byte):
-// 128 x 128, and 64 x 64 where those would leave CUs idle.
+// Tile of a product, in 64 rows and 64 columns.  bf16: 256 x 256, for up to 128 rows 128 x 256 (1024 x 151936, forward: 100 rows 109 us,
+// with 256 x 256 124; 200 rows 141 and 131).  fp32 (16 times the matrix time a byte): 128 x 128, and 64 x 64 where those would be fewer than two
+// for each of the 512 workgroups that the card holds (both directions: 1000 rows x 256 x 4096 99 us, with 128 x 128 142; 1000 x 1024
+// x 8192 434 and 468; 1500 x 1024 x 16384 1155 and 1027).
 struct Tile { int mb, nb; };
 template <typename T>
 Tile tile_of(int64_t rows, int64_t columns, int64_t slices, bool gathered) {
   if (sizeof(T) == 2) return {gathered && rows <= 128 ? 2 : 4, 4};
-  const bool small = (rows + 127) / 128 * ((columns + 127) / 128) * slices < 256;
+  const bool small = (rows + 127) / 128 * ((columns + 127) / 128) * slices < 1024;
   return {small ? 1 : 2, small ? 1 : 2};
 }
 template <typename T, bool TA, bool TB, int EPI>
