@@ -91,6 +91,19 @@ def test_norm(rows, width, centered, dt):
         assert mean is None and db is None
 
 
+@pytest.mark.parametrize("centered", [False, True])
+@pytest.mark.parametrize("rows,width", [(1, 3080), (600, 3400), (1030, 4088)])
+def test_norm_of_wide_bf16_rows(rows, width, centered):
+    g = gen(rows + width)
+    x, w, dy = randn(g, rows, width, dt=BF) * 2 + 0.25, (1 + randn(g, width, std=0.2)).to(BF), randn(g, rows, width, dt=BF)
+    bias = randn(g, width, dt=BF) if centered else None
+    y, mean, rstd = ops.norm_forward(x, w, bias, eps=1e-6, centered=centered)
+    dx, dw, db = ops.norm_backward(dy, x, w, mean, rstd, centered=centered)
+    ref = norm_reference(x, w, bias, 1e-6, centered, dy, BF)
+    for name, got in (("y", y), ("dx", dx), ("dw", dw)) + ((("db", db),) if centered else ()):
+        within(name, got, *ref[name])
+
+
 @pytest.mark.parametrize("dt", [BF, FP])
 def test_norm_of_heads_in_a_fused_projection(dt):
     g = gen(5)
@@ -284,6 +297,21 @@ def test_attention_where_whole_tiles_fill_the_chip(dt, lq, lk, nq, nk, d):
 
 
 @pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("causal,d", [(True, 128), (False, 64)])
+def test_attention_with_a_negative_scale(dt, causal, d):
+    lens, nq, nk = [150, 3, 260], 4, 2
+    g = gen(17)
+    q, do = randn(g, sum(lens), nq, d, dt=dt), randn(g, sum(lens), nq, d, dt=dt)
+    k, v = randn(g, sum(lens), nk, d, dt=dt), randn(g, sum(lens), nk, d, dt=dt)
+    cu = offsets(lens)
+    o, lse = ops.attention_forward(q, k, v, cu, cu, causal=causal, scale=-0.3)
+    dq, dk, dv = ops.attention_backward(do, q, k, v, o, lse, cu, cu, causal=causal, scale=-0.3)
+    want, err = attention_reference(q, k, v, do, lens, lens, causal, -0.3, dt, True)
+    for name, got in (("o", o), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        within(name, got, want[name], err[name])
+
+
+@pytest.mark.parametrize("dt", [BF, FP])
 def test_attention_of_views_and_large_scores(dt):
     g = gen(3)
     lens = [70, 5, 200]
@@ -393,6 +421,22 @@ def test_token_logprobs(rows, hidden, vocab, sampled, dt):
     for name, got in (("logp", logp), ("lse", lse), ("dh", dh), ("dw", dw)):
         within(name, got, *ref[name])
     assert not dh[(y < 0) | (dlogp == 0)].any()
+
+
+@pytest.mark.parametrize("dt,rows,hidden,vocab", [(BF, 300, 64, 160_000), (BF, 90, 8, 150_001), (FP, 300, 64, 20_001), (FP, 700, 8, 40_003),
+                                                  (FP, 40, 4, 70_000)])
+def test_token_logprobs_of_many_tiles_a_workgroup(dt, rows, hidden, vocab):
+    g = gen(rows + vocab)
+    w, h = randn(g, vocab, hidden, dt=dt, std=2 / math.sqrt(hidden)), randn(g, rows, hidden, dt=dt)
+    y = torch.randint(0, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    y[::7] = -1
+    y[1], y[2] = 0, vocab - 1
+    dlogp = randn(g, rows)
+    logp, lse = ops.token_logprobs_forward(h, w, y, 0.7)
+    dh, dw = ops.token_logprobs_backward(dlogp, h, w, y, lse, 0.7)
+    ref = logprob_reference(h, w, y, dlogp, 0.7, dt)
+    for name, got in (("logp", logp), ("lse", lse), ("dh", dh), ("dw", dw)):
+        within(name, got, *ref[name])
 
 
 @pytest.mark.parametrize("dt", [BF, FP])
