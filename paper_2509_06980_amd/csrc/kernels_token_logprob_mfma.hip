@@ -277,6 +277,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
     return *(__attribute__((address_space(3))) unsigned*)(lds + RING + (wave * ARRAYS + which) * (ROWS * 256) + (a * 32 + (ln & 31)) * 4);
   };
   if constexpr (EPI == EPI_SLICE) {
+    // rows up to the padding are written, kept or not; a piece behind the first adds to what is there
     float* const out = P.slice + z * P.slice_stride + (int64_t)i0 * P.ldo + j0;      // offsets inside a tile fit 32 bits
     const unsigned ld = (unsigned)P.ldo;
 #pragma unroll
@@ -285,14 +286,16 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
       for (int b = 0; b < NB; b++) {
         const int j = wn * 32 * NB + b * 32 + (ln & 31), r = (wm * MB + a) * 32 + 4 * (ln >> 5);
         if (j0 + j < P.out_cols) {
-          const unsigned at = (unsigned)r * ld + j;
+          float* const p = out + ((unsigned)r * ld + j);
+          float old[16];
 #pragma unroll
-          for (int e = 0; e < 16; e++) {
-            const int d = 8 * (e >> 2) + (e & 3);
-            if (i0 + r + d >= kept) continue;
-            float* p = out + (at + (unsigned)d * ld);
-            __builtin_nontemporal_store(P.first ? val(a, b, e) : *p + val(a, b, e), p);
+          for (int e = 0; e < 16; e++) old[e] = 0.f;
+          if (!P.first) {
+#pragma unroll
+            for (int e = 0; e < 16; e++) old[e] = p[(unsigned)(8 * (e >> 2) + (e & 3)) * ld];
           }
+#pragma unroll
+          for (int e = 0; e < 16; e++) __builtin_nontemporal_store(old[e] + val(a, b, e), p + (unsigned)(8 * (e >> 2) + (e & 3)) * ld);
         }
         __builtin_amdgcn_sched_barrier(0);      // one block's addresses at a time
       }

@@ -168,8 +168,8 @@ def main():
     from . import RolloutEngine
     shape = SHAPES["small-d128"]
     model = PolicyModel(make_weight_blob(shape, seed=1, weight_std=0.03))
-    optimizer = torch.optim.Adam(model.parameters(), lr=2e-3)
-    prompts, group, n_new = 8, 8, 24
+    optimizer = torch.optim.Adam(model.parameters(), lr=5e-3)
+    prompts, group, n_new = 8, 32, 24
     rng = np.random.default_rng(0)
     for step in range(10):
         engine = RolloutEngine(model.to_blob(), max_context=128, max_trajectories=prompts * group, kv_pool_pages=prompts * group * 8)
