@@ -9,7 +9,7 @@ namespace {
 // z = h W^T / T, lse = log sum_v e^(z_v), logp = z_y - lse.  Backward: dz_v = g / T ([v = y] - e^(z_v - lse)), dh = dz W, dW = dz^T h.
 // Forward: the product's epilogue leaves (max, sum of e^(z - max)) of every row and strip of the vocabulary, a second kernel joins
 // the strips.  Backward: a piece of the vocabulary at a time, its logits are formed again and only dz is stored, in the type of the
-// weights, since it is an operand of the two products behind it; dh is added up over the pieces in 32 bits and rounded once.
+// weights, since it is an operand of the two products behind it (relative error of the gradients: sqrt 2 times that of their last rounding); dh is added up over the pieces in 32 bits and rounded once.
 // Rows without target (observation tokens) or, backward, with g = 0 take no part: the others are gathered first.
 // =============================================================================================
 
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(256) void zeros_kernel(uint16_t* __restrict__ p, in
 }
 
 // ---- where everything lies in the workspace ----------------------------------------------------
-// A piece's dz takes up to 512 MB: enough tokens of the vocabulary for full launches at any number of rows that fits a card, and
+// A piece's dz takes up to 1 GB: enough tokens of the vocabulary for full launches at any number of rows that fits a card, and
 // little beside 288 GB.
 const int64_t kPieceBytes = 1ll << 30;
 struct Workspace {

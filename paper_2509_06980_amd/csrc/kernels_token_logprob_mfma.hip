@@ -14,9 +14,16 @@ namespace {
 //   logits          A = hidden rows            B = weights                epilogue: (max, sum) of a tile's logits of a row, or dz
 //   dz W            A = dz                     B = weights, k-strided     epilogue: a slice's sum in 32 bits
 //   dz^T hidden     A = dz, k-strided          B = rows, k-strided        epilogue: rounded
-// Bound by the matrix units (2 flops x rows x hidden x vocab each, 2.5 PFLOP/s peak, held by power below 1.5 for random data), for few
-// rows by the weights' bytes; fp32: 155 TFLOP/s.  A chunk of 64 bytes of k (32; fp32 16) of both operands goes straight from memory into
-// one of R stages in LDS, R - 1 ahead; operands are read half a chunk ahead of the instructions that use them, one barrier a chunk.
+// dz is rounded to the weights' type once, as the operand that it becomes; all sums are kept in 32 bits.
+// Bound by the matrix units (2 flops x rows x hidden x vocab each, 2.5 PFLOP/s peak, held by power: a large library product of random
+// data reaches 1.47, operands of zeros run these 1.2 times as fast), for few rows by the weights' bytes; fp32: 155 TFLOP/s.
+// Measured in bf16, 2744 rows x 2560 x 151936: logits 1.79 ms (1.19 PFLOP/s), dz 1.98 in two pieces, dz W 1.8 (1.19), dz^T hidden 1.83 (1.17);
+// 4096 x 1024 x 151936, logits 1.20 ms (1.06).
+// A chunk of 64 bytes of k (32; fp32 16) of both operands goes straight from memory into one of R stages in LDS, R - 1 ahead;
+// operands are read half a chunk ahead of the instructions that use them, one barrier a chunk.  A workgroup stays for all its tiles
+// and its loads run on into the next one, so a tile ends with its epilogue alone (without that, the last-named logits 1.35 ms).
+// 256 x 256 tiles with one wave a SIMD: a wave of 128 x 128 reads least from LDS for its flops; 128 x 256 with two workgroups a CU, whose
+// epilogues overlap with the other's products, is slower for what it fetches (logits of 2744 rows 2.35 ms against 1.93 then).
 // Operands as they lie in memory, no copy of the weights in another order:
 //   k-contiguous: [row][32 k], 64 bytes a row.  The 16-byte piece p of row r is kept at p ^ (r / 4 % 4), so the 16 rows that a
 //     read takes in one go lie in different banks.
@@ -197,204 +204,204 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
   }
   int sc = 0, sl = R - 1;                  // stages of chunks c and c + R - 1 (that of chunk c - 1)
   for (int id = blockIdx.x; id < total; id += gridDim.x) {
-  const Place here = place(id);
-  const int i0 = here.i0, j0 = here.j0, z = here.z;
-  if constexpr (EPI == EPI_STRIP || EPI == EPI_DZ) {      // what the epilogue needs of the wave's rows
-    auto fetch = [&](const void* p, int which) {
-      const u32x4 r = buffer_rsrc(p, (unsigned)P.a_n * 4u);
-      asm volatile("s_nop 4" ::: "memory");
+    const Place here = place(id);
+    const int i0 = here.i0, j0 = here.j0, z = here.z;
+    if constexpr (EPI == EPI_STRIP || EPI == EPI_DZ) {      // what the epilogue needs of the wave's rows
+      auto fetch = [&](const void* p, int which) {
+        const u32x4 r = buffer_rsrc(p, (unsigned)P.a_n * 4u);
+        asm volatile("s_nop 4" ::: "memory");
 #pragma unroll
-      for (int m = 0; m < ROWS; m++)
-        load_dword_to_lds(lds0 + RING + (unsigned)(wave * ARRAYS + which) * (ROWS * 256u) + m * 256u, lane * 4, r, (unsigned)(i0 + wm * 32 * MB + m * 64) * 4u);
-    };
-    fetch(P.kept.target, 0);
-    if constexpr (EPI == EPI_DZ) {
-      fetch(P.kept.g, 1);
-      fetch(P.kept.lse, 2);
-    }
-  }
-#pragma unroll
-  for (int a = 0; a < MB; a++)
-#pragma unroll
-    for (int b = 0; b < NB; b++)
-#pragma unroll
-      for (int e = 0; e < 16; e++) acc[a][b][e] = 0.f;
-  if (here.c1 > here.c0) {      // its first chunk has landed for every wave
-    u32x4 av[2][MB], bv[2][NB];
-#pragma unroll
-    for (int x = 0; x < MB; x++) av[0][x] = read_a(x, 0, sc);
-#pragma unroll
-    for (int x = 0; x < NB; x++) bv[0][x] = read_b(x, 0, sc);
-    for (int c = here.c0; c < here.c1; c++) {
-      const int sn = sc + 1 == R ? 0 : sc + 1;
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int g = 0; g < 2 * MB; g++) {
-        const int a = g % MB, st = g / MB;
-        if (g == MB) {     // chunk c + 1 has landed for every wave, chunk c is read out by every wave
-          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((R - 2) * PW) : "memory");
-          __builtin_amdgcn_s_barrier();
-          advance();
-        }
-        const int stage = st == 0 ? sc : sn, kb = 1 - st;
-        // the operands of the next 16 k, in the order of their use
-#pragma unroll
-        for (int q = 0; q < MB + NB; q++)
-          if (q * MB / (MB + NB) == a) {
-            const int x = q == 0 ? 0 : q <= NB ? MB + q - 1 : q - NB;
-            if (x < MB) av[1 - st][x] = read_a(x, kb, stage);
-            else bv[1 - st][x - MB] = read_b(x - MB, kb, stage);
-          }
-        // this step's share of the loads: the rest of chunk c + R - 1, then the first F pieces of chunk c + R
-#pragma unroll
-        for (int j = 0; j < PW; j++) {
-          if (st == 0 && j >= F && (j - F) * MB / (PW - F) == a) load(j, sl);
-          if (st == 1 && j < F && j * MB / F == a) load(j, sc);
-        }
-#pragma unroll
-        for (int b = 0; b < NB; b++) mfma(av[st][a], bv[st][b], acc[a][b]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      sl = sc;
-      sc = sn;
-    }
-  }
-  // results of the last instructions may be read by the assembly below; the rows' data is older than the loads still under way, if
-  // those are all of this tile
-  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-  if ((EPI == EPI_STRIP || EPI == EPI_DZ) && here.c1 - here.c0 < R) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-
-  int ln = lane;
-  asm volatile("" : "+v"(ln));      // or what follows from the lane alone is kept in registers through the products
-  // one element of a result: read as a whole, the 16 registers of an accumulator would be copied and spill
-  auto val = [&](int a, int b, int e) {
-    if (MB * NB <= 8) return acc[a][b][e];
-    float x;
-    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[a][b][e]));
-    return x;
-  };
-  auto row_data = [&](int a, int which) {
-    return *(__attribute__((address_space(3))) unsigned*)(lds + RING + (wave * ARRAYS + which) * (ROWS * 256) + (a * 32 + (ln & 31)) * 4);
-  };
-  if constexpr (EPI == EPI_SLICE) {
-    // rows up to the padding are written, kept or not; a piece behind the first adds to what is there
-    float* const out = P.slice + z * P.slice_stride + (int64_t)i0 * P.ldo + j0;      // offsets inside a tile fit 32 bits
-    const unsigned ld = (unsigned)P.ldo;
-#pragma unroll
-    for (int a = 0; a < MB; a++) {
-#pragma unroll
-      for (int b = 0; b < NB; b++) {
-        const int j = wn * 32 * NB + b * 32 + (ln & 31), r = (wm * MB + a) * 32 + 4 * (ln >> 5);
-        if (j0 + j < P.out_cols) {
-          float* const p = out + ((unsigned)r * ld + j);
-          float old[16];
-#pragma unroll
-          for (int e = 0; e < 16; e++) old[e] = 0.f;
-          if (!P.first) {
-#pragma unroll
-            for (int e = 0; e < 16; e++) old[e] = p[(unsigned)(8 * (e >> 2) + (e & 3)) * ld];
-          }
-#pragma unroll
-          for (int e = 0; e < 16; e++) __builtin_nontemporal_store(old[e] + val(a, b, e), p + (unsigned)(8 * (e >> 2) + (e & 3)) * ld);
-        }
-        __builtin_amdgcn_sched_barrier(0);      // one block's addresses at a time
-      }
-    }
-    continue;
-  }
-  const int jw = wn * 32 * NB + 4 * (ln >> 5);      // column of register e of block b: jw + 32 b + 8 (e / 4) + e % 4
-  const bool crosses = (EPI == EPI_STRIP || EPI == EPI_DZ) && P.v0 + j0 + BN > P.vocab;
-  if constexpr (EPI == EPI_STRIP) {
-    __attribute__((address_space(3))) f32x2* const half = (__attribute__((address_space(3))) f32x2*)(lds + RING + ROW_DATA);
-#pragma unroll
-    for (int a = 0; a < MB; a++) {
-      const int il = (wm * MB + a) * 32 + (ln & 31), i = i0 + il, y = (int)row_data(a, 0) - j0;      // padding: negative
-      float top = -INFINITY, sum = 0.f;
-      auto strip = [&](auto some) {      // some: a target or the vocabulary's end is in the tile
-        float x[NB][16];
-        auto at = [&](int b, int e) {
-          const int j = jw + 32 * b + 8 * (e >> 2) + (e & 3);
-          const float v = val(a, b, e);
-          return decltype(some)::value && j0 + j >= P.vocab ? -INFINITY : v;
-        };
-#pragma unroll
-        for (int b = 0; b < NB; b++)
-#pragma unroll
-          for (int e = 0; e < 16; e++) {
-            const float v = x[b][e] = at(b, e);
-            if (decltype(some)::value && jw + 32 * b + 8 * (e >> 2) + (e & 3) == y) P.zt[i] = v * P.inv_t;
-            top = fmaxf(top, v);
-          }
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float ref = top == -INFINITY ? 0.f : top * P.scale;
-#pragma unroll
-        for (int b = 0; b < NB; b++)
-#pragma unroll
-          for (int e = 0; e < 16; e++) sum += __builtin_amdgcn_exp2f(fmaf(x[b][e], P.scale, -ref));
-        sum += __shfl_xor(sum, 32, 64);
+        for (int m = 0; m < ROWS; m++)
+          load_dword_to_lds(lds0 + RING + (unsigned)(wave * ARRAYS + which) * (ROWS * 256u) + m * 256u, lane * 4, r, (unsigned)(i0 + wm * 32 * MB + m * 64) * 4u);
       };
-      if (crosses || __any(y >= 0 && y < BN)) strip(std::true_type());
-      else strip(std::false_type());
-      if (ln < 32) half[wn * BM + il] = f32x2{top, sum};
-      __builtin_amdgcn_sched_barrier(0);      // one row block at a time
+      fetch(P.kept.target, 0);
+      if constexpr (EPI == EPI_DZ) {
+        fetch(P.kept.g, 1);
+        fetch(P.kept.lse, 2);
+      }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    if (tid < BM && i0 + tid < kept) {
-      const f32x2 a = half[tid], b = half[BM + tid];
-      const float top = fmaxf(a[0], b[0]), ref = top == -INFINITY ? 0.f : top;
-      P.part[(size_t)(j0 / BN) * P.padded + i0 + tid] =
-          make_float2(top * P.inv_t, a[1] * exp2f((a[0] - ref) * P.scale) + b[1] * exp2f((b[0] - ref) * P.scale));
-    }
-    continue;
-  }
-  // 32 rows x SC columns at a time through LDS of the wave's own, rows 16 bytes apart, so that a row is stored in pieces of SC
-  lds_char* const mine = lds + RING + ROW_DATA + wave * (32 * PITCH);
-  auto store = [&](int a, auto out) {      // out(b, e): element e of block b
 #pragma unroll
-    for (int n = 0; n < 32 * NB / SC; n++) {
+    for (int a = 0; a < MB; a++)
 #pragma unroll
-      for (int u = 0; u < SC / 8; u++) {
-        const int b = (n * SC + 8 * u) / 32, e = (n * SC + 8 * u) % 32 / 2;
-        lds_char* const to = mine + (ln & 31) * PITCH + (8 * u + 4 * (ln >> 5)) * EL;
-        if constexpr (EL == 2) {
-          typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
-          *(__attribute__((address_space(3))) bf16x4*)to = bf16x4{(__bf16)out(b, e), (__bf16)out(b, e + 1), (__bf16)out(b, e + 2), (__bf16)out(b, e + 3)};
-        } else {
-          *(__attribute__((address_space(3))) f32x4*)to = f32x4{out(b, e), out(b, e + 1), out(b, e + 2), out(b, e + 3)};
+      for (int b = 0; b < NB; b++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) acc[a][b][e] = 0.f;
+    if (here.c1 > here.c0) {      // its first chunk has landed for every wave
+      u32x4 av[2][MB], bv[2][NB];
+#pragma unroll
+      for (int x = 0; x < MB; x++) av[0][x] = read_a(x, 0, sc);
+#pragma unroll
+      for (int x = 0; x < NB; x++) bv[0][x] = read_b(x, 0, sc);
+      for (int c = here.c0; c < here.c1; c++) {
+        const int sn = sc + 1 == R ? 0 : sc + 1;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int g = 0; g < 2 * MB; g++) {
+          const int a = g % MB, st = g / MB;
+          if (g == MB) {     // chunk c + 1 has landed for every wave, chunk c is read out by every wave
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((R - 2) * PW) : "memory");
+            __builtin_amdgcn_s_barrier();
+            advance();
+          }
+          const int stage = st == 0 ? sc : sn, kb = 1 - st;
+          // the operands of the next 16 k, in the order of their use
+#pragma unroll
+          for (int q = 0; q < MB + NB; q++)
+            if (q * MB / (MB + NB) == a) {
+              const int x = q == 0 ? 0 : q <= NB ? MB + q - 1 : q - NB;
+              if (x < MB) av[1 - st][x] = read_a(x, kb, stage);
+              else bv[1 - st][x - MB] = read_b(x - MB, kb, stage);
+            }
+          // this step's share of the loads: the rest of chunk c + R - 1, then the first F pieces of chunk c + R
+#pragma unroll
+          for (int j = 0; j < PW; j++) {
+            if (st == 0 && j >= F && (j - F) * MB / (PW - F) == a) load(j, sl);
+            if (st == 1 && j < F && j * MB / F == a) load(j, sc);
+          }
+#pragma unroll
+          for (int b = 0; b < NB; b++) mfma(av[st][a], bv[st][b], acc[a][b]);
+          __builtin_amdgcn_sched_barrier(0);
         }
+        sl = sc;
+        sc = sn;
+      }
+    }
+    // results of the last instructions may be read by the assembly below; the rows' data is older than the loads still under way, if
+    // those are all of this tile
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+    if ((EPI == EPI_STRIP || EPI == EPI_DZ) && here.c1 - here.c0 < R) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+
+    int ln = lane;
+    asm volatile("" : "+v"(ln));      // or what follows from the lane alone is kept in registers through the products
+    // one element of a result: read as a whole, the 16 registers of an accumulator would be copied and spill
+    auto val = [&](int a, int b, int e) {
+      if (MB * NB <= 8) return acc[a][b][e];
+      float x;
+      asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[a][b][e]));
+      return x;
+    };
+    auto row_data = [&](int a, int which) {
+      return *(__attribute__((address_space(3))) unsigned*)(lds + RING + (wave * ARRAYS + which) * (ROWS * 256) + (a * 32 + (ln & 31)) * 4);
+    };
+    if constexpr (EPI == EPI_SLICE) {
+      // rows up to the padding are written, kept or not; a piece behind the first adds to what is there
+      float* const out = P.slice + z * P.slice_stride + (int64_t)i0 * P.ldo + j0;      // offsets inside a tile fit 32 bits
+      const unsigned ld = (unsigned)P.ldo;
+#pragma unroll
+      for (int a = 0; a < MB; a++) {
+#pragma unroll
+        for (int b = 0; b < NB; b++) {
+          const int j = wn * 32 * NB + b * 32 + (ln & 31), r = (wm * MB + a) * 32 + 4 * (ln >> 5);
+          if (j0 + j < P.out_cols) {
+            float* const p = out + ((unsigned)r * ld + j);
+            float old[16];
+#pragma unroll
+            for (int e = 0; e < 16; e++) old[e] = 0.f;
+            if (!P.first) {
+#pragma unroll
+              for (int e = 0; e < 16; e++) old[e] = p[(unsigned)(8 * (e >> 2) + (e & 3)) * ld];
+            }
+#pragma unroll
+            for (int e = 0; e < 16; e++) __builtin_nontemporal_store(old[e] + val(a, b, e), p + (unsigned)(8 * (e >> 2) + (e & 3)) * ld);
+          }
+          __builtin_amdgcn_sched_barrier(0);      // one block's addresses at a time
+        }
+      }
+      continue;
+    }
+    const int jw = wn * 32 * NB + 4 * (ln >> 5);      // column of register e of block b: jw + 32 b + 8 (e / 4) + e % 4
+    const bool crosses = (EPI == EPI_STRIP || EPI == EPI_DZ) && P.v0 + j0 + BN > P.vocab;
+    if constexpr (EPI == EPI_STRIP) {
+      __attribute__((address_space(3))) f32x2* const half = (__attribute__((address_space(3))) f32x2*)(lds + RING + ROW_DATA);
+#pragma unroll
+      for (int a = 0; a < MB; a++) {
+        const int il = (wm * MB + a) * 32 + (ln & 31), i = i0 + il, y = (int)row_data(a, 0) - j0;      // padding: negative
+        float top = -INFINITY, sum = 0.f;
+        auto strip = [&](auto some) {      // some: a target or the vocabulary's end is in the tile
+          float x[NB][16];
+          auto at = [&](int b, int e) {
+            const int j = jw + 32 * b + 8 * (e >> 2) + (e & 3);
+            const float v = val(a, b, e);
+            return decltype(some)::value && j0 + j >= P.vocab ? -INFINITY : v;
+          };
+#pragma unroll
+          for (int b = 0; b < NB; b++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) {
+              const float v = x[b][e] = at(b, e);
+              if (decltype(some)::value && jw + 32 * b + 8 * (e >> 2) + (e & 3) == y) P.zt[i] = v * P.inv_t;
+              top = fmaxf(top, v);
+            }
+          top = fmaxf(top, __shfl_xor(top, 32, 64));
+          const float ref = top == -INFINITY ? 0.f : top * P.scale;
+#pragma unroll
+          for (int b = 0; b < NB; b++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) sum += __builtin_amdgcn_exp2f(fmaf(x[b][e], P.scale, -ref));
+          sum += __shfl_xor(sum, 32, 64);
+        };
+        if (crosses || __any(y >= 0 && y < BN)) strip(std::true_type());
+        else strip(std::false_type());
+        if (ln < 32) half[wn * BM + il] = f32x2{top, sum};
+        __builtin_amdgcn_sched_barrier(0);      // one row block at a time
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      constexpr int LANES = SC / V;      // of a row
-      const int c = wn * 32 * NB + n * SC + ln % LANES * V, r0 = (wm * MB + a) * 32;
-#pragma unroll
-      for (int r = ln / LANES; r < 32; r += 64 / LANES) {
-        const u32x4 v = *(__attribute__((address_space(3))) u32x4*)(mine + r * PITCH + ln % LANES * 16);
-        if (j0 + c < P.out_cols && i0 + r0 + r < P.out_rows)
-          __builtin_nontemporal_store(v, (u32x4*)(P.out + (int64_t)(i0 + r0 + r) * P.ldo + j0 + c));
+      __builtin_amdgcn_s_barrier();
+      if (tid < BM && i0 + tid < kept) {
+        const f32x2 a = half[tid], b = half[BM + tid];
+        const float top = fmaxf(a[0], b[0]), ref = top == -INFINITY ? 0.f : top;
+        P.part[(size_t)(j0 / BN) * P.padded + i0 + tid] =
+            make_float2(top * P.inv_t, a[1] * exp2f((a[0] - ref) * P.scale) + b[1] * exp2f((b[0] - ref) * P.scale));
       }
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
+      continue;
     }
-  };
+    // 32 rows x SC columns at a time through LDS of the wave's own, rows 16 bytes apart, so that a row is stored in pieces of SC
+    lds_char* const mine = lds + RING + ROW_DATA + wave * (32 * PITCH);
+    auto store = [&](int a, auto out) {      // out(b, e): element e of block b
 #pragma unroll
-  for (int a = 0; a < MB; a++) {
-    if constexpr (EPI == EPI_DZ) {
-      const int y = (int)row_data(a, 0) - P.v0 - j0;
-      const float g = __builtin_bit_cast(float, row_data(a, 1)), l = __builtin_bit_cast(float, row_data(a, 2)) * 1.44269504f;
-      auto dz = [&](int b, int e) { return -g * __builtin_amdgcn_exp2f(fmaf(val(a, b, e), P.scale, -l)); };
-      if (crosses || __any(y >= 0 && y < BN)) {
-        store(a, [&](int b, int e) {
-          const int j = jw + 32 * b + 8 * (e >> 2) + (e & 3);
-          return P.v0 + j0 + j >= P.vocab ? 0.f : j == y ? dz(b, e) + g : dz(b, e);
-        });
+      for (int n = 0; n < 32 * NB / SC; n++) {
+#pragma unroll
+        for (int u = 0; u < SC / 8; u++) {
+          const int b = (n * SC + 8 * u) / 32, e = (n * SC + 8 * u) % 32 / 2;
+          lds_char* const to = mine + (ln & 31) * PITCH + (8 * u + 4 * (ln >> 5)) * EL;
+          if constexpr (EL == 2) {
+            typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
+            *(__attribute__((address_space(3))) bf16x4*)to = bf16x4{(__bf16)out(b, e), (__bf16)out(b, e + 1), (__bf16)out(b, e + 2), (__bf16)out(b, e + 3)};
+          } else {
+            *(__attribute__((address_space(3))) f32x4*)to = f32x4{out(b, e), out(b, e + 1), out(b, e + 2), out(b, e + 3)};
+          }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        constexpr int LANES = SC / V;      // of a row
+        const int c = wn * 32 * NB + n * SC + ln % LANES * V, r0 = (wm * MB + a) * 32;
+#pragma unroll
+        for (int r = ln / LANES; r < 32; r += 64 / LANES) {
+          const u32x4 v = *(__attribute__((address_space(3))) u32x4*)(mine + r * PITCH + ln % LANES * 16);
+          if (j0 + c < P.out_cols && i0 + r0 + r < P.out_rows)
+            __builtin_nontemporal_store(v, (u32x4*)(P.out + (int64_t)(i0 + r0 + r) * P.ldo + j0 + c));
+        }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+#pragma unroll
+    for (int a = 0; a < MB; a++) {
+      if constexpr (EPI == EPI_DZ) {
+        const int y = (int)row_data(a, 0) - P.v0 - j0;
+        const float g = __builtin_bit_cast(float, row_data(a, 1)), l = __builtin_bit_cast(float, row_data(a, 2)) * 1.44269504f;
+        auto dz = [&](int b, int e) { return -g * __builtin_amdgcn_exp2f(fmaf(val(a, b, e), P.scale, -l)); };
+        if (crosses || __any(y >= 0 && y < BN)) {
+          store(a, [&](int b, int e) {
+            const int j = jw + 32 * b + 8 * (e >> 2) + (e & 3);
+            return P.v0 + j0 + j >= P.vocab ? 0.f : j == y ? dz(b, e) + g : dz(b, e);
+          });
+        } else {
+          store(a, dz);
+        }
       } else {
-        store(a, dz);
+        store(a, [&](int b, int e) { return val(a, b, e); });
       }
-    } else {
-      store(a, [&](int b, int e) { return val(a, b, e); });
     }
-  }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // loads into this LDS
 }
@@ -452,8 +459,8 @@ bool token_logprob_takes_mfma(int64_t padded, int ld, int hidden, int width, con
 
 template <typename T>
 void token_logprob_slice_tile(int rows, int hidden, SliceRule& r) {
-  // us of a tile's 32 k, measured; fp32: two workgroups a CU share its matrix units.  64 x 64 tiles where 64 slices of 128 x 128 tiles are
-  // too few.
+  // us of a tile's 32 k, fitted; fp32: two workgroups a CU share its matrix units.  2744 rows x 75968 x 2560: two slices, 0.94 ms a piece; nine,
+  // which a time of 0.85 would choose: 1.18.  The tile is the one of 16 slices.
   const Tile t = tile_of<T>(rows, hidden, 16, true);
   r.rows = 64 * t.mb;
   r.tiles_j = (hidden + 64 * t.nb - 1) / (64 * t.nb);
