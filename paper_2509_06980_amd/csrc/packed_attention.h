@@ -41,6 +41,30 @@ __device__ __forceinline__ PackedTile packed_tile(const int32_t* cu, int n_seq, 
   t.row0 = row0 < 0 ? t.len : row0 <= t.len / rows ? row0 * rows : t.len;
   return t;
 }
+// Tile `n` of up to 64 sequences, a lane each, those with most tiles of their sequence behind them first.
+__device__ __forceinline__ PackedTile packed_tile_by_rest(const int32_t* cu, int n_seq, int total, int rows, int n) {
+  const int lane = threadIdx.x & 63;
+  const int first = lane < n_seq ? packed_bound(cu, lane, total) : 0, end = lane < n_seq ? packed_bound(cu, lane + 1, total) : 0;
+  const int len = end > first ? end - first : 0, tiles = (len + rows - 1) / rows;
+  int rest = tiles;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) rest = max(rest, __shfl_xor(rest, o, 64));
+  PackedTile t{0, 0, 0, 0};
+  for (rest = __builtin_amdgcn_readfirstlane(rest) - 1; rest >= 0; rest--) {
+    const uint64_t on = __ballot(tiles > rest);
+    const int count = __popcll(on);
+    if (n < count) {
+      const int s = __builtin_ctzll(__ballot((on >> lane & 1) && __popcll(on & ((1ull << lane) - 1)) == n));
+      t.seq = s;
+      t.first = __builtin_amdgcn_readlane(first, s);
+      t.len = __builtin_amdgcn_readlane(len, s);
+      t.row0 = (__builtin_amdgcn_readlane(tiles, s) - 1 - rest) * rows;
+      break;
+    }
+    n -= count;
+  }
+  return t;
+}
 
 // bf16 on matrix instructions: head sizes in multiples of 8, 16-byte aligned rows, nothing beyond 2 GB in one tensor.  o and dout are
 // checked for their alignment alone (null: not in the call).

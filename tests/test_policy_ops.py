@@ -297,6 +297,23 @@ def test_attention_where_whole_tiles_fill_the_chip(dt, lq, lk, nq, nk, d):
 
 
 @pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("n", [2, 63, 64, 65, 130])
+def test_attention_of_many_sequences(dt, n):
+    lq = [(7 * i * i + 3 * i) % 41 * (i % 5 != 2) + 150 * (i % 29 == 11) for i in range(n)]
+    lk = [a + 37 * (i % 3 == 1) - (a > 20 and i % 7 == 3) * 15 for i, a in enumerate(lq)]
+    nq, nk, d = 2, 1, 64
+    g = gen(n)
+    q, do = randn(g, sum(lq), nq, d, dt=dt), randn(g, sum(lq), nq, d, dt=dt)
+    k, v = randn(g, sum(lk), nk, d, dt=dt), randn(g, sum(lk), nk, d, dt=dt)
+    cq, ck = offsets(lq), offsets(lk)
+    o, lse = ops.attention_forward(q, k, v, cq, ck)
+    dq, dk, dv = ops.attention_backward(do, q, k, v, o, lse, cq, ck)
+    want, err = attention_reference(q, k, v, do, lq, lk, True, d ** -0.5, dt, True)
+    for name, got in (("o", o), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        within(name, got, want[name], err[name])
+
+
+@pytest.mark.parametrize("dt", [BF, FP])
 @pytest.mark.parametrize("causal,d", [(True, 128), (False, 64)])
 def test_attention_with_a_negative_scale(dt, causal, d):
     lens, nq, nk = [150, 3, 260], 4, 2
