@@ -13,21 +13,26 @@ namespace {
 // Rows without target (observation tokens) or, backward, with g = 0 take no part: the others are gathered first.
 // =============================================================================================
 
-// Kept rows in order (one workgroup: a scan of the targets).  place[t]: where row t went, -1: nowhere, -2: its target lies
-// behind the vocabulary, which shows as NaN.  Forward (g null): logp and lse of the others are written here.
-__global__ __launch_bounds__(1024) void keep_rows_kernel(const int32_t* __restrict__ targets, int rows, int vocab, const float* __restrict__ g,
-                                                         const float* __restrict__ lse_in, float inv_t, int32_t* __restrict__ count,
-                                                         int32_t* __restrict__ list, int32_t* __restrict__ place,
-                                                         int32_t* __restrict__ target, float* __restrict__ lse_kept,
-                                                         float* __restrict__ g_kept, float* __restrict__ logp, float* __restrict__ lse,
-                                                         SliceRule rule) {
+// Kept rows in order: a scan of the targets by 1024 threads.  place[t]: where row t went, -1: nowhere, -2: its target lies behind the
+// vocabulary, which shows as NaN.  Forward (g null): logp and lse of the others are written here.
+struct RowScan {
+  const int32_t* targets;
+  int rows, vocab;
+  const float *g, *lse_in;
+  float inv_t;
+  int32_t *count, *list, *place, *target;
+  float *lse_kept, *g_kept, *logp, *lse;
+  SliceRule rule;
+};
+// Returns how many rows are kept; found: the row that went to place `wanted`, for one thread at most.
+__device__ __forceinline__ int scan_rows(const RowScan& s, bool write, int wanted, int* found) {
   __shared__ int waves[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int done = 0;
-  for (int t0 = 0; t0 < rows; t0 += 1024) {
-    const int t = t0 + threadIdx.x, y = t < rows ? targets[t] : -1;
-    const float gt = g && t < rows ? g[t] : 1.f;
-    const bool keep = y >= 0 && y < vocab && gt != 0.f;
+  for (int t0 = 0; t0 < s.rows; t0 += 1024) {
+    const int t = t0 + threadIdx.x, y = t < s.rows ? s.targets[t] : -1;
+    const float gt = s.g && t < s.rows ? s.g[t] : 1.f;
+    const bool keep = y >= 0 && y < s.vocab && gt != 0.f;
     const uint64_t mask = __ballot(keep);
     if (lane == 0) waves[wave] = __popcll(mask);
     __syncthreads();
@@ -39,57 +44,73 @@ __global__ __launch_bounds__(1024) void keep_rows_kernel(const int32_t* __restri
     }
     done += all;
     const int at = before + __popcll(mask & ((1ull << lane) - 1));
-    if (keep) {
-      list[at] = t;
-      target[at] = y;
-      if (g) {
-        lse_kept[at] = lse_in[t];
-        g_kept[at] = gt * inv_t;
+    if (keep && at == wanted) *found = t;
+    if (keep && write) {
+      s.list[at] = t;
+      s.target[at] = y;
+      if (s.g) {
+        s.lse_kept[at] = s.lse_in[t];
+        s.g_kept[at] = gt * s.inv_t;
       }
     }
-    if (t < rows) {
-      const float none = y >= vocab ? __builtin_nanf("") : 0.f;
-      if (g) {
-        place[t] = keep ? at : y >= vocab ? -2 : -1;
+    if (t < s.rows && write) {
+      const float none = y >= s.vocab ? __builtin_nanf("") : 0.f;
+      if (s.g) {
+        s.place[t] = keep ? at : y >= s.vocab ? -2 : -1;
       } else if (!keep) {
-        logp[t] = none;
-        lse[t] = none;
+        s.logp[t] = none;
+        s.lse[t] = none;
       }
     }
     __syncthreads();
   }
+  if (!write) return done;
   for (int i = done + threadIdx.x; i < (int)((done + kRowPad - 1) / kRowPad * kRowPad); i += 1024) {
-    target[i] = -1;
-    if (g) lse_kept[i] = 0.f, g_kept[i] = 0.f;
+    s.target[i] = -1;
+    if (s.g) s.lse_kept[i] = 0.f, s.g_kept[i] = 0.f;
   }
   if (threadIdx.x == 0) {
-    count[0] = done;
-    if (g) {
-      const int n = choose_slices(rule, done);
-      count[1] = n;
-      count[2] = ((rule.width + n - 1) / n + 63) / 64 * 64;
+    s.count[0] = done;
+    if (s.g) {
+      const int n = choose_slices(s.rule, done);
+      s.count[1] = n;
+      s.count[2] = ((s.rule.width + n - 1) / n + 63) / 64 * 64;
     }
   }
+  return done;
 }
+__global__ __launch_bounds__(1024) void keep_rows_kernel(RowScan s) { scan_rows(s, true, -1, nullptr); }
 
-// Kept rows of h one after the other, zeros behind column `hidden` and behind the last row up to the padding.
+// A kept row (null: zeros), zeros behind column `hidden`
+template <typename T, int VEC>
+__device__ __forceinline__ void copy_row(const T* src, int hidden, int ld, T* out) {
+  for (int c = threadIdx.x * VEC; c < ld; c += blockDim.x * VEC) {
+    float v[VEC];
+    if (src && c < hidden) {
+      ldv<VEC>(src + c, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; e++) v[e] = 0.f;
+    }
+    stv<VEC>(out + c, v);
+  }
+}
+// Kept rows of h one after the other, zeros behind the last one up to the padding.
 template <typename T, int VEC>
 __global__ __launch_bounds__(256) void gather_rows_kernel(const T* __restrict__ h, int64_t stride, int hidden, int ld,
                                                           const int32_t* __restrict__ list, const int32_t* __restrict__ count,
                                                           T* __restrict__ out) {
   const int r = blockIdx.x, n = *count;
   if (r >= (n + kRowPad - 1) / kRowPad * kRowPad) return;
-  const T* src = h + (r < n ? list[r] : 0) * stride;
-  for (int c = threadIdx.x * VEC; c < ld; c += 256 * VEC) {
-    float v[VEC];
-    if (r < n && c < hidden) {
-      ldv<VEC>(src + c, v);
-    } else {
-#pragma unroll
-      for (int e = 0; e < VEC; e++) v[e] = 0.f;
-    }
-    stv<VEC>(out + (size_t)r * ld + c, v);
-  }
+  copy_row<T, VEC>(r < n ? h + list[r] * stride : nullptr, hidden, ld, out + (size_t)r * ld);
+}
+// Both in one launch: every workgroup scans all rows for its own.
+template <typename T, int VEC>
+__global__ __launch_bounds__(1024) void keep_and_gather_kernel(RowScan s, const T* __restrict__ h, int64_t stride, int hidden, int ld, T* __restrict__ out) {
+  __shared__ int mine;
+  const int r = blockIdx.x, n = scan_rows(s, r == 0, r, &mine);
+  if (r >= (n + kRowPad - 1) / kRowPad * kRowPad) return;
+  copy_row<T, VEC>(r < n ? h + mine * stride : nullptr, hidden, ld, out + (size_t)r * ld);
 }
 
 // ---- products in 32 bits for every type and size ----------------------------------------------
@@ -400,14 +421,23 @@ const char* logprob_argument(int64_t rows, int32_t hidden, int32_t vocab, float 
   return nullptr;
 }
 
+// Kept rows and their data, up to 512 rows in one launch (256 x 4096 in fp32, both directions: 30 rows 53 us, in two launches 57; 288 rows 62
+// and 65; 1024 rows 102 and 101).
+template <typename T, int VEC>
+void keep(const RowScan& scan, const void* h, int64_t stride, int hidden, const Workspace& w, char* ws, hipStream_t s) {
+  T* rows = (T*)(ws + w.rows);
+  if (scan.rows <= 512) {
+    keep_and_gather_kernel<T, VEC><<<(unsigned)w.padded, 1024, 0, s>>>(scan, (const T*)h, stride, hidden, w.ld, rows);
+  } else {
+    keep_rows_kernel<<<1, 1024, 0, s>>>(scan);
+    gather_rows_kernel<T, VEC><<<(unsigned)w.padded, 256, 0, s>>>((const T*)h, stride, hidden, w.ld, scan.list, scan.count, rows);
+  }
+}
 template <typename T>
-void gather(const void* h, int64_t stride, int hidden, const Workspace& w, char* ws, hipStream_t s) {
+void keep(const RowScan& scan, const void* h, int64_t stride, int hidden, const Workspace& w, char* ws, hipStream_t s) {
   constexpr int VEC = 16 / sizeof(T);
-  const int32_t *list = (int32_t*)(ws + w.list), *count = (int32_t*)(ws + w.count);
-  if (hidden % VEC == 0 && stride % VEC == 0 && aligned16(h))
-    gather_rows_kernel<T, VEC><<<(unsigned)w.padded, 256, 0, s>>>((const T*)h, stride, hidden, w.ld, list, count, (T*)(ws + w.rows));
-  else
-    gather_rows_kernel<T, 1><<<(unsigned)w.padded, 256, 0, s>>>((const T*)h, stride, hidden, w.ld, list, count, (T*)(ws + w.rows));
+  if (hidden % VEC == 0 && stride % VEC == 0 && aligned16(h)) keep<T, VEC>(scan, h, stride, hidden, w, ws, s);
+  else keep<T, 1>(scan, h, stride, hidden, w, ws, s);
 }
 
 template <typename T>
@@ -415,9 +445,9 @@ int forward(const void* h, int64_t stride, int rows, int hidden, const void* wei
             float* logp, float* lse, char* ws, hipStream_t s) {
   const Workspace w = plan(rows, hidden, vocab, sizeof(T) == 2 ? RL_DTYPE_BF16 : RL_DTYPE_F32, false);
   const KeptRows kept{(int32_t*)(ws + w.count), (int32_t*)(ws + w.target), nullptr, nullptr};
-  keep_rows_kernel<<<1, 1024, 0, s>>>(targets, rows, vocab, nullptr, nullptr, inv_t, (int32_t*)(ws + w.count), (int32_t*)(ws + w.list),
-                                      nullptr, (int32_t*)(ws + w.target), nullptr, nullptr, logp, lse, SliceRule{});
-  gather<T>(h, stride, hidden, w, ws, s);
+  keep<T>(RowScan{targets, rows, vocab, nullptr, nullptr, inv_t, (int32_t*)(ws + w.count), (int32_t*)(ws + w.list), nullptr,
+                  (int32_t*)(ws + w.target), nullptr, nullptr, logp, lse, SliceRule{}},
+          h, stride, hidden, w, ws, s);
   int strips = (vocab + 127) / 128;
   const bool mfma = token_logprob_takes_mfma<T>(w.padded, w.ld, hidden, 0, weight, nullptr);
   if (mfma)
@@ -438,10 +468,9 @@ int backward(const float* g, const void* h, int64_t stride, int rows, int hidden
              const float* lse, float inv_t, void* dh, void* dw, char* ws, hipStream_t s) {
   const Workspace w = plan(rows, hidden, vocab, sizeof(T) == 2 ? RL_DTYPE_BF16 : RL_DTYPE_F32, true);
   const KeptRows kept{(int32_t*)(ws + w.count), (int32_t*)(ws + w.target), (float*)(ws + w.lse), (float*)(ws + w.g)};
-  keep_rows_kernel<<<1, 1024, 0, s>>>(targets, rows, vocab, g, lse, inv_t, (int32_t*)(ws + w.count), (int32_t*)(ws + w.list),
-                                      (int32_t*)(ws + w.place), (int32_t*)(ws + w.target), (float*)(ws + w.lse), (float*)(ws + w.g), nullptr,
-                                      nullptr, w.slices);
-  gather<T>(h, stride, hidden, w, ws, s);
+  keep<T>(RowScan{targets, rows, vocab, g, lse, inv_t, (int32_t*)(ws + w.count), (int32_t*)(ws + w.list), (int32_t*)(ws + w.place),
+                  (int32_t*)(ws + w.target), (float*)(ws + w.lse), (float*)(ws + w.g), nullptr, nullptr, w.slices},
+          h, stride, hidden, w, ws, s);
   const int vec = hidden % (16 / sizeof(T)) == 0 && aligned16(weight);
   const T *hr = (const T*)(ws + w.rows), *wt = (const T*)weight;
   T* dz = (T*)(ws + w.dz);
