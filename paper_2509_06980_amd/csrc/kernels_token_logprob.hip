@@ -402,8 +402,8 @@ Workspace plan(int64_t rows, int hidden, int vocab, int dtype, bool backward) {
   const int64_t pieces = (vocab + fit - 1) / fit;
   w.width = (int)up((vocab + pieces - 1) / pieces, 256);
   // slices of the vocabulary in dz W: up to 64, 512 MB of sums
-  if (el == 2) token_logprob_slice_tile<bf16_t>((int)rows, hidden, w.slices);
-  else token_logprob_slice_tile<float>((int)rows, hidden, w.slices);
+  if (el == 2) token_logprob_slice_tile<bf16_t>((int)rows, hidden, w.width, w.slices);
+  else token_logprob_slice_tile<float>((int)rows, hidden, w.width, w.slices);
   w.slices.width = w.width;
   w.slices.most = (int)std::max<int64_t>(std::min({(int64_t)64, kPieceBytes / 2 / (w.padded * hidden * 4), (int64_t)w.width / 256}), 1);
   w.slices.slice_us = (float)(hidden * 8 / 4.8e6);

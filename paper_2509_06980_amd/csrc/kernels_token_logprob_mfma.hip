@@ -422,21 +422,31 @@ void go(const Product<T>& p, hipStream_t s) {
   kernel<<<(unsigned)std::min<int64_t>((int64_t)p.tiles_i * p.tiles_j * p.slices, MB * NB > 4 ? 256 : 512), 256, lds, s>>>(p);
 }
 
-// Tile of a product, in 64 rows and 64 columns.  bf16: 256 x 256, for up to 128 rows 128 x 256 (1024 x 151936, forward: 100 rows 109 us,
-// with 256 x 256 124; 200 rows 141 and 131).  fp32 (16 times the matrix time a byte): 128 x 128, and 64 x 64 where those would be fewer than two
+// Tile of a product, in 64 rows and 64 columns.  bf16: 256 x 256; 128 x 128 where those would leave a quarter of the CUs idle (1024 x 4096, both
+// directions: 100 rows 62 us, with the others 86; 288 rows 65 and 129; forward, 500 rows x 2560 x 20000 70 and 73, 500 x 1024 x 30000 50 and 48); 128 x 256 for up to 128 rows
+// otherwise (1024 x 151936, forward: 100 rows 109 us, with 256 x 256 124; 200 rows 141 and 131).  fp32 (16 times the matrix time a byte): 128 x 128, and 64 x 64 where those would be fewer than two
 // for each of the 512 workgroups that the card holds (both directions: 1000 rows x 256 x 4096 99 us, with 128 x 128 142; 1000 x 1024
 // x 8192 434 and 468; 1500 x 1024 x 16384 1155 and 1027).
 struct Tile { int mb, nb; };
 template <typename T>
 Tile tile_of(int64_t rows, int64_t columns, int64_t slices, bool gathered) {
-  if (sizeof(T) == 2) return {gathered && rows <= 128 ? 2 : 4, 4};
+  if (sizeof(T) == 2) {
+    if ((rows + 255) / 256 * ((columns + 255) / 256) * slices < 192) return {2, 2};
+    return {gathered && rows <= 128 ? 2 : 4, 4};
+  }
   const bool small = (rows + 127) / 128 * ((columns + 127) / 128) * slices < 1024;
   return {small ? 1 : 2, small ? 1 : 2};
+}
+// Slices of a piece of the vocabulary that dz W may count on when it chooses a tile
+template <typename T>
+int64_t slices_in(int width) {
+  return sizeof(T) == 2 ? std::min(std::max(width / 2048, 1), 64) : 16;
 }
 template <typename T, bool TA, bool TB, int EPI>
 void go(Product<T>& p, const Tile& t, int64_t rows, int64_t columns, hipStream_t s) {
   p.tiles_i = (int)((rows + 64 * t.mb - 1) / (64 * t.mb)), p.tiles_j = (int)((columns + 64 * t.nb - 1) / (64 * t.nb));
   if constexpr (sizeof(T) == 2) {
+    if (t.nb == 2) return go<T, TA, TB, 2, 2, 6, EPI>(p, s);
     if constexpr (!TA) {
       if (t.mb == 2) return go<T, TA, TB, 2, 4, 5, EPI>(p, s);
     }
@@ -458,13 +468,13 @@ bool token_logprob_takes_mfma(int64_t padded, int ld, int hidden, int width, con
 }
 
 template <typename T>
-void token_logprob_slice_tile(int rows, int hidden, SliceRule& r) {
+void token_logprob_slice_tile(int rows, int hidden, int width, SliceRule& r) {
   // us of a tile's 32 k, fitted; fp32: two workgroups a CU share its matrix units.  2744 rows x 75968 x 2560: two slices, 0.94 ms a piece; nine,
-  // which a time of 0.85 would choose: 1.18.  The tile is the one of 16 slices.
-  const Tile t = tile_of<T>(rows, hidden, 16, true);
+  // which a time of 0.85 would choose: 1.18.
+  const Tile t = tile_of<T>(rows, hidden, slices_in<T>(width), true);
   r.rows = 64 * t.mb;
   r.tiles_j = (hidden + 64 * t.nb - 1) / (64 * t.nb);
-  r.chunk_us = sizeof(T) == 2 ? (t.mb == 4 ? 0.6f : 0.35f) : t.mb == 2 ? 2.4f : 0.6f;
+  r.chunk_us = sizeof(T) == 2 ? (t.mb == 4 ? 0.6f : t.nb == 4 ? 0.35f : 0.2f) : t.mb == 2 ? 2.4f : 0.6f;
 }
 
 template <typename T>
@@ -502,7 +512,7 @@ void launch_hidden_gradient_mfma(hipStream_t s, const T* dz, const VocabPiece& p
   p.b = w + (int64_t)piece.v0 * hidden, p.ldb = hidden, p.b_n = std::min(piece.ld, vocab - piece.v0);
   p.k = piece.width, p.slices = most_slices, p.group = 4;
   p.kept = kept, p.slice = dh, p.slice_stride = slice_stride, p.ldo = hidden, p.out_cols = hidden, p.first = first;
-  go<T, false, true, EPI_SLICE>(p, tile_of<T>(rows, hidden, 16, true), rows, hidden, s);
+  go<T, false, true, EPI_SLICE>(p, tile_of<T>(rows, hidden, slices_in<T>(piece.ld - 128), true), rows, hidden, s);
 }
 
 template <typename T>
@@ -518,7 +528,7 @@ void launch_weight_gradient_mfma(hipStream_t s, const T* dz, const VocabPiece& p
 
 #define RL_OF(T)                                                                                                                              \
   template bool token_logprob_takes_mfma<T>(int64_t, int, int, int, const void*, const void*);                                                \
-  template void token_logprob_slice_tile<T>(int, int, SliceRule&);                                                                            \
+  template void token_logprob_slice_tile<T>(int, int, int, SliceRule&);                                                                         \
   template int launch_logits_strips_mfma<T>(hipStream_t, const T*, int, int, int64_t, const T*, int, int, const KeptRows&, float, float2*,    \
                                             float*);                                                                                          \
   template void launch_logits_gradient_mfma<T>(hipStream_t, const T*, int, int, int64_t, const T*, int, int, const KeptRows&, float,          \

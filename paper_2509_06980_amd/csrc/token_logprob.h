@@ -46,7 +46,7 @@ void launch_logits_gradient_mfma(hipStream_t s, const T* h, int ld, int rows, in
                                  const KeptRows& kept, float inv_t, const VocabPiece& piece, T* dz);
 // Tile of dz W and its time
 template <typename T>
-void token_logprob_slice_tile(int rows, int hidden, SliceRule& r);
+void token_logprob_slice_tile(int rows, int hidden, int width, SliceRule& r);
 template <typename T>
 void launch_hidden_gradient_mfma(hipStream_t s, const T* dz, const VocabPiece& piece, int rows, int64_t padded, const T* w, int vocab, int hidden,
                                  const KeptRows& kept, int most_slices, float* dh, size_t slice_stride, bool first);

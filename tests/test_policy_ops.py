@@ -443,6 +443,16 @@ def test_token_logprobs(rows, hidden, vocab, sampled, dt):
 @pytest.mark.parametrize("dt,rows,hidden,vocab", [(BF, 300, 64, 160_000), (BF, 90, 8, 150_001), (FP, 300, 64, 20_001), (FP, 700, 8, 40_003),
                                                   (FP, 40, 4, 70_000)])
 def test_token_logprobs_of_many_tiles_a_workgroup(dt, rows, hidden, vocab):
+    _check_token_logprobs(dt, rows, hidden, vocab)
+
+
+# many slices of the vocabulary in the gradient of the hidden rows, whole tiles and those of few rows; tiles of 128 in every product
+@pytest.mark.parametrize("rows,hidden,vocab", [(700, 72, 140_000), (90, 776, 135_000), (260, 264, 30_011)])
+def test_token_logprobs_of_large_vocabularies(rows, hidden, vocab):
+    _check_token_logprobs(BF, rows, hidden, vocab)
+
+
+def _check_token_logprobs(dt, rows, hidden, vocab):
     g = gen(rows + vocab)
     w, h = randn(g, vocab, hidden, dt=dt, std=2 / math.sqrt(hidden)), randn(g, rows, hidden, dt=dt)
     y = torch.randint(0, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
