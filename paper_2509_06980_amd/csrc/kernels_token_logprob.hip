@@ -239,26 +239,33 @@ __global__ __launch_bounds__(256) void logits_strip_kernel(const T* __restrict__
   }
 }
 
-// 64 kept rows: their strips joined by 16 threads each, in a fixed order
+// 16 kept rows: their strips joined by 64 threads each, in a fixed order (4096 rows x 594 strips: 10 us, 64 rows by 16 threads each 23)
 __global__ __launch_bounds__(1024) void join_strips_kernel(const float2* __restrict__ part, int strips, int padded, const float* __restrict__ zt,
                                                            const int32_t* __restrict__ list, const int32_t* __restrict__ count,
                                                            float* __restrict__ logp, float* __restrict__ lse) {
-  __shared__ float2 share[16][64];
-  const int n = *count, r = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6;
-  if (blockIdx.x * 64 >= n) return;
+  __shared__ float2 share[16][16];
+  const int n = *count, r = blockIdx.x * 16 + (threadIdx.x & 15), k = threadIdx.x >> 4;
+  if (blockIdx.x * 16 >= n) return;
   float top = -INFINITY, sum = 0.f;
   auto join = [&](float2 p) {
     const float t = fmaxf(top, p.x), ref = t == -INFINITY ? 0.f : t;
     sum = sum * expf(top - ref) + p.y * expf(p.x - ref);
     top = t;
   };
-  if (r < n)
-    for (int i = k; i < strips; i += 16) join(part[(size_t)i * padded + r]);
-  share[k][threadIdx.x & 63] = make_float2(top, sum);
+  if (r < n) {
+#pragma unroll 4
+    for (int i = k; i < strips; i += 64) join(part[(size_t)i * padded + r]);
+  }
+#pragma unroll
+  for (int o = 16; o < 64; o *= 2) {
+    const float2 other = make_float2(__shfl_xor(top, o, 64), __shfl_xor(sum, o, 64));
+    join(other);
+  }
+  if ((threadIdx.x & 63) < 16) share[threadIdx.x >> 6][threadIdx.x & 15] = make_float2(top, sum);
   __syncthreads();
   if (k == 0 && r < n) {
 #pragma unroll
-    for (int i = 1; i < 16; i++) join(share[i][threadIdx.x & 63]);
+    for (int i = 1; i < 16; i++) join(share[i][threadIdx.x]);
     const float l = top + logf(sum);
     logp[list[r]] = zt[r] - l;
     lse[list[r]] = l;
@@ -458,7 +465,7 @@ int forward(const void* h, int64_t stride, int rows, int hidden, const void* wei
     logits_strip_kernel<T><<<dim3((rows + 127) / 128, strips), 256, 0, s>>>((const T*)(ws + w.rows), w.ld, (const T*)weight, hidden, vocab, hidden,
                                                                            vec, kept, inv_t, (float2*)(ws + w.part), (int)w.padded,
                                                                            (float*)(ws + w.zt));
-  join_strips_kernel<<<(rows + 63) / 64, 1024, 0, s>>>((const float2*)(ws + w.part), strips, (int)w.padded, (const float*)(ws + w.zt),
+  join_strips_kernel<<<(rows + 15) / 16, 1024, 0, s>>>((const float2*)(ws + w.part), strips, (int)w.padded, (const float*)(ws + w.zt),
                                                        (const int32_t*)(ws + w.list), kept.count, logp, lse);
   return launched();
 }
