@@ -348,48 +348,44 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(PackedShape p, con
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
   Reads<D> lds((lds_char*)(__attribute__((address_space(3))) void*)smem, lane);      // of the stage in work
   const int mine = w.t.row0 + wave * 32 + (lane & 31);
-  u32x4 qr[D / 16], gr[D / 16];
-  float dl = 0.f;
+  const int tiles = __builtin_amdgcn_readfirstlane((w.last + BN - 1) / BN);
+  const bool few = tiles > 0 && tiles <= 2;
+  Stream<D> ks, vs;
+  ks.init(k + (int64_t)w.k0 * p.kt + (int64_t)w.hk * p.kh, p.kt, max(w.lk, 1), p.d, wave, lane);
+  vs.init(v + (int64_t)w.k0 * p.vt + (int64_t)w.hk * p.vh, p.vt, max(w.lk, 1), p.d, wave, lane);
+  if (tiles > 0) {
+    ks.load(0, lds0, wave);
+    vs.load(0, lds0 + TILE, wave);
+  }
+  if (few && tiles > 1) {
+    ks.load(1, lds0 + STAGE, wave);
+    vs.load(1, lds0 + STAGE + TILE, wave);
+  }
+  // all that the rows need is requested before the first of it is waited for
+  const size_t stat = (size_t)w.h * p.total_q + w.t.first + min(mine, w.t.len - 1);
+  float dl = 0.f, l = lse[stat] * kLog2e;
+  u32x4 qr[D / 16], gr[D / 16], orow[D / 16];
   own_rows<D>(dout + (int64_t)w.t.first * p.ot + (int64_t)w.h * p.oh, p.ot, mine, w.t.len, p.d, lane, gr);
-  own_rows<D>(o + (int64_t)w.t.first * p.ot + (int64_t)w.h * p.oh, p.ot, mine, w.t.len, p.d, lane, qr);
+  own_rows<D>(o + (int64_t)w.t.first * p.ot + (int64_t)w.h * p.oh, p.ot, mine, w.t.len, p.d, lane, orow);
+  own_rows<D>(q + (int64_t)w.t.first * p.qt + (int64_t)w.h * p.qh, p.qt, mine, w.t.len, p.d, lane, qr);
 #pragma unroll
   for (int s = 0; s < D / 16; s++)
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-      dl = fmaf(bf2f((bf16_t)(gr[s][i] & 0xffffu)), bf2f((bf16_t)(qr[s][i] & 0xffffu)), dl);
-      dl = fmaf(bf2f((bf16_t)(gr[s][i] >> 16)), bf2f((bf16_t)(qr[s][i] >> 16)), dl);
+      dl = fmaf(bf2f((bf16_t)(gr[s][i] & 0xffffu)), bf2f((bf16_t)(orow[s][i] & 0xffffu)), dl);
+      dl = fmaf(bf2f((bf16_t)(gr[s][i] >> 16)), bf2f((bf16_t)(orow[s][i] >> 16)), dl);
     }
   dl += __shfl_xor(dl, 32, 64);
-  const size_t stat = (size_t)w.h * p.total_q + w.t.first + mine;
-  float l = 0.f;
-  if (mine < w.t.len) {
-    l = lse[stat] * kLog2e;
-    if (l == -INFINITY) l = INFINITY;
-  }
-  own_rows<D>(q + (int64_t)w.t.first * p.qt + (int64_t)w.h * p.qh, p.qt, mine, w.t.len, p.d, lane, qr);
+  if (l == -INFINITY) l = INFINITY;
   const float c = p.scale * kLog2e;
   const int seen = p.causal ? min(w.lk, mine + w.shift + 1) : w.lk;
   const int row_a = w.t.row0 + wave * 32, row_b = min(row_a + 32, w.t.len);
   const int all = row_a >= w.t.len ? 0 : p.causal ? min(w.lk, row_a + w.shift + 1) : w.lk;
   const int some = row_a >= w.t.len ? 0 : p.causal ? min(w.lk, row_b + w.shift) : w.lk;
-  const int tiles = __builtin_amdgcn_readfirstlane((w.last + BN - 1) / BN);
-  Stream<D> ks, vs;
-  ks.init(k + (int64_t)w.k0 * p.kt + (int64_t)w.hk * p.kh, p.kt, max(w.lk, 1), p.d, wave, lane);
-  vs.init(v + (int64_t)w.k0 * p.vt + (int64_t)w.hk * p.vh, p.vt, max(w.lk, 1), p.d, wave, lane);
-  if (tiles > 0) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // plain loads above are done: none is counted with those into LDS
-    ks.load(0, lds0, wave);
-    vs.load(0, lds0 + TILE, wave);
-  }
   // Queries of few keys: o is large there, its rounding to bf16 moves delta by as much as the gradients of the scores are rounded below.
   // Both stages hold all of their keys, so delta is taken as sum of p dp first (error of dq and dk 1.46 times that of their last
   // rounding, 1.7 without; tiles of more keys are below 1.5 as they are).
-  const bool few = tiles > 0 && tiles <= 2;
   if (few) {
-    if (tiles > 1) {
-      ks.load(1, lds0 + STAGE, wave);
-      vs.load(1, lds0 + STAGE + TILE, wave);
-    }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     dl = 0.f;
@@ -406,10 +402,6 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(PackedShape p, con
         if (j + row_of(e, lane) < seen) dl = fmaf(__builtin_amdgcn_exp2f(fmaf(z[e], c, -l)), dp[e], dl);
     }
     dl += __shfl_xor(dl, 32, 64);
-  }
-  if (mine < w.t.len && lane < 32) {
-    stats[stat] = l / -(p.scale * kLog2e);
-    stats[stat + (size_t)p.nq * p.total_q] = -dl;
   }
   f32x16 acc[D / 32];
 #pragma unroll
@@ -472,6 +464,10 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(PackedShape p, con
     }
     lds.move(t & 1 ? -STAGE : STAGE);
   }
+  if (mine < w.t.len && lane < 32) {
+    stats[stat] = l / -(p.scale * kLog2e);
+    stats[stat + (size_t)p.nq * p.total_q] = -dl;
+  }
   if (mine < w.t.len) store_rows<D>(acc, p.scale, dq + (int64_t)(w.t.first + mine) * p.ot + (int64_t)w.h * p.oh, p.d, lane);
 }
 
@@ -516,7 +512,6 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
   const int mine = t.row0 + 32 * block + (lane & 31);                                   // lane's key
   const int all = p.causal ? max(t.row0 + 32 * block + 31 - shift, 0) : 0;              // queries from here on see all keys of the wave
   u32x4 kr[S];
-  own_rows<D>(k + (int64_t)t.first * p.kt + (int64_t)hk * p.kh, p.kt, mine, t.len, p.d, lane, kr);
   const float c2 = p.scale * kLog2e;
   // The waves of a stream share its loads: the first half takes the queries, the second dO; 1 KB a load, ROWS rows.  A scalar offset
   // never leaves its buffer; a stream without work reads nothing but zeros, which add nothing (queries behind the end are zeros too).
@@ -649,6 +644,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
     load(r * STAGE);
     item += STREAMS;
   }
+  own_rows<D>(k + (int64_t)t.first * p.kt + (int64_t)hk * p.kh, p.kt, mine, t.len, p.d, lane, kr);
   if constexpr (MID) {
     landed();
     begin();
