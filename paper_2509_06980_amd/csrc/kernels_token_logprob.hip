@@ -1,5 +1,6 @@
 // Log-probs of target tokens from hidden rows and the lm-head's weights, with their gradient, without keeping the logits.
 #include <algorithm>
+#include <type_traits>
 
 #include "token_logprob.h"
 
@@ -23,6 +24,7 @@ struct RowScan {
   int32_t *count, *list, *place, *target;
   float *lse_kept, *g_kept, *logp, *lse;
   SliceRule rule;
+  int twins;
 };
 // Returns how many rows are kept; found: the row that went to place `wanted`, for one thread at most.
 __device__ __forceinline__ int scan_rows(const RowScan& s, bool write, int wanted, int* found) {
@@ -47,10 +49,13 @@ __device__ __forceinline__ int scan_rows(const RowScan& s, bool write, int wante
     if (keep && at == wanted) *found = t;
     if (keep && write) {
       s.list[at] = t;
-      s.target[at] = y;
-      if (s.g) {
-        s.lse_kept[at] = s.lse_in[t];
-        s.g_kept[at] = gt * s.inv_t;
+      for (int k = 0; k < (s.twins ? 2 : 1); k++) {
+        const int i = at + k * s.twins;
+        s.target[i] = y;
+        if (s.g) {
+          s.lse_kept[i] = s.lse_in[t];
+          s.g_kept[i] = gt * s.inv_t;
+        }
       }
     }
     if (t < s.rows && write) {
@@ -66,13 +71,15 @@ __device__ __forceinline__ int scan_rows(const RowScan& s, bool write, int wante
   }
   if (!write) return done;
   for (int i = done + threadIdx.x; i < (int)((done + kRowPad - 1) / kRowPad * kRowPad); i += 1024) {
+    if (s.twins && i >= s.twins && i < s.twins + done) continue;
     s.target[i] = -1;
     if (s.g) s.lse_kept[i] = 0.f, s.g_kept[i] = 0.f;
   }
   if (threadIdx.x == 0) {
-    s.count[0] = done;
+    const int all = s.twins && done ? 2 * s.twins : done;
+    s.count[0] = all;
     if (s.g) {
-      const int n = choose_slices(s.rule, done);
+      const int n = choose_slices(s.rule, all);
       s.count[1] = n;
       s.count[2] = ((s.rule.width + n - 1) / n + 63) / 64 * 64;
     }
@@ -108,9 +115,9 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(const T* __restrict__ 
 template <typename T, int VEC>
 __global__ __launch_bounds__(1024) void keep_and_gather_kernel(RowScan s, const T* __restrict__ h, int64_t stride, int hidden, int ld, T* __restrict__ out) {
   __shared__ int mine;
-  const int r = blockIdx.x, n = scan_rows(s, r == 0, r, &mine);
+  const int r = blockIdx.x, at = s.twins && r >= s.twins ? r - s.twins : r, n = scan_rows(s, r == 0, at, &mine);
   if (r >= (n + kRowPad - 1) / kRowPad * kRowPad) return;
-  copy_row<T, VEC>(r < n ? h + mine * stride : nullptr, hidden, ld, out + (size_t)r * ld);
+  copy_row<T, VEC>(at < n ? h + mine * stride : nullptr, hidden, ld, out + (size_t)r * ld);
 }
 
 // ---- products in 32 bits for every type and size ----------------------------------------------
@@ -292,7 +299,7 @@ __global__ __launch_bounds__(256) void logits_gradient_kernel(const T* __restric
       for (int e = 0; e < 16; e++) {
         const int v = i0 + wm * 64 + a * 32 + row32(lane, e);
         const float d = j < n && v < vocab ? g * ((v == y ? 1.f : 0.f) - expf(acc[a][b][e] * inv_t - l)) : 0.f;
-        st1(dz + (size_t)j * piece.ld + (v - piece.v0), d);
+        st1(dz + (size_t)j * piece.ld + (v - piece.v0), kept.twins && j >= kept.twins ? rounding_left(d) : d);
       }
   }
 }
@@ -345,23 +352,48 @@ __global__ __launch_bounds__(256) void weight_gradient_kernel(const T* __restric
     }
 }
 
-// rows of dh: the slices' sum, zeros where a row takes no part
-template <typename T, int VEC>
+// Rows of dh: the slices' sum, zeros where a row takes no part.  SPLIT: waves that share a row's slices, for few rows, which have many
+// (64 rows of 1024 in 64 slices twice: 66 us by one).
+template <typename T, int VEC, int SPLIT>
 __global__ __launch_bounds__(256) void hidden_gradient_rows_kernel(const float* __restrict__ slices, const int32_t* __restrict__ count, size_t slice_stride,
-                                                                   int hidden, const int32_t* __restrict__ place, T* __restrict__ dh) {
-  const int t = blockIdx.x, at = place[t], n_slices = count[1];
-  for (int c = threadIdx.x * VEC; c < hidden; c += 256 * VEC) {
+                                                                   int hidden, const int32_t* __restrict__ place, int twins, T* __restrict__ dh) {
+  constexpr int THREADS = 256 / SPLIT, N = SPLIT > 1 ? 8 : 2;      // threads of a piece of a row
+  __shared__ float part[SPLIT > 1 ? SPLIT : 1][SPLIT > 1 ? THREADS * VEC : 1];
+  const int t = blockIdx.x, at = place[t], n = count[1], all = at < 0 ? 0 : twins ? 2 * n : n, share = threadIdx.x / THREADS, lane = threadIdx.x % THREADS;
+  for (int c0 = blockIdx.y * THREADS * VEC; c0 < hidden; c0 += gridDim.y * THREADS * VEC) {
+    const int c = c0 + lane * VEC;
     float v[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; e++) v[e] = at == -2 ? __builtin_nanf("") : 0.f;
-    if (at >= 0)
-      for (int s = 0; s < n_slices; s++) {
-        float x[VEC];
-        ldv<VEC>(slices + s * slice_stride + (size_t)at * hidden + c, x);
+    if (c < hidden) {
+      const float* p = slices + (size_t)max(at, 0) * hidden + c;
+      for (int s0 = share; s0 < all; s0 += N * SPLIT) {      // N at once
+        float x[N][VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; e++) v[e] += x[e];
+        for (int i = 0; i < N; i++) {
+          const int s = min(s0 + i * SPLIT, all - 1);
+          ldv<VEC>(p + (s < n ? s * slice_stride : (s - n) * slice_stride + (size_t)twins * hidden), x[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < N; i++)
+#pragma unroll
+          for (int e = 0; e < VEC; e++) v[e] += s0 + i * SPLIT < all ? x[i][e] : 0.f;
       }
-    stv<VEC>(dh + (size_t)t * hidden + c, v);
+    }
+    if constexpr (SPLIT > 1) {
+#pragma unroll
+      for (int e = 0; e < VEC; e++) part[share][e * THREADS + lane] = v[e];
+      __syncthreads();
+      if (share == 0) {
+#pragma unroll
+        for (int e = 0; e < VEC; e++) {
+#pragma unroll
+          for (int w = 1; w < SPLIT; w++) v[e] += part[w][e * THREADS + lane];
+        }
+      }
+      __syncthreads();
+    }
+    if (share == 0 && c < hidden) stv<VEC>(dh + (size_t)t * hidden + c, v);
   }
 }
 
@@ -451,9 +483,9 @@ template <typename T>
 int forward(const void* h, int64_t stride, int rows, int hidden, const void* weight, int vocab, const int32_t* targets, float inv_t,
             float* logp, float* lse, char* ws, hipStream_t s) {
   const Workspace w = plan(rows, hidden, vocab, sizeof(T) == 2 ? RL_DTYPE_BF16 : RL_DTYPE_F32, false);
-  const KeptRows kept{(int32_t*)(ws + w.count), (int32_t*)(ws + w.target), nullptr, nullptr};
+  const KeptRows kept{(int32_t*)(ws + w.count), (int32_t*)(ws + w.target), nullptr, nullptr, 0};
   keep<T>(RowScan{targets, rows, vocab, nullptr, nullptr, inv_t, (int32_t*)(ws + w.count), (int32_t*)(ws + w.list), nullptr,
-                  (int32_t*)(ws + w.target), nullptr, nullptr, logp, lse, SliceRule{}},
+                  (int32_t*)(ws + w.target), nullptr, nullptr, logp, lse, SliceRule{}, 0},
           h, stride, hidden, w, ws, s);
   int strips = (vocab + 127) / 128;
   const bool mfma = token_logprob_takes_mfma<T>(w.padded, w.ld, hidden, 0, weight, nullptr);
@@ -474,9 +506,10 @@ template <typename T>
 int backward(const float* g, const void* h, int64_t stride, int rows, int hidden, const void* weight, int vocab, const int32_t* targets,
              const float* lse, float inv_t, void* dh, void* dw, char* ws, hipStream_t s) {
   const Workspace w = plan(rows, hidden, vocab, sizeof(T) == 2 ? RL_DTYPE_BF16 : RL_DTYPE_F32, true);
-  const KeptRows kept{(int32_t*)(ws + w.count), (int32_t*)(ws + w.target), (float*)(ws + w.lse), (float*)(ws + w.g)};
+  const int twins = twins_of(rows, sizeof(T) == 2);
+  const KeptRows kept{(int32_t*)(ws + w.count), (int32_t*)(ws + w.target), (float*)(ws + w.lse), (float*)(ws + w.g), twins};
   keep<T>(RowScan{targets, rows, vocab, g, lse, inv_t, (int32_t*)(ws + w.count), (int32_t*)(ws + w.list), (int32_t*)(ws + w.place),
-                  (int32_t*)(ws + w.target), (float*)(ws + w.lse), (float*)(ws + w.g), nullptr, nullptr, w.slices},
+                  (int32_t*)(ws + w.target), (float*)(ws + w.lse), (float*)(ws + w.g), nullptr, nullptr, w.slices, twins},
           h, stride, hidden, w, ws, s);
   const int vec = hidden % (16 / sizeof(T)) == 0 && aligned16(weight);
   const T *hr = (const T*)(ws + w.rows), *wt = (const T*)weight;
@@ -501,10 +534,17 @@ int backward(const float* g, const void* h, int64_t stride, int rows, int hidden
   const float* slices = (const float*)(ws + w.dh);
   const int32_t* place = (const int32_t*)(ws + w.place);
   constexpr int VEC = 16 / sizeof(T);
-  if (hidden % VEC == 0 && aligned16(dh))
-    hidden_gradient_rows_kernel<T, VEC><<<rows, 256, 0, s>>>(slices, kept.count, (size_t)w.padded * hidden, hidden, place, (T*)dh);
-  else
-    hidden_gradient_rows_kernel<T, 1><<<rows, 256, 0, s>>>(slices, kept.count, (size_t)w.padded * hidden, hidden, place, (T*)dh);
+  auto rows_of_dh = [&](auto vec_of, auto split) {
+    constexpr int W = decltype(vec_of)::value, S = decltype(split)::value;
+    hidden_gradient_rows_kernel<T, W, S><<<dim3(rows, S > 1 ? (hidden + 64 * W - 1) / (64 * W) : 1), 256, 0, s>>>(
+        slices, kept.count, (size_t)w.padded * hidden, hidden, place, twins, (T*)dh);
+  };
+  const std::integral_constant<int, 1> one;
+  const std::integral_constant<int, 4> four;
+  const std::integral_constant<int, VEC> whole;
+  const bool wide = hidden % VEC == 0 && aligned16(dh);
+  if (rows <= 512) wide ? rows_of_dh(whole, four) : rows_of_dh(one, four);
+  else wide ? rows_of_dh(whole, one) : rows_of_dh(one, one);
   return launched();
 }
 

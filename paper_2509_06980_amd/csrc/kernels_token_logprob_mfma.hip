@@ -390,11 +390,15 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
         const int y = (int)row_data(a, 0) - P.v0 - j0;
         const float g = __builtin_bit_cast(float, row_data(a, 1)), l = __builtin_bit_cast(float, row_data(a, 2)) * 1.44269504f;
         auto dz = [&](int b, int e) { return -g * __builtin_amdgcn_exp2f(fmaf(val(a, b, e), P.scale, -l)); };
+        const bool twin = EL == 2 && MB == 2 && P.kept.twins && (wm * MB + a) * 32 + (ln & 31) >= P.kept.twins;      // all rows are in one tile then
         if (crosses || __any(y >= 0 && y < BN)) {
           store(a, [&](int b, int e) {
             const int j = jw + 32 * b + 8 * (e >> 2) + (e & 3);
-            return P.v0 + j0 + j >= P.vocab ? 0.f : j == y ? dz(b, e) + g : dz(b, e);
+            const float v = P.v0 + j0 + j >= P.vocab ? 0.f : j == y ? dz(b, e) + g : dz(b, e);
+            return twin ? rounding_left(v) : v;
           });
+        } else if (__any(twin)) {
+          store(a, [&](int b, int e) { return twin ? rounding_left(dz(b, e)) : dz(b, e); });
         } else {
           store(a, dz);
         }

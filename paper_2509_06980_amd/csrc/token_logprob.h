@@ -24,7 +24,18 @@ struct KeptRows {
   const int32_t* target;     // [rows padded] target of a kept row, -1 in the padding
   const float* lse;          // backward: log-sum-exp of a kept row
   const float* g;            // backward: gradient of its log-prob / temperature, 0 in the padding
+  int twins;                 // backward: as twins_of says
 };
+// Backward in bf16 with up to 64 rows: row twins + r is row r once more and holds what the rounding of its dz left, so that both products
+// behind see dz in 16 bits (relative error of both gradients 0.0017, that of their last rounding).  Without it they were 0.0020 to 0.0028
+// off: few rows do not average the rounding of a row's largest element, its target's.  Few rows fill no tile: 64 x 2560 x 20000, both directions,
+// 152 us with and without; 30 x 4096 x 151936 1.12 ms, without 1.08.  Of more rows the gradients
+// are 0.0024 off.
+static inline int twins_of(int rows, bool bf16) { return !bf16 || rows > 64 ? 0 : rows > 32 ? 64 : rows > 16 ? 32 : 16; }
+static __device__ __forceinline__ float rounding_left(float v) {
+  const float left = v - (float)(__bf16)v;
+  return left == left ? left : 0.f;      // infinite or no number: in the row itself
+}
 // Padding of the kept rows: zeros up to a multiple of this.
 const int kRowPad = 256;
 // One product of the backward pass over `width` tokens of the vocabulary from v0 on; dz [row][ld] holds the gradients of its logits.

@@ -466,6 +466,28 @@ def _check_token_logprobs(dt, rows, hidden, vocab):
         within(name, got, *ref[name])
 
 
+@pytest.mark.parametrize("rows,hidden,vocab", [(1, 64, 1000), (17, 1024, 4096), (63, 100, 30_000), (64, 768, 140_000)])
+def test_token_logprobs_of_few_rows_are_rounded_once(rows, hidden, vocab):
+    # up to 64 rows: the gradient of the logits keeps 16 bits on its way, so the bound of 32 bits holds but for u^2 of it, and one rounding
+    g = gen(rows + hidden)
+    w = randn(g, vocab, hidden, dt=BF, std=2 / math.sqrt(hidden))
+    y = torch.randint(0, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    y[5::6] = -1
+    h = (torch.randn(rows, hidden, generator=g, device="cuda") + w[y.long()].float()).to(BF)
+    dlogp, u = randn(g, rows), unit(BF)
+    logp, lse = ops.token_logprobs_forward(h, w, y, 1.3)
+    got = dict(zip(("dh", "dw"), ops.token_logprobs_backward(dlogp, h, w, y, lse, 1.3)))
+    ref = logprob_reference(h, w, y, dlogp, 1.3, FP)
+    gk = torch.where(y >= 0, dlogp.double(), 0.0)[:, None] / 1.3
+    dz = gk.abs() * (h.double() @ w.double().t() / 1.3 - lse.double()[:, None]).exp()
+    dz.scatter_add_(1, y.clamp(min=0).long()[:, None], gk.abs())
+    left = {"dh": dz @ w.double().abs(), "dw": dz.t() @ h.double().abs()}
+    for name in ("dh", "dw"):
+        want, err = ref[name]
+        err = err + u * u * left[name]
+        within(name, got[name], want, err + u * (want.abs() + err))
+
+
 @pytest.mark.parametrize("dt", [BF, FP])
 def test_token_logprobs_over_several_pieces_of_the_vocabulary(dt):
     # pieces hold at least 1024 tokens: rows enough that the budget of a piece stays at that, few of them with a target
