@@ -380,6 +380,10 @@ int rl_attention_forward(const void* d_q, int64_t q_token_stride, int64_t q_head
                          int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float scale, int32_t causal, int32_t dtype,
                          void* d_o, float* d_lse, void* stream);
 int64_t rl_attention_workspace(int32_t total_q, int32_t n_q_heads);      /* of the backward call */
+/* The same with room for sums of dk and dv in 32 bits: where there are few keys and KV heads for a launch that fills the GPU, their
+ * gradients are then formed by several workgroups a key and added up (16-byte aligned; never less than the above).  0: refused sizes. */
+int64_t rl_attention_fast_workspace(int32_t n_seq, int32_t total_q, int32_t total_k, int32_t n_q_heads, int32_t n_kv_heads,
+                                    int32_t head_dim, int32_t dtype);
 int rl_attention_backward(const void* d_do, const void* d_q, int64_t q_token_stride, int64_t q_head_stride, const void* d_k,
                           int64_t k_token_stride, int64_t k_head_stride, const void* d_v, int64_t v_token_stride,
                           int64_t v_head_stride, const void* d_o, const float* d_lse, const int32_t* d_cu_q,

@@ -15,6 +15,7 @@ EXPORTED_SYMBOLS = [
     "rl_decode_step_with_appends", "rl_decode_step_forced_with_appends", "rl_grpo_objective", "rl_debug_pass_plan",
     "rl_debug_residual_plan", "rl_debug_many_row_loads", "rl_debug_staging_plan",
     "rl_norm_forward", "rl_norm_workspace", "rl_norm_backward", "rl_rotary", "rl_attention_forward", "rl_attention_workspace",
+    "rl_attention_fast_workspace",
     "rl_attention_backward", "rl_token_logprobs_workspace", "rl_token_logprobs_forward", "rl_token_logprobs_backward",
 ]
 
@@ -107,7 +108,7 @@ def load_library():
     lib.rl_attention_backward.argtypes = [p, p, l, l, p, l, l, p, l, l, p, p, p, p, i, i, i, i, i, i, f, i, i, p, p, p, p, l, p]
     lib.rl_token_logprobs_forward.argtypes = [p, l, i, i, p, i, p, f, i, p, p, p, l, p]
     lib.rl_token_logprobs_backward.argtypes = [p, p, l, i, i, p, i, p, p, f, i, p, p, p, l, p]
-    for name, args in (("rl_norm_workspace", [l, i, i]), ("rl_attention_workspace", [i, i]),
+    for name, args in (("rl_norm_workspace", [l, i, i]), ("rl_attention_workspace", [i, i]), ("rl_attention_fast_workspace", [i] * 7),
                        ("rl_token_logprobs_workspace", [i, i, i, i, i])):
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = l

@@ -276,7 +276,7 @@ __global__ __launch_bounds__(256) void attention_rows_dq(PackedShape p, int vec,
 template <typename T, int D, int SPLIT>
 __global__ __launch_bounds__(256) void attention_rows_dkv(PackedShape p, int vec, const T* __restrict__ dout, const T* __restrict__ q,
                                                           const T* __restrict__ k, const T* __restrict__ v, const float* __restrict__ lse,
-                                                          const float* __restrict__ delta, T* __restrict__ dk, T* __restrict__ dv) {
+                                                          const float* __restrict__ delta, T* __restrict__ dk, T* __restrict__ dv, KeyParts parts) {
   constexpr int BM = 64 / SPLIT, BT = BN * SPLIT;
   extern __shared__ f32 dynamic[];
   f32(*qs)[D + PAD] = (f32(*)[D + PAD])dynamic;
@@ -297,44 +297,44 @@ __global__ __launch_bounds__(256) void attention_rows_dkv(PackedShape p, int vec
 #pragma unroll
   for (int j = 0; j < D / 16; j++) ak[j] = av[j] = {0.f, 0.f, 0.f, 0.f};
   const int first = p.causal ? max(t.row0 - shift, 0) / BN * BN : 0;
-  for (int h = hk * group; h < (hk + 1) * group; h++) {
+  const int per_head = max((lq - first + BT - 1) / BT, 0);
+  for (int pair = blockIdx.z; pair < per_head * group; pair += parts.n) {      // (query head, query tile)
+    const int h = hk * group + pair / per_head, i0 = first + pair % per_head * BT;
     const T* qb = q + (int64_t)q0 * p.qt + (int64_t)h * p.qh;
     const T* gb = dout + (int64_t)q0 * ds_ + (int64_t)h * p.d;
-    for (int i0 = first; i0 < lq; i0 += BT) {
-      __syncthreads();
-      stage<T, D>(qb, p.qt, i0, BT, lq, p.d, vec, qs);
-      stage<T, D>(gb, ds_, i0, BT, lq, p.d, vec, gs);
-      __syncthreads();
-      f32x4 z[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, dp[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    __syncthreads();
+    stage<T, D>(qb, p.qt, i0, BT, lq, p.d, vec, qs);
+    stage<T, D>(gb, ds_, i0, BT, lq, p.d, vec, gs);
+    __syncthreads();
+    f32x4 z[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, dp[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-      for (int s = 0; s < D / 4; s++)
-#pragma unroll
-        for (int c = 0; c < 2; c++) {
-          z[c] = mfma4(a[s], qs[part + c * 16 + l16][4 * s + l4], z[c]);
-          dp[c] = mfma4(b[s], gs[part + c * 16 + l16][4 * s + l4], dp[c]);
-        }
+    for (int s = 0; s < D / 4; s++)
 #pragma unroll
       for (int c = 0; c < 2; c++) {
-        const int i = i0 + part + c * 16 + l16;
-        const bool in = i < lq;
-        const f32 l = in ? lse[(size_t)h * p.total_q + q0 + i] : 0.f, dl = in ? delta[(size_t)h * p.total_q + q0 + i] : 0.f;
-        const int end = !in ? 0 : p.causal ? min(t.len, i + shift + 1) : t.len;      // this query sees the keys [0, end)
-#pragma unroll
-        for (int r = 0; r < 4; r++) {
-          const f32 e = t.row0 + own + 4 * l4 + r < end ? expf(z[c][r] * p.scale - l) : 0.f;
-          pt[wave][4 * l4 + r][c * 16 + l16] = e;
-          dt[wave][4 * l4 + r][c * 16 + l16] = e != 0.f ? e * (dp[c][r] - dl) * p.scale : 0.f;
-        }
+        z[c] = mfma4(a[s], qs[part + c * 16 + l16][4 * s + l4], z[c]);
+        dp[c] = mfma4(b[s], gs[part + c * 16 + l16][4 * s + l4], dp[c]);
       }
-      __syncthreads();
 #pragma unroll
-      for (int s = 0; s < BN / 4; s++) {
-        const f32 x = pt[wave][l16][4 * s + l4], y = dt[wave][l16][4 * s + l4];
+    for (int c = 0; c < 2; c++) {
+      const int i = i0 + part + c * 16 + l16;
+      const bool in = i < lq;
+      const f32 l = in ? lse[(size_t)h * p.total_q + q0 + i] : 0.f, dl = in ? delta[(size_t)h * p.total_q + q0 + i] : 0.f;
+      const int end = !in ? 0 : p.causal ? min(t.len, i + shift + 1) : t.len;      // this query sees the keys [0, end)
 #pragma unroll
-        for (int j = 0; j < D / 16; j++) {
-          av[j] = mfma4(x, gs[part + 4 * s + l4][16 * j + l16], av[j]);
-          ak[j] = mfma4(y, qs[part + 4 * s + l4][16 * j + l16], ak[j]);
-        }
+      for (int r = 0; r < 4; r++) {
+        const f32 e = t.row0 + own + 4 * l4 + r < end ? expf(z[c][r] * p.scale - l) : 0.f;
+        pt[wave][4 * l4 + r][c * 16 + l16] = e;
+        dt[wave][4 * l4 + r][c * 16 + l16] = e != 0.f ? e * (dp[c][r] - dl) * p.scale : 0.f;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < BN / 4; s++) {
+      const f32 x = pt[wave][l16][4 * s + l4], y = dt[wave][l16][4 * s + l4];
+#pragma unroll
+      for (int j = 0; j < D / 16; j++) {
+        av[j] = mfma4(x, gs[part + 4 * s + l4][16 * j + l16], av[j]);
+        ak[j] = mfma4(y, qs[part + 4 * s + l4][16 * j + l16], ak[j]);
       }
     }
   }
@@ -355,8 +355,14 @@ __global__ __launch_bounds__(256) void attention_rows_dkv(PackedShape p, int vec
 #pragma unroll
       for (int j = 0; j < D / 16; j++)
         if (16 * j + l16 < p.d) {
-          st1(dk + at + row * dks + 16 * j + l16, ak[j][r]);
-          st1(dv + at + row * dks + 16 * j + l16, av[j][r]);
+          const int64_t i = at + row * dks + 16 * j + l16;
+          if (parts.n > 1) {
+            parts.of(p, blockIdx.z, 0)[i] = ak[j][r];
+            parts.of(p, blockIdx.z, 1)[i] = av[j][r];
+          } else {
+            st1(dk + i, ak[j][r]);
+            st1(dv + i, av[j][r]);
+          }
         }
     }
   }
@@ -367,8 +373,25 @@ template <typename T>
 bool fours(const void* x, int64_t ts, int64_t hs, int d) {
   return ((uintptr_t)x & (4 * sizeof(T) - 1)) == 0 && ts % 4 == 0 && hs % 4 == 0 && d % 4 == 0;
 }
+// dk and dv of 8 keys of one KV head from the sums of their parts, in their order
+template <typename T>
+__global__ __launch_bounds__(256) void attention_join_parts(PackedShape p, KeyParts parts, T* __restrict__ dk, T* __restrict__ dv) {
+  const PackedTile t = packed_tile(p.cu_k, p.n_seq, p.total_k, 64, blockIdx.x);
+  const int row0 = t.row0 + blockIdx.z * 8, rows = min(t.len - row0, 8);
+  const int64_t step = (int64_t)p.total_k * p.nkv * p.d;
+  for (int i = threadIdx.x; i < rows * p.d; i += 256) {
+    const int64_t at = ((int64_t)(t.first + row0 + i / p.d) * p.nkv + blockIdx.y) * p.d + i % p.d;
+    const float* x = parts.sums + at;
+    f32 a = 0.f, b = 0.f;
+#pragma unroll 4
+    for (int n = 0; n < parts.n; n++) a += x[2 * n * step], b += x[(2 * n + 1) * step];
+    st1(dk + at, a);
+    st1(dv + at, b);
+  }
+}
+
 template <auto kernel, typename... A>
-void launch_rows(int tiles, int heads, int lds, hipStream_t s, A... args) {
+void launch_rows(int tiles, int heads, int depth, int lds, hipStream_t s, A... args) {
   static std::atomic<uint64_t> done;      // more than 64 KB of LDS need an opt-in, once per kernel and device
   int dev = 0;
   (void)hipGetDevice(&dev);
@@ -377,7 +400,7 @@ void launch_rows(int tiles, int heads, int lds, hipStream_t s, A... args) {
     (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     done.fetch_or(bit, std::memory_order_release);
   }
-  kernel<<<dim3(tiles, heads), 256, lds, s>>>(args...);
+  kernel<<<dim3(tiles, heads, depth), 256, lds, s>>>(args...);
 }
 // 16 rows split over four waves in place of 64 rows, 16 a wave, where tiles of 64 would leave half the CUs idle.  Measured, forward and
 // backward of one sequence in 64 and 128 dimensions: 1024 tokens, 4 heads (68 tiles) 148 and 347 us, unsplit 324 and 629; 8 heads (136) 373
@@ -392,21 +415,21 @@ template <typename T, int D>
 void forward(hipStream_t s, const PackedShape& p, const void* q, const void* k, const void* v, void* o, float* lse) {
   const int vec = fours<T>(k, p.kt, p.kh, p.d) && fours<T>(v, p.vt, p.vh, p.d);
   if (split_rows(p.total_q, p.n_seq, p.nq))
-    launch_rows<attention_rows_forward<T, D, 4>>(packed_tiles(p.total_q, p.n_seq, 16), p.nq, rows_lds<D>(4), s, p, vec, (const T*)q, (const T*)k,
+    launch_rows<attention_rows_forward<T, D, 4>>(packed_tiles(p.total_q, p.n_seq, 16), p.nq, 1, rows_lds<D>(4), s, p, vec, (const T*)q, (const T*)k,
                 (const T*)v, (T*)o, lse);
   else
-    launch_rows<attention_rows_forward<T, D, 1>>(packed_tiles(p.total_q, p.n_seq, 64), p.nq, rows_lds<D>(1), s, p, vec, (const T*)q, (const T*)k,
+    launch_rows<attention_rows_forward<T, D, 1>>(packed_tiles(p.total_q, p.n_seq, 64), p.nq, 1, rows_lds<D>(1), s, p, vec, (const T*)q, (const T*)k,
                 (const T*)v, (T*)o, lse);
 }
 template <typename T, int D>
 void backward(hipStream_t s, const PackedShape& p, const void* dout, const void* q, const void* k, const void* v, const void* o,
-              const float* lse, void* dq, void* dk, void* dv, float* delta) {
+              const float* lse, void* dq, void* dk, void* dv, float* delta, const KeyParts& parts) {
   const int by_key = fours<T>(k, p.kt, p.kh, p.d) && fours<T>(v, p.vt, p.vh, p.d);
   const int by_query = fours<T>(q, p.qt, p.qh, p.d) && fours<T>(dout, p.ot, p.oh, p.d);
   if (p.total_q > 0) {
     auto go = [&](auto split) {
       constexpr int S = decltype(split)::value;
-      launch_rows<attention_rows_dq<T, D, S>>(packed_tiles(p.total_q, p.n_seq, 64 / S), p.nq, rows_lds<D>(S), s, p, by_key, (const T*)dout,
+      launch_rows<attention_rows_dq<T, D, S>>(packed_tiles(p.total_q, p.n_seq, 64 / S), p.nq, 1, rows_lds<D>(S), s, p, by_key, (const T*)dout,
                   (const T*)q, (const T*)k, (const T*)v, (const T*)o, lse, (T*)dq, delta);
     };
     if (split_rows(p.total_q, p.n_seq, p.nq)) go(std::integral_constant<int, 4>());
@@ -415,12 +438,22 @@ void backward(hipStream_t s, const PackedShape& p, const void* dout, const void*
   if (p.total_k > 0) {
     auto go = [&](auto split) {
       constexpr int S = decltype(split)::value;
-      launch_rows<attention_rows_dkv<T, D, S>>(packed_tiles(p.total_k, p.n_seq, 64 / S), p.nkv, rows_lds<D>(S), s, p, by_query, (const T*)dout,
-                  (const T*)q, (const T*)k, (const T*)v, lse, delta, (T*)dk, (T*)dv);
+      launch_rows<attention_rows_dkv<T, D, S>>(packed_tiles(p.total_k, p.n_seq, 64 / S), p.nkv, parts.n, rows_lds<D>(S), s, p, by_query, (const T*)dout,
+                  (const T*)q, (const T*)k, (const T*)v, lse, delta, (T*)dk, (T*)dv, parts);
     };
-    if (split_rows(p.total_k, p.n_seq, p.nkv)) go(std::integral_constant<int, 4>());
+    if (parts.n == 1 && split_rows(p.total_k, p.n_seq, p.nkv)) go(std::integral_constant<int, 4>());
     else go(std::integral_constant<int, 1>());
   }
+}
+
+int64_t parts_bytes(const PackedShape& p) { return (int64_t)p.total_k * p.nkv * p.d * 2 * (int64_t)sizeof(float); }
+// bf16: a workgroup a CU, fp32: two, and where rows could be split over waves instead, four parts or none.  Measured, both directions, with
+// parts and without: bf16, one sequence of 2000, 8 heads over 1 of 128, 129 and 301 us, of 6000 583 and 882, 8 sequences of 256, 8 heads
+// over 1 of 64, 33 and 40; fp32, one of 2000, 1118 and 2520, of 1500, 32 over 8, 2047 and 2521; 4 heads of 64, 1024 tokens, two parts 179, split 152.
+int parts_of(const PackedShape& p, int32_t dtype) {
+  if (dtype == RL_DTYPE_BF16) return key_parts(p, 256);
+  const int n = key_parts(p, 512);
+  return n < 4 && split_rows(p.total_k, p.n_seq, p.nkv) ? 1 : n;
 }
 
 const char* attention_argument(const PackedShape& p, int32_t dtype) {
@@ -464,6 +497,15 @@ extern "C" int64_t rl_attention_workspace(int32_t total_q, int32_t n_q_heads) {
   return total_q < 0 || n_q_heads < 1 ? 0 : (int64_t)total_q * n_q_heads * 2 * (int64_t)sizeof(float);
 }
 
+extern "C" int64_t rl_attention_fast_workspace(int32_t n_seq, int32_t total_q, int32_t total_k, int32_t n_q_heads, int32_t n_kv_heads,
+                                               int32_t head_dim, int32_t dtype) {
+  const int32_t none = 0;      // offsets are not looked at
+  const PackedShape p{&none, &none, n_seq, total_q, total_k, n_q_heads, n_kv_heads, head_dim, 0, 0, 0, 0, 0, 0, 0, 0, 1.f, 0};
+  if (attention_argument(p, dtype)) return 0;
+  const int parts = parts_of(p, dtype);
+  return up(rl_attention_workspace(total_q, n_q_heads), 256) + (parts > 1 ? parts * parts_bytes(p) : 0);
+}
+
 extern "C" int rl_attention_backward(const void* d_do, const void* d_q, int64_t q_token_stride, int64_t q_head_stride, const void* d_k,
                                      int64_t k_token_stride, int64_t k_head_stride, const void* d_v, int64_t v_token_stride,
                                      int64_t v_head_stride, const void* d_o, const float* d_lse, const int32_t* d_cu_q,
@@ -481,17 +523,27 @@ extern "C" int rl_attention_backward(const void* d_do, const void* d_q, int64_t 
   if ((uintptr_t)d_workspace & 3) return rl_fail(RL_E_ARG, "workspace not aligned to 4 bytes");
   hipStream_t s = (hipStream_t)stream;
   float* delta = (float*)d_workspace;
-#define RL_GO(T, D) backward<T, D>(s, p, d_do, d_q, d_k, d_v, d_o, d_lse, d_dq, d_dk, d_dv, delta)
+  // parts where the workspace has room for them
+  const int64_t base = up(rl_attention_workspace(total_q, n_q_heads), 256);
+  const int most = parts_of(p, dtype);
+  const bool room = most > 1 && aligned16(d_workspace) && workspace_bytes >= base + most * parts_bytes(p);
+  const KeyParts parts{room ? most : 1, room ? (float*)((char*)d_workspace + base) : nullptr};
+#define RL_GO(T, D) backward<T, D>(s, p, d_do, d_q, d_k, d_v, d_o, d_lse, d_dq, d_dk, d_dv, delta, parts)
   if (dtype == RL_DTYPE_F32) {
     if (head_dim <= 64) RL_GO(float, 64);
     else RL_GO(float, 128);
   } else if (attention_takes_mfma(p, d_q, d_k, d_v, d_o, d_do) && aligned16(d_dq) && aligned16(d_dk) && aligned16(d_dv)) {
     launch_attention_mfma_backward(s, p, (const bf16_t*)d_do, (const bf16_t*)d_q, (const bf16_t*)d_k, (const bf16_t*)d_v, (const bf16_t*)d_o,
-                                   d_lse, (bf16_t*)d_dq, (bf16_t*)d_dk, (bf16_t*)d_dv, delta);
+                                   d_lse, (bf16_t*)d_dq, (bf16_t*)d_dk, (bf16_t*)d_dv, delta, parts);
   } else {
     if (head_dim <= 64) RL_GO(bf16_t, 64);
     else RL_GO(bf16_t, 128);
   }
 #undef RL_GO
+  if (parts.n > 1) {
+    const dim3 grid(packed_tiles(total_k, n_seq, 64), n_kv_heads, 8);
+    if (dtype == RL_DTYPE_F32) attention_join_parts<float><<<grid, 256, 0, s>>>(p, parts, (float*)d_dk, (float*)d_dv);
+    else attention_join_parts<bf16_t><<<grid, 256, 0, s>>>(p, parts, (bf16_t*)d_dk, (bf16_t*)d_dv);
+  }
   return launched();
 }

@@ -480,7 +480,7 @@ template <int D, int BLOCKS, int R>
 __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, const bf16_t* __restrict__ dout, const bf16_t* __restrict__ q,
                                                                const bf16_t* __restrict__ k, const bf16_t* __restrict__ v,
                                                                const float* __restrict__ query_stats, bf16_t* __restrict__ dk,
-                                                               bf16_t* __restrict__ dv) {
+                                                               bf16_t* __restrict__ dv, KeyParts parts) {
   constexpr int STREAMS = 8 / BLOCKS, KEYS = 32 * BLOCKS;
   constexpr int TILE = 32 * D * 2, STAGE = 2 * TILE + 512;      // of a stream: queries, dO, then - lse / scale and - delta of the queries
   constexpr int S = D / 16, SLOTS = 4 * S, AHEAD = 3, VA = 2, PER = 16 / S;
@@ -508,7 +508,8 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
     if (2 * (wave >> 2) < BLOCKS) vs.load(t.row0 / 64 + (wave >> 2), lds0 + STREAMS * R * STAGE + (unsigned)(wave >> 2) * (2 * TILE), wave & 3);
   }
   const int first = p.causal ? max(t.row0 - shift, 0) / 32 : 0, per_head = max((lq + 31) / 32 - first, 0);
-  const int rounds = (per_head * group + STREAMS - 1) / STREAMS;
+  const int step_by = STREAMS * parts.n, begin_at = blockIdx.y * STREAMS;      // this workgroup's share of the (query head, query tile) pairs
+  const int rounds = max((per_head * group - begin_at + step_by - 1) / step_by, 0);
   const int mine = t.row0 + 32 * block + (lane & 31);                                   // lane's key
   const int all = p.causal ? max(t.row0 + 32 * block + 31 - shift, 0) : 0;              // queries from here on see all keys of the wave
   u32x4 kr[S];
@@ -522,7 +523,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
   const int64_t ts = second ? p.ot : p.qt, hs = second ? p.oh : p.qh;
   const float* const stats_from = query_stats + (second ? (size_t)p.nq * p.total_q : 0);
   const unsigned full = (unsigned)(((int64_t)(lq - 1) * ts + p.d) * 2);
-  int item = stream, h = hk * group;      // next tile of the current head
+  int item = begin_at + stream, h = hk * group;      // next tile of the current head
   auto load = [&](int at) {
     while (h < (hk + 1) * group && item >= per_head) {
       item -= per_head;
@@ -628,7 +629,7 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
   };
   // Loads go R - 1 rounds ahead, whether there is work or not.  Tiles of the rounds in work are counted apart from those loaded: the
   // same walk over (head, tile).
-  int done = stream;
+  int done = begin_at + stream;
   int at = 0, next = (R - 1) * STAGE;
   auto landed = [&]() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -636,13 +637,13 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
   };
   auto load_next = [&]() {
     load(next);
-    item += STREAMS;
+    item += step_by;
     next = next + STAGE == R * STAGE ? 0 : next + STAGE;
   };
 #pragma unroll
   for (int r = 0; r < R - 1; r++) {
     load(r * STAGE);
-    item += STREAMS;
+    item += step_by;
   }
   own_rows<D>(k + (int64_t)t.first * p.kt + (int64_t)hk * p.kh, p.kt, mine, t.len, p.d, lane, kr);
   if constexpr (MID) {
@@ -666,13 +667,13 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
       lds.move(after - at);
     }
     at = after;
-    done += STREAMS;
+    done += step_by;
   }
   asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");      // results of the assembly's last products
   // the streams' sums: [stream][key][D + 4] in LDS; several threads add up and store a key
   constexpr int PITCH = D + 4;
   lds_float* const sums = (lds_float*)lds_base;
-  auto join = [&](const f32x16 (&acc)[D / 32], float f, bf16_t* out) {
+  auto join = [&](const f32x16 (&acc)[D / 32], float f, bf16_t* out, int which) {
     __syncthreads();
 #pragma unroll
     for (int b = 0; b < D / 32; b++)
@@ -684,7 +685,9 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
     constexpr int SHARE = 512 / KEYS;      // threads of a key
     const int key = threadIdx.x / SHARE;
     if (t.row0 + key < t.len) {
-      bf16_t* row = out + (int64_t)(t.first + t.row0 + key) * p.nkv * p.d + (int64_t)hk * p.d;
+      const int64_t row_at = (int64_t)(t.first + t.row0 + key) * p.nkv * p.d + (int64_t)hk * p.d;
+      bf16_t* row = out + row_at;
+      float* const sum_row = parts.n > 1 ? parts.of(p, blockIdx.y, which) + row_at : nullptr;
 #pragma unroll
       for (int j = 0; j < D / 8 / SHARE; j++) {
         const int col = (threadIdx.x % SHARE) * 8 + 8 * SHARE * j;
@@ -699,13 +702,16 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
             y[4 + e] = w ? y[4 + e] + hi[e] : hi[e];
           }
         }
-        if (col < p.d)
+        if (col < p.d && sum_row) {
+          *(float4*)(sum_row + col) = make_float4(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
+          *(float4*)(sum_row + col + 4) = make_float4(y[4] * f, y[5] * f, y[6] * f, y[7] * f);
+        } else if (col < p.d)
           *(u32x4*)(row + col) = u32x4{pack2(y[0] * f, y[1] * f), pack2(y[2] * f, y[3] * f), pack2(y[4] * f, y[5] * f), pack2(y[6] * f, y[7] * f)};
       }
     }
   };
-  join(ak, p.scale, dk);
-  join(av, 1.f, dv);
+  join(ak, p.scale, dk, 0);
+  join(av, 1.f, dv, 1);
 }
 
 // More than 64 KB of dynamic LDS need an opt-in, once per kernel and device.
@@ -736,7 +742,7 @@ void forward(hipStream_t s, const PackedShape& p, const bf16_t* q, const bf16_t*
 }
 template <int D>
 void backward(hipStream_t s, const PackedShape& p, const bf16_t* dout, const bf16_t* q, const bf16_t* k, const bf16_t* v, const bf16_t* o,
-              const float* lse, bf16_t* dq, bf16_t* dk, bf16_t* dv, float* stats) {
+              const float* lse, bf16_t* dq, bf16_t* dk, bf16_t* dv, float* stats, const KeyParts& parts) {
   static std::atomic<uint64_t> done[3];
   const int lds = 4 * BN * D * 2;
   if (p.total_q > 0) {
@@ -749,7 +755,7 @@ void backward(hipStream_t s, const PackedShape& p, const bf16_t* dout, const bf1
       constexpr int ring = STREAMS * R * (2 * 32 * D * 2 + 512) + KEYS * D * 2, sums = STREAMS * KEYS * (D + 4) * 4, bytes = ring > sums ? ring : sums;
       auto kernel = attention_dkv_kernel<D, BLOCKS, R>;
       allow_lds(done[BLOCKS / 2], kernel, bytes);
-      kernel<<<(unsigned)(packed_tiles(p.total_k, p.n_seq, KEYS) * p.nkv), 512, bytes, s>>>(p, dout, q, k, v, stats, dk, dv);
+      kernel<<<dim3(packed_tiles(p.total_k, p.n_seq, KEYS) * p.nkv, parts.n), 512, bytes, s>>>(p, dout, q, k, v, stats, dk, dv, parts);
     };
     if (many_keys(p)) go(std::integral_constant<int, 4>(), std::integral_constant<int, 3>());
     else go(std::integral_constant<int, 2>(), std::integral_constant<int, D == 128 ? 2 : 3>());
@@ -778,7 +784,7 @@ void launch_attention_mfma_forward(hipStream_t s, const PackedShape& p, const bf
 }
 void launch_attention_mfma_backward(hipStream_t s, const PackedShape& p, const bf16_t* dout, const bf16_t* q, const bf16_t* k,
                                     const bf16_t* v, const bf16_t* o, const float* lse, bf16_t* dq, bf16_t* dk, bf16_t* dv,
-                                    float* stats) {
-  if (p.d <= 64) backward<64>(s, p, dout, q, k, v, o, lse, dq, dk, dv, stats);
-  else backward<128>(s, p, dout, q, k, v, o, lse, dq, dk, dv, stats);
+                                    float* stats, const KeyParts& parts) {
+  if (p.d <= 64) backward<64>(s, p, dout, q, k, v, o, lse, dq, dk, dv, stats, parts);
+  else backward<128>(s, p, dout, q, k, v, o, lse, dq, dk, dv, stats, parts);
 }

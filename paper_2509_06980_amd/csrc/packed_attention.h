@@ -66,6 +66,23 @@ __device__ __forceinline__ PackedTile packed_tile_by_rest(const int32_t* cu, int
   return t;
 }
 
+// dk and dv of few key tiles: each tile's (query head, query tile) pairs are dealt to `n` workgroups, whose sums another kernel adds up in
+// their order.  sums: [n][dk, dv][total_k][nkv][d].
+struct KeyParts {
+  int n;
+  float* sums;
+  __device__ __forceinline__ float* of(const PackedShape& p, int part, int which) const {
+    return sums + (int64_t)(part * 2 + which) * p.total_k * p.nkv * p.d;
+  }
+};
+// Parts for about `workgroups` in all, each with eight pairs of 64 queries on average or more.
+static inline int key_parts(const PackedShape& p, int workgroups) {
+  const int64_t tiles = (int64_t)packed_tiles(p.total_k, p.n_seq, 64) * p.nkv;
+  const int64_t pairs = (int64_t)(p.nq / p.nkv) * ((p.total_q / (p.n_seq > 0 ? p.n_seq : 1) + 63) / 64);
+  const int64_t n = workgroups / (tiles > 0 ? tiles : 1) < pairs / 8 ? workgroups / (tiles > 0 ? tiles : 1) : pairs / 8;
+  return n < 2 ? 1 : n < 32 ? (int)n : 32;
+}
+
 // bf16 on matrix instructions: head sizes in multiples of 8, 16-byte aligned rows, nothing beyond 2 GB in one tensor.  o and dout are
 // checked for their alignment alone (null: not in the call).
 bool attention_takes_mfma(const PackedShape& p, const void* q, const void* k, const void* v, const void* o, const void* dout);
@@ -73,4 +90,4 @@ void launch_attention_mfma_forward(hipStream_t s, const PackedShape& p, const bf
                                    float* lse);
 void launch_attention_mfma_backward(hipStream_t s, const PackedShape& p, const bf16_t* dout, const bf16_t* q, const bf16_t* k,
                                     const bf16_t* v, const bf16_t* o, const float* lse, bf16_t* dq, bf16_t* dk, bf16_t* dv,
-                                    float* stats);      // stats: 2 floats a query and head
+                                    float* stats, const KeyParts& parts);      // stats: 2 floats a query and head

@@ -197,7 +197,7 @@ std::tuple<Tensor, Tensor, Tensor> attention_backward(const Tensor& dout, const 
   const c10::DeviceGuard guard(q.device());
   const Tensor g = dout.contiguous(), oc = o.contiguous();
   Tensor dq = fresh(q.sizes(), q), dk = fresh(k.sizes(), q), dv = fresh(v.sizes(), q);
-  const int64_t n = rl_attention_workspace(p.total_q, p.nq);
+  const int64_t n = rl_attention_fast_workspace(p.n_seq, p.total_q, p.total_k, p.nq, p.nkv, p.d, p.dt);
   const Tensor ws = bytes(n, q);
   done(rl_attention_backward(g.data_ptr(), p.q.data_ptr(), p.q.stride(0), p.q.stride(1), p.k.data_ptr(), p.k.stride(0), p.k.stride(1),
                              p.v.data_ptr(), p.v.stride(0), p.v.stride(1), oc.data_ptr(), lse.data_ptr<float>(), cu_q.data_ptr<int32_t>(),

@@ -108,3 +108,12 @@ def test_operators_refuse_tensors_that_are_not_on_a_gpu(lib):
         assert e.value.code == -1
     table = ops.rotary_table(6, 8, theta=100.0, device="cpu")
     assert table.shape == (6, 4, 2) and np.allclose(table[5, 1], [math.cos(5 * 100 ** -0.25), math.sin(5 * 100 ** -0.25)])
+
+
+def test_the_larger_workspace_of_attention(lib):
+    least = lib.rl_attention_workspace(2000, 8)
+    assert lib.rl_attention_fast_workspace(1, 2000, 2000, 8, 1, 128, 1) >= least + 2 * 2 * 2000 * 128 * 4      # two parts at least
+    assert least <= lib.rl_attention_fast_workspace(1, 2000, 2000, 8, 8, 128, 1) < least + 2000 * 8 * 128 * 8 * 32
+    assert lib.rl_attention_fast_workspace(64, 100_000, 100_000, 32, 8, 128, 1) == lib.rl_attention_workspace(100_000, 32)      # 25.6 MB, a multiple of 256
+    assert lib.rl_attention_fast_workspace(1, 2000, 2000, 8, 3, 128, 1) == 0 and lib.rl_attention_fast_workspace(1, 10, 10, 8, 1, 129, 0) == 0
+    assert lib.rl_attention_fast_workspace(0, 0, 0, 8, 1, 64, 0) == 0

@@ -314,6 +314,23 @@ def test_attention_of_many_sequences(dt, n):
 
 
 @pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lq,lk,nq,nk,d", [([1100], None, 8, 1, 128), ([700, 0, 90, 333], None, 16, 2, 64), ([400, 260], [20, 900], 12, 1, 40),
+                                           ([513], None, 16, 1, 7)])
+def test_attention_of_few_kv_heads(dt, causal, lq, lk, nq, nk, d):
+    lk = lk or lq
+    g = gen(sum(lq) + d)
+    q, do = randn(g, sum(lq), nq, d, dt=dt), randn(g, sum(lq), nq, d, dt=dt)
+    k, v = randn(g, sum(lk), nk, d, dt=dt), randn(g, sum(lk), nk, d, dt=dt)
+    cq, ck = offsets(lq), offsets(lk)
+    o, lse = ops.attention_forward(q, k, v, cq, ck, causal=causal)
+    dq, dk, dv = ops.attention_backward(do, q, k, v, o, lse, cq, ck, causal=causal)
+    want, err = attention_reference(q, k, v, do, lq, lk, causal, d ** -0.5, dt, True)
+    for name, got in (("o", o), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        within(name, got, want[name], err[name])
+
+
+@pytest.mark.parametrize("dt", [BF, FP])
 @pytest.mark.parametrize("causal,d", [(True, 128), (False, 64)])
 def test_attention_with_a_negative_scale(dt, causal, d):
     lens, nq, nk = [150, 3, 260], 4, 2
