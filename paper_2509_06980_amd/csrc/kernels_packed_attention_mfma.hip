@@ -83,7 +83,7 @@ struct Stream {
       const int r = (j * 4 + wave) * ROWS + lane / PIECES, p8 = (lane % PIECES) ^ swizzle(r);
       off[j] = p8 * 8 < d ? (int)(r * stride * 2) + p8 * 16 : kFar;
     }
-    asm volatile("s_nop 4" ::: "memory");      // scalars from vector instructions, read by the loads
+    settle(rsrc);
   }
   static __device__ __forceinline__ int swizzle(int r) {
     return D == 128 ? ((r & 3) << 2) | (r >> 2 & 3) : ((r >> 1 & 1) << 2) | (r >> 2 & 3);
@@ -532,9 +532,9 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
     const bool some = h < (hk + 1) * group;
     const unsigned bytes = some ? full : 0u, sbytes = some ? (unsigned)lq * 4u : 0u;
     const int hd = some ? h : 0;
-    const u32x4 rsrc = buffer_rsrc(from + (int64_t)q0 * ts + (int64_t)hd * hs, bytes);
+    u32x4 rsrc = buffer_rsrc(from + (int64_t)q0 * ts + (int64_t)hd * hs, bytes);
     const u32x4 srsrc = buffer_rsrc(stats_from + (size_t)hd * p.total_q + q0, sbytes);
-    asm volatile("s_nop 4" ::: "memory");      // scalars from vector instructions, read by the loads below
+    settle(rsrc);
     const int i = first + item;
     int ln = lane;
     asm volatile("" : "+v"(ln));      // the offsets are formed anew: registers

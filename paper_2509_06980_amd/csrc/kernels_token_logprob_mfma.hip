@@ -129,7 +129,8 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
       rb = TB ? buffer_rsrc(P.b + t.j0, (unsigned)(((int64_t)P.b_n * P.ldb - t.j0) * EL))
               : buffer_rsrc(P.b + (int64_t)t.j0 * P.ldb, (unsigned)((int64_t)min(P.b_n - t.j0, BN) * P.ldb * EL));
       lc = t.c0, lend = t.c1;
-      asm volatile("s_nop 4" ::: "memory");      // scalars from vector instructions, read by the loads
+      settle(ra);
+      settle(rb);
       return;
     }
     lc = lend - 1;
@@ -209,7 +210,6 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
     if constexpr (EPI == EPI_STRIP || EPI == EPI_DZ) {      // what the epilogue needs of the wave's rows
       auto fetch = [&](const void* p, int which) {
         const u32x4 r = buffer_rsrc(p, (unsigned)P.a_n * 4u);
-        asm volatile("s_nop 4" ::: "memory");
 #pragma unroll
         for (int m = 0; m < ROWS; m++)
           load_dword_to_lds(lds0 + RING + (unsigned)(wave * ARRAYS + which) * (ROWS * 256u) + m * 256u, lane * 4, r, (unsigned)(i0 + wm * 32 * MB + m * 64) * 4u);
