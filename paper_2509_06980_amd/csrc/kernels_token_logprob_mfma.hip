@@ -126,8 +126,10 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
       if (t.c1 <= t.c0) continue;
       ra = TA ? buffer_rsrc(P.a + t.i0, (unsigned)(((int64_t)P.a_n * P.lda - t.i0) * EL))
               : buffer_rsrc(P.a + (int64_t)t.i0 * P.lda, (unsigned)((int64_t)min(P.a_n - t.i0, BM) * P.lda * EL));
+      // a tile of dz may begin behind the vocabulary (its columns go on to a multiple of 256): it reads the last row, and stores zeros
+      const int row = TB ? 0 : min(t.j0, P.b_n - 1);
       rb = TB ? buffer_rsrc(P.b + t.j0, (unsigned)(((int64_t)P.b_n * P.ldb - t.j0) * EL))
-              : buffer_rsrc(P.b + (int64_t)t.j0 * P.ldb, (unsigned)((int64_t)min(P.b_n - t.j0, BN) * P.ldb * EL));
+              : buffer_rsrc(P.b + (int64_t)row * P.ldb, (unsigned)((int64_t)min(P.b_n - row, BN) * P.ldb * EL));
       lc = t.c0, lend = t.c1;
       settle(ra);
       settle(rb);
