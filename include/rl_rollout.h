@@ -366,7 +366,8 @@ int rl_rotary(const void* d_q, void* d_q_out, int32_t n_q_heads, int64_t q_token
 /*
  * Attention over packed sequences with grouped heads: query head h reads KV head h / (n_q_heads / n_kv_heads).  Sequence s has the
  * queries d_cu_q[s] .. d_cu_q[s + 1] - 1 and the keys and values d_cu_k[s] .. d_cu_k[s + 1] - 1 (n_seq + 1 ascending offsets each,
- * on the device, from 0 to total_q and total_k; tokens of no sequence are left out).  Causal: query i of lq sees the keys
+ * on the device, within 0 .. total_q and 0 .. total_k).  Tokens before the first offset and from the last one on (padding) are of no sequence:
+ * they are not read, their o is 0, their lse -infinity, their gradients are 0.  Causal: query i of lq sees the keys
  * j <= i + lk - lq, so fewer queries than keys are the last ones of their sequence.  z = scale * q.k, d_lse[head][token] =
  * log(sum of e^z), o = sum of e^(z - lse) v.  A query that sees no key gets o = 0 and lse = -infinity, and no gradient.
  * head_dim at most 128.  o and all gradients are contiguous [tokens, heads, head_dim].

@@ -80,7 +80,9 @@ __global__ __launch_bounds__(256) void attention_rows_forward(PackedShape p, int
   f32(*ps)[16][BN + 4] = (f32(*)[16][BN + 4])(dynamic + BT * 2 * (D + PAD));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y, l16 = lane & 15, l4 = lane >> 4;
   const int mine = SPLIT == 1 ? wave * 16 : 0, part = SPLIT == 1 ? 0 : wave * BN;      // wave's rows, and its share of what is in LDS
+  const OutsideRows outside(p.cu_q, p.n_seq, p.total_q);
   const PackedTile t = packed_tile(p.cu_q, p.n_seq, p.total_q, BM, blockIdx.x);
+  outside.clear<T>(p.nq * p.d, o, nullptr, lse, p.nq);
   if (t.row0 >= t.len) return;
   const int k0 = packed_bound(p.cu_k, t.seq, p.total_k), lk = max(packed_bound(p.cu_k, t.seq + 1, p.total_k) - k0, 0);
   const int hk = h / (p.nq / p.nkv), shift = lk - t.len;
@@ -198,7 +200,9 @@ __global__ __launch_bounds__(256) void attention_rows_dq(PackedShape p, int vec,
   f32(*ds)[16][BN + 4] = (f32(*)[16][BN + 4])(dynamic + BT * 2 * (D + PAD));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.y, l16 = lane & 15, l4 = lane >> 4;
   const int own = SPLIT == 1 ? wave * 16 : 0, part = SPLIT == 1 ? 0 : wave * BN;
+  const OutsideRows outside(p.cu_q, p.n_seq, p.total_q);
   const PackedTile t = packed_tile(p.cu_q, p.n_seq, p.total_q, BM, blockIdx.x);
+  outside.clear<T>(p.nq * p.d, dq, nullptr, nullptr, 0);
   if (t.row0 >= t.len) return;
   const int k0 = packed_bound(p.cu_k, t.seq, p.total_k), lk = max(packed_bound(p.cu_k, t.seq + 1, p.total_k) - k0, 0);
   const int hk = h / (p.nq / p.nkv), shift = lk - t.len;
@@ -285,7 +289,9 @@ __global__ __launch_bounds__(256) void attention_rows_dkv(PackedShape p, int vec
   f32(*dt)[16][BN + 4] = pt + 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hk = blockIdx.y, l16 = lane & 15, l4 = lane >> 4;
   const int own = SPLIT == 1 ? wave * 16 : 0, part = SPLIT == 1 ? 0 : wave * BN;
+  const OutsideRows outside(p.cu_k, p.n_seq, p.total_k);
   const PackedTile t = packed_tile(p.cu_k, p.n_seq, p.total_k, BM, blockIdx.x);
+  outside.clear<T>(p.nkv * p.d, dk, dv, nullptr, 0);
   if (t.row0 >= t.len) return;
   const int q0 = packed_bound(p.cu_q, t.seq, p.total_q), lq = max(packed_bound(p.cu_q, t.seq + 1, p.total_q) - q0, 0);
   const int group = p.nq / p.nkv, shift = t.len - lq, mine = t.row0 + own + l16;

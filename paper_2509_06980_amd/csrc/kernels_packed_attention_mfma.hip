@@ -186,8 +186,11 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(PackedShape p
   constexpr int TILE = BN * D * 2;      // LDS: two tiles of keys, three of values
   extern __shared__ u32x4 smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const OutsideRows outside(p.cu_q, p.n_seq, p.total_q);
   QuerySide w;
-  if (!query_side(p, w)) return;
+  const bool some_rows = query_side(p, w);
+  outside.clear<bf16_t>(p.nq * p.d, o, nullptr, lse, p.nq);
+  if (!some_rows) return;
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
   Reads<D> lds((lds_char*)(__attribute__((address_space(3))) void*)smem, lane);      // of the keys, of the values in work
   lds.tr += 2 * TILE;
@@ -343,8 +346,11 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(PackedShape p, con
   constexpr int TILE = BN * D * 2, STAGE = 2 * TILE;
   extern __shared__ u32x4 smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const OutsideRows outside(p.cu_q, p.n_seq, p.total_q);
   QuerySide w;
-  if (!query_side(p, w)) return;
+  const bool some_rows = query_side(p, w);
+  outside.clear<bf16_t>(p.nq * p.d, dq, nullptr, nullptr, 0);
+  if (!some_rows) return;
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
   Reads<D> lds((lds_char*)(__attribute__((address_space(3))) void*)smem, lane);      // of the stage in work
   const int mine = w.t.row0 + wave * 32 + (lane & 31);
@@ -486,12 +492,14 @@ __global__ __launch_bounds__(512, 2) void attention_dkv_kernel(PackedShape p, co
   constexpr int S = D / 16, SLOTS = 4 * S, AHEAD = 3, VA = 2, PER = 16 / S;
   extern __shared__ u32x4 smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, block = wave % BLOCKS, stream = wave / BLOCKS;
+  const OutsideRows outside(p.cu_k, p.n_seq, p.total_k);
   const int hk = blockIdx.x % p.nkv, group = p.nq / p.nkv;
   // The tiles that most queries see first: a workgroup that begins last should not be the longest.  Measured, 16 sequences of 97 to 1511:
   // 171 us, in the order of the sequences 184; one sequence is in order as it is (562 us, counted through 569).
   const int tile = blockIdx.x / p.nkv;
   const PackedTile t = p.n_seq > 1 && p.n_seq <= 64 ? packed_tile_by_rest(p.cu_k, p.n_seq, p.total_k, KEYS, tile)
                                                     : packed_tile(p.cu_k, p.n_seq, p.total_k, KEYS, tile);
+  outside.clear<bf16_t>(p.nkv * p.d, dk, dv, nullptr, 0);
   if (t.row0 >= t.len) return;
   const int q0 = packed_bound(p.cu_q, t.seq, p.total_q), lq = max(packed_bound(p.cu_q, t.seq + 1, p.total_q) - q0, 0);
   const int shift = t.len - lq;

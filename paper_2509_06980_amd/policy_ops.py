@@ -77,12 +77,12 @@ def rotary(q, k, positions, table, interleaved=False, inverse=False, q_out=None,
 # ---- attention over packed trajectories ------------------------------------------------------------------------------
 def attention_forward(q, k, v, cu_q, cu_k, causal=True, scale=None):
     """Attention of packed sequences -> (o [tokens, heads, head_dim], lse [heads, tokens]); see rl_attention_forward.  Tokens of
-    no sequence keep what the new tensors happen to hold.  scale None: head_dim^-1/2."""
+    no sequence (padding before cu[0] and from cu[-1] on) get o = 0 and lse = -infinity.  scale None: head_dim^-1/2."""
     return _native.attention_forward(q, k, v, cu_q, cu_k, causal, scale, _stream(q))
 
 
 def attention_backward(do, q, k, v, o, lse, cu_q, cu_k, causal=True, scale=None):
-    """Gradients of attention_forward -> (dq, dk, dv), contiguous."""
+    """Gradients of attention_forward -> (dq, dk, dv), contiguous; those of tokens of no sequence are 0."""
     return _native.attention_backward(do, q, k, v, o, lse, cu_q, cu_k, causal, scale, _stream(q))
 
 

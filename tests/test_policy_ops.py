@@ -405,6 +405,54 @@ def test_attention_tokens_of_no_sequence_are_left_out():
         assert torch.equal(a[10:90], b)
 
 
+def _dirty():
+    """Memory that the allocator gives out next holds NaN."""
+    hold = [torch.full((n,), math.nan, device="cuda") for n in [1 << k for k in range(7, 25)] * 3]
+    del hold
+
+
+@pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lq,lk,lead,tail,nq,nk,d", [
+    # lengths; tokens of no sequence before the first and behind the last one, of the queries and of the keys
+    ([30, 50], None, (10, 10), (10, 10), 2, 2, 64), ([30, 50], [45, 60], (0, 7), (300, 0), 4, 2, 40), ([1, 70], None, (1, 1), (0, 129), 2, 1, 33),
+    ([1100], None, (3, 3), (200, 200), 8, 1, 128), ([0, 0], [0, 0], (2, 0), (3, 90), 4, 2, 128), ([40], [0], (0, 0), (0, 5), 2, 2, 64),
+    ([0], [40], (700, 0), (0, 1), 2, 2, 64), ([4100], None, (0, 0), (150, 150), 16, 16, 64), ([40, 3, 77] * 12, None, (5, 70), (70, 5), 16, 16, 64)])
+def test_attention_of_tokens_outside_all_sequences_is_nothing(lq, lk, lead, tail, nq, nk, d, causal, dt):
+    lk = lk or lq
+    g = gen(sum(lq) + d)
+    tq, tk = lead[0] + sum(lq) + tail[0], lead[1] + sum(lk) + tail[1]
+    iq, ik = slice(lead[0], lead[0] + sum(lq)), slice(lead[1], lead[1] + sum(lk))
+    q, k, v, do = (randn(g, n, h, d, dt=dt) for n, h in ((tq, nq), (tk, nk), (tk, nk), (tq, nq)))
+    want, err = attention_reference(q[iq], k[ik], v[ik], do[iq], lq, lk, causal, d ** -0.5, dt, True)
+    for t, inside in ((q, iq), (k, ik), (v, ik), (do, iq)):      # nothing outside is looked at
+        t[:inside.start], t[inside.stop:] = math.nan, math.nan
+    cq, ck = offsets(lq) + lead[0], offsets(lk) + lead[1]
+    _dirty()
+    o, lse = ops.attention_forward(q, k, v, cq, ck, causal=causal)
+    dq, dk, dv = ops.attention_backward(do, q, k, v, o, lse, cq, ck, causal=causal)
+    for name, got, inside, none in (("o", o, iq, 0.0), ("lse", lse.t(), iq, -math.inf), ("dq", dq, iq, 0.0), ("dk", dk, ik, 0.0), ("dv", dv, ik, 0.0)):
+        to = (lambda x: x.t()) if name == "lse" else (lambda x: x)
+        assert (got[:inside.start] == none).all() and (got[inside.stop:] == none).all(), name
+        within(name, to(got[inside]), want[name], err[name])
+
+
+@pytest.mark.parametrize("dt", [BF, FP])
+def test_gradients_of_a_padded_batch_reach_the_projections_whole(dt):
+    g = gen(12)
+    x, w = randn(g, 120, 96, dt=dt), (randn(g, 6 * 64, 96, dt=dt, std=0.1)).requires_grad_()
+    cu = torch.tensor([0, 30, 83], dtype=torch.int32, device="cuda")
+    grads = []
+    for n in (120, 83):      # with padding behind the sequences, and without
+        q, k, v = (x @ w.t())[:n].view(n, 6, 64).split([4, 1, 1], 1)
+        _dirty()
+        o = ops.attention(q, k, v, cu, cu)
+        w.grad = None
+        o[:83].float().square().sum().backward()
+        grads.append(w.grad)
+    assert torch.equal(*grads) and grads[0].any()
+
+
 # ---- log-probs -----------------------------------------------------------------------------------------------------
 def logprob_reference(h, w, y, g, temperature, dt):
     kept = y >= 0
