@@ -339,6 +339,7 @@ int rl_measure_stream_read(size_t bytes, int32_t iters, double* gb_per_s);
  * i * inner_stride (heads of a fused projection): n = (x - mean) * rstd, y = n * weight + bias, rstd = 1 / sqrt(mean((x - mean)^2) +
  * eps), mean = 0 in the RMS form.  d_bias may be NULL.  y: contiguous rows.  d_rstd, d_mean: one float per row, for the backward
  * call; d_mean is not used when centered = 0.
+ * At most 2^31 - 1 rows, of at most 2^27 - 32 elements.
  * Backward: d_dx [rows, width], d_dweight [width] and, unless NULL, d_dbias [width], from d_dy with strides of its own.
  */
 int rl_norm_forward(const void* d_x, int64_t outer, int32_t inner, int32_t width, int64_t outer_stride, int64_t inner_stride,
@@ -355,7 +356,7 @@ int rl_norm_backward(const void* d_dy, int64_t dy_outer_stride, int64_t dy_inner
  * interleaved; (a, b) becomes (a c - b s, b c + a s) with (c, s) = table[position][i]; elements from rot_dim on are copied.
  * inverse = 1 takes -s: the backward pass.  d_table: [n_positions][rot_dim / 2] pairs of floats (any scaling of the angles for long
  * contexts is in it).  d_positions: one per token; a token whose position is outside the table gets NaN in its rotated part.
- * d_k may be NULL with n_k_heads = 0.  Output may be the input itself.  head_dim at most 512.
+ * d_k may be NULL with n_k_heads = 0.  Output may be the input itself.  head_dim at most 512, tokens below 2^31.
  */
 int rl_rotary(const void* d_q, void* d_q_out, int32_t n_q_heads, int64_t q_token_stride, int64_t q_head_stride,
               int64_t q_out_token_stride, int64_t q_out_head_stride, const void* d_k, void* d_k_out, int32_t n_k_heads,
@@ -370,7 +371,7 @@ int rl_rotary(const void* d_q, void* d_q_out, int32_t n_q_heads, int64_t q_token
  * they are not read, their o is 0, their lse -infinity, their gradients are 0.  Causal: query i of lq sees the keys
  * j <= i + lk - lq, so fewer queries than keys are the last ones of their sequence.  z = scale * q.k, d_lse[head][token] =
  * log(sum of e^z), o = sum of e^(z - lse) v.  A query that sees no key gets o = 0 and lse = -infinity, and no gradient.
- * head_dim at most 128.  o and all gradients are contiguous [tokens, heads, head_dim].
+ * head_dim at most 128, tokens at most 2^30, n_seq + the larger token count / 64 below 2^24.  o and all gradients are contiguous [tokens, heads, head_dim].
  * Backward: from do, the forward call's inputs and its o and lse; probabilities are formed again.  In bf16 the probabilities and
  * the gradients of the scores are rounded to bf16 where they enter a matrix product.
  * A value that is no number or infinite can reach every query of its own sequence, even one that does not see it; never another.
@@ -396,7 +397,7 @@ int rl_attention_backward(const void* d_do, const void* d_q, int64_t q_token_str
  * Log-probs of target tokens from hidden rows (behind the final norm) and the lm-head, without keeping the logits: z = hidden W^T /
  * temperature, d_lse[row] = log(sum of e^z), d_logp[row] = z[target] - lse.  A row with a negative target (observation
  * tokens: Section 2.2, the loss mask of Section 2.3.2) takes no part: both are 0 and it costs nothing.  A target of `vocab` or above
- * gives NaN.  W: [vocab, hidden], contiguous.  temperature > 0.
+ * gives NaN.  W: [vocab, hidden], contiguous.  temperature > 0.  rows at most 2^24 - 256, hidden 65536, vocab 2^22.
  * Backward: d_dlogp[row] is the gradient of the objective by the row's log-prob; d_dhidden [rows, hidden] (0 for rows without target)
  * and d_dweight [vocab, hidden].  Rows with dlogp = 0 take no part either.  The logits are formed again, a piece of the vocabulary
  * at a time; their gradients are rounded to dtype where they enter the two products.  Workspace 256-byte aligned.

@@ -1,4 +1,5 @@
 // Attention over packed sequences, forward and backward: entry points, and the kernels for every type and layout.
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -466,6 +467,7 @@ const char* attention_argument(const PackedShape& p, int32_t dtype) {
   if (dtype != RL_DTYPE_F32 && dtype != RL_DTYPE_BF16) return "dtype is RL_DTYPE_F32 or RL_DTYPE_BF16";
   if (p.n_seq < 0 || p.n_seq > (1 << 24) || p.total_q < 0 || p.total_k < 0) return "sequences or tokens out of range";
   if (p.total_q > (1 << 30) || p.total_k > (1 << 30)) return "more than 2^30 tokens";
+  if (packed_tiles(std::max(p.total_q, p.total_k), p.n_seq, 64) > most_workgroups(256)) return "more sequences and tokens than a launch takes";
   if (p.nq < 1 || p.nkv < 1 || p.nq % p.nkv || p.nq > 4096) return "n_q_heads is a multiple of n_kv_heads, at most 4096";
   if (p.d < 1 || p.d > 128) return "head_dim is 1 to 128";
   if (!(p.scale == p.scale) || p.scale - p.scale != 0.f) return "scale is no finite number";

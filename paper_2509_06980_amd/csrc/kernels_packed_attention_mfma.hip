@@ -781,8 +781,8 @@ bool attention_takes_mfma(const PackedShape& p, const void* q, const void* k, co
   };
   // the backward pass divides by the scale
   return fabsf(p.scale) > 1e-30f && p.d % 8 == 0 && takes(q, p.qt, p.qh, p.total_q) && takes(k, p.kt, p.kh, p.total_k) && takes(v, p.vt, p.vh, p.total_k) &&
-         takes(o, p.ot, p.oh, p.total_q) && takes(dout, p.ot, p.oh, p.total_q) && (int64_t)packed_tiles(p.total_q, p.n_seq, BM) * p.nq < (1ll << 31) &&
-         (int64_t)packed_tiles(p.total_k, p.n_seq, 64) * p.nkv < (1ll << 31);
+         takes(o, p.ot, p.oh, p.total_q) && takes(dout, p.ot, p.oh, p.total_q) && (int64_t)packed_tiles(p.total_q, p.n_seq, BM) * p.nq <= most_workgroups(256) &&
+         (int64_t)packed_tiles(p.total_k, p.n_seq, 64) * p.nkv <= most_workgroups(512);
 }
 
 void launch_attention_mfma_forward(hipStream_t s, const PackedShape& p, const bf16_t* q, const bf16_t* k, const bf16_t* v, bf16_t* o,

@@ -1,5 +1,7 @@
 // Norms and rotary positions of packed rows, forward and backward (the policy update's form of them; a decode step has its own
 // inside its products and attention).
+#include <algorithm>
+
 #include "policy_common.h"
 
 namespace {
@@ -48,12 +50,12 @@ __device__ __forceinline__ float group_sum(float v, float* lds) {
 }
 
 template <typename T, int VEC, int L, int NV>
-__global__ __launch_bounds__(256) void norm_forward_kernel(const T* __restrict__ x, Rows rows, int width, const T* __restrict__ w,
+__global__ __launch_bounds__(256) void norm_forward_kernel(const T* __restrict__ x, Rows rows, int first, int width, const T* __restrict__ w,
                                                            const T* __restrict__ b, float eps, int centered, T* __restrict__ y,
                                                            float* __restrict__ mean_out, float* __restrict__ rstd_out) {
   __shared__ float lds[4];
   const int lane = threadIdx.x % L;
-  const int row = (int)blockIdx.x * (256 / L) + (L >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : threadIdx.x / L);
+  const int row = first + (int)blockIdx.x * (256 / L) + (L >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : threadIdx.x / L);
   const bool live = row < rows.n;      // groups without a row run along: their lanes take part in no other group's sums
   const T* xr = x + (live ? rows.at(row) : 0);
   T* yr = y + (int64_t)(live ? row : 0) * width;
@@ -392,8 +394,10 @@ int norm_forward(const void* x, const Rows& rows, int width, const void* w, cons
   const RowPlan p = row_plan(width, VEC);
   with_row_plan<VEC>(p, [&](auto l, auto v) {
     constexpr int L = decltype(l)::value, NV = decltype(v)::value;
-    norm_forward_kernel<T, VEC, L, NV><<<(unsigned)((rows.n - 1) / (256 / L) + 1), 256, 0, s>>>(
-        (const T*)x, rows, width, (const T*)w, (const T*)b, eps, centered, (T*)y, mean, rstd);
+    constexpr int64_t most = most_workgroups(256);
+    for (int64_t first = 0; first < rows.n; first += most * (256 / L))
+      norm_forward_kernel<T, VEC, L, NV><<<(unsigned)std::min(most, (rows.n - first - 1) / (256 / L) + 1), 256, 0, s>>>(
+          (const T*)x, rows, (int)first, width, (const T*)w, (const T*)b, eps, centered, (T*)y, mean, rstd);
   });
   return launched();
 }
@@ -416,8 +420,10 @@ int norm_backward(const void* dy, const Rows& drows, const void* x, const Rows& 
   return launched();
 }
 
+const int64_t kMostWidth = 32 * most_workgroups(1024);      // what the sums over rows launch for
 const char* norm_argument(const void* x, int64_t outer, int32_t inner, int32_t width, int32_t dtype) {
-  if (outer < 0 || inner < 1 || width < 1 || outer > 0x7fffffff / inner) return "outer, inner or width out of range (rows: below 2^31)";
+  if (outer < 0 || inner < 1 || width < 1 || outer > 0x7fffffff / inner || width > kMostWidth)
+    return "outer, inner or width out of range (rows: below 2^31, width: below 2^27 - 32)";
   if (dtype != RL_DTYPE_F32 && dtype != RL_DTYPE_BF16) return "dtype is RL_DTYPE_F32 or RL_DTYPE_BF16";
   if (outer > 0 && !x) return "null pointer";
   return nullptr;
@@ -445,7 +451,7 @@ extern "C" int rl_norm_forward(const void* d_x, int64_t outer, int32_t inner, in
 }
 
 extern "C" int64_t rl_norm_workspace(int64_t rows, int32_t width, int32_t biased) {
-  if (rows < 0 || width < 1) return 0;
+  if (rows < 0 || rows > 0x7fffffff || width < 1 || width > kMostWidth) return 0;
   const int64_t n = rows < kShares ? rows : kShares;      // as many shares as any plan makes
   return n * width * (biased ? 2 : 1) * (int64_t)sizeof(float);
 }
@@ -573,7 +579,16 @@ int rotary(const RotaryTensor& q, const RotaryTensor& k, int64_t tokens, const i
   constexpr int P = INTERLEAVED && VEC > 1 ? VEC / 2 : VEC;
   const int nc = rot_dim / 2 / P + (head_dim - rot_dim) / VEC, heads = q.heads + k.heads;
   const int hl = 256 / nc < 1 ? 1 : 256 / nc < heads ? 256 / nc : heads;
-  rotary_kernel<T, VEC, INTERLEAVED><<<(unsigned)tokens, dim3(nc, hl), 0, s>>>(q, k, positions, table, n_positions, rot_dim, head_dim, sign);
+  const int64_t most = most_workgroups(nc * hl);
+  auto from = [](const RotaryTensor& x, int64_t t) {      // tokens from t on; a null tensor has no heads
+    RotaryTensor y = x;
+    y.in = (const T*)x.in + t * x.it;
+    y.out = (T*)x.out + t * x.ot;
+    return y;
+  };
+  for (int64_t t = 0; t < tokens; t += most)
+    rotary_kernel<T, VEC, INTERLEAVED><<<(unsigned)std::min(most, tokens - t), dim3(nc, hl), 0, s>>>(from(q, t), from(k, t), positions + t, table,
+                                                                                                   n_positions, rot_dim, head_dim, sign);
   return launched();
 }
 

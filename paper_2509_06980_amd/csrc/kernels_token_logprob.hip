@@ -454,7 +454,7 @@ Workspace plan(int64_t rows, int hidden, int vocab, int dtype, bool backward) {
 
 const char* logprob_argument(int64_t rows, int32_t hidden, int32_t vocab, float temperature, int32_t dtype) {
   if (dtype != RL_DTYPE_F32 && dtype != RL_DTYPE_BF16) return "dtype is RL_DTYPE_F32 or RL_DTYPE_BF16";
-  if (rows < 0 || rows > (1 << 24) || hidden < 1 || hidden > 65536 || vocab < 1 || vocab > (1 << 22)) return "rows, hidden or vocab out of range";
+  if (rows < 0 || up(rows, kRowPad) > most_workgroups(256) || hidden < 1 || hidden > 65536 || vocab < 1 || vocab > (1 << 22)) return "rows, hidden or vocab out of range";
   if (!(temperature > 0.f) || temperature - temperature != 0.f || !(1.f / temperature <= 3.4e38f))
     return "temperature is a positive finite number with a finite reciprocal";
   return nullptr;

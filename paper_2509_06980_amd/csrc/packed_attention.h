@@ -107,7 +107,8 @@ static inline int key_parts(const PackedShape& p, int workgroups) {
   return n < 2 ? 1 : n < 32 ? (int)n : 32;
 }
 
-// bf16 on matrix instructions: head sizes in multiples of 8, 16-byte aligned rows, nothing beyond 2 GB in one tensor.  o and dout are
+// bf16 on matrix instructions: head sizes in multiples of 8, 16-byte aligned rows, nothing beyond 2 GB in one tensor, no more (tile, head) than
+// a launch takes (2^19 sequences of 32 heads; the other kernels have the heads in a dimension of their own).  o and dout are
 // checked for their alignment alone (null: not in the call).
 bool attention_takes_mfma(const PackedShape& p, const void* q, const void* k, const void* v, const void* o, const void* dout);
 void launch_attention_mfma_forward(hipStream_t s, const PackedShape& p, const bf16_t* q, const bf16_t* k, const bf16_t* v, bf16_t* o,

@@ -54,6 +54,9 @@ __device__ __forceinline__ void stv(bf16_t* p, const float (&v)[N]) {
 
 static inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 static inline int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+// Workgroups that one launch takes along a grid's first dimension: its threads are counted in 32 bits, and a launch of more runs some
+// of them and reports no error.
+constexpr int64_t most_workgroups(int threads) { return ((1ll << 32) - 1) / threads; }
 // What a C entry point returns after its launches.
 static inline int launched() {
   const hipError_t e = hipGetLastError();

@@ -117,3 +117,15 @@ def test_the_larger_workspace_of_attention(lib):
     assert lib.rl_attention_fast_workspace(64, 100_000, 100_000, 32, 8, 128, 1) == lib.rl_attention_workspace(100_000, 32)      # 25.6 MB, a multiple of 256
     assert lib.rl_attention_fast_workspace(1, 2000, 2000, 8, 3, 128, 1) == 0 and lib.rl_attention_fast_workspace(1, 10, 10, 8, 1, 129, 0) == 0
     assert lib.rl_attention_fast_workspace(0, 0, 0, 8, 1, 64, 0) == 0
+
+
+def test_sizes_that_no_launch_takes_are_refused(lib):
+    for call, changes in ((norm_forward, dict(width=(1 << 27) - 31)), (norm_backward, dict(width=(1 << 27) - 31, nbytes=1 << 50)), (attention_forward, dict(n=(1 << 24) - 4, tq=1 << 10)),
+                          (attention_forward, dict(n=1 << 24)), (attention_backward, dict(n=1 << 23, tk=1 << 30, nbytes=1 << 50)),
+                          (logprobs_forward, dict(rows=(1 << 24) - 255, nbytes=1 << 60)), (logprobs_backward, dict(rows=1 << 24, nbytes=1 << 60))):
+        assert call(lib, **changes) == -1 and b"workspace" not in lib.rl_last_error(), (call.__name__, changes)
+    # the largest that are taken
+    assert lib.rl_token_logprobs_workspace((1 << 24) - 256, 8, 9, F32, 1) > 0 and lib.rl_token_logprobs_workspace((1 << 24) - 255, 8, 9, F32, 1) == 0
+    assert lib.rl_attention_fast_workspace((1 << 24) - 17, 1 << 10, 1 << 10, 2, 1, 8, F32) > 0 and lib.rl_attention_fast_workspace((1 << 24) - 16, 1 << 10, 1 << 10, 2, 1, 8, F32) == 0
+    assert lib.rl_norm_workspace(1, (1 << 27) - 32, 0) > 0 and lib.rl_norm_workspace(1, (1 << 27) - 31, 0) == lib.rl_norm_workspace(1 << 31, 8, 0) == 0
+    assert norm_forward(lib, width=(1 << 27) - 32, outer=0) == 0

@@ -689,6 +689,44 @@ def test_the_same_bits_again_on_another_stream_and_in_a_graph(dt):
         assert all(torch.equal(a, b) for a, b in zip(first, run()))
 
 
+# ---- more than a launch takes ---------------------------------------------------------------------------------------
+# (fewer than 2^32 threads along a grid's first dimension; a launch of more runs some of them and reports no error)
+def test_norm_of_more_rows_than_a_launch_takes():
+    rows, width = (1 << 26) + 5, 33      # four rows a workgroup of 256
+    x = torch.empty(rows, width, dtype=BF, device="cuda").normal_(generator=gen(41))
+    w, b = randn(gen(42), width, dt=BF), randn(gen(43), width, dt=BF)
+    y, mean, rstd = ops.norm_forward(x, w, b, centered=True)
+    for at in (0, (1 << 25) - 3, (1 << 26) - 3, rows - 8):
+        part = ops.norm_forward(x[at:at + 8], w, b, centered=True)
+        assert all(torch.equal(a[at:at + 8], c) for a, c in zip((y, mean, rstd), part)), at
+
+
+def test_rotary_of_more_tokens_than_a_launch_takes():
+    tokens, d = (1 << 24) + 5, 257       # a workgroup of 256 a token
+    x = torch.empty(tokens, 1, d, dtype=BF, device="cuda").normal_(generator=gen(44))
+    table = ops.rotary_table(1000, 2)
+    pos = torch.arange(tokens, device="cuda", dtype=torch.int32) % 1000
+    places = [slice(at, at + 8) for at in (0, (1 << 23) - 3, (1 << 24) - 3, tokens - 8)]
+    want = [ops.rotary(x[p].clone(), None, pos[p], table)[0] for p in places]
+    ops.rotary(x, None, pos, table, q_out=x)
+    for p, c in zip(places, want):
+        assert torch.equal(x[p], c), p
+
+
+def test_attention_of_more_sequences_than_one_grid_takes():
+    n, nq, nk, d = 1 << 19, 32, 16, 8      # one token each: o = v, lse = scale q.k
+    g = gen(45)
+    q, k, v, do = randn(g, n, nq, d, dt=BF), randn(g, n, nk, d, dt=BF), randn(g, n, nk, d, dt=BF), randn(g, n, nq, d, dt=BF)
+    cu = torch.arange(n + 1, device="cuda", dtype=torch.int32)
+    o, lse = ops.attention_forward(q, k, v, cu, cu, scale=0.5)
+    assert torch.equal(o.view(n, nk, 2, d), v[:, :, None].expand(n, nk, 2, d))
+    assert torch.allclose(lse.t().view(n, nk, 2), 0.5 * (q.view(n, nk, 2, d).float() * k[:, :, None].float()).sum(-1), atol=1e-4, rtol=1e-5)
+    dq, dk, dv = ops.attention_backward(do, q, k, v, o, lse, cu, cu, scale=0.5)
+    # zero but for what 32 bits leave of dp - delta: 40 roundings of 8 products of values up to 6, times scale, key or queries
+    assert dq.abs().max() < 0.01 and dk.abs().max() < 0.01
+    assert torch.allclose(dv.float(), do.view(n, nk, 2, d).float().sum(2), atol=1e-3, rtol=2.0 ** -7)
+
+
 # ---- refusals ------------------------------------------------------------------------------------------------------
 def test_refusals():
     x, w = torch.ones(4, 2, 8, device="cuda"), torch.ones(8, device="cuda")
