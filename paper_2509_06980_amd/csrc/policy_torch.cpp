@@ -1,7 +1,9 @@
 // The policy update's operators on torch tensors: checks of the arguments, results and workspaces from torch's allocator, then the
 // calls of include/rl_rollout.h.  Host code only; small calls take as long as their launch, so it is compiled.
 #include <ATen/ATen.h>
+#include <ATen/MemoryOverlap.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/utils/pybind.h>
 
 #include <optional>
@@ -138,11 +140,17 @@ std::tuple<Tensor, Maybe> rotary(const Tensor& q, const Maybe& k, const Tensor& 
     if (!given) return fresh(x.sizes(), x);
     like(*given, q);
     check(given->sizes() == x.sizes() && rows_contiguous(*given), "an output has its input's shape and contiguous heads");
+    // written behind autograd's back: no gradient may be wanted of it, none of its elements may share memory
+    check(!(c10::GradMode::is_enabled() && given->requires_grad()), "an output that requires a gradient (use rotate)");
+    check(at::has_internal_overlap(*given) != at::MemOverlap::Yes, "elements of an output share memory");
     return *given;
   };
   const Tensor a = in(q), y = out(q, q_out);
   Tensor b, z;
   if (k) b = in(*k), z = out(*k, k_out);
+  // whoever kept the old contents for a backward pass is told
+  for (const Maybe& given : {q_out, k ? k_out : Maybe()})
+    if (given) given->unsafeGetTensorImpl()->bump_version();
   auto stride = [](const Tensor& x, int i) { return x.defined() ? x.stride(i) : 0; };
   if (a.size(1) > 0)
     done(rl_rotary(a.data_ptr(), y.data_ptr(), small(a.size(1), "too many heads"), a.stride(0), a.stride(1), y.stride(0), y.stride(1),

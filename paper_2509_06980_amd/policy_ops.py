@@ -70,7 +70,8 @@ def rotary_table(n_positions, rot_dim, theta=10000.0, stretch=1.0, trained_posit
 
 def rotary(q, k, positions, table, interleaved=False, inverse=False, q_out=None, k_out=None):
     """Turn the heads of q [tokens, heads, head_dim] and k (or None) by their positions -> (q, k); `inverse`: the backward pass.
-    Results are new contiguous tensors unless q_out / k_out say where (they may be q and k themselves)."""
+    Results are new contiguous tensors unless q_out / k_out say where (they may be q and k themselves, but lie over no other part of them);
+    autograd sees these as changed in place, and one that requires a gradient is refused."""
     return _native.rotary(q, k, positions, table, interleaved, inverse, q_out, k_out, _stream(q))
 
 

@@ -198,6 +198,29 @@ def test_rotary_table_rules():
     assert torch.equal(plain.cpu(), torch.stack([want.cos(), want.sin()], -1).float()) or torch.allclose(plain.cpu().double(), torch.stack([want.cos(), want.sin()], -1), atol=2e-7)
 
 
+def test_rotary_outputs_are_known_to_autograd():
+    g = gen(14)
+    table, pos = ops.rotary_table(50, 64), torch.arange(9, device="cuda", dtype=torch.int32)
+    x, k = randn(g, 9, 4, 64), randn(g, 9, 2, 64)
+    y, z = x.clone(), k.clone()
+    a = torch.ones_like(x).requires_grad_()
+    product = (a * y).sum()      # keeps y for its gradient
+    before = y._version, z._version
+    ops.rotary(y, z, pos, table, q_out=y, k_out=z)
+    assert y._version > before[0] and z._version > before[1]
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        product.backward()
+    # an output that a gradient is wanted of, and one whose elements share memory
+    for bad in (dict(q_out=x.clone().requires_grad_()), dict(k_out=k.clone().requires_grad_()), dict(q_out=(x.clone().requires_grad_() * 1)),
+                dict(q_out=x[:, :1].expand(9, 4, 64)), dict(k_out=k[:1].expand(9, 2, 64))):
+        with pytest.raises(RolloutError):
+            ops.rotary(x, k, pos, table, **bad)
+    leaf = x.clone().requires_grad_()
+    with torch.no_grad():
+        ops.rotary(x, None, pos, table, q_out=leaf)
+    assert torch.equal(leaf, y)
+
+
 # ---- attention -----------------------------------------------------------------------------------------------------
 def attention_reference(q, k, v, do, lq, lk, causal, scale, dt, mfma):
     """(results, bounds) in float64; `mfma`: probabilities and score gradients are rounded to bf16 on their way."""
