@@ -35,6 +35,14 @@ def _tensors(c):
     return names if c.tie_embeddings else names + [("lm_head", (c.vocab, c.hidden))]
 
 
+def _lengths(lens, total, least):
+    """lens as a list of numbers, `least` or more each, that add up to `total`."""
+    lens = [int(n) for n in torch.as_tensor(lens).tolist()]
+    if not lens or min(lens) < least or sum(lens) != total:
+        raise ValueError("lens are the lengths of " + ("non-empty " if least else "") + "packed trajectories, together all of their tokens")
+    return lens
+
+
 class PolicyModel:
     """The engine's decoder as torch parameters, from and to its weight blob."""
 
@@ -69,10 +77,22 @@ class PolicyModel:
         parts = [self.header] + [p.detach().reshape(-1).view(torch.uint8).cpu().numpy() for p in self.params.values()]
         return np.concatenate(parts)
 
+    def _in_vocabulary(self, tokens):
+        """Refuses other tokens: looked up on a GPU, one would end the process.  Waits for tokens that are on one."""
+        if tokens.numel():
+            low, high = torch.aminmax(tokens)
+            if low < 0 or high >= self.config.vocab:
+                raise ValueError(f"tokens outside the vocabulary of {self.config.vocab}")
+
     def hidden(self, tokens, lens):
         """Rows behind the final norm [tokens, hidden] of packed trajectories; residual stream and norms in 32 bits."""
+        lens = _lengths(lens, tokens.shape[0], 1)
+        self._in_vocabulary(tokens)
+        return self._rows(tokens, lens)
+
+    def _rows(self, tokens, lens):
         c, p = self.config, self.params
-        total, longest = int(sum(lens)), int(max(lens))
+        total, longest = sum(lens), max(lens)
         offsets = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
         cu = torch.from_numpy(offsets).to(self.device)
         positions = (torch.arange(total, device=self.device, dtype=torch.int32)
@@ -102,17 +122,19 @@ class PolicyModel:
     def logprobs(self, tokens, obs_mask, lens, temperature=1.0):
         """Differentiable rl_recompute_logprobs: one float32 a token of the packed trajectories, the log-prob of a sampled token
         given all before it, 0 for appended tokens and first ones.  tokens, obs_mask: integers on any device; lens: per trajectory."""
-        lens = [int(n) for n in lens]
-        tokens = torch.as_tensor(np.asarray(tokens), device=self.device).long()
+        tokens = torch.as_tensor(np.asarray(tokens))
         sampled = torch.as_tensor(np.asarray(obs_mask), device=self.device) == 0
-        if not lens or min(lens) < 1 or sum(lens) != tokens.shape[0] or sampled.shape != tokens.shape:
-            raise ValueError("lens are the lengths of non-empty packed trajectories, one mask a token")
+        if tokens.dim() != 1 or sampled.shape != tokens.shape:
+            raise ValueError("one token id and one mask a token")
+        lens = _lengths(lens, tokens.shape[0], 1)
+        self._in_vocabulary(tokens)
+        tokens = tokens.to(self.device).long()
         first = torch.zeros_like(sampled)
         first[torch.as_tensor(np.concatenate([[0], np.cumsum(lens)[:-1]]), device=self.device)] = True
         target = torch.where(sampled & ~first, tokens, -1).int()      # of the row before
         head = self.params["embed" if self.config.tie_embeddings else "lm_head"]
         temperature = 1.0 if temperature == 0 else float(temperature)
-        lp = ops.token_logprobs(self.hidden(tokens, lens), head, torch.cat([target[1:], target.new_full((1,), -1)]), temperature)
+        lp = ops.token_logprobs(self._rows(tokens, lens), head, torch.cat([target[1:], target.new_full((1,), -1)]), temperature)
         return torch.cat([lp.new_zeros(1), lp[:-1]])
 
 
@@ -124,19 +146,23 @@ def group_advantages(rewards, group_size, eps_std=1e-6, std_ddof=0):
 
 def grpo_objective(logprobs, old_logprobs, obs_mask, lens, advantages, clip_eps, beta=0.0, ref_logprobs=None):
     """The masked GRPO objective of rl_grpo_objective, differentiable by `logprobs` (all arrays packed, one value a token): mean
-    over trajectories of the mean over their sampled tokens of min(rho A, clip(rho) A) - beta k3."""
-    dev = logprobs.device
-    lens = torch.as_tensor(lens, device=dev)
-    which = torch.repeat_interleave(torch.arange(len(lens), device=dev), lens)
+    over trajectories of the mean over their sampled tokens (0 of one that has none) of min(rho A, clip(rho) A) - beta k3."""
+    dev, total = logprobs.device, logprobs.shape[0]
+    counts = _lengths(lens, total, 0)
+    lens = torch.as_tensor(counts, device=dev)
     used = torch.as_tensor(np.asarray(obs_mask), device=dev) == 0
-    used[torch.cumsum(lens, 0) - lens] = False      # a first token has no log-prob
-    lp = logprobs[used].double()
-    old = torch.as_tensor(np.asarray(old_logprobs), device=dev).double()[used]
-    a = torch.as_tensor(advantages, device=dev).double()[which[used]]
+    old = torch.as_tensor(np.asarray(old_logprobs), device=dev).double()
+    a = torch.as_tensor(advantages, device=dev).double()
+    ref = None if ref_logprobs is None else torch.as_tensor(np.asarray(ref_logprobs), device=dev).double()
+    if any(x is not None and x.shape != logprobs.shape for x in (used, old, ref)) or a.shape != lens.shape:
+        raise ValueError("one mask and log-prob a token, one advantage a trajectory")
+    which = torch.repeat_interleave(torch.arange(len(lens), device=dev), lens, output_size=total)
+    used[(torch.cumsum(lens, 0) - lens)[lens > 0]] = False      # a first token has no log-prob
+    lp, old, a = logprobs[used].double(), old[used], a[which[used]]
     rho = (lp - old).exp()
     term = torch.minimum(rho * a, rho.clamp(1 - clip_eps, 1 + clip_eps) * a)
-    if ref_logprobs is not None:
-        d = torch.as_tensor(np.asarray(ref_logprobs), device=dev).double()[used] - lp
+    if ref is not None:
+        d = ref[used] - lp
         term = term - beta * (d.exp() - d - 1)
     count = torch.zeros(len(lens), dtype=torch.float64, device=dev).index_add_(0, which[used], torch.ones_like(term))
     return (term / count[which[used]]).sum() / len(lens)
