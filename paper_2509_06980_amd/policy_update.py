@@ -37,10 +37,15 @@ def _tensors(c):
 
 def _lengths(lens, total, least):
     """lens as a list of numbers, `least` or more each, that add up to `total`."""
-    lens = [int(n) for n in torch.as_tensor(lens).tolist()]
+    lens = [int(n) for n in _tensor(lens).tolist()]
     if not lens or min(lens) < least or sum(lens) != total:
         raise ValueError("lens are the lengths of " + ("non-empty " if least else "") + "packed trajectories, together all of their tokens")
     return lens
+
+
+def _tensor(x, device=None):
+    """x as a tensor on `device` (None: where it is)."""
+    return torch.as_tensor(x if isinstance(x, torch.Tensor) else np.asarray(x), device=device)
 
 
 class PolicyModel:
@@ -122,8 +127,8 @@ class PolicyModel:
     def logprobs(self, tokens, obs_mask, lens, temperature=1.0):
         """Differentiable rl_recompute_logprobs: one float32 a token of the packed trajectories, the log-prob of a sampled token
         given all before it, 0 for appended tokens and first ones.  tokens, obs_mask: integers on any device; lens: per trajectory."""
-        tokens = torch.as_tensor(np.asarray(tokens))
-        sampled = torch.as_tensor(np.asarray(obs_mask), device=self.device) == 0
+        tokens = _tensor(tokens)
+        sampled = _tensor(obs_mask, self.device) == 0
         if tokens.dim() != 1 or sampled.shape != tokens.shape:
             raise ValueError("one token id and one mask a token")
         lens = _lengths(lens, tokens.shape[0], 1)
@@ -145,15 +150,15 @@ def group_advantages(rewards, group_size, eps_std=1e-6, std_ddof=0):
 
 
 def grpo_objective(logprobs, old_logprobs, obs_mask, lens, advantages, clip_eps, beta=0.0, ref_logprobs=None):
-    """The masked GRPO objective of rl_grpo_objective, differentiable by `logprobs` (all arrays packed, one value a token): mean
+    """The masked GRPO objective of rl_grpo_objective, differentiable by `logprobs` (all arrays packed, one value a token, on any device): mean
     over trajectories of the mean over their sampled tokens (0 of one that has none) of min(rho A, clip(rho) A) - beta k3."""
     dev, total = logprobs.device, logprobs.shape[0]
     counts = _lengths(lens, total, 0)
     lens = torch.as_tensor(counts, device=dev)
-    used = torch.as_tensor(np.asarray(obs_mask), device=dev) == 0
-    old = torch.as_tensor(np.asarray(old_logprobs), device=dev).double()
-    a = torch.as_tensor(advantages, device=dev).double()
-    ref = None if ref_logprobs is None else torch.as_tensor(np.asarray(ref_logprobs), device=dev).double()
+    used = _tensor(obs_mask, dev) == 0
+    old = _tensor(old_logprobs, dev).double()
+    a = _tensor(advantages, dev).double()
+    ref = None if ref_logprobs is None else _tensor(ref_logprobs, dev).double()
     if any(x is not None and x.shape != logprobs.shape for x in (used, old, ref)) or a.shape != lens.shape:
         raise ValueError("one mask and log-prob a token, one advantage a trajectory")
     which = torch.repeat_interleave(torch.arange(len(lens), device=dev), lens, output_size=total)

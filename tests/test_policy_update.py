@@ -157,3 +157,22 @@ def test_refuses_what_is_no_blob_or_no_batch():
     for tokens, mask, lens in (([1, 2], [0, 0], [1]), ([1, 2], [0], [2]), ([1, 2], [0, 0], [2, 0])):
         with pytest.raises(ValueError):
             model.logprobs(tokens, mask, lens)
+
+
+def test_trajectories_may_be_anywhere():
+    from paper_2509_06980_amd import policy_update as pu
+    blob = make_weight_blob(SMALL, seed=9, weight_std=0.05)
+    engine, ids = rollout(SMALL, blob)
+    model = pu.PolicyModel(blob)
+    tokens, mask, old, lens = pu.read_trajectories(engine, ids)
+    engine.close()
+    adv = pu.group_advantages(np.random.default_rng(1).random(len(ids)), 4)
+    lp = model.logprobs(tokens, mask, lens)
+    ref = old - 0.1
+    want = pu.grpo_objective(lp, old, mask, lens, adv, 0.2, 0.05, ref)
+    there = lambda x: torch.as_tensor(x, device="cuda")  # noqa: E731
+    for to in (there, torch.as_tensor, list):
+        assert torch.equal(model.logprobs(to(tokens), to(mask), to(lens)), lp)
+        assert torch.equal(pu.grpo_objective(lp, to(old), to(mask), to(lens), to(adv), 0.2, 0.05, to(ref)), want)
+    # a reference policy's own log-probs, as they come
+    assert torch.equal(pu.grpo_objective(lp, there(old), mask, lens, adv, 0.2, 0.05, lp.detach()), pu.grpo_objective(lp, old, mask, lens, adv, 0.2))
