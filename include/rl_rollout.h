@@ -410,6 +410,12 @@ int rl_token_logprobs_backward(const float* d_dlogp, const void* d_hidden, int64
                                const void* d_weight, int32_t vocab, const int32_t* d_targets, const float* d_lse,
                                float temperature, int32_t dtype, void* d_dhidden, void* d_dweight, void* d_workspace,
                                int64_t workspace_bytes, void* stream);
+/*
+ * Memory accesses of these calls' products (kernels of 16-byte rows) with `kept` of the rows taking part: host arithmetic only, for tests.
+ * out: by how many bytes the buffers of their loads reach beyond the operands, the loads' scalar offsets beyond those buffers, and
+ * their stores beyond the results (0: nowhere).  Errors: ARG (also a size that these kernels do not take).
+ */
+int rl_debug_token_logprob_loads(int32_t rows, int32_t kept, int32_t hidden, int32_t vocab, int32_t dtype, int32_t backward, int64_t* out);
 
 #ifdef __cplusplus
 }

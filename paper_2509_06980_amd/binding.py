@@ -17,6 +17,7 @@ EXPORTED_SYMBOLS = [
     "rl_norm_forward", "rl_norm_workspace", "rl_norm_backward", "rl_rotary", "rl_attention_forward", "rl_attention_workspace",
     "rl_attention_fast_workspace",
     "rl_attention_backward", "rl_token_logprobs_workspace", "rl_token_logprobs_forward", "rl_token_logprobs_backward",
+    "rl_debug_token_logprob_loads",
 ]
 
 
@@ -108,6 +109,7 @@ def load_library():
     lib.rl_attention_backward.argtypes = [p, p, l, l, p, l, l, p, l, l, p, p, p, p, i, i, i, i, i, i, f, i, i, p, p, p, p, l, p]
     lib.rl_token_logprobs_forward.argtypes = [p, l, i, i, p, i, p, f, i, p, p, p, l, p]
     lib.rl_token_logprobs_backward.argtypes = [p, p, l, i, i, p, i, p, p, f, i, p, p, p, l, p]
+    lib.rl_debug_token_logprob_loads.argtypes = [i, i, i, i, i, i, C.POINTER(C.c_int64)]
     for name, args in (("rl_norm_workspace", [l, i, i]), ("rl_attention_workspace", [i, i]), ("rl_attention_fast_workspace", [i] * 7),
                        ("rl_token_logprobs_workspace", [i, i, i, i, i])):
         getattr(lib, name).argtypes = args
@@ -167,6 +169,14 @@ def debug_many_row_loads(rows, n, k, plan):
     out = (C.c_int64 * 3)()
     _check(load_library().rl_debug_many_row_loads(int(rows), int(n), int(k), _GEMM_KERNELS.index(kernel), int(width), int(slices),
                                                   {v: k for k, v in _GEMM_EPILOGUES.items()}[epilogue], out))
+    return tuple(out)
+
+
+def debug_token_logprob_loads(rows, kept, hidden, vocab, bf16, backward):
+    """Bytes that the log-prob products' load buffers reach beyond their operands, their scalar offsets beyond the buffers and their stores
+    beyond the results."""
+    out = (C.c_int64 * 3)()
+    _check(load_library().rl_debug_token_logprob_loads(int(rows), int(kept), int(hidden), int(vocab), int(bool(bf16)), int(bool(backward)), out))
     return tuple(out)
 
 

@@ -81,7 +81,7 @@ __device__ __forceinline__ int scan_rows(const RowScan& s, bool write, int wante
     if (s.g) {
       const int n = choose_slices(s.rule, all);
       s.count[1] = n;
-      s.count[2] = ((s.rule.width + n - 1) / n + 63) / 64 * 64;
+      s.count[2] = slice_width(s.rule, n);
     }
   }
   return done;
@@ -592,4 +592,21 @@ extern "C" int rl_token_logprobs_backward(const float* d_dlogp, const void* d_hi
               (char*)d_workspace, (hipStream_t)stream)
   return dtype == RL_DTYPE_F32 ? RL_GO(float) : RL_GO(bf16_t);
 #undef RL_GO
+}
+
+extern "C" int rl_debug_token_logprob_loads(int32_t rows, int32_t kept, int32_t hidden, int32_t vocab, int32_t dtype, int32_t backward,
+                                            int64_t* out) {
+  if (!out || rows < 1 || kept < 0 || kept > rows) return rl_fail(RL_E_ARG, "bad argument");
+  if (const char* m = logprob_argument(rows, hidden, vocab, 1.f, dtype)) return rl_fail(RL_E_ARG, m);
+  const Workspace w = plan(rows, hidden, vocab, dtype, backward != 0);
+  const bool bf16 = dtype == RL_DTYPE_BF16;
+  const int twins = backward ? twins_of(rows, bf16) : 0, all = twins && kept ? 2 * twins : kept;
+  if (!(bf16 ? token_logprob_takes_mfma<bf16_t>(w.padded, w.ld, hidden, w.ldz, nullptr, nullptr)
+             : token_logprob_takes_mfma<float>(w.padded, w.ld, hidden, w.ldz, nullptr, nullptr)))
+    return rl_fail(RL_E_ARG, "a size that other kernels take");
+  const int slices = backward ? choose_slices(w.slices, all) : 1;
+  const LogprobSizes n{rows, all, hidden, vocab, backward, w.padded, w.ld, w.strips, w.width, w.ldz, w.slices.most, slices, backward ? slice_width(w.slices, slices) : 0};
+  const LoadOverreach most = bf16 ? token_logprob_overreach<bf16_t>(n) : token_logprob_overreach<float>(n);
+  out[0] = most.buffers, out[1] = most.offsets, out[2] = most.stores;
+  return RL_OK;
 }

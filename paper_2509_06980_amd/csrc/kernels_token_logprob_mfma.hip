@@ -60,6 +60,30 @@ struct Product {
   int out_rows, out_cols, first;
 };
 
+// What a tile's loads of one operand may reach, from element `begin` on: its rows (k-contiguous), or all of the operand behind its
+// first column (k-strided).  Scalar offsets have to stay inside: the hardware compares a lane's offset with the size less the scalar one.
+struct Reach {
+  int64_t begin;
+  unsigned bytes;
+};
+// The operand has n rows of ld elements, the tile begins at row (k-strided: column) `at` and has `rows` of them.  A tile of dz may begin behind
+// the vocabulary (its columns go on to a multiple of 256): it reads the last row, and stores zeros.
+template <typename T>
+__host__ __device__ __forceinline__ Reach reach_of(bool strided, int64_t ld, int n, int at, int rows) {
+  if (strided) return {at, (unsigned)((n * ld - at) * (int64_t)sizeof(T))};
+  const int first = at < n ? at : n - 1, left = n - first;
+  return {first * ld, (unsigned)((left < rows ? left : rows) * ld * (int64_t)sizeof(T))};
+}
+// Scalar offset of chunk c: that many times a chunk's step
+__host__ __device__ __forceinline__ unsigned chunk_step(bool strided, int64_t ld) { return strided ? (unsigned)ld * 64u : 64u; }
+// Chunks [first, end) of a slice of k
+template <typename T>
+__host__ __device__ __forceinline__ void chunks_of(int slice, int per_slice, int k_all, int& first, int& end) {
+  constexpr int KC = 64 / sizeof(T);
+  const int lo = slice * per_slice, hi = k_all < lo + per_slice ? k_all : lo + per_slice;
+  first = lo / KC, end = (hi + KC - 1) / KC;
+}
+
 // LDS of a workgroup: the ring of stages, behind it what an epilogue takes, so that it does not touch the next tile's chunks
 template <typename T, int MB, int NB, int R, int EPI>
 struct Lds {
@@ -95,11 +119,10 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
     t.i0 = __builtin_amdgcn_readfirstlane(first + in % gm) * BM;
     t.j0 = __builtin_amdgcn_readfirstlane(in / gm) * BN;
     t.z = __builtin_amdgcn_readfirstlane(slice);
-    const int k_lo = t.z * per_slice;
-    t.c0 = k_lo / KC, t.c1 = (min(k_all, k_lo + per_slice) + KC - 1) / KC;
+    chunks_of<T>(t.z, per_slice, k_all, t.c0, t.c1);
     return t;
   };
-  const unsigned sa = TA ? (unsigned)P.lda * 64u : 64u, sb = TB ? (unsigned)P.ldb * 64u : 64u;      // bytes of a chunk's step
+  const unsigned sa = chunk_step(TA, P.lda), sb = chunk_step(TB, P.ldb);
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
   int va[MB], vb[NB];      // this lane's offset of each piece that its wave loads
   auto offset = [&](int piece, int64_t ld, bool strided, int row_bytes) {
@@ -124,12 +147,9 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Produ
     for (at += gridDim.x; at < total; at += gridDim.x) {
       const Place t = place(at);
       if (t.c1 <= t.c0) continue;
-      ra = TA ? buffer_rsrc(P.a + t.i0, (unsigned)(((int64_t)P.a_n * P.lda - t.i0) * EL))
-              : buffer_rsrc(P.a + (int64_t)t.i0 * P.lda, (unsigned)((int64_t)min(P.a_n - t.i0, BM) * P.lda * EL));
-      // a tile of dz may begin behind the vocabulary (its columns go on to a multiple of 256): it reads the last row, and stores zeros
-      const int row = TB ? 0 : min(t.j0, P.b_n - 1);
-      rb = TB ? buffer_rsrc(P.b + t.j0, (unsigned)(((int64_t)P.b_n * P.ldb - t.j0) * EL))
-              : buffer_rsrc(P.b + (int64_t)row * P.ldb, (unsigned)((int64_t)min(P.b_n - row, BN) * P.ldb * EL));
+      const Reach a = reach_of<T>(TA, P.lda, P.a_n, t.i0, BM), b = reach_of<T>(TB, P.ldb, P.b_n, t.j0, BN);
+      ra = buffer_rsrc(P.a + a.begin, a.bytes);
+      rb = buffer_rsrc(P.b + b.begin, b.bytes);
       lc = t.c0, lend = t.c1;
       settle(ra);
       settle(rb);
@@ -448,9 +468,19 @@ template <typename T>
 int64_t slices_in(int width) {
   return sizeof(T) == 2 ? std::min(std::max(width / 2048, 1), 64) : 16;
 }
+// A product of rows x columns with its tiles
+template <typename T>
+struct Planned {
+  Product<T> p;
+  Tile t;
+  Planned(const Product<T>& product, const Tile& tile, int64_t rows, int64_t columns) : p(product), t(tile) {
+    p.tiles_i = (int)((rows + 64 * t.mb - 1) / (64 * t.mb)), p.tiles_j = (int)((columns + 64 * t.nb - 1) / (64 * t.nb));
+  }
+};
 template <typename T, bool TA, bool TB, int EPI>
-void go(Product<T>& p, const Tile& t, int64_t rows, int64_t columns, hipStream_t s) {
-  p.tiles_i = (int)((rows + 64 * t.mb - 1) / (64 * t.mb)), p.tiles_j = (int)((columns + 64 * t.nb - 1) / (64 * t.nb));
+void go(const Planned<T>& planned, hipStream_t s) {
+  const Product<T>& p = planned.p;
+  const Tile& t = planned.t;
   if constexpr (sizeof(T) == 2) {
     if (t.nb == 2) return go<T, TA, TB, 2, 2, 6, EPI>(p, s);
     if constexpr (!TA) {
@@ -483,23 +513,22 @@ void token_logprob_slice_tile(int rows, int hidden, int width, SliceRule& r) {
   r.chunk_us = sizeof(T) == 2 ? (t.mb == 4 ? 0.6f : t.nb == 4 ? 0.35f : 0.2f) : t.mb == 2 ? 2.4f : 0.6f;
 }
 
+namespace {
+
 template <typename T>
-int launch_logits_strips_mfma(hipStream_t s, const T* h, int ld, int rows, int64_t padded, const T* w, int vocab, int hidden,
-                              const KeptRows& kept, float inv_t, float2* part, float* zt) {
+Planned<T> logits_strips(const T* h, int ld, int rows, int64_t padded, const T* w, int vocab, int hidden, const KeptRows& kept, float inv_t,
+                         float2* part, float* zt) {
   Product<T> p{};
   p.a = h, p.lda = ld, p.a_n = (int)padded;
   p.b = w, p.ldb = hidden, p.b_n = vocab;
   p.k = hidden, p.slices = 1, p.group = 4;
   p.kept = kept, p.vocab = vocab, p.v0 = 0, p.scale = (float)(1.4426950408889634 * inv_t), p.inv_t = inv_t;
   p.part = part, p.padded = (int)padded, p.zt = zt;
-  const Tile t = tile_of<T>(rows, vocab, 1, true);
-  go<T, false, false, EPI_STRIP>(p, t, rows, vocab, s);
-  return p.tiles_j;
+  return {p, tile_of<T>(rows, vocab, 1, true), rows, vocab};
 }
-
 template <typename T>
-void launch_logits_gradient_mfma(hipStream_t s, const T* h, int ld, int rows, int64_t padded, const T* w, int vocab, int hidden,
-                                 const KeptRows& kept, float inv_t, const VocabPiece& piece, T* dz) {
+Planned<T> logits_gradient(const T* h, int ld, int rows, int64_t padded, const T* w, int vocab, int hidden, const KeptRows& kept, float inv_t,
+                           const VocabPiece& piece, T* dz) {
   Product<T> p{};
   p.a = h, p.lda = ld, p.a_n = (int)padded;
   p.b = w + (int64_t)piece.v0 * hidden, p.ldb = hidden, p.b_n = vocab - piece.v0;
@@ -507,33 +536,116 @@ void launch_logits_gradient_mfma(hipStream_t s, const T* h, int ld, int rows, in
   p.kept = kept, p.vocab = vocab, p.v0 = piece.v0, p.scale = (float)(1.4426950408889634 * inv_t), p.inv_t = inv_t;
   p.out = dz, p.ldo = piece.ld, p.out_rows = (int)padded, p.out_cols = (int)up(piece.width, 256);
   // whole multiples of 256 columns: the products behind it read beyond the vocabulary's end
-  go<T, false, false, EPI_DZ>(p, tile_of<T>(rows, piece.width, 1, true), rows, p.out_cols, s);
+  return {p, tile_of<T>(rows, piece.width, 1, true), rows, p.out_cols};
 }
-
 template <typename T>
-void launch_hidden_gradient_mfma(hipStream_t s, const T* dz, const VocabPiece& piece, int rows, int64_t padded, const T* w, int vocab, int hidden,
-                                 const KeptRows& kept, int most_slices, float* dh, size_t slice_stride, bool first) {
+Planned<T> hidden_gradient(const T* dz, const VocabPiece& piece, int rows, int64_t padded, const T* w, int vocab, int hidden,
+                           const KeptRows& kept, int most_slices, float* dh, size_t slice_stride, bool first) {
   Product<T> p{};
   p.a = dz, p.lda = piece.ld, p.a_n = (int)padded;
   p.b = w + (int64_t)piece.v0 * hidden, p.ldb = hidden, p.b_n = std::min(piece.ld, vocab - piece.v0);
   p.k = piece.width, p.slices = most_slices, p.group = 4;
   p.kept = kept, p.slice = dh, p.slice_stride = slice_stride, p.ldo = hidden, p.out_cols = hidden, p.first = first;
-  go<T, false, true, EPI_SLICE>(p, tile_of<T>(rows, hidden, slices_in<T>(piece.ld - 128), true), rows, hidden, s);
+  return {p, tile_of<T>(rows, hidden, slices_in<T>(piece.ld - 128), true), rows, hidden};
 }
-
 template <typename T>
-void launch_weight_gradient_mfma(hipStream_t s, const T* dz, const VocabPiece& piece, const T* h, int ld, int64_t padded, int hidden,
-                                 const KeptRows& kept, T* dw) {
+Planned<T> weight_gradient(const T* dz, const VocabPiece& piece, const T* h, int ld, int64_t padded, int hidden, const KeptRows& kept, T* dw) {
   Product<T> p{};
   p.a = dz, p.lda = piece.ld, p.a_n = (int)padded;
   p.b = h, p.ldb = ld, p.b_n = (int)padded;
   p.k = 0, p.slices = 1, p.group = 4;
   p.kept = kept, p.out = dw + (int64_t)piece.v0 * hidden, p.ldo = hidden, p.out_rows = piece.width, p.out_cols = hidden;
-  go<T, true, true, EPI_OUT>(p, tile_of<T>(piece.width, hidden, 1, false), piece.width, hidden, s);
+  return {p, tile_of<T>(piece.width, hidden, 1, false), piece.width, hidden};
+}
+
+// How far the loads of a planned product reach beyond its operands and its stores beyond its results, with `kept` rows and `slices` of
+// per_slice k on the device: the kernel's own arithmetic over all of its tiles.
+template <typename T, bool TA, bool TB, int EPI>
+void find_overreach(const Planned<T>& planned, int kept, int slices, int per_slice, const Extent& a, const Extent& b, const Extent& out,
+                    LoadOverreach& most) {
+  const Product<T>& P = planned.p;
+  const int64_t el = sizeof(T), BM = 64 * planned.t.mb, BN = 64 * planned.t.nb;
+  const int ti = EPI == EPI_OUT ? P.tiles_i : std::min<int64_t>(P.tiles_i, (kept + BM - 1) / BM), k_all = EPI == EPI_OUT ? kept : P.k;
+  if (EPI != EPI_SLICE) slices = 1, per_slice = k_all;
+  auto operand = [&](bool strided, const T* p, int64_t ld, int n, int tiles, int64_t size, const Extent& in) {
+    for (int i = 0; i < tiles; i++) {
+      const Reach r = reach_of<T>(strided, ld, n, (int)(i * size), (int)size);
+      const int64_t at = ((int64_t)(uintptr_t)p - in.base) / el + r.begin;
+      most.buffers = std::max({most.buffers, -at * el, at * el + r.bytes - in.bytes});
+      for (int z = 0; z < slices; z++) {
+        int c0, c1;
+        chunks_of<T>(z, per_slice, k_all, c0, c1);
+        if (c1 > c0) most.offsets = std::max(most.offsets, (int64_t)(c1 - 1) * chunk_step(strided, ld) + 1 - r.bytes);
+      }
+    }
+  };
+  operand(TA, P.a, P.lda, P.a_n, ti, BM, a);
+  if (ti > 0) operand(TB, P.b, P.ldb, P.b_n, P.tiles_j, BN, b);
+  // the last element that is stored
+  const int64_t rows = std::min<int64_t>(ti * BM, EPI == EPI_DZ || EPI == EPI_OUT ? P.out_rows : ti * BM);
+  if (rows == 0) return;
+  int64_t end;
+  if (EPI == EPI_STRIP) end = ((int64_t)(P.tiles_j - 1) * P.padded + std::min<int64_t>(rows, kept)) * (int64_t)sizeof(float2);
+  else if (EPI == EPI_SLICE) end = ((slices - 1) * (int64_t)P.slice_stride + (rows - 1) * P.ldo + P.out_cols) * (int64_t)sizeof(float);
+  else end = (int64_t)(uintptr_t)P.out - out.base + ((rows - 1) * P.ldo + P.out_cols) * el;
+  most.stores = std::max(most.stores, end - out.bytes);
+}
+
+}  // namespace
+
+template <typename T>
+LoadOverreach token_logprob_overreach(const LogprobSizes& n) {
+  const int64_t el = sizeof(T);
+  // addresses that nothing is at: only distances count
+  const Extent h{1ll << 44, n.padded * n.ld * el}, w{2ll << 44, (int64_t)n.vocab * n.hidden * el}, dz{3ll << 44, n.padded * n.ldz * el},
+      dw{4ll << 44, (int64_t)n.vocab * n.hidden * el}, part{0, n.padded * n.strips * (int64_t)sizeof(float2)},
+      dh{0, n.padded * n.hidden * (int64_t)sizeof(float) * n.most_slices};
+  auto at = [](const Extent& x) { return (T*)(uintptr_t)x.base; };
+  const KeptRows none{};
+  LoadOverreach most{0, 0, 0};
+  if (!n.backward) {
+    find_overreach<T, false, false, EPI_STRIP>(logits_strips<T>(at(h), n.ld, n.rows, n.padded, at(w), n.vocab, n.hidden, none, 1.f, nullptr, nullptr),
+                                               n.kept, 1, 0, h, w, part, most);
+    return most;
+  }
+  for (int v0 = 0; v0 < n.vocab; v0 += n.width) {
+    const VocabPiece piece{v0, std::min(n.width, n.vocab - v0), n.ldz};
+    find_overreach<T, false, false, EPI_DZ>(logits_gradient<T>(at(h), n.ld, n.rows, n.padded, at(w), n.vocab, n.hidden, none, 1.f, piece, at(dz)),
+                                            n.kept, 1, 0, h, w, dz, most);
+    find_overreach<T, false, true, EPI_SLICE>(hidden_gradient<T>(at(dz), piece, n.rows, n.padded, at(w), n.vocab, n.hidden, none, n.most_slices, nullptr,
+                                                                 (size_t)n.padded * n.hidden, v0 == 0),
+                                              n.kept, n.slices, n.per_slice, dz, w, dh, most);
+    find_overreach<T, true, true, EPI_OUT>(weight_gradient<T>(at(dz), piece, at(h), n.ld, n.padded, n.hidden, none, at(dw)), n.kept, 1, 0, dz, h, dw, most);
+  }
+  return most;
+}
+
+template <typename T>
+int launch_logits_strips_mfma(hipStream_t s, const T* h, int ld, int rows, int64_t padded, const T* w, int vocab, int hidden,
+                              const KeptRows& kept, float inv_t, float2* part, float* zt) {
+  const Planned<T> p = logits_strips<T>(h, ld, rows, padded, w, vocab, hidden, kept, inv_t, part, zt);
+  go<T, false, false, EPI_STRIP>(p, s);
+  return p.p.tiles_j;
+}
+template <typename T>
+void launch_logits_gradient_mfma(hipStream_t s, const T* h, int ld, int rows, int64_t padded, const T* w, int vocab, int hidden,
+                                 const KeptRows& kept, float inv_t, const VocabPiece& piece, T* dz) {
+  go<T, false, false, EPI_DZ>(logits_gradient<T>(h, ld, rows, padded, w, vocab, hidden, kept, inv_t, piece, dz), s);
+}
+template <typename T>
+void launch_hidden_gradient_mfma(hipStream_t s, const T* dz, const VocabPiece& piece, int rows, int64_t padded, const T* w, int vocab, int hidden,
+                                 const KeptRows& kept, int most_slices, float* dh, size_t slice_stride, bool first) {
+  go<T, false, true, EPI_SLICE>(hidden_gradient<T>(dz, piece, rows, padded, w, vocab, hidden, kept, most_slices, dh, slice_stride, first), s);
+}
+template <typename T>
+void launch_weight_gradient_mfma(hipStream_t s, const T* dz, const VocabPiece& piece, const T* h, int ld, int64_t padded, int hidden,
+                                 const KeptRows& kept, T* dw) {
+  go<T, true, true, EPI_OUT>(weight_gradient<T>(dz, piece, h, ld, padded, hidden, kept, dw), s);
 }
 
 #define RL_OF(T)                                                                                                                              \
   template bool token_logprob_takes_mfma<T>(int64_t, int, int, int, const void*, const void*);                                                \
+  template LoadOverreach token_logprob_overreach<T>(const LogprobSizes&);                                                                     \
   template void token_logprob_slice_tile<T>(int, int, int, SliceRule&);                                                                         \
   template int launch_logits_strips_mfma<T>(hipStream_t, const T*, int, int, int64_t, const T*, int, int, const KeptRows&, float, float2*,    \
                                             float*);                                                                                          \

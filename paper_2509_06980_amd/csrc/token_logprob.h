@@ -8,7 +8,7 @@ struct SliceRule {
   float chunk_us, slice_us;            // time of a tile's 32 k; of writing and reading a slice's sums of one row
 };
 // The number of slices that ends first: a round of tiles on 256 CUs takes what its k take and 6 us to begin and end.
-static __device__ __forceinline__ int choose_slices(const SliceRule& r, int kept) {
+static __host__ __device__ __forceinline__ int choose_slices(const SliceRule& r, int kept) {
   const int tiles = (kept + r.rows - 1) / r.rows * r.tiles_j;
   float best = 3e38f;
   int slices = 1;
@@ -18,6 +18,8 @@ static __device__ __forceinline__ int choose_slices(const SliceRule& r, int kept
   }
   return slices;
 }
+// Vocabulary of a slice
+static __host__ __device__ __forceinline__ int slice_width(const SliceRule& r, int slices) { return ((r.width + slices - 1) / slices + 63) / 64 * 64; }
 // The rows that take part are gathered to the front; how many there are only the device knows.
 struct KeptRows {
   const int32_t* count;      // kept rows; backward also [1]: K-slices of dz W, [2]: vocabulary of one (multiple of 64)
@@ -64,3 +66,15 @@ void launch_hidden_gradient_mfma(hipStream_t s, const T* dz, const VocabPiece& p
 template <typename T>
 void launch_weight_gradient_mfma(hipStream_t s, const T* dz, const VocabPiece& piece, const T* h, int ld, int64_t padded, int hidden,
                                  const KeptRows& kept, T* dw);
+
+// ---- the same arithmetic on the host: what the loads and stores of a call's products would reach ------------------------------------
+struct Extent { int64_t base, bytes; };
+// By how many bytes at most, 0: not at all: buffers beyond their operands, scalar offsets beyond their buffers, stores beyond the results
+struct LoadOverreach { int64_t buffers, offsets, stores; };
+struct LogprobSizes {
+  int rows, kept, hidden, vocab, backward;      // kept: as counted on the device
+  int64_t padded;
+  int ld, strips, width, ldz, most_slices, slices, per_slice;
+};
+template <typename T>
+LoadOverreach token_logprob_overreach(const LogprobSizes& n);

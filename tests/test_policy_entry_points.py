@@ -1,6 +1,7 @@
 """CPU-side checks of the policy update's C entry points: what they refuse before anything touches a GPU, and workspace sizes."""
 import math
 import os
+import random
 
 import numpy as np
 import pytest
@@ -129,3 +130,33 @@ def test_sizes_that_no_launch_takes_are_refused(lib):
     assert lib.rl_attention_fast_workspace((1 << 24) - 17, 1 << 10, 1 << 10, 2, 1, 8, F32) > 0 and lib.rl_attention_fast_workspace((1 << 24) - 16, 1 << 10, 1 << 10, 2, 1, 8, F32) == 0
     assert lib.rl_norm_workspace(1, (1 << 27) - 32, 0) > 0 and lib.rl_norm_workspace(1, (1 << 27) - 31, 0) == lib.rl_norm_workspace(1 << 31, 8, 0) == 0
     assert norm_forward(lib, width=(1 << 27) - 32, outer=0) == 0
+
+
+def test_loads_of_the_token_logprob_products_stay_inside_their_operands():
+    # also where the last tile of dz begins behind the vocabulary (its columns go on to a multiple of 256: 60032 of 60000 in tiles of 64),
+    # with few rows kept or none, in several pieces of the vocabulary and slices of it
+    rng = random.Random(11)
+    cases = [(300, 201, 4096, 60000), (300, 64, 20001 // 8 * 8, 20001), (700, 700, 8, 40003), (1100, 500, 64, 600), (4096, 2744, 2560, 151936), (8191, 4096, 1024, 151936),
+             (30, 20, 4096, 151936), (64, 64, 768, 140_000), (1, 1, 8, 1), (1, 0, 8, 257), (16384, 9000, 2560, 151936), (2000, 1999, 65536, 3000)]
+    for _ in range(200):
+        rows = int(math.exp(rng.uniform(0, math.log(9000))))
+        hidden, vocab = 8 * int(math.exp(rng.uniform(0, math.log(600)))), int(math.exp(rng.uniform(0, math.log(160_000))))
+        cases.append((rows, rng.choice([0, 1, rows, rng.randint(0, rows)]), hidden, rng.choice([vocab, vocab // 256 * 256 + 1, vocab // 64 * 64 + 32])))
+    taken = 0
+    for rows, kept, hidden, vocab in cases:
+        for bf16 in (False, True):
+            for backward in (False, True):
+                try:
+                    beyond = rl.debug_token_logprob_loads(rows, kept, hidden, vocab, bf16, backward)
+                except rl.RolloutError as e:
+                    assert "other kernels" in str(e)
+                    continue
+                taken += 1
+                assert beyond == (0, 0, 0), (rows, kept, hidden, vocab, bf16, backward, beyond)
+    assert taken > 3.5 * len(cases)
+
+
+def test_loads_of_sizes_that_the_products_do_not_take_are_refused(lib):
+    for bad in ((0, 0, 8, 9, 1, 1), (4, 5, 8, 9, 1, 1), (4, -1, 8, 9, 1, 1), (4, 4, 6, 9, 1, 0), (4, 4, 8, 0, 0, 0), (1 << 23, 1, 4096, 9, 1, 1)):
+        with pytest.raises(rl.RolloutError):
+            rl.debug_token_logprob_loads(*bad)

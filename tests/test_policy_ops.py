@@ -12,7 +12,7 @@ import pytest
 import torch
 
 from paper_2509_06980_amd import policy_ops as ops
-from paper_2509_06980_amd.binding import RolloutError
+from paper_2509_06980_amd.binding import RolloutError, debug_token_logprob_loads
 
 pytestmark = pytest.mark.gpu
 BF, FP = torch.bfloat16, torch.float32
@@ -538,6 +538,14 @@ def test_token_logprobs_of_many_tiles_a_workgroup(dt, rows, hidden, vocab):
 @pytest.mark.parametrize("rows,hidden,vocab", [(700, 72, 140_000), (90, 776, 135_000), (260, 264, 30_011)])
 def test_token_logprobs_of_large_vocabularies(rows, hidden, vocab):
     _check_token_logprobs(BF, rows, hidden, vocab)
+
+
+# The columns of dz go on to a multiple of 256: a tile can begin behind the vocabulary, at 60032 of 60000 and at 20096 of 20001 in tiles of
+# 128 columns, at 20032 of 20001 in tiles of 64.
+@pytest.mark.parametrize("dt,rows,hidden,vocab", [(BF, 260, 512, 20_001), (FP, 60, 512, 20_001), (FP, 300, 4096, 60_000)])
+def test_token_logprobs_where_a_tile_begins_behind_the_vocabulary(dt, rows, hidden, vocab):
+    assert debug_token_logprob_loads(rows, rows - len(range(0, rows, 7)), hidden, vocab, dt == BF, True) == (0, 0, 0)
+    _check_token_logprobs(dt, rows, hidden, vocab)
 
 
 def _check_token_logprobs(dt, rows, hidden, vocab):
