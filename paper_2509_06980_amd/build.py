@@ -56,8 +56,12 @@ def build(verbose=False):
 
 
 def build_torch_binding():
-    """_policy_torch.so: the policy update's operators on torch tensors, linked against the library beside it."""
-    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    """_policy_torch.so: the policy update's operators on torch tensors, linked against the library beside it.  None where torch is not
+    installed: the engine and the C boundary need none."""
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        return None
+    torch = spec.submodule_search_locations[0]
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-fPIC", "-shared", "-std=c++17", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=1",
            "-I" + os.path.join(torch, "include"), "-I" + os.path.join(torch, "include", "torch", "csrc", "api", "include"),
            "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "policy_torch.cpp"), "-o", TORCH_OUT,
