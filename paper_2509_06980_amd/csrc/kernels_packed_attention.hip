@@ -16,7 +16,7 @@ namespace {
 // different rows and share what is in LDS; SPLIT = 4: they have the same 16 rows, each takes every fourth 32 of the other side, and
 // their sums are joined at the end.  The first reads a quarter of the bytes, the second has four times the workgroups and a quarter
 // of the steps: it is taken where the first would not fill the chip (4 sequences of 96 rows, 4 heads over 2, forward and backward: 56 us against 41).  Bound by the
-// fp32 matrix rate (8 sequences of 1024, 8 heads of 128, causal: 1.44 ms), the small ones by one tile's chain of loads and products.
+// fp32 matrix rate (8 sequences of 1024, 8 heads of 128, causal: 1.54 ms), the small ones by one tile's chain of loads and products.
 // A query head reads KV head h / (nq / nkv); the gradient of a KV head is added up over its query heads in the workgroup that owns
 // its rows, in a fixed order.
 // =============================================================================================

@@ -21,10 +21,11 @@ namespace {
 // The backward pass forms the scores twice, in both kernels (14 instead of 10 products' flops), rather than add dq up by atomics in an
 // order that changes, or write the gradients of the scores out.  Probabilities and gradients of the scores are rounded to bf16, as the
 // operands that they become; all sums, and the softmax's statistics, are kept in 32 bits.
-// Bound by the matrix units (busy 44 to 60 % of the time) with the exponentials beside them, by the LDS (1 KB per product instruction), and by
-// power: with zeros for data the same kernels take 20 % less.  Measured, one sequence of 8192, 16 heads over 8 of 128, causal: forward 0.28 ms
-// (0.99 PFLOP/s of the pairs that are seen), dq 0.36 (1.15), dk and dv 0.56 (0.98); 16 sequences of 97 to 1511, 32 heads over 8: 97, 128
-// and 176 us.
+// Bound by the matrix units (busy 53 to 70 % of the cycles for one sequence of 8192, 25 to 31 % for 16 ragged ones) with the exponentials beside
+// them and by the LDS (1 KB per product instruction); the long case also by the clock that its data leaves: 1.6 to 1.8 GHz against 2.1 to
+// 2.2 in the ragged case, in the same number of cycles on two GPUs whose clocks differ by 4 %, and zeros for data take 20 % less time.
+// Measured, one sequence of 8192, 16 heads over 8 of 128, causal: forward 0.28 ms (0.98 PFLOP/s of the pairs that are seen), dq 0.36
+// (1.16), dk and dv 0.57 (0.97); 16 sequences of 97 to 1511, 32 heads over 8: 100, 129 and 175 us.
 // LDS: rows of D elements, 16-byte piece p of row r at p ^ f(r).  f moves 16 rows of one piece (read as they lie) to different
 // banks, and the 4 rows x 32 columns of a transposing read as well.
 // The two waves of a SIMD ought to be in different parts of a step, one at the products alone while the other has exponentials to
@@ -389,8 +390,9 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(PackedShape p, con
   const int all = row_a >= w.t.len ? 0 : p.causal ? min(w.lk, row_a + w.shift + 1) : w.lk;
   const int some = row_a >= w.t.len ? 0 : p.causal ? min(w.lk, row_b + w.shift) : w.lk;
   // Queries of few keys: o is large there, its rounding to bf16 moves delta by as much as the gradients of the scores are rounded below.
-  // Both stages hold all of their keys, so delta is taken as sum of p dp first (error of dq and dk 1.46 times that of their last
-  // rounding, 1.7 without; tiles of more keys are below 1.5 as they are).
+  // Up to 128 keys fit both stages, so delta is taken as sum of p dp without reading any twice: relative error of these queries' dq 0.0024,
+  // from the rounded o 0.0026, of the last rounding alone 0.0017.  Of more keys o is smaller, about by the root of their number, and its
+  // rounding counts for less: 0.0025 at 128 to 512 keys, 0.0024 beyond.
   if (few) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -734,8 +736,10 @@ void allow_lds(std::atomic<uint64_t>& done, K kernel, int bytes) {
 }
 
 // Keys of a workgroup of dk and dv.  128 (each tile of queries read by four waves, three stages) where there are workgroups enough for that,
-// 64 otherwise.  Measured, forward and backward, 128 and 64 keys, 8 KV heads of 128: one sequence of 8192 1092 and 1140 us, of 4096 704 and
-// 602; 4 sequences of 4096 1162 and 1208, of 2048 691 and 649; 32 of 1024 1568 and 1608; 16 of 97 to 1511 353 and 333.
+// 64 otherwise.  Measured, backward alone, 128 and 64 keys, 16 heads over 8 KV heads of 128: one sequence of 4096 320 and 274 us, of 5000 405
+// and 389, of 6000 521 and 521, of 7000 643 and 672, of 8192 833 and 880; 2 of 4096 441 and 473; 4 of 3000 507 and 531, of 4096 875 and 945;
+// forward and backward: 4 of 2048 691 and 649; 32 of 1024 1568 and 1608; 16 of 97 to 1511 353 and 333.  The sides cross below both of the
+// rule's bounds, at n = 375 for one sequence and between 512 and 750 for four; between there and the bounds it gives away up to 5 %.
 bool many_keys(const PackedShape& p) {
   const int64_t n = (int64_t)p.total_k * p.nkv / 128;
   return n >= 1024 || (n >= 512 && p.n_seq <= 2);

@@ -15,10 +15,11 @@ namespace {
 //   dz W            A = dz                     B = weights, k-strided     epilogue: a slice's sum in 32 bits
 //   dz^T hidden     A = dz, k-strided          B = rows, k-strided        epilogue: rounded
 // dz is rounded to the weights' type once, as the operand that it becomes; all sums are kept in 32 bits.
-// Bound by the matrix units (2 flops x rows x hidden x vocab each, 2.5 PFLOP/s peak, held by power: a large library product of random
-// data reaches 1.47, operands of zeros run these 1.2 times as fast), for few rows by the weights' bytes; fp32: 155 TFLOP/s.
-// Measured in bf16, 2744 rows x 2560 x 151936: logits 1.79 ms (1.19 PFLOP/s), dz 1.98 in two pieces, dz W 1.8 (1.19), dz^T hidden 1.83 (1.17);
-// 4096 x 1024 x 151936, logits 1.20 ms (1.06).
+// Bound by the matrix units (2 flops x rows x hidden x vocab each; busy 60 to 63 % of the cycles) at the clock that the data leaves them, 1.71 to
+// 1.77 GHz: of 2.5 PFLOP/s at the full clock a large library product of random data reaches 1.47, and operands of zeros run these 1.2 times as
+// fast.  For few rows by the weights' bytes; fp32: 155 TFLOP/s.
+// Measured in bf16 on two GPUs, 2744 rows x 2560 x 151936: logits 1.79 and 1.85 ms (1.19 and 1.15 PFLOP/s), dz 1.95 and 2.00 in two pieces,
+// dz W 1.78 and 1.83 (1.20, 1.17), dz^T hidden 1.80 and 1.86 (1.19, 1.15); 4096 x 1024 x 151936, logits 1.20 and 1.23 ms (1.06, 1.04).
 // A chunk of 64 bytes of k (32; fp32 16) of both operands goes straight from memory into one of R stages in LDS, R - 1 ahead;
 // operands are read half a chunk ahead of the instructions that use them, one barrier a chunk.  A workgroup stays for all its tiles
 // and its loads run on into the next one, so a tile ends with its epilogue alone (without that, the last-named logits 1.35 ms).

@@ -30,9 +30,10 @@ struct KeptRows {
 };
 // Backward in bf16 with up to 64 rows: row twins + r is row r once more and holds what the rounding of its dz left, so that both products
 // behind see dz in 16 bits (relative error of both gradients 0.0017, that of their last rounding).  Without it they were 0.0020 to 0.0028
-// off: few rows do not average the rounding of a row's largest element, its target's.  Few rows fill no tile: 64 x 2560 x 20000, both directions,
-// 152 us with and without; 30 x 4096 x 151936 1.12 ms, without 1.08.  Of more rows the gradients
-// are 0.0024 off.
+// off: few rows do not average the rounding of a row's largest element, its target's.  The bound of 64 is one of cost alone: twice as many
+// rows still fit one tile and cost next to nothing (64 x 2560 x 20000, both directions, 152 us with and without; 30 x 4096 x 151936 1.12
+// ms, without 1.08), beyond it they would double the products.  From 65 rows on the gradients are 0.0023 to 0.0024 off, less exact than those of
+// 64.
 static inline int twins_of(int rows, bool bf16) { return !bf16 || rows > 64 ? 0 : rows > 32 ? 64 : rows > 16 ? 32 : 16; }
 static __device__ __forceinline__ float rounding_left(float v) {
   const float left = v - (float)(__bf16)v;

@@ -175,5 +175,5 @@ def attention(q, k, v, cu_q, cu_k, causal=True, scale=None):
 
 
 def token_logprobs(hidden, weight, targets, temperature=1.0):
-    """Differentiable token_logprobs_forward -> logp."""
+    """Differentiable token_logprobs_forward -> logp.  Its backward pass forms both gradients, also where only one is asked for."""
     return _TokenLogprobs.apply(hidden, weight, targets, temperature)
