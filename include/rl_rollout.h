@@ -417,6 +417,78 @@ int rl_token_logprobs_backward(const float* d_dlogp, const void* d_hidden, int64
  */
 int rl_debug_token_logprob_loads(int32_t rows, int32_t kept, int32_t hidden, int32_t vocab, int32_t dtype, int32_t backward, int64_t* out);
 
+/*
+ * Linear layers with what follows them: z = x W^T + bias, u = x U^T + up_bias where d_up is not NULL; y = act(z) [* u] [+ residual].  x: [rows,
+ * inner], W and U: [outer, inner], y: [rows, outer], contiguous; strides are those of rows.  d_bias, d_up_bias, d_residual may be NULL.
+ * dtype is that of x, the weights and the biases; the residual is of that type or float32, y of the residual's type (without one: dtype).
+ * GELU is z Phi(z); RL_ACT_GELU_TANH the form with a hyperbolic tangent.
+ * d_kept, unless NULL: z (and u behind it) in 32 bits, [rows][1 or 2][outer], for the backward call, which needs it where there is an activation or U.
+ * Backward: from d_dy, of y's type; each of the results may be NULL if it is not wanted.  The gradients of z and u are rounded to dtype where they enter
+ * the products.  The residual's gradient is dy.  rows = 0: gradients of weights and biases are 0.
+ * rows at most 2^26, inner and outer 1 to 2^20 - 8, outer x inner (inner to a multiple of 8) at most 2^30 - 2^20.
+ * Workspace 256-byte aligned; aligned = 1: its size for 16-byte aligned x, W and U with row strides in multiples of 16 bytes (at most 2^20
+ * elements, W and U alike); 0: for any.  Rows that do not lie so, or are no whole 16 bytes long, are copied into it first.
+ */
+#define RL_ACT_NONE 0
+#define RL_ACT_RELU 1
+#define RL_ACT_SILU 2
+#define RL_ACT_GELU 3
+#define RL_ACT_GELU_TANH 4
+int64_t rl_linear_workspace(int32_t rows, int32_t inner, int32_t outer, int32_t gated, int32_t dtype, int32_t backward, int32_t aligned);
+int rl_linear_forward(const void* d_x, int64_t x_stride, int32_t rows, int32_t inner, const void* d_weight, int64_t weight_stride,
+                      const void* d_up, int64_t up_stride, int32_t outer, const void* d_bias, const void* d_up_bias, int32_t activation,
+                      const void* d_residual, int64_t residual_stride, int32_t residual_dtype, int32_t dtype, void* d_y, float* d_kept,
+                      void* d_workspace, int64_t workspace_bytes, void* stream);
+int rl_linear_backward(const void* d_dy, int64_t dy_stride, int32_t dy_dtype, const void* d_x, int64_t x_stride, int32_t rows, int32_t inner,
+                       const void* d_weight, int64_t weight_stride, const void* d_up, int64_t up_stride, int32_t outer, int32_t activation,
+                       const float* d_kept, int32_t dtype, void* d_dx, void* d_dweight, void* d_dup, void* d_dbias, void* d_dup_bias,
+                       void* d_workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The residual stream around a block, rows x width: u = y, or norm(y) * post_weight (+ post_bias) where d_post_weight is not NULL;
+ * h' = residual_scale * h + block_scale * g * u; a = norm(h') * weight (+ bias) where d_weight is not NULL.  The norms are those of
+ * rl_norm_forward (RMS, or layer norm where centered).  The stream h, h' is of stream_dtype: dtype, or float32; all else of dtype.  a is the norm of
+ * h' before its rounding.  d_gate, unless NULL: one number a column (gate_columns = 1, row stride 0), a row (gate_columns = 0) or an element.
+ * Strides are those of rows; outputs are contiguous.  d_stats: four floats a row, 16-byte aligned, for the backward call.
+ * Backward, from the gradients of h' and of a (one of the two may be NULL: 0): of h, y, the weights and, unless NULL, the biases and the gate:
+ * d_dgate as the gate is (gate_rows = 1: one number a row, or an element; 0: one a column, summed over rows).  d_dweight and d_dbias are written
+ * where d_da is not NULL.  rows and width at most 2^24.  Workspace 16-byte aligned.
+ */
+int rl_residual_norm_forward(const void* d_h, int64_t h_stride, const void* d_y, int64_t y_stride, int32_t rows, int32_t width,
+                             const void* d_weight, const void* d_bias, const void* d_post_weight, const void* d_post_bias,
+                             const void* d_gate, int64_t gate_row_stride, int32_t gate_columns, float residual_scale,
+                             float block_scale, float eps, int32_t centered, int32_t stream_dtype, int32_t dtype, void* d_out,
+                             void* d_a, float* d_stats, void* stream);
+int64_t rl_residual_norm_workspace(int32_t rows, int32_t width);      /* of the backward call */
+int rl_residual_norm_backward(const void* d_dout, int64_t dout_stride, const void* d_da, int64_t da_stride, const void* d_out,
+                              int64_t out_stride, const void* d_y, int64_t y_stride, const float* d_stats, int32_t rows,
+                              int32_t width, const void* d_weight, const void* d_post_weight, const void* d_post_bias,
+                              const void* d_gate, int64_t gate_row_stride, int32_t gate_columns, float residual_scale,
+                              float block_scale, int32_t centered, int32_t stream_dtype, int32_t dtype, void* d_dh, void* d_dy,
+                              void* d_dweight, void* d_dbias, void* d_dpost_weight, void* d_dpost_bias, void* d_dgate,
+                              int32_t gate_rows, void* d_workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Orthogonalised updates of `count` matrices G, rows x columns each: X = G / (|G| + eps), |G| the root of the sum of squares, then `steps` times
+ * X <- a X + b (X X^T) X + c (X X^T)^2 X with (a, b, c) = coefficients[3 step ..] (a HOST pointer, read during the call): a singular value s
+ * becomes a s + b s^3 + c s^5.  d_out: contiguous, of G's type; it may be a contiguous G itself.  A matrix of zeros gives zeros (eps > 0);
+ * values that are no number or infinite make that matrix no numbers, never another one.
+ * float32: sums and operands in 32 bits.  bf16: from a smaller side of 256 on the operands of the products are rounded to fp16, X itself and all sums
+ * stay in 32 bits (coefficients that let singular values or intermediate values grow beyond fp16's range take float32).
+ * steps 1 to 64, count at most 65535, sides at most 2^20 - 8, a matrix (sides + 8) at most 2^30 - 2^20 elements.  Workspace 256-byte aligned.
+ */
+int64_t rl_orthogonalize_workspace(int32_t count, int32_t rows, int32_t columns, int32_t dtype);
+int rl_orthogonalize(const void* d_x, int64_t matrix_stride, int64_t row_stride, int32_t count, int32_t rows, int32_t columns,
+                     int32_t steps, const float* coefficients, float eps, int32_t dtype, void* d_out, void* d_workspace,
+                     int64_t workspace_bytes, void* stream);
+/*
+ * Memory accesses of these calls' products and of the linear layers': host arithmetic only, for tests.  out: by how many bytes the buffers of their loads
+ * reach beyond the operands, the loads' scalar offsets beyond those buffers (0 or less: nowhere), and how many products were looked at.
+ */
+int rl_debug_linear_loads(int32_t rows, int32_t inner, int32_t outer, int64_t x_stride, int64_t weight_stride, int64_t dy_stride,
+                          int32_t gated, int32_t dtype, int32_t backward, int64_t* out);
+int rl_debug_orthogonalize_loads(int32_t count, int32_t rows, int32_t columns, int32_t dtype, int64_t* out);
+
 #ifdef __cplusplus
 }
 #endif

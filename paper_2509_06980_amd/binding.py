@@ -18,6 +18,8 @@ EXPORTED_SYMBOLS = [
     "rl_attention_fast_workspace",
     "rl_attention_backward", "rl_token_logprobs_workspace", "rl_token_logprobs_forward", "rl_token_logprobs_backward",
     "rl_debug_token_logprob_loads",
+    "rl_linear_workspace", "rl_linear_forward", "rl_linear_backward", "rl_residual_norm_forward", "rl_residual_norm_workspace",
+    "rl_residual_norm_backward", "rl_orthogonalize_workspace", "rl_orthogonalize", "rl_debug_linear_loads", "rl_debug_orthogonalize_loads",
 ]
 
 
@@ -109,9 +111,17 @@ def load_library():
     lib.rl_attention_backward.argtypes = [p, p, l, l, p, l, l, p, l, l, p, p, p, p, i, i, i, i, i, i, f, i, i, p, p, p, p, l, p]
     lib.rl_token_logprobs_forward.argtypes = [p, l, i, i, p, i, p, f, i, p, p, p, l, p]
     lib.rl_token_logprobs_backward.argtypes = [p, p, l, i, i, p, i, p, p, f, i, p, p, p, l, p]
+    lib.rl_linear_forward.argtypes = [p, l, i, i, p, l, p, l, i, p, p, i, p, l, i, i, p, p, p, l, p]
+    lib.rl_linear_backward.argtypes = [p, l, i, p, l, i, i, p, l, p, l, i, i, p, i, p, p, p, p, p, p, l, p]
+    lib.rl_residual_norm_forward.argtypes = [p, l, p, l, i, i, p, p, p, p, p, l, i, f, f, f, i, i, i, p, p, p, p]
+    lib.rl_residual_norm_backward.argtypes = [p, l, p, l, p, l, p, l, p, i, i, p, p, p, p, l, i, f, f, i, i, i, p, p, p, p, p, p, p, i, p, l, p]
+    lib.rl_orthogonalize.argtypes = [p, l, l, i, i, i, i, C.POINTER(f), f, i, p, p, l, p]
+    lib.rl_debug_linear_loads.argtypes = [i, i, i, l, l, l, i, i, i, C.POINTER(l)]
+    lib.rl_debug_orthogonalize_loads.argtypes = [i, i, i, i, C.POINTER(l)]
     lib.rl_debug_token_logprob_loads.argtypes = [i, i, i, i, i, i, C.POINTER(C.c_int64)]
     for name, args in (("rl_norm_workspace", [l, i, i]), ("rl_attention_workspace", [i, i]), ("rl_attention_fast_workspace", [i] * 7),
-                       ("rl_token_logprobs_workspace", [i, i, i, i, i])):
+                       ("rl_token_logprobs_workspace", [i, i, i, i, i]), ("rl_linear_workspace", [i] * 7),
+                       ("rl_residual_norm_workspace", [i, i]), ("rl_orthogonalize_workspace", [i] * 4)):
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = l
     _lib = lib
@@ -177,6 +187,21 @@ def debug_token_logprob_loads(rows, kept, hidden, vocab, bf16, backward):
     beyond the results."""
     out = (C.c_int64 * 3)()
     _check(load_library().rl_debug_token_logprob_loads(int(rows), int(kept), int(hidden), int(vocab), int(bool(bf16)), int(bool(backward)), out))
+    return tuple(out)
+
+
+def debug_linear_loads(rows, inner, outer, x_stride, weight_stride, dy_stride, gated, bf16, backward):
+    """Bytes that a linear layer's load buffers reach beyond their operands, their scalar offsets beyond the buffers, and the number of its products."""
+    out = (C.c_int64 * 3)()
+    _check(load_library().rl_debug_linear_loads(int(rows), int(inner), int(outer), int(x_stride), int(weight_stride), int(dy_stride), int(bool(gated)),
+                                                int(bool(bf16)), int(bool(backward)), out))
+    return tuple(out)
+
+
+def debug_orthogonalize_loads(count, rows, columns, bf16):
+    """The same of an orthogonalised update's products."""
+    out = (C.c_int64 * 3)()
+    _check(load_library().rl_debug_orthogonalize_loads(int(count), int(rows), int(columns), int(bool(bf16)), out))
     return tuple(out)
 
 

@@ -23,6 +23,9 @@ SOURCES = {
     "kernels_packed_attention_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "kernels_token_logprob.hip": [],
     "kernels_token_logprob_mfma.hip": [],
+    "kernels_linear.hip": [],
+    "kernels_residual_norm.hip": [],
+    "kernels_orthogonal.hip": [],
     "engine.hip": [],
 }
 

@@ -1,0 +1,337 @@
+// Orthogonalised updates: Newton-Schulz products on whole stacks of matrices.
+#include <cmath>
+
+#include "product.h"
+
+namespace {
+using namespace product;
+
+// =============================================================================================
+// X = G / (|G| + eps), then in every step  A = X X^T, B = b A + c A^2, X <- a X + B X  (matrices with more rows than columns: A = X^T X, X <- a X +
+// X B, so that A has the smaller of the two sizes and nothing is transposed).  Singular values s become p(s) = a s + b s^3 + c s^5, again and
+// again; the singular vectors stay.
+// A and B are symmetric: tiles on and under the diagonal are computed, the others are stored from them.
+// Bound by the matrix units.  fp32: everything in 32 bits.  bf16: the operands of the products are rounded to fp16 (11 bits instead of the 8 of bf16, at
+// the same rate), X times a power of two so that its elements lie in the middle of that range, and X itself is kept in 32 bits beside them, since a X
+// carries the small singular values, which the steps enlarge (500 times in five of them) with whatever roundings are in them.  A's diagonal, near 1 towards
+// the end, is what the rounding of B would cost most, so B's diagonal is kept in 32 bits too.  Relative error of the result against 64 bits, of
+// which its last rounding alone is 0.0017: 0.0017 to 0.0022 (rounded products without the 32 bits beside them: 0.02 for a matrix of 32 strong directions over
+// a floor of noise; operands in bf16: 0.2).  Matrices with a side below 256 take the fp32 products, where these cost nothing: fp16's error is largest there.
+// =============================================================================================
+const int kNormShares = 64;
+const int kHalfFrom = 256;
+
+// Sums of squares of a matrix in shares: part[matrix][share], in 64 bits (no overflow, no order to choose)
+template <typename T>
+__global__ __launch_bounds__(256) void squares_kernel(const T* __restrict__ x, int64_t matrix, int64_t stride, int rows, int columns, double* __restrict__ part) {
+  __shared__ double join[4];
+  const T* p = x + blockIdx.y * matrix;
+  double s = 0.0;
+  const int64_t n = (int64_t)rows * columns;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / columns;
+    const double v = (double)wide(p[r * stride + (i - r * columns)]);
+    s += v * v;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if ((threadIdx.x & 63) == 0) join[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) part[blockIdx.y * gridDim.x + blockIdx.x] = (join[0] + join[1]) + (join[2] + join[3]);
+}
+// X in 32 bits and, times `scale`, as operands of the products; rows of ld, zeros behind the last column
+template <typename T>
+__global__ __launch_bounds__(256) void normalise_kernel(const T* __restrict__ x, int64_t matrix, int64_t stride, int rows, int columns, int ld,
+                                                        const double* __restrict__ part, int shares, double eps, float scale, float* __restrict__ x32,
+                                                        _Float16* __restrict__ x16) {
+  __shared__ double factor;
+  if (threadIdx.x < 64) {
+    double s = (int)threadIdx.x < shares ? part[blockIdx.y * shares + threadIdx.x] : 0.0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if (threadIdx.x == 0) factor = 1.0 / (sqrt(s) + eps);
+  }
+  __syncthreads();
+  const double f = factor;
+  const T* p = x + blockIdx.y * matrix;
+  const int64_t n = (int64_t)rows * ld, base = blockIdx.y * n;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / ld;
+    const int c = (int)(i - r * ld);
+    const float v = c < columns ? (float)((double)wide(p[r * stride + c]) * f) : 0.f;
+    x32[base + i] = v;
+    if (x16) x16[base + i] = (_Float16)(v * scale);
+  }
+}
+
+// A = alpha (sums); rows of ld, zeros behind the last column
+template <typename T>
+struct Gram {
+  static constexpr bool GATED = false, SYMMETRIC = true;
+  static constexpr int V = kPiece<T>;
+  T* out;
+  int64_t matrix;
+  int ld, n;
+  float alpha;
+  __device__ __forceinline__ void across(int batch, int row, int col, float (&v)[V]) const {
+#pragma unroll
+    for (int e = 0; e < V; e++)
+      if (col + e >= n) v[e] = 0.f;
+    store_row<T, V>(out + batch * matrix + (int64_t)row * ld + col, true, V, v);
+  }
+  __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V]) const {
+#pragma unroll
+    for (int e = 0; e < V; e++) v[e] *= alpha;
+    across(batch, row, col, v);
+  }
+};
+// B = b A + c A^2; 16 bits: its diagonal apart
+template <typename T>
+struct Polynomial {
+  static constexpr bool GATED = false, SYMMETRIC = true;
+  static constexpr int V = kPiece<T>;
+  const T* a;
+  T* out;
+  float* diagonal;
+  int64_t matrix;
+  int ld, n;
+  float b, c;
+  __device__ __forceinline__ void across(int batch, int row, int col, float (&v)[V]) const {
+#pragma unroll
+    for (int e = 0; e < V; e++)
+      if (col + e >= n) v[e] = 0.f;
+    store_row<T, V>(out + batch * matrix + (int64_t)row * ld + col, true, V, v);
+  }
+  __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V]) const {
+    float x[V];
+    load_row<T, V>(a + batch * matrix + (int64_t)row * ld + col, true, V, x);
+#pragma unroll
+    for (int e = 0; e < V; e++) {
+      v[e] = b * x[e] + c * v[e];
+      if (sizeof(T) == 2 && col + e == row) {
+        diagonal[(int64_t)batch * n + row] = v[e];
+        v[e] = 0.f;
+      }
+    }
+    across(batch, row, col, v);
+  }
+};
+// X <- a X + B X; the last step's goes out in the caller's type (bf16 where `narrow_out`)
+template <typename T>
+struct Step {
+  static constexpr bool GATED = false, SYMMETRIC = false;
+  static constexpr int V = kPiece<T>;
+  const float* x32;
+  const T* x;              // the products' operand, 16 bits: x32 times `scale`
+  float* next32;           // 16 bits: x32 itself
+  T* next;
+  void* out;               // the last step's results, else null
+  const float* diagonal;
+  int64_t matrix;
+  int rows, cols, ld, by_column, bf16_out, vec;
+  float a, scale, inverse;
+  __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V]) const {
+    const int64_t at = batch * matrix + (int64_t)row * ld + col;
+    const int left = cols - col;
+    float x[V];
+    load_row<float, V>(x32 + at, true, V, x);
+    if constexpr (sizeof(T) == 2) {
+      float h[V], d[V];
+      load_row<T, V>(this->x + at, true, V, h);
+#pragma unroll
+      for (int e = 0; e < V; e++) d[e] = 0.f;
+      if (by_column) {
+        load_row<float, V>(diagonal + (int64_t)batch * cols + col, false, left, d);
+      } else {
+        const float one = diagonal[(int64_t)batch * rows + row];
+#pragma unroll
+        for (int e = 0; e < V; e++) d[e] = one;
+      }
+#pragma unroll
+      for (int e = 0; e < V; e++) v[e] = fmaf(a, x[e], fmaf(d[e], h[e], v[e]) * inverse);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; e++) v[e] = fmaf(a, x[e], v[e]);
+    }
+    if (out) {
+      const int64_t to = ((int64_t)batch * rows + row) * cols + col;
+      if (bf16_out) return store_row<bf16_t, V>((bf16_t*)out + to, vec, left, v);
+      return store_row<float, V>((float*)out + to, vec, left, v);
+    }
+#pragma unroll
+    for (int e = 0; e < V; e++)
+      if (e >= left) v[e] = 0.f;
+    store_row<float, V>(next32 + at, true, V, v);
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int e = 0; e < V; e++) v[e] *= scale;
+      store_row<T, V>(next + at, true, V, v);
+    }
+  }
+};
+
+struct Stack {
+  int count, rows, columns;
+  int small() const { return std::min(rows, columns); }
+};
+template <typename T>
+struct Layout {      // of the workspace
+  int ld, ld_small;
+  Plan gram, square, step;
+  int64_t matrix, small, shares, x32, x32b, x16, x16b, a, b, diagonal, part, bytes;
+  explicit Layout(const Stack& n) {
+    constexpr int V = kPiece<T>;
+    const int s = n.small(), l = std::max(n.rows, n.columns);
+    ld = (int)up(n.columns, V), ld_small = (int)up(s, V);
+    gram = plan_of<T>(s, s, n.count, chunks<T>(l), true, false);
+    square = plan_of<T>(s, s, n.count, chunks<T>(s), true, false);
+    step = plan_of<T>(n.rows, n.columns, n.count, chunks<T>(s), false, false);
+    matrix = (int64_t)n.rows * ld, small = (int64_t)s * ld_small;
+    int64_t at = 0;
+    auto take = [&](int64_t b) {
+      const int64_t p = at;
+      at += up(b, 256);
+      return p;
+    };
+    const bool half = sizeof(T) == 2;
+    shares = take((int64_t)n.count * kNormShares * sizeof(double));
+    x32 = take(n.count * matrix * sizeof(float));
+    x32b = half ? x32 : take(n.count * matrix * sizeof(float));
+    x16 = half ? take(n.count * matrix * sizeof(T)) : 0;
+    x16b = half ? take(n.count * matrix * sizeof(T)) : 0;
+    a = take(n.count * small * sizeof(T));
+    b = take(n.count * small * sizeof(T));
+    diagonal = half ? take((int64_t)n.count * s * sizeof(float)) : 0;
+    part = take(part_bytes(step, n.rows, n.columns, n.count, false));
+    bytes = at;
+  }
+};
+
+// Whether fp16 holds what arises: the largest singular value after every step, sampled over all that there can be, stays below 32
+bool fits_half(int steps, const float* coefficients) {
+  double most = 1.0;
+  for (int t = 0; t < steps; t++) {
+    const double a = coefficients[3 * t], b = coefficients[3 * t + 1], c = coefficients[3 * t + 2];
+    if (!(std::fabs(b) * most * most + std::fabs(c) * most * most * most * most < 16384.0)) return false;      // B
+    double next = 0.0;
+    for (int i = 1; i <= 1024; i++) {
+      const double s = most * i / 1024, s2 = s * s;
+      next = std::max(next, std::fabs(s * (a + s2 * (b + c * s2))));
+    }
+    if (!(next < 32.0)) return false;
+    most = next * 1.01;
+  }
+  return true;
+}
+
+template <typename T, typename G>
+int orthogonalize(const G* x, int64_t x_matrix, int64_t x_stride, const Stack& n, int steps, const float* coefficients, float eps, void* out, char* ws,
+                  hipStream_t s) {
+  constexpr bool HALF = sizeof(T) == 2;
+  const Layout<T> w(n);
+  const int small = n.small(), rows = n.rows, columns = n.columns;
+  const bool tall = rows > columns;
+  // elements of an orthogonalised matrix are 1 / sqrt(its longer side) on average: that becomes about 1
+  const float scale = HALF ? std::exp2(std::floor(0.5f * std::log2((float)std::max(rows, columns)))) : 1.f;
+  double* const shares = (double*)(ws + w.shares);
+  const int64_t elements = (int64_t)rows * columns;
+  const int n_shares = (int)std::min<int64_t>(kNormShares, (elements + 1023) / 1024);
+  float *x32 = (float*)(ws + w.x32), *next32 = (float*)(ws + w.x32b);
+  T *now = HALF ? (T*)(ws + w.x16) : (T*)x32, *next = HALF ? (T*)(ws + w.x16b) : (T*)next32;
+  if (!probe) {
+  squares_kernel<G><<<dim3(n_shares, n.count), 256, 0, s>>>(x, x_matrix, x_stride, rows, columns, shares);
+  normalise_kernel<G><<<dim3((unsigned)std::min<int64_t>((w.matrix + 1023) / 1024, 2048), n.count), 256, 0, s>>>(
+      x, x_matrix, x_stride, rows, columns, w.ld, shares, n_shares, (double)eps, scale, x32, HALF ? (_Float16*)now : nullptr);
+  }
+  T *const a = (T*)(ws + w.a), *const b = (T*)(ws + w.b);
+  float* const diagonal = (float*)(ws + w.diagonal);
+  for (int t = 0; t < steps; t++) {
+    const float* c = coefficients + 3 * t;
+    const bool last = t == steps - 1;
+    Product<T> p{};
+    p.segments = 1, p.batches = n.count;
+    {
+      const Operand<T> o{now, w.ld, w.matrix, 0, rows, rows, w.ld, w.ld, n.count * w.matrix};
+      p.a = p.b = o;
+      p.k = p.last_k = tall ? rows : w.ld, p.rows = p.cols = small;
+      const Gram<T> e{a, w.small, w.ld_small, small, 1.f / (scale * scale)};
+      if (tall) launch<T, true, true>(p, w.gram, e, s);
+      else launch<T, false, false>(p, w.gram, e, s);
+    }
+    const Operand<T> square{a, w.ld_small, w.small, 0, small, small, w.ld_small, w.ld_small, n.count * w.small};
+    p.a = p.b = square, p.k = p.last_k = w.ld_small;
+    launch<T, false, false>(p, w.square, Polynomial<T>{a, b, diagonal, w.small, w.ld_small, small, c[1], c[2]}, s);
+    {
+      const Operand<T> o{now, w.ld, w.matrix, 0, rows, rows, w.ld, w.ld, n.count * w.matrix};
+      Operand<T> poly = square;
+      poly.p = b;
+      p.part = (float*)(ws + w.part), p.rows = rows, p.cols = columns;
+      Step<T> e{x32, now, next32, next, last ? out : nullptr, diagonal, w.matrix, rows, columns, w.ld, tall, std::is_same<G, bf16_t>::value, 0, c[0], scale, 1.f / scale};
+      e.vec = columns % kPiece<T> == 0 && columns % (16 / sizeof(G)) == 0 && aligned16(out);
+      p.k = p.last_k = w.ld_small;
+      if (tall) {
+        p.a = o, p.b = poly;
+        launch<T, false, false>(p, w.step, e, s);
+      } else {
+        p.a = poly, p.b = o;
+        launch<T, false, true>(p, w.step, e, s);
+      }
+    }
+    std::swap(now, next);
+    if (!HALF) std::swap(x32, next32);
+  }
+  return probe ? RL_OK : launched();
+}
+
+bool takes_half(const Stack& n, int dtype, int steps, const float* coefficients) {
+  return dtype == RL_DTYPE_BF16 && n.small() >= kHalfFrom && fits_half(steps, coefficients);
+}
+const char* stack_argument(int32_t count, int32_t rows, int32_t columns, int32_t dtype) {
+  if (dtype != RL_DTYPE_F32 && dtype != RL_DTYPE_BF16) return "dtype is RL_DTYPE_F32 or RL_DTYPE_BF16";
+  if (count < 0 || count > 65535 || rows < 1 || columns < 1 || rows > (1 << 20) - 8 || columns > (1 << 20) - 8) return "count, rows or columns out of range";
+  const int64_t l = std::max(rows, columns), s = std::min(rows, columns);
+  if ((l + 8) * (s + 8) > (1ll << 30) - (1 << 20)) return "matrices of more than 2^30 - 2^20 elements";
+  return nullptr;
+}
+}  // namespace
+
+extern "C" int64_t rl_orthogonalize_workspace(int32_t count, int32_t rows, int32_t columns, int32_t dtype) {
+  if (stack_argument(count, rows, columns, dtype) || count == 0) return 0;
+  const Stack n{count, rows, columns};
+  const int64_t full = Layout<float>(n).bytes;
+  return dtype == RL_DTYPE_BF16 && n.small() >= kHalfFrom ? std::max(full, Layout<_Float16>(n).bytes) : full;
+}
+
+extern "C" int rl_orthogonalize(const void* d_x, int64_t matrix_stride, int64_t row_stride, int32_t count, int32_t rows, int32_t columns, int32_t steps,
+                                const float* coefficients, float eps, int32_t dtype, void* d_out, void* d_workspace, int64_t workspace_bytes, void* stream) {
+  if (const char* m = stack_argument(count, rows, columns, dtype)) return rl_fail(RL_E_ARG, m);
+  if (steps < 1 || steps > 64 || !coefficients) return rl_fail(RL_E_ARG, "1 to 64 steps with three coefficients each");
+  for (int i = 0; i < 3 * steps; i++)
+    if (!std::isfinite(coefficients[i])) return rl_fail(RL_E_ARG, "a coefficient is infinite or no number");
+  if (!(eps >= 0.f)) return rl_fail(RL_E_ARG, "eps is negative or no number");
+  if (count == 0) return RL_OK;
+  if (!d_x || !d_out || !d_workspace) return rl_fail(RL_E_ARG, "null pointer");
+  if (workspace_bytes < rl_orthogonalize_workspace(count, rows, columns, dtype)) return rl_fail(RL_E_ARG, "workspace smaller than rl_orthogonalize_workspace says");
+  if ((uintptr_t)d_workspace & 255) return rl_fail(RL_E_ARG, "workspace not aligned to 256 bytes");
+  const Stack n{count, rows, columns};
+  hipStream_t s = (hipStream_t)stream;
+  char* ws = (char*)d_workspace;
+  if (dtype == RL_DTYPE_F32) return orthogonalize<float>((const float*)d_x, matrix_stride, row_stride, n, steps, coefficients, eps, d_out, ws, s);
+  if (takes_half(n, dtype, steps, coefficients))
+    return orthogonalize<_Float16>((const bf16_t*)d_x, matrix_stride, row_stride, n, steps, coefficients, eps, d_out, ws, s);
+  return orthogonalize<float>((const bf16_t*)d_x, matrix_stride, row_stride, n, steps, coefficients, eps, d_out, ws, s);
+}
+
+extern "C" int rl_debug_orthogonalize_loads(int32_t count, int32_t rows, int32_t columns, int32_t dtype, int64_t* out) {
+  if (!out || count < 1) return rl_fail(RL_E_ARG, "null pointer or no matrices");
+  Probe found{};
+  probe = &found;
+  const float c[3] = {3.4445f, -4.7750f, 2.0315f};
+  char* const at = (char*)(1ll << 44);      // nothing is there: only distances count
+  const int rc = rl_orthogonalize(at, (int64_t)rows * columns, columns, count, rows, columns, 1, c, 1e-7f, dtype, at + (1ll << 42), at + (2ll << 42),
+                                  rl_orthogonalize_workspace(count, rows, columns, dtype), nullptr);
+  probe = nullptr;
+  if (rc != RL_OK) return rc;
+  out[0] = found.buffers, out[1] = found.offsets, out[2] = found.products;
+  return RL_OK;
+}

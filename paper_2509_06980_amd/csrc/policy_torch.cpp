@@ -9,6 +9,7 @@
 #include <optional>
 #include <string>
 #include <tuple>
+#include <vector>
 
 #include "../../include/rl_rollout.h"
 
@@ -256,6 +257,240 @@ std::tuple<Tensor, Tensor> token_logprobs_backward(const Tensor& dlogp, const Te
   return {dhidden, dweight};
 }
 
+// ---- linear layers ----------------------------------------------------------------------------------------------------------
+// x's rows as a matrix: leading dimensions are one
+struct Matrix {
+  Tensor x;
+  int32_t rows, columns;
+  int64_t stride;
+};
+Matrix matrix_of(const Tensor& x, const char* message) {
+  check(x.dim() >= 1, message);
+  const int64_t w = x.size(-1), n = w ? x.numel() / w : 0;
+  const bool strided = x.dim() == 2 && rows_contiguous(x) && (x.size(0) <= 1 || x.stride(0) >= 0);
+  const Tensor c = strided ? x : x.contiguous();
+  const int64_t stride = strided && x.size(0) > 1 ? x.stride(0) : w;
+  return {c, small(n, message), small(w, message), stride};
+}
+// an operand's stride has to keep its rows apart (an expanded one is copied)
+Matrix operand_of(const Tensor& x, const char* message) {
+  Matrix m = matrix_of(x, message);
+  if (m.rows > 1 && m.stride < m.columns) m.x = x.contiguous(), m.stride = m.columns;
+  return m;
+}
+int activation_of(const std::string& name) {
+  static const char* const names[] = {"none", "relu", "silu", "gelu", "gelu_tanh"};
+  for (int i = 0; i < 5; i++)
+    if (name == names[i]) return i;
+  throw Refused{RL_E_ARG, "activation is none, relu, silu, gelu or gelu_tanh"};
+}
+bool lies_in_16_bytes(const Matrix& m) {
+  return ((uintptr_t)m.x.data_ptr() & 15) == 0 && m.stride * m.x.element_size() % 16 == 0 && m.stride <= (1 << 20);
+}
+struct Layer {
+  Matrix x, w, u;
+  bool gated;
+  int dt, act;
+  int32_t outer;
+  int aligned;
+  const void* up() const { return gated ? u.x.data_ptr() : nullptr; }
+};
+Layer layer_of(const Tensor& x, const Tensor& weight, const Maybe& up, const std::string& activation) {
+  Layer l{};
+  l.dt = type_of(x);
+  like(weight, x);
+  check(x.dim() >= 1 && weight.dim() == 2 && weight.size(1) == x.size(-1) && weight.size(0) >= 1 && weight.size(1) >= 1, "x is [.., inner], weight [outer, inner]");
+  l.act = activation_of(activation);
+  l.x = operand_of(x, "x has too many rows or too long ones");
+  l.w = operand_of(weight, "weight is too large");
+  l.gated = up.has_value();
+  if (up) {
+    like(*up, x);
+    check(up->sizes() == weight.sizes(), "up has to have weight's shape");
+    l.u = operand_of(*up, "up is too large");
+  }
+  l.outer = l.w.rows;
+  l.aligned = lies_in_16_bytes(l.x) && lies_in_16_bytes(l.w) && (!up || (lies_in_16_bytes(l.u) && l.u.stride == l.w.stride));
+  return l;
+}
+at::DimVector with_last(const Tensor& x, int64_t n) {
+  at::DimVector shape(x.sizes().begin(), x.sizes().end());
+  shape.back() = n;
+  return shape;
+}
+void bias_of(const Maybe& bias, const Tensor& x, int64_t outer) {
+  if (!bias) return;
+  like(*bias, x);
+  check(bias->dim() == 1 && bias->size(0) == outer && bias->is_contiguous(), "a bias has to be contiguous, one number a row of its weight");
+}
+
+std::tuple<Tensor, Maybe> linear_forward(const Tensor& x, const Tensor& weight, const Maybe& bias, const Maybe& up, const Maybe& up_bias,
+                                         const std::string& activation, const Maybe& residual, bool keep, int64_t stream) {
+  const c10::DeviceGuard guard(x.is_cuda() ? x.device() : c10::Device(c10::kCPU));
+  const Layer l = layer_of(x, weight, up, activation);
+  bias_of(bias, x, l.outer);
+  check(!up_bias || up, "up_bias without up");
+  bias_of(up_bias, x, l.outer);
+  const at::DimVector shape = with_last(x, l.outer);
+  Matrix r{};
+  if (residual) {
+    check(residual->device() == x.device() && (residual->scalar_type() == x.scalar_type() || residual->scalar_type() == at::kFloat),
+          "the residual is of x's type or float32, on the same GPU");
+    check(residual->sizes() == at::IntArrayRef(shape), "the residual has the result's shape");
+    r = matrix_of(*residual, "the residual is too large");
+  }
+  Tensor y = at::empty(shape, residual ? residual->options() : x.options());
+  Maybe kept;
+  if (keep && (l.act != RL_ACT_NONE || l.gated)) kept = floats({l.x.rows, l.gated ? 2 : 1, l.outer}, x);
+  const int64_t n = rl_linear_workspace(l.x.rows, l.x.columns, l.outer, l.gated, l.dt, 0, l.aligned);
+  const Tensor ws = bytes(n, x);
+  done(rl_linear_forward(l.x.x.data_ptr(), l.x.stride, l.x.rows, l.x.columns, l.w.x.data_ptr(), l.w.stride, l.up(), l.u.stride, l.outer,
+                         bias ? bias->data_ptr() : nullptr, up_bias ? up_bias->data_ptr() : nullptr, l.act, residual ? r.x.data_ptr() : nullptr, r.stride,
+                         residual && residual->scalar_type() == at::kFloat ? RL_DTYPE_F32 : l.dt, l.dt, y.data_ptr(),
+                         kept ? kept->data_ptr<float>() : nullptr, ws.data_ptr(), n, at_stream(stream)));
+  return {y, kept};
+}
+
+std::tuple<Maybe, Maybe, Maybe, Maybe, Maybe> linear_backward(const Tensor& dy, const Tensor& x, const Tensor& weight, const Maybe& kept, const Maybe& up,
+                                                              const std::string& activation, bool biased, bool up_biased, bool want_dx, bool want_dweight,
+                                                              bool want_dup, int64_t stream) {
+  const c10::DeviceGuard guard(x.is_cuda() ? x.device() : c10::Device(c10::kCPU));
+  const Layer l = layer_of(x, weight, up, activation);
+  check(dy.device() == x.device() && (dy.scalar_type() == x.scalar_type() || dy.scalar_type() == at::kFloat), "dy is of x's type or float32, on the same GPU");
+  check(dy.sizes() == at::IntArrayRef(with_last(x, l.outer)), "dy has the result's shape");
+  check(!up_biased || up, "up_biased without up");
+  if (l.act != RL_ACT_NONE || l.gated) {
+    check(kept.has_value(), "an activation's backward pass needs what the forward call kept (keep=True)");
+    plain(*kept, at::kFloat, x, "kept has to be contiguous float32 on the same GPU");
+    check(kept->numel() == (int64_t)l.x.rows * (l.gated ? 2 : 1) * l.outer, "kept is of another call");
+  }
+  const Matrix d = matrix_of(dy, "dy is too large");
+  Maybe dx, dw, dup, db, dub;
+  if (want_dx) dx = fresh(x.sizes(), x);
+  if (want_dweight) dw = fresh(weight.sizes(), x);
+  if (want_dup && up) dup = fresh(weight.sizes(), x);
+  if (biased) db = fresh({l.outer}, x);
+  if (up_biased) dub = fresh({l.outer}, x);
+  const int64_t n = rl_linear_workspace(l.x.rows, l.x.columns, l.outer, l.gated, l.dt, 1, l.aligned);
+  const Tensor ws = bytes(n, x);
+  auto at = [](const Maybe& t) { return t ? t->data_ptr() : nullptr; };
+  done(rl_linear_backward(d.x.data_ptr(), d.stride, dy.scalar_type() == at::kFloat ? RL_DTYPE_F32 : l.dt, l.x.x.data_ptr(), l.x.stride, l.x.rows,
+                          l.x.columns, l.w.x.data_ptr(), l.w.stride, l.up(), l.u.stride, l.outer, l.act, kept ? kept->data_ptr<float>() : nullptr, l.dt,
+                          at(dx), at(dw), at(dup), at(db), at(dub), ws.data_ptr(), n, at_stream(stream)));
+  return {dx, dw, dup, db, dub};
+}
+
+// ---- the residual stream with its norms -----------------------------------------------------------------------------------------
+struct Block {
+  int dt, stream_dt, gate_columns, gate_rows;
+  Matrix gate;
+};
+void parameter(const Maybe& w, const Tensor& y, const char* message) {
+  if (!w) return;
+  like(*w, y);
+  check(w->dim() == 1 && w->size(0) == y.size(-1) && w->is_contiguous(), message);
+}
+Block block_of(const Tensor& stream_like, const Tensor& y, const Maybe& weight, const Maybe& post_weight, const Maybe& post_bias, const Maybe& gate) {
+  Block b{};
+  b.dt = type_of(y);
+  check(stream_like.device() == y.device() && (stream_like.scalar_type() == y.scalar_type() || stream_like.scalar_type() == at::kFloat),
+        "the stream is of y's type or float32, on the same GPU");
+  check(y.dim() >= 1 && y.size(-1) >= 1 && stream_like.sizes() == y.sizes(), "the stream has y's shape");
+  b.stream_dt = stream_like.scalar_type() == at::kFloat ? RL_DTYPE_F32 : b.dt;
+  parameter(weight, y, "weight has to be contiguous, of the length of a row");
+  parameter(post_weight, y, "post_weight has to be contiguous, of the length of a row");
+  check(!post_bias || post_weight, "post_bias without post_weight");
+  parameter(post_bias, y, "post_bias has to be contiguous, of the length of a row");
+  if (gate) {
+    like(*gate, y);
+    if (gate->sizes() == y.sizes() && (gate->dim() > 1 || !gate->is_contiguous())) {
+      b.gate = matrix_of(*gate, "gate is too large"), b.gate_columns = b.gate_rows = 1;
+    } else if (gate->dim() == 1 && gate->size(0) == y.size(-1)) {
+      b.gate = {gate->contiguous(), 1, small(y.size(-1), "rows are too long"), 0}, b.gate_columns = 1;
+    } else {
+      check(gate->sizes() == at::IntArrayRef(with_last(y, 1)), "gate is [width], of y's shape, or of y's shape with one column");
+      const Tensor g = gate->contiguous();
+      b.gate = {g, small(g.numel(), "gate is too large"), 1, 1}, b.gate_rows = 1;
+    }
+  }
+  return b;
+}
+
+std::tuple<Tensor, Maybe, Tensor> residual_norm_forward(const Tensor& h, const Tensor& y, const Maybe& weight, const Maybe& bias, const Maybe& post_weight,
+                                                        const Maybe& post_bias, const Maybe& gate, double residual_scale, double block_scale, double eps,
+                                                        bool centered, int64_t stream) {
+  const c10::DeviceGuard guard(y.is_cuda() ? y.device() : c10::Device(c10::kCPU));
+  const Block b = block_of(h, y, weight, post_weight, post_bias, gate);
+  check(!bias || weight, "bias without weight");
+  parameter(bias, y, "bias has to be contiguous, of the length of a row");
+  const Matrix hm = matrix_of(h, "too many rows or too long ones"), ym = matrix_of(y, "too many rows or too long ones");
+  Tensor out = fresh(h.sizes(), h), stats = floats({ym.rows, 4}, y);
+  Maybe a;
+  if (weight) a = fresh(y.sizes(), y);
+  auto at = [](const Maybe& t) { return t ? t->data_ptr() : nullptr; };
+  done(rl_residual_norm_forward(hm.x.data_ptr(), hm.stride, ym.x.data_ptr(), ym.stride, ym.rows, ym.columns, at(weight), at(bias), at(post_weight),
+                                at(post_bias), gate ? b.gate.x.data_ptr() : nullptr, b.gate.stride, b.gate_columns, (float)residual_scale,
+                                (float)block_scale, (float)eps, centered, b.stream_dt, b.dt, out.data_ptr(), at(a), stats.data_ptr<float>(),
+                                at_stream(stream)));
+  return {out, a, stats};
+}
+
+std::tuple<Tensor, Tensor, Maybe, Maybe, Maybe, Maybe, Maybe> residual_norm_backward(
+    const Maybe& dout, const Maybe& da, const Tensor& out, const Tensor& y, const Tensor& stats, const Maybe& weight, const Maybe& post_weight,
+    const Maybe& post_bias, const Maybe& gate, double residual_scale, double block_scale, bool centered, bool biased, int64_t stream) {
+  const c10::DeviceGuard guard(y.is_cuda() ? y.device() : c10::Device(c10::kCPU));
+  const Block b = block_of(out, y, weight, post_weight, post_bias, gate);
+  check(dout || da, "one of the two gradients at least");
+  check(!da || weight, "a gradient of the norm without its weight");
+  check(!biased || weight, "biased without weight");
+  if (dout) check(dout->device() == y.device() && dout->scalar_type() == out.scalar_type() && dout->sizes() == y.sizes(), "the stream's gradient is like the stream");
+  if (da) {
+    like(*da, y);
+    check(da->sizes() == y.sizes(), "the norm's gradient has y's shape");
+  }
+  const Matrix ym = matrix_of(y, "too many rows or too long ones"), om = matrix_of(out, "too many rows or too long ones");
+  plain(stats, at::kFloat, y, "stats has to be contiguous float32 on the same GPU");
+  check(stats.numel() == (int64_t)ym.rows * 4, "stats are four numbers a row");
+  Matrix dm{}, am{};
+  if (dout) dm = matrix_of(*dout, "too many rows or too long ones");
+  if (da) am = matrix_of(*da, "too many rows or too long ones");
+  Tensor dh = fresh(out.sizes(), out), dy = fresh(y.sizes(), y);
+  auto like_row = [&](bool wanted) { return wanted ? Maybe(at::empty({y.size(-1)}, y.options())) : Maybe(); };
+  auto zeros = [&](bool wanted) { return wanted ? Maybe(at::zeros({y.size(-1)}, y.options())) : Maybe(); };
+  Maybe dw = da ? like_row(true) : zeros(weight.has_value()), db = da ? like_row(biased) : zeros(biased), dpw = like_row(post_weight.has_value()),
+        dpb = like_row(post_bias.has_value()), dg;
+  if (gate) dg = fresh(gate->sizes(), y);
+  const int64_t n = rl_residual_norm_workspace(ym.rows, ym.columns);
+  const Tensor ws = bytes(n, y);
+  auto at = [](const Maybe& t) { return t ? t->data_ptr() : nullptr; };
+  done(rl_residual_norm_backward(dout ? dm.x.data_ptr() : nullptr, dm.stride, da ? am.x.data_ptr() : nullptr, am.stride, om.x.data_ptr(), om.stride,
+                                 ym.x.data_ptr(), ym.stride, stats.data_ptr<float>(), ym.rows, ym.columns, at(weight), at(post_weight), at(post_bias),
+                                 gate ? b.gate.x.data_ptr() : nullptr, b.gate.stride, b.gate_columns, (float)residual_scale, (float)block_scale, centered,
+                                 b.stream_dt, b.dt, dh.data_ptr(), dy.data_ptr(), da ? at(dw) : nullptr, da ? at(db) : nullptr, at(dpw), at(dpb), at(dg),
+                                 b.gate_rows, ws.data_ptr(), n, at_stream(stream)));
+  return {dh, dy, dw, db, dpw, dpb, dg};
+}
+
+// ---- orthogonalised updates -----------------------------------------------------------------------------------------------------
+Tensor orthogonalize(const Tensor& x, const std::vector<float>& coefficients, double eps, int64_t stream) {
+  const int dt = type_of(x);
+  check(x.dim() >= 2, "x is [.., rows, columns]");
+  check(coefficients.size() % 3 == 0, "three coefficients a step");
+  const c10::DeviceGuard guard(x.device());
+  const int64_t rows = x.size(-2), columns = x.size(-1), count = rows && columns ? x.numel() / (rows * columns) : 0;
+  const bool strided = x.dim() <= 3 && rows_contiguous(x) && (x.dim() < 3 || x.size(0) <= 1 || x.stride(0) >= 0) && (rows <= 1 || x.stride(-2) >= 0);
+  const Tensor in = strided ? x : x.contiguous();
+  Tensor out = fresh(x.sizes(), x);
+  if (x.numel() == 0) return out;
+  const int32_t n = small(count, "too many matrices"), r = small(rows, "matrices are too large"), c = small(columns, "matrices are too large");
+  const int64_t need = rl_orthogonalize_workspace(n, r, c, dt);
+  const Tensor ws = bytes(need, x);
+  done(rl_orthogonalize(in.data_ptr(), strided && x.dim() == 3 ? in.stride(0) : rows * columns, rows > 1 ? in.stride(-2) : columns, n, r, c,
+                        small((int64_t)coefficients.size() / 3, "too many steps"), coefficients.data(), (float)eps, dt, out.data_ptr(), ws.data_ptr(), need,
+                        at_stream(stream)));
+  return out;
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_policy_torch, m) {
@@ -274,4 +509,9 @@ PYBIND11_MODULE(_policy_torch, m) {
   m.def("attention_backward", &attention_backward);
   m.def("token_logprobs_forward", &token_logprobs_forward);
   m.def("token_logprobs_backward", &token_logprobs_backward);
+  m.def("linear_forward", &linear_forward);
+  m.def("linear_backward", &linear_backward);
+  m.def("residual_norm_forward", &residual_norm_forward);
+  m.def("residual_norm_backward", &residual_norm_backward);
+  m.def("orthogonalize", &orthogonalize);
 }

@@ -1,5 +1,6 @@
-"""The policy update's operators on torch tensors: norms, rotary positions, attention over packed trajectories and log-probs
-of tokens, forward and backward (the calls of include/rl_rollout.h under the same names), and as functions of torch.autograd.
+"""The policy update's operators on torch tensors: norms, rotary positions, attention over packed trajectories, log-probs of tokens,
+linear layers with what follows them and the residual stream with its norms, forward and backward (the calls of include/rl_rollout.h
+under the same names), and as functions of torch.autograd; orthogonalised updates.
 
 Tensors live on one GPU; work is enqueued on torch's current stream and nothing waits for it.  Arguments are checked in
 compiled code; what is refused raises RolloutError.
@@ -99,6 +100,55 @@ def token_logprobs_backward(dlogp, hidden, weight, targets, lse, temperature=1.0
     return _native.token_logprobs_backward(dlogp, hidden, weight, targets, lse, temperature, _stream(hidden))
 
 
+# ---- linear layers ---------------------------------------------------------------------------------------------------
+def linear_forward(x, weight, bias=None, up=None, up_bias=None, activation="none", residual=None, keep=False):
+    """act(x weight^T + bias) [* (x up^T + up_bias)] [+ residual] -> (y, kept); see rl_linear_forward.  x: [.., inner], weights: [outer, inner];
+    activation: none, relu, silu, gelu or gelu_tanh.  The residual has y's shape and x's type or float32; y has its type.  kept: what the
+    backward call needs, where `keep` (None where it needs nothing)."""
+    return _native.linear_forward(x, weight, bias, up, up_bias, activation, residual, keep, _stream(x))
+
+
+def linear_backward(dy, x, weight, kept=None, up=None, activation="none", biased=False, up_biased=False, wanted=(True, True, True)):
+    """Gradients of linear_forward -> (dx, dweight, dbias, dup, dup_bias), each None where there is none or, of dx, dweight and dup, it is not
+    `wanted`.  dy is of y's type; it is the residual's gradient too."""
+    dx, dw, dup, db, dub = _native.linear_backward(dy, x, weight, kept, up, activation, biased, up_biased, *wanted, _stream(x))
+    return dx, dw, db, dup, dub
+
+
+# ---- the residual stream around a block --------------------------------------------------------------------------------
+def residual_norm_forward(h, y, weight, bias=None, post_weight=None, post_bias=None, gate=None, residual_scale=1.0, block_scale=1.0, eps=1e-6,
+                          centered=False):
+    """A block's result y joins the stream h, the next block's norm follows -> (h_new, a, stats); see rl_residual_norm_forward.
+
+    h_new = residual_scale h + block_scale gate u, with u = y, or norm(y) post_weight + post_bias; a = norm(h_new) weight + bias (None without
+    weight).  Norms over the last dimension, RMS (layer norm where `centered`).  h is float32 or of y's type.  gate: [width], y's shape, or
+    y's shape with one column."""
+    return _native.residual_norm_forward(h, y, weight, bias, post_weight, post_bias, gate, residual_scale, block_scale, eps, centered, _stream(y))
+
+
+def residual_norm_backward(dh_new, da, h_new, y, stats, weight, post_weight=None, post_bias=None, gate=None, residual_scale=1.0, block_scale=1.0,
+                           centered=False, biased=False):
+    """Gradients of residual_norm_forward from those of h_new and of a (one of the two may be None) -> (dh, dy, dweight, dbias, dpost_weight,
+    dpost_bias, dgate), None where there is none."""
+    return _native.residual_norm_backward(dh_new, da, h_new, y, stats, weight, post_weight, post_bias, gate, residual_scale, block_scale, centered,
+                                          biased, _stream(y))
+
+
+# ---- orthogonalised updates --------------------------------------------------------------------------------------------
+def orthogonalize(x, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7):
+    """Every matrix of x [.., rows, columns] with its singular values driven towards 1 -> a new tensor: x / (|x| + eps), then `steps` times
+    X <- a X + b (X X^T) X + c (X X^T)^2 X; see rl_orthogonalize.  coefficients: (a, b, c), or one such triple a step."""
+    try:
+        triples = [coefficients] * steps if not hasattr(coefficients[0], "__len__") else coefficients
+        table = [(float(a), float(b), float(c)) for a, b, c in triples]
+    except (TypeError, ValueError):
+        table = []
+    if len(table) != steps:
+        _refuse("1 to 64 steps; coefficients are three numbers, or three numbers for each step")
+    table = [v for triple in table for v in triple]
+    return _native.orthogonalize(x, table, eps, _stream(x))
+
+
 # ---- torch.autograd --------------------------------------------------------------------------------------------------
 class _Norm(torch.autograd.Function):
     @staticmethod
@@ -159,6 +209,44 @@ class _TokenLogprobs(torch.autograd.Function):
         return (*token_logprobs_backward(dlogp.contiguous(), hidden, weight, targets, lse, ctx.temperature), None, None)
 
 
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, up, up_bias, activation, residual, keep):
+        y, kept = linear_forward(x, weight, bias, up, up_bias, activation, residual, keep)
+        ctx.save_for_backward(x, weight, up, kept)
+        ctx.activation = activation
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, up, kept = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        grads = (None,) * 5
+        if any(need[:5]):
+            dx, dw, db, dup, dub = linear_backward(dy, x, weight, kept, up, ctx.activation, need[2], need[4], (need[0], need[1], need[3]))
+            grads = dx, dw, db, dup, dub
+        return (*grads, None, dy if need[6] else None, None)
+
+
+class _ResidualNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, h, y, weight, bias, post_weight, post_bias, gate, residual_scale, block_scale, eps, centered):
+        h_new, a, stats = residual_norm_forward(h, y, weight, bias, post_weight, post_bias, gate, residual_scale, block_scale, eps, centered)
+        ctx.save_for_backward(h_new, y, stats, weight, post_weight, post_bias, gate)
+        ctx.rest = residual_scale, block_scale, centered, bias is not None
+        ctx.set_materialize_grads(False)
+        return h_new, a
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh_new, da):
+        h_new, y, stats, weight, post_weight, post_bias, gate = ctx.saved_tensors
+        if dh_new is None and da is None:
+            return (None,) * 11
+        return (*residual_norm_backward(dh_new, da, h_new, y, stats, weight, post_weight, post_bias, gate, *ctx.rest), None, None, None, None)
+
+
 def norm(x, weight, bias=None, eps=1e-6, centered=False):
     """Differentiable norm_forward -> y."""
     return _Norm.apply(x, weight, bias, eps, centered)
@@ -177,3 +265,14 @@ def attention(q, k, v, cu_q, cu_k, causal=True, scale=None):
 def token_logprobs(hidden, weight, targets, temperature=1.0):
     """Differentiable token_logprobs_forward -> logp.  Its backward pass forms both gradients, also where only one is asked for."""
     return _TokenLogprobs.apply(hidden, weight, targets, temperature)
+
+
+def linear(x, weight, bias=None, up=None, up_bias=None, activation="none", residual=None):
+    """Differentiable linear_forward -> y."""
+    keep = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias, up, up_bias))
+    return _Linear.apply(x, weight, bias, up, up_bias, activation, residual, keep)
+
+
+def residual_norm(h, y, weight, bias=None, post_weight=None, post_bias=None, gate=None, residual_scale=1.0, block_scale=1.0, eps=1e-6, centered=False):
+    """Differentiable residual_norm_forward -> (h_new, a)."""
+    return _ResidualNorm.apply(h, y, weight, bias, post_weight, post_bias, gate, residual_scale, block_scale, eps, centered)

@@ -1,0 +1,582 @@
+"""Linear layers, the residual stream with its norms and orthogonalised updates on the GPU against their formulas in float64, at sizes where tiles,
+slices, strides and types can go wrong.  Bounds: tests/balls.py, and for the orthogonalised updates the roundings of the method itself."""
+import math
+
+import pytest
+import torch
+import torch.nn.functional as F
+
+from balls import E32, Ball, unit, within
+from paper_2509_06980_amd import policy_ops as ops
+from paper_2509_06980_amd.binding import RolloutError
+
+pytestmark = pytest.mark.gpu
+BF, FP = torch.bfloat16, torch.float32
+
+
+def gen(seed):
+    return torch.Generator("cuda").manual_seed(seed)
+
+
+def randn(g, *shape, dt=FP, std=1.0):
+    return (torch.randn(*shape, generator=g, device="cuda") * std).to(dt)
+
+
+# ---- linear layers -------------------------------------------------------------------------------------------------
+def activated(z, name):
+    """act(z) and act'(z) as Balls.  The functions' own evaluation: 32 roundings of the value's size and of |z|; slopes are at most 1.2, their own slopes
+    at most 1."""
+    x = z.v.clone().requires_grad_()
+    f = {"none": lambda v: v * 1.0, "relu": F.relu, "silu": F.silu, "gelu": F.gelu, "gelu_tanh": lambda v: F.gelu(v, approximate="tanh")}[name]
+    y = f(x)
+    slope, = torch.autograd.grad(y.sum(), x)
+    own = 0.0 if name in ("none", "relu") else 32 * E32
+    value = Ball(y.detach(), (1.2 if own else 1.0) * z.e + own * z.v.abs())
+    if name == "none":
+        return value, Ball(slope)
+    jump = (z.v.abs() <= z.e).double() if name == "relu" else 0.0      # the slope of relu where z may have either sign
+    return value, Ball(slope, (z.e if name != "relu" else 0.0) + 2 * own + jump)
+
+
+def linear_reference(x, w, b, u, ub, act, r, dy):
+    dt = x.dtype
+    x, w = Ball(x), Ball(w)
+    z = x @ w.t()
+    z = z if b is None else z + Ball(b)
+    value, slope = activated(z, act)
+    y, out = value, {}
+    dyb = Ball(dy)
+    dz = dyb * slope
+    if u is not None:
+        u = Ball(u)
+        up = x @ u.t()
+        up = up if ub is None else up + Ball(ub)
+        y, dz, du = value * up, dz * up, dyb * value
+    if r is not None:
+        y = y + Ball(r)
+    out["y"] = y
+    operand = dz.rounded(dt)
+    dx = operand @ w
+    out["dw"], out["db"] = operand.t() @ x, dz.sum(0)
+    if u is not None:
+        operand = du.rounded(dt)
+        dx = dx + operand @ u
+        out["dup"], out["dub"] = operand.t() @ x, du.sum(0)
+    out["dx"] = dx
+    return out
+
+
+def linear_case(g, rows, inner, outer, dt, gated=False, bias=True, residual=None):
+    case = dict(x=randn(g, rows, inner, dt=dt), w=randn(g, outer, inner, dt=dt, std=inner ** -0.5), b=randn(g, outer, dt=dt) if bias else None,
+                u=randn(g, outer, inner, dt=dt, std=inner ** -0.5) if gated else None, ub=randn(g, outer, dt=dt) if gated and bias else None,
+                r=None if residual is None else randn(g, rows, outer, dt=residual))
+    return case, randn(g, rows, outer, dt=residual or dt)
+
+
+def linear_check(case, dy, act, wanted=(True, True, True)):
+    c = case
+    y, kept = ops.linear_forward(c["x"], c["w"], c["b"], up=c["u"], up_bias=c["ub"], activation=act, residual=c["r"], keep=True)
+    assert torch.equal(y, ops.linear_forward(c["x"], c["w"], c["b"], up=c["u"], up_bias=c["ub"], activation=act, residual=c["r"])[0])
+    dx, dw, db, dup, dub = ops.linear_backward(dy, c["x"], c["w"], kept, up=c["u"], activation=act, biased=c["b"] is not None,
+                                               up_biased=c["ub"] is not None, wanted=wanted)
+    want = linear_reference(c["x"], c["w"], c["b"], c["u"], c["ub"], act, c["r"], dy)
+    got = dict(y=y, dx=dx, dw=dw, db=db, dup=dup, dub=dub)
+    assert [dx is not None, dw is not None, dup is not None] == [wanted[0], wanted[1], wanted[2] and c["u"] is not None]
+    for name, t in got.items():
+        if t is not None:
+            within(name, t, want[name])
+    return got
+
+
+@pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("rows,inner,outer", [(1, 1, 1), (1, 8, 8), (2, 7, 9), (1, 256, 512), (3, 33, 65), (61, 257, 517), (64, 64, 64), (65, 72, 136), (127, 128, 129),
+                                              (130, 264, 40), (300, 40, 700), (257, 520, 264), (700, 1000, 24), (16, 4096, 48), (5, 2048, 1000), (1100, 96, 300)])
+def test_linear(rows, inner, outer, gated, dt):
+    g = gen(rows + 3 * inner + 7 * outer)
+    act = ["silu", "gelu", "gelu_tanh", "relu", "none"][(rows + inner + outer) % (4 if not gated else 5)]
+    case, dy = linear_case(g, rows, inner, outer, dt, gated)
+    linear_check(case, dy, act)
+
+
+@pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu", "gelu_tanh"])
+def test_linear_activations_and_residuals(act, dt):
+    for i, (gated, bias, residual) in enumerate([(False, False, None), (False, True, FP), (True, False, dt), (False, False, dt), (True, True, FP)]):
+        case, dy = linear_case(gen(i), 70, 136, 200, dt, gated, bias, residual)
+        got = linear_check(case, dy, act)
+        assert got["y"].dtype == (residual or dt)
+
+
+@pytest.mark.parametrize("rows,inner,outer", [(1500, 2560, 1024), (4100, 512, 2600), (300, 9728, 2560)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_linear_of_large_tiles(rows, inner, outer, gated):
+    case, dy = linear_case(gen(rows), rows, inner, outer, BF, gated, True, None if gated else FP)
+    linear_check(case, dy, "silu" if gated else "none")
+
+
+def test_linear_gradients_that_are_wanted():
+    for gated in (False, True):
+        case, dy = linear_case(gen(3), 40, 72, 100, BF, gated)
+        full = linear_check(case, dy, "silu")
+        for wanted in ((True, False, False), (False, True, False), (False, False, True), (False, False, False), (True, False, True)):
+            part = linear_check(case, dy, "silu", wanted)
+            assert all(part[n] is None or torch.equal(part[n], full[n]) for n in full)
+
+
+@pytest.mark.parametrize("dt", [BF, FP])
+def test_linear_strides_and_places(dt):
+    g = gen(8)
+    rows, inner, outer = 50, 64, 88
+    wide_x, wide_w = randn(g, rows, 200, dt=dt), randn(g, 2 * outer, 104, dt=dt, std=0.2)
+    r, dy = randn(g, rows, 3 * outer, dt=FP)[:, outer:2 * outer], randn(g, rows, 2 * outer, dt=FP)[:, outer:]
+    for at in (0, 8, 3):      # in whole 16 bytes or not
+        case = dict(x=wide_x[:, at:at + inner], w=wide_w[:outer, at:at + inner], b=None, u=wide_w[outer:, at:at + inner], ub=None, r=r)
+        same = {n: t if t is None else t.contiguous() for n, t in case.items()}
+        a, b = linear_check(case, dy, "gelu"), linear_check(same, dy.contiguous(), "gelu")
+        assert all(a[n] is None or torch.equal(a[n], b[n]) for n in a)
+    # transposed, expanded, of other strides in the two weights, with leading dimensions
+    xt, wt = randn(g, inner, rows, dt=dt).t(), randn(g, inner, outer, dt=dt, std=0.2).t()
+    linear_check(dict(x=xt, w=wt, b=None, u=wide_w[:outer, :inner], ub=None, r=None), randn(g, rows, outer, dt=dt), "silu")
+    one = randn(g, 1, inner, dt=dt)
+    linear_check(dict(x=one.expand(rows, inner), w=wide_w[:outer, :inner], b=None, u=None, ub=None, r=None), randn(g, 1, outer, dt=dt).expand(rows, outer), "relu")
+    x3 = randn(g, 5, 10, inner, dt=dt)
+    w = wide_w[:outer, :inner].contiguous()
+    y3, kept = ops.linear_forward(x3, w, activation="silu", keep=True)
+    y2, kept2 = ops.linear_forward(x3.flatten(0, 1), w, activation="silu", keep=True)
+    assert y3.shape == (5, 10, outer) and torch.equal(y3.flatten(0, 1), y2) and torch.equal(kept, kept2)
+    d3 = ops.linear_backward(y3, x3, w, kept, activation="silu")
+    d2 = ops.linear_backward(y2, x3.flatten(0, 1), w, kept, activation="silu")
+    assert d3[0].shape == x3.shape and torch.equal(d3[0].flatten(0, 1), d2[0]) and torch.equal(d3[1], d2[1])
+    assert torch.equal(ops.linear_forward(x3[0, 0], w)[0], ops.linear_forward(x3[0, :1], w)[0][0])
+    transposed = x3.transpose(0, 1)
+    assert torch.equal(ops.linear_forward(transposed, w)[0], ops.linear_forward(transposed.contiguous(), w)[0])
+
+
+def test_linear_without_rows():
+    w, b = torch.ones(8, 16, device="cuda"), torch.ones(8, device="cuda")
+    x = torch.empty(0, 16, device="cuda")
+    y, kept = ops.linear_forward(x, w, b, up=w, activation="silu", keep=True)
+    grads = ops.linear_backward(y, x, w, kept, up=w, activation="silu", biased=True)
+    assert y.shape == (0, 8) and grads[0].shape == (0, 16) and all(not t.any() for t in grads[1:4]) and grads[4] is None
+
+
+@pytest.mark.parametrize("dt", [BF, FP])
+def test_linear_values_that_are_no_numbers_stay_in_their_rows(dt):
+    # 40 of 48 k in a tile of 64, rows and columns behind the last ones
+    g = gen(12)
+    for inner in (40, 35, 520):
+        x, w = randn(g, 70, inner, dt=dt), randn(g, 90, inner, dt=dt)
+        clean = ops.linear_forward(x, w)[0]
+        x[7, inner - 1], x[8, 0], w[11, 2] = math.nan, math.inf, math.nan
+        y = ops.linear_forward(x, w)[0]
+        ok = torch.ones_like(y, dtype=torch.bool)
+        ok[7], ok[8], ok[:, 11] = False, False, False
+        assert torch.equal(y[ok], clean[ok]) and y[7].isnan().all() and y[:, 11].isnan().all() and not y[8].isfinite().any()
+        dy = randn(g, 70, 90, dt=dt)
+        dx, dw, db, _, _ = ops.linear_backward(dy, x, w, biased=True)
+        assert dx[:, 3:].isfinite().all() and dx[:, 2].isnan().all()      # column 2 meets w[11, 2]
+        assert dw[:, 1:inner - 1].isfinite().all() and dw[:, inner - 1].isnan().all() and db.isfinite().all()
+        dy[5, 4] = math.nan
+        w[11, 2] = x[7, inner - 1] = x[8, 0] = 0
+        dx, dw, db, _, _ = ops.linear_backward(dy, x, w, biased=True)
+        assert dx.isnan().any(1).nonzero().flatten().tolist() == [5] and dw.isnan().any(1).nonzero().flatten().tolist() == [4]
+        assert db.isnan().nonzero().flatten().tolist() == [4]
+
+
+def test_activations_far_out():
+    x = torch.tensor([[-math.inf], [-3e38], [-200.0], [-100.0], [-20.0], [-0.0], [20.0], [100.0], [3e38], [math.inf], [math.nan]], device="cuda")
+    w = torch.ones(1, 1, device="cuda")
+    dy = torch.ones(11, 1, device="cuda")
+    for act in ("relu", "silu", "gelu", "gelu_tanh"):
+        y, kept = ops.linear_forward(x, w, activation=act, keep=True)
+        dx = ops.linear_backward(dy, x, w, kept, activation=act, wanted=(True, False, False))[0]
+        assert not y[:4].abs().gt(1e-35).any() and y[4].abs() < 1e-7 and torch.equal(y[6:10], x[6:10]) and y[10].isnan(), act
+        assert not dx[:4].abs().gt(1e-35).any() and torch.equal(dx[6:9], dy[6:9]), (act, dx)
+
+
+# ---- the residual stream ---------------------------------------------------------------------------------------------
+def normed(x, eps, centered):
+    d = x - x.mean() if centered else x
+    r = ((d * d).mean() + eps).rsqrt()
+    return d * r, r
+
+
+def residual_reference(c, dh, da, eps):
+    h, y = Ball(c["h"]), Ball(c["y"])
+    stream, dt = c["h"].dtype, c["y"].dtype
+    param = lambda n: None if c.get(n) is None else Ball(c[n])  # noqa: E731
+    w, b, pw, pb, g = (param(n) for n in ("w", "b", "pw", "pb", "g"))
+    centered, rs, bs = c["centered"], c["rs"], c["bs"]
+    u = y
+    if pw is not None:
+        pn, pr = normed(y, eps, centered)
+        u = pn * pw if pb is None else pn * pw + pb
+    gated = u if g is None else u * g
+    new = h * rs + gated * bs
+    out = {"h": new}
+    dH = Ball(dh) if dh is not None else Ball(torch.zeros_like(h.v))
+
+    def gradient(d, n, r):      # of a norm, from that of its n
+        t = d - n * (d * n).mean()
+        return (t - d.mean() if centered else t) * r
+
+    if w is not None:
+        n, r = normed(new, eps, centered)
+        out["a"] = n * w if b is None else n * w + b
+        if da is not None:
+            # the backward pass takes the rows of the stream as they were stored
+            kept = Ball(n.v, n.e + unit(stream) * (new.v.abs() * r.v))
+            d = Ball(da)
+            out["dw"], out["db"] = (d * kept).sum(0), d.sum(0)
+            dH = dH + gradient(d * w, kept, r)
+    out["dh"] = dH * rs
+    dU = dH * bs
+    if g is not None:
+        dg = dU * u
+        out["dg"] = dg if c["kind"] == "full" else dg.sum(0) if c["kind"] == "channel" else dg.sum(1, True)
+        dU = dU * g
+    if pw is not None:
+        out["dpw"], out["dpb"] = (dU * pn).sum(0), dU.sum(0)
+        dU = gradient(dU * pw, pn, pr)
+    out["dy"] = dU
+    return out, stream, dt
+
+
+def residual_case(g, rows, width, stream, dt, centered=False, bias=False, post=False, kind="none", rs=1.0, bs=1.0):
+    shape = {"none": None, "channel": (width,), "full": (rows, width), "row": (rows, 1)}[kind]
+    return dict(h=randn(g, rows, width, dt=stream) * 2 + 0.2, y=randn(g, rows, width, dt=dt) + 0.1, w=(1 + randn(g, width, std=0.2)).to(dt),
+                b=randn(g, width, dt=dt) if bias else None, pw=(1 + randn(g, width, std=0.2)).to(dt) if post else None,
+                pb=randn(g, width, dt=dt) if bias and post else None, g=None if shape is None else (0.5 + randn(g, *shape, std=0.3)).to(dt), kind=kind,
+                centered=centered, rs=rs, bs=bs)
+
+
+def residual_check(c, dh, da, eps=1e-6):
+    rest = dict(residual_scale=c["rs"], block_scale=c["bs"], centered=c["centered"])
+    h, a, stats = ops.residual_norm_forward(c["h"], c["y"], c["w"], c["b"], post_weight=c["pw"], post_bias=c["pb"], gate=c["g"], eps=eps, **rest)
+    got = dict(zip(("dh", "dy", "dw", "db", "dpw", "dpb", "dg"), ops.residual_norm_backward(
+        dh, da, h, c["y"], stats, c["w"], post_weight=c["pw"], post_bias=c["pb"], gate=c["g"], biased=c["b"] is not None, **rest)))
+    got |= dict(h=h, a=a)
+    want, stream, dt = residual_reference(c, dh, da, eps)
+    assert h.dtype == got["dh"].dtype == stream and all(t is None or t.dtype == dt for n, t in got.items() if n not in ("h", "dh"))
+    for name, t in got.items():
+        if t is None:
+            continue
+        if name in want:
+            within(name, t, want[name])
+        else:
+            assert not t.any(), name
+    assert [got[n] is not None for n in ("a", "dw", "db", "dpw", "dpb", "dg")] == [c[n] is not None for n in ("w", "w", "b", "pw", "pb", "g")]
+    return got
+
+
+@pytest.mark.parametrize("stream,dt", [(FP, BF), (BF, BF), (FP, FP)])
+@pytest.mark.parametrize("rows,width", [(1, 2), (1, 8), (3, 5), (1, 2560), (61, 1023), (5, 64), (700, 128), (33, 513), (130, 4096), (3, 4104), (7, 8192), (2, 16384), (3, 16392),
+                                        (2, 20001), (2100, 256), (9, 2049), (800, 1000), (5, 2048)])
+def test_residual_norm(rows, width, stream, dt):
+    g = gen(rows * 7 + width)
+    for i, (centered, bias, post, kind) in enumerate([(False, False, False, "none"), (False, False, True, "channel"), (True, True, True, "full"), (True, True, False, "row")]):
+        c = residual_case(g, rows, width, stream, dt, centered, bias, post, kind, 1.0 if i % 2 else 0.8, 0.25 if i else 1.0)
+        residual_check(c, randn(g, rows, width, dt=stream), randn(g, rows, width, dt=dt), 1e-6 if width > 8 else 1e-2)
+
+
+@pytest.mark.parametrize("stream,dt", [(FP, BF), (FP, FP)])
+@pytest.mark.parametrize("kind", ["none", "channel", "full", "row"])
+def test_residual_norm_of_one_gradient_and_without_a_norm(kind, stream, dt):
+    g = gen(5)
+    for post in (False, True):
+        c = residual_case(g, 37, 264, stream, dt, False, post, post, kind)
+        dh, da = randn(g, 37, 264, dt=stream), randn(g, 37, 264, dt=dt)
+        residual_check(c, dh, None)
+        residual_check(c, None, da)
+        c["w"] = c["b"] = None
+        got = residual_check(c, dh, None)
+        assert got["a"] is None and got["dw"] is None
+
+
+@pytest.mark.parametrize("dt", [BF, FP])
+def test_residual_norm_strides(dt):
+    g = gen(6)
+    rows, width = 45, 128
+    for at in (0, 8, 5):
+        c = residual_case(g, rows, width, FP, dt, False, False, True, "full")
+        for n in ("h", "y", "g"):
+            wide = randn(g, rows, 3 * width, dt=c[n].dtype)
+            wide[:, at:at + width] = c[n]
+            c[n] = wide[:, at:at + width]
+        dh, da = randn(g, rows, 2 * width, dt=FP)[:, at:at + width], randn(g, rows, 2 * width, dt=dt)[:, at:at + width]
+        residual_check(c, dh, da)
+    # an expanded gate has a gradient for every element; leading dimensions
+    c = residual_case(g, rows, width, FP, dt, kind="full")
+    c["g"] = c["g"][:1].expand(rows, width)
+    residual_check(c, dh, da)
+    one = ops.residual_norm_forward(c["h"].view(5, 9, width), c["y"].view(5, 9, width), c["w"], gate=c["g"].contiguous().view(5, 9, width))
+    two = ops.residual_norm_forward(c["h"], c["y"], c["w"], gate=c["g"])
+    assert all(torch.equal(a.flatten(), b.flatten()) for a, b in zip(one, two)) and one[0].shape == (5, 9, width)
+
+
+def test_residual_norm_without_rows_and_of_odd_values():
+    w = torch.ones(64, device="cuda")
+    x = torch.zeros(0, 64, device="cuda")
+    h, a, stats = ops.residual_norm_forward(x, x, w, post_weight=w, gate=w)
+    grads = ops.residual_norm_backward(h, a, h, x, stats, w, post_weight=w, gate=w)
+    assert h.shape == a.shape == grads[0].shape == (0, 64) and not any(grads[i].any() for i in (2, 4, 6))
+    x = torch.ones(6, 64, device="cuda")
+    y = torch.zeros(6, 64, device="cuda")
+    y[2, 3], y[4, 5] = math.nan, math.inf
+    h, a, stats = ops.residual_norm_forward(x, y, w)
+    assert h.isfinite().all(1).tolist() == [True, True, False, True, False, True] == a.isfinite().all(1).tolist()
+    dh, dy = ops.residual_norm_backward(x, x, h, y, stats, w)[:2]
+    assert dh[[0, 1, 3, 5]].isfinite().all() and dy[[0, 1, 3, 5]].isfinite().all() and dh[2].isnan().all()
+
+
+# ---- orthogonalised updates ------------------------------------------------------------------------------------------
+NEWTON = (3.4445, -4.7750, 2.0315)
+
+
+def newton(x, half, g, steps=5, coefficients=NEWTON, eps=1e-7, roundings=True):
+    """The steps in float64, with the method's roundings as random ones of their size where `roundings`: operands (fp16 where `half`) and the sums of k
+    products in 32 bits, each addition of which rounds a sum of the terms so far."""
+    x = x.double()
+    x = x / (x.norm() + eps)
+    tall = x.shape[0] > x.shape[1]
+    x = x.t() if tall else x
+    scale = 2.0 ** math.floor(0.5 * math.log2(max(x.shape)))
+
+    def product(a, b):
+        y = a @ b
+        if not roundings:
+            return y
+        size = torch.maximum(y.abs(), (a * a @ (b * b)).sqrt())
+        return y + torch.randn(y.shape, generator=g, device="cuda", dtype=torch.float64) * size * E32 * math.sqrt(a.shape[1]) / 2
+
+    def operand(t, s=1.0):
+        if not roundings:
+            return t
+        return (t * s).half().double() / s if half else t.float().double()
+
+    for _ in range(steps):
+        a, b, c = coefficients
+        xo = operand(x, scale)
+        gram = operand(product(xo, xo.t()))
+        poly = b * gram + c * product(gram, gram)
+        if roundings:
+            diagonal = poly.diagonal().float().double()
+            poly = operand(poly)
+            poly.diagonal().copy_(diagonal)
+        x = a * x + product(poly, xo)
+        x = x.float().double() if roundings else x
+    return x.t() if tall else x
+
+
+def matrices(g, count, rows, columns, dt, kind):
+    if kind == "noise":
+        x = torch.randn(count, rows, columns, generator=g, device="cuda")
+    else:
+        r = min(rows, columns, 8)
+        x = torch.randn(count, rows, r, generator=g, device="cuda") @ torch.randn(count, r, columns, generator=g, device="cuda")
+        x = x + 0.3 * torch.randn(count, rows, columns, generator=g, device="cuda")
+    return (x * 1e-3).to(dt)
+
+
+def orthogonal_check(x, got, half):
+    """Errors of a matrix are sums of many roundings: of twice the size of the model's at most, together with the last rounding; the largest of n below what a
+    normal variable exceeds once in 10^4 times n, of a spread that differs by 4 between directions."""
+    g = gen(1)
+    for m, y in zip(x.reshape(-1, *x.shape[-2:]), got.reshape(-1, *x.shape[-2:])):
+        want = newton(m, half, g, roundings=False)
+        model = (newton(m, half, g) - want).norm()
+        last = unit(x.dtype) * want.norm()
+        off = (y.double() - want).norm()
+        assert off <= 2 * model + last + 1e-6 * want.norm(), (off / want.norm(), model / want.norm())
+        z = math.sqrt(2 * math.log(1e4 * m.numel()))
+        biggest = ((y.double() - want).abs() - unit(x.dtype) * want.abs()).max()
+        assert biggest <= 4 * z * (2 * model / math.sqrt(m.numel()) + 1e-6), (biggest, model)
+
+
+@pytest.mark.parametrize("dt", [BF, FP])
+@pytest.mark.parametrize("kind", ["noise", "strong"])
+@pytest.mark.parametrize("count,rows,columns", [(1, 1, 1), (2, 1, 9), (3, 8, 8), (1, 64, 33), (2, 65, 130), (1, 129, 127), (2, 256, 256), (3, 512, 256), (1, 300, 700), (2, 1000, 264),
+                                                (1, 257, 1023), (5, 40, 2000)])
+def test_orthogonalize(count, rows, columns, kind, dt):
+    x = matrices(gen(rows + columns), count, rows, columns, dt, kind)
+    before = x.clone()
+    got = ops.orthogonalize(x)
+    assert torch.equal(x, before) and got.shape == x.shape and got.dtype == dt
+    orthogonal_check(x, got, dt == BF and min(rows, columns) >= 256)
+
+
+@pytest.mark.parametrize("rows,columns", [(1024, 2304), (2560, 1024)])
+def test_orthogonalize_of_large_tiles(rows, columns):
+    x = matrices(gen(rows), 3, rows, columns, BF, "strong")
+    got = ops.orthogonalize(x)
+    orthogonal_check(x, got, True)
+    assert all(torch.equal(ops.orthogonalize(x[i]), got[i]) for i in range(3))
+    s = torch.linalg.svdvals(got[0].float())
+    assert 0.5 < s.min() and s.max() < 1.3      # where the steps drive singular values to, but for the smallest ones
+
+
+def test_orthogonalize_strides_coefficients_and_odd_values():
+    g = gen(4)
+    wide = randn(g, 4, 70, 100)
+    x = wide[:, 3:60, 5:90]
+    assert torch.equal(ops.orthogonalize(x), ops.orthogonalize(x.contiguous()))
+    assert torch.equal(ops.orthogonalize(x.transpose(1, 2)), ops.orthogonalize(x.transpose(1, 2).contiguous()))
+    assert torch.equal(ops.orthogonalize(x.view(2, 2, 57, 85) if x.is_contiguous() else x.reshape(2, 2, 57, 85)).view(4, 57, 85), ops.orthogonalize(x))
+    assert torch.equal(ops.orthogonalize(x, steps=3), ops.orthogonalize(x, coefficients=[NEWTON] * 3, steps=3))
+    cubic = ops.orthogonalize(wide[0, :20, :20], steps=40, coefficients=(1.5, -0.5, 0.0))      # Newton's own: all singular values to 1
+    assert torch.allclose(cubic @ cubic.t(), torch.eye(20, device="cuda"), atol=1e-4)
+    x = randn(g, 5, 300, 260, dt=BF)
+    clean = ops.orthogonalize(x)
+    x[1, 7, 3], x[3] = math.nan, 0.0
+    x[4] *= 2.0 ** 100
+    got = ops.orthogonalize(x)
+    assert got[1].isnan().all() and not got[3].any() and torch.equal(got[[0, 2]], clean[[0, 2]]) and got[4].isfinite().all()
+    assert torch.allclose(got[4].float(), clean[4].float(), atol=1e-2)      # 1e-7 in the norm is all that its size changes
+    # coefficients whose values leave fp16: in 32 bits
+    wild = ops.orthogonalize(x[0], steps=2, coefficients=(500.0, 0.0, 0.0))
+    assert torch.allclose(wild.float(), x[0].float() / x[0].float().norm() * 250000.0, rtol=2.0 ** -7)
+    assert ops.orthogonalize(x[:0]).shape == (0, 300, 260)
+
+
+# ---- together: gradients, repetition, streams, graphs -----------------------------------------------------------------
+def test_gradients_against_differences_of_the_formulas():
+    g = gen(21)
+    n, hidden, inter = 14, 24, 40
+    x = [randn(g, n, hidden), randn(g, n, hidden), randn(g, inter, hidden, std=0.3), randn(g, inter, hidden, std=0.3), randn(g, hidden, inter, std=0.3),
+         1 + randn(g, hidden, std=0.2), 1 + randn(g, hidden, std=0.2), randn(g, hidden), randn(g, inter)]
+    c, d = randn(g, n, hidden), randn(g, n, hidden)
+
+    def through_the_kernels(h, y, wg, wu, wd, w, pw, gate, b):
+        h, a = ops.residual_norm(h, y, w, post_weight=pw, gate=gate, block_scale=0.5)
+        m = ops.linear(a, wg, b, up=wu, activation="silu")
+        h = ops.linear(m, wd, residual=h)
+        h, a = ops.residual_norm(h, h * 0.1, w, centered=True)
+        return (h * c + a * d).sum()
+
+    def in_64_bits(h, y, wg, wu, wd, w, pw, gate, b):
+        rms = lambda v: v / (v.square().mean(-1, keepdim=True) + 1e-6).sqrt()  # noqa: E731
+        h = h + 0.5 * gate * rms(y) * pw
+        a = rms(h) * w
+        h = h + (F.silu(a @ wg.t() + b) * (a @ wu.t())) @ wd.t()
+        h = h * 1.1
+        e = h - h.mean(-1, keepdim=True)
+        return (h * c.double() + rms(e) * w * d.double()).sum()
+
+    leaves = [t.clone().requires_grad_() for t in x]
+    value = through_the_kernels(*leaves)
+    value.backward()
+    x64 = [t.double() for t in x]
+    assert abs(value.item() - in_64_bits(*x64).item()) < 1e-3
+    for i in range(len(x)):
+        v = torch.randn(x[i].shape, generator=g, device="cuda", dtype=torch.float64)
+        h = 1e-5
+        plus, minus = ([t + (s * h * v if j == i else 0) for j, t in enumerate(x64)] for s in (1, -1))
+        slope = ((in_64_bits(*plus) - in_64_bits(*minus)) / (2 * h)).item()
+        got = (leaves[i].grad.double() * v).sum().item()
+        # differences: h^2 times third derivatives and 1e-16 / h; gradients: fp32 over sums of some hundred terms
+        size = (leaves[i].grad.double() * v).abs().sum().item()
+        assert abs(got - slope) < 2e-5 * size + 1e-6, (i, got, slope)
+
+
+def test_gradients_of_parts():
+    g = gen(22)
+    x, w, r = randn(g, 9, 16), randn(g, 24, 16).requires_grad_(), randn(g, 9, 24).requires_grad_()
+    with torch.no_grad():
+        assert not ops.linear(x, w, activation="silu").requires_grad
+    ops.linear(x, w, activation="silu", residual=r).sum().backward()
+    assert torch.equal(r.grad, torch.ones_like(r)) and w.grad is not None
+    frozen = ops.linear(x, w.detach(), activation="silu", residual=r)
+    r.grad = None
+    frozen.sum().backward()
+    assert torch.equal(r.grad, torch.ones_like(r))
+    h = randn(g, 9, 16).requires_grad_()
+    new, a = ops.residual_norm(h, x, torch.ones(16, device="cuda"))
+    one, = torch.autograd.grad(new.sum(), h, retain_graph=True)
+    assert torch.equal(one, torch.ones_like(h))
+    both = torch.autograd.grad(new.sum() + a.sum(), h)[0]
+    other = torch.autograd.grad(ops.residual_norm(h, x, torch.ones(16, device="cuda"))[1].sum(), h)[0]
+    assert torch.allclose(both, one + other, atol=1e-5)
+
+
+def _everything(dt, seed):
+    g = gen(seed)
+    case, dy = linear_case(g, 300, 264, 520, dt, True, True, FP)
+    tall, dy2 = linear_case(g, 30, 2048, 72, dt)
+    c = residual_case(g, 300, 520, FP, dt, True, True, True, "channel")
+    da, x = randn(g, 300, 520, dt=dt), matrices(g, 3, 300, 520, dt, "strong")
+
+    def run():
+        out = []
+        for k, d in ((case, dy), (tall, dy2)):
+            y, kept = ops.linear_forward(k["x"], k["w"], k["b"], up=k["u"], up_bias=k["ub"], activation="gelu", residual=k["r"], keep=True)
+            out += [y, *ops.linear_backward(d, k["x"], k["w"], kept, up=k["u"], activation="gelu", biased=True, up_biased=k["u"] is not None)]
+        h, a, stats = ops.residual_norm_forward(c["h"], c["y"], c["w"], c["b"], post_weight=c["pw"], post_bias=c["pb"], gate=c["g"], centered=True)
+        out += [h, a, *ops.residual_norm_backward(h, da, h, c["y"], stats, c["w"], post_weight=c["pw"], post_bias=c["pb"], gate=c["g"], centered=True, biased=True)]
+        return [t for t in out + [ops.orthogonalize(x)] if t is not None]
+    return run
+
+
+@pytest.mark.parametrize("dt", [BF, FP])
+def test_the_same_bits_again_on_another_stream_and_in_a_graph(dt):
+    run = _everything(dt, 31)
+    first = [t.clone() for t in run()]
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(first, run()))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        second = run()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, second))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = run()
+    for _ in range(3):
+        for t in captured:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(first, captured))
+        assert all(torch.equal(a, b) for a, b in zip(first, run()))
+
+
+def test_a_row_does_not_depend_on_the_rows_beside_it_for_the_same_plan():
+    g = gen(33)
+    x, w = randn(g, 200, 264, dt=BF), randn(g, 520, 264, dt=BF)
+    y = ops.linear_forward(x, w)[0]
+    shuffled = torch.randperm(200, generator=g, device="cuda")
+    assert torch.equal(ops.linear_forward(x[shuffled], w)[0], y[shuffled])
+
+
+# ---- refusals --------------------------------------------------------------------------------------------------------
+def test_refusals():
+    x, w, b = torch.ones(4, 8, device="cuda"), torch.ones(6, 8, device="cuda"), torch.ones(6, device="cuda")
+    y, kept = ops.linear_forward(x, w, activation="silu", keep=True)
+    v = torch.ones(8, device="cuda")
+    h, a, stats = ops.residual_norm_forward(x, x, v)
+    calls = [
+        lambda: ops.linear_forward(x.half(), w.half()), lambda: ops.linear_forward(x, w.to(BF)), lambda: ops.linear_forward(x, w.t()), lambda: ops.linear_forward(x, w[0]),
+        lambda: ops.linear_forward(x, w, b[:3]), lambda: ops.linear_forward(x, w, b.to(BF)), lambda: ops.linear_forward(x, w, activation="tanh"),
+        lambda: ops.linear_forward(x, w, up=w[:3]), lambda: ops.linear_forward(x, w, up_bias=b), lambda: ops.linear_forward(x, w, residual=x),
+        lambda: ops.linear_forward(x, w, residual=y.double()), lambda: ops.linear_forward(x, w, residual=y.to(BF)), lambda: ops.linear_forward(x, w.cpu()),
+        lambda: ops.linear_forward(x[:, :0], w[:, :0]), lambda: ops.linear_forward(x, w[:0]),
+        lambda: ops.linear_backward(y, x, w, activation="silu"), lambda: ops.linear_backward(y, x, w, kept[:2], activation="silu"),
+        lambda: ops.linear_backward(y[:2], x, w, kept, activation="silu"), lambda: ops.linear_backward(y.to(BF), x, w, kept, activation="silu"),
+        lambda: ops.linear_backward(y, x, w, kept, activation="silu", up_biased=True), lambda: ops.linear_backward(y, x, w, kept.to(BF), activation="silu"),
+        lambda: ops.linear_backward(y, x, w, kept, up=w, activation="silu"),
+        lambda: ops.residual_norm_forward(x, x, v[:4]), lambda: ops.residual_norm_forward(x, x[:2], v), lambda: ops.residual_norm_forward(x.to(BF), x, v),
+        lambda: ops.residual_norm_forward(x, x, v, post_bias=v), lambda: ops.residual_norm_forward(x, x, None, v), lambda: ops.residual_norm_forward(x, x, v, gate=v[:4]),
+        lambda: ops.residual_norm_forward(x, x, v, gate=x[:2]), lambda: ops.residual_norm_forward(x, x, v, eps=-1.0), lambda: ops.residual_norm_forward(x, x, v, eps=math.nan),
+        lambda: ops.residual_norm_forward(x, x, v, gate=v.to(BF)), lambda: ops.residual_norm_forward(x.cpu(), x.cpu(), v.cpu()),
+        lambda: ops.residual_norm_backward(None, None, h, x, stats, v), lambda: ops.residual_norm_backward(x, x[:2], h, x, stats, v),
+        lambda: ops.residual_norm_backward(x, x, h, x, stats[:2], v), lambda: ops.residual_norm_backward(x, x, h, x, stats, None),
+        lambda: ops.residual_norm_backward(x.to(BF), x, h, x, stats, v),
+        lambda: ops.orthogonalize(x[0]), lambda: ops.orthogonalize(x.half()), lambda: ops.orthogonalize(x.cpu()), lambda: ops.orthogonalize(x, steps=0),
+        lambda: ops.orthogonalize(x, steps=65), lambda: ops.orthogonalize(x, eps=-1.0), lambda: ops.orthogonalize(x, coefficients=(1.0, math.nan, 0.0)),
+        lambda: ops.orthogonalize(x, coefficients=(1.0, 2.0)), lambda: ops.orthogonalize(x, coefficients=[(1.0, 2.0)] * 5),
+    ]
+    for i, call in enumerate(calls):
+        with pytest.raises(RolloutError):
+            call()
+            pytest.fail(f"call {i} was not refused")
