@@ -111,6 +111,77 @@ struct Finish {
   }
 };
 
+// ---- few rows ---------------------------------------------------------------------------------------------------------------------
+// Up to 16 rows: bound by the weights' bytes.  A workgroup takes 16 rows of W (and of U) and all rows of x; its waves share k, operands go from memory straight
+// into registers (weights as the row operand of 16x16x32 instructions, fp32 16x16x4; a lane's 16 bytes are 8 or 4 k of one row), and the waves'
+// sums are added in LDS in a fixed order.  x comes from the caches.  What a block of 16 rows has too many reads the last row again and is not stored.
+// One row x 4096 x 2560 with a residual: 7.3 us, by the tiles of many rows 14.  From 17 rows on those tiles are faster (37 rows x 2560 x 9728, gated, weights from
+// memory: 33 + 5 us for the slices' sums, this way with three blocks of rows 50).
+const int kFewRows = 16, kFewWaves = 8;
+template <typename T, typename EPI>
+__global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(const T* __restrict__ x, int64_t x_ld, const T* __restrict__ w, int64_t w_ld, int64_t second,
+                                                                  int rows, int k, int outer, EPI epi) {
+  constexpr int E = 16 / sizeof(T), KS = 4 * E, M = EPI::GATED ? 2 : 1, U = 8, V = kPiece<T>;
+  __shared__ float sums[M][kFewWaves][16][17];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n0 = blockIdx.x * 16, r = lane & 15, kl = lane / 16 * E;
+  const T* const wp = w + (int64_t)min(n0 + r, outer - 1) * w_ld + kl;
+  const T* const xp = x + (int64_t)min(r, rows - 1) * x_ld + kl;
+  f32x4 acc[M];
+#pragma unroll
+  for (int m = 0; m < M; m++) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int steps = (k + KS - 1) / KS, begin = slice_begin(wave, kFewWaves, steps), end = slice_begin(wave + 1, kFewWaves, steps);
+  for (int s = begin; s < end; s += U) {
+    u32x4 a[U][M], b[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int at = (s + u) * KS;
+      b[u] = u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int m = 0; m < M; m++) a[u][m] = u32x4{0, 0, 0, 0};
+      if (s + u < end && at + kl < k) {
+#pragma unroll
+        for (int m = 0; m < M; m++) a[u][m] = *(const u32x4*)(wp + (m ? second : 0) + at);
+        b[u] = *(const u32x4*)(xp + at);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++)
+#pragma unroll
+      for (int m = 0; m < M; m++) {
+        if constexpr (sizeof(T) == 2) {
+          acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[u][m]), __builtin_bit_cast(bf16x8, b[u]), acc[m], 0, 0, 0);
+        } else {
+          const f32x4 p = __builtin_bit_cast(f32x4, a[u][m]), q = __builtin_bit_cast(f32x4, b[u]);
+#pragma unroll
+          for (int e = 0; e < 4; e++) acc[m] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[e], q[e], acc[m], 0, 0, 0);
+        }
+      }
+  }
+#pragma unroll
+  for (int m = 0; m < M; m++)
+#pragma unroll
+    for (int e = 0; e < 4; e++) sums[m][wave][r][lane / 16 * 4 + e] = acc[m][e];
+  __syncthreads();
+  constexpr int PIECES = 16 / V;
+  const int i = threadIdx.x, row = i / PIECES, c = i % PIECES * V;
+  if (row >= rows || n0 + c >= outer) return;
+  float v[V], u[V];
+#pragma unroll
+  for (int e = 0; e < V; e++) {
+    v[e] = u[e] = 0.f;
+#pragma unroll
+    for (int q = 0; q < kFewWaves; q++) {
+      v[e] += sums[0][q][row][c + e];
+      if constexpr (M == 2) u[e] += sums[1][q][row][c + e];
+    }
+  }
+  epi(0, row, n0 + c, v, u);
+}
+template <typename T, typename EPI>
+void launch_few_rows(const T* x, int64_t x_ld, const T* w, int64_t w_ld, int64_t second, int rows, int k, int outer, const EPI& epi, hipStream_t s) {
+  if (!probe) few_rows_kernel<T, EPI><<<(outer + 15) / 16, 64 * kFewWaves, 0, s>>>(x, x_ld, w, w_ld, second, rows, k, outer, epi);
+}
+
 // ---- rows of an operand in whole 16 bytes: [rows][ld], zeros behind `width` -----------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(256) void copy_rows_kernel(const T* __restrict__ x, int64_t stride, int64_t rows, int width, int ld, T* __restrict__ to) {
@@ -124,7 +195,7 @@ __global__ __launch_bounds__(256) void copy_rows_kernel(const T* __restrict__ x,
 
 // ---- dz and du, and their sums over rows --------------------------------------------------------------------------------------
 // A thread takes 8 columns of every fourth row of a workgroup's share of rows.  Bound by memory.
-const int kGradColumns = 512, kGradShares = 64;
+const int kGradColumns = 512, kGradShares = 256;
 template <typename T>
 struct Gradient {
   const void* dy;
@@ -259,18 +330,24 @@ template <typename T>
 int64_t segment_rows(int64_t ld) { return std::max<int64_t>((1ll << 31) / (ld * (int64_t)sizeof(T)) / kChunk<T> * kChunk<T>, kChunk<T>); }
 
 template <typename T>
-Plan forward_plan(const Shape& n) { return plan_of<T>(n.rows, n.outer, 1, chunks<T>(n.inner), false, n.mats == 2); }
+Plan forward_plan(const Shape& n) {      // results, and as a guess a residual or what is kept of each matrix
+  return plan_of<T>({n.rows, n.outer, 1, chunks<T>(n.inner), false, n.mats == 2, false, n.mats == 2 ? 10.f : 8.f});
+}
 template <typename T>
-Plan dx_plan(const Shape& n) { return plan_of<T>(n.rows, n.inner, 1, (int64_t)chunks<T>(n.outer) * n.mats, false, false); }
+Plan dx_plan(const Shape& n) { return plan_of<T>({n.rows, n.inner, 1, (int64_t)chunks<T>(n.outer) * n.mats, false, false, true, (float)sizeof(T)}); }
 template <typename T>
-Plan dw_plan(const Shape& n, int batches) { return plan_of<T>(n.outer, n.inner, batches, chunks<T>(n.rows), false, false); }
+Plan dw_plan(const Shape& n, int batches) { return plan_of<T>({n.outer, n.inner, batches, chunks<T>(n.rows), false, false, true, (float)sizeof(T)}); }
 
 template <typename T>
 int64_t forward_room(const Shape& n, bool x_direct, bool w_direct) {
   return (x_direct ? 0 : copy_bytes<T>(n.rows, n.inner)) + (w_direct ? 0 : n.mats * copy_bytes<T>(n.outer, n.inner)) +
-         up(part_bytes(forward_plan<T>(n), n.rows, n.outer, 1, n.mats == 2), kAlign);
+         (n.rows <= kFewRows ? 0 : up(part_bytes(forward_plan<T>(n), n.rows, n.outer, 1, n.mats == 2), kAlign));
 }
-int shares_of(int rows) { return std::min((rows + 15) / 16, kGradShares); }
+// Shares of rows: enough workgroups for the card, four rows each (of a wave one) at least
+int shares_of(const Shape& n) {
+  const int strips = (n.outer + kGradColumns - 1) / kGradColumns;
+  return std::min({(n.rows + 3) / 4, std::max(2048 / strips, 1), kGradShares});
+}
 template <typename T>
 int64_t backward_room(const Shape& n, bool x_direct, bool w_direct) {
   const int64_t dz = n.mats * up((int64_t)n.rows * up(n.outer, 8) * (int64_t)sizeof(T), kAlign);
@@ -331,7 +408,7 @@ int forward(const Shape& n, const Forward& f, void* ws, hipStream_t s) {
   p.b = {w.p, w.ld, 0, 0, n.outer, n.outer, w.width, w.width, w.elements};
   p.rows = n.rows, p.cols = n.outer;
   const Plan plan = forward_plan<T>(n);
-  p.part = (float*)room.take(part_bytes(plan, n.rows, n.outer, 1, n.mats == 2));
+  if (n.rows > kFewRows) p.part = (float*)room.take(part_bytes(plan, n.rows, n.outer, 1, n.mats == 2));
   auto finish = [&](auto e) {
     e.y = f.y, e.cols = n.outer, e.act = f.act, e.wide = f.wide, e.bias = (const T*)f.bias, e.up_bias = (const T*)f.up_bias;
     e.residual = f.residual, e.residual_stride = f.residual_stride, e.kept = f.kept;
@@ -339,14 +416,18 @@ int forward(const Shape& n, const Forward& f, void* ws, hipStream_t s) {
             aligned16(f.kept);
     return e;
   };
+  auto product = [&](const auto& e) {
+    if (n.rows <= kFewRows) launch_few_rows<T>(x.p, x.ld, w.p, w.ld, p.b2, n.rows, w.width, n.outer, e, s);
+    else launch<T, false, false>(p, plan, e, s);
+  };
   if (n.mats == 2) {
     p.b2 = u.p - w.p;
     if (probe) p.b2 = 0, p.b.elements = std::min(w.elements, u.elements);
-    launch<T, false, false>(p, plan, finish(Finish<T, true, false>{}), s);
+    product(finish(Finish<T, true, false>{}));
   } else if (f.act == RL_ACT_NONE && !f.bias && !f.residual && !f.kept) {
-    launch<T, false, false>(p, plan, finish(Finish<T, false, true>{}), s);
+    product(finish(Finish<T, false, true>{}));
   } else {
-    launch<T, false, false>(p, plan, finish(Finish<T, false, false>{}), s);
+    product(finish(Finish<T, false, false>{}));
   }
   return probe ? RL_OK : launched();
 }
@@ -372,7 +453,7 @@ int backward(const Shape& n, const Backward& f, void* ws, hipStream_t s) {
   // gradients of the products' sums
   const bool same = f.act == RL_ACT_NONE && n.mats == 1 && (!f.wide || sizeof(T) == 4) && direct<T>(f.dy, f.dy_stride, n.outer);
   In<T> dz{(const T*)f.dy, f.dy_stride, n.outer, (n.rows - 1) * f.dy_stride + n.outer};
-  const int ldz = (int)up(n.outer, 8), shares = shares_of(n.rows);
+  const int ldz = (int)up(n.outer, 8), shares = shares_of(n);
   T* own = nullptr;
   if (!same) {
     own = (T*)room.take(n.mats * up((int64_t)n.rows * ldz * (int64_t)sizeof(T), kAlign));

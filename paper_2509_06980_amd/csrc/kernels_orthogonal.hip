@@ -11,60 +11,78 @@ using namespace product;
 // X B, so that A has the smaller of the two sizes and nothing is transposed).  Singular values s become p(s) = a s + b s^3 + c s^5, again and
 // again; the singular vectors stay.
 // A and B are symmetric: tiles on and under the diagonal are computed, the others are stored from them.
-// Bound by the matrix units.  fp32: everything in 32 bits.  bf16: the operands of the products are rounded to fp16 (11 bits instead of the 8 of bf16, at
-// the same rate), X times a power of two so that its elements lie in the middle of that range, and X itself is kept in 32 bits beside them, since a X
-// carries the small singular values, which the steps enlarge (500 times in five of them) with whatever roundings are in them.  A's diagonal, near 1 towards
-// the end, is what the rounding of B would cost most, so B's diagonal is kept in 32 bits too.  Relative error of the result against 64 bits, of
-// which its last rounding alone is 0.0017: 0.0017 to 0.0022 (rounded products without the 32 bits beside them: 0.02 for a matrix of 32 strong directions over
-// a floor of noise; operands in bf16: 0.2).  Matrices with a side below 256 take the fp32 products, where these cost nothing: fp16's error is largest there.
+// Bound by the matrix units, and the last product of a step by memory too.  fp32: everything in 32 bits.  bf16: the operands of the products are rounded to fp16
+// (11 bits instead of the 8 of bf16, at the same rate), X times a power of two so that its elements lie in the middle of that range.  What the rounding of X
+// leaves is kept beside it in fp16 where more than one step follows, since a X carries the small singular values, which the steps enlarge (500 times in five of
+// them) with whatever roundings are in them; the first X is exact as it is.  B's diagonal, near b + c towards the end, is kept in 32 bits.  Relative error of the
+// result against 64 bits, of which its last rounding alone is 0.0017: 0.0017 to 0.0021 (fp16 alone: 0.02 for a matrix of 32 strong directions over a floor of
+// noise; operands in bf16: 0.2).  Matrices with a side below 256 take the fp32 products, where these cost nothing: fp16's error is largest there.
 // =============================================================================================
-const int kNormShares = 64;
+const int kNormShares = 1024;
 const int kHalfFrom = 256;
+const float kLow = 2048.f;      // the low half of an element is kept times this
 
-// Sums of squares of a matrix in shares: part[matrix][share], in 64 bits (no overflow, no order to choose)
-template <typename T>
-__global__ __launch_bounds__(256) void squares_kernel(const T* __restrict__ x, int64_t matrix, int64_t stride, int rows, int columns, double* __restrict__ part) {
-  __shared__ double join[4];
-  const T* p = x + blockIdx.y * matrix;
-  double s = 0.0;
-  const int64_t n = (int64_t)rows * columns;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / columns;
-    const double v = (double)wide(p[r * stride + (i - r * columns)]);
-    s += v * v;
+// Elements of a matrix in pieces of V, by all threads of a grid's first dimension: f(piece's row, its first column)
+template <int V, typename F>
+__device__ __forceinline__ void for_pieces(int rows, int width, F f) {
+  const unsigned per = (unsigned)(width + V - 1) / V, n = (unsigned)rows * per;      // at most 2^30
+  for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+    const unsigned r = i / per;
+    f((int)r, (int)(i - r * per) * V);
   }
+}
+__device__ __forceinline__ double block_sum(double s, double* join) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   if ((threadIdx.x & 63) == 0) join[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) part[blockIdx.y * gridDim.x + blockIdx.x] = (join[0] + join[1]) + (join[2] + join[3]);
+  return (join[0] + join[1]) + (join[2] + join[3]);
 }
-// X in 32 bits and, times `scale`, as operands of the products; rows of ld, zeros behind the last column
+// Sums of squares of a matrix in shares: part[matrix][share], in 64 bits: no size of the elements overflows
 template <typename T>
-__global__ __launch_bounds__(256) void normalise_kernel(const T* __restrict__ x, int64_t matrix, int64_t stride, int rows, int columns, int ld,
-                                                        const double* __restrict__ part, int shares, double eps, float scale, float* __restrict__ x32,
-                                                        _Float16* __restrict__ x16) {
-  __shared__ double factor;
-  if (threadIdx.x < 64) {
-    double s = (int)threadIdx.x < shares ? part[blockIdx.y * shares + threadIdx.x] : 0.0;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-    if (threadIdx.x == 0) factor = 1.0 / (sqrt(s) + eps);
-  }
-  __syncthreads();
-  const double f = factor;
+__global__ __launch_bounds__(256) void squares_kernel(const T* __restrict__ x, int64_t matrix, int64_t stride, int rows, int columns, int vec,
+                                                      double* __restrict__ part) {
+  __shared__ double join[4];
   const T* p = x + blockIdx.y * matrix;
-  const int64_t n = (int64_t)rows * ld, base = blockIdx.y * n;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / ld;
-    const int c = (int)(i - r * ld);
-    const float v = c < columns ? (float)((double)wide(p[r * stride + c]) * f) : 0.f;
-    x32[base + i] = v;
-    if (x16) x16[base + i] = (_Float16)(v * scale);
+  double s = 0.0;
+  for_pieces<8>(rows, columns, [&](int r, int c) {
+    float v[8];
+    load_row<T, 8>(p + r * stride + c, vec, columns - c, v);
+#pragma unroll
+    for (int e = 0; e < 8; e++) s = fma((double)v[e], (double)v[e], s);
+  });
+  s = block_sum(s, join);
+  if (threadIdx.x == 0) part[blockIdx.y * gridDim.x + blockIdx.x] = s;
+}
+// The products' first operand, rows of ld with zeros behind the last column: X in 32 bits, or in fp16 G times a power of two that makes it about `scale`
+// X (exact for bf16, but for what is far below the average element), and what takes that to X as factor[matrix].
+template <typename T, typename X>
+__global__ __launch_bounds__(256) void normalise_kernel(const T* __restrict__ x, int64_t matrix, int64_t stride, int rows, int columns, int ld, int vec,
+                                                        const double* __restrict__ part, int shares, double eps, double scale, X* __restrict__ to,
+                                                        float* __restrict__ factor) {
+  constexpr bool HALF = sizeof(X) == 2;
+  __shared__ double join[4];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < shares; i += 256) s += part[blockIdx.y * shares + i];
+  const double norm = sqrt(block_sum(s, join)) + eps, inverse = 1.0 / norm;
+  int power = 0;
+  if constexpr (HALF) {
+    power = ilogb(scale * inverse);      // of infinities and no numbers: any, the factor is no number then
+    if (blockIdx.x == 0 && threadIdx.x == 0) factor[blockIdx.y] = (float)ldexp(inverse, -power);
   }
+  const T* p = x + blockIdx.y * matrix;
+  X* const out = to + (int64_t)blockIdx.y * rows * ld;
+  constexpr int V = kPiece<X>;
+  for_pieces<V>(rows, ld, [&](int r, int c) {
+    float v[V];
+    load_row<T, V>(p + r * stride + c, vec, columns - c, v);
+#pragma unroll
+    for (int e = 0; e < V; e++) v[e] = HALF ? ldexpf(v[e], power) : (float)((double)v[e] * inverse);
+    store_row<X, V>(out + (int64_t)r * ld + c, true, V, v);
+  });
 }
 
-// A = alpha (sums); rows of ld, zeros behind the last column
+// A = alpha^2 (sums), or that of its matrix; rows of ld, zeros behind the last column
 template <typename T>
 struct Gram {
   static constexpr bool GATED = false, SYMMETRIC = true;
@@ -73,6 +91,7 @@ struct Gram {
   int64_t matrix;
   int ld, n;
   float alpha;
+  const float* factor;
   __device__ __forceinline__ void across(int batch, int row, int col, float (&v)[V]) const {
 #pragma unroll
     for (int e = 0; e < V; e++)
@@ -80,8 +99,10 @@ struct Gram {
     store_row<T, V>(out + batch * matrix + (int64_t)row * ld + col, true, V, v);
   }
   __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V]) const {
+    float f = alpha;
+    if (factor) f = factor[batch];
 #pragma unroll
-    for (int e = 0; e < V; e++) v[e] *= alpha;
+    for (int e = 0; e < V; e++) v[e] *= f * f;
     across(batch, row, col, v);
   }
 };
@@ -109,63 +130,71 @@ struct Polynomial {
     for (int e = 0; e < V; e++) {
       v[e] = b * x[e] + c * v[e];
       if (sizeof(T) == 2 && col + e == row) {
-        diagonal[(int64_t)batch * n + row] = v[e];
+        diagonal[batch * padded(n) + row] = v[e];
         v[e] = 0.f;
       }
     }
     across(batch, row, col, v);
   }
 };
-// X <- a X + B X; the last step's goes out in the caller's type (bf16 where `narrow_out`)
+// X <- a X + B X; the last step's goes out in the caller's type
 template <typename T>
 struct Step {
   static constexpr bool GATED = false, SYMMETRIC = false;
   static constexpr int V = kPiece<T>;
-  const float* x32;
-  const T* x;              // the products' operand, 16 bits: x32 times `scale`
-  float* next32;           // 16 bits: x32 itself
+  const T* x;              // the products' operand; 16 bits: X times `scale` (the first step's: X / factor), rounded,
+  const _Float16* low;     // and what the rounding left, unless null
   T* next;
+  _Float16* next_low;
   void* out;               // the last step's results, else null
-  const float* diagonal;
+  const float *diagonal, *factor;
   int64_t matrix;
   int rows, cols, ld, by_column, bf16_out, vec;
-  float a, scale, inverse;
+  float a, scale;
   __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V]) const {
     const int64_t at = batch * matrix + (int64_t)row * ld + col;
     const int left = cols - col;
-    float x[V];
-    load_row<float, V>(x32 + at, true, V, x);
+    float h[V];
+    load_row<T, V>(x + at, true, V, h);
     if constexpr (sizeof(T) == 2) {
-      float h[V], d[V];
-      load_row<T, V>(this->x + at, true, V, h);
+      float d[V], l[V];
 #pragma unroll
-      for (int e = 0; e < V; e++) d[e] = 0.f;
+      for (int e = 0; e < V; e++) d[e] = l[e] = 0.f;
+      if (low) load_row<_Float16, V>(low + at, true, V, l);
       if (by_column) {
-        load_row<float, V>(diagonal + (int64_t)batch * cols + col, false, left, d);
+        load_row<float, V>(diagonal + (int64_t)batch * padded(cols) + col, true, V, d);
       } else {
-        const float one = diagonal[(int64_t)batch * rows + row];
+        const float one = diagonal[(int64_t)batch * padded(rows) + row];
 #pragma unroll
         for (int e = 0; e < V; e++) d[e] = one;
       }
+      float f = 1.f;      // to X times `scale`
+      if (factor) f = factor[batch] * scale;
 #pragma unroll
-      for (int e = 0; e < V; e++) v[e] = fmaf(a, x[e], fmaf(d[e], h[e], v[e]) * inverse);
+      for (int e = 0; e < V; e++) v[e] = fmaf(a, fmaf(l[e], 1.f / kLow, h[e]), fmaf(d[e], h[e], v[e])) * f;
     } else {
 #pragma unroll
-      for (int e = 0; e < V; e++) v[e] = fmaf(a, x[e], v[e]);
+      for (int e = 0; e < V; e++) v[e] = fmaf(a, h[e], v[e]);
     }
     if (out) {
       const int64_t to = ((int64_t)batch * rows + row) * cols + col;
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int e = 0; e < V; e++) v[e] *= 1.f / scale;
+      }
       if (bf16_out) return store_row<bf16_t, V>((bf16_t*)out + to, vec, left, v);
       return store_row<float, V>((float*)out + to, vec, left, v);
     }
 #pragma unroll
     for (int e = 0; e < V; e++)
       if (e >= left) v[e] = 0.f;
-    store_row<float, V>(next32 + at, true, V, v);
+    store_row<T, V>(next + at, true, V, v);
     if constexpr (sizeof(T) == 2) {
+      if (next_low) {
 #pragma unroll
-      for (int e = 0; e < V; e++) v[e] *= scale;
-      store_row<T, V>(next + at, true, V, v);
+        for (int e = 0; e < V; e++) v[e] = (v[e] - (float)(_Float16)v[e]) * kLow;
+        store_row<_Float16, V>(next_low + at, true, V, v);
+      }
     }
   }
 };
@@ -178,14 +207,14 @@ template <typename T>
 struct Layout {      // of the workspace
   int ld, ld_small;
   Plan gram, square, step;
-  int64_t matrix, small, shares, x32, x32b, x16, x16b, a, b, diagonal, part, bytes;
+  int64_t matrix, small, shares, factor, x, next, low, a, b, diagonal, part, bytes;
   explicit Layout(const Stack& n) {
     constexpr int V = kPiece<T>;
     const int s = n.small(), l = std::max(n.rows, n.columns);
     ld = (int)up(n.columns, V), ld_small = (int)up(s, V);
-    gram = plan_of<T>(s, s, n.count, chunks<T>(l), true, false);
-    square = plan_of<T>(s, s, n.count, chunks<T>(s), true, false);
-    step = plan_of<T>(n.rows, n.columns, n.count, chunks<T>(s), false, false);
+    gram = plan_of<T>({s, s, n.count, chunks<T>(l), true, false, true, (float)sizeof(T)});
+    square = plan_of<T>({s, s, n.count, chunks<T>(s), true, false, true, 2.f * sizeof(T)});
+    step = plan_of<T>({n.rows, n.columns, n.count, chunks<T>(s), false, false, n.rows <= n.columns, 8.f});
     matrix = (int64_t)n.rows * ld, small = (int64_t)s * ld_small;
     int64_t at = 0;
     auto take = [&](int64_t b) {
@@ -195,13 +224,13 @@ struct Layout {      // of the workspace
     };
     const bool half = sizeof(T) == 2;
     shares = take((int64_t)n.count * kNormShares * sizeof(double));
-    x32 = take(n.count * matrix * sizeof(float));
-    x32b = half ? x32 : take(n.count * matrix * sizeof(float));
-    x16 = half ? take(n.count * matrix * sizeof(T)) : 0;
-    x16b = half ? take(n.count * matrix * sizeof(T)) : 0;
+    factor = take((int64_t)n.count * sizeof(float));
+    x = take(n.count * matrix * sizeof(T));
+    next = take(n.count * matrix * sizeof(T));
+    low = half ? take(n.count * matrix * sizeof(T)) : 0;
     a = take(n.count * small * sizeof(T));
     b = take(n.count * small * sizeof(T));
-    diagonal = half ? take((int64_t)n.count * s * sizeof(float)) : 0;
+    diagonal = half ? take((int64_t)n.count * padded(s) * sizeof(float)) : 0;
     part = take(part_bytes(step, n.rows, n.columns, n.count, false));
     bytes = at;
   }
@@ -234,14 +263,16 @@ int orthogonalize(const G* x, int64_t x_matrix, int64_t x_stride, const Stack& n
   // elements of an orthogonalised matrix are 1 / sqrt(its longer side) on average: that becomes about 1
   const float scale = HALF ? std::exp2(std::floor(0.5f * std::log2((float)std::max(rows, columns)))) : 1.f;
   double* const shares = (double*)(ws + w.shares);
-  const int64_t elements = (int64_t)rows * columns;
-  const int n_shares = (int)std::min<int64_t>(kNormShares, (elements + 1023) / 1024);
-  float *x32 = (float*)(ws + w.x32), *next32 = (float*)(ws + w.x32b);
-  T *now = HALF ? (T*)(ws + w.x16) : (T*)x32, *next = HALF ? (T*)(ws + w.x16b) : (T*)next32;
+  float* const factor = (float*)(ws + w.factor);
+  const int64_t pieces = (int64_t)rows * (w.ld / kPiece<T>);
+  const int n_shares = (int)std::min<int64_t>((pieces + 1023) / 1024, std::max(std::min(2048 / n.count, kNormShares), 1));
+  T *now = (T*)(ws + w.x), *next = (T*)(ws + w.next);
+  _Float16* const low = (_Float16*)(ws + w.low);
   if (!probe) {
-  squares_kernel<G><<<dim3(n_shares, n.count), 256, 0, s>>>(x, x_matrix, x_stride, rows, columns, shares);
-  normalise_kernel<G><<<dim3((unsigned)std::min<int64_t>((w.matrix + 1023) / 1024, 2048), n.count), 256, 0, s>>>(
-      x, x_matrix, x_stride, rows, columns, w.ld, shares, n_shares, (double)eps, scale, x32, HALF ? (_Float16*)now : nullptr);
+    const bool whole = aligned16(x) && columns % 8 == 0 && x_stride % 8 == 0 && x_matrix % 8 == 0;
+    squares_kernel<G><<<dim3(n_shares, n.count), 256, 0, s>>>(x, x_matrix, x_stride, rows, columns, whole, shares);
+    normalise_kernel<G, T><<<dim3((unsigned)std::min<int64_t>((pieces + 511) / 512, std::max(2048 / n.count, 1)), n.count), 256, 0, s>>>(
+        x, x_matrix, x_stride, rows, columns, w.ld, whole, shares, n_shares, (double)eps, (double)scale, now, factor);
   }
   T *const a = (T*)(ws + w.a), *const b = (T*)(ws + w.b);
   float* const diagonal = (float*)(ws + w.diagonal);
@@ -254,7 +285,7 @@ int orthogonalize(const G* x, int64_t x_matrix, int64_t x_stride, const Stack& n
       const Operand<T> o{now, w.ld, w.matrix, 0, rows, rows, w.ld, w.ld, n.count * w.matrix};
       p.a = p.b = o;
       p.k = p.last_k = tall ? rows : w.ld, p.rows = p.cols = small;
-      const Gram<T> e{a, w.small, w.ld_small, small, 1.f / (scale * scale)};
+      const Gram<T> e{a, w.small, w.ld_small, small, 1.f / scale, HALF && t == 0 ? factor : nullptr};
       if (tall) launch<T, true, true>(p, w.gram, e, s);
       else launch<T, false, false>(p, w.gram, e, s);
     }
@@ -266,7 +297,8 @@ int orthogonalize(const G* x, int64_t x_matrix, int64_t x_stride, const Stack& n
       Operand<T> poly = square;
       poly.p = b;
       p.part = (float*)(ws + w.part), p.rows = rows, p.cols = columns;
-      Step<T> e{x32, now, next32, next, last ? out : nullptr, diagonal, w.matrix, rows, columns, w.ld, tall, std::is_same<G, bf16_t>::value, 0, c[0], scale, 1.f / scale};
+      Step<T> e{now, HALF && t > 0 && !last ? low : nullptr, next, HALF && t + 2 < steps ? low : nullptr, last ? out : nullptr, diagonal,
+                HALF && t == 0 ? factor : nullptr, w.matrix, rows, columns, w.ld, tall, std::is_same<G, bf16_t>::value, 0, c[0], scale};
       e.vec = columns % kPiece<T> == 0 && columns % (16 / sizeof(G)) == 0 && aligned16(out);
       p.k = p.last_k = w.ld_small;
       if (tall) {
@@ -278,7 +310,6 @@ int orthogonalize(const G* x, int64_t x_matrix, int64_t x_stride, const Stack& n
       }
     }
     std::swap(now, next);
-    if (!HALF) std::swap(x32, next32);
   }
   return probe ? RL_OK : launched();
 }

@@ -495,7 +495,7 @@ void go(const Product<T>& p, const EPI& epi, hipStream_t s) {
   }
   const int64_t tiles = (EPI::SYMMETRIC ? (int64_t)p.tiles_i * (p.tiles_i + 1) / 2 : (int64_t)p.tiles_i * p.tiles_j) * p.slices * p.batches;
   // as many workgroups as the 256 CUs hold at once
-  kernel<<<(unsigned)std::min<int64_t>(tiles, lds > 80 * 1024 ? 256 : 512), 256, lds, s>>>(Arguments<T, EPI>{p, epi});
+  kernel<<<(unsigned)std::min<int64_t>(tiles, 256 * (160 * 1024 / lds)), 256, lds, s>>>(Arguments<T, EPI>{p, epi});
   if constexpr (SLICED) {
     const int64_t n = (int64_t)p.batches * p.rows * ((p.cols + kPiece<T> - 1) / kPiece<T>);
     join_kernel<T, EPI><<<(unsigned)std::min<int64_t>((n + 255) / 256, 4096), 256, 0, s>>>(p, epi);
@@ -504,20 +504,32 @@ void go(const Product<T>& p, const EPI& epi, hipStream_t s) {
 
 // ---- the plan of a product: tile and slices -----------------------------------------------------------------------------------
 struct Plan { int mb, nb, slices; };
-// The cheapest by estimate: a round of tiles on 256 CUs takes what its chunks take and some us to begin and end; sums of slices are written and read.
+// The cheapest by estimate.  A round of tiles takes what its chunks take and some us to begin and end; what the epilogue reads and writes (`bytes` an
+// element of C) goes at 4.5 TB/s, half of it beside the other workgroup's products where a CU holds two; sums of slices are written and read at that rate
+// too.  us of a chunk fitted on products of 2744 to 4096 rows, K of 1024 to 9728, batches of 28: 256 x 256 (one workgroup a CU) 0.87, 192 x 256
+// 0.79, 128 x 128 (two a CU) 0.57, gated 0.75; estimates within 15 % of what was measured, their order right in 13 of 14 pairs.
+struct Sizes {
+  int64_t rows, cols, batches, n_chunks;
+  bool symmetric, gated, strided;      // strided: one of the operands
+  float bytes;
+};
 template <typename T>
-Plan plan_of(int64_t rows, int64_t cols, int64_t batches, int64_t n_chunks, bool symmetric, bool gated) {
-  struct Option { int mb, nb; float chunk_us; };
-  static const Option half[] = {{4, 4, 0.6f}, {2, 2, 0.2f}}, full[] = {{2, 2, 2.4f}, {1, 1, 0.6f}};
+Plan plan_of(const Sizes& z) {
+  struct Option { int mb, nb, resident; float chunk_us, gated_us; };      // resident: workgroups that a round has
+  constexpr int N = sizeof(T) == 2 ? 3 : 2;
+  static const Option half[] = {{4, 4, 256, 0.87f, 0.87f}, {3, 4, 256, 0.79f, 0.79f}, {2, 2, 512, 0.57f, 0.75f}}, full[] = {{2, 2, 512, 4.8f, 4.8f}, {1, 1, 768, 1.8f, 1.8f}};
+  const float elements = (float)(z.batches * z.rows * z.cols);
   Plan best{0, 0, 1};
   float best_us = 3e38f;
-  for (const Option& o : sizeof(T) == 2 ? half : full) {
-    if (gated && o.nb < 2) continue;
-    const int64_t ti = (rows + 64 * o.mb - 1) / (64 * o.mb), bn = gated ? 32 * o.nb : 64 * o.nb, tj = (cols + bn - 1) / bn;
-    const int64_t tiles = (symmetric ? ti * (ti + 1) / 2 : ti * tj) * batches;
-    for (int s = 1; s <= (symmetric ? 1 : 16) && s <= std::max<int64_t>(n_chunks / 8, 1); s++) {
-      const float sums = s == 1 ? 0.f : 4.f + (float)s * (float)(batches * rows * cols) * (gated ? 2.f : 1.f) * 8e-6f / 4.f;
-      const float us = (float)((tiles * s + 255) / 256) * ((float)((n_chunks + s - 1) / s) * o.chunk_us + 4.f) + sums;
+  for (int i = 0; i < N; i++) {
+    const Option& o = sizeof(T) == 2 ? half[i] : full[i];
+    if ((z.gated && o.nb < 2) || (o.mb == 3 && z.strided) || (sizeof(T) == 2 && o.mb > 2 && z.symmetric)) continue;
+    const int64_t ti = (z.rows + 64 * o.mb - 1) / (64 * o.mb), bn = z.gated ? 32 * o.nb : 64 * o.nb, tj = (z.cols + bn - 1) / bn;
+    const int64_t tiles = (z.symmetric ? ti * (ti + 1) / 2 : ti * tj) * z.batches;
+    const float epilogue = elements * z.bytes / 4.5e6f * (o.resident > 256 && tiles > o.resident ? 0.5f : 1.f);
+    for (int s = 1; s <= (z.symmetric ? 1 : 16) && s <= std::max<int64_t>(z.n_chunks / 8, 1); s++) {
+      const float sums = s == 1 ? 0.f : 5.f + (float)s * elements * (z.gated ? 2.f : 1.f) * 8.f / 4.5e6f;
+      const float us = (float)((tiles * s + o.resident - 1) / o.resident) * ((float)((z.n_chunks + s - 1) / s) * (z.gated ? o.gated_us : o.chunk_us) + 5.f) + epilogue + sums;
       if (us < best_us) best_us = us, best = {o.mb, o.nb, s};
     }
   }
@@ -570,8 +582,13 @@ void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
   };
 #define RL_I(x) std::integral_constant<int, x>()
   if constexpr (sizeof(T) == 2) {
-    if (plan.mb == 4) with(RL_I(4), RL_I(4), RL_I(4));
-    else with(RL_I(2), RL_I(2), RL_I(3));
+    if constexpr (!EPI::SYMMETRIC) {
+      if (plan.mb == 4) return with(RL_I(4), RL_I(4), RL_I(4));
+    }
+    if constexpr (!TA && !TB && !EPI::SYMMETRIC) {
+      if (plan.mb == 3) return with(RL_I(3), RL_I(4), RL_I(4));
+    }
+    with(RL_I(2), RL_I(2), RL_I(3));
   } else {
     if constexpr (!EPI::GATED) {
       if (plan.mb == 1) return with(RL_I(1), RL_I(1), RL_I(4));

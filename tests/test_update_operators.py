@@ -355,9 +355,10 @@ def newton(x, half, g, steps=5, coefficients=NEWTON, eps=1e-7, roundings=True):
             return t
         return (t * s).half().double() / s if half else t.float().double()
 
-    for _ in range(steps):
+    for i in range(steps):
         a, b, c = coefficients
         xo = operand(x, scale)
+        x = xo if half and i + 1 == steps else x      # what that rounding leaves goes on until the last step
         gram = operand(product(xo, xo.t()))
         poly = b * gram + c * product(gram, gram)
         if roundings:
