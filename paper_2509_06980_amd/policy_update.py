@@ -2,11 +2,12 @@
 
 The trajectories that the rollout engine generated are run through the same decoder again, packed one after the other, with the
 operators of `policy_ops`: norms, rotary positions, attention over packed trajectories and the log-probs of the sampled
-tokens, each with its backward pass; the projections between them are plain matrix products.  The objective is the masked GRPO
+tokens, each with its backward pass; the projections between them are plain matrix products, or (`fused`) linear layers with the gate
+in their epilogue and the residual stream with its norms.  `Muon` takes orthogonalised steps with the gradients.  The objective is the masked GRPO
 objective that the engine evaluates forward (rl_grpo_objective); here it has a gradient, and `to_blob` gives the updated
 weights back in the form that the engine loads.
 
-    python -m paper_2509_06980_amd.policy_update        # rollouts of a small model, reward, updates, rollouts of the updated model
+    python -m paper_2509_06980_amd.policy_update [--fused] [--muon]     # rollouts of a small model, reward, updates, rollouts of the updated model
 """
 import struct
 from types import SimpleNamespace
@@ -49,9 +50,10 @@ def _tensor(x, device=None):
 
 
 class PolicyModel:
-    """The engine's decoder as torch parameters, from and to its weight blob."""
+    """The engine's decoder as torch parameters, from and to its weight blob.  fused: products with `ops.linear`, gate and up in one, and the residual
+    stream with `ops.residual_norm`; the same roundings, but for that of gate and up before they are multiplied."""
 
-    def __init__(self, blob, device="cuda"):
+    def __init__(self, blob, device="cuda", fused=False):
         raw = np.ascontiguousarray(np.asarray(blob, np.uint8))
         if raw.size < _HEADER or bytes(raw[:4]) != b"RLW1":
             raise ValueError("no weight blob")
@@ -72,10 +74,17 @@ class PolicyModel:
             self.params[name] = t.requires_grad_()
             at += n
         self.device = torch.device(device)
+        self.fused = fused
         self._table = None
 
     def parameters(self):
         return list(self.params.values())
+
+    def parameter_groups(self):
+        """Groups for `Muon`: the layers' matrices, and all others (embedding, lm-head, gains)."""
+        inner = [p for n, p in self.params.items() if ".w_" in n]
+        rest = [p for n, p in self.params.items() if ".w_" not in n]
+        return [dict(params=inner, orthogonal=True), dict(params=rest, orthogonal=False)]
 
     def to_blob(self):
         """The weights as rl_model_load takes them."""
@@ -112,17 +121,29 @@ class PolicyModel:
             x = x.view(total, n, c.head_dim)
             return ops.norm(x, p[gain], eps=c.rms_eps) if c.qk_norm else x
 
+        linear = ops.linear if self.fused else F.linear
+
+        def attended(a, w):
+            q, k = heads(linear(a, p[w("w_q")]), w("g_q"), c.n_q_heads), heads(linear(a, p[w("w_k")]), w("g_k"), c.n_kv_heads)
+            v = linear(a, p[w("w_v")]).view(total, c.n_kv_heads, c.head_dim)
+            q, k = ops.rotate(q, k, positions, self._table)
+            return linear(ops.attention(q, k, v, cu, cu).flatten(1), p[w("w_o")])
+
         h = F.embedding(tokens, p["embed"]).float()
+        a = norm(h, "l0.g_in")
         for i in range(c.n_layers):
             w = lambda name: f"l{i}.{name}"  # noqa: B023,E731
-            a = norm(h, w("g_in"))
-            q, k = heads(F.linear(a, p[w("w_q")]), w("g_q"), c.n_q_heads), heads(F.linear(a, p[w("w_k")]), w("g_k"), c.n_kv_heads)
-            v = F.linear(a, p[w("w_v")]).view(total, c.n_kv_heads, c.head_dim)
-            q, k = ops.rotate(q, k, positions, self._table)
-            h = h + F.linear(ops.attention(q, k, v, cu, cu).flatten(1), p[w("w_o")]).float()
-            b = norm(h, w("g_post"))
-            h = h + F.linear(F.silu(F.linear(b, p[w("w_gate")])) * F.linear(b, p[w("w_up")]), p[w("w_down")]).float()
-        return norm(h, "g_final")
+            after = f"l{i + 1}.g_in" if i + 1 < c.n_layers else "g_final"
+            if self.fused:
+                h, b = ops.residual_norm(h, attended(a, w), p[w("g_post")], eps=c.rms_eps)
+                m = ops.linear(b, p[w("w_gate")], up=p[w("w_up")], activation="silu")
+                h, a = ops.residual_norm(h, ops.linear(m, p[w("w_down")]), p[after], eps=c.rms_eps)
+            else:
+                h = h + attended(a, w).float()
+                b = norm(h, w("g_post"))
+                h = h + F.linear(F.silu(F.linear(b, p[w("w_gate")])) * F.linear(b, p[w("w_up")]), p[w("w_down")]).float()
+                a = norm(h, after)
+        return a
 
     def logprobs(self, tokens, obs_mask, lens, temperature=1.0):
         """Differentiable rl_recompute_logprobs: one float32 a token of the packed trajectories, the log-prob of a sampled token
@@ -141,6 +162,57 @@ class PolicyModel:
         temperature = 1.0 if temperature == 0 else float(temperature)
         lp = ops.token_logprobs(self._rows(tokens, lens), head, torch.cat([target[1:], target.new_full((1,), -1)]), temperature)
         return torch.cat([lp.new_zeros(1), lp[:-1]])
+
+
+class Muon(torch.optim.Optimizer):
+    """Steps with orthogonalised momentum for matrices (groups with orthogonal=True: W <- W - lr max(1, rows / columns)^1/2 O with O the
+    orthogonalised m, or gradient + momentum m in Nesterov's form, and m <- momentum m + gradient), Adam's for everything else.
+    Matrices of one shape are orthogonalised together; momenta are kept in 32 bits."""
+
+    def __init__(self, params, lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7,
+                 adam_lr=3e-4, betas=(0.9, 0.95), adam_eps=1e-8):
+        super().__init__(params, dict(orthogonal=False, lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, steps=steps,
+                                      coefficients=coefficients, eps=eps, adam_lr=adam_lr, betas=betas, adam_eps=adam_eps))
+        for group in self.param_groups:
+            if group["orthogonal"] and any(p.dim() != 2 for p in group["params"]):
+                raise ValueError("orthogonal steps are for matrices")
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for group in self.param_groups:
+            params = [p for p in group["params"] if p.grad is not None]
+            if group["orthogonal"]:
+                alike = {}
+                for p in params:
+                    alike.setdefault((p.shape, p.dtype, p.device), []).append(p)
+                for (shape, dtype, _), ps in alike.items():
+                    updates = ops.orthogonalize(torch.stack([self._momentum(p, group) for p in ps]).to(dtype), group["steps"], group["coefficients"], group["eps"])
+                    for p, o in zip(ps, updates):
+                        p.mul_(1 - group["lr"] * group["weight_decay"]).add_(o, alpha=-group["lr"] * max(1.0, shape[0] / shape[1]) ** 0.5)
+            else:
+                for p in params:
+                    self._adam(p, group)
+        return loss
+
+    def _momentum(self, p, group):
+        state, g = self.state[p], p.grad.float()
+        if "momentum" not in state:
+            state["momentum"] = torch.zeros_like(g)
+        m = state["momentum"].mul_(group["momentum"]).add_(g)
+        return g + group["momentum"] * m if group["nesterov"] else m
+
+    def _adam(self, p, group):
+        state, g, (b1, b2) = self.state[p], p.grad.float(), group["betas"]
+        if "step" not in state:
+            state["step"], state["first"], state["second"] = 0, torch.zeros_like(g), torch.zeros_like(g)
+        state["step"] += 1
+        first = state["first"].lerp_(g, 1 - b1) / (1 - b1 ** state["step"])
+        second = state["second"].mul_(b2).addcmul_(g, g, value=1 - b2) / (1 - b2 ** state["step"])
+        p.mul_(1 - group["adam_lr"] * group["weight_decay"]).add_((first / (second.sqrt() + group["adam_eps"])).to(p.dtype), alpha=-group["adam_lr"])
 
 
 def group_advantages(rewards, group_size, eps_std=1e-6, std_ddof=0):
@@ -190,19 +262,25 @@ def update(model, optimizer, engine, traj_ids, rewards, group_size, temperature=
     return value.item()
 
 
-def main():
+def main(arguments=None):
+    import argparse
     import sys
     from pathlib import Path
+    parser = argparse.ArgumentParser(description="Rollouts of a small model, a reward, updates, rollouts of the updated model")
+    parser.add_argument("--fused", action="store_true", help="linear layers and residual stream by the operators of their own")
+    parser.add_argument("--muon", action="store_true", help="orthogonalised steps instead of Adam's")
+    parser.add_argument("--updates", type=int, default=10)
+    options = parser.parse_args(arguments)
     sys.path.insert(0, str(Path(__file__).resolve().parent.parent))
     from synthetic import SHAPES, make_weight_blob
 
     from . import RolloutEngine
     shape = SHAPES["small-d128"]
-    model = PolicyModel(make_weight_blob(shape, seed=1, weight_std=0.03))
-    optimizer = torch.optim.Adam(model.parameters(), lr=5e-3)
+    model = PolicyModel(make_weight_blob(shape, seed=1, weight_std=0.03), fused=options.fused)
+    optimizer = Muon(model.parameter_groups(), lr=0.01, adam_lr=5e-3) if options.muon else torch.optim.Adam(model.parameters(), lr=5e-3)
     prompts, group, n_new = 8, 32, 24
     rng = np.random.default_rng(0)
-    for step in range(10):
+    for step in range(options.updates):
         engine = RolloutEngine(model.to_blob(), max_context=128, max_trajectories=prompts * group, kv_pool_pages=prompts * group * 8)
         ids = np.arange(prompts * group)
         engine.append_observation(ids[::group], rng.integers(0, shape.vocab, prompts * 16), [16] * prompts)
