@@ -330,32 +330,33 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
       for (int c = here.c0; c < here.c1; c++) {
         const int sn = sc + 1 == R ? 0 : sc + 1;
         __builtin_amdgcn_sched_barrier(0);
+        // the instructions of half a chunk (16 k), one memory instruction behind each: the operands of the next half first, then this half's share of the loads,
+        // the rest of chunk c + R - 1 or the first F pieces of chunk c + R
+        constexpr int S = MB * NB, Q = MB + NB;
 #pragma unroll
         for (int g = 0; g < 2 * MB; g++) {
           const int a = g % MB, st = g / MB;
           if (g == MB) {     // chunk c + 1 has landed for every wave, chunk c is read out by every wave
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((R - 2) * PW) : "memory");
             __builtin_amdgcn_s_barrier();
-            advance();
           }
-          const int stage = st == 0 ? sc : sn, kb = 1 - st;
-          // the operands of the next 16 k, in the order of their use
+          const int stage = st == 0 ? sc : sn, kb = 1 - st, first = st == 0 ? F : 0, n = st == 0 ? PW - F : F;
 #pragma unroll
-          for (int q = 0; q < MB + NB; q++)
-            if (q * MB / (MB + NB) == a) {
-              const int x = q == 0 ? 0 : q <= NB ? MB + q - 1 : q - NB;
-              if (x < MB) av[1 - st][x] = read_a(x, kb, stage);
-              else bv[1 - st][x - MB] = read_b(x - MB, kb, stage);
-            }
-          // this step's share of the loads: the rest of chunk c + R - 1, then the first F pieces of chunk c + R
+          for (int b = 0; b < NB; b++) {
+            mfma(av[st][a], bv[st][b], acc[a][b]);
 #pragma unroll
-          for (int j = 0; j < PW; j++) {
-            if (st == 0 && j >= F && (j - F) * MB / (PW - F) == a) load(j, sl);
-            if (st == 1 && j < F && j * MB / F == a) load(j, sc);
+            for (int q = 0; q < Q; q++)      // in the order of their use
+              if (q * S / (2 * Q) == a * NB + b) {
+                const int x = q == 0 ? 0 : q <= NB ? MB + q - 1 : q - NB;
+                if (x < MB) av[1 - st][x] = read_a(x, kb, stage);
+                else bv[1 - st][x - MB] = read_b(x - MB, kb, stage);
+              }
+#pragma unroll
+            for (int j = 0; j < PW; j++)
+              if (j < n && S / 2 + j * (S - S / 2) / n == a * NB + b) load(first + j, st == 0 ? sl : sc);
+            if (g == MB - 1 && b == NB - 1) advance();
+            __builtin_amdgcn_sched_barrier(0);
           }
-#pragma unroll
-          for (int b = 0; b < NB; b++) mfma(av[st][a], bv[st][b], acc[a][b]);
-          __builtin_amdgcn_sched_barrier(0);
         }
         sl = sc;
         sc = sn;
