@@ -90,8 +90,8 @@ struct Finish {
       }
       if (kept) {
         float* const k = kept + (int64_t)row * cols * (GATED ? 2 : 1) + col;
-        store_row<float, V>(k, vec, left, v);
-        if constexpr (GATED) store_row<float, V>(k + cols, vec, left, u);
+        store_row<float, V, true>(k, vec, left, v);
+        if constexpr (GATED) store_row<float, V, true>(k + cols, vec, left, u);
       }
       activate_all<false, V>(v, act, v, x);
       if constexpr (GATED) {
@@ -105,9 +105,9 @@ struct Finish {
 #pragma unroll
         for (int e = 0; e < V; e++) v[e] += x[e];
       }
-      if (wide) return store_row<float, V>((float*)y + (int64_t)row * cols + col, vec, left, v);
+      if (wide) return store_row<float, V, true>((float*)y + (int64_t)row * cols + col, vec, left, v);
     }
-    store_row<T, V>((T*)y + batch * y_batch + (int64_t)row * cols + col, vec, left, v);
+    store_row<T, V, true>((T*)y + batch * y_batch + (int64_t)row * cols + col, vec, left, v);
   }
 };
 

@@ -20,6 +20,9 @@ using namespace product;
 // =============================================================================================
 const int kNormShares = 1024;
 const int kHalfFrom = 256;
+// X goes past the caches where it would not stay in the last one of 256 MB with what else a step reads: 28 x 2048 x 1024 (117 MB) 1930 -> 1885 us, 2560 x 9728
+// (50 MB) 1460 -> 1545, which keeps the caches.
+const int64_t kStream = 80 << 20;
 const float kLow = 2048.f;      // the low half of an element is kept times this
 
 // Elements of a matrix in pieces of V, by all threads of a grid's first dimension: f(piece's row, its first column)
@@ -149,7 +152,7 @@ struct Step {
   void* out;               // the last step's results, else null
   const float *diagonal, *factor;
   int64_t matrix;
-  int rows, cols, ld, by_column, bf16_out, vec;
+  int rows, cols, ld, by_column, bf16_out, vec, stream;
   float a, scale;
   __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V]) const {
     const int64_t at = batch * matrix + (int64_t)row * ld + col;
@@ -188,12 +191,14 @@ struct Step {
 #pragma unroll
     for (int e = 0; e < V; e++)
       if (e >= left) v[e] = 0.f;
-    store_row<T, V>(next + at, true, V, v);
+    if (stream) store_row<T, V, true>(next + at, true, V, v);
+    else store_row<T, V>(next + at, true, V, v);
     if constexpr (sizeof(T) == 2) {
       if (next_low) {
 #pragma unroll
         for (int e = 0; e < V; e++) v[e] = (v[e] - (float)(_Float16)v[e]) * kLow;
-        store_row<_Float16, V>(next_low + at, true, V, v);
+        if (stream) store_row<_Float16, V, true>(next_low + at, true, V, v);
+        else store_row<_Float16, V>(next_low + at, true, V, v);
       }
     }
   }
@@ -231,7 +236,7 @@ struct Layout {      // of the workspace
     a = take(n.count * small * sizeof(T));
     b = take(n.count * small * sizeof(T));
     diagonal = half ? take((int64_t)n.count * padded(s) * sizeof(float)) : 0;
-    part = take(part_bytes(step, n.rows, n.columns, n.count, false));
+    part = take(std::max({part_bytes(step, n.rows, n.columns, n.count, false), part_bytes(gram, s, s, n.count, false), part_bytes(square, s, s, n.count, false)}));
     bytes = at;
   }
 };
@@ -280,7 +285,7 @@ int orthogonalize(const G* x, int64_t x_matrix, int64_t x_stride, const Stack& n
     const float* c = coefficients + 3 * t;
     const bool last = t == steps - 1;
     Product<T> p{};
-    p.segments = 1, p.batches = n.count;
+    p.segments = 1, p.batches = n.count, p.part = (float*)(ws + w.part);
     {
       const Operand<T> o{now, w.ld, w.matrix, 0, rows, rows, w.ld, w.ld, n.count * w.matrix};
       p.a = p.b = o;
@@ -296,9 +301,9 @@ int orthogonalize(const G* x, int64_t x_matrix, int64_t x_stride, const Stack& n
       const Operand<T> o{now, w.ld, w.matrix, 0, rows, rows, w.ld, w.ld, n.count * w.matrix};
       Operand<T> poly = square;
       poly.p = b;
-      p.part = (float*)(ws + w.part), p.rows = rows, p.cols = columns;
+      p.rows = rows, p.cols = columns;
       Step<T> e{now, HALF && t > 0 && !last ? low : nullptr, next, HALF && t + 2 < steps ? low : nullptr, last ? out : nullptr, diagonal,
-                HALF && t == 0 ? factor : nullptr, w.matrix, rows, columns, w.ld, tall, std::is_same<G, bf16_t>::value, 0, c[0], scale};
+                HALF && t == 0 ? factor : nullptr, w.matrix, rows, columns, w.ld, tall, std::is_same<G, bf16_t>::value, 0, n.count * w.matrix * (int64_t)sizeof(T) > kStream, c[0], scale};
       e.vec = columns % kPiece<T> == 0 && columns % (16 / sizeof(G)) == 0 && aligned16(out);
       p.k = p.last_k = w.ld_small;
       if (tall) {

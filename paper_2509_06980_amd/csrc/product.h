@@ -55,13 +55,21 @@ __device__ __forceinline__ void load_row(const T* p, bool vec, int left, float (
     for (int e = 0; e < N; e++) v[e] = e < left ? wide(p[e]) : 0.f;
   }
 }
-template <typename T, int N>
+// STREAM: past the caches
+template <typename T, int N, bool STREAM = false>
 __device__ __forceinline__ void store_row(T* p, bool vec, int left, const float (&v)[N]) {
   if (vec) {
     struct alignas(N * sizeof(T) < 16 ? N * sizeof(T) : 16) Piece { T x[N]; } q;
 #pragma unroll
     for (int e = 0; e < N; e++) q.x[e] = narrow<T>(v[e]);
-    *(Piece*)p = q;
+    if constexpr (STREAM && N * sizeof(T) >= 16) {
+      struct Words { u32x4 x[N * sizeof(T) / 16]; };
+      const Words w = __builtin_bit_cast(Words, q);
+#pragma unroll
+      for (unsigned i = 0; i < N * sizeof(T) / 16; i++) __builtin_nontemporal_store(w.x[i], (u32x4*)p + i);
+    } else {
+      *(Piece*)p = q;
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < N; e++)
@@ -139,7 +147,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
   constexpr int JN = GATED ? BN / 2 : BN;      // columns of C that a tile covers
   static_assert((!TA || BM * EL >= 256) && (!TB || BN * EL >= 256), "four blocks of 64 bytes a row");
   static_assert(!GATED || (!TB && NB >= 2), "rows of two matrices in a tile");
-  static_assert(!SYM || (MB == NB && !SLICED), "square tiles");
+  static_assert(!SYM || MB == NB, "square tiles");
   using L = Lds<T, MB, NB, R>;
   extern __shared__ u32x4 smem[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, wm = wave >> 1, wn = wave & 1;
@@ -414,7 +422,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
             epi(here.batch, r0 + r, col + c, v, u);
           }
         }
-        if constexpr (SYM) {
+        if constexpr (SYM && !SLICED) {
           if (here.i0 != here.j0) {
 #pragma unroll
             for (int q = 0; q < V / 4; q++)
@@ -422,7 +430,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
           }
         }
       }
-      if constexpr (SYM) {
+      if constexpr (SYM && !SLICED) {
         if (here.i0 != here.j0) {      // column c of these 32 rows is a part of row c across the diagonal
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll 1
@@ -482,6 +490,45 @@ __global__ __launch_bounds__(256) void join_kernel(Product<T> P, EPI epi) {
   }
 }
 
+// The same for a symmetric product, of which the slices hold the tiles on and under the diagonal: a workgroup takes 64 x 64 elements and stores them across too.
+template <typename T, typename EPI>
+__global__ __launch_bounds__(256) void join_symmetric_kernel(Product<T> P, EPI epi) {
+  constexpr int V = kPiece<T>, B = 64;
+  __shared__ float block[B][B + 1];
+  const int v0 = blockIdx.x;
+  int i = (int)((__builtin_sqrtf(8.f * v0 + 1.f) - 1.f) * 0.5f);
+  while ((i + 1) * (i + 2) / 2 <= v0) i++;
+  while (i * (i + 1) / 2 > v0) i--;
+  const int j = v0 - i * (i + 1) / 2, batch = blockIdx.y, r0 = i * B, c0 = j * B;
+  const int64_t ld = padded(P.cols), rows = (int64_t)P.batches * P.rows;
+  for (int p = threadIdx.x; p < B * B / V; p += 256) {
+    const int r = p / (B / V), c = p % (B / V) * V;
+    if (r0 + r >= P.rows || c0 + c >= P.cols) continue;
+    float v[V], u[V];
+#pragma unroll
+    for (int e = 0; e < V; e++) v[e] = u[e] = 0.f;
+    for (int s = 0; s < P.slices; s++) {
+      float x[V];
+      load_row<float, V>(P.part + (s * rows + (int64_t)batch * P.rows + r0 + r) * ld + c0 + c, true, V, x);
+#pragma unroll
+      for (int e = 0; e < V; e++) v[e] += x[e];
+    }
+    epi(batch, r0 + r, c0 + c, v, u);
+#pragma unroll
+    for (int e = 0; e < V; e++) block[r][c + e] = v[e];
+  }
+  if (i == j) return;
+  __syncthreads();
+  for (int p = threadIdx.x; p < B * B / V; p += 256) {
+    const int c = p % B, r = p / B * V;
+    if (r0 + r >= P.rows || c0 + c >= P.cols) continue;
+    float v[V];
+#pragma unroll
+    for (int e = 0; e < V; e++) v[e] = block[r + e][c];      // what is behind the last row is set to zero by the epilogue
+    epi.across(batch, c0 + c, r0 + r, v);
+  }
+}
+
 template <typename T, bool TA, bool TB, int MB, int NB, int R, bool SLICED, typename EPI>
 void go(const Product<T>& p, const EPI& epi, hipStream_t s) {
   constexpr int lds = Lds<T, MB, NB, R>::BYTES;
@@ -497,7 +544,10 @@ void go(const Product<T>& p, const EPI& epi, hipStream_t s) {
   const int64_t tiles = (EPI::SYMMETRIC ? (int64_t)p.tiles_i * (p.tiles_i + 1) / 2 : (int64_t)p.tiles_i * p.tiles_j) * p.slices * p.batches;
   // as many workgroups as the 256 CUs hold at once
   kernel<<<(unsigned)std::min<int64_t>(tiles, 256 * (160 * 1024 / lds)), 256, lds, s>>>(Arguments<T, EPI>{p, epi});
-  if constexpr (SLICED) {
+  if constexpr (SLICED && EPI::SYMMETRIC) {
+    const unsigned n = (unsigned)(p.rows + 63) / 64;
+    join_symmetric_kernel<T, EPI><<<dim3(n * (n + 1) / 2, p.batches), 256, 0, s>>>(p, epi);
+  } else if constexpr (SLICED) {
     const int64_t n = (int64_t)p.batches * p.rows * ((p.cols + kPiece<T> - 1) / kPiece<T>);
     join_kernel<T, EPI><<<(unsigned)std::min<int64_t>((n + 255) / 256, 4096), 256, 0, s>>>(p, epi);
   }
@@ -528,8 +578,8 @@ Plan plan_of(const Sizes& z) {
     const int64_t ti = (z.rows + 64 * o.mb - 1) / (64 * o.mb), bn = z.gated ? 32 * o.nb : 64 * o.nb, tj = (z.cols + bn - 1) / bn;
     const int64_t tiles = (z.symmetric ? ti * (ti + 1) / 2 : ti * tj) * z.batches;
     const float epilogue = elements * z.bytes / 4.5e6f * (o.resident > 256 && tiles > o.resident ? 0.5f : 1.f);
-    for (int s = 1; s <= (z.symmetric ? 1 : 16) && s <= std::max<int64_t>(z.n_chunks / 8, 1); s++) {
-      const float sums = s == 1 ? 0.f : 5.f + (float)s * elements * (z.gated ? 2.f : 1.f) * 8.f / 4.5e6f;
+    for (int s = 1; s <= 16 && s <= std::max<int64_t>(z.n_chunks / 8, 1); s++) {
+      const float sums = s == 1 ? 0.f : 5.f + (float)s * elements * (z.gated ? 2.f : z.symmetric ? 0.5f : 1.f) * 8.f / 4.5e6f;
       const float us = (float)((tiles * s + o.resident - 1) / o.resident) * ((float)((z.n_chunks + s - 1) / s) * (z.gated ? o.gated_us : o.chunk_us) + 5.f) + epilogue + sums;
       if (us < best_us) best_us = us, best = {o.mb, o.nb, s};
     }
@@ -576,9 +626,7 @@ void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
   if (probe) return find_overreach(p, TA, TB, 64 * plan.mb, bn, EPI::GATED ? p.b2 : 0);
   auto with = [&](auto mb, auto nb, auto r) {
     constexpr int MB = decltype(mb)::value, NB = decltype(nb)::value, R = decltype(r)::value;
-    if constexpr (!EPI::SYMMETRIC) {
-      if (plan.slices > 1) return go<T, TA, TB, MB, NB, R, true>(p, epi, s);
-    }
+    if (plan.slices > 1) return go<T, TA, TB, MB, NB, R, true>(p, epi, s);
     go<T, TA, TB, MB, NB, R, false>(p, epi, s);
   };
 #define RL_I(x) std::integral_constant<int, x>()
