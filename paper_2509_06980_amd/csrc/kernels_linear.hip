@@ -59,9 +59,10 @@ __device__ __forceinline__ void activate_all(const float (&z)[N], int act, float
 }
 
 // What follows a product's sums; PLAIN: they are rounded and stored, nothing else.
-template <typename T, bool GATED_, bool PLAIN>
+// SHORT: no activation and nothing kept.
+template <typename T, bool GATED_, bool PLAIN, bool SHORT = PLAIN>
 struct Finish {
-  static constexpr bool GATED = GATED_, SYMMETRIC = false;
+  static constexpr bool GATED = GATED_, SYMMETRIC = false, UNROLL = SHORT;
   static constexpr int V = kPiece<T>;
   void* y;
   int64_t y_batch;               // elements from one batch's results to the next's
@@ -72,7 +73,18 @@ struct Finish {
   int64_t residual_stride;
   float* kept;
 
-  __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&u)[V]) const {
+  struct None {};
+  struct Joins { float r[V]; };
+  using Extra = std::conditional_t<PLAIN, None, Joins>;
+  __device__ __forceinline__ void fetch(int, int row, int col, Extra& x) const {
+    if constexpr (!PLAIN) {
+      if (!residual) return;
+      const int64_t at = (int64_t)row * residual_stride + col;
+      if (wide) load_row<float, V>((const float*)residual + at, vec, cols - col, x.r);
+      else load_row<T, V>((const T*)residual + at, vec, cols - col, x.r);
+    }
+  }
+  __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&u)[V], const Extra& joins) const {
     const int left = cols - col;
     if constexpr (!PLAIN) {
       float x[V];
@@ -88,22 +100,21 @@ struct Finish {
           for (int e = 0; e < V; e++) u[e] += x[e];
         }
       }
-      if (kept) {
-        float* const k = kept + (int64_t)row * cols * (GATED ? 2 : 1) + col;
-        store_row<float, V, true>(k, vec, left, v);
-        if constexpr (GATED) store_row<float, V, true>(k + cols, vec, left, u);
+      if constexpr (!SHORT) {
+        if (kept) {
+          float* const k = kept + (int64_t)row * cols * (GATED ? 2 : 1) + col;
+          store_row<float, V, true>(k, vec, left, v);
+          if constexpr (GATED) store_row<float, V, true>(k + cols, vec, left, u);
+        }
+        activate_all<false, V>(v, act, v, x);
       }
-      activate_all<false, V>(v, act, v, x);
       if constexpr (GATED) {
 #pragma unroll
         for (int e = 0; e < V; e++) v[e] *= u[e];
       }
       if (residual) {
-        const int64_t at = (int64_t)row * residual_stride + col;
-        if (wide) load_row<float, V>((const float*)residual + at, vec, left, x);
-        else load_row<T, V>((const T*)residual + at, vec, left, x);
 #pragma unroll
-        for (int e = 0; e < V; e++) v[e] += x[e];
+        for (int e = 0; e < V; e++) v[e] += joins.r[e];
       }
       if (wide) return store_row<float, V, true>((float*)y + (int64_t)row * cols + col, vec, left, v);
     }
@@ -175,7 +186,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(const T* __res
       if constexpr (M == 2) u[e] += sums[1][q][row][c + e];
     }
   }
-  epi(0, row, n0 + c, v, u);
+  typename EPI::Extra extra;
+  epi.fetch(0, row, n0 + c, extra);
+  epi(0, row, n0 + c, v, u, extra);
 }
 template <typename T, typename EPI>
 void launch_few_rows(const T* x, int64_t x_ld, const T* w, int64_t w_ld, int64_t second, int rows, int k, int outer, const EPI& epi, hipStream_t s) {
@@ -327,16 +340,16 @@ In<T> taken(const void* p, int64_t stride, int64_t rows, int width, Room& room, 
 }
 // Rows of a k-strided operand that one descriptor takes: whole chunks in less than 2 GiB
 template <typename T>
-int64_t segment_rows(int64_t ld) { return std::max<int64_t>((1ll << 31) / (ld * (int64_t)sizeof(T)) / kChunk<T> * kChunk<T>, kChunk<T>); }
+int64_t segment_rows(int64_t ld) { return std::max<int64_t>((1ll << 31) / (ld * (int64_t)sizeof(T)) / 64 * 64, 64); }
 
 template <typename T>
 Plan forward_plan(const Shape& n) {      // results, and as a guess a residual or what is kept of each matrix
-  return plan_of<T>({n.rows, n.outer, 1, chunks<T>(n.inner), false, n.mats == 2, false, n.mats == 2 ? 10.f : 8.f});
+  return plan_of<T>({n.rows, n.outer, 1, chunks<T>(n.inner, 64), false, n.mats == 2, false, n.mats == 2 ? 10.f : 8.f});
 }
 template <typename T>
-Plan dx_plan(const Shape& n) { return plan_of<T>({n.rows, n.inner, 1, (int64_t)chunks<T>(n.outer) * n.mats, false, false, true, (float)sizeof(T)}); }
+Plan dx_plan(const Shape& n) { return plan_of<T>({n.rows, n.inner, 1, (int64_t)chunks<T>(n.outer, 64) * n.mats, false, false, true, (float)sizeof(T)}); }
 template <typename T>
-Plan dw_plan(const Shape& n, int batches) { return plan_of<T>({n.outer, n.inner, batches, chunks<T>(n.rows), false, false, true, (float)sizeof(T)}); }
+Plan dw_plan(const Shape& n, int batches) { return plan_of<T>({n.outer, n.inner, batches, chunks<T>(n.rows, 64), false, false, true, (float)sizeof(T)}); }
 
 template <typename T>
 int64_t forward_room(const Shape& n, bool x_direct, bool w_direct) {
@@ -426,6 +439,8 @@ int forward(const Shape& n, const Forward& f, void* ws, hipStream_t s) {
     product(finish(Finish<T, true, false>{}));
   } else if (f.act == RL_ACT_NONE && !f.bias && !f.residual && !f.kept) {
     product(finish(Finish<T, false, true>{}));
+  } else if (f.act == RL_ACT_NONE && !f.kept) {
+    product(finish(Finish<T, false, false, true>{}));
   } else {
     product(finish(Finish<T, false, false>{}));
   }

@@ -95,13 +95,16 @@ struct Gram {
   int ld, n;
   float alpha;
   const float* factor;
+  struct Extra {};
+  static constexpr bool UNROLL = false;
+  __device__ __forceinline__ void fetch(int, int, int, Extra&) const {}
   __device__ __forceinline__ void across(int batch, int row, int col, float (&v)[V]) const {
 #pragma unroll
     for (int e = 0; e < V; e++)
       if (col + e >= n) v[e] = 0.f;
     store_row<T, V>(out + batch * matrix + (int64_t)row * ld + col, true, V, v);
   }
-  __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V]) const {
+  __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V], const Extra&) const {
     float f = alpha;
     if (factor) f = factor[batch];
 #pragma unroll
@@ -120,18 +123,19 @@ struct Polynomial {
   int64_t matrix;
   int ld, n;
   float b, c;
+  struct Extra { float a[V]; };
+  static constexpr bool UNROLL = false;
+  __device__ __forceinline__ void fetch(int batch, int row, int col, Extra& x) const { load_row<T, V>(a + batch * matrix + (int64_t)row * ld + col, true, V, x.a); }
   __device__ __forceinline__ void across(int batch, int row, int col, float (&v)[V]) const {
 #pragma unroll
     for (int e = 0; e < V; e++)
       if (col + e >= n) v[e] = 0.f;
     store_row<T, V>(out + batch * matrix + (int64_t)row * ld + col, true, V, v);
   }
-  __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V]) const {
-    float x[V];
-    load_row<T, V>(a + batch * matrix + (int64_t)row * ld + col, true, V, x);
+  __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V], const Extra& x) const {
 #pragma unroll
     for (int e = 0; e < V; e++) {
-      v[e] = b * x[e] + c * v[e];
+      v[e] = b * x.a[e] + c * v[e];
       if (sizeof(T) == 2 && col + e == row) {
         diagonal[batch * padded(n) + row] = v[e];
         v[e] = 0.f;
@@ -154,16 +158,29 @@ struct Step {
   int64_t matrix;
   int rows, cols, ld, by_column, bf16_out, vec, stream;
   float a, scale;
-  __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V]) const {
+  struct Extra { u32x4 x, low; };      // as they lie in memory
+  static constexpr bool UNROLL = true;
+  __device__ __forceinline__ void fetch(int batch, int row, int col, Extra& e) const {
+    const int64_t at = batch * matrix + (int64_t)row * ld + col;
+    e.x = *(const u32x4*)(x + at);
+    if (sizeof(T) == 2) {
+      e.low = u32x4{0, 0, 0, 0};
+      if (low) e.low = *(const u32x4*)(low + at);
+    }
+  }
+  __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V], const Extra& given) const {
     const int64_t at = batch * matrix + (int64_t)row * ld + col;
     const int left = cols - col;
+    struct alignas(16) Pieces { T x[V]; };
+    const Pieces hp = __builtin_bit_cast(Pieces, given.x);
     float h[V];
-    load_row<T, V>(x + at, true, V, h);
+#pragma unroll
+    for (int e = 0; e < V; e++) h[e] = wide(hp.x[e]);
     if constexpr (sizeof(T) == 2) {
+      const Pieces lp = __builtin_bit_cast(Pieces, given.low);
       float d[V], l[V];
 #pragma unroll
-      for (int e = 0; e < V; e++) d[e] = l[e] = 0.f;
-      if (low) load_row<_Float16, V>(low + at, true, V, l);
+      for (int e = 0; e < V; e++) d[e] = 0.f, l[e] = wide(lp.x[e]);
       if (by_column) {
         load_row<float, V>(diagonal + (int64_t)batch * padded(cols) + col, true, V, d);
       } else {
@@ -217,9 +234,9 @@ struct Layout {      // of the workspace
     constexpr int V = kPiece<T>;
     const int s = n.small(), l = std::max(n.rows, n.columns);
     ld = (int)up(n.columns, V), ld_small = (int)up(s, V);
-    gram = plan_of<T>({s, s, n.count, chunks<T>(l), true, false, true, (float)sizeof(T)});
-    square = plan_of<T>({s, s, n.count, chunks<T>(s), true, false, true, 2.f * sizeof(T)});
-    step = plan_of<T>({n.rows, n.columns, n.count, chunks<T>(s), false, false, n.rows <= n.columns, 8.f});
+    gram = plan_of<T>({s, s, n.count, chunks<T>(l, 64), true, false, true, (float)sizeof(T)});
+    square = plan_of<T>({s, s, n.count, chunks<T>(s, 64), true, false, true, 2.f * sizeof(T)});
+    step = plan_of<T>({n.rows, n.columns, n.count, chunks<T>(s, 64), false, false, n.rows <= n.columns, 8.f});
     matrix = (int64_t)n.rows * ld, small = (int64_t)s * ld_small;
     int64_t at = 0;
     auto take = [&](int64_t b) {

@@ -11,7 +11,7 @@
 // =============================================================================================
 // C[i, j] = sum over k of A[i, k] B[j, k] over tiles of 64 MB rows i and 64 NB columns j: four waves of 32 MB x 32 NB on 32x32x16 (fp32:
 // 32x32x2) matrix instructions, sums in 32 bits.
-// Operands as they lie in memory: k-contiguous ([row][k]) or k-strided (TA, TB: [k][column]).  A chunk of 64 bytes of k (32 elements; fp32 16) of both
+// Operands as they lie in memory: k-contiguous ([row][k]) or k-strided (TA, TB: [k][column]).  A chunk of 64 or 128 bytes of k (32 or 64 elements; fp32 16) of both
 // goes straight from memory into one of R stages in LDS, R - 1 ahead; operands are read half a chunk ahead of the instructions that use them, one
 // barrier a chunk.  A workgroup stays for all its tiles and its loads run on into the next one.
 //   k-contiguous: 64 bytes a row.  The 16-byte piece p of row r is kept at p ^ (r / 4 % 4), so the 16 rows that a read takes in one go lie in
@@ -77,6 +77,15 @@ __device__ __forceinline__ void store_row(T* p, bool vec, int left, const float 
   }
 }
 
+// f(0), f(1), .. f(N - 1) with constants: an array of accumulators indexed by anything else would leave the registers
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void each_part(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>());
+    each_part<N, I + 1>(f);
+  }
+}
+
 // One operand in memory: rows of ld elements, n of them (of one segment), `width` elements of a row used.  k-contiguous: rows are i (or j) and width
 // is k; k-strided: rows are k.
 template <typename T>
@@ -109,30 +118,30 @@ __host__ __device__ __forceinline__ Reach reach_of(bool strided, int64_t ld, int
   const int left = n - at;
   return {at * ld, (unsigned)((((left < rows ? left : rows) - 1) * ld + width) * (int64_t)sizeof(T))};
 }
-__host__ __device__ __forceinline__ unsigned chunk_step(bool strided, int64_t ld) { return strided ? (unsigned)ld * 64u : 64u; }
-template <typename T>
-constexpr int kChunk = 64 / sizeof(T);
+__host__ __device__ __forceinline__ unsigned chunk_step(bool strided, int64_t ld, int bytes) { return (strided ? (unsigned)ld : 1u) * (unsigned)bytes; }
 template <typename T>
 constexpr int kPiece = sizeof(T) == 2 ? 8 : 4;      // columns that a lane of the epilogue takes
 // Chunks of all segments, and those of a slice
 template <typename T>
-__host__ __device__ __forceinline__ int chunks(int k) { return (k + kChunk<T> - 1) / kChunk<T>; }
+__host__ __device__ __forceinline__ int chunks(int k, int bytes) { return (k + bytes / (int)sizeof(T) - 1) / (bytes / (int)sizeof(T)); }
 __host__ __device__ __forceinline__ int slice_begin(int slice, int slices, int n) { return (int)((int64_t)n * slice / slices); }
 
-template <typename T, int MB, int NB, int R>
+template <typename T, int MB, int NB, int R, int CB>
 struct Lds {
-  static constexpr int RING = R * (MB + NB) * 4096, WAVE = 32 * (NB == 1 ? 128 : 256), BYTES = RING + 4 * WAVE;
+  static constexpr int RING = R * (MB + NB) * CB * 64, WAVE = 32 * (NB == 1 ? 128 : 256), BYTES = RING + 4 * WAVE;
 };
 
 // EPI: struct with GATED, SYMMETRIC (lower triangle of tiles only; the epilogue's values are stored a second time across the diagonal), and
-//   void operator()(int batch, int row, int col, float (&v)[V], float (&u)[V], Mirror) const
-// which finishes V columns of a row: u holds the second matrix's sums where GATED.
+//   void fetch(int batch, int row, int col, Extra&) const           what joins these sums from memory
+//   void operator()(int batch, int row, int col, float (&v)[V], float (&u)[V], const Extra&) const
+// which finishes V columns of a row: u holds the second matrix's sums where GATED.  UNROLL: short enough that it may stand there for every row, so that
+// fetch runs a part of the tile ahead.
 template <typename T, typename EPI>
 struct Arguments {
   Product<T> p;
   EPI epi;
 };
-template <typename T, bool TA, bool TB, int MB, int NB, int R, bool SLICED, typename EPI>
+template <typename T, bool TA, bool TB, int MB, int NB, int R, int CB, bool SLICED, typename EPI>
 __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Arguments<T, EPI>) {
   // The arguments are read where they are used, by scalar loads: kept in registers through the products, they would push the descriptors of the loads out of
   // theirs, and one that a vector instruction brings back has to be waited for.
@@ -141,20 +150,22 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
     asm volatile("" : "+s"(p));
     return (const Arguments<T, EPI>*)p;
   };
-  constexpr int BM = 64 * MB, BN = 64 * NB, EL = sizeof(T), KC = kChunk<T>, V = kPiece<T>;
-  constexpr int NA = 4 * MB, PW = MB + NB, BUF = (NA + 4 * NB) * 1024, F = PW / 2;
+  constexpr int BM = 64 * MB, BN = 64 * NB, EL = sizeof(T), KC = CB / EL, V = kPiece<T>;
+  constexpr int NS = CB / 32, KS = KC / NS, PR = CB / 16;      // steps of a chunk, their k; pieces of a row
+  constexpr int PA = MB * (CB / 64), PB = NB * (CB / 64), PW = PA + PB, BUF = PW * 4096, F = PW / 2;      // pieces of 1 KB that a wave loads
+  static_assert(CB == 64 || CB == 128, "chunks of a row");
   constexpr bool GATED = EPI::GATED, SYM = EPI::SYMMETRIC;
   constexpr int JN = GATED ? BN / 2 : BN;      // columns of C that a tile covers
   static_assert((!TA || BM * EL >= 256) && (!TB || BN * EL >= 256), "four blocks of 64 bytes a row");
   static_assert(!GATED || (!TB && NB >= 2), "rows of two matrices in a tile");
   static_assert(!SYM || MB == NB, "square tiles");
-  using L = Lds<T, MB, NB, R>;
+  using L = Lds<T, MB, NB, R, CB>;
   extern __shared__ u32x4 smem[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, wm = wave >> 1, wn = wave & 1;
   const Product<T>& P = arguments()->p;
   const int per_batch = SYM ? P.tiles_i * (P.tiles_i + 1) / 2 : P.tiles_i * P.tiles_j, slices = SLICED ? P.slices : 1;
   const int tiles = per_batch * slices, total = tiles * P.batches;
-  const int c_seg = chunks<T>(P.k), c_all = c_seg * (P.segments - 1) + chunks<T>(P.last_k);
+  const int c_seg = chunks<T>(P.k, CB), c_all = c_seg * (P.segments - 1) + chunks<T>(P.last_k, CB);
   struct Place {
     int i0, j0, batch, slice, c0, c1;      // first row and column of C, batch, slice, its chunks of k
   };
@@ -182,29 +193,34 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
     t.c1 = SLICED ? slice_begin(t.slice + 1, slices, c_all) : c_all;
     return t;
   };
-  const unsigned sa = chunk_step(TA, P.a.ld), sb = chunk_step(TB, P.b.ld);
+  const unsigned sa = chunk_step(TA, P.a.ld, CB), sb = chunk_step(TB, P.b.ld, CB);
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
-  int va[MB], vb[NB];      // this lane's offset of each piece that its wave loads
-  auto offset = [&](int row16, int64_t ld, bool strided, int row_bytes) {      // row16: the 16-row block, k-strided: the KB
+  // k of the lane's piece of a k-contiguous row
+  const int kpos = (CB == 64 ? (lane & 3) ^ (lane >> 4 & 3) : (lane & 7) ^ (lane >> 3 & 7)) * (16 / EL);
+  int va[PA], vb[PB];      // this lane's offset of each piece that its wave loads
+  auto offset = [&](int kb, int64_t ld, bool strided, int row_bytes) {      // kb: the KB of the operand
     if (strided) {
-      const int lanes = row_bytes / 16, k = row16 * (64 / lanes) + lane / lanes, p = lane % lanes;
+      const int lanes = row_bytes / 16, k = kb * (64 / lanes) + lane / lanes, p = lane % lanes;
       const int block = (p >> 2) ^ (EL == 2 ? k & 3 : (k >> 2 & 1) << 1);
       return (int)(k * ld * EL) + (block << 6) + ((p & 3) << 4);
     }
-    return (int)((row16 * 16 + (lane >> 2)) * ld * EL) + (((lane & 3) ^ (lane >> 4 & 3)) << 4);
+    return (int)((kb * (64 / PR) + lane / PR) * ld * EL) + kpos * EL;
   };
 #pragma unroll
-  for (int j = 0; j < MB; j++) va[j] = offset(j * 4 + wave, P.a.ld, TA, BM * EL);
+  for (int j = 0; j < PA; j++) va[j] = offset(j * 4 + wave, P.a.ld, TA, BM * EL);
 #pragma unroll
   // gated: a wave column's rows are half of the first matrix, half of the second: 64 and 64 (NB = 4) or 32 and 32
-  for (int j = 0; j < NB; j++) vb[j] = offset(!GATED ? j * 4 + wave : NB == 4 ? (j >> 1) * 4 + wave : j * 2 + (wave & 1), P.b.ld, TB, BN * EL);
+  for (int j = 0; j < PB; j++) {
+    constexpr int KBS = CB / 64;      // of 16 rows
+    const int n = j * 4 + wave, in = n / (4 * KBS), rest = n % (4 * KBS);      // group of 64 rows, KB of it
+    vb[j] = offset(!GATED ? n : NB == 4 ? (in >> 1) * (4 * KBS) + rest : in * (2 * KBS) + rest % (2 * KBS), P.b.ld, TB, BN * EL);
+  }
   // The loads run R - 1 chunks ahead of the products, from one tile of the workgroup into the next: tile `at`, its chunk lc (li in its segment), operands
   // behind its descriptors (what is read past their end arrives as zeros).  Behind the last tile: its last chunk again, never read.
   u32x4 ra, rb, rb2;
   int at = (int)blockIdx.x - (int)gridDim.x, lc = 0, lend = 0, li = 0, lseg_end = 0;
   Place next{};
   unsigned tail = 0;      // k-contiguous: pieces of the chunk behind the end of k lie out of reach
-  const int kpos = ((lane & 3) ^ (lane >> 4 & 3)) * (16 / EL);
   int seg_k = 0;
   auto enter = [&](int seg) {      // a segment of tile `next`
     const Product<T>& P = arguments()->p;
@@ -247,11 +263,11 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
   };
   auto load = [&](int j, int stage) {      // piece j of this wave
     const unsigned dst = lds0 + (unsigned)stage * BUF + (unsigned)(j * 4 + wave) * 1024u;
-    if (j < MB) {
+    if (j < PA) {
       load_to_lds(dst, TA ? va[j] : (int)(va[j] | tail), ra, (unsigned)li * sa);
     } else {
-      const int off = TB ? vb[j - MB] : (int)(vb[j - MB] | tail);
-      const bool second = GATED && (NB == 4 ? (j - MB) & 1 : wave >> 1);
+      const int off = TB ? vb[j - PA] : (int)(vb[j - PA] | tail);
+      const bool second = GATED && (NB == 4 ? (j - PA) / (CB / 64) & 1 : CB == 64 ? wave >> 1 : (j - PA) & 1);
       if (GATED && second) load_to_lds(dst, off, rb2, (unsigned)li * sb);
       else load_to_lds(dst, off, rb, (unsigned)li * sb);
     }
@@ -269,7 +285,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
     }
   };
   // lane parts of the operand reads: k-contiguous by half a chunk, k-strided by 32-column block
-  int la[TA ? MB : 2], lb[TB ? NB : 2];
+  int la[TA ? MB : NS], lb[TB ? NB : NS];
   auto part = [&](int x, int row_bytes) {
     if constexpr (EL == 2) {
       const int s = lane >> 2 & 3;
@@ -278,11 +294,11 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
       return (lane >> 5) * 4 * row_bytes + (((2 * x) ^ (lane >> 5 << 1)) << 6) + ((lane & 31) << 2);
     }
   };
-  auto part2 = [&](int x) { return (lane & 31) * 64 + (((x * 2 + (lane >> 5)) ^ (lane >> 2 & 3)) << 4); };
+  auto part2 = [&](int x) { return (lane & 31) * CB + (((x * 2 + (lane >> 5)) ^ (CB == 64 ? lane >> 2 & 3 : lane & 7)) << 4); };
 #pragma unroll
-  for (int x = 0; x < (TA ? MB : 2); x++) la[x] = TA ? part(wm * MB + x, BM * EL) : part2(x);
+  for (int x = 0; x < (TA ? MB : NS); x++) la[x] = TA ? part(wm * MB + x, BM * EL) : part2(x);
 #pragma unroll
-  for (int x = 0; x < (TB ? NB : 2); x++) lb[x] = TB ? part(wn * NB + x, BN * EL) : part2(x);
+  for (int x = 0; x < (TB ? NB : NS); x++) lb[x] = TB ? part(wn * NB + x, BN * EL) : part2(x);
   lds_char* const lds = (lds_char*)(__attribute__((address_space(3))) void*)smem;
   auto strided = [&](int at, auto row_bytes) {
     constexpr int RB = decltype(row_bytes)::value;
@@ -299,13 +315,13 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
   };
   auto read_a = [&](int x, int kb, int stage) {
     const int base = stage * BUF;
-    if constexpr (TA) return strided(base + kb * (KC / 2) * BM * EL + la[x], std::integral_constant<int, BM * EL>());
-    else return *(__attribute__((address_space(3))) u32x4*)(lds + base + (wm * MB + x) * 2048 + la[kb]);
+    if constexpr (TA) return strided(base + kb * KS * BM * EL + la[x], std::integral_constant<int, BM * EL>());
+    else return *(__attribute__((address_space(3))) u32x4*)(lds + base + (wm * MB + x) * (32 * CB) + la[kb]);
   };
   auto read_b = [&](int x, int kb, int stage) {
-    const int base = stage * BUF + NA * 1024;
-    if constexpr (TB) return strided(base + kb * (KC / 2) * BN * EL + lb[x], std::integral_constant<int, BN * EL>());
-    else return *(__attribute__((address_space(3))) u32x4*)(lds + base + (wn * NB + x) * 2048 + lb[kb]);
+    const int base = stage * BUF + PA * 4096;
+    if constexpr (TB) return strided(base + kb * KS * BN * EL + lb[x], std::integral_constant<int, BN * EL>());
+    else return *(__attribute__((address_space(3))) u32x4*)(lds + base + (wn * NB + x) * (32 * CB) + lb[kb]);
   };
   if ((int)blockIdx.x >= total) return;
   lc = -1, li = -1;
@@ -338,30 +354,30 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
       for (int c = here.c0; c < here.c1; c++) {
         const int sn = sc + 1 == R ? 0 : sc + 1;
         __builtin_amdgcn_sched_barrier(0);
-        // the instructions of half a chunk (16 k), one memory instruction behind each: the operands of the next half first, then this half's share of the loads,
-        // the rest of chunk c + R - 1 or the first F pieces of chunk c + R
+        // the instructions of a step (16 k), one memory instruction behind each: the operands of the next step first, then this step's share of the loads: in
+        // the chunk's last step, which begins with the barrier, the first F pieces of chunk c + R; in its first the rest of chunk c + R - 1
         constexpr int S = MB * NB, Q = MB + NB;
 #pragma unroll
-        for (int g = 0; g < 2 * MB; g++) {
-          const int a = g % MB, st = g / MB;
-          if (g == MB) {     // chunk c + 1 has landed for every wave, chunk c is read out by every wave
+        for (int g = 0; g < NS * MB; g++) {
+          const int a = g % MB, st = g / MB, now = st & 1;
+          if (g == (NS - 1) * MB) {     // chunk c + 1 has landed for every wave, chunk c is read out by every wave
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((R - 2) * PW) : "memory");
             __builtin_amdgcn_s_barrier();
           }
-          const int stage = st == 0 ? sc : sn, kb = 1 - st, first = st == 0 ? F : 0, n = st == 0 ? PW - F : F;
+          const int stage = st < NS - 1 ? sc : sn, kb = st < NS - 1 ? st + 1 : 0, first = st == 0 ? F : 0, n = st == 0 ? PW - F : st == NS - 1 ? F : 0;
 #pragma unroll
           for (int b = 0; b < NB; b++) {
-            mfma(av[st][a], bv[st][b], acc[a][b]);
+            mfma(av[now][a], bv[now][b], acc[a][b]);
 #pragma unroll
             for (int q = 0; q < Q; q++)      // in the order of their use
               if (q * S / (2 * Q) == a * NB + b) {
                 const int x = q == 0 ? 0 : q <= NB ? MB + q - 1 : q - NB;
-                if (x < MB) av[1 - st][x] = read_a(x, kb, stage);
-                else bv[1 - st][x - MB] = read_b(x - MB, kb, stage);
+                if (x < MB) av[1 - now][x] = read_a(x, kb, stage);
+                else bv[1 - now][x - MB] = read_b(x - MB, kb, stage);
               }
 #pragma unroll
             for (int j = 0; j < PW; j++)
-              if (j < n && S / 2 + j * (S - S / 2) / n == a * NB + b) load(first + j, st == 0 ? sl : sc);
+              if (j < n && (n > S / 2 ? j * S / n : S / 2 + j * (S - S / 2) / n) == a * NB + b) load(first + j, st == 0 ? sl : sc);
             if (g == MB - 1 && b == NB - 1) advance();
             __builtin_amdgcn_sched_barrier(0);
           }
@@ -375,7 +391,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
     int ln = lane;
     asm volatile("" : "+v"(ln));      // or what follows from the lane alone is kept in registers through the products
     // one element of a result: read as a whole, the 16 registers of an accumulator would be copied and spill
-    auto val = [&](int a, int b, int e) {
+    auto val = [&](int a, int b, int e) __attribute__((always_inline)) {
       if (MB * NB <= 8) return acc[a][b][e];
       float x;
       asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[a][b][e]));
@@ -384,11 +400,28 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
     constexpr int W = NB == 1 ? 32 : 64, PR = W / 4;      // columns through LDS at a time, 16-byte pieces of a row
     lds_char* const mine = lds + L::RING + wave * L::WAVE;
     auto piece = [&](int r, int p) { return mine + r * (W * 4) + ((p ^ (r & (PR - 1))) << 4); };
-    auto through = [&](int a, int b0, int b1, int col) {      // blocks b0 and b1 (gated: of the second matrix); col: of C, the first of b0
+    constexpr int CN = GATED ? W / 2 : W, LANES = CN / V, PASSES = 32 * LANES / 64;      // columns of C, lanes of a row
+    constexpr int GROUPS = GATED ? NB / 2 : NB == 1 ? 1 : NB / 2, PARTS = MB * GROUPS;       // parts of 32 rows
+    auto column = [&](int group) { return here.j0 + (GATED ? wn * 16 * NB + group * 32 : wn * 32 * NB + group * 64) + ln % LANES * V; };
+    // what joins the sums from memory is requested a part ahead
+    using Extra = typename EPI::Extra;
+    Extra extra[2][EPI::UNROLL ? PASSES : 1];
+    auto fetch = [&](auto constant) __attribute__((always_inline)) {
+      constexpr int part = decltype(constant)::value;
+      if constexpr (EPI::UNROLL && !SLICED) {
+        const Arguments<T, EPI>& all = *arguments();
+        const int r0 = here.i0 + (wm * MB + part / GROUPS) * 32 + ln / LANES, col = column(part % GROUPS);
+#pragma unroll
+        for (int i = 0; i < PASSES; i++)
+          if (r0 + i * (64 / LANES) < all.p.rows && col < all.p.cols) all.epi.fetch(here.batch, r0 + i * (64 / LANES), col, extra[part & 1][i]);
+      }
+    };
+    auto through = [&](auto constant) __attribute__((always_inline)) {      // block a of rows, blocks b0 and b1 (gated: of the second matrix) of columns
+      constexpr int part = decltype(constant)::value, a = part / GROUPS, group = part % GROUPS, b0 = GATED ? group : 2 * group, b1 = GATED ? group + NB / 2 : b0 + 1;
       const Arguments<T, EPI>& all = *arguments();
       const Product<T>& P = all.p;
       const EPI& epi = all.epi;
-      auto put = [&](int b, int half) {
+      auto put = [&](int b, int half) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < 4; u++)
           *(__attribute__((address_space(3))) f32x4*)piece(ln & 31, half * 8 + 2 * u + (ln >> 5)) =
@@ -397,12 +430,10 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
       put(b0, 0);
       if constexpr (NB > 1) put(b1, 1);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      constexpr int CN = GATED ? W / 2 : W, LANES = CN / V;      // columns of C, lanes of a row
-      const int r0 = here.i0 + (wm * MB + a) * 32, c = ln % LANES * V;
-#pragma unroll 1
-      for (int r = ln / LANES; r < 32; r += 64 / LANES) {
+      const int r0 = here.i0 + (wm * MB + a) * 32, c = ln % LANES * V, col = column(group) - c;
+      auto pass = [&](int r, const Extra* given) __attribute__((always_inline)) {
         float v[V], u[V];
-        auto get = [&](int first, float (&to)[V]) {
+        auto get = [&](int first, float (&to)[V]) __attribute__((always_inline)) {
 #pragma unroll
           for (int q = 0; q < V / 4; q++) {
             const f32x4 x = *(__attribute__((address_space(3))) f32x4*)piece(r, first + q);
@@ -418,8 +449,12 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
             float* to = P.part + (((int64_t)here.slice * P.batches + here.batch) * P.rows + r0 + r) * (GATED ? 2 * ld : ld) + col + c;
             store_row<float, V>(to, true, V, v);
             if constexpr (GATED) store_row<float, V>(to + ld, true, V, u);
+          } else if (given) {
+            epi(here.batch, r0 + r, col + c, v, u, *given);
           } else {
-            epi(here.batch, r0 + r, col + c, v, u);
+            Extra own;
+            epi.fetch(here.batch, r0 + r, col + c, own);
+            epi(here.batch, r0 + r, col + c, v, u, own);
           }
         }
         if constexpr (SYM && !SLICED) {
@@ -429,6 +464,13 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
               *(__attribute__((address_space(3))) f32x4*)piece(r, c / 4 + q) = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
           }
         }
+      };
+      if constexpr (EPI::UNROLL && !SLICED) {
+#pragma unroll
+        for (int i = 0; i < PASSES; i++) pass(ln / LANES + i * (64 / LANES), &extra[part & 1][i]);
+      } else {
+#pragma unroll 1
+        for (int r = ln / LANES; r < 32; r += 64 / LANES) pass(r, nullptr);
       }
       if constexpr (SYM && !SLICED) {
         if (here.i0 != here.j0) {      // column c of these 32 rows is a part of row c across the diagonal
@@ -446,18 +488,12 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_sched_barrier(0);
     };
-#pragma unroll
-    for (int a = 0; a < MB; a++) {
-      if constexpr (GATED) {
-#pragma unroll
-        for (int b = 0; b < NB / 2; b++) through(a, b, b + NB / 2, here.j0 + wn * 16 * NB + b * 32);
-      } else if constexpr (NB == 1) {
-        through(a, 0, 0, here.j0 + wn * 32);
-      } else {
-#pragma unroll
-        for (int b = 0; b < NB; b += 2) through(a, b, b + 1, here.j0 + wn * 32 * NB + b * 32);
-      }
-    }
+    fetch(std::integral_constant<int, 0>());
+    each_part<PARTS>([&](auto part) __attribute__((always_inline)) {
+      constexpr int next = decltype(part)::value + 1;
+      if constexpr (next < PARTS) fetch(std::integral_constant<int, next>());
+      through(part);
+    });
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // loads into this LDS
 }
@@ -486,7 +522,9 @@ __global__ __launch_bounds__(256) void join_kernel(Product<T> P, EPI epi) {
         for (int e = 0; e < V; e++) u[e] += x[e];
       }
     }
-    epi((int)(row / P.rows), (int)(row % P.rows), c, v, u);
+    typename EPI::Extra x;
+    epi.fetch((int)(row / P.rows), (int)(row % P.rows), c, x);
+    epi((int)(row / P.rows), (int)(row % P.rows), c, v, u, x);
   }
 }
 
@@ -513,7 +551,9 @@ __global__ __launch_bounds__(256) void join_symmetric_kernel(Product<T> P, EPI e
 #pragma unroll
       for (int e = 0; e < V; e++) v[e] += x[e];
     }
-    epi(batch, r0 + r, c0 + c, v, u);
+    typename EPI::Extra extra;
+    epi.fetch(batch, r0 + r, c0 + c, extra);
+    epi(batch, r0 + r, c0 + c, v, u, extra);
 #pragma unroll
     for (int e = 0; e < V; e++) block[r][c + e] = v[e];
   }
@@ -529,10 +569,10 @@ __global__ __launch_bounds__(256) void join_symmetric_kernel(Product<T> P, EPI e
   }
 }
 
-template <typename T, bool TA, bool TB, int MB, int NB, int R, bool SLICED, typename EPI>
+template <typename T, bool TA, bool TB, int MB, int NB, int R, int CB, bool SLICED, typename EPI>
 void go(const Product<T>& p, const EPI& epi, hipStream_t s) {
-  constexpr int lds = Lds<T, MB, NB, R>::BYTES;
-  auto kernel = product_kernel<T, TA, TB, MB, NB, R, SLICED, EPI>;
+  constexpr int lds = Lds<T, MB, NB, R, CB>::BYTES;
+  auto kernel = product_kernel<T, TA, TB, MB, NB, R, CB, SLICED, EPI>;
   static std::atomic<uint64_t> done;      // more than 64 KB of LDS need an opt-in, once per kernel and device
   int dev = 0;
   (void)hipGetDevice(&dev);
@@ -555,6 +595,9 @@ void go(const Product<T>& p, const EPI& epi, hipStream_t s) {
 
 // ---- the plan of a product: tile and slices -----------------------------------------------------------------------------------
 struct Plan { int mb, nb, slices; };
+// Bytes of a row in a chunk of the tile
+template <typename T>
+constexpr int chunk_bytes(int mb, bool strided) { return sizeof(T) == 2 && mb == 4 && !strided ? 128 : 64; }
 // The cheapest by estimate.  A round of tiles takes what its chunks take and some us to begin and end; what the epilogue reads and writes (`bytes` an
 // element of C) goes at 4.5 TB/s, half of it beside the other workgroup's products where a CU holds two; sums of slices are written and read at that rate
 // too.  us of a chunk fitted on products of 2744 to 4096 rows, K of 1024 to 9728, batches of 28: 256 x 256 (one workgroup a CU) 0.87, 192 x 256
@@ -596,7 +639,7 @@ struct Probe {
 };
 inline thread_local Probe* probe = nullptr;
 template <typename T>
-void find_overreach(const Product<T>& p, bool strided_a, bool strided_b, int rows_i, int rows_j, int64_t second) {
+void find_overreach(const Product<T>& p, bool strided_a, bool strided_b, int rows_i, int rows_j, int64_t second, int bytes) {
   const int64_t el = sizeof(T);
   probe->products++;
   auto operand = [&](bool strided, const Operand<T>& o, int tiles, int size, int64_t more) {
@@ -606,11 +649,11 @@ void find_overreach(const Product<T>& p, bool strided_a, bool strided_b, int row
           const bool end = seg == p.segments - 1;
           const Reach r = reach_of<T>(strided, o.ld, end ? o.last_rows : o.rows, end ? o.last_width : o.width, i * size, size);
           const int64_t at = batch * o.batch + seg * o.segment + r.begin + more;
-          const int n = chunks<T>(end ? p.last_k : p.k);
+          const int n = chunks<T>(end ? p.last_k : p.k, bytes);
           probe->buffers = std::max({probe->buffers, -at * el, at * el + (int64_t)r.bytes - o.elements * el});
           // 64 bits beside what the kernel computes in 32
-          const int64_t step = strided ? o.ld * 64 : 64, rows = strided ? kChunk<T> : std::min<int64_t>(size, (end ? o.last_rows : o.rows) - i * size);
-          const int64_t furthest = strided ? (kChunk<T> - 1) * o.ld * el + size * el : (rows - 1) * o.ld * el + 64;
+          const int64_t step = strided ? o.ld * bytes : bytes, rows = strided ? bytes / el : std::min<int64_t>(size, (end ? o.last_rows : o.rows) - i * size);
+          const int64_t furthest = strided ? (bytes / el - 1) * o.ld * el + size * el : (rows - 1) * o.ld * el + bytes;
           if (furthest >= 1ll << 31 || (n - 1) * step >= 1ll << 32 || (int64_t)r.bytes < 0) probe->offsets = std::max<int64_t>(probe->offsets, 1ll << 32);
           probe->offsets = std::max(probe->offsets, (n - 1) * step + 1 - (int64_t)r.bytes);
         }
@@ -623,26 +666,26 @@ template <typename T, bool TA, bool TB, typename EPI>
 void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
   const int bn = EPI::GATED ? 32 * plan.nb : 64 * plan.nb;
   p.tiles_i = (p.rows + 64 * plan.mb - 1) / (64 * plan.mb), p.tiles_j = (p.cols + bn - 1) / bn, p.slices = plan.slices, p.group = 4;
-  if (probe) return find_overreach(p, TA, TB, 64 * plan.mb, bn, EPI::GATED ? p.b2 : 0);
-  auto with = [&](auto mb, auto nb, auto r) {
-    constexpr int MB = decltype(mb)::value, NB = decltype(nb)::value, R = decltype(r)::value;
-    if (plan.slices > 1) return go<T, TA, TB, MB, NB, R, true>(p, epi, s);
-    go<T, TA, TB, MB, NB, R, false>(p, epi, s);
+  if (probe) return find_overreach(p, TA, TB, 64 * plan.mb, bn, EPI::GATED ? p.b2 : 0, chunk_bytes<T>(plan.mb, TA || TB));
+  auto with = [&](auto mb, auto nb, auto r, auto cb) {
+    constexpr int MB = decltype(mb)::value, NB = decltype(nb)::value, R = decltype(r)::value, CB = decltype(cb)::value;
+    if (plan.slices > 1) return go<T, TA, TB, MB, NB, R, CB, true>(p, epi, s);
+    go<T, TA, TB, MB, NB, R, CB, false>(p, epi, s);
   };
 #define RL_I(x) std::integral_constant<int, x>()
   if constexpr (sizeof(T) == 2) {
     if constexpr (!EPI::SYMMETRIC) {
-      if (plan.mb == 4) return with(RL_I(4), RL_I(4), RL_I(4));
+      if (plan.mb == 4) return with(RL_I(4), RL_I(4), std::integral_constant<int, TA || TB ? 4 : 2>(), std::integral_constant<int, TA || TB ? 64 : 128>());
     }
     if constexpr (!TA && !TB && !EPI::SYMMETRIC) {
-      if (plan.mb == 3) return with(RL_I(3), RL_I(4), RL_I(4));
+      if (plan.mb == 3) return with(RL_I(3), RL_I(4), RL_I(4), RL_I(64));
     }
-    with(RL_I(2), RL_I(2), RL_I(3));
+    with(RL_I(2), RL_I(2), RL_I(3), RL_I(64));
   } else {
     if constexpr (!EPI::GATED) {
-      if (plan.mb == 1) return with(RL_I(1), RL_I(1), RL_I(4));
+      if (plan.mb == 1) return with(RL_I(1), RL_I(1), RL_I(4), RL_I(64));
     }
-    with(RL_I(2), RL_I(2), RL_I(3));
+    with(RL_I(2), RL_I(2), RL_I(3), RL_I(64));
   }
 #undef RL_I
 }
