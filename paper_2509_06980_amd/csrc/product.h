@@ -128,7 +128,7 @@ __host__ __device__ __forceinline__ int slice_begin(int slice, int slices, int n
 
 template <typename T, int MB, int NB, int R, int CB>
 struct Lds {
-  static constexpr int RING = R * (MB + NB) * CB * 64, WAVE = 32 * (NB == 1 ? 128 : 256), BYTES = RING + 4 * WAVE;
+  static constexpr int RING = R * (MB + NB) * CB * 64, W = NB == 1 || (NB == 2 && CB == 128) ? 32 : 64, WAVE = 32 * W * 4, BYTES = RING + 4 * WAVE;
 };
 
 // EPI: struct with GATED, SYMMETRIC (lower triangle of tiles only; the epilogue's values are stored a second time across the diagonal), and
@@ -397,12 +397,13 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
       asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[a][b][e]));
       return x;
     };
-    constexpr int W = NB == 1 ? 32 : 64, PR = W / 4;      // columns through LDS at a time, 16-byte pieces of a row
+    constexpr int W = L::W, PW_ROW = W / 4;      // columns through LDS at a time, 16-byte pieces of a row
+    static_assert(!GATED || W == 64, "halves of two matrices");
     lds_char* const mine = lds + L::RING + wave * L::WAVE;
-    auto piece = [&](int r, int p) { return mine + r * (W * 4) + ((p ^ (r & (PR - 1))) << 4); };
+    auto piece = [&](int r, int p) { return mine + r * (W * 4) + ((p ^ (r & (PW_ROW - 1))) << 4); };
     constexpr int CN = GATED ? W / 2 : W, LANES = CN / V, PASSES = 32 * LANES / 64;      // columns of C, lanes of a row
-    constexpr int GROUPS = GATED ? NB / 2 : NB == 1 ? 1 : NB / 2, PARTS = MB * GROUPS;       // parts of 32 rows
-    auto column = [&](int group) { return here.j0 + (GATED ? wn * 16 * NB + group * 32 : wn * 32 * NB + group * 64) + ln % LANES * V; };
+    constexpr int GROUPS = GATED ? NB / 2 : 32 * NB / W, PARTS = MB * GROUPS;       // parts of 32 rows
+    auto column = [&](int group) { return here.j0 + (GATED ? wn * 16 * NB + group * 32 : wn * 32 * NB + group * W) + ln % LANES * V; };
     // what joins the sums from memory is requested a part ahead
     using Extra = typename EPI::Extra;
     Extra extra[2][EPI::UNROLL ? PASSES : 1];
@@ -417,7 +418,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
       }
     };
     auto through = [&](auto constant) __attribute__((always_inline)) {      // block a of rows, blocks b0 and b1 (gated: of the second matrix) of columns
-      constexpr int part = decltype(constant)::value, a = part / GROUPS, group = part % GROUPS, b0 = GATED ? group : 2 * group, b1 = GATED ? group + NB / 2 : b0 + 1;
+      constexpr int part = decltype(constant)::value, a = part / GROUPS, group = part % GROUPS, b0 = GATED ? group : W / 32 * group, b1 = GATED ? group + NB / 2 : b0 + 1;
       const Arguments<T, EPI>& all = *arguments();
       const Product<T>& P = all.p;
       const EPI& epi = all.epi;
@@ -428,7 +429,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
               f32x4{val(a, b, 4 * u), val(a, b, 4 * u + 1), val(a, b, 4 * u + 2), val(a, b, 4 * u + 3)};
       };
       put(b0, 0);
-      if constexpr (NB > 1) put(b1, 1);
+      if constexpr (W == 64) put(b1, 1);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       const int r0 = here.i0 + (wm * MB + a) * 32, c = ln % LANES * V, col = column(group) - c;
       auto pass = [&](int r, const Extra* given) __attribute__((always_inline)) {
@@ -597,7 +598,7 @@ void go(const Product<T>& p, const EPI& epi, hipStream_t s) {
 struct Plan { int mb, nb, slices; };
 // Bytes of a row in a chunk of the tile
 template <typename T>
-constexpr int chunk_bytes(int mb, bool strided) { return sizeof(T) == 2 && mb == 4 && !strided ? 128 : 64; }
+constexpr int chunk_bytes(int mb, bool strided, bool gated) { return sizeof(T) == 2 && ((mb == 4 && !strided) || (mb == 2 && !gated)) ? 128 : 64; }
 // The cheapest by estimate.  A round of tiles takes what its chunks take and some us to begin and end; what the epilogue reads and writes (`bytes` an
 // element of C) goes at 4.5 TB/s, half of it beside the other workgroup's products where a CU holds two; sums of slices are written and read at that rate
 // too.  us of a chunk fitted on products of 2744 to 4096 rows, K of 1024 to 9728, batches of 28: 256 x 256 (one workgroup a CU) 0.87, 192 x 256
@@ -622,7 +623,7 @@ Plan plan_of(const Sizes& z) {
     const int64_t tiles = (z.symmetric ? ti * (ti + 1) / 2 : ti * tj) * z.batches;
     const float epilogue = elements * z.bytes / 4.5e6f * (o.resident > 256 && tiles > o.resident ? 0.5f : 1.f);
     for (int s = 1; s <= 16 && s <= std::max<int64_t>(z.n_chunks / 8, 1); s++) {
-      const float sums = s == 1 ? 0.f : 5.f + (float)s * elements * (z.gated ? 2.f : z.symmetric ? 0.5f : 1.f) * 8.f / 4.5e6f;
+      const float sums = s == 1 ? 0.f : (z.symmetric ? 25.f : 5.f) + (float)s * elements * (z.gated ? 2.f : z.symmetric ? 0.5f : 1.f) * 8.f / 4.5e6f;
       const float us = (float)((tiles * s + o.resident - 1) / o.resident) * ((float)((z.n_chunks + s - 1) / s) * (z.gated ? o.gated_us : o.chunk_us) + 5.f) + epilogue + sums;
       if (us < best_us) best_us = us, best = {o.mb, o.nb, s};
     }
@@ -666,7 +667,7 @@ template <typename T, bool TA, bool TB, typename EPI>
 void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
   const int bn = EPI::GATED ? 32 * plan.nb : 64 * plan.nb;
   p.tiles_i = (p.rows + 64 * plan.mb - 1) / (64 * plan.mb), p.tiles_j = (p.cols + bn - 1) / bn, p.slices = plan.slices, p.group = 4;
-  if (probe) return find_overreach(p, TA, TB, 64 * plan.mb, bn, EPI::GATED ? p.b2 : 0, chunk_bytes<T>(plan.mb, TA || TB));
+  if (probe) return find_overreach(p, TA, TB, 64 * plan.mb, bn, EPI::GATED ? p.b2 : 0, chunk_bytes<T>(plan.mb, TA || TB, EPI::GATED));
   auto with = [&](auto mb, auto nb, auto r, auto cb) {
     constexpr int MB = decltype(mb)::value, NB = decltype(nb)::value, R = decltype(r)::value, CB = decltype(cb)::value;
     if (plan.slices > 1) return go<T, TA, TB, MB, NB, R, CB, true>(p, epi, s);
@@ -680,7 +681,8 @@ void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
     if constexpr (!TA && !TB && !EPI::SYMMETRIC) {
       if (plan.mb == 3) return with(RL_I(3), RL_I(4), RL_I(4), RL_I(64));
     }
-    with(RL_I(2), RL_I(2), RL_I(3), RL_I(64));
+    if constexpr (!EPI::GATED) with(RL_I(2), RL_I(2), RL_I(2), RL_I(128));
+    else with(RL_I(2), RL_I(2), RL_I(3), RL_I(64));
   } else {
     if constexpr (!EPI::GATED) {
       if (plan.mb == 1) return with(RL_I(1), RL_I(1), RL_I(4), RL_I(64));
