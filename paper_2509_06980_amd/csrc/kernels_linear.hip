@@ -196,13 +196,26 @@ void launch_few_rows(const T* x, int64_t x_ld, const T* w, int64_t w_ld, int64_t
 }
 
 // ---- rows of an operand in whole 16 bytes: [rows][ld], zeros behind `width` -----------------------------------------------------------
+// up to three at once
 template <typename T>
-__global__ __launch_bounds__(256) void copy_rows_kernel(const T* __restrict__ x, int64_t stride, int64_t rows, int width, int ld, T* __restrict__ to) {
-  const int64_t n = rows * ld;
+struct Copies {
+  struct One {
+    const T* x;
+    int64_t stride, rows;
+    int width, ld;
+    T* to;
+  } one[3];
+  int n = 0;
+  int64_t most = 0;      // elements of the largest
+};
+template <typename T>
+__global__ __launch_bounds__(256) void copy_rows_kernel(Copies<T> copies) {
+  const typename Copies<T>::One& c = copies.one[blockIdx.y];
+  const int64_t n = c.rows * c.ld;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / ld;
-    const int c = (int)(i - r * ld);
-    to[i] = c < width ? x[r * stride + c] : T(0);
+    const int64_t r = i / c.ld;
+    const int j = (int)(i - r * c.ld);
+    c.to[i] = j < c.width ? c.x[r * c.stride + j] : T(0);
   }
 }
 
@@ -331,12 +344,21 @@ bool direct(const void* p, int64_t stride, int width) {
 template <typename T>
 int64_t copy_bytes(int64_t rows, int width) { return up(rows * up(width, 16 / sizeof(T)) * (int64_t)sizeof(T), kAlign); }
 template <typename T>
-In<T> taken(const void* p, int64_t stride, int64_t rows, int width, Room& room, hipStream_t s) {
-  if (direct<T>(p, stride, width)) return {(const T*)p, stride, width, (rows - 1) * stride + width};
+In<T> copied(const void* p, int64_t stride, int64_t rows, int width, Room& room, Copies<T>& copies) {
   const int ld = (int)up(width, 16 / sizeof(T));
   T* to = (T*)room.take(rows * ld * (int64_t)sizeof(T));
-  if (!probe) copy_rows_kernel<T><<<blocks_for(rows * ld), 256, 0, s>>>((const T*)p, stride, rows, width, ld, to);
+  copies.one[copies.n++] = {(const T*)p, stride, rows, width, ld, to};
+  copies.most = std::max(copies.most, rows * ld);
   return {to, ld, ld, rows * ld};
+}
+template <typename T>
+In<T> taken(const void* p, int64_t stride, int64_t rows, int width, Room& room, Copies<T>& copies) {
+  if (direct<T>(p, stride, width)) return {(const T*)p, stride, width, (rows - 1) * stride + width};
+  return copied<T>(p, stride, rows, width, room, copies);
+}
+template <typename T>
+void make(const Copies<T>& copies, hipStream_t s) {
+  if (copies.n > 0 && !probe) copy_rows_kernel<T><<<dim3((unsigned)std::min<int64_t>((copies.most + 255) / 256, 8192), copies.n), 256, 0, s>>>(copies);
 }
 // Rows of a k-strided operand that one descriptor takes: whole chunks in less than 2 GiB
 template <typename T>
@@ -391,7 +413,7 @@ bool weights_direct(const void* w, int64_t w_stride, const void* up, int64_t up_
 }
 // both matrices alike: both as they lie or both copied
 template <typename T>
-void take_weights(const void* w, int64_t w_stride, const void* up_, int64_t up_stride, const Shape& n, Room& room, hipStream_t s, In<T>& a, In<T>& b) {
+void take_weights(const void* w, int64_t w_stride, const void* up_, int64_t up_stride, const Shape& n, Room& room, Copies<T>& copies, In<T>& a, In<T>& b) {
   b = {};
   if (weights_direct<T>(w, w_stride, up_, up_stride, n)) {
     const int64_t elements = (n.outer - 1) * w_stride + n.inner;
@@ -399,22 +421,18 @@ void take_weights(const void* w, int64_t w_stride, const void* up_, int64_t up_s
     if (n.mats == 2) b = {(const T*)up_, up_stride, n.inner, elements};
     return;
   }
-  auto copy = [&](const void* p, int64_t stride) {
-    const int ld = (int)up(n.inner, 16 / sizeof(T));
-    T* to = (T*)room.take((int64_t)n.outer * ld * (int64_t)sizeof(T));
-    if (!probe) copy_rows_kernel<T><<<blocks_for((int64_t)n.outer * ld), 256, 0, s>>>((const T*)p, stride, n.outer, n.inner, ld, to);
-    return In<T>{to, ld, ld, (int64_t)n.outer * ld};
-  };
-  a = copy(w, w_stride);
-  if (n.mats == 2) b = copy(up_, up_stride);
+  a = copied<T>(w, w_stride, n.outer, n.inner, room, copies);
+  if (n.mats == 2) b = copied<T>(up_, up_stride, n.outer, n.inner, room, copies);
 }
 
 template <typename T>
 int forward(const Shape& n, const Forward& f, void* ws, hipStream_t s) {
   Room room{(char*)ws};
-  const In<T> x = taken<T>(f.x, f.x_stride, n.rows, n.inner, room, s);
+  Copies<T> copies;
+  const In<T> x = taken<T>(f.x, f.x_stride, n.rows, n.inner, room, copies);
   In<T> w, u;
-  take_weights<T>(f.w, f.w_stride, f.up, f.up_stride, n, room, s, w, u);
+  take_weights<T>(f.w, f.w_stride, f.up, f.up_stride, n, room, copies, w, u);
+  make(copies, s);
   Product<T> p{};
   p.k = p.last_k = w.width, p.segments = 1, p.batches = 1;
   p.a = {x.p, x.ld, 0, 0, n.rows, n.rows, w.width, w.width, x.elements};
@@ -490,11 +508,13 @@ int backward(const Shape& n, const Backward& f, void* ws, hipStream_t s) {
   const int64_t dz_matrix = (int64_t)n.rows * ldz;      // from dz to du
   Finish<T, false, true> e{};
   e.cols = n.inner;
-  Room rest = room;
+  Copies<T> copies;
+  In<T> w, u, x;
+  if (f.dx) take_weights<T>(f.w, f.w_stride, f.up, f.up_stride, n, room, copies, w, u);
+  if (f.dw || f.dup) x = taken<T>(f.x, f.x_stride, n.rows, n.inner, room, copies);
+  make(copies, s);
   if (f.dx) {
-    In<T> w, u;
-    Room r = rest;
-    take_weights<T>(f.w, f.w_stride, f.up, f.up_stride, n, r, s, w, u);
+    Room r = room;      // both products' sums of slices lie in one place
     Product<T> p{};
     p.a = {dz.p, dz.ld, 0, dz_matrix, n.rows, n.rows, dz.width, dz.width, dz.elements};
     p.b = {w.p, w.ld, 0, n.mats == 2 && !probe ? u.p - w.p : 0, n.outer, n.outer, w.width, w.width, w.elements};
@@ -506,8 +526,7 @@ int backward(const Shape& n, const Backward& f, void* ws, hipStream_t s) {
     launch<T, false, true>(p, plan, e, s);
   }
   if (f.dw || f.dup) {
-    Room r = rest;
-    const In<T> x = taken<T>(f.x, f.x_stride, n.rows, n.inner, r, s);
+    Room r = room;
     const int64_t most = segment_rows<T>(std::max(dz.ld, x.ld)), segments = (n.rows + most - 1) / most, last = n.rows - (segments - 1) * most;
     const int each = (int)std::min<int64_t>(most, n.rows);
     const bool first = f.dw, both = f.dw && f.dup;

@@ -529,10 +529,12 @@ __global__ __launch_bounds__(256) void join_kernel(Product<T> P, EPI epi) {
   }
 }
 
-// The same for a symmetric product, of which the slices hold the tiles on and under the diagonal: a workgroup takes 64 x 64 elements and stores them across too.
+template <typename T>
+constexpr int kJoinBlock = sizeof(T) == 2 ? 64 : 32;
+// The same for a symmetric product, of which the slices hold the tiles on and under the diagonal: a workgroup takes B x B elements and stores them across too.
 template <typename T, typename EPI>
 __global__ __launch_bounds__(256) void join_symmetric_kernel(Product<T> P, EPI epi) {
-  constexpr int V = kPiece<T>, B = 64;
+  constexpr int V = kPiece<T>, B = kJoinBlock<T>;
   __shared__ float block[B][B + 1];
   const int v0 = blockIdx.x;
   int i = (int)((__builtin_sqrtf(8.f * v0 + 1.f) - 1.f) * 0.5f);
@@ -586,7 +588,7 @@ void go(const Product<T>& p, const EPI& epi, hipStream_t s) {
   // as many workgroups as the 256 CUs hold at once
   kernel<<<(unsigned)std::min<int64_t>(tiles, 256 * (160 * 1024 / lds)), 256, lds, s>>>(Arguments<T, EPI>{p, epi});
   if constexpr (SLICED && EPI::SYMMETRIC) {
-    const unsigned n = (unsigned)(p.rows + 63) / 64;
+    const unsigned n = (unsigned)(p.rows + kJoinBlock<T> - 1) / kJoinBlock<T>;
     join_symmetric_kernel<T, EPI><<<dim3(n * (n + 1) / 2, p.batches), 256, 0, s>>>(p, epi);
   } else if constexpr (SLICED) {
     const int64_t n = (int64_t)p.batches * p.rows * ((p.cols + kPiece<T> - 1) / kPiece<T>);
@@ -623,7 +625,7 @@ Plan plan_of(const Sizes& z) {
     const int64_t tiles = (z.symmetric ? ti * (ti + 1) / 2 : ti * tj) * z.batches;
     const float epilogue = elements * z.bytes / 4.5e6f * (o.resident > 256 && tiles > o.resident ? 0.5f : 1.f);
     for (int s = 1; s <= 16 && s <= std::max<int64_t>(z.n_chunks / 8, 1); s++) {
-      const float sums = s == 1 ? 0.f : (z.symmetric ? 25.f : 5.f) + (float)s * elements * (z.gated ? 2.f : z.symmetric ? 0.5f : 1.f) * 8.f / 4.5e6f;
+      const float sums = s == 1 ? 0.f : (z.symmetric ? sizeof(T) == 2 ? 25.f : 8.f : 5.f) + (float)s * elements * (z.gated ? 2.f : z.symmetric ? 0.5f : 1.f) * 8.f / 4.5e6f;
       const float us = (float)((tiles * s + o.resident - 1) / o.resident) * ((float)((z.n_chunks + s - 1) / s) * (z.gated ? o.gated_us : o.chunk_us) + 5.f) + epilogue + sums;
       if (us < best_us) best_us = us, best = {o.mb, o.nb, s};
     }
