@@ -126,9 +126,11 @@ template <typename T>
 __host__ __device__ __forceinline__ int chunks(int k, int bytes) { return (k + bytes / (int)sizeof(T) - 1) / (bytes / (int)sizeof(T)); }
 __host__ __device__ __forceinline__ int slice_begin(int slice, int slices, int n) { return (int)((int64_t)n * slice / slices); }
 
-template <typename T, int MB, int NB, int R, int CB>
+template <typename T, int MB, int NB, int R, int CB, bool GATED>
 struct Lds {
-  static constexpr int RING = R * (MB + NB) * CB * 64, W = NB == 1 || (NB == 2 && CB == 128) ? 32 : 64, WAVE = 32 * W * 4, BYTES = RING + 4 * WAVE;
+  // of an epilogue: columns and rows of a part; of 128 x 128 tiles half as much, so that a CU holds two workgroups
+  static constexpr bool HALF = NB == 2 && CB == 128;
+  static constexpr int RING = R * (MB + NB) * CB * 64, W = NB == 1 || (HALF && !GATED) ? 32 : 64, ROWS = HALF && GATED ? 16 : 32, WAVE = ROWS * W * 4, BYTES = RING + 4 * WAVE;
 };
 
 // EPI: struct with GATED, SYMMETRIC (lower triangle of tiles only; the epilogue's values are stored a second time across the diagonal), and
@@ -159,7 +161,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
   static_assert((!TA || BM * EL >= 256) && (!TB || BN * EL >= 256), "four blocks of 64 bytes a row");
   static_assert(!GATED || (!TB && NB >= 2), "rows of two matrices in a tile");
   static_assert(!SYM || MB == NB, "square tiles");
-  using L = Lds<T, MB, NB, R, CB>;
+  using L = Lds<T, MB, NB, R, CB, GATED>;
   extern __shared__ u32x4 smem[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, wm = wave >> 1, wn = wave & 1;
   const Product<T>& P = arguments()->p;
@@ -401,8 +403,8 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
     static_assert(!GATED || W == 64, "halves of two matrices");
     lds_char* const mine = lds + L::RING + wave * L::WAVE;
     auto piece = [&](int r, int p) { return mine + r * (W * 4) + ((p ^ (r & (PW_ROW - 1))) << 4); };
-    constexpr int CN = GATED ? W / 2 : W, LANES = CN / V, PASSES = 32 * LANES / 64;      // columns of C, lanes of a row
-    constexpr int GROUPS = GATED ? NB / 2 : 32 * NB / W, PARTS = MB * GROUPS;       // parts of 32 rows
+    constexpr int CN = GATED ? W / 2 : W, LANES = CN / V, PR = L::ROWS, PASSES = PR * LANES / 64;      // columns of C, lanes of a row, rows of a part
+    constexpr int GROUPS = GATED ? NB / 2 : 32 * NB / W, SPLIT = 32 / PR, PARTS = MB * GROUPS * SPLIT;
     auto column = [&](int group) { return here.j0 + (GATED ? wn * 16 * NB + group * 32 : wn * 32 * NB + group * W) + ln % LANES * V; };
     // what joins the sums from memory is requested a part ahead
     using Extra = typename EPI::Extra;
@@ -411,27 +413,28 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
       constexpr int part = decltype(constant)::value;
       if constexpr (EPI::UNROLL && !SLICED) {
         const Arguments<T, EPI>& all = *arguments();
-        const int r0 = here.i0 + (wm * MB + part / GROUPS) * 32 + ln / LANES, col = column(part % GROUPS);
+        const int r0 = here.i0 + (wm * MB + part / SPLIT / GROUPS) * 32 + part % SPLIT * PR + ln / LANES, col = column(part / SPLIT % GROUPS);
 #pragma unroll
         for (int i = 0; i < PASSES; i++)
           if (r0 + i * (64 / LANES) < all.p.rows && col < all.p.cols) all.epi.fetch(here.batch, r0 + i * (64 / LANES), col, extra[part & 1][i]);
       }
     };
     auto through = [&](auto constant) __attribute__((always_inline)) {      // block a of rows, blocks b0 and b1 (gated: of the second matrix) of columns
-      constexpr int part = decltype(constant)::value, a = part / GROUPS, group = part % GROUPS, b0 = GATED ? group : W / 32 * group, b1 = GATED ? group + NB / 2 : b0 + 1;
+      constexpr int part = decltype(constant)::value, a = part / SPLIT / GROUPS, group = part / SPLIT % GROUPS, split = part % SPLIT, b0 = GATED ? group : W / 32 * group, b1 = GATED ? group + NB / 2 : b0 + 1;
       const Arguments<T, EPI>& all = *arguments();
       const Product<T>& P = all.p;
       const EPI& epi = all.epi;
       auto put = [&](int b, int half) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < 4; u++)
-          *(__attribute__((address_space(3))) f32x4*)piece(ln & 31, half * 8 + 2 * u + (ln >> 5)) =
-              f32x4{val(a, b, 4 * u), val(a, b, 4 * u + 1), val(a, b, 4 * u + 2), val(a, b, 4 * u + 3)};
+        for (int u = 0; u < 4; u++) {
+          const f32x4 x = f32x4{val(a, b, 4 * u), val(a, b, 4 * u + 1), val(a, b, 4 * u + 2), val(a, b, 4 * u + 3)};
+          if (SPLIT == 1 || (ln & 31) / PR == split) *(__attribute__((address_space(3))) f32x4*)piece(ln & (PR - 1), half * 8 + 2 * u + (ln >> 5)) = x;
+        }
       };
       put(b0, 0);
       if constexpr (W == 64) put(b1, 1);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      const int r0 = here.i0 + (wm * MB + a) * 32, c = ln % LANES * V, col = column(group) - c;
+      const int r0 = here.i0 + (wm * MB + a) * 32 + split * PR, c = ln % LANES * V, col = column(group) - c;
       auto pass = [&](int r, const Extra* given) __attribute__((always_inline)) {
         float v[V], u[V];
         auto get = [&](int first, float (&to)[V]) __attribute__((always_inline)) {
@@ -471,7 +474,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
         for (int i = 0; i < PASSES; i++) pass(ln / LANES + i * (64 / LANES), &extra[part & 1][i]);
       } else {
 #pragma unroll 1
-        for (int r = ln / LANES; r < 32; r += 64 / LANES) pass(r, nullptr);
+        for (int r = ln / LANES; r < PR; r += 64 / LANES) pass(r, nullptr);
       }
       if constexpr (SYM && !SLICED) {
         if (here.i0 != here.j0) {      // column c of these 32 rows is a part of row c across the diagonal
@@ -574,7 +577,7 @@ __global__ __launch_bounds__(256) void join_symmetric_kernel(Product<T> P, EPI e
 
 template <typename T, bool TA, bool TB, int MB, int NB, int R, int CB, bool SLICED, typename EPI>
 void go(const Product<T>& p, const EPI& epi, hipStream_t s) {
-  constexpr int lds = Lds<T, MB, NB, R, CB>::BYTES;
+  constexpr int lds = Lds<T, MB, NB, R, CB, EPI::GATED>::BYTES;
   auto kernel = product_kernel<T, TA, TB, MB, NB, R, CB, SLICED, EPI>;
   static std::atomic<uint64_t> done;      // more than 64 KB of LDS need an opt-in, once per kernel and device
   int dev = 0;
@@ -600,7 +603,7 @@ void go(const Product<T>& p, const EPI& epi, hipStream_t s) {
 struct Plan { int mb, nb, slices; };
 // Bytes of a row in a chunk of the tile
 template <typename T>
-constexpr int chunk_bytes(int mb, bool strided, bool gated) { return sizeof(T) == 2 && ((mb == 4 && !strided) || (mb == 2 && !gated)) ? 128 : 64; }
+constexpr int chunk_bytes(int mb, bool strided) { return sizeof(T) == 2 && (mb == 2 || (mb == 4 && !strided)) ? 128 : 64; }
 // The cheapest by estimate.  A round of tiles takes what its chunks take and some us to begin and end; what the epilogue reads and writes (`bytes` an
 // element of C) goes at 4.5 TB/s, half of it beside the other workgroup's products where a CU holds two; sums of slices are written and read at that rate
 // too.  us of a chunk fitted on products of 2744 to 4096 rows, K of 1024 to 9728, batches of 28: 256 x 256 (one workgroup a CU) 0.87, 192 x 256
@@ -669,7 +672,7 @@ template <typename T, bool TA, bool TB, typename EPI>
 void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
   const int bn = EPI::GATED ? 32 * plan.nb : 64 * plan.nb;
   p.tiles_i = (p.rows + 64 * plan.mb - 1) / (64 * plan.mb), p.tiles_j = (p.cols + bn - 1) / bn, p.slices = plan.slices, p.group = 4;
-  if (probe) return find_overreach(p, TA, TB, 64 * plan.mb, bn, EPI::GATED ? p.b2 : 0, chunk_bytes<T>(plan.mb, TA || TB, EPI::GATED));
+  if (probe) return find_overreach(p, TA, TB, 64 * plan.mb, bn, EPI::GATED ? p.b2 : 0, chunk_bytes<T>(plan.mb, TA || TB));
   auto with = [&](auto mb, auto nb, auto r, auto cb) {
     constexpr int MB = decltype(mb)::value, NB = decltype(nb)::value, R = decltype(r)::value, CB = decltype(cb)::value;
     if (plan.slices > 1) return go<T, TA, TB, MB, NB, R, CB, true>(p, epi, s);
@@ -683,8 +686,7 @@ void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
     if constexpr (!TA && !TB && !EPI::SYMMETRIC) {
       if (plan.mb == 3) return with(RL_I(3), RL_I(4), RL_I(4), RL_I(64));
     }
-    if constexpr (!EPI::GATED) with(RL_I(2), RL_I(2), RL_I(2), RL_I(128));
-    else with(RL_I(2), RL_I(2), RL_I(3), RL_I(64));
+    with(RL_I(2), RL_I(2), RL_I(2), RL_I(128));
   } else {
     if constexpr (!EPI::GATED) {
       if (plan.mb == 1) return with(RL_I(1), RL_I(1), RL_I(4), RL_I(64));
