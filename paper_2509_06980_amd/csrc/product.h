@@ -617,7 +617,7 @@ template <typename T>
 Plan plan_of(const Sizes& z) {
   struct Option { int mb, nb, resident; float chunk_us, gated_us; };      // resident: workgroups that a round has
   constexpr int N = sizeof(T) == 2 ? 3 : 2;
-  static const Option half[] = {{4, 4, 256, 0.87f, 0.87f}, {3, 4, 256, 0.79f, 0.79f}, {2, 2, 512, 0.57f, 0.75f}}, full[] = {{2, 2, 512, 4.8f, 4.8f}, {1, 1, 768, 1.8f, 1.8f}};
+  static const Option half[] = {{4, 4, 256, 0.87f, 0.87f}, {3, 4, 256, 0.79f, 0.79f}, {2, 2, 512, 0.54f, 0.62f}}, full[] = {{2, 2, 512, 4.8f, 4.8f}, {1, 1, 768, 1.8f, 1.8f}};
   const float elements = (float)(z.batches * z.rows * z.cols);
   Plan best{0, 0, 1};
   float best_us = 3e38f;
