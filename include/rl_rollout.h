@@ -427,7 +427,7 @@ int rl_debug_token_logprob_loads(int32_t rows, int32_t kept, int32_t hidden, int
  * the products.  The residual's gradient is dy.  rows = 0: gradients of weights and biases are 0.
  * rows at most 2^26, inner and outer 1 to 2^20 - 8, outer x inner (inner to a multiple of 8) at most 2^30 - 2^20.
  * Workspace 256-byte aligned; aligned = 1: its size for 16-byte aligned x, W and U with row strides in multiples of 16 bytes (at most 2^20
- * elements, W and U alike); 0: for any.  Rows that do not lie so, or are no whole 16 bytes long, are copied into it first.
+ * elements; W and U alike, their last rows within 4 GB - 1 MB); 0: for any.  Rows that do not lie so, or are no whole 16 bytes long, are copied into it first.
  */
 #define RL_ACT_NONE 0
 #define RL_ACT_RELU 1

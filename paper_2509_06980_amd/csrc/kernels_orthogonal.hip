@@ -258,19 +258,26 @@ struct Layout {      // of the workspace
   }
 };
 
-// Whether fp16 holds what arises: the largest singular value after every step, sampled over all that there can be, stays below 32
+// Whether fp16 holds what arises: the largest singular value that each step can leave stays below 32, B below 2^14
 bool fits_half(int steps, const float* coefficients) {
   double most = 1.0;
   for (int t = 0; t < steps; t++) {
-    const double a = coefficients[3 * t], b = coefficients[3 * t + 1], c = coefficients[3 * t + 2];
-    if (!(std::fabs(b) * most * most + std::fabs(c) * most * most * most * most < 16384.0)) return false;      // B
-    double next = 0.0;
-    for (int i = 1; i <= 1024; i++) {
-      const double s = most * i / 1024, s2 = s * s;
-      next = std::max(next, std::fabs(s * (a + s2 * (b + c * s2))));
+    const double a = coefficients[3 * t], b = coefficients[3 * t + 1], c = coefficients[3 * t + 2], m2 = most * most;
+    if (!(std::fabs(b) * m2 + std::fabs(c) * m2 * m2 < 16384.0)) return false;
+    auto size = [&](double s2) { return std::fabs(std::sqrt(s2) * (a + s2 * (b + c * s2))); };
+    double next = size(m2);
+    // where a + 3 b s^2 + 5 c s^4 is 0
+    const double root = 9.0 * b * b - 20.0 * a * c;
+    if (c == 0.0) {
+      if (b != 0.0 && -a / (3.0 * b) > 0.0) next = std::max(next, size(std::min(m2, -a / (3.0 * b))));
+    } else if (root >= 0.0) {
+      for (double sign : {-1.0, 1.0}) {
+        const double s2 = (-3.0 * b + sign * std::sqrt(root)) / (10.0 * c);
+        if (s2 > 0.0) next = std::max(next, size(std::min(m2, s2)));
+      }
     }
     if (!(next < 32.0)) return false;
-    most = next * 1.01;
+    most = next * 1.01;      // roundings
   }
   return true;
 }

@@ -564,8 +564,16 @@ int shares_of(int rows, const RowPlan& p) {
 template <typename S, typename T, int VEC>
 int forward(const ForwardCall<S, T>& f, hipStream_t s) {
   with_forward(forward_plan(f.n.width, VEC), [&](auto l, auto v) {
-    constexpr int L = decltype(l)::value, NV = decltype(v)::value, G = L == 64 ? 4 : 1;
-    residual_norm_forward_kernel<S, T, VEC, L, NV><<<(f.n.rows - 1) / G + 1, L > 256 ? L : 256, 0, s>>>(f);
+    constexpr int L = decltype(l)::value, NV = decltype(v)::value, G = L == 64 ? 4 : 1, THREADS = L > 256 ? L : 256;
+    constexpr int64_t most = most_workgroups(THREADS) * G;      // rows of one launch
+    for (int64_t first = 0; first < f.n.rows; first += most) {
+      ForwardCall<S, T> part = f;
+      part.n.rows = (int)std::min<int64_t>(most, f.n.rows - first);
+      part.h += first * f.n.h, part.y += first * f.n.y, part.out += first * f.n.width, part.stats += first;
+      if (f.a) part.a += first * f.n.width;
+      if (f.gate) part.gate += first * f.n.gate;
+      residual_norm_forward_kernel<S, T, VEC, L, NV><<<(part.n.rows - 1) / G + 1, THREADS, 0, s>>>(part);
+    }
   });
   return launched();
 }

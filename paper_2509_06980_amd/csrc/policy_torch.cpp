@@ -310,7 +310,8 @@ Layer layer_of(const Tensor& x, const Tensor& weight, const Maybe& up, const std
     l.u = operand_of(*up, "up is too large");
   }
   l.outer = l.w.rows;
-  l.aligned = lies_in_16_bytes(l.x) && lies_in_16_bytes(l.w) && (!up || (lies_in_16_bytes(l.u) && l.u.stride == l.w.stride));
+  const bool small_weights = (int64_t)l.outer * l.w.stride * x.element_size() < (1ll << 32) - (1 << 20);
+  l.aligned = small_weights && lies_in_16_bytes(l.x) && lies_in_16_bytes(l.w) && (!up || (lies_in_16_bytes(l.u) && l.u.stride == l.w.stride));
   return l;
 }
 at::DimVector with_last(const Tensor& x, int64_t n) {

@@ -434,6 +434,11 @@ def test_orthogonalize_strides_coefficients_and_odd_values():
     got = ops.orthogonalize(x)
     assert got[1].isnan().all() and not got[3].any() and torch.equal(got[[0, 2]], clean[[0, 2]]) and got[4].isfinite().all()
     assert torch.allclose(got[4].float(), clean[4].float(), atol=1e-2)      # 1e-7 in the norm is all that its size changes
+    y = clean.clone()
+    y[0, 299, 259] = math.inf
+    for t in (y, y.float(), y[:, :70]):      # fp16 products, fp32 ones
+        got = ops.orthogonalize(t)
+        assert got[0].isnan().all() == t[0].isinf().any() and got[2].isfinite().all()
     # coefficients whose values leave fp16: in 32 bits
     wild = ops.orthogonalize(x[0], steps=2, coefficients=(500.0, 0.0, 0.0))
     assert torch.allclose(wild.float(), x[0].float() / x[0].float().norm() * 250000.0, rtol=2.0 ** -7)
@@ -492,6 +497,8 @@ def test_gradients_of_parts():
     frozen.sum().backward()
     assert torch.equal(r.grad, torch.ones_like(r))
     h = randn(g, 9, 16).requires_grad_()
+    new, none = ops.residual_norm(h, x, None, gate=torch.full((16,), 0.5, device="cuda"), residual_scale=2.0)
+    assert none is None and torch.allclose(new, 2 * h + 0.5 * x) and torch.equal(torch.autograd.grad(new.sum(), h)[0], torch.full_like(h, 2.0))
     new, a = ops.residual_norm(h, x, torch.ones(16, device="cuda"))
     one, = torch.autograd.grad(new.sum(), h, retain_graph=True)
     assert torch.equal(one, torch.ones_like(h))
