@@ -198,7 +198,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
   const unsigned sa = chunk_step(TA, P.a.ld, CB), sb = chunk_step(TB, P.b.ld, CB);
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
   // k of the lane's piece of a k-contiguous row
-  const int kpos = (CB == 64 ? (lane & 3) ^ (lane >> 4 & 3) : (lane & 7) ^ (lane >> 3 & 7)) * (16 / EL);
+  const int kpos = (CB == 64 ? (lane & 3) ^ (lane >> 4 & 3) : (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4 & 3))) * (16 / EL);
   int va[PA], vb[PB];      // this lane's offset of each piece that its wave loads
   auto offset = [&](int kb, int64_t ld, bool strided, int row_bytes) {      // kb: the KB of the operand
     if (strided) {
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
       return (lane >> 5) * 4 * row_bytes + (((2 * x) ^ (lane >> 5 << 1)) << 6) + ((lane & 31) << 2);
     }
   };
-  auto part2 = [&](int x) { return (lane & 31) * CB + (((x * 2 + (lane >> 5)) ^ (CB == 64 ? lane >> 2 & 3 : lane & 7)) << 4); };
+  auto part2 = [&](int x) { return (lane & 31) * CB + (((x * 2 + (lane >> 5)) ^ (CB == 64 ? lane >> 2 & 3 : lane >> 1 & 7)) << 4); };
 #pragma unroll
   for (int x = 0; x < (TA ? MB : NS); x++) la[x] = TA ? part(wm * MB + x, BM * EL) : part2(x);
 #pragma unroll

@@ -330,6 +330,16 @@ def test_residual_norm_without_rows_and_of_odd_values():
     assert dh[[0, 1, 3, 5]].isfinite().all() and dy[[0, 1, 3, 5]].isfinite().all() and dh[2].isnan().all()
 
 
+def test_residual_norm_of_more_rows_than_a_launch_takes():
+    rows, width = 1 << 24, 385      # a workgroup of 256 a row: 2^32 threads; a launch counts them in 32 bits
+    x = torch.empty(rows, width, dtype=BF, device="cuda").normal_(generator=gen(41))
+    w = randn(gen(42), width, dt=BF)
+    h, a, stats = ops.residual_norm_forward(x, x, w, gate=w)
+    for at in (0, (1 << 23) - 3, rows - 8):
+        part = ops.residual_norm_forward(x[at:at + 8], x[at:at + 8], w, gate=w)
+        assert all(torch.equal(t[at:at + 8], p) for t, p in zip((h, a, stats), part)), at
+
+
 # ---- orthogonalised updates ------------------------------------------------------------------------------------------
 NEWTON = (3.4445, -4.7750, 2.0315)
 
