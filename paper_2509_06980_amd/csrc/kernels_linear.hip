@@ -10,16 +10,16 @@ using namespace product;
 // Backward: dz = dy act'(z) [u], du = dy act(z);  dx = dz W [+ du U], dW = dz^T x, db = sum over rows of dz, dr = dy.
 // z and u are kept in 32 bits for the backward call: rounded to bf16 they alone would make the gradients of a gated layer 0.0029 off (relative; the
 // roundings of dz and of the gradient itself 0.0024).  dz and du are rounded to the weights' type once, as the operands that they become.
+// Many rows are bound by the matrix units: 4096 rows, 9728 -> 2560 with a residual, forward and backward 612 us (1.00 PFLOP/s): 243 forward, 11 for dz, 231
+// for dx, 218 for dW.  2744 rows, 2560 -> 9728 twice, gated by silu: 887 us (0.93 PFLOP/s): 353 to 395, 71, 237 to 271 and 13 to join slices, 225 to 248.
+// Few by the weights' bytes.
 // =============================================================================================
-struct Sums {      // act(z) and act'(z)
+struct Activated {      // act(z) and act'(z)
   float value, slope;
 };
 __device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + __expf(-z)); }
-__device__ __forceinline__ float tanh_of(float z) {      // 1 - 2 / (1 + e^(2 z)); e^(2 z) = infinity: 1
-  return 1.f - 2.f / (1.f + __expf(2.f * z));
-}
 template <bool SLOPE>
-__device__ __forceinline__ Sums activate(float z, int act) {
+__device__ __forceinline__ Activated activate(float z, int act) {
   switch (act) {
     case RL_ACT_RELU: return {z > 0.f || z != z ? z : 0.f, z > 0.f ? 1.f : 0.f};
     case RL_ACT_SILU: {
@@ -44,7 +44,7 @@ __device__ __forceinline__ void activate_all(const float (&z)[N], int act, float
   auto all = [&](auto a) {
 #pragma unroll
     for (int e = 0; e < N; e++) {
-      const Sums s = activate<SLOPE>(z[e], decltype(a)::value);
+      const Activated s = activate<SLOPE>(z[e], decltype(a)::value);
       value[e] = s.value;
       if (SLOPE) slope[e] = s.slope;
     }
@@ -126,8 +126,8 @@ struct Finish {
 // Up to 16 rows: bound by the weights' bytes.  A workgroup takes 16 rows of W (and of U) and all rows of x; its waves share k, operands go from memory straight
 // into registers (weights as the row operand of 16x16x32 instructions, fp32 16x16x4; a lane's 16 bytes are 8 or 4 k of one row), and the waves'
 // sums are added in LDS in a fixed order.  x comes from the caches.  What a block of 16 rows has too many reads the last row again and is not stored.
-// One row x 4096 x 2560 with a residual: 7.3 us, by the tiles of many rows 14.  From 17 rows on those tiles are faster (37 rows x 2560 x 9728, gated, weights from
-// memory: 33 + 5 us for the slices' sums, this way with three blocks of rows 50).
+// One row x 4096 x 2560 with a residual: 6.9 us (3.0 TB/s, of it 2 us to begin and end), by the tiles of many rows 14.  From 17 rows on those tiles are faster (37 rows x 2560 x 9728, gated: 29 us with
+// the slices' sums; this way, three blocks of rows a workgroup, 50).
 const int kFewRows = 16, kFewWaves = 8;
 template <typename T, typename EPI>
 __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(const T* __restrict__ x, int64_t x_ld, const T* __restrict__ w, int64_t w_ld, int64_t second,
@@ -220,7 +220,8 @@ __global__ __launch_bounds__(256) void copy_rows_kernel(Copies<T> copies) {
 }
 
 // ---- dz and du, and their sums over rows --------------------------------------------------------------------------------------
-// A thread takes 8 columns of every fourth row of a workgroup's share of rows.  Bound by memory.
+// A thread takes 8 columns of every fourth row of a workgroup's share of rows.  Bound by memory: 2744 x 9728 of a gated layer reads dy, z and u and writes dz and
+// du, 374 MB, in 71 us (5.3 TB/s, z and u partly still in the last cache).
 const int kGradColumns = 512, kGradShares = 256;
 template <typename T>
 struct Gradient {

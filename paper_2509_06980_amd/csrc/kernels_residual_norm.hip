@@ -15,6 +15,8 @@ namespace {
 // Bound by memory: h and y in, h' and a out; backward dh', da, h' and y in, dh and dy out.  A row is held in registers by L threads, NV pieces of VEC
 // elements each, so everything is read once; NV = 0 takes rows too long for that in several passes.  The stream may be in 32 bits beside a block
 // in bf16 (S, T).  Everything is computed in 32 bits and rounded once; a is the norm of h' before its rounding.
+// 7777 x 2560, stream in 32 bits, block in bf16: forward 239 MB in 56 us (4.3 TB/s), backward 319 MB in 57 us (5.6 TB/s, h' partly still in the last cache)
+// and 4.7 us for the sums of the shares; 128 rows forward 6.2 us, of which a launch alone is most.
 // =============================================================================================
 struct Shape {
   int rows, width;
@@ -512,7 +514,8 @@ __global__ __launch_bounds__(1024) void reduce_kernel(const float* __restrict__ 
   if (x == 0 && blockIdx.x * 32 + k < width) st1(to + blockIdx.x * 32 + k, s);
 }
 
-// Threads that hold a row, and pieces of it a thread holds (0: the row is read again instead).
+// Threads that hold a row, and pieces of it a thread holds (0: the row is read again instead): one wave as long as its registers hold the row, for its sums need no
+// barrier.  The backward pass keeps up to four sums a column beside it and goes to more threads earlier.
 struct RowPlan { int L, NV; };
 RowPlan forward_plan(int width, int vec) {
   const int n = (width + vec - 1) / vec;
@@ -554,7 +557,8 @@ void with_backward(const RowPlan& p, F f) {
   is(RL_I(1024), RL_I(4)); is(RL_I(256), RL_I(0));
 }
 #undef RL_I
-// Workgroups of the backward pass, each with a share of the sums
+// Workgroups of the backward pass, each with a share of the sums: three a CU.  4001 x 1024 with a norm behind the block and a gate takes 18 us; 25 with 256
+// of them, 22 with 1024, whose shares take longer to add.
 const int kShares = 768;
 int shares_of(int rows, const RowPlan& p) {
   const int group = p.L == 64 ? 4 : 1, n = (rows - 1) / group + 1;

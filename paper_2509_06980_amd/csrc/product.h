@@ -11,11 +11,11 @@
 // =============================================================================================
 // C[i, j] = sum over k of A[i, k] B[j, k] over tiles of 64 MB rows i and 64 NB columns j: four waves of 32 MB x 32 NB on 32x32x16 (fp32:
 // 32x32x2) matrix instructions, sums in 32 bits.
-// Operands as they lie in memory: k-contiguous ([row][k]) or k-strided (TA, TB: [k][column]).  A chunk of 64 or 128 bytes of k (32 or 64 elements; fp32 16) of both
-// goes straight from memory into one of R stages in LDS, R - 1 ahead; operands are read half a chunk ahead of the instructions that use them, one
-// barrier a chunk.  A workgroup stays for all its tiles and its loads run on into the next one.
-//   k-contiguous: 64 bytes a row.  The 16-byte piece p of row r is kept at p ^ (r / 4 % 4), so the 16 rows that a read takes in one go lie in
-//     different banks.
+// Operands as they lie in memory: k-contiguous ([row][k]) or k-strided (TA, TB: [k][column]).  A chunk of CB = 64 or 128 bytes of k of both goes
+// straight from memory into one of R stages in LDS, R - 1 ahead; operands are read 32 bytes of k ahead of the instructions that use them, one barrier a
+// chunk.  A workgroup stays for all its tiles and its loads run on into the next one.
+//   k-contiguous: rows of CB bytes.  The 16-byte piece p of row r is kept at p ^ (r / 4 % 4), of 128 bytes at p ^ (r / 2 % 8), so the 16 rows that a read
+//     takes in one go lie in different banks.
 //   k-strided, 16-bit types: read with the transposing LDS read, 16 lanes take 4 k x 16 columns, lane i gets column i of the 4 k.  The 64-byte
 //     block b of row k is kept at b ^ (k % 4).  fp32: read one by one; block b of row k is kept at b ^ 2 (k / 4 % 2).
 // fp32 instructions take 2 k, of a lane's 16 bytes element e in step e: k = e and 4 + e of the eight, the same for both operands.
@@ -24,7 +24,15 @@
 // Nothing is read behind an operand's last row and column, and what a tile has too many (rows, columns, k) enters as zeros: a value that is
 // no number reaches its own row and column of C only.
 // Epilogue: 32 rows x 64 columns of a wave at a time through LDS of its own, so that rows are read and written in pieces of 8 columns (fp32: 4);
-// the 16-byte piece p of row r is kept at p ^ (r % 16).
+// the 16-byte piece p of row r is kept at p ^ (r % 16) (32 columns: r % 8).
+//
+// Tiles and stages, 16-bit types: 256 x 256, one workgroup a CU, with two stages of 128 bytes where both operands are k-contiguous and four of 64 where one is
+// strided (two of 128 there: 0 to 10 % slower); 192 x 256 where that leaves fewer CUs without a tile (4096 x 2560 from k 9728: 252 us by 160 of 256
+// CUs' tiles of 256 x 256, 220 tiles of 192 x 256 take 243); 128 x 128, two workgroups a CU, with two stages of 128 bytes: its CU asks the caches for twice as
+// much, and in requests of 64 bytes it gets 25 bytes a clock however many are under way (2560 x 9728 orthogonalised 1564 us with 64, 1390 with 128).
+// What bounds the large ones is the power that the matrix units draw: 8192 x 8192 x 8192 in bf16 takes 835 us (1.32 PFLOP/s; operands strided as in the
+// backward pass 819 to 826), of zeros 569.  4096 rows x 2560 -> 9728 takes 222 us (0.92 PFLOP/s): 608 tiles in 2.4 rounds.  Matrix units are busy 44 % of a
+// launch's clocks, LDS reads wait for no bank.
 // =============================================================================================
 namespace product {
 
@@ -607,7 +615,7 @@ constexpr int chunk_bytes(int mb, bool strided) { return sizeof(T) == 4 ? mb == 
 // The cheapest by estimate.  A round of tiles takes what its chunks take and some us to begin and end; what the epilogue reads and writes (`bytes` an
 // element of C) goes at 4.5 TB/s, half of it beside the other workgroup's products where a CU holds two; sums of slices are written and read at that rate
 // too.  us of a chunk fitted on products of 2744 to 4096 rows, K of 1024 to 9728, batches of 28: 256 x 256 (one workgroup a CU) 0.87, 192 x 256
-// 0.79, 128 x 128 (two a CU) 0.57, gated 0.75; estimates within 15 % of what was measured, their order right in 13 of 14 pairs.
+// 0.79, 128 x 128 (two a CU) 0.54, gated 0.62; estimates within 15 % of what was measured, their order right in 13 of 14 pairs.
 struct Sizes {
   int64_t rows, cols, batches, n_chunks;
   bool symmetric, gated, strided;      // strided: one of the operands
