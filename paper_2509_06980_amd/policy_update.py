@@ -198,6 +198,14 @@ class Muon(torch.optim.Optimizer):
                     self._adam(p, group)
         return loss
 
+    def load_state_dict(self, state_dict):
+        super().load_state_dict(state_dict)      # which rounds states to their parameter's type
+        ids, params = ([p for group in groups for p in group["params"]] for groups in (state_dict["param_groups"], self.param_groups))
+        for i, p in zip(ids, params):
+            for name, value in state_dict["state"].get(i, {}).items():
+                if torch.is_tensor(value):
+                    self.state[p][name] = value.to(p.device, torch.float32, copy=True)
+
     def _momentum(self, p, group):
         state, g = self.state[p], p.grad.float()
         if "momentum" not in state:

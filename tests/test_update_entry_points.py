@@ -132,3 +132,23 @@ def test_loads_of_the_products_stay_inside_their_operands(lib):
         rl.debug_linear_loads(0, 8, 8, 8, 8, 8, False, False, False)
     with pytest.raises(rl.RolloutError):
         rl.debug_orthogonalize_loads(0, 8, 8, False)
+
+
+def test_states_of_muon_stay_in_32_bits_when_they_are_loaded():
+    torch = pytest.importorskip("torch")
+    from paper_2509_06980_amd.policy_update import Muon
+    def stepped():
+        p, q = (torch.ones(5, dtype=torch.bfloat16, requires_grad=True) for _ in range(2))
+        return [p, q], Muon([dict(params=[p]), dict(params=[q])])
+    params, muon = stepped()
+    for k in range(3):
+        for p in params[:1]:                      # the other one has no gradient and no state
+            p.grad = torch.linspace(0.1, 0.7 + k, 5).bfloat16()
+        muon.step()
+    saved = muon.state_dict()
+    again, other = stepped()
+    other.load_state_dict(saved)
+    state, loaded = muon.state[params[0]], other.state[again[0]]
+    assert loaded["step"] == 3 and not other.state.get(again[1])
+    for name in ("first", "second"):
+        assert loaded[name].dtype == torch.float32 and torch.equal(loaded[name], state[name]) and loaded[name].data_ptr() != state[name].data_ptr()
