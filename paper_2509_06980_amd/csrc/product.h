@@ -611,7 +611,7 @@ void go(const Product<T>& p, const EPI& epi, hipStream_t s) {
 struct Plan { int mb, nb, slices; };
 // Bytes of a row in a chunk of the tile
 template <typename T>
-constexpr int chunk_bytes(int mb, bool strided) { return sizeof(T) == 4 ? mb == 1 ? 128 : 64 : mb == 2 || (mb == 4 && !strided) ? 128 : 64; }
+constexpr int chunk_bytes(int mb, bool strided) { return sizeof(T) == 4 || mb == 2 || (mb == 4 && !strided) ? 128 : 64; }
 // The cheapest by estimate.  A round of tiles takes what its chunks take and some us to begin and end; what the epilogue reads and writes (`bytes` an
 // element of C) goes at 4.5 TB/s, half of it beside the other workgroup's products where a CU holds two; sums of slices are written and read at that rate
 // too.  us of a chunk fitted on products of 2744 to 4096 rows, K of 1024 to 9728, batches of 28: 256 x 256 (one workgroup a CU) 0.87, 192 x 256
@@ -699,7 +699,7 @@ void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
     if constexpr (!EPI::GATED) {
       if (plan.mb == 1) return with(RL_I(1), RL_I(1), RL_I(2), RL_I(128));
     }
-    with(RL_I(2), RL_I(2), RL_I(3), RL_I(64));
+    with(RL_I(2), RL_I(2), RL_I(2), RL_I(128));
   }
 #undef RL_I
 }
