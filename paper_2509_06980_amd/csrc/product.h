@@ -27,9 +27,10 @@
 // the 16-byte piece p of row r is kept at p ^ (r % 16) (32 columns: r % 8).
 //
 // Tiles and stages, 16-bit types: 256 x 256, one workgroup a CU, with two stages of 128 bytes where both operands are k-contiguous and four of 64 where one is
-// strided (two of 128 there: 0 to 10 % slower); 192 x 256 where that leaves fewer CUs without a tile (4096 x 2560 from k 9728: 252 us by 160 of 256
-// CUs' tiles of 256 x 256, 220 tiles of 192 x 256 take 243); 128 x 128, two workgroups a CU, with two stages of 128 bytes: its CU asks the caches for twice as
-// much, and in requests of 64 bytes it gets 25 bytes a clock however many are under way (2560 x 9728 orthogonalised 1564 us with 64, 1390 with 128).
+// strided (two of 128 there: 0 to 10 % slower); 192 x 256 where that leaves fewer CUs without a tile (4096 x 2560 from k 9728: 220 tiles in 243 us; 160 of
+// 256 x 256 by the estimate below 270); 128 x 128, two workgroups a CU, with two stages of 128 bytes (where there are no more tiles than CUs four): a CU asks
+// the caches for twice as much there, and in requests of 64 bytes it gets 25 bytes a clock however many are under way (2560 x 9728 orthogonalised 1564 us
+// with 64, 1420 with 128).  fp32: 128 x 128 and 64 x 64, two stages of 128 bytes (1024 x 1024 orthogonalised 373 us, 391 with 64).
 // What bounds the large ones is the power that the matrix units draw: 8192 x 8192 x 8192 in bf16 takes 835 us (1.32 PFLOP/s; operands strided as in the
 // backward pass 819 to 826), of zeros 569.  4096 rows x 2560 -> 9728 takes 222 us (0.92 PFLOP/s): 608 tiles in 2.4 rounds.  Matrix units are busy 44 % of a
 // launch's clocks, LDS reads wait for no bank.
@@ -694,6 +695,9 @@ void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
     if constexpr (!TA && !TB && !EPI::SYMMETRIC) {
       if (plan.mb == 3) return with(RL_I(3), RL_I(4), RL_I(4), RL_I(64));
     }
+    // one workgroup a CU or fewer: nothing else covers the latency of its loads (512 x 512 orthogonalised 218 us with two stages, 209 with four; 1024 x 4096
+    // 336 and 320, 2560 x 9728 1398 and 1374)
+    if ((int64_t)(EPI::SYMMETRIC ? p.tiles_i * (p.tiles_i + 1) / 2 : p.tiles_i * p.tiles_j) * p.slices * p.batches <= 256) return with(RL_I(2), RL_I(2), RL_I(4), RL_I(128));
     with(RL_I(2), RL_I(2), RL_I(2), RL_I(128));
   } else {
     if constexpr (!EPI::GATED) {
