@@ -27,13 +27,13 @@
 // the 16-byte piece p of row r is kept at p ^ (r % 16) (32 columns: r % 8).
 //
 // Tiles and stages, 16-bit types: 256 x 256, one workgroup a CU, with two stages of 128 bytes where both operands are k-contiguous and four of 64 where one is
-// strided (two of 128 there: 0 to 10 % slower); 192 x 256 where that leaves fewer CUs without a tile (4096 x 2560 from k 9728: 220 tiles in 243 us; 160 of
+// strided (two of 128 there: 0 to 10 % slower); 192 x 256 where that leaves fewer CUs without a tile (4096 x 2560 from k 9728: 220 tiles in 236 us; 160 of
 // 256 x 256 by the estimate below 270); 128 x 128, two workgroups a CU, with two stages of 128 bytes (where there are no more tiles than CUs four): a CU asks
 // the caches for twice as much there, and in requests of 64 bytes it gets 25 bytes a clock however many are under way (2560 x 9728 orthogonalised 1564 us
 // with 64, 1420 with 128).  fp32: 128 x 128 and 64 x 64, two stages of 128 bytes (1024 x 1024 orthogonalised 373 us, 391 with 64).
 // What bounds the large ones is the power that the matrix units draw: 8192 x 8192 x 8192 in bf16 takes 835 us (1.32 PFLOP/s; operands strided as in the
-// backward pass 819 to 826), of zeros 569.  4096 rows x 2560 -> 9728 takes 222 us (0.92 PFLOP/s): 608 tiles in 2.4 rounds.  Matrix units are busy 44 % of a
-// launch's clocks, LDS reads wait for no bank.
+// backward pass 819 to 826), of zeros 569.  4096 rows x 2560 -> 9728 takes 222 us (0.92 PFLOP/s): 608 tiles in 2.4 rounds.  Matrix units are busy 39 to
+// 67 % of a launch's clocks, LDS reads wait for a bank in 0 to 5 % of theirs.
 // =============================================================================================
 namespace product {
 
