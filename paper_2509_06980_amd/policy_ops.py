@@ -138,12 +138,14 @@ def residual_norm_backward(dh_new, da, h_new, y, stats, weight, post_weight=None
 def orthogonalize(x, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7):
     """Every matrix of x [.., rows, columns] with its singular values driven towards 1 -> a new tensor: x / (|x| + eps), then `steps` times
     X <- a X + b (X X^T) X + c (X X^T)^2 X; see rl_orthogonalize.  coefficients: (a, b, c), or one such triple a step."""
+    table = []
     try:
-        triples = [coefficients] * steps if not hasattr(coefficients[0], "__len__") else coefficients
-        table = [(float(a), float(b), float(c)) for a, b, c in triples]
-    except (TypeError, ValueError):
-        table = []
-    if len(table) != steps:
+        if steps in range(1, 65):
+            triples = [coefficients] * steps if not hasattr(coefficients[0], "__len__") else coefficients
+            table = [(float(a), float(b), float(c)) for a, b, c in triples]
+    except (TypeError, ValueError, LookupError):
+        pass
+    if not table or len(table) != steps:
         _refuse("1 to 64 steps; coefficients are three numbers, or three numbers for each step")
     table = [v for triple in table for v in triple]
     return _native.orthogonalize(x, table, eps, _stream(x))

@@ -152,3 +152,13 @@ def test_states_of_muon_stay_in_32_bits_when_they_are_loaded():
     assert loaded["step"] == 3 and not other.state.get(again[1])
     for name in ("first", "second"):
         assert loaded[name].dtype == torch.float32 and torch.equal(loaded[name], state[name]) and loaded[name].data_ptr() != state[name].data_ptr()
+
+
+@pytest.mark.parametrize("changes", [dict(coefficients=()), dict(coefficients=None), dict(coefficients={"a": 1.0}), dict(coefficients=(1.0, "b", 2.0)),
+                                     dict(coefficients=[(1.0, 2.0, 3.0), (1.0,)], steps=2), dict(steps=0), dict(steps=10 ** 12), dict(steps=2.5)])
+def test_steps_and_coefficients_that_are_none_are_refused(lib, changes):
+    torch = pytest.importorskip("torch")
+    from paper_2509_06980_amd import policy_ops as ops
+    with pytest.raises(rl.RolloutError, match="coefficients") as e:
+        ops.orthogonalize(torch.ones(4, 8), **changes)
+    assert e.value.code == -1
