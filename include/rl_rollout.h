@@ -473,8 +473,10 @@ int rl_residual_norm_backward(const void* d_dout, int64_t dout_stride, const voi
  * X <- a X + b (X X^T) X + c (X X^T)^2 X with (a, b, c) = coefficients[3 step ..] (a HOST pointer, read during the call): a singular value s
  * becomes a s + b s^3 + c s^5.  d_out: contiguous, of G's type; it may be a contiguous G itself.  A matrix of zeros gives zeros (eps > 0);
  * values that are no number or infinite make that matrix no numbers, never another one.
- * float32: sums and operands in 32 bits.  bf16: from a smaller side of 256 on the operands of the products are rounded to fp16, X itself and all sums
- * stay in 32 bits (coefficients that let singular values or intermediate values grow beyond fp16's range take float32).
+ * float32: sums and operands in 32 bits.  bf16: from a smaller side of 256 on the operands of the products are rounded to fp16 (11 bits), scaled by powers of two so that
+ * neither |G| beside eps nor the steps take them out of its range; X is kept with 22 bits between the steps, with 11 in the last; sums in 32 bits.  Results are then
+ * 0.0017 to 0.0025 off in five steps (relative, by their norm; their last rounding alone 0.0017).  Coefficients whose factor a + b s^2 + c s^4 may come near 0 or change its
+ * sign take float32.
  * steps 1 to 64, count at most 65535, sides at most 2^20 - 8, a matrix (sides + 8) at most 2^30 - 2^20 elements.  Workspace 256-byte aligned.
  */
 int64_t rl_orthogonalize_workspace(int32_t count, int32_t rows, int32_t columns, int32_t dtype);

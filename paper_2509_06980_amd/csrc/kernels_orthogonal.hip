@@ -12,19 +12,31 @@ using namespace product;
 // again; the singular vectors stay.
 // A and B are symmetric: tiles on and under the diagonal are computed, the others are stored from them.
 // Bound by the matrix units: 2560 x 9728 in five steps 1.36 ms (0.77 PFLOP/s of the products as computed, half of the symmetric ones), 28 x 2048 x 1024
-// 1.82 ms; small stacks by the ten products' and joins' length one after another (3 x 512 x 256 168 us).  fp32: everything in 32 bits.  bf16: the operands of the products are rounded to fp16
-// (11 bits instead of the 8 of bf16, at the same rate), X times a power of two so that its elements lie in the middle of that range.  What the rounding of X
-// leaves is kept beside it in fp16 where more than one step follows, since a X carries the small singular values, which the steps enlarge (500 times in five of
-// them) with whatever roundings are in them; the first X is exact as it is.  B's diagonal, near b + c towards the end, is kept in 32 bits.  Relative error of the
-// result against 64 bits, of which its last rounding alone is 0.0017: 0.0017 to 0.0021 (fp16 alone: 0.02 for a matrix of 32 strong directions over a floor of
-// noise; operands in bf16: 0.2).  Matrices with a side below 256 take the fp32 products, where these cost nothing: fp16's error is largest there.
+// 1.82 ms; small stacks by the ten products' and joins' length one after another (3 x 512 x 256 168 us).
+// fp32: everything in 32 bits.  bf16: the operands of the products are rounded to fp16 (11 bits instead of the 8 of bf16, at the same rate), X and A times powers of two
+// that keep their elements in the middle of that range (Schedule).  What the rounding of X leaves is kept beside it in fp16 where more than one step follows, since a X
+// carries the small singular values, which the steps enlarge (400 times in five of them) with whatever roundings are in them; the first X is exact as it is.  B's diagonal, near
+// b + c towards the end, is kept in 32 bits.  Relative error of the result against 64 bits, of which its last rounding alone is 0.0017: 0.0017 to 0.0021 in five steps, to 0.0025 where
+// a few elements or rows hold nearly all of |G| (fp16 alone: 0.02 for a matrix of 32 strong directions over a floor of noise; operands in bf16: 0.2).  Steps
+// whose roundings would show more (schedule_of) and matrices with a side below 256 take the fp32 products, which cost nothing there: fp16's error is largest in small ones.
 // =============================================================================================
+const int kMostSteps = 64;
 const int kNormShares = 1024;
 const int kHalfFrom = 256;
 // X goes past the caches where it would not stay in the last one of 256 MB with what else a step reads: 28 x 2048 x 1024 (117 MB) 2.3 % faster,
 // 2560 x 9728 (50 MB) 6 % slower, which keeps the caches.
 const int64_t kStream = 80 << 20;
 const float kLow = 2048.f;      // the low half of an element is kept times this
+// fp16: X_t is kept times 2^(kTop - e_t), where none of its singular values is above 2^e_t: elements stay below 2^kTop (four times that fits) and as far above
+// fp16's smallest as they can, however small |G| is beside eps and whatever the steps do to X.  A is that of X_t 2^-e_t, its size goes into the next two
+// coefficients, and all three are kept times 2^-g_t.
+const int kTop = 14;
+struct Schedule {
+  int steps;
+  // singular values of X_t are at most 2^bound[t]; and at most 2^growth[t] times those of X_0, which may be any below 1 where eps outweighs |G|
+  int16_t bound[kMostSteps + 1], growth[kMostSteps + 1], g[kMostSteps];
+  float a[kMostSteps], b[kMostSteps], c[kMostSteps];      // times 2^-g
+};
 
 // Elements of a matrix in pieces of V, by all threads of a grid's first dimension: f(piece's row, its first column)
 template <int V, typename F>
@@ -58,21 +70,31 @@ __global__ __launch_bounds__(256) void squares_kernel(const T* __restrict__ x, i
   s = block_sum(s, join);
   if (threadIdx.x == 0) part[blockIdx.y * gridDim.x + blockIdx.x] = s;
 }
-// The products' first operand, rows of ld with zeros behind the last column: X in 32 bits, or in fp16 G times a power of two that makes it about `scale`
-// X (exact for bf16, but for what is far below the average element), and what takes that to X as factor[matrix].
+// The products' first operand, rows of ld with zeros behind the last column: X in 32 bits; or in fp16 G times the power of two that brings |G| to 2^(kTop - 1) or above,
+// exact for bf16 but for elements below 2^-30 |G|.  With it what a matrix's steps take, scales[matrix][step]: b and c for A as it is kept, and what takes a step's
+// sums to the next X as it is kept, or the last one's to X: in two factors, where X is only just in a float's range and one of them would not be.
 template <typename T, typename X>
 __global__ __launch_bounds__(256) void normalise_kernel(const T* __restrict__ x, int64_t matrix, int64_t stride, int rows, int columns, int ld, int vec,
-                                                        const double* __restrict__ part, int shares, double eps, double scale, X* __restrict__ to,
-                                                        float* __restrict__ factor) {
+                                                        const double* __restrict__ part, int shares, double eps, Schedule schedule, X* __restrict__ to,
+                                                        float4* __restrict__ scales) {
   constexpr bool HALF = sizeof(X) == 2;
   __shared__ double join[4];
   double s = 0.0;
   for (int i = threadIdx.x; i < shares; i += 256) s += part[blockIdx.y * shares + i];
-  const double norm = sqrt(block_sum(s, join)) + eps, inverse = 1.0 / norm;
+  const double size = sqrt(block_sum(s, join)), norm = size + eps, inverse = 1.0 / norm;
   int power = 0;
   if constexpr (HALF) {
-    power = ilogb(scale * inverse);      // of infinities and no numbers: any, the factor is no number then
-    if (blockIdx.x == 0 && threadIdx.x == 0) factor[blockIdx.y] = (float)ldexp(inverse, -power);
+    const bool some = size > 0.0 && size < 1e300;
+    if (some) power = kTop - 1 - ilogb(size);
+    const int t = threadIdx.x;
+    if (blockIdx.x == 0 && t < schedule.steps) {
+      const int first = some ? ilogb(size * inverse) + 1 : 0;      // no singular value of X_0 is above 2^first
+      auto e = [&](int t) { return min((int)schedule.bound[t], first + schedule.growth[t]); };
+      const double unit = t > 0 ? ldexp(1.0, e(t)) : some ? ldexp(inverse, kTop - power) : 0.0, square = unit * unit;
+      const int to_next = schedule.g[t] - kTop + (t + 1 == schedule.steps ? 0 : kTop - e(t + 1)), down = to_next + ilogb(unit) < -60 ? 64 : 0;
+      const float nan = size < 1e300 && norm > 0.0 ? 0.f : __builtin_nanf("");      // X_0 is no number: neither is all that follows
+      scales[blockIdx.y * kMostSteps + t] = make_float4((float)(schedule.b[t] * square) + nan, (float)(schedule.c[t] * square * square) + nan, (float)ldexp(unit, to_next + down) + nan, (float)ldexp(1.0, -down));
+    }
   }
   const T* p = x + blockIdx.y * matrix;
   X* const out = to + (int64_t)blockIdx.y * rows * ld;
@@ -86,7 +108,7 @@ __global__ __launch_bounds__(256) void normalise_kernel(const T* __restrict__ x,
   });
 }
 
-// A = alpha^2 (sums), or that of its matrix; rows of ld, zeros behind the last column
+// A = the sums (fp16: of X as it is kept, times 2^-2 kTop); rows of ld, zeros behind the last column
 template <typename T>
 struct Gram {
   static constexpr bool GATED = false, SYMMETRIC = true;
@@ -94,8 +116,6 @@ struct Gram {
   T* out;
   int64_t matrix;
   int ld, n;
-  float alpha;
-  const float* factor;
   struct Extra {};
   static constexpr bool UNROLL = false;
   __device__ __forceinline__ void fetch(int, int, int, Extra&) const {}
@@ -106,14 +126,14 @@ struct Gram {
     store_row<T, V>(out + batch * matrix + (int64_t)row * ld + col, true, V, v);
   }
   __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V], const Extra&) const {
-    float f = alpha;
-    if (factor) f = factor[batch];
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int e = 0; e < V; e++) v[e] *= f * f;
+      for (int e = 0; e < V; e++) v[e] *= 1.f / (1 << (2 * kTop));
+    }
     across(batch, row, col, v);
   }
 };
-// B = b A + c A^2; 16 bits: its diagonal apart
+// B = b A + c A^2; fp16: its diagonal apart
 template <typename T>
 struct Polynomial {
   static constexpr bool GATED = false, SYMMETRIC = true;
@@ -124,6 +144,7 @@ struct Polynomial {
   int64_t matrix;
   int ld, n;
   float b, c;
+  const float4* scales;      // fp16: of a step, in place of b and c
   struct Extra { float a[V]; };
   static constexpr bool UNROLL = false;
   __device__ __forceinline__ void fetch(int batch, int row, int col, Extra& x) const { load_row<T, V>(a + batch * matrix + (int64_t)row * ld + col, true, V, x.a); }
@@ -134,9 +155,11 @@ struct Polynomial {
     store_row<T, V>(out + batch * matrix + (int64_t)row * ld + col, true, V, v);
   }
   __device__ __forceinline__ void operator()(int batch, int row, int col, float (&v)[V], float (&)[V], const Extra& x) const {
+    float first = b, second = c;
+    if constexpr (sizeof(T) == 2) first = scales[batch * kMostSteps].x, second = scales[batch * kMostSteps].y;
 #pragma unroll
     for (int e = 0; e < V; e++) {
-      v[e] = b * x.a[e] + c * v[e];
+      v[e] = first * x.a[e] + second * v[e];
       if (sizeof(T) == 2 && col + e == row) {
         diagonal[batch * padded(n) + row] = v[e];
         v[e] = 0.f;
@@ -150,15 +173,16 @@ template <typename T>
 struct Step {
   static constexpr bool GATED = false, SYMMETRIC = false;
   static constexpr int V = kPiece<T>;
-  const T* x;              // the products' operand; 16 bits: X times `scale` (the first step's: X / factor), rounded,
+  const T* x;              // the products' operand; fp16: X as it is kept, rounded,
   const _Float16* low;     // and what the rounding left, unless null
   T* next;
   _Float16* next_low;
   void* out;               // the last step's results, else null
-  const float *diagonal, *factor;
+  const float* diagonal;
+  const float4* scales;    // fp16: of a step
   int64_t matrix;
   int rows, cols, ld, by_column, bf16_out, vec, stream;
-  float a, scale;
+  float a;
   struct Extra { u32x4 x, low; };      // as they lie in memory
   static constexpr bool UNROLL = true;
   __device__ __forceinline__ void fetch(int batch, int row, int col, Extra& e) const {
@@ -189,20 +213,15 @@ struct Step {
 #pragma unroll
         for (int e = 0; e < V; e++) d[e] = one;
       }
-      float f = 1.f;      // to X times `scale`
-      if (factor) f = factor[batch] * scale;
+      const float4 f = scales[batch * kMostSteps];
 #pragma unroll
-      for (int e = 0; e < V; e++) v[e] = fmaf(a, fmaf(l[e], 1.f / kLow, h[e]), fmaf(d[e], h[e], v[e])) * f;
+      for (int e = 0; e < V; e++) v[e] = fmaf(a, fmaf(l[e], 1.f / kLow, h[e]), fmaf(d[e], h[e], v[e])) * f.w * f.z;
     } else {
 #pragma unroll
       for (int e = 0; e < V; e++) v[e] = fmaf(a, h[e], v[e]);
     }
     if (out) {
       const int64_t to = ((int64_t)batch * rows + row) * cols + col;
-      if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int e = 0; e < V; e++) v[e] *= 1.f / scale;
-      }
       if (bf16_out) return store_row<bf16_t, V>((bf16_t*)out + to, vec, left, v);
       return store_row<float, V>((float*)out + to, vec, left, v);
     }
@@ -230,7 +249,7 @@ template <typename T>
 struct Layout {      // of the workspace
   int ld, ld_small;
   Plan gram, square, step;
-  int64_t matrix, small, shares, factor, x, next, low, a, b, diagonal, part, bytes;
+  int64_t matrix, small, shares, scales, x, next, low, a, b, diagonal, part, bytes;
   explicit Layout(const Stack& n) {
     constexpr int V = kPiece<T>;
     const int s = n.small(), l = std::max(n.rows, n.columns);
@@ -247,7 +266,7 @@ struct Layout {      // of the workspace
     };
     const bool half = sizeof(T) == 2;
     shares = take((int64_t)n.count * kNormShares * sizeof(double));
-    factor = take((int64_t)n.count * sizeof(float));
+    scales = half ? take((int64_t)n.count * kMostSteps * sizeof(float4)) : 0;
     x = take(n.count * matrix * sizeof(T));
     next = take(n.count * matrix * sizeof(T));
     low = half ? take(n.count * matrix * sizeof(T)) : 0;
@@ -259,41 +278,65 @@ struct Layout {      // of the workspace
   }
 };
 
-// Whether fp16 holds what arises: the largest singular value that each step can leave stays below 32, B below 2^14
-bool fits_half(int steps, const float* coefficients) {
-  double most = 1.0;
+// The schedule of fp16 products; false where their roundings would show.  In 64 bits, of q(s) = a + b s^2 + c s^4, what a step multiplies a singular value s
+// by, over 0 <= s <= m, the largest that can be.
+//   Gap: by how much |X_t| may fall below its bound, for any |X_0|: up to 2^10 elements are 2^14 times fp16's smallest in matrices of 2^30 elements.
+//   A q that changes its sign may bring |X_t| to nothing.
+bool schedule_of(int steps, const float* coefficients, Schedule& to) {
+  const int points = 64;
+  double most = 1.0, gap = 1.0, growth = 0.0;
+  to.steps = steps;
+  to.bound[0] = to.growth[0] = 0;
   for (int t = 0; t < steps; t++) {
     const double a = coefficients[3 * t], b = coefficients[3 * t + 1], c = coefficients[3 * t + 2], m2 = most * most;
-    if (!(std::fabs(b) * m2 + std::fabs(c) * m2 * m2 < 16384.0)) return false;
-    auto size = [&](double s2) { return std::fabs(std::sqrt(s2) * (a + s2 * (b + c * s2))); };
-    double next = size(m2);
-    // where a + 3 b s^2 + 5 c s^4 is 0
-    const double root = 9.0 * b * b - 20.0 * a * c;
-    if (c == 0.0) {
-      if (b != 0.0 && -a / (3.0 * b) > 0.0) next = std::max(next, size(std::min(m2, -a / (3.0 * b))));
-    } else if (root >= 0.0) {
-      for (double sign : {-1.0, 1.0}) {
-        const double s2 = (-3.0 * b + sign * std::sqrt(root)) / (10.0 * c);
-        if (s2 > 0.0) next = std::max(next, size(std::min(m2, s2)));
-      }
+    auto factor = [&](double s2) { return a + s2 * (b + c * s2); };
+    // where q and s q are largest: at the ends, or where 2 b + 4 c s^2 or a + 3 b s^2 + 5 c s^4 is 0
+    double at[points + 4];      // s^2
+    int n = 0;
+    auto inside = [&](double s2) {
+      if (s2 > 0.0 && s2 < m2) at[n++] = s2;
+    };
+    for (int i = 0; i <= points; i++) at[n++] = m2 * i * i / (points * points);
+    if (c != 0.0) {
+      inside(-b / (2.0 * c));
+      const double root = 9.0 * b * b - 20.0 * a * c;
+      if (root >= 0.0)
+        for (double sign : {-1.0, 1.0}) inside((-3.0 * b + sign * std::sqrt(root)) / (10.0 * c));
+    } else if (b != 0.0) {
+      inside(-a / (3.0 * b));
     }
-    if (!(next < 32.0)) return false;
-    most = next * 1.01;      // roundings
+    std::sort(at, at + n);
+    double largest = 0.0, next = 0.0;
+    for (int i = 0; i < n; i++) largest = std::max(largest, std::fabs(factor(at[i]))), next = std::max(next, std::sqrt(at[i]) * std::fabs(factor(at[i])));
+    if (!(next > 1e-30 && next < 1e36 && largest < 1e36)) return false;
+    next *= 1.01;      // roundings
+    double least = largest, fall = 1.0;
+    for (int i = 0; i < n; i++) {
+      const double q = factor(at[i]);
+      if (q == 0.0 || (q > 0.0) != (a > 0.0)) return false;
+      least = std::min(least, std::fabs(q));
+      fall = std::max(fall, (at[i] > 0.0 ? std::min(largest, next / std::sqrt(at[i])) : largest) / least);
+    }
+    gap *= fall;
+    growth += std::log2(largest * 1.01);
+    const int g = (int)std::ceil(std::log2(largest));
+    to.g[t] = (int16_t)g;
+    to.a[t] = (float)std::ldexp(a, -g), to.b[t] = (float)std::ldexp(b, -g), to.c[t] = (float)std::ldexp(c, -g);
+    to.bound[t + 1] = (int16_t)std::ceil(std::log2(next)), to.growth[t + 1] = (int16_t)std::ceil(growth);
+    most = next;
   }
-  return true;
+  return gap <= 1024.0;
 }
 
 template <typename T, typename G>
-int orthogonalize(const G* x, int64_t x_matrix, int64_t x_stride, const Stack& n, int steps, const float* coefficients, float eps, void* out, char* ws,
-                  hipStream_t s) {
+int orthogonalize(const G* x, int64_t x_matrix, int64_t x_stride, const Stack& n, int steps, const float* coefficients, const Schedule& schedule, float eps,
+                  void* out, char* ws, hipStream_t s) {
   constexpr bool HALF = sizeof(T) == 2;
   const Layout<T> w(n);
   const int small = n.small(), rows = n.rows, columns = n.columns;
   const bool tall = rows > columns;
-  // elements of an orthogonalised matrix are 1 / sqrt(its longer side) on average: that becomes about 1
-  const float scale = HALF ? std::exp2(std::floor(0.5f * std::log2((float)std::max(rows, columns)))) : 1.f;
   double* const shares = (double*)(ws + w.shares);
-  float* const factor = (float*)(ws + w.factor);
+  float4* const scales = (float4*)(ws + w.scales);
   const int64_t pieces = (int64_t)rows * (w.ld / kPiece<T>);
   const int n_shares = (int)std::min<int64_t>((pieces + 1023) / 1024, std::max(std::min(2048 / n.count, kNormShares), 1));
   T *now = (T*)(ws + w.x), *next = (T*)(ws + w.next);
@@ -302,7 +345,7 @@ int orthogonalize(const G* x, int64_t x_matrix, int64_t x_stride, const Stack& n
     const bool whole = aligned16(x) && columns % 8 == 0 && x_stride % 8 == 0 && x_matrix % 8 == 0;
     squares_kernel<G><<<dim3(n_shares, n.count), 256, 0, s>>>(x, x_matrix, x_stride, rows, columns, whole, shares);
     normalise_kernel<G, T><<<dim3((unsigned)std::min<int64_t>((pieces + 511) / 512, std::max(2048 / n.count, 1)), n.count), 256, 0, s>>>(
-        x, x_matrix, x_stride, rows, columns, w.ld, whole, shares, n_shares, (double)eps, (double)scale, now, factor);
+        x, x_matrix, x_stride, rows, columns, w.ld, whole, shares, n_shares, (double)eps, schedule, now, scales);
   }
   T *const a = (T*)(ws + w.a), *const b = (T*)(ws + w.b);
   float* const diagonal = (float*)(ws + w.diagonal);
@@ -315,20 +358,20 @@ int orthogonalize(const G* x, int64_t x_matrix, int64_t x_stride, const Stack& n
       const Operand<T> o{now, w.ld, w.matrix, 0, rows, rows, w.ld, w.ld, n.count * w.matrix};
       p.a = p.b = o;
       p.k = p.last_k = tall ? rows : w.ld, p.rows = p.cols = small;
-      const Gram<T> e{a, w.small, w.ld_small, small, 1.f / scale, HALF && t == 0 ? factor : nullptr};
+      const Gram<T> e{a, w.small, w.ld_small, small};
       if (tall) launch<T, true, true>(p, w.gram, e, s);
       else launch<T, false, false>(p, w.gram, e, s);
     }
     const Operand<T> square{a, w.ld_small, w.small, 0, small, small, w.ld_small, w.ld_small, n.count * w.small};
     p.a = p.b = square, p.k = p.last_k = w.ld_small;
-    launch<T, false, false>(p, w.square, Polynomial<T>{a, b, diagonal, w.small, w.ld_small, small, c[1], c[2]}, s);
+    launch<T, false, false>(p, w.square, Polynomial<T>{a, b, diagonal, w.small, w.ld_small, small, c[1], c[2], scales + t}, s);
     {
       const Operand<T> o{now, w.ld, w.matrix, 0, rows, rows, w.ld, w.ld, n.count * w.matrix};
       Operand<T> poly = square;
       poly.p = b;
       p.rows = rows, p.cols = columns;
       Step<T> e{now, HALF && t > 0 && !last ? low : nullptr, next, HALF && t + 2 < steps ? low : nullptr, last ? out : nullptr, diagonal,
-                HALF && t == 0 ? factor : nullptr, w.matrix, rows, columns, w.ld, tall, std::is_same<G, bf16_t>::value, 0, n.count * w.matrix * (int64_t)sizeof(T) > kStream, c[0], scale};
+                scales + t, w.matrix, rows, columns, w.ld, tall, std::is_same<G, bf16_t>::value, 0, n.count * w.matrix * (int64_t)sizeof(T) > kStream, HALF ? schedule.a[t] : c[0]};
       e.vec = columns % kPiece<T> == 0 && columns % (16 / sizeof(G)) == 0 && aligned16(out);
       p.k = p.last_k = w.ld_small;
       if (tall) {
@@ -344,8 +387,8 @@ int orthogonalize(const G* x, int64_t x_matrix, int64_t x_stride, const Stack& n
   return probe ? RL_OK : launched();
 }
 
-bool takes_half(const Stack& n, int dtype, int steps, const float* coefficients) {
-  return dtype == RL_DTYPE_BF16 && n.small() >= kHalfFrom && fits_half(steps, coefficients);
+bool takes_half(const Stack& n, int dtype, int steps, const float* coefficients, Schedule& schedule) {
+  return dtype == RL_DTYPE_BF16 && n.small() >= kHalfFrom && schedule_of(steps, coefficients, schedule);
 }
 const char* stack_argument(int32_t count, int32_t rows, int32_t columns, int32_t dtype) {
   if (dtype != RL_DTYPE_F32 && dtype != RL_DTYPE_BF16) return "dtype is RL_DTYPE_F32 or RL_DTYPE_BF16";
@@ -366,7 +409,7 @@ extern "C" int64_t rl_orthogonalize_workspace(int32_t count, int32_t rows, int32
 extern "C" int rl_orthogonalize(const void* d_x, int64_t matrix_stride, int64_t row_stride, int32_t count, int32_t rows, int32_t columns, int32_t steps,
                                 const float* coefficients, float eps, int32_t dtype, void* d_out, void* d_workspace, int64_t workspace_bytes, void* stream) {
   if (const char* m = stack_argument(count, rows, columns, dtype)) return rl_fail(RL_E_ARG, m);
-  if (steps < 1 || steps > 64 || !coefficients) return rl_fail(RL_E_ARG, "1 to 64 steps with three coefficients each");
+  if (steps < 1 || steps > kMostSteps || !coefficients) return rl_fail(RL_E_ARG, "1 to 64 steps with three coefficients each");
   for (int i = 0; i < 3 * steps; i++)
     if (!std::isfinite(coefficients[i])) return rl_fail(RL_E_ARG, "a coefficient is infinite or no number");
   if (!(eps >= 0.f)) return rl_fail(RL_E_ARG, "eps is negative or no number");
@@ -377,10 +420,11 @@ extern "C" int rl_orthogonalize(const void* d_x, int64_t matrix_stride, int64_t 
   const Stack n{count, rows, columns};
   hipStream_t s = (hipStream_t)stream;
   char* ws = (char*)d_workspace;
-  if (dtype == RL_DTYPE_F32) return orthogonalize<float>((const float*)d_x, matrix_stride, row_stride, n, steps, coefficients, eps, d_out, ws, s);
-  if (takes_half(n, dtype, steps, coefficients))
-    return orthogonalize<_Float16>((const bf16_t*)d_x, matrix_stride, row_stride, n, steps, coefficients, eps, d_out, ws, s);
-  return orthogonalize<float>((const bf16_t*)d_x, matrix_stride, row_stride, n, steps, coefficients, eps, d_out, ws, s);
+  Schedule schedule{};
+  if (dtype == RL_DTYPE_F32) return orthogonalize<float>((const float*)d_x, matrix_stride, row_stride, n, steps, coefficients, schedule, eps, d_out, ws, s);
+  if (takes_half(n, dtype, steps, coefficients, schedule))
+    return orthogonalize<_Float16>((const bf16_t*)d_x, matrix_stride, row_stride, n, steps, coefficients, schedule, eps, d_out, ws, s);
+  return orthogonalize<float>((const bf16_t*)d_x, matrix_stride, row_stride, n, steps, coefficients, schedule, eps, d_out, ws, s);
 }
 
 extern "C" int rl_debug_orthogonalize_loads(int32_t count, int32_t rows, int32_t columns, int32_t dtype, int64_t* out) {
