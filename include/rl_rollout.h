@@ -475,8 +475,8 @@ int rl_residual_norm_backward(const void* d_dout, int64_t dout_stride, const voi
  * values that are no number or infinite make that matrix no numbers, never another one.
  * float32: sums and operands in 32 bits.  bf16: from a smaller side of 256 on the operands of the products are rounded to fp16 (11 bits), scaled by powers of two so that
  * neither |G| beside eps nor the steps take them out of its range; X is kept with 22 bits between the steps, with 11 in the last; sums in 32 bits.  Results are then
- * 0.0017 to 0.0025 off in five steps (relative, by their norm; their last rounding alone 0.0017).  Coefficients whose factor a + b s^2 + c s^4 may come near 0 or change its
- * sign take float32.
+ * 0.0017 to 0.003 off (relative, by their norm; their last rounding alone 0.0017).  Coefficients whose steps enlarge small singular values beside the largest by more than 2^15
+ * together, or whose factor a + b s^2 + c s^4 may come near 0 or change its sign, take float32.
  * steps 1 to 64, count at most 65535, sides at most 2^20 - 8, a matrix (sides + 8) at most 2^30 - 2^20 elements.  Workspace 256-byte aligned.
  */
 int64_t rl_orthogonalize_workspace(int32_t count, int32_t rows, int32_t columns, int32_t dtype);

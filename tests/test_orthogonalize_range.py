@@ -1,4 +1,4 @@
-"""Orthogonalised updates in bf16 whose X is far from 1: |G| far below eps, coefficients that shrink or enlarge;
+"""Orthogonalised updates in bf16 whose X is far from 1: |G| far below eps, coefficients that shrink or enlarge, steps that enlarge the smallest singular values;
 against the same steps in float64."""
 import pytest
 import torch
@@ -65,6 +65,20 @@ def test_steps_that_shrink_or_enlarge(coefficients):
         # a step's B is rounded twice, 2^-11 of it each time, and |b| + |c| is at most half of |a|, so B at most what is left of a: 2^-10 in the first step, after which X is a
         # hundredth and B nothing.  64 roundings of 2^-22 in chains of 64 steps
         assert off(ops.orthogonalize(x, steps=len(c32), coefficients=coefficients, eps=0.0), want) < last_rounding(want) + PLAIN + 2 * F16 + 64 * 2.0 ** -22, kind
+
+
+@pytest.mark.parametrize("steps", [5, 8, 10, 12, 16])
+@pytest.mark.parametrize("power", [12, 16, 20, 24])
+def test_singular_values_that_many_steps_enlarge(steps, power):
+    for tall in (False, True):
+        x = sized(matrices(gen(9), 1, 256, 1024, torch.float64, "noise"), 1.0)[0]
+        x[32:] *= 2.0 ** -power
+        x = x.t().contiguous() if tall else x
+        got = ops.orthogonalize(x, steps=steps, eps=0.0)
+        want = newton(x, False, None, steps=steps, eps=0.0, roundings=False)
+        # fp16's share as stated, 0.003 together with the last rounding; where 2^15 is passed, from nine steps on, that of the fp32 products' model
+        bound = 0.003 if steps <= 8 else last_rounding(want) + 2 * off(newton(x, False, gen(4), steps=steps, eps=0.0), want) + 1e-6
+        assert off(got, want) < bound, (tall, off(got, want), bound)
 
 
 @pytest.mark.parametrize("coefficients,steps", [((1.5, -0.5, 0.0), 20), ((15 / 8, -10 / 8, 3 / 8), 12)])
