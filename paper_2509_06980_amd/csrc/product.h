@@ -116,13 +116,15 @@ struct Product {
 };
 
 // What a tile's loads of one operand may reach, from element `begin` on.  Scalar offsets stay inside: the hardware compares a lane's offset with the
-// size less the scalar one.
+// size less the scalar one.  A tile behind the operand, which no product has, reaches what the first
+// one does: a size below 0 would be one of 4 GiB, and a size of 0 less a scalar offset too.
 struct Reach {
   int64_t begin;
   unsigned bytes;
 };
 template <typename T>
 __host__ __device__ __forceinline__ Reach reach_of(bool strided, int64_t ld, int n, int width, int at, int rows) {
+  if (at >= (strided ? width : n)) at = 0;
   if (strided) return {at, (unsigned)(((n - 1) * ld + width - at) * (int64_t)sizeof(T))};
   const int left = n - at;
   return {at * ld, (unsigned)((((left < rows ? left : rows) - 1) * ld + width) * (int64_t)sizeof(T))};
@@ -610,9 +612,6 @@ void go(const Product<T>& p, const EPI& epi, hipStream_t s) {
 
 // ---- the plan of a product: tile and slices -----------------------------------------------------------------------------------
 struct Plan { int mb, nb, slices; };
-// Bytes of a row in a chunk of the tile
-template <typename T>
-constexpr int chunk_bytes(int mb, bool strided) { return sizeof(T) == 4 || mb == 2 || (mb == 4 && !strided) ? 128 : 64; }
 // The cheapest by estimate.  A round of tiles takes what its chunks take and some us to begin and end; what the epilogue reads and writes (`bytes` an
 // element of C) goes at 4.5 TB/s, half of it beside the other workgroup's products where a CU holds two; sums of slices are written and read at that rate
 // too.  us of a chunk fitted on products of 2744 to 4096 rows, K of 1024 to 9728, batches of 28: 256 x 256 (one workgroup a CU) 0.87, 192 x 256
@@ -677,13 +676,14 @@ void find_overreach(const Product<T>& p, bool strided_a, bool strided_b, int row
   operand(strided_b, p.b, p.tiles_j, rows_j, 0);
   if (second) operand(strided_b, p.b, p.tiles_j, rows_j, second);
 }
+// A product by the plan's tile, or by the one that is built in its place: its tiles are counted for the kernel that runs, whatever the plan says.
 template <typename T, bool TA, bool TB, typename EPI>
 void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
-  const int bn = EPI::GATED ? 32 * plan.nb : 64 * plan.nb;
-  p.tiles_i = (p.rows + 64 * plan.mb - 1) / (64 * plan.mb), p.tiles_j = (p.cols + bn - 1) / bn, p.slices = plan.slices, p.group = 4;
-  if (probe) return find_overreach(p, TA, TB, 64 * plan.mb, bn, EPI::GATED ? p.b2 : 0, chunk_bytes<T>(plan.mb, TA || TB));
+  p.slices = plan.slices, p.group = 4;
   auto with = [&](auto mb, auto nb, auto r, auto cb) {
-    constexpr int MB = decltype(mb)::value, NB = decltype(nb)::value, R = decltype(r)::value, CB = decltype(cb)::value;
+    constexpr int MB = decltype(mb)::value, NB = decltype(nb)::value, R = decltype(r)::value, CB = decltype(cb)::value, BM = 64 * MB, BN = EPI::GATED ? 32 * NB : 64 * NB;
+    p.tiles_i = (p.rows + BM - 1) / BM, p.tiles_j = (p.cols + BN - 1) / BN;
+    if (probe) return find_overreach(p, TA, TB, BM, BN, EPI::GATED ? p.b2 : 0, CB);
     if (plan.slices > 1) return go<T, TA, TB, MB, NB, R, CB, true>(p, epi, s);
     go<T, TA, TB, MB, NB, R, CB, false>(p, epi, s);
   };
@@ -697,7 +697,8 @@ void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
     }
     // one workgroup a CU or fewer: nothing else covers the latency of its loads (512 x 512 orthogonalised 218 us with two stages, 209 with four; 1024 x 4096
     // 336 and 320, 2560 x 9728 1398 and 1374)
-    if ((int64_t)(EPI::SYMMETRIC ? p.tiles_i * (p.tiles_i + 1) / 2 : p.tiles_i * p.tiles_j) * p.slices * p.batches <= 256) return with(RL_I(2), RL_I(2), RL_I(4), RL_I(128));
+    const int64_t ti = (p.rows + 127) / 128, tj = (p.cols + (EPI::GATED ? 63 : 127)) / (EPI::GATED ? 64 : 128);
+    if ((EPI::SYMMETRIC ? ti * (ti + 1) / 2 : ti * tj) * p.slices * p.batches <= 256) return with(RL_I(2), RL_I(2), RL_I(4), RL_I(128));
     with(RL_I(2), RL_I(2), RL_I(2), RL_I(128));
   } else {
     if constexpr (!EPI::GATED) {
