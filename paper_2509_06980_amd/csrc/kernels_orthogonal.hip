@@ -158,12 +158,16 @@ struct Polynomial {
     float first = b, second = c;
     if constexpr (sizeof(T) == 2) first = scales[batch * kMostSteps].x, second = scales[batch * kMostSteps].y;
 #pragma unroll
-    for (int e = 0; e < V; e++) {
-      v[e] = first * x.a[e] + second * v[e];
-      if (sizeof(T) == 2 && col + e == row) {
-        diagonal[batch * padded(n) + row] = v[e];
-        v[e] = 0.f;
+    for (int e = 0; e < V; e++) v[e] = first * x.a[e] + second * v[e];
+    asm volatile("" : "+v"(row), "+v"(col));      // or parts of their difference are kept in scalar registers, of which there are too few, through the products
+    if (sizeof(T) == 2 && (unsigned)(row - col) < V) {
+      float one = 0.f;
+#pragma unroll
+      for (int e = 0; e < V; e++) {
+        one = col + e == row ? v[e] : one;
+        v[e] = col + e == row ? 0.f : v[e];
       }
+      diagonal[batch * padded(n) + row] = one;
     }
     across(batch, row, col, v);
   }

@@ -32,6 +32,7 @@ __device__ __forceinline__ void load_to_lds(unsigned lds, int voff, u32x4 rsrc, 
 // Scalars that vector instructions wrote have to be five wait states old when the loads above read them.  The wait takes them as its operand:
 // one that only stood between them in the source could be moved ahead of them.
 __device__ __forceinline__ void settle(u32x4& rsrc) { asm volatile("s_nop 4" : "+s"(rsrc)); }
+__device__ __forceinline__ void settle(unsigned& a, unsigned& b) { asm volatile("s_nop 4" : "+s"(a), "+s"(b)); }
 // The same with 4 bytes per lane (lane l's at lds + 4 l), whatever wrote the scalars: few of them, so each waits by itself.
 __device__ __forceinline__ void load_dword_to_lds(unsigned lds, int voff, u32x4 rsrc, unsigned soff) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc),

@@ -235,6 +235,7 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
   Place next{};
   unsigned tail = 0;      // k-contiguous: pieces of the chunk behind the end of k lie out of reach
   int seg_k = 0;
+  unsigned oa = 0, ob = 0;      // scalar offsets of the chunk
   auto enter = [&](int seg) {      // a segment of tile `next`
     const Product<T>& P = arguments()->p;
     const bool end = seg == P.segments - 1;
@@ -252,8 +253,10 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
     settle(rb);
     if constexpr (GATED) settle(rb2);
   };
-  auto set_tail = [&]() {
+  auto set_chunk = [&]() {
     if constexpr (!TA || !TB) tail = li * KC + kpos >= seg_k ? 0x80000000u : 0u;
+    oa = (unsigned)li * sa, ob = (unsigned)li * sb;
+    settle(oa, ob);
   };
   auto advance = [&]() {
     lc++, li++;
@@ -272,17 +275,17 @@ __global__ __launch_bounds__(256, MB * NB > 4 ? 1 : 2) void product_kernel(Argum
         }
       }
     }
-    set_tail();
+    set_chunk();
   };
   auto load = [&](int j, int stage) {      // piece j of this wave
     const unsigned dst = lds0 + (unsigned)stage * BUF + (unsigned)(j * 4 + wave) * 1024u;
     if (j < PA) {
-      load_to_lds(dst, TA ? va[j] : (int)(va[j] | tail), ra, (unsigned)li * sa);
+      load_to_lds(dst, TA ? va[j] : (int)(va[j] | tail), ra, oa);
     } else {
       const int off = TB ? vb[j - PA] : (int)(vb[j - PA] | tail);
       const bool second = GATED && (NB == 4 ? (j - PA) / (CB / 64) & 1 : CB == 64 ? wave >> 1 : (j - PA) & 1);
-      if (GATED && second) load_to_lds(dst, off, rb2, (unsigned)li * sb);
-      else load_to_lds(dst, off, rb, (unsigned)li * sb);
+      if (GATED && second) load_to_lds(dst, off, rb2, ob);
+      else load_to_lds(dst, off, rb, ob);
     }
   };
   f32x16 acc[MB][NB];
