@@ -130,14 +130,16 @@ struct Finish {
 // One row x 4096 x 2560 with a residual: 6.9 us (3.0 TB/s, of it 2 us to begin and end), by the tiles of many rows 14.  From 17 rows on those tiles are faster (37 rows x 2560 x 9728, gated: 29 us with
 // the slices' sums; this way, three blocks of rows a workgroup, 50).
 const int kFewRows = 16, kFewWaves = 8;
+// Where a lane's reads of an operand begin, in elements: row `row`, or the last one in place of those behind it
+__host__ __device__ __forceinline__ int64_t few_rows_begin(int row, int rows, int64_t ld) { return (int64_t)(row < rows ? row : rows - 1) * ld; }
 template <typename T, typename EPI>
 __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(const T* __restrict__ x, int64_t x_ld, const T* __restrict__ w, int64_t w_ld, int64_t second,
                                                                   int rows, int k, int outer, EPI epi) {
   constexpr int E = 16 / sizeof(T), KS = 4 * E, M = EPI::GATED ? 2 : 1, U = 8, V = kPiece<T>;
   __shared__ float sums[M][kFewWaves][16][17];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n0 = blockIdx.x * 16, r = lane & 15, kl = lane / 16 * E;
-  const T* const wp = w + (int64_t)min(n0 + r, outer - 1) * w_ld + kl;
-  const T* const xp = x + (int64_t)min(r, rows - 1) * x_ld + kl;
+  const T* const wp = w + few_rows_begin(n0 + r, outer, w_ld) + kl;
+  const T* const xp = x + few_rows_begin(r, rows, x_ld) + kl;
   f32x4 acc[M];
 #pragma unroll
   for (int m = 0; m < M; m++) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -192,8 +194,18 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(const T* __res
   epi(0, row, n0 + c, v, u, extra);
 }
 template <typename T, typename EPI>
-void launch_few_rows(const T* x, int64_t x_ld, const T* w, int64_t w_ld, int64_t second, int rows, int k, int outer, const EPI& epi, hipStream_t s) {
-  if (!probe) few_rows_kernel<T, EPI><<<(outer + 15) / 16, 64 * kFewWaves, 0, s>>>(x, x_ld, w, w_ld, second, rows, k, outer, epi);
+void launch_few_rows(const Product<T>& p, const EPI& epi, hipStream_t s) {
+  const int groups = (p.cols + 15) / 16;
+  if (probe) {      // a row's pieces begin before k, which is whole pieces
+    auto look = [&](int64_t from, int last, int rows, int64_t ld, int64_t elements) {
+      probe->buffers = std::max({probe->buffers, -from * (int64_t)sizeof(T), (from + few_rows_begin(last, rows, ld) + p.k - elements) * (int64_t)sizeof(T)});
+    };
+    look(0, 15, p.rows, p.a.ld, p.a.elements);
+    look(0, groups * 16 - 1, p.cols, p.b.ld, p.b.elements);
+    if (EPI::GATED) look(p.b.p + p.b2 - p.u, groups * 16 - 1, p.cols, p.b.ld, p.u_elements);
+    return;
+  }
+  few_rows_kernel<T, EPI><<<groups, 64 * kFewWaves, 0, s>>>(p.a.p, p.a.ld, p.b.p, p.b.ld, p.b2, p.rows, p.k, p.cols, epi);
 }
 
 // ---- rows of an operand in whole 16 bytes: [rows][ld], zeros behind `width` -----------------------------------------------------------
@@ -450,12 +462,11 @@ int forward(const Shape& n, const Forward& f, void* ws, hipStream_t s) {
     return e;
   };
   auto product = [&](const auto& e) {
-    if (n.rows <= kFewRows) launch_few_rows<T>(x.p, x.ld, w.p, w.ld, p.b2, n.rows, w.width, n.outer, e, s);
+    if (n.rows <= kFewRows) launch_few_rows<T>(p, e, s);
     else launch<T, false, false>(p, plan, e, s);
   };
   if (n.mats == 2) {
-    p.b2 = u.p - w.p;
-    if (probe) p.b2 = 0, p.b.elements = std::min(w.elements, u.elements);
+    p.b2 = u.p - w.p, p.u = u.p, p.u_elements = u.elements;
     product(finish(Finish<T, true, false>{}));
   } else if (f.act == RL_ACT_NONE && !f.bias && !f.residual && !f.kept) {
     product(finish(Finish<T, false, true>{}));
@@ -519,7 +530,8 @@ int backward(const Shape& n, const Backward& f, void* ws, hipStream_t s) {
     Room r = room;      // both products' sums of slices lie in one place
     Product<T> p{};
     p.a = {dz.p, dz.ld, 0, dz_matrix, n.rows, n.rows, dz.width, dz.width, dz.elements};
-    p.b = {w.p, w.ld, 0, n.mats == 2 && !probe ? u.p - w.p : 0, n.outer, n.outer, w.width, w.width, w.elements};
+    p.b = {w.p, w.ld, 0, n.mats == 2 ? u.p - w.p : 0, n.outer, n.outer, w.width, w.width, w.elements};
+    p.u = u.p, p.u_elements = u.elements;
     p.k = p.last_k = dz.width, p.segments = n.mats, p.batches = 1;
     p.rows = n.rows, p.cols = n.inner;
     const Plan plan = dx_plan<T>(n);

@@ -108,6 +108,8 @@ template <typename T>
 struct Product {
   Operand<T> a, b;
   int64_t b2;                     // gated: from B to the second matrix's rows, in elements
+  const T* u;                     // where B's second matrix lies (gated) or its second segment, if that is a matrix of its own, and the elements from there on: for the check of
+  int64_t u_elements;             // the loads
   int tiles_i, tiles_j, batches, segments, slices;
   int k, last_k;                  // of a segment; of the last
   int group;                      // row tiles that an XCD takes together
@@ -656,18 +658,18 @@ struct Probe {
 };
 inline thread_local Probe* probe = nullptr;
 template <typename T>
-void find_overreach(const Product<T>& p, bool strided_a, bool strided_b, int rows_i, int rows_j, int64_t second, int bytes) {
+void find_overreach(const Product<T>& p, bool strided_a, bool strided_b, int rows_i, int rows_j, bool gated, int bytes) {
   const int64_t el = sizeof(T);
   probe->products++;
-  auto operand = [&](bool strided, const Operand<T>& o, int tiles, int size, int64_t more) {
+  auto operand = [&](bool strided, const Operand<T>& o, int tiles, int size, int64_t more, bool of_b, bool other) {
     for (int batch : {0, p.batches - 1})
       for (int seg = 0; seg < p.segments; seg++)
         for (int i = 0; i < tiles; i++) {
-          const bool end = seg == p.segments - 1;
+          const bool end = seg == p.segments - 1, second = of_b && p.u && (other || seg > 0);
           const Reach r = reach_of<T>(strided, o.ld, end ? o.last_rows : o.rows, end ? o.last_width : o.width, i * size, size);
-          const int64_t at = batch * o.batch + seg * o.segment + r.begin + more;
+          const int64_t at = batch * o.batch + seg * o.segment + r.begin + more - (second ? p.u - o.p : 0);
           const int n = chunks<T>(end ? p.last_k : p.k, bytes);
-          probe->buffers = std::max({probe->buffers, -at * el, at * el + (int64_t)r.bytes - o.elements * el});
+          probe->buffers = std::max({probe->buffers, -at * el, at * el + (int64_t)r.bytes - (second ? p.u_elements : o.elements) * el});
           // 64 bits beside what the kernel computes in 32
           const int64_t step = strided ? o.ld * bytes : bytes, rows = strided ? bytes / el : std::min<int64_t>(size, (end ? o.last_rows : o.rows) - i * size);
           const int64_t furthest = strided ? (bytes / el - 1) * o.ld * el + size * el : (rows - 1) * o.ld * el + bytes;
@@ -675,9 +677,9 @@ void find_overreach(const Product<T>& p, bool strided_a, bool strided_b, int row
           probe->offsets = std::max(probe->offsets, (n - 1) * step + 1 - (int64_t)r.bytes);
         }
   };
-  operand(strided_a, p.a, p.tiles_i, rows_i, 0);
-  operand(strided_b, p.b, p.tiles_j, rows_j, 0);
-  if (second) operand(strided_b, p.b, p.tiles_j, rows_j, second);
+  operand(strided_a, p.a, p.tiles_i, rows_i, 0, false, false);
+  operand(strided_b, p.b, p.tiles_j, rows_j, 0, true, false);
+  if (gated) operand(strided_b, p.b, p.tiles_j, rows_j, p.b2, true, true);
 }
 // A product by the plan's tile, or by the one that is built in its place: its tiles are counted for the kernel that runs, whatever the plan says.
 template <typename T, bool TA, bool TB, typename EPI>
@@ -686,7 +688,7 @@ void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
   auto with = [&](auto mb, auto nb, auto r, auto cb) {
     constexpr int MB = decltype(mb)::value, NB = decltype(nb)::value, R = decltype(r)::value, CB = decltype(cb)::value, BM = 64 * MB, BN = EPI::GATED ? 32 * NB : 64 * NB;
     p.tiles_i = (p.rows + BM - 1) / BM, p.tiles_j = (p.cols + BN - 1) / BN;
-    if (probe) return find_overreach(p, TA, TB, BM, BN, EPI::GATED ? p.b2 : 0, CB);
+    if (probe) return find_overreach(p, TA, TB, BM, BN, EPI::GATED, CB);
     if (plan.slices > 1) return go<T, TA, TB, MB, NB, R, CB, true>(p, epi, s);
     go<T, TA, TB, MB, NB, R, CB, false>(p, epi, s);
   };
