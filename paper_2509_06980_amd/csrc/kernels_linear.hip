@@ -197,6 +197,7 @@ template <typename T, typename EPI>
 void launch_few_rows(const Product<T>& p, const EPI& epi, hipStream_t s) {
   const int groups = (p.cols + 15) / 16;
   if (probe) {      // a row's pieces begin before k, which is whole pieces
+    probe->form(__PRETTY_FUNCTION__, 1);
     auto look = [&](int64_t from, int last, int rows, int64_t ld, int64_t elements) {
       probe->buffers = std::max({probe->buffers, -from * (int64_t)sizeof(T), (from + few_rows_begin(last, rows, ld) + p.k - elements) * (int64_t)sizeof(T)});
     };

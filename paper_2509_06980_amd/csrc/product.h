@@ -592,6 +592,8 @@ __global__ __launch_bounds__(256) void join_symmetric_kernel(Product<T> P, EPI e
 }
 
 template <typename T, bool TA, bool TB, int MB, int NB, int R, int CB, bool SLICED, typename EPI>
+const char* form_of() { return __PRETTY_FUNCTION__; }
+template <typename T, bool TA, bool TB, int MB, int NB, int R, int CB, bool SLICED, typename EPI>
 void go(const Product<T>& p, const EPI& epi, hipStream_t s) {
   constexpr int lds = Lds<T, MB, NB, R, CB, EPI::GATED>::BYTES;
   auto kernel = product_kernel<T, TA, TB, MB, NB, R, CB, SLICED, EPI>;
@@ -655,6 +657,14 @@ inline int64_t part_bytes(const Plan& p, int64_t rows, int64_t cols, int64_t bat
 // arithmetic over all tiles, in place of the launches, while a thread's `probe` is set.
 struct Probe {
   int64_t buffers, offsets, products;
+  struct Form {
+    const char* kernel;
+    int segments;
+  } forms[8];                   // of the products that the call launches, the first eight
+  int n_forms;
+  void form(const char* kernel, int segments) {
+    if (n_forms < 8) forms[n_forms++] = {kernel, segments};
+  }
 };
 inline thread_local Probe* probe = nullptr;
 template <typename T>
@@ -688,6 +698,7 @@ void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
   auto with = [&](auto mb, auto nb, auto r, auto cb) {
     constexpr int MB = decltype(mb)::value, NB = decltype(nb)::value, R = decltype(r)::value, CB = decltype(cb)::value, BM = 64 * MB, BN = EPI::GATED ? 32 * NB : 64 * NB;
     p.tiles_i = (p.rows + BM - 1) / BM, p.tiles_j = (p.cols + BN - 1) / BN;
+    if (probe) probe->form(plan.slices > 1 ? form_of<T, TA, TB, MB, NB, R, CB, true, EPI>() : form_of<T, TA, TB, MB, NB, R, CB, false, EPI>(), p.segments);
     if (probe) return find_overreach(p, TA, TB, BM, BN, EPI::GATED, CB);
     if (plan.slices > 1) return go<T, TA, TB, MB, NB, R, CB, true>(p, epi, s);
     go<T, TA, TB, MB, NB, R, CB, false>(p, epi, s);
