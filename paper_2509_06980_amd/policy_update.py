@@ -167,7 +167,8 @@ class PolicyModel:
 class Muon(torch.optim.Optimizer):
     """Steps with orthogonalised momentum for matrices (groups with orthogonal=True: W <- W - lr max(1, rows / columns)^1/2 O with O the
     orthogonalised m, or gradient + momentum m in Nesterov's form, and m <- momentum m + gradient), Adam's for everything else.
-    Matrices of one shape are orthogonalised together; momenta are kept in 32 bits."""
+    Matrices of one shape are orthogonalised together; momenta are kept in 32 bits, what is orthogonalised is rounded to the matrices' type, and so is the moved
+    matrix, once."""
 
     def __init__(self, params, lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7,
                  adam_lr=3e-4, betas=(0.9, 0.95), adam_eps=1e-8):
@@ -192,7 +193,7 @@ class Muon(torch.optim.Optimizer):
                 for (shape, dtype, _), ps in alike.items():
                     updates = ops.orthogonalize(torch.stack([self._momentum(p, group) for p in ps]).to(dtype), group["steps"], group["coefficients"], group["eps"])
                     for p, o in zip(ps, updates):
-                        p.mul_(1 - group["lr"] * group["weight_decay"]).add_(o, alpha=-group["lr"] * max(1.0, shape[0] / shape[1]) ** 0.5)
+                        self._move(p, o, group["lr"], max(1.0, shape[0] / shape[1]) ** 0.5, group["weight_decay"])
             else:
                 for p in params:
                     self._adam(p, group)
@@ -220,7 +221,14 @@ class Muon(torch.optim.Optimizer):
         state["step"] += 1
         first = state["first"].lerp_(g, 1 - b1) / (1 - b1 ** state["step"])
         second = state["second"].mul_(b2).addcmul_(g, g, value=1 - b2) / (1 - b2 ** state["step"])
-        p.mul_(1 - group["adam_lr"] * group["weight_decay"]).add_((first / (second.sqrt() + group["adam_eps"])).to(p.dtype), alpha=-group["adam_lr"])
+        self._move(p, first / (second.sqrt() + group["adam_eps"]), group["adam_lr"], 1.0, group["weight_decay"])
+
+    @staticmethod
+    def _move(p, update, lr, scale, decay):
+        """p <- (1 - lr decay) p - lr scale update in 32 bits, rounded once: parameters of 16 bits would lose most of a small decay to a rounding of its own."""
+        w = p.float()      # p itself where it has 32 bits
+        w = w * (1 - lr * decay) if decay else w
+        p.copy_(w.add_(update, alpha=-lr * scale))
 
 
 def group_advantages(rewards, group_size, eps_std=1e-6, std_ddof=0):
