@@ -174,9 +174,13 @@ class Muon(torch.optim.Optimizer):
                  adam_lr=3e-4, betas=(0.9, 0.95), adam_eps=1e-8):
         super().__init__(params, dict(orthogonal=False, lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, steps=steps,
                                       coefficients=coefficients, eps=eps, adam_lr=adam_lr, betas=betas, adam_eps=adam_eps))
-        for group in self.param_groups:
-            if group["orthogonal"] and any(p.dim() != 2 for p in group["params"]):
-                raise ValueError("orthogonal steps are for matrices")
+
+    def add_param_group(self, param_group):
+        super().add_param_group(param_group)
+        group = self.param_groups[-1]
+        if group["orthogonal"] and any(p.dim() != 2 for p in group["params"]):
+            del self.param_groups[-1]
+            raise ValueError("orthogonal steps are for matrices")
 
     @torch.no_grad()
     def step(self, closure=None):

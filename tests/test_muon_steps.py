@@ -42,3 +42,15 @@ def test_orthogonal_steps_of_muon_are_rounded_once():
             o = ops.orthogonalize((p.grad.float() + 0.95 * m).to(BF)).double()
             muon.step()
             assert within_half_a_step(p.detach(), before * (1 - 0.1 * decay) - 0.1 * (96 / 40) ** 0.5 * o), (decay, step)
+
+
+def test_groups_that_are_added_later_are_checked_too():
+    q = torch.ones(4, 4, requires_grad=True)
+    muon = pu.Muon([dict(params=[torch.ones(3, 4, requires_grad=True)], orthogonal=True)])
+    for shape in ((3,), (2, 3, 4), ()):
+        with pytest.raises(ValueError, match="matrices"):
+            muon.add_param_group(dict(params=iter([q, torch.ones(shape, requires_grad=True)]), orthogonal=True))
+        assert len(muon.param_groups) == 1
+    muon.add_param_group(dict(params=[q], orthogonal=True))      # nothing of a refused group stays
+    muon.add_param_group(dict(params=[torch.ones(3, requires_grad=True)]))
+    assert [len(g["params"]) for g in muon.param_groups] == [1, 1, 1]
