@@ -282,7 +282,7 @@ def update(model, optimizer, engine, traj_ids, rewards, group_size, temperature=
     return value.item()
 
 
-def main(arguments=None):
+def main(arguments=()):
     import argparse
     import sys
     from pathlib import Path
@@ -318,4 +318,5 @@ def main(arguments=None):
 
 
 if __name__ == "__main__":
-    main()
+    import sys
+    main(sys.argv[1:])
