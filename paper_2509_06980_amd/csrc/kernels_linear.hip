@@ -59,7 +59,9 @@ __device__ __forceinline__ void activate_all(const float (&z)[N], int act, float
   }
 }
 
-// What follows a product's sums; PLAIN: they are rounded and stored, nothing else.
+// What follows a product's sums; PLAIN: they are rounded and stored, nothing else.  Results go past the caches, which keeps the operands there: 4096 rows x 2560 -> 9728 196 us,
+// 210 through them, 8192 rows 337 and 365, 512 rows 37 and 40, up to 128 rows the same.  The next operator pays for it where it would have found them in the caches: gate, up, down and
+// the norm behind them of 2744 rows 495 and 487 us, of 64 rows 57.8 and 56.3, of 4096 rows the same, of 8192 rows 1308 and 1341.
 // SHORT: no activation and nothing kept.
 template <typename T, bool GATED_, bool PLAIN, bool SHORT = PLAIN>
 struct Finish {

@@ -23,8 +23,9 @@ using namespace product;
 const int kMostSteps = 64;
 const int kNormShares = 1024;
 const int kHalfFrom = 256;
-// X goes past the caches where it would not stay in the last one of 256 MB with what else a step reads: 28 x 2048 x 1024 (117 MB) 2.3 % faster,
-// 2560 x 9728 (50 MB) 6 % slower, which keeps the caches.
+// X goes past the caches where it would not stay in the last one of 256 MB with what else a step reads.  Past them | through them: 10 x 2048 x 1024 (42 MB) 759 | 737 us,
+// 2560 x 9728 (50 MB) 1407 | 1377, 4096 x 8192 (67 MB) 2990 | 2969; 24 x 2048 x 1024 (101 MB) 1621 | 1644, 28 of them (117 MB) 1844 | 1866, 3 x 2560 x 9728 (149 MB) 4290 | 4429;
+// 18 x 2048 x 1024 (75 MB), 2 x 4096 x 8192 (134 MB), 40 x 2048 x 1024 (168 MB) the same within 0.4 %; 20 x 2048 x 1024 (84 MB), at the border, 1325 | 1369.
 const int64_t kStream = 80 << 20;
 const float kLow = 2048.f;      // the low half of an element is kept times this
 // fp16: X_t is kept times 2^(kTop - e_t), where none of its singular values is above 2^e_t: elements stay below 2^kTop (four times that fits) and as far above

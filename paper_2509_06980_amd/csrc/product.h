@@ -31,9 +31,10 @@
 // 256 x 256 by the estimate below 270); 128 x 128, two workgroups a CU, with two stages of 128 bytes (where there are no more tiles than CUs four): a CU asks
 // the caches for twice as much there, and in requests of 64 bytes it gets 25 bytes a clock however many are under way (2560 x 9728 orthogonalised 1564 us
 // with 64, 1420 with 128).  fp32: 128 x 128 and 64 x 64, two stages of 128 bytes (1024 x 1024 orthogonalised 373 us, 391 with 64).
-// What bounds the large ones is the power that the matrix units draw: 8192 x 8192 x 8192 in bf16 takes 835 us (1.32 PFLOP/s; operands strided as in the
-// backward pass 819 to 826), of zeros 569.  4096 rows x 2560 -> 9728 takes 222 us (0.92 PFLOP/s): 608 tiles in 2.4 rounds.  Matrix units are busy 39 to
-// 67 % of a launch's clocks, LDS reads wait for a bank in 0 to 5 % of theirs.
+// What bounds the large ones: the clock that the power of the matrix units leaves (8192 x 8192 x 8192 in bf16 takes 835 us, 1.32 PFLOP/s, operands strided as in the
+// backward pass 819 to 826; of zeros 569), and that these are busy in 39 to 67 % of a launch's clocks in linear layers, 20 to 43 % in orthogonalised updates.  The rest of
+// the clocks goes to last rounds with few tiles (4096 rows x 2560 -> 9728: 222 us, 0.92 PFLOP/s, 608 tiles in 2.4 rounds of the CUs), to epilogues with no products beside
+// them and to what a chunk's schedule leaves open; LDS reads wait for a bank in 0 to 5 % of theirs.
 // =============================================================================================
 namespace product {
 
@@ -622,7 +623,10 @@ struct Plan { int mb, nb, slices; };
 // The cheapest by estimate.  A round of tiles takes what its chunks take and some us to begin and end; what the epilogue reads and writes (`bytes` an
 // element of C) goes at 4.5 TB/s, half of it beside the other workgroup's products where a CU holds two; sums of slices are written and read at that rate
 // too.  us of a chunk fitted on products of 2744 to 4096 rows, K of 1024 to 9728, batches of 28: 256 x 256 (one workgroup a CU) 0.87, 192 x 256
-// 0.79, 128 x 128 (two a CU) 0.54, gated 0.62; estimates within 15 % of what was measured, their order right in 13 of 14 pairs.
+// 0.79, 128 x 128 (two a CU) 0.54, gated 0.62; estimates within 15 % of what was measured, their order right in 13 of 14 pairs.  Slices of a symmetric product cost
+// more than their join of 3 to 10 us, for their sums cross the diagonal once more: counted as 25 us in 16-bit types, 8 in fp32.  Orthogonalised updates with that | with 5 us |
+// without such slices: 1024 x 1024 bf16 254 | 269 | 255 us, 2048 x 2048 405 | 448 | 406, 1024 x 4096 324 | 326 | 363, 512 x 8000 282 | 283 | 425, 2560 x 9728 1386 | 1418 | 1347,
+// 2 x 2048 x 8192 1646 | 1626 | 1646; 1024 x 4096 fp32 780 | 780 | 950, 3 x 512 x 256 169 | 168 | 188.
 struct Sizes {
   int64_t rows, cols, batches, n_chunks;
   bool symmetric, gated, strided;      // strided: one of the operands
