@@ -10,9 +10,9 @@ using namespace product;
 // Backward: dz = dy act'(z) [u], du = dy act(z);  dx = dz W [+ du U], dW = dz^T x, db = sum over rows of dz, dr = dy.
 // z and u are kept in 32 bits for the backward call: rounded to bf16 they alone would make the gradients of a gated layer 0.0029 off (relative; the
 // roundings of dz and of the gradient itself 0.0024).  dz and du are rounded to the weights' type once, as the operands that they become.
-// Many rows are bound by the matrix units: 4096 rows, 9728 -> 2560 with a residual, forward and backward 600 us (1.02 PFLOP/s): 236 forward, 11 for dz, 227
-// for dx, 214 for dW.  2744 rows, 2560 -> 9728 twice, gated by silu: 885 us (0.93 PFLOP/s): 368, 71, 263 and 13 to join slices, 237 (profiled, which takes
-// 5 % longer).
+// Many rows are bound by the matrix units: 4096 rows, 9728 -> 2560 with a residual, forward and backward 616 us (0.99 PFLOP/s): 239 forward, 12 for dz, 231
+// for dx, 214 for dW.  2744 rows, 2560 -> 9728 twice, gated by silu: 892 us (0.92 PFLOP/s): 384, 70, 271 and 13 to join slices, 249 (profiled, which takes
+// 5 to 10 % longer).
 // Few by the weights' bytes.
 // =============================================================================================
 struct Activated {      // act(z) and act'(z)

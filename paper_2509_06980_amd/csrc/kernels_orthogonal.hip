@@ -11,8 +11,8 @@ using namespace product;
 // X B, so that A has the smaller of the two sizes and nothing is transposed).  Singular values s become p(s) = a s + b s^3 + c s^5, again and
 // again; the singular vectors stay.
 // A and B are symmetric: tiles on and under the diagonal are computed, the others are stored from them.
-// Bound by the matrix units: 2560 x 9728 in five steps 1.36 ms (0.77 PFLOP/s of the products as computed, half of the symmetric ones), 28 x 2048 x 1024
-// 1.82 ms; small stacks by the ten products' and joins' length one after another (3 x 512 x 256 168 us).
+// Bound by the matrix units: 2560 x 9728 in five steps 1.38 ms (0.75 PFLOP/s of the products as computed, half of the symmetric ones), 28 x 2048 x 1024
+// 1.84 ms; small stacks by the ten products' and joins' length one after another (3 x 512 x 256 169 us).
 // fp32: everything in 32 bits.  bf16: the operands of the products are rounded to fp16 (11 bits instead of the 8 of bf16, at the same rate), X and A times powers of two
 // that keep their elements in the middle of that range (Schedule).  What the rounding of X leaves is kept beside it in fp16 where more than one step follows, since a X
 // carries the small singular values, which the steps enlarge (400 times in five of them) with whatever roundings are in them; the first X is exact as it is.  B's diagonal, near
