@@ -229,8 +229,8 @@ class Muon(torch.optim.Optimizer):
 
     @staticmethod
     def _move(p, update, lr, scale, decay):
-        """p <- (1 - lr decay) p - lr scale update in 32 bits, rounded once: parameters of 16 bits would lose most of a small decay to a rounding of its own."""
-        w = p.float()      # p itself where it has 32 bits
+        """p <- (1 - lr decay) p - lr scale update in 32 bits or more, rounded once: parameters of 16 bits would lose most of a small decay to a rounding of its own."""
+        w = p.float() if p.element_size() < 4 else p
         w = w * (1 - lr * decay) if decay else w
         p.copy_(w.add_(update, alpha=-lr * scale))
 

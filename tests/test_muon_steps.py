@@ -28,6 +28,14 @@ def test_adam_steps_of_muon_are_rounded_once():
             assert within_half_a_step(p.detach(), exact), (decay, step)
 
 
+def test_parameters_of_64_bits_stay_that_precise():
+    p = torch.linspace(0.1, 1.0, 50, dtype=torch.float64).requires_grad_()
+    muon, before = pu.Muon([dict(params=[p])], adam_lr=2.0 ** -10, weight_decay=0.5), p.detach().clone()
+    p.grad = torch.zeros_like(p)
+    muon.step()
+    assert torch.equal(p.detach(), before * (1 - 2.0 ** -11))      # the step is 0
+
+
 @pytest.mark.gpu
 def test_orthogonal_steps_of_muon_are_rounded_once():
     from paper_2509_06980_amd import policy_ops as ops
