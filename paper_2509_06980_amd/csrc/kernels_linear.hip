@@ -66,6 +66,7 @@ __device__ __forceinline__ void activate_all(const float (&z)[N], int act, float
 template <typename T, bool GATED_, bool PLAIN, bool SHORT = PLAIN>
 struct Finish {
   static constexpr bool GATED = GATED_, SYMMETRIC = false, UNROLL = SHORT;
+  static constexpr int SLICED = 16;
   static constexpr int V = kPiece<T>;
   void* y;
   int64_t y_batch;               // elements from one batch's results to the next's

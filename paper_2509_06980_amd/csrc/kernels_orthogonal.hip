@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void normalise_kernel(const T* __restrict__ x,
 template <typename T>
 struct Gram {
   static constexpr bool GATED = false, SYMMETRIC = true;
-  static constexpr int V = kPiece<T>;
+  static constexpr int V = kPiece<T>, SLICED = 4;
   T* out;
   int64_t matrix;
   int ld, n;
@@ -138,7 +138,7 @@ struct Gram {
 template <typename T>
 struct Polynomial {
   static constexpr bool GATED = false, SYMMETRIC = true;
-  static constexpr int V = kPiece<T>;
+  static constexpr int V = kPiece<T>, SLICED = sizeof(T) == 2 ? 0 : 4;
   const T* a;
   T* out;
   float* diagonal;
@@ -177,7 +177,7 @@ struct Polynomial {
 template <typename T>
 struct Step {
   static constexpr bool GATED = false, SYMMETRIC = false;
-  static constexpr int V = kPiece<T>;
+  static constexpr int V = kPiece<T>, SLICED = 4;
   const T* x;              // the products' operand; fp16: X as it is kept, rounded,
   const _Float16* low;     // and what the rounding left, unless null
   T* next;
@@ -259,9 +259,9 @@ struct Layout {      // of the workspace
     constexpr int V = kPiece<T>;
     const int s = n.small(), l = std::max(n.rows, n.columns);
     ld = (int)up(n.columns, V), ld_small = (int)up(s, V);
-    gram = plan_of<T>({s, s, n.count, chunks<T>(l, 64), true, false, true, (float)sizeof(T)});
-    square = plan_of<T>({s, s, n.count, chunks<T>(s, 64), true, false, true, 2.f * sizeof(T)});
-    step = plan_of<T>({n.rows, n.columns, n.count, chunks<T>(s, 64), false, false, n.rows <= n.columns, 8.f});
+    gram = plan_of<T>({s, s, n.count, chunks<T>(l, 64), true, false, true, (float)sizeof(T), Gram<T>::SLICED});
+    square = plan_of<T>({s, s, n.count, chunks<T>(s, 64), true, false, true, 2.f * sizeof(T), Polynomial<T>::SLICED});
+    step = plan_of<T>({n.rows, n.columns, n.count, chunks<T>(s, 64), false, false, n.rows <= n.columns, 8.f, Step<T>::SLICED});
     matrix = (int64_t)n.rows * ld, small = (int64_t)s * ld_small;
     int64_t at = 0;
     auto take = [&](int64_t b) {

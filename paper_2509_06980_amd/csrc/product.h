@@ -151,7 +151,7 @@ struct Lds {
 //   void fetch(int batch, int row, int col, Extra&) const           what joins these sums from memory
 //   void operator()(int batch, int row, int col, float (&v)[V], float (&u)[V], const Extra&) const
 // which finishes V columns of a row: u holds the second matrix's sums where GATED.  UNROLL: short enough that it may stand there for every row, so that
-// fetch runs a part of the tile ahead.
+// fetch runs a part of the tile ahead.  SLICED: in slices, tiles of up to so many blocks of 64 x 64 are built; larger ones are never the cheapest there.
 template <typename T, typename EPI>
 struct Arguments {
   Product<T> p;
@@ -631,6 +631,7 @@ struct Sizes {
   int64_t rows, cols, batches, n_chunks;
   bool symmetric, gated, strided;      // strided: one of the operands
   float bytes;
+  int sliced = 16;                     // the epilogue's SLICED
 };
 template <typename T>
 Plan plan_of(const Sizes& z) {
@@ -646,7 +647,8 @@ Plan plan_of(const Sizes& z) {
     const int64_t ti = (z.rows + 64 * o.mb - 1) / (64 * o.mb), bn = z.gated ? 32 * o.nb : 64 * o.nb, tj = (z.cols + bn - 1) / bn;
     const int64_t tiles = (z.symmetric ? ti * (ti + 1) / 2 : ti * tj) * z.batches;
     const float epilogue = elements * z.bytes / 4.5e6f * (o.resident > 256 && tiles > o.resident ? 0.5f : 1.f);
-    for (int s = 1; s <= 16 && s <= std::max<int64_t>(z.n_chunks / 8, 1); s++) {
+    const int64_t most = o.mb * o.nb <= z.sliced ? std::min<int64_t>(std::max<int64_t>(z.n_chunks / 8, 1), 16) : 1;
+    for (int s = 1; s <= most; s++) {
       const float sums = s == 1 ? 0.f : (z.symmetric ? sizeof(T) == 2 ? 25.f : 8.f : 5.f) + (float)s * elements * (z.gated ? 2.f : z.symmetric ? 0.5f : 1.f) * 8.f / 4.5e6f;
       const float us = (float)((tiles * s + o.resident - 1) / o.resident) * ((float)((z.n_chunks + s - 1) / s) * (z.gated ? o.gated_us : o.chunk_us) + 5.f) + epilogue + sums;
       if (us < best_us) best_us = us, best = {o.mb, o.nb, s};
@@ -702,9 +704,13 @@ void launch(Product<T> p, const Plan& plan, const EPI& epi, hipStream_t s) {
   auto with = [&](auto mb, auto nb, auto r, auto cb) {
     constexpr int MB = decltype(mb)::value, NB = decltype(nb)::value, R = decltype(r)::value, CB = decltype(cb)::value, BM = 64 * MB, BN = EPI::GATED ? 32 * NB : 64 * NB;
     p.tiles_i = (p.rows + BM - 1) / BM, p.tiles_j = (p.cols + BN - 1) / BN;
-    if (probe) probe->form(plan.slices > 1 ? form_of<T, TA, TB, MB, NB, R, CB, true, EPI>() : form_of<T, TA, TB, MB, NB, R, CB, false, EPI>(), p.segments);
+    constexpr bool CUT = MB * NB <= EPI::SLICED;
+    if (!CUT) p.slices = 1;
+    if (probe) probe->form(p.slices > 1 ? form_of<T, TA, TB, MB, NB, R, CB, true, EPI>() : form_of<T, TA, TB, MB, NB, R, CB, false, EPI>(), p.segments);
     if (probe) return find_overreach(p, TA, TB, BM, BN, EPI::GATED, CB);
-    if (plan.slices > 1) return go<T, TA, TB, MB, NB, R, CB, true>(p, epi, s);
+    if constexpr (CUT) {
+      if (p.slices > 1) return go<T, TA, TB, MB, NB, R, CB, true>(p, epi, s);
+    }
     go<T, TA, TB, MB, NB, R, CB, false>(p, epi, s);
   };
 #define RL_I(x) std::integral_constant<int, x>()

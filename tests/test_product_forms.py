@@ -7,6 +7,8 @@ import subprocess
 import pytest
 import torch
 
+import paper_2509_06980_amd as rl
+from test_kernel_resources import _kernels
 from test_product_tiles import CSRC, HIPCC
 
 BF, FP = torch.bfloat16, torch.float32
@@ -69,6 +71,12 @@ def test_every_kernel_that_a_call_can_come_to_is_in_the_list(tmp_path):
     found = [line.split(" ", 1) for line in out.splitlines()]
     reachable, listed = {name for n, name in found if n == "0"}, {name for n, name in found if n != "0"}
     assert len(reachable) > 100 and not reachable - listed, sorted(reachable - listed)
+    # and no kernel is built that none comes to
+    if not os.path.exists(rl.LIB_PATH):
+        from paper_2509_06980_amd import build
+        build.build()
+    built = [k for k in _kernels(rl.LIB_PATH)["product", ()] if "product_kernel" in k[".name"]]
+    assert len(built) == len({name.split("[")[1] for name in reachable if not name.startswith("few rows")})
 
 
 @pytest.mark.gpu
