@@ -137,7 +137,8 @@ def residual_norm_backward(dh_new, da, h_new, y, stats, weight, post_weight=None
 # ---- orthogonalised updates --------------------------------------------------------------------------------------------
 def orthogonalize(x, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7):
     """Every matrix of x [.., rows, columns] with its singular values driven towards 1 -> a new tensor: x / (|x| + eps), then `steps` times
-    X <- a X + b (X X^T) X + c (X X^T)^2 X; see rl_orthogonalize.  coefficients: (a, b, c), or one such triple a step."""
+    X <- a X + b (X X^T) X + c (X X^T)^2 X; see rl_orthogonalize.  coefficients: (a, b, c), or one such triple a step.
+    No gradient passes through it."""
     table = []
     try:
         if steps in range(1, 65):
